@@ -1,5 +1,5 @@
-"""ctypes binding over librapid_pg.so: same names as the C ABI (include/rapid_pg.h), argument
-marshalling only.  Tensors are PyTorch CUDA tensors used purely as device memory; every step of
+"""ctypes binding over librapid_pg.so: same names as the C ABI (include/rapid_pg.h and
+include/rapid_policy_ops.h), argument marshalling only.  Tensors are PyTorch CUDA tensors used purely as device memory; every step of
 the computation runs in the library's kernels on torch's current stream.
 
 There is no fallback: if the shared library is missing the first call raises.
@@ -39,12 +39,21 @@ FLAG_HEAD_CTA_PAIRS = 128
 FLAG_HEAD_SINGLE_CTA = 256
 FLAG_HEAD_DW_BF16 = 512
 
-# every symbol declared in include/rapid_pg.h
+EMBED_DTABLE_BF16 = 1
+EMBED_ACCUMULATE = 2
+
+QK_NO_NORM = 1
+QK_UNIT_OFFSET = 2
+QK_INTERLEAVED = 4
+
+# every symbol declared in include/
 EXPORTS = (
     "rapid_status_string", "rapid_version", "rapid_workspace_bytes", "rapid_group_advantage",
     "rapid_pg_loss_fwd_bwd", "rapid_pg_stats_chunk", "rapid_pg_finalize", "rapid_pg_dlogits_chunk",
     "rapid_pg_loss_fwd_bwd_noalloc", "rapid_fused_head_workspace_bytes", "rapid_pg_loss_fused_head",
     "rapid_pg_loss_onpolicy_fwd_bwd", "rapid_pg_loss_fwd_bwd_hostlogits", "rapid_selftest_bounded_wait",
+    "rapid_embedding_fwd", "rapid_embedding_bwd_workspace_bytes", "rapid_embedding_bwd",
+    "rapid_qk_norm_rope_fwd", "rapid_qk_norm_rope_bwd_workspace_bytes", "rapid_qk_norm_rope_bwd",
 )
 
 
@@ -61,6 +70,19 @@ class RapidStats(C.Structure):
 
 
 STATS_BYTES = C.sizeof(RapidStats)
+
+
+class EmbedDesc(C.Structure):
+    _fields_ = [("n_rows", C.c_int64), ("vocab", C.c_int32), ("dim", C.c_int32), ("ld_table", C.c_int64),
+                ("ld_rows", C.c_int64), ("dtype", C.c_int32), ("flags", C.c_uint32), ("scale", C.c_float),
+                ("reserved", C.c_int32)]
+
+
+class QkDesc(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("seq_len", C.c_int32), ("n_q_heads", C.c_int32), ("n_k_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("ld_q", C.c_int64), ("ld_k", C.c_int64),
+                ("ld_q_out", C.c_int64), ("ld_k_out", C.c_int64), ("ld_dq", C.c_int64), ("ld_dk", C.c_int64), ("dtype", C.c_int32), ("flags", C.c_uint32),
+                ("eps", C.c_float), ("reserved", C.c_int32)]
 
 
 class RapidError(RuntimeError):
@@ -110,6 +132,17 @@ def lib():
         L.rapid_pg_finalize.argtypes = [dp] + [vp] * 8 + [sz, vp]
         L.rapid_pg_dlogits_chunk.restype = C.c_int
         L.rapid_pg_dlogits_chunk.argtypes = [dp, vp, vp, i64, i64, vp, vp, vp, sz, vp]
+        ep, qp = C.POINTER(EmbedDesc), C.POINTER(QkDesc)
+        for name, argtypes in {
+            "rapid_embedding_fwd": [ep] + [vp] * 6,
+            "rapid_embedding_bwd_workspace_bytes": [ep, C.POINTER(sz)],
+            "rapid_embedding_bwd": [ep] + [vp] * 5 + [sz, vp],
+            "rapid_qk_norm_rope_fwd": [qp] + [vp] * 10,
+            "rapid_qk_norm_rope_bwd_workspace_bytes": [qp, C.POINTER(sz)],
+            "rapid_qk_norm_rope_bwd": [qp] + [vp] * 14 + [sz, vp],
+        }.items():
+            getattr(L, name).restype = C.c_int
+            getattr(L, name).argtypes = argtypes
         _lib = L
     return _lib
 
@@ -320,3 +353,270 @@ def pg_loss(logits: torch.Tensor, targets, mask, behav_logp, rewards, group_offs
     rapid_pg_loss_fwd_bwd(desc, logits, targets, mask, behav_logp, rewards, group_offsets, dlogits,
                           loss, token_logp, adv, stats, ws)
     return PgResult(loss, dlogits, token_logp, adv, stats)
+
+
+# ---- policy-network operators (include/rapid_policy_ops.h) ---------------------------------------------------
+#
+# The rapid_* functions marshal the arguments of the C calls; embedding(), embedding_grad(), qk_norm_rope() and
+# qk_norm_rope_grad() check shapes and types, allocate the outputs and make one call.
+
+
+def _dtype_code(dtype: torch.dtype) -> int:
+    if dtype == torch.float32:
+        return RAPID_F32
+    if dtype == torch.bfloat16:
+        return RAPID_BF16
+    raise TypeError(f"float32 or bfloat16 expected, got {dtype}")
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _one_device(*tensors: Optional[torch.Tensor]) -> torch.device:
+    """The CUDA device that all the tensors lie on."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        _need(t.is_cuda, "tensors must be CUDA tensors")
+        _need(dev is None or t.device == dev, "tensors lie on different devices")
+        dev = t.device
+    return dev
+
+
+def _vector(t: Optional[torch.Tensor], n: int, dtype, name: str) -> None:
+    if t is None:
+        return
+    _need(t.numel() == n and t.is_contiguous(), f"{name}: {n} contiguous elements expected")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: {dtype} expected, got {t.dtype}")
+
+
+def _mask8(mask: Optional[torch.Tensor], n: int) -> Optional[torch.Tensor]:
+    if mask is None:
+        return None
+    if mask.dtype == torch.bool:
+        mask = mask.view(torch.uint8)
+    _vector(mask, n, torch.uint8, "mask")
+    return mask
+
+
+def _pitch(t: torch.Tensor, name: str) -> int:
+    """Row pitch of a matrix [rows, cols] or of rows of heads [rows, heads, head_dim]."""
+    inner = t.stride(-1) == 1 or t.shape[-1] == 1
+    if t.dim() == 3:
+        inner = inner and (t.shape[1] == 1 or t.stride(1) == t.shape[2])
+    width = t.shape[-1] * (t.shape[1] if t.dim() == 3 else 1)
+    _need(inner, f"{name}: the elements of a row must lie side by side")
+    if t.shape[0] == 1:  # one row has no pitch: the narrowest that 16-byte rows allow
+        step = 16 // t.element_size()
+        return -(-width // step) * step
+    return t.stride(0)
+
+
+def _matrix(rows: int, cols: int, dtype, device) -> torch.Tensor:
+    """An uninitialised [rows, cols] whose rows begin on 16-byte boundaries."""
+    step = 16 // torch.empty(0, dtype=dtype).element_size()
+    pitch = -(-cols // step) * step
+    buf = torch.empty(rows, pitch, dtype=dtype, device=device)
+    return buf if pitch == cols else buf[:, :cols]
+
+
+def _like(out: Optional[torch.Tensor], x: torch.Tensor, name: str) -> torch.Tensor:
+    """`out`, or a contiguous tensor of x's shape and type where there is none."""
+    if out is None:
+        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _need(out.shape == x.shape, f"{name}: shape {tuple(x.shape)} expected")
+    if out.dtype != x.dtype:
+        raise TypeError(f"{name}: {x.dtype} expected, got {out.dtype}")
+    return out
+
+
+class _on:
+    """Make `device` current for the calls inside (nothing to do when it is already)."""
+
+    def __init__(self, device: torch.device):
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def make_embed_desc(n_rows: int, vocab: int, dim: int, dtype: torch.dtype, ld_table: Optional[int] = None,
+                    ld_rows: Optional[int] = None, scale: float = 1.0, flags: int = 0) -> EmbedDesc:
+    return EmbedDesc(n_rows, vocab, dim, dim if ld_table is None else ld_table, dim if ld_rows is None else ld_rows,
+                     _dtype_code(dtype), flags, float(scale), 0)
+
+
+def rapid_embedding_fwd(desc: EmbedDesc, tokens: torch.Tensor, mask: Optional[torch.Tensor], table: torch.Tensor,
+                        out: torch.Tensor, stats: Optional[torch.Tensor]) -> None:
+    _check(lib().rapid_embedding_fwd(C.byref(desc), _ptr(tokens), _ptr(mask), _ptr(table), _ptr(out), _ptr(stats),
+                                     _stream()), "rapid_embedding_fwd")
+
+
+def rapid_embedding_bwd_workspace_bytes(desc: EmbedDesc) -> int:
+    n = C.c_size_t(0)
+    _check(lib().rapid_embedding_bwd_workspace_bytes(C.byref(desc), C.byref(n)), "rapid_embedding_bwd_workspace_bytes")
+    return int(n.value)
+
+
+def rapid_embedding_bwd(desc: EmbedDesc, tokens: torch.Tensor, mask: Optional[torch.Tensor], dout: torch.Tensor,
+                        dtable: torch.Tensor, workspace: torch.Tensor) -> None:
+    _check(lib().rapid_embedding_bwd(C.byref(desc), _ptr(tokens), _ptr(mask), _ptr(dout), _ptr(dtable), _ptr(workspace),
+                                     workspace.numel(), _stream()), "rapid_embedding_bwd")
+
+
+def embedding(table: torch.Tensor, tokens: torch.Tensor, mask: Optional[torch.Tensor] = None, scale: float = 1.0,
+              stats: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """scale * table[tokens], [T, D] in the table's type; rows that are masked or whose token is no row of the table are
+    zeros.  tokens [T] int32, table [V, D] (rows on 16-byte boundaries)."""
+    _need(table.dim() == 2, "table: a matrix [V, D] expected")
+    T, (V, D) = tokens.numel(), table.shape
+    mask = _mask8(mask, T)
+    _vector(tokens, T, torch.int32, "tokens")
+    dev = _one_device(table, tokens, mask, stats)
+    if T == 0:
+        return _matrix(0, D, table.dtype, dev)
+    with _on(dev):
+        out = _matrix(T, D, table.dtype, dev)
+        desc = make_embed_desc(T, V, D, table.dtype, _pitch(table, "table"), _pitch(out, "out"), scale)
+        rapid_embedding_fwd(desc, tokens, mask, table, out, stats)
+    return out
+
+
+def embedding_grad(dout: torch.Tensor, tokens: torch.Tensor, mask: Optional[torch.Tensor], vocab: int, scale: float = 1.0,
+                   dtable_dtype: torch.dtype = torch.float32, dtable: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient of embedding() with respect to its table: [vocab, D] in `dtable_dtype`, or added to `dtable`, which
+    is then returned (its type counts, not `dtable_dtype`)."""
+    _need(dout.dim() == 2, "dout: a matrix [T, D] expected")
+    T, D = dout.shape
+    mask = _mask8(mask, T)
+    _vector(tokens, T, torch.int32, "tokens")
+    flags = 0
+    if dtable is not None:
+        _need(tuple(dtable.shape) == (vocab, D), "dtable: [vocab, D] expected")
+        dtable_dtype, flags = dtable.dtype, EMBED_ACCUMULATE
+    if _dtype_code(dtable_dtype) == RAPID_BF16:
+        if dout.dtype != torch.bfloat16:
+            raise TypeError("a bfloat16 dtable needs a bfloat16 dout")
+        flags |= EMBED_DTABLE_BF16
+    dev = _one_device(dout, tokens, mask, dtable)
+    with _on(dev):
+        if T == 0:
+            return torch.zeros(vocab, D, dtype=dtable_dtype, device=dev) if dtable is None else dtable
+        out = _matrix(vocab, D, dtable_dtype, dev) if dtable is None else dtable
+        desc = make_embed_desc(T, vocab, D, dout.dtype, _pitch(out, "dtable"), _pitch(dout, "dout"), scale, flags)
+        ws = torch.empty(rapid_embedding_bwd_workspace_bytes(desc), dtype=torch.uint8, device=dev)
+        rapid_embedding_bwd(desc, tokens, mask, dout, out, ws)
+    return out
+
+
+def make_qk_desc(n_seq: int, seq_len: int, n_q_heads: int, n_k_heads: int, head_dim: int, dtype: torch.dtype,
+                 rot_dim: Optional[int] = None, ld_q: Optional[int] = None, ld_k: Optional[int] = None,
+                 ld_q_out: Optional[int] = None, ld_k_out: Optional[int] = None, ld_dq: Optional[int] = None,
+                 ld_dk: Optional[int] = None, eps: float = 1e-6, flags: int = 0) -> QkDesc:
+    wq, wk = n_q_heads * head_dim, n_k_heads * head_dim
+    pitches = [w if ld is None else ld for w, ld in ((wq, ld_q), (wk, ld_k), (wq, ld_q_out), (wk, ld_k_out), (wq, ld_dq), (wk, ld_dk))]
+    return QkDesc(n_seq, seq_len, n_q_heads, n_k_heads, head_dim, head_dim if rot_dim is None else rot_dim, *pitches,
+                  _dtype_code(dtype), flags, float(eps), 0)
+
+
+def rapid_qk_norm_rope_fwd(desc: QkDesc, q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Tensor],
+                           k_weight: Optional[torch.Tensor], inv_freq: torch.Tensor, positions: Optional[torch.Tensor],
+                           mask: Optional[torch.Tensor], q_out: torch.Tensor, k_out: torch.Tensor) -> None:
+    _check(lib().rapid_qk_norm_rope_fwd(C.byref(desc), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq),
+                                        _ptr(positions), _ptr(mask), _ptr(q_out), _ptr(k_out), _stream()),
+           "rapid_qk_norm_rope_fwd")
+
+
+def rapid_qk_norm_rope_bwd_workspace_bytes(desc: QkDesc) -> int:
+    n = C.c_size_t(0)
+    _check(lib().rapid_qk_norm_rope_bwd_workspace_bytes(C.byref(desc), C.byref(n)), "rapid_qk_norm_rope_bwd_workspace_bytes")
+    return int(n.value)
+
+
+def rapid_qk_norm_rope_bwd(desc: QkDesc, q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Tensor],
+                           k_weight: Optional[torch.Tensor], inv_freq: torch.Tensor, positions: Optional[torch.Tensor],
+                           mask: Optional[torch.Tensor], dq_out: torch.Tensor, dk_out: torch.Tensor, dq: torch.Tensor,
+                           dk: torch.Tensor, dq_weight: Optional[torch.Tensor], dk_weight: Optional[torch.Tensor],
+                           workspace: Optional[torch.Tensor]) -> None:
+    _check(lib().rapid_qk_norm_rope_bwd(
+        C.byref(desc), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq), _ptr(positions), _ptr(mask),
+        _ptr(dq_out), _ptr(dk_out), _ptr(dq), _ptr(dk), _ptr(dq_weight), _ptr(dk_weight), _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _stream()), "rapid_qk_norm_rope_bwd")
+
+
+def _qk_args(q, k, q_weight, k_weight, inv_freq, n_seq, seq_len, positions, mask, flags):
+    T = n_seq * seq_len
+    _need(q.dim() == 3 and k.dim() == 3 and q.shape[0] == T and k.shape[0] == T and q.shape[2] == k.shape[2],
+          "q, k: [n_seq * seq_len, heads, head_dim] expected")
+    if q.dtype != k.dtype:
+        raise TypeError("q and k must have one type")
+    hd = q.shape[2]
+    if flags & QK_NO_NORM:
+        q_weight = k_weight = None
+    else:
+        _need(q_weight is not None and k_weight is not None, "weights are needed unless QK_NO_NORM is set")
+    _vector(q_weight, hd, torch.float32, "q_weight")
+    _vector(k_weight, hd, torch.float32, "k_weight")
+    _vector(inv_freq, inv_freq.numel(), torch.float32, "inv_freq")
+    _vector(positions, T, torch.int32, "positions")
+    return q_weight, k_weight, _mask8(mask, T)
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor],
+                 inv_freq: torch.Tensor, n_seq: int, seq_len: int, positions: Optional[torch.Tensor] = None,
+                 mask: Optional[torch.Tensor] = None, eps: float = 1e-6, flags: int = 0):
+    """Norm of every head of q [T, Hq, D] and k [T, Hk, D], then rotation by position (2 * inv_freq.numel() elements of a
+    head); returns contiguous (q_out, k_out).  q and k may be slices of one projection's rows."""
+    q_weight, k_weight, mask = _qk_args(q, k, q_weight, k_weight, inv_freq, n_seq, seq_len, positions, mask, flags)
+    dev = _one_device(q, k, q_weight, k_weight, inv_freq, positions, mask)
+    with _on(dev):
+        q_out, k_out = torch.empty(q.shape, dtype=q.dtype, device=dev), torch.empty(k.shape, dtype=k.dtype, device=dev)
+        if q.shape[0] == 0:
+            return q_out, k_out
+        desc = make_qk_desc(n_seq, seq_len, q.shape[1], k.shape[1], q.shape[2], q.dtype, 2 * inv_freq.numel(), _pitch(q, "q"),
+                            _pitch(k, "k"), eps=eps, flags=flags)
+        rapid_qk_norm_rope_fwd(desc, q, k, q_weight, k_weight, inv_freq, positions, mask, q_out, k_out)
+    return q_out, k_out
+
+
+@dataclass
+class QkGrads:
+    dq: torch.Tensor                    # [T, Hq, D]
+    dk: torch.Tensor                    # [T, Hk, D]
+    dq_weight: Optional[torch.Tensor]   # [D] float32; None with QK_NO_NORM
+    dk_weight: Optional[torch.Tensor]
+
+
+def qk_norm_rope_grad(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor],
+                      inv_freq: torch.Tensor, dq_out: torch.Tensor, dk_out: torch.Tensor, n_seq: int, seq_len: int,
+                      positions: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                      flags: int = 0, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None) -> QkGrads:
+    """The gradient of qk_norm_rope() from its inputs and the gradients of its outputs.  dq and dk may be given (slices of the
+    gradient of one projection, say, or dq_out and dk_out themselves)."""
+    q_weight, k_weight, mask = _qk_args(q, k, q_weight, k_weight, inv_freq, n_seq, seq_len, positions, mask, flags)
+    _need(dq_out.shape == q.shape and dk_out.shape == k.shape, "dq_out, dk_out: the shapes of q and k expected")
+    if dq_out.dtype != q.dtype or dk_out.dtype != k.dtype:
+        raise TypeError("dq_out and dk_out must have the type of q and k")
+    dev = _one_device(q, k, q_weight, k_weight, inv_freq, positions, mask, dq_out, dk_out, dq, dk)
+    with _on(dev):
+        T, hq, hd = q.shape
+        hk = k.shape[1]
+        dq, dk = _like(dq, q, "dq"), _like(dk, k, "dk")
+        norm = not flags & QK_NO_NORM
+        dw = torch.empty(2, hd, device=dev) if norm else (None, None)
+        if T == 0:
+            return QkGrads(dq, dk, *(x.zero_() for x in dw)) if norm else QkGrads(dq, dk, None, None)
+        desc = make_qk_desc(n_seq, seq_len, hq, hk, hd, q.dtype, 2 * inv_freq.numel(), _pitch(q, "q"), _pitch(k, "k"),
+                            _pitch(dq_out, "dq_out"), _pitch(dk_out, "dk_out"), _pitch(dq, "dq"), _pitch(dk, "dk"), eps, flags)
+        ws = torch.empty(rapid_qk_norm_rope_bwd_workspace_bytes(desc), dtype=torch.uint8, device=dev) if norm else None
+        rapid_qk_norm_rope_bwd(desc, q, k, q_weight, k_weight, inv_freq, positions, mask, dq_out, dk_out, dq, dk, dw[0], dw[1], ws)
+    return QkGrads(dq, dk, dw[0], dw[1])

@@ -1,0 +1,512 @@
+// Token embedding with scaling, and its gradient over sorted tokens.  Both are bound by HBM bytes.
+//
+// Forward: a warp copies up to 2048 columns of one row (8 vectors of 8 elements a lane, all loads in flight before the first
+// store), times the scale.
+//
+// Gradient: dtable[v] = s * sum of the rows of dout whose token is v.  No float atomics: the row numbers are sorted by
+// token with a stable radix sort (9-bit digits, written here), so a token's rows lie next to each other in row order, and
+// every sum has a fixed order.  Frequent tokens (a few per cent of all rows each) would keep one warp busy for long, so any
+// 32 sorted positions [32 j, 32 j + 32) that hold one token are summed first, by a warp of their own; a row of dtable
+// is then at most 31 rows + the pieces + 31 rows.  Rows of dtable are dealt out interleaved over the blocks because the
+// frequent tokens have neighbouring numbers in most vocabularies.
+#include <math.h>
+
+#include "policy_ops.cuh"
+
+namespace rapid {
+namespace policy {
+namespace {
+
+constexpr int kSegVecs = 8;                 // forward: vectors of 8 elements a lane takes of a row
+constexpr int kFwdSeg = kSegVecs * 32 * 8;  // columns a warp takes of a row
+
+template <class T>
+__global__ void __launch_bounds__(256)
+embed_fwd_kernel(int64_t n_rows, int segs, int vocab, int dim, int64_t ld_table, int64_t ld_out, float scale,
+                 const int32_t* __restrict__ tokens, const uint8_t* __restrict__ mask, const T* __restrict__ table,
+                 T* __restrict__ out, rapid_stats_t* stats) {
+    __shared__ int counts[2];
+    const int lane = threadIdx.x & 31;
+    const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (stats) {
+        if (threadIdx.x < 2) counts[threadIdx.x] = 0;
+        __syncthreads();
+    }
+    if (unit < n_rows * segs) {
+        const int64_t r = unit / segs;
+        const int seg = (int)(unit - r * segs);
+        const int tok = tokens[r];
+        const bool live = mask == nullptr || mask[r] != 0;
+        const bool ok = live && tok >= 0 && tok < vocab;
+        if (stats && seg == 0 && lane == 0 && live) atomicAdd(&counts[ok ? 0 : 1], 1);
+        const T* src = table + (ok ? (int64_t)tok * ld_table : 0);
+        T* dst = out + r * ld_out;
+        const int c0 = seg * kFwdSeg + lane * 8;
+        Vec8<T> v[kSegVecs];
+        if (ok) {
+#pragma unroll
+            for (int i = 0; i < kSegVecs; ++i)
+                if (c0 + i * 256 + 8 <= dim) v[i].load(src + c0 + i * 256);
+        }
+#pragma unroll
+        for (int i = 0; i < kSegVecs; ++i) {
+            const int c = c0 + i * 256;
+            if (c + 8 <= dim) {
+                float f[8];
+                v[i].get(f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = ok ? f[j] * scale : 0.f;
+                Vec8<T>::store(dst + c, f);
+            } else {  // the row's ragged end
+                for (int j = c; j < dim; ++j) from_float(dst + j, ok ? to_float(src[j]) * scale : 0.f);
+            }
+        }
+    }
+    if (stats) {
+        __syncthreads();
+        if (threadIdx.x == 0 && counts[0]) atomicAdd(reinterpret_cast<unsigned long long*>(&stats->n_tokens), (unsigned long long)counts[0]);
+        if (threadIdx.x == 0 && counts[1]) atomicAdd(&stats->n_bad_token, counts[1]);
+    }
+}
+
+// ---- stable radix sort of (token, row) ----------------------------------------------------------------------
+
+constexpr int kRadixBits = 9, kBins = 1 << kRadixBits;
+constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;  // one thread a digit value
+constexpr int kMaxSortBlocks = 128;
+constexpr int kMinSortRows = 512;
+
+// The rows of block b are [b * per_block, (b + 1) * per_block); within it warp w has a run of per_block / 16 of them.
+struct SortShape {
+    int64_t n_rows, per_block;
+    int blocks, passes;
+};
+
+inline SortShape sort_shape(int64_t n_rows, int32_t vocab) {
+    SortShape s;
+    s.n_rows = n_rows;
+    // one block does not need the histograms of others and finishes in one launch
+    const int64_t want = n_rows <= 4096 ? 1 : (n_rows + kMinSortRows - 1) / kMinSortRows;
+    s.blocks = (int)(want < kMaxSortBlocks ? want : kMaxSortBlocks);
+    s.per_block = (n_rows + s.blocks - 1) / s.blocks;
+    s.per_block = (s.per_block + kSortThreads - 1) / kSortThreads * kSortThreads;  // whole warps' runs
+    s.blocks = (int)((n_rows + s.per_block - 1) / s.per_block);
+    int bits = 0;
+    while ((1ll << bits) <= (int64_t)vocab) ++bits;  // keys 0 .. vocab; `vocab` marks rows that do not count
+    s.passes = (bits + kRadixBits - 1) / kRadixBits;
+    return s;
+}
+
+struct SortArgs {
+    const int32_t* tokens;
+    const uint8_t* mask;
+    int vocab;
+    const uint32_t* key_in;  // nullptr in the first pass: keys come from the tokens
+    const uint32_t* row_in;
+    uint32_t* key_out;
+    uint32_t* row_out;
+    uint32_t* hist;  // [blocks][kBins]
+    int shift;
+};
+
+__device__ __forceinline__ uint32_t sort_key(const SortArgs& a, int64_t i) {
+    if (a.key_in) return a.key_in[i];
+    const int tok = a.tokens[i];
+    const bool ok = (a.mask == nullptr || a.mask[i] != 0) && tok >= 0 && tok < a.vocab;
+    return ok ? (uint32_t)tok : (uint32_t)a.vocab;
+}
+
+__global__ void __launch_bounds__(kSortThreads) sort_hist_kernel(SortArgs a, SortShape s) {
+    __shared__ uint32_t bins[kBins];
+    bins[threadIdx.x] = 0;
+    __syncthreads();
+    const int64_t lo = (int64_t)blockIdx.x * s.per_block, hi = min(lo + s.per_block, s.n_rows);
+    for (int64_t i = lo + threadIdx.x; i < hi; i += kSortThreads) atomicAdd(&bins[(sort_key(a, i) >> a.shift) & (kBins - 1)], 1u);
+    __syncthreads();
+    a.hist[(size_t)blockIdx.x * kBins + threadIdx.x] = bins[threadIdx.x];
+}
+
+// One pass of one block.  `alone`: the block holds all rows, its own counts are the totals.
+__device__ __forceinline__ void sort_scatter(const SortArgs& a, const SortShape& s, bool alone, uint32_t (*cnt)[kBins],
+                                             uint32_t* scan) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    for (int i = tid; i < kSortWarps * kBins; i += kSortThreads) (&cnt[0][0])[i] = 0;
+    __syncthreads();
+    const int64_t run = s.per_block / kSortWarps;  // a multiple of 32
+    const int64_t lo = (int64_t)blockIdx.x * s.per_block + warp * run, hi = min(lo + run, s.n_rows);
+    for (int64_t i = lo + lane; i < hi; i += 32) atomicAdd(&cnt[warp][(sort_key(a, i) >> a.shift) & (kBins - 1)], 1u);
+    // this thread's digit: how many rows lie in blocks before this one, and how many in all
+    uint32_t before = 0, total = 0;
+    if (!alone) {
+#pragma unroll 16
+        for (int b = 0; b < s.blocks; ++b) {
+            const uint32_t h = a.hist[(size_t)b * kBins + tid];
+            total += h;
+            before += b < (int)blockIdx.x ? h : 0u;
+        }
+    }
+    __syncthreads();
+    if (alone) {
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) total += cnt[w][tid];
+    }
+    // exclusive sum of the totals over the digits
+    uint32_t incl = total;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += x;
+    }
+    if (lane == 31) scan[warp] = incl;
+    __syncthreads();
+    uint32_t base = incl - total + before;
+    for (int w = 0; w < warp; ++w) base += scan[w];
+    // first place of each warp's rows of this digit
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) {
+        const uint32_t c = cnt[w][tid];
+        cnt[w][tid] = base;
+        base += c;
+    }
+    __syncthreads();
+    // in row order, 32 rows at a time: a row's place is the digit's next one plus the equal digits in lower lanes
+    for (int64_t i0 = lo; i0 < hi; i0 += 32) {
+        const int64_t i = i0 + lane;
+        const bool on = i < hi;
+        const uint32_t key = on ? sort_key(a, i) : 0u;
+        const uint32_t digit = on ? (key >> a.shift) & (kBins - 1) : (uint32_t)kBins;
+        const unsigned peers = __match_any_sync(0xffffffffu, digit);
+        const int first = __ffs(peers) - 1;
+        uint32_t place = 0;
+        if (on && lane == first) {
+            place = cnt[warp][digit];
+            cnt[warp][digit] = place + __popc(peers);
+        }
+        place = __shfl_sync(0xffffffffu, place, first) + __popc(peers & ((1u << lane) - 1u));
+        if (on) {
+            a.key_out[place] = key;
+            a.row_out[place] = a.row_in ? a.row_in[i] : (uint32_t)i;
+        }
+        __syncwarp();
+    }
+}
+
+__global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(SortArgs a, SortShape s) {
+    __shared__ uint32_t cnt[kSortWarps][kBins];
+    __shared__ uint32_t scan[kSortWarps];
+    sort_scatter(a, s, false, cnt, scan);
+}
+
+// All passes of a sort that fits one block.  Ends in (key_b, row_b) after an even number of passes, (key_a, row_a) after an
+// odd one, like the multi-block form.
+__global__ void __launch_bounds__(kSortThreads)
+sort_one_block_kernel(SortArgs a, SortShape s, uint32_t* key_a, uint32_t* row_a, uint32_t* key_b, uint32_t* row_b) {
+    __shared__ uint32_t cnt[kSortWarps][kBins];
+    __shared__ uint32_t scan[kSortWarps];
+    for (int p = 0; p < s.passes; ++p) {
+        a.shift = p * kRadixBits;
+        a.key_in = p == 0 ? nullptr : (p & 1) ? key_a : key_b;
+        a.row_in = p == 0 ? nullptr : (p & 1) ? row_a : row_b;
+        a.key_out = (p & 1) ? key_b : key_a;
+        a.row_out = (p & 1) ? row_b : row_a;
+        sort_scatter(a, s, true, cnt, scan);
+        __syncthreads();  // the block's own writes are its next pass's inputs
+    }
+}
+
+// ---- sums over a token's rows -------------------------------------------------------------------------------
+
+constexpr int kPiece = 32;       // sorted positions of a piece
+constexpr int kVecs = 2;         // vectors of 8 columns a lane sums
+constexpr int kSeg = kVecs * 256;  // columns a warp sums
+constexpr int kRowsPerBlock = 8;   // rows of dtable a block writes
+constexpr int kAhead = 4;          // rows of dout in flight
+
+// acc += rows of dout at sorted positions [lo, hi), in order
+template <class T>
+__device__ __forceinline__ void add_rows(float (&acc)[kVecs][8], const uint32_t* __restrict__ rows, int64_t lo, int64_t hi,
+                                         const T* __restrict__ dout, int64_t ld, int c0, int dim, int lane) {
+    for (int64_t i0 = lo; i0 < hi; i0 += 32) {
+        const int n = (int)min((int64_t)32, hi - i0);
+        const uint32_t mine = lane < n ? rows[i0 + lane] : 0u;
+        for (int i = 0; i < n; i += kAhead) {
+            Vec8<T> v[kAhead][kVecs];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const T* src = dout + (int64_t)__shfl_sync(0xffffffffu, mine, min(i + u, n - 1)) * ld;
+#pragma unroll
+                for (int k = 0; k < kVecs; ++k) {
+                    const int c = c0 + k * 256;
+                    if (i + u < n && c + 8 <= dim) v[u][k].load(src + c);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const T* src = dout + (int64_t)__shfl_sync(0xffffffffu, mine, min(i + u, n - 1)) * ld;
+                if (i + u < n) {
+#pragma unroll
+                    for (int k = 0; k < kVecs; ++k) {
+                        const int c = c0 + k * 256;
+                        if (c + 8 <= dim) {
+                            float f[8];
+                            v[u][k].get(f);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) acc[k][j] += f[j];
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                if (c + j < dim) acc[k][j] += to_float(src[c + j]);
+                        }
+                    }
+                }
+            }
+        }
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(256)
+embed_pieces_kernel(int64_t n_rows, int segs, int dim, int64_t ld, int vocab, const uint32_t* __restrict__ keys,
+                    const uint32_t* __restrict__ rows, const T* __restrict__ dout, float* __restrict__ pieces, int64_t ldp) {
+    const int lane = threadIdx.x & 31;
+    const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int64_t piece = unit / segs;
+    const int64_t lo = piece * kPiece, hi = lo + kPiece;
+    if (hi > n_rows) return;  // whole pieces only
+    const uint32_t key = keys[lo];
+    if (key != keys[hi - 1] || key >= (uint32_t)vocab) return;
+    const int c0 = (int)(unit - piece * segs) * kSeg + lane * 8;
+    float acc[kVecs][8] = {};
+    add_rows(acc, rows, lo, hi, dout, ld, c0, dim, lane);
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k)
+        if (c0 + k * 256 < dim) Vec8<float>::store(pieces + piece * ldp + c0 + k * 256, acc[k]);
+}
+
+__device__ __forceinline__ int64_t lower_bound(const uint32_t* __restrict__ keys, int64_t n, uint32_t v) {
+    int64_t lo = 0, hi = n;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (keys[mid] < v) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+template <class T, class G>
+__global__ void __launch_bounds__(256, 2)
+embed_rows_kernel(int64_t n_rows, int segs, int dim, int64_t ld, int vocab, float scale, bool accumulate,
+                  const uint32_t* __restrict__ keys, const uint32_t* __restrict__ rows, const T* __restrict__ dout,
+                  const float* __restrict__ pieces, int64_t ldp, G* __restrict__ dtable, int64_t ld_table) {
+    __shared__ int64_t bound[kRowsPerBlock][2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x < 2 * kRowsPerBlock) {
+        const int64_t v = (int64_t)(threadIdx.x >> 1) * gridDim.x + blockIdx.x;
+        bound[threadIdx.x >> 1][threadIdx.x & 1] = v < vocab ? lower_bound(keys, n_rows, (uint32_t)v + (threadIdx.x & 1)) : 0;
+    }
+    __syncthreads();
+    for (int item = warp; item < kRowsPerBlock * segs; item += 8) {
+        const int j = item / segs;
+        const int64_t v = (int64_t)j * gridDim.x + blockIdx.x;
+        const int64_t lo = bound[j][0], hi = bound[j][1];
+        if (v >= vocab || (accumulate && lo == hi)) continue;
+        const int c0 = (item - j * segs) * kSeg + lane * 8;
+        float acc[kVecs][8] = {};
+        // rows before the first whole piece, the pieces, rows after the last one (all rows first when there is no piece)
+        int64_t a = (lo + kPiece - 1) / kPiece, b = hi / kPiece;
+        const bool whole = a < b;
+#pragma unroll 1
+        for (int part = 0; part < 2; ++part) {
+            const int64_t from = part == 0 ? lo : whole ? b * kPiece : hi, to = part == 0 && whole ? a * kPiece : hi;
+            add_rows(acc, rows, from, to, dout, ld, c0, dim, lane);
+            if (part == 0 && whole) {
+#pragma unroll 2
+                for (int64_t p = a; p < b; ++p) {
+#pragma unroll
+                    for (int k = 0; k < kVecs; ++k)
+                        if (c0 + k * 256 < dim) {
+                            Vec8<float> x;
+                            x.load(pieces + p * ldp + c0 + k * 256);
+                            float f[8];
+                            x.get(f);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) acc[k][i] += f[i];
+                        }
+                }
+            }
+        }
+        G* dst = dtable + v * ld_table;
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) {
+            const int c = c0 + k * 256;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[k][i] *= scale;
+            if (c + 8 <= dim) {
+                if (accumulate) {
+                    Vec8<G> x;
+                    x.load(dst + c);
+                    float f[8];
+                    x.get(f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[k][i] += f[i];
+                }
+                Vec8<G>::store(dst + c, acc[k]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (c + i < dim) from_float(dst + c + i, accumulate ? acc[k][i] + to_float(dst[c + i]) : acc[k][i]);
+            }
+        }
+    }
+}
+
+// ---- host side ------------------------------------------------------------------------------------------------
+
+struct EmbedScratch {
+    uint32_t *key_a, *row_a, *key_b, *row_b, *hist;
+    float* pieces;  // [n_rows / kPiece][ldp]
+    int64_t ldp;
+};
+
+size_t carve_embed(const rapid_embed_desc_t& d, void* base, EmbedScratch* out) {
+    size_t off = 0;
+    char* p = static_cast<char*>(base);
+    auto take = [&](size_t bytes) {
+        char* q = p ? p + off : nullptr;
+        off = align_up(off + bytes, 256);
+        return q;
+    };
+    EmbedScratch s;
+    const size_t n = (size_t)d.n_rows;
+    s.key_a = reinterpret_cast<uint32_t*>(take(n * 4));
+    s.row_a = reinterpret_cast<uint32_t*>(take(n * 4));
+    s.key_b = reinterpret_cast<uint32_t*>(take(n * 4));
+    s.row_b = reinterpret_cast<uint32_t*>(take(n * 4));
+    s.hist = reinterpret_cast<uint32_t*>(take((size_t)kMaxSortBlocks * kBins * 4));
+    s.ldp = (int64_t)align_up((size_t)d.dim, 8);
+    s.pieces = reinterpret_cast<float*>(take(n / kPiece * (size_t)s.ldp * 4));
+    if (out) *out = s;
+    return off;
+}
+
+rapid_status_t check_embed(const rapid_embed_desc_t* d, bool bwd) {
+    if (!d || d->n_rows <= 0 || d->vocab <= 0 || d->dim <= 0 || d->reserved != 0) return RAPID_ERR_INVALID_ARG;
+    if (d->dtype != RAPID_F32 && d->dtype != RAPID_BF16) return RAPID_ERR_INVALID_ARG;
+    if (d->flags & ~(uint32_t)(RAPID_EMBED_DTABLE_BF16 | RAPID_EMBED_ACCUMULATE)) return RAPID_ERR_INVALID_ARG;
+    if ((d->flags & RAPID_EMBED_DTABLE_BF16) && d->dtype != RAPID_BF16) return RAPID_ERR_INVALID_ARG;
+    if (!isfinite(d->scale) || d->ld_table < d->dim || d->ld_rows < d->dim) return RAPID_ERR_INVALID_ARG;
+    if (d->n_rows > 0x7fffffffll || d->vocab > (1 << 27) - 2 || d->dim > (1 << 24)) return RAPID_ERR_UNSUPPORTED;
+    // far beyond any device's memory; keeps every size below in 64 bits
+    if (d->ld_table > (1ll << 32) || d->ld_rows > (1ll << 32)) return RAPID_ERR_UNSUPPORTED;
+    const size_t rows = elem_size(d->dtype);
+    const size_t table = !bwd ? rows : (d->flags & RAPID_EMBED_DTABLE_BF16) ? 2 : 4;
+    if ((size_t)d->ld_rows * rows % 16 != 0 || (size_t)d->ld_table * table % 16 != 0) return RAPID_ERR_ALIGNMENT;
+    return RAPID_OK;
+}
+
+// blocks of 8 warps, one unit a warp; false when the grid would not fit
+bool blocks_of_8(int64_t units, unsigned* grid) {
+    const int64_t b = (units + 7) / 8;
+    *grid = (unsigned)b;
+    return b <= 0x7fffffffll;
+}
+
+template <class T, class G>
+rapid_status_t run_bwd(const rapid_embed_desc_t& d, const int32_t* tokens, const uint8_t* mask, const T* dout, G* dtable,
+                       const EmbedScratch& w, cudaStream_t st) {
+    const SortShape s = sort_shape(d.n_rows, d.vocab);
+    SortArgs a{};
+    a.tokens = tokens;
+    a.mask = mask;
+    a.vocab = d.vocab;
+    a.hist = w.hist;
+    const int segs = (d.dim + kSeg - 1) / kSeg;
+    unsigned piece_grid = 0;
+    if (!blocks_of_8(d.n_rows / kPiece * segs, &piece_grid)) return RAPID_ERR_UNSUPPORTED;
+    if (s.blocks == 1) {
+        sort_one_block_kernel<<<1, kSortThreads, 0, st>>>(a, s, w.key_a, w.row_a, w.key_b, w.row_b);
+    } else {
+        for (int p = 0; p < s.passes; ++p) {
+            a.shift = p * kRadixBits;
+            a.key_in = p == 0 ? nullptr : (p & 1) ? w.key_a : w.key_b;
+            a.row_in = p == 0 ? nullptr : (p & 1) ? w.row_a : w.row_b;
+            a.key_out = (p & 1) ? w.key_b : w.key_a;
+            a.row_out = (p & 1) ? w.row_b : w.row_a;
+            sort_hist_kernel<<<s.blocks, kSortThreads, 0, st>>>(a, s);
+            sort_scatter_kernel<<<s.blocks, kSortThreads, 0, st>>>(a, s);
+        }
+    }
+    const uint32_t* keys = (s.passes & 1) ? w.key_a : w.key_b;
+    const uint32_t* rows = (s.passes & 1) ? w.row_a : w.row_b;
+    if (piece_grid)
+        embed_pieces_kernel<T><<<piece_grid, 256, 0, st>>>(d.n_rows, segs, d.dim, d.ld_rows, d.vocab, keys, rows, dout,
+                                                           w.pieces, w.ldp);
+    embed_rows_kernel<T, G><<<(unsigned)((d.vocab + kRowsPerBlock - 1) / kRowsPerBlock), 256, 0, st>>>(
+        d.n_rows, segs, d.dim, d.ld_rows, d.vocab, d.scale, (d.flags & RAPID_EMBED_ACCUMULATE) != 0, keys, rows, dout, w.pieces,
+        w.ldp, dtable, d.ld_table);
+    return cudaGetLastError() == cudaSuccess ? RAPID_OK : RAPID_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace policy
+}  // namespace rapid
+
+using namespace rapid;
+using namespace rapid::policy;
+
+extern "C" rapid_status_t rapid_embedding_fwd(const rapid_embed_desc_t* desc, const int32_t* tokens, const uint8_t* mask,
+                                              const void* table, void* out, rapid_stats_t* stats, void* stream) {
+    rapid_status_t s = check_embed(desc, false);
+    if (s != RAPID_OK) return s;
+    if (!tokens || !table || !out) return RAPID_ERR_INVALID_ARG;
+    if (!aligned(table, 16) || !aligned(out, 16) || !aligned(tokens, 4)) return RAPID_ERR_ALIGNMENT;
+    const rapid_embed_desc_t& d = *desc;
+    const size_t es = elem_size(d.dtype);
+    if (overlap(table, (size_t)d.vocab * d.ld_table * es, out, (size_t)d.n_rows * d.ld_rows * es)) return RAPID_ERR_INVALID_ARG;
+    const int segs = (d.dim + kFwdSeg - 1) / kFwdSeg;
+    unsigned grid = 0;
+    if (!blocks_of_8(d.n_rows * segs, &grid)) return RAPID_ERR_UNSUPPORTED;
+    int sms = 0;
+    if ((s = check_device(&sms)) != RAPID_OK) return s;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (clear_stats(stats, st) != cudaSuccess) return RAPID_ERR_CUDA;
+    if (d.dtype == RAPID_BF16)
+        embed_fwd_kernel<uint16_t><<<grid, 256, 0, st>>>(d.n_rows, segs, d.vocab, d.dim, d.ld_table, d.ld_rows, d.scale, tokens,
+                                                         mask, static_cast<const uint16_t*>(table), static_cast<uint16_t*>(out), stats);
+    else
+        embed_fwd_kernel<float><<<grid, 256, 0, st>>>(d.n_rows, segs, d.vocab, d.dim, d.ld_table, d.ld_rows, d.scale, tokens, mask,
+                                                      static_cast<const float*>(table), static_cast<float*>(out), stats);
+    return cudaGetLastError() == cudaSuccess ? RAPID_OK : RAPID_ERR_CUDA;
+}
+
+extern "C" rapid_status_t rapid_embedding_bwd_workspace_bytes(const rapid_embed_desc_t* desc, size_t* bytes) {
+    if (!bytes) return RAPID_ERR_INVALID_ARG;
+    rapid_status_t s = check_embed(desc, true);
+    if (s != RAPID_OK) return s;
+    *bytes = carve_embed(*desc, nullptr, nullptr);
+    return RAPID_OK;
+}
+
+extern "C" rapid_status_t rapid_embedding_bwd(const rapid_embed_desc_t* desc, const int32_t* tokens, const uint8_t* mask,
+                                              const void* dout, void* dtable, void* workspace, size_t workspace_bytes,
+                                              void* stream) {
+    rapid_status_t s = check_embed(desc, true);
+    if (s != RAPID_OK) return s;
+    if (!tokens || !dout || !dtable) return RAPID_ERR_INVALID_ARG;
+    if (!aligned(dout, 16) || !aligned(dtable, 16) || !aligned(tokens, 4)) return RAPID_ERR_ALIGNMENT;
+    const rapid_embed_desc_t& d = *desc;
+    const bool grad_bf16 = (d.flags & RAPID_EMBED_DTABLE_BF16) != 0;
+    if (overlap(dout, (size_t)d.n_rows * d.ld_rows * elem_size(d.dtype), dtable, (size_t)d.vocab * d.ld_table * (grad_bf16 ? 2 : 4)))
+        return RAPID_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256)) return RAPID_ERR_WORKSPACE;
+    EmbedScratch w;
+    if (workspace_bytes < carve_embed(d, workspace, &w)) return RAPID_ERR_WORKSPACE;
+    int sms = 0;
+    if ((s = check_device(&sms)) != RAPID_OK) return s;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (d.dtype == RAPID_F32)
+        return run_bwd(d, tokens, mask, static_cast<const float*>(dout), static_cast<float*>(dtable), w, st);
+    if (grad_bf16)
+        return run_bwd(d, tokens, mask, static_cast<const uint16_t*>(dout), static_cast<uint16_t*>(dtable), w, st);
+    return run_bwd(d, tokens, mask, static_cast<const uint16_t*>(dout), static_cast<float*>(dtable), w, st);
+}
