@@ -4,6 +4,7 @@
  *
  *   rapid_embedding_*      token embedding with scaling; its gradient, summed over sorted tokens
  *   rapid_qk_norm_rope_*   root-mean-square norm of every query and key head and the rotation by position, in one pass
+ *   rapid_attention_*      causal attention over the padded token grid; its gradient, from recomputed probabilities
  *
  * The conventions are those of rapid_pg.h: plain scalars and descriptors are HOST memory, every array is a DEVICE
  * pointer valid on the current device; the calls only enqueue work on `stream` (several launches may be enqueued, all
@@ -122,6 +123,56 @@ rapid_status_t rapid_qk_norm_rope_bwd(const rapid_qk_desc_t* desc, const void* q
                                       const uint8_t* mask, const void* dq_out, const void* dk_out, void* dq, void* dk,
                                       float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes,
                                       void* stream);
+
+/* ---- causal attention ------------------------------------------------------------------------------------- */
+
+typedef struct rapid_attn_desc {
+    int32_t n_seq, seq_len;       /* T = n_seq * seq_len rows                                                     */
+    int32_t n_heads, n_kv_heads;  /* n_heads a multiple of n_kv_heads; query head h reads key head h / (n_heads / n_kv_heads) */
+    int32_t head_dim;             /* a multiple of 8, 8 .. 128                                                    */
+    int32_t window;               /* 0 = none; w > 0: position i sees the keys j with i - w < j <= i              */
+    int64_t ld_q, ld_k, ld_v;     /* row pitch, in elements, of q, k and v                                        */
+    int64_t ld_out, ld_dout;      /* of out and dout                                                              */
+    int64_t ld_dq, ld_dk, ld_dv;  /* of the gradients (ld_dout too: rapid_attention_bwd only)                     */
+    int32_t dtype;                /* RAPID_BF16                                                                   */
+    uint32_t flags;               /* 0                                                                            */
+    double scale;                 /* factor of the scores, > 0 and finite (1 / sqrt(head_dim) as a rule)          */
+} rapid_attn_desc_t;
+
+/*
+ * For every generation n and head h, over the live positions b0 <= t < b1 of n:
+ *     s_ij = scale * q_i . k_j  for j <= i (and i - j < window),   lse_i = log sum_j exp s_ij,
+ *     out_i = sum_j exp(s_ij - lse_i) v_j
+ *   q [T, ld_q], k [T, ld_k], v [T, ld_v], out [T, ld_out]  bf16, heads side by side (head h of row r starts at
+ *            r * ld + h * head_dim); bases 16-byte aligned, pitches multiples of 8 elements
+ *   bounds [n_seq][2] int32: b0, b1 of each generation (padding may lie on either side); NULL = 0, seq_len.  Values are
+ *            clipped to [0, seq_len]; b1 <= b0 leaves the generation without a live position
+ *   out      rows outside the bounds are written as zeros
+ *   lse      [n_seq, n_heads, seq_len] float out, natural logarithm, -infinity outside the bounds; may be NULL
+ *   stats    may be NULL; only status is meaningful: RAPID_OK, or RAPID_ERR_TIMEOUT when a bounded wait gave up (the
+ *            outputs are then unspecified)
+ * Rows outside the bounds may hold anything (infinities and NaN too) and influence nothing.  Rows inside must be finite.
+ * The products run on the tensor cores in bf16 with float accumulation; scores, maximum and sum of the softmax are float;
+ * the probabilities are rounded to bf16 for their product with v (relative error 2^-9, as independent roundings).
+ */
+rapid_status_t rapid_attention_fwd(const rapid_attn_desc_t* desc, const void* q, const void* k, const void* v,
+                                   const int32_t* bounds, void* out, float* lse, rapid_stats_t* stats, void* stream);
+
+/* Scratch of rapid_attention_bwd: two floats for each row and head. */
+rapid_status_t rapid_attention_bwd_workspace_bytes(const rapid_attn_desc_t* desc, size_t* bytes);
+
+/*
+ * The gradient, from the inputs, out and lse of the forward call and the gradient dout of out:
+ *     p_ij = exp(s_ij - lse_i),  delta_i = dout_i . out_i,  ds_ij = scale * p_ij * (dout_i . v_j - delta_i)
+ *     dq_i = sum_j ds_ij k_j,   dk_j = sum_i ds_ij q_i,   dv_j = sum_i p_ij dout_i    (dk, dv summed over the heads that
+ * share a key head).  Rows outside the bounds are written as zeros and read from nowhere.  p and ds are rounded to bf16 for
+ * the last three products; the sums are float, each gradient is rounded once.
+ *   dout [T, ld_dout], dq [T, ld_dq], dk [T, ld_dk], dv [T, ld_dv] bf16;  workspace 256-byte aligned
+ */
+rapid_status_t rapid_attention_bwd(const rapid_attn_desc_t* desc, const void* q, const void* k, const void* v,
+                                   const int32_t* bounds, const void* out, const float* lse, const void* dout, void* dq,
+                                   void* dk, void* dv, rapid_stats_t* stats, void* workspace, size_t workspace_bytes,
+                                   void* stream);
 
 #ifdef __cplusplus
 }

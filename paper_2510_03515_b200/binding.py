@@ -54,6 +54,7 @@ EXPORTS = (
     "rapid_pg_loss_onpolicy_fwd_bwd", "rapid_pg_loss_fwd_bwd_hostlogits", "rapid_selftest_bounded_wait",
     "rapid_embedding_fwd", "rapid_embedding_bwd_workspace_bytes", "rapid_embedding_bwd",
     "rapid_qk_norm_rope_fwd", "rapid_qk_norm_rope_bwd_workspace_bytes", "rapid_qk_norm_rope_bwd",
+    "rapid_attention_fwd", "rapid_attention_bwd_workspace_bytes", "rapid_attention_bwd",
 )
 
 
@@ -83,6 +84,13 @@ class QkDesc(C.Structure):
                 ("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("ld_q", C.c_int64), ("ld_k", C.c_int64),
                 ("ld_q_out", C.c_int64), ("ld_k_out", C.c_int64), ("ld_dq", C.c_int64), ("ld_dk", C.c_int64), ("dtype", C.c_int32), ("flags", C.c_uint32),
                 ("eps", C.c_float), ("reserved", C.c_int32)]
+
+
+class AttnDesc(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("seq_len", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("window", C.c_int32), ("ld_q", C.c_int64), ("ld_k", C.c_int64), ("ld_v", C.c_int64),
+                ("ld_out", C.c_int64), ("ld_dout", C.c_int64), ("ld_dq", C.c_int64), ("ld_dk", C.c_int64),
+                ("ld_dv", C.c_int64), ("dtype", C.c_int32), ("flags", C.c_uint32), ("scale", C.c_double)]
 
 
 class RapidError(RuntimeError):
@@ -132,7 +140,7 @@ def lib():
         L.rapid_pg_finalize.argtypes = [dp] + [vp] * 8 + [sz, vp]
         L.rapid_pg_dlogits_chunk.restype = C.c_int
         L.rapid_pg_dlogits_chunk.argtypes = [dp, vp, vp, i64, i64, vp, vp, vp, sz, vp]
-        ep, qp = C.POINTER(EmbedDesc), C.POINTER(QkDesc)
+        ep, qp, ap = C.POINTER(EmbedDesc), C.POINTER(QkDesc), C.POINTER(AttnDesc)
         for name, argtypes in {
             "rapid_embedding_fwd": [ep] + [vp] * 6,
             "rapid_embedding_bwd_workspace_bytes": [ep, C.POINTER(sz)],
@@ -140,6 +148,9 @@ def lib():
             "rapid_qk_norm_rope_fwd": [qp] + [vp] * 10,
             "rapid_qk_norm_rope_bwd_workspace_bytes": [qp, C.POINTER(sz)],
             "rapid_qk_norm_rope_bwd": [qp] + [vp] * 14 + [sz, vp],
+            "rapid_attention_fwd": [ap] + [vp] * 8,
+            "rapid_attention_bwd_workspace_bytes": [ap, C.POINTER(sz)],
+            "rapid_attention_bwd": [ap] + [vp] * 12 + [sz, vp],
         }.items():
             getattr(L, name).restype = C.c_int
             getattr(L, name).argtypes = argtypes
@@ -357,8 +368,8 @@ def pg_loss(logits: torch.Tensor, targets, mask, behav_logp, rewards, group_offs
 
 # ---- policy-network operators (include/rapid_policy_ops.h) ---------------------------------------------------
 #
-# The rapid_* functions marshal the arguments of the C calls; embedding(), embedding_grad(), qk_norm_rope() and
-# qk_norm_rope_grad() check shapes and types, allocate the outputs and make one call.
+# The rapid_* functions marshal the arguments of the C calls; embedding(), embedding_grad(), qk_norm_rope(),
+# qk_norm_rope_grad(), attention() and attention_grad() check shapes and types, allocate the outputs and make one call.
 
 
 def _dtype_code(dtype: torch.dtype) -> int:
@@ -620,3 +631,93 @@ def qk_norm_rope_grad(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch
         ws = torch.empty(rapid_qk_norm_rope_bwd_workspace_bytes(desc), dtype=torch.uint8, device=dev) if norm else None
         rapid_qk_norm_rope_bwd(desc, q, k, q_weight, k_weight, inv_freq, positions, mask, dq_out, dk_out, dq, dk, dw[0], dw[1], ws)
     return QkGrads(dq, dk, dw[0], dw[1])
+
+
+def make_attn_desc(n_seq: int, seq_len: int, n_heads: int, n_kv_heads: int, head_dim: int, window: int = 0,
+                   scale: Optional[float] = None, ld_q: Optional[int] = None, ld_k: Optional[int] = None,
+                   ld_v: Optional[int] = None, ld_out: Optional[int] = None, ld_dout: Optional[int] = None,
+                   ld_dq: Optional[int] = None, ld_dk: Optional[int] = None, ld_dv: Optional[int] = None,
+                   dtype: torch.dtype = torch.bfloat16, flags: int = 0) -> AttnDesc:
+    wq, wk = n_heads * head_dim, n_kv_heads * head_dim
+    pitches = [w if ld is None else ld for w, ld in ((wq, ld_q), (wk, ld_k), (wk, ld_v), (wq, ld_out), (wq, ld_dout), (wq, ld_dq),
+                                                     (wk, ld_dk), (wk, ld_dv))]
+    return AttnDesc(n_seq, seq_len, n_heads, n_kv_heads, head_dim, window, *pitches, _dtype_code(dtype), flags,
+                    max(head_dim, 1) ** -0.5 if scale is None else float(scale))
+
+
+def rapid_attention_fwd(desc: AttnDesc, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, bounds: Optional[torch.Tensor],
+                        out: torch.Tensor, lse: Optional[torch.Tensor], stats: Optional[torch.Tensor]) -> None:
+    _check(lib().rapid_attention_fwd(C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(bounds), _ptr(out), _ptr(lse), _ptr(stats),
+                                     _stream()), "rapid_attention_fwd")
+
+
+def rapid_attention_bwd_workspace_bytes(desc: AttnDesc) -> int:
+    n = C.c_size_t(0)
+    _check(lib().rapid_attention_bwd_workspace_bytes(C.byref(desc), C.byref(n)), "rapid_attention_bwd_workspace_bytes")
+    return int(n.value)
+
+
+def rapid_attention_bwd(desc: AttnDesc, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, bounds: Optional[torch.Tensor],
+                        out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor,
+                        dv: torch.Tensor, stats: Optional[torch.Tensor], workspace: torch.Tensor) -> None:
+    _check(lib().rapid_attention_bwd(
+        C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(bounds), _ptr(out), _ptr(lse), _ptr(dout), _ptr(dq), _ptr(dk), _ptr(dv),
+        _ptr(stats), _ptr(workspace), workspace.numel(), _stream()), "rapid_attention_bwd")
+
+
+def _attn_args(q, k, v, n_seq, seq_len, bounds):
+    T = n_seq * seq_len
+    _need(q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and q.shape[0] == T and k.shape[0] == T and q.shape[2] == k.shape[2],
+          "q: [n_seq * seq_len, heads, head_dim], k, v: [n_seq * seq_len, kv_heads, head_dim] expected")
+    if not q.dtype == k.dtype == v.dtype == torch.bfloat16:
+        raise TypeError("q, k and v must be bfloat16")
+    _vector(bounds, 2 * n_seq, torch.int32, "bounds")
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_seq: int, seq_len: int, bounds: Optional[torch.Tensor] = None,
+              window: int = 0, scale: Optional[float] = None, stats: Optional[torch.Tensor] = None):
+    """Causal attention over the padded token grid, q [T, H, D], k and v [T, Hk, D] bfloat16 (rows may be slices of one
+    projection); bounds [n_seq, 2] int32 gives each generation's live positions.  Returns out [T, H, D] and lse
+    [n_seq, H, seq_len] float32.  The default scale is D ** -0.5."""
+    _attn_args(q, k, v, n_seq, seq_len, bounds)
+    dev = _one_device(q, k, v, bounds, stats)
+    with _on(dev):
+        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        lse = torch.empty(n_seq, q.shape[1], seq_len, device=dev)
+        if q.shape[0] == 0:
+            return out, lse
+        desc = make_attn_desc(n_seq, seq_len, q.shape[1], k.shape[1], q.shape[2], window, scale, _pitch(q, "q"), _pitch(k, "k"),
+                              _pitch(v, "v"))
+        rapid_attention_fwd(desc, q, k, v, bounds, out, lse, stats)
+    return out, lse
+
+
+@dataclass
+class AttnGrads:
+    dq: torch.Tensor  # [T, H, D]
+    dk: torch.Tensor  # [T, Hk, D]
+    dv: torch.Tensor  # [T, Hk, D]
+
+
+def attention_grad(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor,
+                   n_seq: int, seq_len: int, bounds: Optional[torch.Tensor] = None, window: int = 0, scale: Optional[float] = None,
+                   stats: Optional[torch.Tensor] = None, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                   dv: Optional[torch.Tensor] = None) -> AttnGrads:
+    """The gradient of attention() from its inputs, its outputs out and lse, and the gradient of out.  dq, dk and dv may be
+    given (slices of the gradient of one projection, say)."""
+    _attn_args(q, k, v, n_seq, seq_len, bounds)
+    _need(out.shape == q.shape and dout.shape == q.shape, "out, dout: the shape of q expected")
+    if not out.dtype == dout.dtype == torch.bfloat16:
+        raise TypeError("out and dout must be bfloat16")
+    _vector(lse, q.shape[0] * q.shape[1], torch.float32, "lse")
+    dev = _one_device(q, k, v, out, lse, dout, bounds, stats, dq, dk, dv)
+    with _on(dev):
+        dq, dk, dv = _like(dq, q, "dq"), _like(dk, k, "dk"), _like(dv, v, "dv")
+        if q.shape[0] == 0:
+            return AttnGrads(dq, dk, dv)
+        desc = make_attn_desc(n_seq, seq_len, q.shape[1], k.shape[1], q.shape[2], window, scale, _pitch(q, "q"), _pitch(k, "k"),
+                              _pitch(v, "v"), _pitch(out, "out"), _pitch(dout, "dout"), _pitch(dq, "dq"), _pitch(dk, "dk"),
+                              _pitch(dv, "dv"))
+        ws = torch.empty(rapid_attention_bwd_workspace_bytes(desc), dtype=torch.uint8, device=dev)
+        rapid_attention_bwd(desc, q, k, v, bounds, out, lse, dout, dq, dk, dv, stats, ws)
+    return AttnGrads(dq, dk, dv)

@@ -10,6 +10,8 @@
 namespace rapid {
 namespace policy {
 
+static_assert(sizeof(rapid_embed_desc_t) == 48 && sizeof(rapid_qk_desc_t) == 88 && sizeof(rapid_attn_desc_t) == 104, "bindings rely on these");
+
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline size_t elem_size(int32_t dtype) { return dtype == RAPID_BF16 ? 2 : 4; }
 
@@ -17,6 +19,17 @@ inline size_t elem_size(int32_t dtype) { return dtype == RAPID_BF16 ? 2 : 4; }
 inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return x < y + nb && y < x + na;
+}
+
+// Rows of `width` elements at pitch `ld`: do the two matrices share an element?  Matrices of one pitch may lie side by
+// side in the same rows (queries, keys and values of one projection); of two pitches, they have to be apart altogether.
+inline bool rows_overlap(const void* a, int64_t wa, int64_t lda, const void* b, int64_t wb, int64_t ldb, int64_t n, size_t es) {
+    if (!overlap(a, ((size_t)(n - 1) * lda + wa) * es, b, ((size_t)(n - 1) * ldb + wb) * es)) return false;
+    if (lda != ldb) return true;
+    const int64_t pitch = lda * (int64_t)es;
+    int64_t off = ((int64_t)reinterpret_cast<uintptr_t>(b) - (int64_t)reinterpret_cast<uintptr_t>(a)) % pitch;
+    if (off < 0) off += pitch;
+    return off < wa * (int64_t)es || off + wb * (int64_t)es > pitch;
 }
 
 // sm_100 only.  Returns the SM count of the current device through *sm_count.

@@ -345,17 +345,6 @@ rapid_status_t check_qk(const rapid_qk_desc_t* d, bool bwd) {
     return RAPID_OK;
 }
 
-// Rows of `width` elements at pitch `ld`: do the two matrices share an element?  Matrices of one pitch may lie side by
-// side in the same rows (queries, keys and values of one projection); of two pitches, they have to be apart altogether.
-bool rows_overlap(const void* a, int64_t wa, int64_t lda, const void* b, int64_t wb, int64_t ldb, int64_t n, size_t es) {
-    if (!overlap(a, ((size_t)(n - 1) * lda + wa) * es, b, ((size_t)(n - 1) * ldb + wb) * es)) return false;
-    if (lda != ldb) return true;
-    const int64_t pitch = lda * (int64_t)es;
-    int64_t off = ((int64_t)reinterpret_cast<uintptr_t>(b) - (int64_t)reinterpret_cast<uintptr_t>(a)) % pitch;
-    if (off < 0) off += pitch;
-    return off < wa * (int64_t)es || off + wb * (int64_t)es > pitch;
-}
-
 QkArgs make_args(const rapid_qk_desc_t& d, const float* q_weight, const float* k_weight, const float* inv_freq,
                  const int32_t* positions, const uint8_t* mask, int sms) {
     QkArgs p{};

@@ -3,6 +3,7 @@
 // the (static) CUDA runtime.
 #include <mutex>
 
+#include "attention.cuh"
 #include "umma_gemm.cuh"
 
 namespace rapid {
@@ -53,4 +54,20 @@ bool make_map_f32(CUtensorMap* map, const void* base, uint64_t rows, uint64_t co
 }
 
 }  // namespace umma
+
+namespace attn {
+
+bool make_head_map(CUtensorMap* map, const void* base, const rapid_attn_desc_t& d, int heads, int64_t ld) {
+    umma::EncodeFn enc = umma::encoder();
+    if (!enc) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)d.head_dim, (cuuint64_t)heads, (cuuint64_t)d.seq_len, (cuuint64_t)d.n_seq};
+    const cuuint64_t strides[3] = {(cuuint64_t)d.head_dim * 2, (cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)d.seq_len};
+    const cuuint32_t box[4] = {64, 1, (cuuint32_t)kTile, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace attn
 }  // namespace rapid

@@ -24,6 +24,7 @@ def _args(names, **over):
 
 def test_struct_sizes():
     assert C.sizeof(rb.EmbedDesc) == 48 and rb.EmbedDesc.scale.offset == 40
+    assert C.sizeof(rb.AttnDesc) == 104 and rb.AttnDesc.ld_q.offset == 24 and rb.AttnDesc.scale.offset == 96
     assert C.sizeof(rb.QkDesc) == 88 and rb.QkDesc.ld_q.offset == 24 and rb.QkDesc.eps.offset == 80
 
 
@@ -132,6 +133,56 @@ def test_qk_slices_of_one_projection_are_accepted():
     assert _qk_bwd(d2, ws=None, ws_bytes=0, qw=None, kw=None, dqw=None, dkw=None) == rb.RAPID_ERR_CUDA
 
 
+# ---- attention ----------------------------------------------------------------------------------------------------
+
+def _attn_fwd(d, **over):
+    a = _args(["q", "k", "v", "bounds", "out", "lse"], **over)
+    return rb.lib().rapid_attention_fwd(C.byref(d), *a, None, None)
+
+
+def _attn_bwd(d, ws=FAKE, ws_bytes=1 << 50, **over):
+    a = _args(["q", "k", "v", "bounds", "out", "lse", "dout", "dq", "dk", "dv"], **over)
+    return rb.lib().rapid_attention_bwd(C.byref(d), *a, None, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("call", [_attn_fwd, _attn_bwd])
+def test_attention_refusals(call):
+    def d(n=4, length=8, h=4, hk=2, hd=64, **kw):
+        return rb.make_attn_desc(n, length, h, hk, hd, **kw)
+    for kw in (dict(n=0), dict(length=0), dict(h=0), dict(hk=0), dict(hd=0), dict(h=5), dict(window=-1), dict(scale=0.0), dict(scale=-1.0),
+               dict(scale=math.inf), dict(scale=math.nan), dict(flags=1), dict(dtype=F32), dict(ld_q=248), dict(ld_k=120),
+               dict(ld_v=64), dict(ld_out=0)):
+        assert call(d(**kw)) == INVALID, kw
+    for kw in (dict(hd=20), dict(hd=136), dict(n=1 << 20, length=1 << 12), dict(length=(1 << 24) + 1, n=1), dict(ld_q=1 << 36),
+               dict(h=8192, hk=8192)):
+        assert call(d(**kw)) == UNSUP, kw
+    for kw in (dict(ld_q=260), dict(ld_k=132), dict(ld_v=129), dict(ld_out=257)):
+        assert call(d(**kw)) == ALIGN, kw
+    bwd = call is _attn_bwd
+    names = ["q", "k", "v", "out"] + (["dout", "dq", "dk", "dv"] if bwd else [])
+    for name in names + (["lse"] if bwd else []):
+        assert call(d(), **{name: None}) == INVALID, name
+    for name in names:
+        assert call(d(), **{name: FAKE + FAR // 2 + 8}) == ALIGN, name
+    for name in ("dq", "dk", "dv") if bwd else ("out",):
+        assert call(d(), **{name: FAKE + 256}) == INVALID, name  # on q
+        assert call(d(), **{name: FAKE + 2 * FAR}) == INVALID, name  # on v
+    if bwd:
+        assert call(d(), dk=FAKE + 7 * FAR) == INVALID  # on dq
+        for kw in (dict(ld_dout=248), dict(ld_dq=8), dict(ld_dk=64), dict(ld_dv=120)):
+            assert call(d(**kw)) == INVALID, kw
+        assert call(d(ld_dq=258)) == ALIGN and call(d(ld_dk=1 << 36)) == UNSUP
+        n = rb.rapid_attention_bwd_workspace_bytes(d())
+        assert n == 2 * 4 * 4 * 4 * 128
+        assert call(d(), ws=None) == WORK and call(d(), ws=FAKE + 8) == WORK and call(d(), ws_bytes=n - 1) == WORK
+
+
+@no_gpu
+def test_attention_without_a_device():
+    d = rb.make_attn_desc(4, 8, 4, 2, 64)
+    assert _attn_fwd(d, bounds=None, lse=None) == rb.RAPID_ERR_CUDA and _attn_bwd(d) == rb.RAPID_ERR_CUDA
+
+
 def test_wrappers_check_shapes_and_types_before_the_call():
     x = torch.zeros(4, 2, 16)
     w = torch.zeros(16)
@@ -152,3 +203,12 @@ def test_wrappers_check_shapes_and_types_before_the_call():
         rb.embedding_grad(torch.zeros(4, 8), tok, None, 5, dtable_dtype=torch.bfloat16)
     with pytest.raises(ValueError):
         rb.embedding_grad(torch.zeros(4, 8), tok, None, 5, dtable=torch.zeros(5, 9))
+    b = x.to(BF)
+    with pytest.raises(TypeError):
+        rb.attention(x, x, x, 2, 2)
+    with pytest.raises(ValueError):
+        rb.attention(b, b, b, 2, 3)
+    with pytest.raises(TypeError):
+        rb.attention(b, b, b, 2, 2, torch.zeros(2, 2))
+    with pytest.raises(ValueError):
+        rb.attention_grad(b, b, b, b, torch.zeros(3), b, 2, 2)
