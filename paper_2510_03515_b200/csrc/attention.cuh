@@ -7,7 +7,7 @@
 // reaches past the end of a generation reads zeros there and its stores are cut off.
 //
 // Positions outside a generation's bounds may hold anything.  They are masked out of the scores, and wherever such a
-// row is summed over (0 x NaN is NaN), the issuing warp overwrites it with zeros in shared memory before the product.
+// row is summed over (0 x NaN is NaN), a warp overwrites it with zeros in shared memory before the product.
 #pragma once
 
 #include <cuda.h>
@@ -21,10 +21,6 @@
 namespace rapid {
 namespace attn {
 
-using umma::mma_commit;
-using umma::mma_f16;
-using umma::smem_desc;
-using umma::swz128;
 using umma::tc_fence_after;
 using umma::tc_fence_before;
 using umma::tmem_alloc;
@@ -50,20 +46,49 @@ __device__ __forceinline__ void tma_load_4d(void* smem_dst, const CUtensorMap* m
         "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(h), "r"(t), "r"(n)
         : "memory");
 }
-__device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, const void* smem_src, int x, int h, int t, int n) {
-    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(map),
-                 "r"(smem_u32(smem_src)), "r"(x), "r"(h), "r"(t), "r"(n)
-                 : "memory");
-}
-// D[tmem] (+)= A[tmem] * B[smem]: lane i of A holds row i, a 32-bit column two consecutive bf16 along K
-__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+// True in one lane of a converged warp.  The whole loop that issues products runs inside `if (elect_one())`: the compiler
+// then knows that one lane runs and keeps operands in uniform registers.  Measured for 128 x 64 x 16 (operands in tensor
+// and shared memory): one product takes 33 cycles this way, 67 when the lane is chosen by a predicate.  Products are
+// accepted only a few ahead, so what the lane does between two groups of them is time the tensor cores lose: a group of
+// four with a wait before it and two commits after takes 326 cycles in one lane, 549 when the whole warp waits and votes.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t e;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(e));
+    return e != 0;
+}
+
+// A shared-memory descriptor as umma::smem_desc builds it, split in halves: the upper one is the same for every tile, and
+// stepping through a tile is an addition to the lower one.
+constexpr uint32_t kDescHi = 0x40004040u;  // stride offset 1024, version 1, 128-byte swizzle
+__device__ __forceinline__ uint32_t desc_lo(uint32_t saddr, uint32_t lbo_bytes) { return (saddr >> 4) | ((lbo_bytes >> 4) << 16); }
+
+// D[tmem] (+)= A[smem] * B[smem]
+__device__ __forceinline__ void mma_ss_1(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        "mov.b64 a, {%1, %5};\n\t"
+        "mov.b64 b, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(kDescHi)
         : "memory");
 }
+// D[tmem] (+)= A[tmem] * B[smem]: lane i of A holds row i, a 32-bit column two consecutive bf16 along K
+__device__ __forceinline__ void mma_ts_1(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "mov.b64 b, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "n"(kDescHi)
+        : "memory");
+}
+using umma::mma_commit;  // arrive on a barrier once every product issued so far by this lane has ended
+
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
@@ -83,12 +108,16 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
         "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
         : "memory");
 }
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-// barrier of `count` threads of the block (id 1 .. 15; whole warps)
-__device__ __forceinline__ void named_barrier(int id, int count) {
-    asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(count) : "memory");
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
 }
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // ---- descriptors ------------------------------------------------------------------------------------------------
 
@@ -96,19 +125,30 @@ __device__ __forceinline__ void named_barrier(int id, int count) {
 __host__ __device__ constexpr uint32_t instr_desc(int n, bool b_mn) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
 }
-// Step `ks` of 16 elements along the head: the K-major form of a tile.
-__device__ __forceinline__ uint64_t desc_k(uint32_t tile, int ks) {
-    return smem_desc(tile + (uint32_t)(ks >> 2) * kBoxBytes + (uint32_t)(ks & 3) * 32u, 16);
-}
-// Step `ks` of 16 positions: the MN-major form (the head's elements are the other dimension).
-__device__ __forceinline__ uint64_t desc_mn(uint32_t tile, int ks) { return smem_desc(tile + (uint32_t)ks * 2048u, kBoxBytes); }
+// Lower descriptor halves of a tile: contraction over the head's elements (K-major; step `ks` of 16 elements), and over
+// positions (MN-major; a step of 16 positions is 2048 bytes further on).
+__device__ __forceinline__ uint32_t tile_k(uint32_t tile) { return desc_lo(tile, 16); }
+__device__ __forceinline__ uint32_t tile_mn(uint32_t tile) { return desc_lo(tile, kBoxBytes); }
+__device__ __forceinline__ constexpr uint32_t step_k(int ks) { return (uint32_t)((ks >> 2) * kBoxBytes + (ks & 3) * 32) >> 4; }
+__device__ __forceinline__ constexpr uint32_t step_mn(int ks) { return (uint32_t)ks * 2048u >> 4; }
 
 // D[128 x 128] = A[128 x D] * B[128 x D]^T, both tiles K-major in shared memory
 template <int D>
-__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_tile, uint32_t b_tile) {
-    constexpr uint32_t idesc = instr_desc(kTile, false);
+__device__ __forceinline__ void mma_rows(uint32_t d_tmem, uint32_t a_tile, uint32_t b_tile) {
+    const uint32_t a = tile_k(a_tile), b = tile_k(b_tile);
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) mma_f16(d_tmem, desc_k(a_tile, ks), desc_k(b_tile, ks), idesc, ks > 0 ? 1u : 0u);
+    for (int ks = 0; ks < D / 16; ++ks)
+        mma_ss_1(d_tmem, a + step_k(ks), b + step_k(ks), instr_desc(kTile, false), ks > 0 ? 1u : 0u);
+}
+
+// acc[128 x D] (+)= M[128 x 128] * B[128 x D], M in tensor memory as bf16 (its second 64 columns start `half` 32-bit
+// columns after the first), B a tile used MN-major
+template <int D>
+__device__ __forceinline__ void mma_sum(uint32_t acc, uint32_t m, uint32_t half, uint32_t b_tile, uint32_t more) {
+    const uint32_t b = tile_mn(b_tile);
+#pragma unroll
+    for (int ks = 0; ks < kTile / 16; ++ks)
+        mma_ts_1(acc, m + (ks >> 2) * half + (ks & 3) * 8u, b + step_mn(ks), instr_desc(D, true), ks > 0 ? 1u : more);
 }
 
 template <int D>
@@ -116,17 +156,69 @@ __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* map, 
 #pragma unroll
     for (int b = 0; b < D / 64; ++b) tma_load_4d(dst + b * kBoxBytes, map, b * 64, h, t0, n, bar);
 }
-template <int D>
-__device__ __forceinline__ void store_tile(const CUtensorMap* map, const uint8_t* src, int head_dim, int h, int t0, int n) {
-#pragma unroll
-    for (int b = 0; b < D / 64; ++b)
-        if (b * 64 < head_dim) tma_store_4d(map, src + b * kBoxBytes, b * 64, h, t0, n);
+// Wait for a phase of a barrier, bounded.  The first poll has no suspension hint: a phase that is over already then costs
+// a few tens of cycles.
+__device__ __forceinline__ bool wait_one(uint64_t* bar, uint32_t parity, volatile int* abortp) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return done ? true : mbar_wait_bounded(bar, parity, abortp);
+}
+// The same for a whole warp; all lanes get the same answer.
+__device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity, volatile int* abortp) {
+    return __all_sync(0xffffffffu, wait_one(bar, parity, abortp));
+}
+
+// Place in a ring of `N` buffers: buffer number and the parity of its current use.
+template <uint32_t N>
+struct Place {
+    uint32_t s = 0, parity = 0;
+    __device__ __forceinline__ void step(uint32_t by = 1) {
+        s += by;
+        if (s >= N) {
+            s -= N;
+            parity ^= 1u;
+        }
+    }
+};
+
+// Tiles that hold dead rows ("dirty") come through a warp of their own: the copy reports to `raw`, the cleaning warp zeroes
+// the dead rows and reports to the tile's ordinary barrier in the copy's place, and the readers notice nothing.
+struct RawParity {
+    uint32_t bits = 0;  // one for each buffer of a ring
+    __device__ __forceinline__ uint32_t flip(uint32_t s) {  // parity of this use
+        const uint32_t p = (bits >> s) & 1u;
+        bits ^= 1u << s;
+        return p;
+    }
+};
+__device__ __forceinline__ bool dirty(int tile, int lo, int hi) { return tile * kTile < lo || tile * kTile + kTile > hi; }
+
+// After giving up: wait (again bounded) for something that is under way to arrive.
+__device__ __forceinline__ void wait_landed(uint64_t* bar, uint32_t parity) {
+    const unsigned long long t0 = global_timer_ns();
+    while (!mbar_try_wait(bar, parity))
+        if (global_timer_ns() - t0 > kWaitLimitNs) break;
+}
+
+// Wait for the commit of the last products, with the wait's own limit.
+__device__ __forceinline__ void wait_drained(uint64_t* bar, volatile int* abortp) {
+    const unsigned long long t0 = global_timer_ns();
+    while (!mbar_try_wait(bar, 0))
+        if (global_timer_ns() - t0 > kWaitLimitNs) {
+            *abortp = 1;
+            break;
+        }
 }
 
 // One warp overwrites with zeros the rows of a tile that lie outside [lo, hi), before a product reads them.
 template <int D>
 __device__ __forceinline__ void zero_rows_outside(uint8_t* tile, int t0, int lo, int hi, int lane) {
-    if (t0 >= lo && t0 + kTile <= hi) return;
     for (int i = lane; i < D / 64 * kTile * 8; i += 32) {
         const int row = (i >> 3) & (kTile - 1);
         if (t0 + row < lo || t0 + row >= hi) reinterpret_cast<uint4*>(tile)[i] = make_uint4(0, 0, 0, 0);
@@ -135,15 +227,122 @@ __device__ __forceinline__ void zero_rows_outside(uint8_t* tile, int t0, int lo,
     __syncwarp();
 }
 
-// Row `row` of a tile in shared memory <- 32 values at columns [32 c, 32 c + 32), as bf16, in the layout of the copies.
-__device__ __forceinline__ void stage_row32(uint8_t* tile, int row, int c, const float (&f)[32]) {
-    uint8_t* box = tile + (c >> 1) * kBoxBytes;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        *reinterpret_cast<uint4*>(box + swz128(row, (c & 1) * 4 + k)) =
-            make_uint4(pack_bf16x2(f[8 * k], f[8 * k + 1]), pack_bf16x2(f[8 * k + 2], f[8 * k + 3]),
-                       pack_bf16x2(f[8 * k + 4], f[8 * k + 5]), pack_bf16x2(f[8 * k + 6], f[8 * k + 7]));
+// ---- work handed out by the hardware ------------------------------------------------------------------------------
+//
+// A grid has one block for each piece of work, but a block that is done cancels the launch of a waiting one and does its
+// work instead (clusterlaunchcontrol), until none is left.  Barriers, tensor memory and the copies' descriptors are set up
+// once for each SM, the next piece's loads run under the end of this one, and the pieces still go to whoever is free.
+// One lane asks, when it has issued the last loads of a piece (asking earlier would tie the next piece to a block that is
+// still busy for long: dK, dV of 64 x 1024 took 410 us instead of 325); every role reads the answer.
+struct WorkQueue {
+    __align__(16) uint4 answer[2];
+    __align__(8) uint64_t full[2], empty[2];
+};
+
+__device__ __forceinline__ void work_init(WorkQueue* q, uint32_t readers) {
+    for (int i = 0; i < 2; ++i) {
+        mbar_init(&q->full[i], 1);
+        mbar_init(&q->empty[i], readers);
+    }
 }
+// Ask for the piece after number k (0, 1, ...).  False: gave up.
+__device__ __forceinline__ bool work_ask(WorkQueue* q, uint32_t k, volatile int* abortp) {
+    const uint32_t s = k & 1u;
+    if (k >= 2 && !mbar_wait_bounded(&q->empty[s], ((k >> 1) & 1u) ^ 1u, abortp)) return false;
+    mbar_arrive_expect_tx(&q->full[s], 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                     smem_u32(&q->answer[s])),
+                 "r"(smem_u32(&q->full[s]))
+                 : "memory");
+    return true;
+}
+// The answer to the request after piece k: the block number to do next, or -1.
+__device__ __forceinline__ int work_read(WorkQueue* q, uint32_t k) {
+    uint32_t x, got;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b128 r;\n\t"
+        "ld.shared.b128 r, [%2];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+        "selp.u32 %1, 1, 0, p;\n\t"
+        "mov.u32 %0, 0;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, r;\n\t}"
+        : "=r"(x), "=r"(got)
+        : "r"(smem_u32(&q->answer[k & 1u]))
+        : "memory");
+    return got ? (int)x : -1;
+}
+// One lane as a reader: wait, read, give the slot back.  -1 too when the wait gave up.
+__device__ __forceinline__ int work_next_one(WorkQueue* q, uint32_t k, volatile int* abortp) {
+    if (!wait_one(&q->full[k & 1u], (k >> 1) & 1u, abortp)) return -1;
+    const int next = work_read(q, k);
+    fence_proxy_async_smem();  // the read comes before the next answer's write
+    mbar_arrive(&q->empty[k & 1u]);
+    return next;
+}
+// The same for a whole warp.
+__device__ __forceinline__ int work_next(WorkQueue* q, uint32_t k, int lane, volatile int* abortp) {
+    if (!wait_all(&q->full[k & 1u], (k >> 1) & 1u, abortp)) return -1;
+    const int next = __shfl_sync(0xffffffffu, work_read(q, k), 0);
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&q->empty[k & 1u]);
+    return next;
+}
+
+// ---- exponentials -------------------------------------------------------------------------------------------------
+//
+// The special-function unit forms 16 exponentials a cycle and SM, which is what bounds these kernels' inner loops (1024
+// cycles for a 128 x 128 tile against 512 for a product with D = 128).  So a part of them is formed by the multiply-add
+// units: 2^x = 2^n 2^f with n = round(x) and f in [-1/2, 1/2]; 2^f by the polynomial of degree 4 with the least maximal
+// relative error (2.6e-6; coefficients from a Remez iteration), 2^n by adding n to the exponent's bits.  Below 2^-126 the
+// result is not zero but some value below 1.2e-38.
+__device__ __forceinline__ void exp2_pair_poly(uint64_t x2, float& lo, float& hi) {
+    constexpr float kRound = 12582912.f;  // 1.5 * 2^23: adding it rounds to an integer, which lands in the low bits
+    float x, y;
+    f32x2_split(x2, x, y);
+    x2 = f32x2(fmaxf(x, -126.f), fmaxf(y, -126.f));
+    const uint64_t r = f32x2_add(x2, f32x2(kRound, kRound));
+    const uint64_t n = f32x2_add(r, f32x2(-kRound, -kRound));
+    const uint64_t f = f32x2_fma(n, f32x2(-1.f, -1.f), x2);
+    uint64_t p = f32x2(0.009570102207362652f, 0.009570102207362652f);
+    p = f32x2_fma(p, f, f32x2(0.05591785907745361f, 0.05591785907745361f));
+    p = f32x2_fma(p, f, f32x2(0.240247443318367f, 0.240247443318367f));
+    p = f32x2_fma(p, f, f32x2(0.6931217908859253f, 0.6931217908859253f));
+    p = f32x2_fma(p, f, f32x2(0.9999992847442627f, 0.9999992847442627f));
+    float a, b, u, v;
+    f32x2_split(p, a, b);
+    f32x2_split(r, u, v);
+    lo = __int_as_float(__float_as_int(a) + (__float_as_int(u) << 23));
+    hi = __int_as_float(__float_as_int(b) + (__float_as_int(v) << 23));
+}
+
+// ---- results ------------------------------------------------------------------------------------------------------
+
+// 32 columns [c, c + 32) of a row of `head_dim` bf16 at `row`.  `wide`: rows and heads begin on 32-byte boundaries, so that
+// whole sectors can be written at once.
+__device__ __forceinline__ void store_row32(uint16_t* row, int c, int head_dim, bool wide, const float (&f)[32]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = pack_bf16x2(f[16 * k + 2 * i], f[16 * k + 2 * i + 1]);
+        uint16_t* p = row + c + 16 * k;
+        if (wide && c + 16 * k + 16 <= head_dim) {
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                         "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                         : "memory");
+        } else {
+            if (c + 16 * k + 8 <= head_dim) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+            if (c + 16 * k + 16 <= head_dim) *reinterpret_cast<uint4*>(p + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+    }
+}
+
+// Registers of the four warps that call it together: the eight warps that hold rows take what the four others leave (both
+// shares add up to the launch's 3 x 168 for each quarter of an SM).
+__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
+__device__ __forceinline__ void leave_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
+constexpr int kThreads = 384;  // warps 0-7: rows; 8: copies; 9: products; 10: dead rows; 11: only its registers are needed
 
 // ---- geometry -----------------------------------------------------------------------------------------------------
 
@@ -176,6 +375,9 @@ __device__ __forceinline__ void key_tiles(const Geometry& g, int t, int lo, int 
 // Argument checks that both directions share, and the kernels' view of a descriptor.
 rapid_status_t check_attn(const rapid_attn_desc_t* d);
 Geometry make_geometry(const rapid_attn_desc_t& d, const int32_t* bounds);
+
+// Whether 32-byte stores to 16-element groups of every row and head are aligned.
+inline bool wide_rows(const void* p, int64_t ld, int head_dim) { return policy::aligned(p, 32) && ld % 16 == 0 && head_dim % 16 == 0; }
 
 // Tensor map of [n_seq][seq_len][heads][head_dim] bf16 with row pitch `ld` elements, boxes of 128 positions x 64 elements.
 bool make_head_map(CUtensorMap* map, const void* base, const rapid_attn_desc_t& d, int heads, int64_t ld);

@@ -11,8 +11,8 @@
 // its partial sums in memory), which would make results depend on the order of blocks.
 //
 // In both main kernels warps 0-7 hold 64 columns of a row each thread, warp 8 issues copies, warp 9 products.  The order of
-// the products is such that the tensor cores have two products (1024 cycles at D = 128) to work on while the exponentials
-// of one step are formed, and two more during its dS.
+// the products is such that the tensor cores have two of them to work on while the exponentials of one step are formed, and
+// one or two more during its dS.
 #include <math.h>
 
 #include "attention.cuh"
@@ -21,7 +21,6 @@ namespace rapid {
 namespace attn {
 namespace {
 
-constexpr int kThreads = 320;
 constexpr int kVecBytes = kTile * 4;  // one float for each position of a tile
 
 struct BwdArgs {
@@ -30,6 +29,9 @@ struct BwdArgs {
     int tiles;         // of a generation
     const float* shift;   // [n_seq][heads][tiles * 128]: -lse in base 2
     const float* ndelta;  // the same: -delta
+    uint16_t *dq, *dk, *dv;
+    int64_t ld_dq, ld_dk, ld_dv;
+    bool wide_dq, wide_dk, wide_dv;  // see store_row32
     rapid_stats_t* stats;
 };
 
@@ -73,287 +75,432 @@ attn_row_terms_kernel(Geometry g, int tiles, int lanes_log2, const uint16_t* __r
     }
 }
 
+// 64 scores of a row (raw, as read from tensor memory) -> exponentials of score * c + shift.  `shift_at(k)`: the pair of
+// shifts of columns 2 k, 2 k + 1.  One pair in four by polynomial (measured against none and against one in two).
+template <class F>
+__device__ __forceinline__ void probabilities(const uint32_t (&s)[2][32], uint64_t c2, F shift_at, float (&p)[64]) {
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+        const uint32_t* x = &s[k >> 4][(k & 15) * 2];
+        const uint64_t z = f32x2_fma(f32x2(__uint_as_float(x[0]), __uint_as_float(x[1])), c2, shift_at(k));
+        if ((k & 3) == 3) {
+            exp2_pair_poly(z, p[2 * k], p[2 * k + 1]);
+        } else {
+            float u, v;
+            f32x2_split(z, u, v);
+            p[2 * k] = ex2_approx(u);
+            p[2 * k + 1] = ex2_approx(v);
+        }
+    }
+}
+__device__ __forceinline__ void round_pairs(const float (&p)[64], uint32_t (&b)[32]) {
+#pragma unroll
+    for (int k = 0; k < 32; ++k) b[k] = pack_bf16x2(p[2 * k], p[2 * k + 1]);
+}
+// p * (dp - delta) as bf16
+template <class F>
+__device__ __forceinline__ void score_grads(const uint32_t (&s)[2][32], const float (&p)[64], F ndelta_at, uint32_t (&b)[32]) {
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+        const uint32_t* x = &s[k >> 4][(k & 15) * 2];
+        float u, v;
+        f32x2_split(f32x2_mul(f32x2(p[2 * k], p[2 * k + 1]), f32x2_add(f32x2(__uint_as_float(x[0]), __uint_as_float(x[1])), ndelta_at(k))), u, v);
+        b[k] = pack_bf16x2(u, v);
+    }
+}
+
+// One lane's `D / 32` chunks [from, to) of an accumulator row, times `factor`, to memory (zeros where not `live`).
+__device__ __forceinline__ void write_row(uint32_t acc, int from, int to, bool any, bool live, float factor, uint16_t* dst, int head_dim,
+                                          bool wide, bool mine) {
+#pragma unroll 1
+    for (int i = from; i < to; ++i) {
+        float f[32];
+        if (any) {
+            uint32_t o[32];
+            tmem_ld32(acc + 32u * i, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) f[k] = live ? __uint_as_float(o[k]) * factor : 0.f;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) f[k] = 0.f;
+        }
+        if (mine) store_row32(dst, 32 * i, head_dim, wide, f);
+    }
+}
+
 // ---- dK, dV -----------------------------------------------------------------------------------------------------
 
 template <int D>
 struct DkvCfg {
-    static constexpr int kStages = D == 128 ? 4 : 8;  // tiles of q and dout in flight, alternating
-    static constexpr size_t kSmem = (size_t)(2 + kStages) * tile_bytes<D>() + (size_t)kStages * kVecBytes + 1024;
+    static constexpr uint32_t kQ = D == 128 ? 3 : 4, kDo = D == 128 ? 2 : 4;  // tiles of q (needed the longest) and of dout in flight
+    static constexpr uint32_t kVec = 2;                                       // row terms of query tiles in flight
+    // At D = 128 tensor memory is full (S', dP', dV, dK): P' lies over S' and dS' over dP', each half of the columns over its
+    // own half.  At D = 64 they have columns of their own and the next S', dP' start as soon as the last are in registers.
+    static constexpr bool kOverlay = D == 128;
+    static constexpr size_t kTiles = (size_t)(2 + kQ + kDo) * tile_bytes<D>();
+    struct Barriers {
+        WorkQueue queue;
+        // k_*, v_*, acc_* count pieces of work that have steps, the others steps
+        uint64_t k_full, k_empty, v_full, v_empty, acc_full, acc_empty, s_full, s_empty, dp_full, dp_empty, p_full, p_empty, ds_full,
+            ds_empty, all_done;
+        uint64_t q_full[kQ], q_empty[kQ], q_raw[kQ], do_full[kDo], do_empty[kDo], do_raw[kDo], vec_full[kVec], vec_empty[kVec];
+        uint32_t tmem_slot;
+        int abort_flag;
+    };
+    // everything in one dynamic block, so that no byte goes to alignment: at D = 128 it fills the SM's 227 KB but for 600 bytes
+    static constexpr size_t kSmem = kTiles + kVec * 2 * kVecBytes + sizeof(Barriers);
+    static_assert(kSmem <= 232448, "shared memory of an SM");
+};
+
+// Work: a key tile of one key head; steps: the heads of its group times the query tiles that see it.
+struct DkvWork {
+    int n, hk, kt, lo, hi, q_from, q_tiles, steps;
+
+    __device__ __forceinline__ DkvWork(const BwdArgs& a, int block) {
+        const Geometry& g = a.g;
+        // the first key tiles are seen by the most queries: they go first
+        kt = (int)((unsigned)block / (unsigned)(g.n_seq * g.kv_heads));
+        const int nk = (int)((unsigned)block % (unsigned)(g.n_seq * g.kv_heads));
+        n = nk / g.kv_heads;
+        hk = nk - n * g.kv_heads;
+        live_range(g, n, lo, hi);
+        const int key_last = min(kt * kTile + kTile, hi) - 1;
+        q_from = kt;
+        q_tiles = 0;
+        if (max(kt * kTile, lo) <= key_last) q_tiles = min(hi - 1, key_last + g.window - 1) / kTile + 1 - kt;
+        steps = q_tiles * g.group;
+    }
 };
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
-                const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo,
-                const __grid_constant__ CUtensorMap mdk, const __grid_constant__ CUtensorMap mdv, BwdArgs a) {
-    constexpr int kStages = DkvCfg<D>::kStages;
+                const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ BwdArgs a) {
+    using Cfg = DkvCfg<D>;
+    constexpr uint32_t kQ = Cfg::kQ, kDo = Cfg::kDo, kVec = Cfg::kVec;
+    constexpr bool kOverlay = Cfg::kOverlay;
     constexpr int TB = tile_bytes<D>();
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    __shared__ __align__(8) uint64_t kv_full, s_full, dp_full, p_full, ds_full, all_done, full[kStages], empty[kStages];
-    __shared__ uint32_t tmem_slot;
-    __shared__ int abort_flag;
-    volatile int* abortp = &abort_flag;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    typename Cfg::Barriers& m = *reinterpret_cast<typename Cfg::Barriers*>(smem + Cfg::kTiles + kVec * 2 * kVecBytes);
+    if ((smem_u32(smem) & 1023u) != 0) {  // the copies' swizzle counts from 1024-byte boundaries; there is no slack to move to one
+        if (threadIdx.x == 0 && a.stats) atomicMax(&a.stats->status, (int)RAPID_ERR_ALIGNMENT);
+        return;
+    }
+    volatile int* abortp = &m.abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const Geometry& g = a.g;
 
-    // the first key tiles are seen by the most queries: they go first
-    const int kt = (int)(blockIdx.x / (unsigned)(g.n_seq * g.kv_heads));
-    const int nk = (int)(blockIdx.x % (unsigned)(g.n_seq * g.kv_heads));
-    const int n = nk / g.kv_heads, hk = nk - n * g.kv_heads;
-    int lo, hi;
-    live_range(g, n, lo, hi);
-    const int key_last = min(kt * kTile + kTile, hi) - 1;
-    int q_from = 0, q_tiles = 0;
-    if (max(kt * kTile, lo) <= key_last) {
-        q_from = kt;
-        const int64_t last = min((int64_t)hi - 1, (int64_t)key_last + g.window - 1);
-        q_tiles = (int)(last / kTile) + 1 - kt;
-    }
-    const int steps = q_tiles * g.group;  // step i: head hk * group + i / q_tiles, query tile q_from + i % q_tiles
-
     if (tid == 0) {
-        mbar_init(&kv_full, 1);
-        mbar_init(&s_full, 1);
-        mbar_init(&dp_full, 1);
-        mbar_init(&p_full, 8);
-        mbar_init(&ds_full, 8);
-        mbar_init(&all_done, 1);
-        for (int s = 0; s < kStages; ++s) {
-            mbar_init(&full[s], 1);
-            mbar_init(&empty[s], 1);
+        mbar_init(&m.k_full, 1);
+        mbar_init(&m.k_empty, 1);
+        mbar_init(&m.v_full, 1);
+        mbar_init(&m.v_empty, 1);
+        mbar_init(&m.acc_full, 1);
+        mbar_init(&m.acc_empty, 8);
+        mbar_init(&m.s_full, 1);
+        mbar_init(&m.s_empty, 8);
+        mbar_init(&m.dp_full, 1);
+        mbar_init(&m.dp_empty, 8);
+        mbar_init(&m.p_full, 8);
+        mbar_init(&m.p_empty, 1);
+        mbar_init(&m.ds_full, 8);
+        mbar_init(&m.ds_empty, 1);
+        mbar_init(&m.all_done, 1);
+        for (uint32_t s = 0; s < kQ; ++s) {
+            mbar_init(&m.q_full[s], 1);
+            mbar_init(&m.q_empty[s], 1);
+            mbar_init(&m.q_raw[s], 1);
         }
-        abort_flag = 0;
+        for (uint32_t s = 0; s < kDo; ++s) {
+            mbar_init(&m.do_full[s], 1);
+            mbar_init(&m.do_empty[s], 1);
+            mbar_init(&m.do_raw[s], 1);
+        }
+        for (uint32_t s = 0; s < kVec; ++s) {
+            mbar_init(&m.vec_full[s], 1);
+            mbar_init(&m.vec_empty[s], 8);
+        }
+        work_init(&m.queue, 10);
+        m.abort_flag = 0;
         mbar_init_fence();
     }
     if (warp == 9) {
-        tmem_alloc(&tmem_slot, 512);
+        tmem_alloc(&m.tmem_slot, 512);
         tmem_relinquish();
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, m.tmem_slot, 0);
     const uint32_t s_t = tmem, dp_t = tmem + 128u, dv_t = tmem + 256u, dk_t = tmem + 256u + D;
+    const uint32_t p_t = kOverlay ? s_t : tmem + 384u, ds_t = kOverlay ? dp_t : tmem + 448u;
+    constexpr uint32_t kHalf = kOverlay ? 64u : 32u;  // columns from the first half of P' or dS' to the second
     uint8_t* k_tile = smem;
     uint8_t* v_tile = smem + TB;
-    // ring number 2 i is the query tile of step i, 2 i + 1 its dout tile; both row terms come and go with the query tile,
-    // which is released after the step's last reader of either (dS, then dK)
-    auto tile_of = [&](uint32_t it) { return smem + (size_t)(2 + it % kStages) * TB; };
-    auto vec_of = [&](uint32_t it) { return reinterpret_cast<float*>(smem + (size_t)(2 + kStages) * TB) + (it % kStages) * kTile; };
+    auto q_tile = [&](uint32_t s) { return smem + (2u + s) * (uint32_t)TB; };
+    auto do_tile = [&](uint32_t s) { return smem + (2u + kQ + s) * (uint32_t)TB; };
+    auto vec_of = [&](uint32_t s) { return reinterpret_cast<float*>(smem + Cfg::kTiles) + s * 2u * kTile; };
 
+    if (warp >= 8) leave_registers();
     if (warp == 8) {
         // ------------------------------------ copies ------------------------------------------------------
-        if (lane == 0 && steps > 0) {
-            mbar_arrive_expect_tx(&kv_full, 2 * TB);
-            load_tile<D>(k_tile, &mk, hk, kt * kTile, n, &kv_full);
-            load_tile<D>(v_tile, &mv, hk, kt * kTile, n, &kv_full);
+        if (lane == 0) {
+            uint32_t steps = 0, n_do = 0, n_vec = 0, pieces = 0, v_pieces = 0, k = 0, q_was_raw = 0, do_was_raw = 0;
+            RawParity q_raw, do_raw;
+            Place<kQ> qa;
+            Place<kDo> da;
+            Place<kVec> ca;
             bool ok = true;
-            uint32_t it = 0;
-            for (int i = 0; i < steps && ok; ++i) {
-                const int h = hk * g.group + i / q_tiles, qt = q_from + i % q_tiles;
-                const size_t at = (((size_t)n * g.heads + h) * a.tiles + qt) * kTile;
-                for (int half = 0; half < 2; ++half, ++it) {
-                    const int s = it % kStages;
-                    const uint32_t use = it / kStages;
-                    if (use > 0 && !mbar_wait_bounded(&empty[s], (use & 1u) ^ 1u, abortp)) {
-                        ok = false;
-                        break;
+            int block = (int)blockIdx.x;
+            while (block >= 0) {
+                const DkvWork x(a, block);
+                if (x.steps > 0) {
+                    if (pieces > 0 && !(ok = wait_one(&m.k_empty, (pieces - 1u) & 1u, abortp))) break;
+                    mbar_arrive_expect_tx(&m.k_full, TB);
+                    load_tile<D>(k_tile, &mk, x.hk, x.kt * kTile, x.n, &m.k_full);
+                    ++pieces;
+                }
+                int h = x.hk * g.group, qt = x.q_from;
+                for (int i = 0; i < x.steps; ++i) {
+                    const bool clean = dirty(qt, x.lo, x.hi);
+                    if (steps >= kQ && !(ok = wait_one(&m.q_empty[qa.s], qa.parity ^ 1u, abortp))) break;
+                    uint64_t* bar = clean ? &m.q_raw[qa.s] : &m.q_full[qa.s];
+                    q_was_raw = clean ? q_was_raw | (1u << qa.s) : q_was_raw & ~(1u << qa.s);
+                    if (clean) q_raw.flip(qa.s);
+                    mbar_arrive_expect_tx(bar, TB);
+                    load_tile<D>(q_tile(qa.s), &mq, h, qt * kTile, x.n, bar);
+                    ++steps;
+                    qa.step();
+
+                    if (n_vec >= kVec && !(ok = wait_one(&m.vec_empty[ca.s], ca.parity ^ 1u, abortp))) break;
+                    const size_t at = (((size_t)x.n * g.heads + h) * a.tiles + qt) * kTile;
+                    mbar_arrive_expect_tx(&m.vec_full[ca.s], 2 * kVecBytes);
+                    bulk_load(vec_of(ca.s), a.shift + at, kVecBytes, &m.vec_full[ca.s]);
+                    bulk_load(vec_of(ca.s) + kTile, a.ndelta + at, kVecBytes, &m.vec_full[ca.s]);
+                    ++n_vec;
+                    ca.step();
+
+                    if (i == 0) {  // V after the first query tile: its old tile is needed the longest
+                        if (v_pieces > 0 && !(ok = wait_one(&m.v_empty, (v_pieces - 1u) & 1u, abortp))) break;
+                        mbar_arrive_expect_tx(&m.v_full, TB);
+                        load_tile<D>(v_tile, &mv, x.hk, x.kt * kTile, x.n, &m.v_full);
+                        ++v_pieces;
                     }
-                    mbar_arrive_expect_tx(&full[s], half ? TB : TB + 2 * kVecBytes);
-                    load_tile<D>(tile_of(it), half ? &mdo : &mq, h, qt * kTile, n, &full[s]);
-                    if (!half) {
-                        bulk_load(vec_of(it), a.shift + at, kVecBytes, &full[s]);
-                        bulk_load(vec_of(it) + kTile, a.ndelta + at, kVecBytes, &full[s]);
+
+                    if (n_do >= kDo && !(ok = wait_one(&m.do_empty[da.s], da.parity ^ 1u, abortp))) break;
+                    bar = clean ? &m.do_raw[da.s] : &m.do_full[da.s];
+                    do_was_raw = clean ? do_was_raw | (1u << da.s) : do_was_raw & ~(1u << da.s);
+                    if (clean) do_raw.flip(da.s);
+                    mbar_arrive_expect_tx(bar, TB);
+                    load_tile<D>(do_tile(da.s), &mdo, h, qt * kTile, x.n, bar);
+                    ++n_do;
+                    da.step();
+
+                    if (++qt == x.q_from + x.q_tiles) {
+                        qt = x.q_from;
+                        ++h;
                     }
                 }
+                if (!ok || !(ok = work_ask(&m.queue, k, abortp))) break;
+                ++k;
+                if (!(ok = mbar_wait_bounded(&m.queue.full[(k - 1u) & 1u], ((k - 1u) >> 1) & 1u, abortp))) break;
+                block = work_read(&m.queue, k - 1u);
+                fence_proxy_async_smem();
             }
-            if (!ok || *abortp) {  // gave up: let the copies land before the block's memory goes away
-                for (uint32_t x = it > (uint32_t)kStages ? it - kStages : 0u; x <= it; ++x) {
-                    uint64_t* bar = x < it ? &full[x % kStages] : &kv_full;
-                    const uint32_t parity = x < it ? (x / kStages) & 1u : 0u;
-                    const unsigned long long t0 = global_timer_ns();
-                    while (!mbar_try_wait(bar, parity))
-                        if (global_timer_ns() - t0 > kWaitLimitNs) break;
+            if (!ok || *abortp) {  // gave up: what is under way lands before the block's memory goes away
+                for (uint32_t s = 0; s < kQ && s < steps; ++s) {
+                    if ((q_was_raw >> s) & 1u) wait_landed(&m.q_raw[s], ((q_raw.bits >> s) & 1u) ^ 1u);
+                    else wait_landed(&m.q_full[s], s < qa.s ? qa.parity : qa.parity ^ 1u);
                 }
+                for (uint32_t s = 0; s < kDo && s < n_do; ++s) {
+                    if ((do_was_raw >> s) & 1u) wait_landed(&m.do_raw[s], ((do_raw.bits >> s) & 1u) ^ 1u);
+                    else wait_landed(&m.do_full[s], s < da.s ? da.parity : da.parity ^ 1u);
+                }
+                for (uint32_t s = 0; s < kVec && s < n_vec; ++s) wait_landed(&m.vec_full[s], s < ca.s ? ca.parity : ca.parity ^ 1u);
+                if (pieces > 0) wait_landed(&m.k_full, (pieces - 1u) & 1u);
+                if (v_pieces > 0) wait_landed(&m.v_full, (v_pieces - 1u) & 1u);
+                if (k > 0) wait_landed(&m.queue.full[(k - 1u) & 1u], ((k - 1u) >> 1) & 1u);
             }
+        }
+    } else if (warp == 10) {
+        // ------------------------------------ dead rows ---------------------------------------------------
+        RawParity q_raw, do_raw;
+        Place<kQ> qa;
+        Place<kDo> da;
+        bool ok = true;
+        int block = (int)blockIdx.x;
+        for (uint32_t k = 0; block >= 0 && ok; ++k) {
+            const DkvWork x(a, block);
+            int qt = x.q_from;
+            for (int i = 0; i < x.steps && ok; ++i) {
+                if (dirty(qt, x.lo, x.hi)) {
+                    ok = wait_all(&m.q_raw[qa.s], q_raw.flip(qa.s), abortp);
+                    if (ok) zero_rows_outside<D>(q_tile(qa.s), qt * kTile, x.lo, x.hi, lane);
+                    if (ok && lane == 0) mbar_arrive(&m.q_full[qa.s]);
+                    ok = ok && wait_all(&m.do_raw[da.s], do_raw.flip(da.s), abortp);
+                    if (ok) zero_rows_outside<D>(do_tile(da.s), qt * kTile, x.lo, x.hi, lane);
+                    if (ok && lane == 0) mbar_arrive(&m.do_full[da.s]);
+                }
+                qa.step();
+                da.step();
+                qt = qt + 1 < x.q_from + x.q_tiles ? qt + 1 : x.q_from;
+            }
+            if (ok) block = work_next(&m.queue, k, lane, abortp);
         }
     } else if (warp == 9) {
         // ------------------------------------ products ----------------------------------------------------
-        bool ok = true;
-        auto wait = [&](uint64_t* bar, uint32_t parity) {
-            ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abortp));
-            tc_fence_after();
-            return ok;
-        };
-        // wait for a tile of the ring and clear its dead rows
-        auto take = [&](uint32_t it) {
-            if (!wait(&full[it % kStages], (it / kStages) & 1u)) return false;
-            const int qt = q_from + (int)(it >> 1) % q_tiles;
-            zero_rows_outside<D>(tile_of(it), qt * kTile, lo, hi, lane);
-            return true;
-        };
-        // acc (+)= M (128 x 128 bf16 in tensor memory: 64 columns of a half in 32 of its own) * tile (MN-major)
-        auto mma_acc = [&](uint32_t acc, uint32_t m, uint32_t tile, bool more) {
-#pragma unroll
-            for (int ks = 0; ks < kTile / 16; ++ks)
-                mma_f16_ts(acc, m + (ks >> 2) * 64u + (ks & 3) * 8u, desc_mn(tile, ks), instr_desc(D, true), (more || ks) ? 1u : 0u);
-        };
-        if (steps > 0 && wait(&kv_full, 0)) {
+        if (elect_one()) {
+            bool ok = true;
+            auto wait = [&](uint64_t* bar, uint32_t parity) {
+                ok = ok && wait_one(bar, parity, abortp);
+                tc_fence_after();
+            };
             const uint32_t kb = smem_u32(k_tile), vb = smem_u32(v_tile);
-            if (take(0) && lane == 0) {
-                mma_ss<D>(s_t, kb, smem_u32(tile_of(0)));
-                mma_commit(&s_full);
-            }
-            if (ok && take(1) && lane == 0) {
-                mma_ss<D>(dp_t, vb, smem_u32(tile_of(1)));
-                mma_commit(&dp_full);
-            }
-            for (int i = 0; i < steps && ok; ++i) {
-                const uint32_t iq = 2u * i, id = iq + 1u;
-                if (!wait(&p_full, i & 1)) break;
-                if (lane == 0) {
-                    mma_acc(dv_t, s_t, smem_u32(tile_of(id)), i > 0);
-                    mma_commit(&empty[id % kStages]);
+            auto q_addr = [&](uint32_t s) { return kb + (2u + s) * (uint32_t)TB; };
+            auto do_addr = [&](uint32_t s) { return kb + (2u + kQ + s) * (uint32_t)TB; };
+            uint32_t pieces = 0, gi = 0;   // gi: steps so far, over all pieces
+            Place<kQ> qa, qd;              // the query tile of the next scores, of the next dK
+            Place<kDo> da, dd;             // the dout tile of the next dP, of the next dV
+            auto scores = [&](bool last) {  // S' of the next step
+                wait(&m.q_full[qa.s], qa.parity);
+                if (!ok) return;
+                mma_rows<D>(s_t, kb, q_addr(qa.s));
+                mma_commit(&m.s_full);
+                if (last) mma_commit(&m.k_empty);
+                qa.step();
+            };
+            auto dps = [&](bool last) {  // dP' of the next step
+                wait(&m.do_full[da.s], da.parity);
+                if (!ok) return;
+                mma_rows<D>(dp_t, vb, do_addr(da.s));
+                mma_commit(&m.dp_full);
+                if (last) mma_commit(&m.v_empty);
+                da.step();
+            };
+            int block = (int)blockIdx.x;
+            for (uint32_t k = 0; block >= 0 && ok; ++k) {
+                const DkvWork x(a, block);
+                if (x.steps > 0) {
+                    wait(&m.k_full, pieces & 1u);
+                    if (!kOverlay && gi > 0) wait(&m.s_empty, (gi - 1u) & 1u);
+                    scores(x.steps == 1);
+                    wait(&m.v_full, pieces & 1u);
+                    if (!kOverlay && gi > 0) wait(&m.dp_empty, (gi - 1u) & 1u);
+                    dps(x.steps == 1);
+                    if (pieces > 0) wait(&m.acc_empty, (pieces - 1u) & 1u);
                 }
-                if (i + 1 < steps) {
-                    if (!take(iq + 2)) break;
-                    if (lane == 0) {
-                        mma_ss<D>(s_t, kb, smem_u32(tile_of(iq + 2)));
-                        mma_commit(&s_full);
+                for (int i = 0; i < x.steps && ok; ++i, ++gi) {
+                    const bool more = i + 1 < x.steps, last = i + 2 == x.steps;
+                    if (!kOverlay && more) {
+                        wait(&m.s_empty, gi & 1u);
+                        scores(last);
                     }
-                }
-                if (!wait(&ds_full, i & 1)) break;
-                if (lane == 0) {
-                    mma_acc(dk_t, dp_t, smem_u32(tile_of(iq)), i > 0);
-                    mma_commit(&empty[iq % kStages]);
-                }
-                if (i + 1 < steps) {
-                    if (!take(id + 2)) break;
-                    if (lane == 0) {
-                        mma_ss<D>(dp_t, vb, smem_u32(tile_of(id + 2)));
-                        mma_commit(&dp_full);
+                    wait(&m.p_full, gi & 1u);
+                    if (!ok) break;
+                    mma_sum<D>(dv_t, p_t, kHalf, do_addr(dd.s), (uint32_t)i);
+                    if (kOverlay && more) scores(last);
+                    mma_commit(&m.do_empty[dd.s]);
+                    dd.step();
+                    if (!kOverlay) mma_commit(&m.p_empty);
+                    if (!kOverlay && more) {
+                        wait(&m.dp_empty, gi & 1u);
+                        dps(last);
                     }
+                    wait(&m.ds_full, gi & 1u);
+                    if (!ok) break;
+                    mma_sum<D>(dk_t, ds_t, kHalf, q_addr(qd.s), (uint32_t)i);
+                    if (!more) mma_commit(&m.acc_full);
+                    if (kOverlay && more) dps(last);
+                    mma_commit(&m.q_empty[qd.s]);
+                    qd.step();
+                    if (!kOverlay) mma_commit(&m.ds_empty);
                 }
+                if (x.steps > 0) ++pieces;
+                if (ok) block = work_next_one(&m.queue, k, abortp);
             }
+            // every product has ended before tensor memory is given back
+            mma_commit(&m.all_done);
+            wait_drained(&m.all_done, abortp);
         }
         __syncwarp();
-        if (lane == 0) {  // every product has ended before results are read and tensor memory is given back
-            mma_commit(&all_done);
-            const unsigned long long t0 = global_timer_ns();
-            while (!mbar_try_wait(&all_done, 0))
-                if (global_timer_ns() - t0 > kWaitLimitNs) {
-                    *abortp = 1;
-                    break;
-                }
-        }
-    } else {
+    } else if (warp < 8) {
         // ------------------------------------ probabilities, dS -------------------------------------------
+        take_registers();
         const int half = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t mine = lanes + (uint32_t)half * 64u;
-        const int key = kt * kTile + row;
-        const float c = a.scale_log2;
-        const uint64_t c2 = f32x2(c, c);
+        const uint32_t mine = lanes + (uint32_t)half * 64u, packed = lanes + (uint32_t)half * kHalf;
+        const uint64_t c2 = f32x2(a.scale_log2, a.scale_log2);
         bool ok = true;
         auto wait = [&](uint64_t* bar, uint32_t parity) {
-            ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abortp));
+            ok = ok && wait_all(bar, parity, abortp);
             tc_fence_after();
             return ok;
         };
-        for (int i = 0; i < steps; ++i) {
-            const uint32_t iq = 2u * i;
-            const int q0 = (q_from + i % q_tiles) * kTile;
-            float p[64];
-            if (!wait(&full[iq % kStages], (iq / kStages) & 1u) || !wait(&s_full, i & 1)) break;
-            {
-                uint32_t s[2][32];
+        auto tell = [&](uint64_t* bar) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+        };
+        uint32_t gi = 0, pieces = 0;
+        Place<kVec> ca;
+        int block = (int)blockIdx.x;
+        for (uint32_t k = 0; block >= 0; ++k) {
+            const DkvWork x(a, block);
+            const int key = x.kt * kTile + row;
+            int qt = x.q_from;
+            for (int i = 0; i < x.steps; ++i, ++gi) {
+                const int q0 = qt * kTile;
+                qt = qt + 1 < x.q_from + x.q_tiles ? qt + 1 : x.q_from;
+                float p[64];
+                uint32_t s[2][32], b[32];
+                if (!wait(&m.vec_full[ca.s], ca.parity) || !wait(&m.s_full, gi & 1u)) break;
                 tmem_ld32(s_t + mine, s[0]);
                 tmem_ld32(s_t + mine + 32u, s[1]);
-                const ulonglong2* sh = reinterpret_cast<const ulonglong2*>(vec_of(iq) + half * 64);
                 tmem_ld_wait();
+                if (!kOverlay) tell(&m.s_empty);
+                const ulonglong2* shift = reinterpret_cast<const ulonglong2*>(vec_of(ca.s) + half * 64);
+                probabilities(s, c2, [&](int e) { return e & 1 ? shift[e >> 1].y : shift[e >> 1].x; }, p);
+                // the diagonal, and the far edge of a window
+                if (q0 <= x.kt * kTile || q0 + kTile - 1 - x.kt * kTile >= g.window) {
+                    const int first = q0 + half * 64 - key;
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    const ulonglong2 l = sh[k];
-                    const uint32_t* x = &s[k >> 3][(k & 7) * 4];
-                    f32x2_split(f32x2_fma(f32x2(__uint_as_float(x[0]), __uint_as_float(x[1])), c2, l.x), p[4 * k], p[4 * k + 1]);
-                    f32x2_split(f32x2_fma(f32x2(__uint_as_float(x[2]), __uint_as_float(x[3])), c2, l.y), p[4 * k + 2], p[4 * k + 3]);
+                    for (int e = 0; e < 64; ++e)
+                        if ((unsigned)(first + e) >= (unsigned)g.window) p[e] = 0.f;
                 }
-            }
-#pragma unroll
-            for (int k = 0; k < 64; ++k) p[k] = ex2_approx(p[k]);
-            // the diagonal, and the far edge of a window
-            if (q0 <= kt * kTile || q0 + kTile - 1 - kt * kTile >= g.window) {
-                const int first = q0 + half * 64 - key;
-#pragma unroll
-                for (int k = 0; k < 64; ++k)
-                    if ((unsigned)(first + k) >= (unsigned)g.window) p[k] = 0.f;
-            }
-            {
-                uint32_t b[32];
-#pragma unroll
-                for (int k = 0; k < 32; ++k) b[k] = pack_bf16x2(p[2 * k], p[2 * k + 1]);
-                tmem_st32(s_t + mine, b);
-            }
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&p_full);
+                round_pairs(p, b);
+                if (!kOverlay && gi > 0 && !wait(&m.p_empty, (gi - 1u) & 1u)) break;
+                tmem_st32(p_t + packed, b);
+                tmem_st_wait();
+                tell(&m.p_full);
 
-            if (!wait(&dp_full, i & 1)) break;
-            {
-                uint32_t s[2][32], b[32];
+                if (!wait(&m.dp_full, gi & 1u)) break;
                 tmem_ld32(dp_t + mine, s[0]);
                 tmem_ld32(dp_t + mine + 32u, s[1]);
-                const ulonglong2* nd = reinterpret_cast<const ulonglong2*>(vec_of(iq) + kTile + half * 64);
                 tmem_ld_wait();
-#pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    const ulonglong2 d = nd[k];
-                    const uint32_t* x = &s[k >> 3][(k & 7) * 4];
-                    float e, f;
-                    f32x2_split(f32x2_mul(f32x2(p[4 * k], p[4 * k + 1]), f32x2_add(f32x2(__uint_as_float(x[0]), __uint_as_float(x[1])), d.x)), e, f);
-                    b[2 * k] = pack_bf16x2(e, f);
-                    f32x2_split(f32x2_mul(f32x2(p[4 * k + 2], p[4 * k + 3]), f32x2_add(f32x2(__uint_as_float(x[2]), __uint_as_float(x[3])), d.y)), e, f);
-                    b[2 * k + 1] = pack_bf16x2(e, f);
-                }
-                tmem_st32(dp_t + mine, b);
+                if (!kOverlay) tell(&m.dp_empty);
+                const ulonglong2* ndelta = reinterpret_cast<const ulonglong2*>(vec_of(ca.s) + kTile + half * 64);
+                score_grads(s, p, [&](int e) { return e & 1 ? ndelta[e >> 1].y : ndelta[e >> 1].x; }, b);
+                if (!kOverlay && gi > 0 && !wait(&m.ds_empty, (gi - 1u) & 1u)) break;
+                tmem_st32(ds_t + packed, b);
+                tmem_st_wait();
+                tell(&m.ds_full);
+                if (lane == 0) mbar_arrive(&m.vec_empty[ca.s]);
+                ca.step();
             }
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&ds_full);
-        }
-        // warps 0-3 write dV, warps 4-7 dK, through the tile in shared memory that is no longer needed
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&all_done, 0, abortp));
-        tc_fence_after();
-        const bool live = key >= lo && key < hi;
-        const float factor = half ? a.scale : 1.f;
-        uint8_t* stage = half ? k_tile : v_tile;
-        const uint32_t acc = (half ? dk_t : dv_t) + lanes;
-        if (ok) {
-#pragma unroll 1
-            for (int i = 0; i < D / 32; ++i) {
-                float f[32];
-                if (steps > 0) {
-                    uint32_t o[32];
-                    tmem_ld32(acc + 32u * i, o);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) f[k] = live ? __uint_as_float(o[k]) * factor : 0.f;
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) f[k] = 0.f;
-                }
-                stage_row32(stage, row, i, f);
+            // warps 0-3 write dV, warps 4-7 dK
+            if (ok && x.steps > 0) wait(&m.acc_full, pieces & 1u);
+            if (!ok) break;
+            const bool live = key >= x.lo && key < x.hi;
+            const int64_t r = (int64_t)x.n * g.seq_len + key;
+            uint16_t* dst = (half ? a.dk + r * a.ld_dk : a.dv + r * a.ld_dv) + x.hk * g.head_dim;
+            write_row((half ? dk_t : dv_t) + lanes, 0, D / 32, x.steps > 0, live, half ? a.scale : 1.f, dst, g.head_dim,
+                      half ? a.wide_dk : a.wide_dv, key < g.seq_len);
+            if (x.steps > 0) {
+                tell(&m.acc_empty);
+                ++pieces;
             }
-            fence_proxy_async_smem();
-        }
-        named_barrier(1 + half, 128);
-        if ((warp & 3) == 0 && lane == 0 && !*abortp) {
-            store_tile<D>(half ? &mdk : &mdv, stage, g.head_dim, hk, kt * kTile, n);
-            bulk_commit();
-            bulk_wait_all<0>();
+            block = work_next(&m.queue, k, lane, abortp);
         }
     }
     tc_fence_before();
@@ -362,46 +509,60 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
-    if (tid == 0 && abort_flag && a.stats) atomicMax(&a.stats->status, (int)RAPID_ERR_TIMEOUT);
+    if (tid == 0 && m.abort_flag && a.stats) atomicMax(&a.stats->status, (int)RAPID_ERR_TIMEOUT);
 }
 
 // ---- dQ ---------------------------------------------------------------------------------------------------------
 
 template <int D>
 struct DqCfg {
-    static constexpr int kKeys = 3, kVals = 2;  // tiles of keys (needed for two steps) and of values in flight
+    static constexpr int kKeys = D == 128 ? 3 : 4, kVals = D == 128 ? 2 : 3;  // tiles of keys (needed for two steps) and values in flight
     static constexpr size_t kSmem = (size_t)(2 + kKeys + kVals) * tile_bytes<D>() + 1024;
+};
+
+// Work: a query tile of one head; steps: the key tiles that it sees.
+struct DqWork {
+    int n, h, t, lo, hi, from, steps;
+
+    __device__ __forceinline__ DqWork(const BwdArgs& a, int block) {
+        const Geometry& g = a.g;
+        // the longest rows first; the heads of a group next to one another, they read the same keys
+        t = a.tiles - 1 - (int)((unsigned)block / (unsigned)(g.n_seq * g.heads));
+        const int nh = (int)((unsigned)block % (unsigned)(g.n_seq * g.heads));
+        n = nh / g.heads;
+        h = nh - n * g.heads;
+        live_range(g, n, lo, hi);
+        int to;
+        key_tiles(g, t, lo, hi, from, to);
+        steps = to - from;
+    }
 };
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
-               const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo,
-               const __grid_constant__ CUtensorMap mdq, BwdArgs a) {
+               const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ BwdArgs a) {
     constexpr uint32_t kKeys = DqCfg<D>::kKeys, kVals = DqCfg<D>::kVals;
     constexpr int TB = tile_bytes<D>();
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    __shared__ __align__(8) uint64_t q_full, do_full, s_full[2], dp_full, ds_full, all_done, k_full[kKeys], k_empty[kKeys],
-        v_full[kVals], v_empty[kVals];
+    // q_*, do_*, acc_* count pieces of work that have steps, the others steps
+    __shared__ __align__(8) uint64_t q_full, q_empty, do_full, do_empty, acc_full, acc_empty, s_full[2], dp_full, ds_full, all_done,
+        k_full[kKeys], k_empty[kKeys], k_raw[kKeys], v_full[kVals], v_empty[kVals], v_raw[kVals];
+    __shared__ WorkQueue queue;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     volatile int* abortp = &abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const Geometry& g = a.g;
 
-    // the longest rows first; the heads of a group next to one another, they read the same keys
-    const int t = a.tiles - 1 - (int)(blockIdx.x / (unsigned)(g.n_seq * g.heads));
-    const int nh = (int)(blockIdx.x % (unsigned)(g.n_seq * g.heads));
-    const int n = nh / g.heads, h = nh - n * g.heads, hk = h / g.group;
-    int lo, hi, from, to;
-    live_range(g, n, lo, hi);
-    key_tiles(g, t, lo, hi, from, to);
-    const int steps = to - from;
-
     if (tid == 0) {
         mbar_init(&q_full, 1);
+        mbar_init(&q_empty, 1);
         mbar_init(&do_full, 1);
+        mbar_init(&do_empty, 1);
+        mbar_init(&acc_full, 1);
+        mbar_init(&acc_empty, 8);
         mbar_init(&s_full[0], 1);
         mbar_init(&s_full[1], 1);
         mbar_init(&dp_full, 1);
@@ -410,11 +571,14 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         for (uint32_t s = 0; s < kKeys; ++s) {
             mbar_init(&k_full[s], 1);
             mbar_init(&k_empty[s], 1);
+            mbar_init(&k_raw[s], 1);
         }
         for (uint32_t s = 0; s < kVals; ++s) {
             mbar_init(&v_full[s], 1);
             mbar_init(&v_empty[s], 1);
+            mbar_init(&v_raw[s], 1);
         }
+        work_init(&queue, 10);
         abort_flag = 0;
         mbar_init_fence();
     }
@@ -425,197 +589,235 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_slot;
-    // scores of even and odd steps, dP, dQ
-    auto s_addr = [&](int i) { return tmem + (uint32_t)(i & 1) * 128u; };
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
+    // scores of even and odd steps (dS of a step lies over its scores), dP, dQ
+    auto s_addr = [&](uint32_t i) { return tmem + (i & 1u) * 128u; };
     const uint32_t dp_t = tmem + 256u, dq_t = tmem + 384u;
     uint8_t* q_tile = smem;
     uint8_t* do_tile = smem + TB;
-    auto k_tile = [&](uint32_t i) { return smem + (size_t)(2 + i % kKeys) * TB; };
-    auto v_tile = [&](uint32_t i) { return smem + (size_t)(2 + kKeys + i % kVals) * TB; };
+    auto k_tile = [&](uint32_t s) { return smem + (2u + s) * (uint32_t)TB; };
+    auto v_tile = [&](uint32_t s) { return smem + (2u + kKeys + s) * (uint32_t)TB; };
 
+    if (warp >= 8) leave_registers();
     if (warp == 8) {
         // ------------------------------------ copies ------------------------------------------------------
-        if (lane == 0 && steps > 0) {
-            mbar_arrive_expect_tx(&q_full, TB);
-            load_tile<D>(q_tile, &mq, h, t * kTile, n, &q_full);
-            mbar_arrive_expect_tx(&do_full, TB);
-            load_tile<D>(do_tile, &mdo, h, t * kTile, n, &do_full);
+        if (lane == 0) {
             bool ok = true;
-            uint32_t nkeys = 0, nvals = 0;
-            // in the order of use: K_0 V_0 K_1 V_1 ...
-            for (uint32_t i = 0; i < (uint32_t)steps && ok; ++i) {
-                if (i >= kKeys && !mbar_wait_bounded(&k_empty[i % kKeys], ((i / kKeys) & 1u) ^ 1u, abortp)) {
-                    ok = false;
-                    break;
+            uint32_t nk = 0, nv = 0, nq = 0, ndo = 0, k = 0, k_was_raw = 0, v_was_raw = 0;
+            RawParity kr, vr;
+            Place<kKeys> ka;
+            Place<kVals> va;
+            int block = (int)blockIdx.x;
+            while (block >= 0) {
+                const DqWork x(a, block);
+                if (x.steps > 0) {
+                    if (nq > 0 && !(ok = wait_one(&q_empty, (nq - 1u) & 1u, abortp))) break;
+                    mbar_arrive_expect_tx(&q_full, TB);
+                    load_tile<D>(q_tile, &mq, x.h, x.t * kTile, x.n, &q_full);
+                    ++nq;
                 }
-                mbar_arrive_expect_tx(&k_full[i % kKeys], TB);
-                load_tile<D>(k_tile(i), &mk, hk, (from + (int)i) * kTile, n, &k_full[i % kKeys]);
-                ++nkeys;
-                if (i >= kVals && !mbar_wait_bounded(&v_empty[i % kVals], ((i / kVals) & 1u) ^ 1u, abortp)) {
-                    ok = false;
-                    break;
+                // in the order of use: K_0 dout V_0 K_1 V_1 ...
+                const int hk = x.h / g.group;
+                for (int i = 0; i < x.steps; ++i) {
+                    const int t0 = (x.from + i) * kTile;
+                    const bool clean = dirty(x.from + i, x.lo, x.hi);
+                    if (nk >= kKeys && !(ok = wait_one(&k_empty[ka.s], ka.parity ^ 1u, abortp))) break;
+                    uint64_t* bar = clean ? &k_raw[ka.s] : &k_full[ka.s];
+                    k_was_raw = clean ? k_was_raw | (1u << ka.s) : k_was_raw & ~(1u << ka.s);
+                    if (clean) kr.flip(ka.s);
+                    mbar_arrive_expect_tx(bar, TB);
+                    load_tile<D>(k_tile(ka.s), &mk, hk, t0, x.n, bar);
+                    ++nk;
+                    ka.step();
+                    if (i == 0) {
+                        if (ndo > 0 && !(ok = wait_one(&do_empty, (ndo - 1u) & 1u, abortp))) break;
+                        mbar_arrive_expect_tx(&do_full, TB);
+                        load_tile<D>(do_tile, &mdo, x.h, x.t * kTile, x.n, &do_full);
+                        ++ndo;
+                    }
+                    if (nv >= kVals && !(ok = wait_one(&v_empty[va.s], va.parity ^ 1u, abortp))) break;
+                    bar = clean ? &v_raw[va.s] : &v_full[va.s];
+                    v_was_raw = clean ? v_was_raw | (1u << va.s) : v_was_raw & ~(1u << va.s);
+                    if (clean) vr.flip(va.s);
+                    mbar_arrive_expect_tx(bar, TB);
+                    load_tile<D>(v_tile(va.s), &mv, hk, t0, x.n, bar);
+                    ++nv;
+                    va.step();
                 }
-                mbar_arrive_expect_tx(&v_full[i % kVals], TB);
-                load_tile<D>(v_tile(i), &mv, hk, (from + (int)i) * kTile, n, &v_full[i % kVals]);
-                ++nvals;
+                if (!ok || !(ok = work_ask(&queue, k, abortp))) break;
+                ++k;
+                if (!(ok = mbar_wait_bounded(&queue.full[(k - 1u) & 1u], ((k - 1u) >> 1) & 1u, abortp))) break;
+                block = work_read(&queue, k - 1u);
+                fence_proxy_async_smem();
             }
-            if (!ok || *abortp) {  // gave up: let the copies land before the block's memory goes away
-                auto land = [&](uint64_t* bar, uint32_t parity) {
-                    const unsigned long long t0 = global_timer_ns();
-                    while (!mbar_try_wait(bar, parity))
-                        if (global_timer_ns() - t0 > kWaitLimitNs) break;
-                };
-                land(&q_full, 0);
-                land(&do_full, 0);
-                for (uint32_t i = nkeys > kKeys ? nkeys - kKeys : 0u; i < nkeys; ++i) land(&k_full[i % kKeys], (i / kKeys) & 1u);
-                for (uint32_t i = nvals > kVals ? nvals - kVals : 0u; i < nvals; ++i) land(&v_full[i % kVals], (i / kVals) & 1u);
+            if (!ok || *abortp) {  // gave up: what is under way lands before the block's memory goes away
+                if (nq > 0) wait_landed(&q_full, (nq - 1u) & 1u);
+                if (ndo > 0) wait_landed(&do_full, (ndo - 1u) & 1u);
+                for (uint32_t s = 0; s < kKeys && s < nk; ++s) {
+                    if ((k_was_raw >> s) & 1u) wait_landed(&k_raw[s], ((kr.bits >> s) & 1u) ^ 1u);
+                    else wait_landed(&k_full[s], s < ka.s ? ka.parity : ka.parity ^ 1u);
+                }
+                for (uint32_t s = 0; s < kVals && s < nv; ++s) {
+                    if ((v_was_raw >> s) & 1u) wait_landed(&v_raw[s], ((vr.bits >> s) & 1u) ^ 1u);
+                    else wait_landed(&v_full[s], s < va.s ? va.parity : va.parity ^ 1u);
+                }
+                if (k > 0) wait_landed(&queue.full[(k - 1u) & 1u], ((k - 1u) >> 1) & 1u);
             }
+        }
+    } else if (warp == 10) {
+        // ------------------------------------ dead rows ---------------------------------------------------
+        RawParity kr, vr;
+        Place<kKeys> ka;
+        Place<kVals> va;
+        bool ok = true;
+        int block = (int)blockIdx.x;
+        for (uint32_t k = 0; block >= 0 && ok; ++k) {
+            const DqWork x(a, block);
+            for (int i = 0; i < x.steps && ok; ++i) {
+                const int t0 = (x.from + i) * kTile;
+                if (dirty(x.from + i, x.lo, x.hi)) {
+                    ok = wait_all(&k_raw[ka.s], kr.flip(ka.s), abortp);
+                    if (ok) zero_rows_outside<D>(k_tile(ka.s), t0, x.lo, x.hi, lane);
+                    if (ok && lane == 0) mbar_arrive(&k_full[ka.s]);
+                    ok = ok && wait_all(&v_raw[va.s], vr.flip(va.s), abortp);
+                    if (ok) zero_rows_outside<D>(v_tile(va.s), t0, x.lo, x.hi, lane);
+                    if (ok && lane == 0) mbar_arrive(&v_full[va.s]);
+                }
+                ka.step();
+                va.step();
+            }
+            if (ok) block = work_next(&queue, k, lane, abortp);
         }
     } else if (warp == 9) {
         // ------------------------------------ products ----------------------------------------------------
-        bool ok = true;
-        auto wait = [&](uint64_t* bar, uint32_t parity) {
-            ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abortp));
-            tc_fence_after();
-            return ok;
-        };
-        auto scores = [&](uint32_t i) {
-            if (!wait(&k_full[i % kKeys], (i / kKeys) & 1u)) return;
-            zero_rows_outside<D>(k_tile(i), (from + (int)i) * kTile, lo, hi, lane);
-            if (lane == 0) {
-                mma_ss<D>(s_addr(i), smem_u32(q_tile), smem_u32(k_tile(i)));
-                mma_commit(&s_full[i & 1]);
-            }
-        };
-        auto dps = [&](uint32_t i) {
-            if (!wait(&v_full[i % kVals], (i / kVals) & 1u)) return;
-            zero_rows_outside<D>(v_tile(i), (from + (int)i) * kTile, lo, hi, lane);
-            if (lane == 0) {
-                mma_ss<D>(dp_t, smem_u32(do_tile), smem_u32(v_tile(i)));
+        if (elect_one()) {
+            bool ok = true;
+            auto wait = [&](uint64_t* bar, uint32_t parity) {
+                ok = ok && wait_one(bar, parity, abortp);
+                tc_fence_after();
+            };
+            const uint32_t qb = smem_u32(q_tile), dob = smem_u32(do_tile);
+            auto k_addr = [&](uint32_t s) { return qb + (2u + s) * (uint32_t)TB; };
+            auto v_addr = [&](uint32_t s) { return qb + (2u + kKeys + s) * (uint32_t)TB; };
+            uint32_t pieces = 0, gi = 0, gs = 0;  // gi: steps so far; gs: scores so far
+            Place<kKeys> ka, kd;                  // the key tile of the next scores, of the next dQ
+            Place<kVals> va;
+            auto scores = [&](bool last) {
+                wait(&k_full[ka.s], ka.parity);
+                if (!ok) return;
+                mma_rows<D>(s_addr(gs), qb, k_addr(ka.s));
+                mma_commit(&s_full[gs & 1u]);
+                if (last) mma_commit(&q_empty);
+                ka.step();
+                ++gs;
+            };
+            auto dps = [&](bool last) {
+                if (!ok) return;
+                mma_rows<D>(dp_t, dob, v_addr(va.s));
                 mma_commit(&dp_full);
-                mma_commit(&v_empty[i % kVals]);
-            }
-        };
-        if (steps > 0 && wait(&q_full, 0)) {
-            scores(0);
-            if (ok && wait(&do_full, 0)) dps(0);
-            if (ok && steps > 1) scores(1);
-            for (uint32_t i = 0; i < (uint32_t)steps && ok; ++i) {
-                if (!wait(&ds_full, i & 1u)) break;
-                if (lane == 0) {
-                    const uint32_t kb = smem_u32(k_tile(i));
-#pragma unroll
-                    for (int ks = 0; ks < kTile / 16; ++ks)
-                        mma_f16_ts(dq_t, s_addr(i) + (ks >> 2) * 64u + (ks & 3) * 8u, desc_mn(kb, ks), instr_desc(D, true), (i | ks) ? 1u : 0u);
-                    mma_commit(&k_empty[i % kKeys]);
+                mma_commit(&v_empty[va.s]);
+                if (last) mma_commit(&do_empty);
+                va.step();
+            };
+            int block = (int)blockIdx.x;
+            for (uint32_t k = 0; block >= 0 && ok; ++k) {
+                const DqWork x(a, block);
+                if (x.steps > 0) {
+                    wait(&q_full, pieces & 1u);
+                    scores(x.steps == 1);
+                    wait(&do_full, pieces & 1u);
+                    wait(&v_full[va.s], va.parity);
+                    dps(x.steps == 1);
+                    if (x.steps > 1) scores(x.steps == 2);
+                    if (pieces > 0) wait(&acc_empty, (pieces - 1u) & 1u);
                 }
-                if (i + 1 < (uint32_t)steps) dps(i + 1);
-                if (ok && i + 2 < (uint32_t)steps) scores(i + 2);
+                for (int i = 0; i < x.steps && ok; ++i, ++gi) {
+                    if (i + 1 < x.steps) wait(&v_full[va.s], va.parity);
+                    wait(&ds_full, gi & 1u);  // dP has been read, dS is there
+                    if (i + 1 < x.steps) dps(i + 2 == x.steps);
+                    if (!ok) break;
+                    mma_sum<D>(dq_t, s_addr(gi), 64u, k_addr(kd.s), (uint32_t)i);
+                    if (i + 1 == x.steps) mma_commit(&acc_full);
+                    mma_commit(&k_empty[kd.s]);
+                    kd.step();
+                    if (i + 2 < x.steps) scores(i + 3 == x.steps);
+                }
+                if (x.steps > 0) ++pieces;
+                if (ok) block = work_next_one(&queue, k, abortp);
             }
+            mma_commit(&all_done);
+            wait_drained(&all_done, abortp);
         }
         __syncwarp();
-        if (lane == 0) {
-            mma_commit(&all_done);
-            const unsigned long long t0 = global_timer_ns();
-            while (!mbar_try_wait(&all_done, 0))
-                if (global_timer_ns() - t0 > kWaitLimitNs) {
-                    *abortp = 1;
-                    break;
-                }
-        }
-    } else {
+    } else if (warp < 8) {
         // ------------------------------------ probabilities, dS -------------------------------------------
+        take_registers();
         const int half = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t mine = lanes + (uint32_t)half * 64u;
-        const int pos = t * kTile + row;
-        const bool live = pos >= lo && pos < hi;
-        const int see = max(lo, pos - g.window + 1);
-        const unsigned count = live ? (unsigned)(pos + 1 - see) : 0u;
-        int full_from = 1 << 30, full_to = 0;  // key tiles that every row of the tile sees whole
-        if (t * kTile >= lo && t * kTile + kTile <= hi) {
-            full_from = (max(lo, t * kTile + kTile - g.window) + kTile - 1) / kTile;
-            full_to = t;
-        }
-        const size_t at = (((size_t)n * g.heads + h) * a.tiles + t) * kTile + row;
-        const float shift = a.shift[at], ndelta = a.ndelta[at];
-        const float c = a.scale_log2;
-        const uint64_t c2 = f32x2(c, c), shift2 = f32x2(shift, shift), ndelta2 = f32x2(ndelta, ndelta);
+        const uint64_t c2 = f32x2(a.scale_log2, a.scale_log2);
         bool ok = true;
         auto wait = [&](uint64_t* bar, uint32_t parity) {
-            ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abortp));
+            ok = ok && wait_all(bar, parity, abortp);
             tc_fence_after();
             return ok;
         };
-        for (int i = 0; i < steps; ++i) {
-            const int j = from + i;
-            float p[64];
-            if (!wait(&s_full[i & 1], (i >> 1) & 1)) break;
-            {
-                uint32_t s[2][32];
-                tmem_ld32(s_addr(i) + mine, s[0]);
-                tmem_ld32(s_addr(i) + mine + 32u, s[1]);
-                tmem_ld_wait();
-#pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                    const uint32_t* x = &s[k >> 4][(k & 15) * 2];
-                    f32x2_split(f32x2_fma(f32x2(__uint_as_float(x[0]), __uint_as_float(x[1])), c2, shift2), p[2 * k], p[2 * k + 1]);
-                }
+        auto tell = [&](uint64_t* bar) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+        };
+        uint32_t gi = 0, pieces = 0;
+        int block = (int)blockIdx.x;
+        for (uint32_t k = 0; block >= 0; ++k) {
+            const DqWork x(a, block);
+            const int pos = x.t * kTile + row;
+            const bool live = pos >= x.lo && pos < x.hi;
+            const int see = max(x.lo, pos - g.window + 1);
+            const unsigned count = live ? (unsigned)(pos + 1 - see) : 0u;
+            int full_from = 1 << 30, full_to = 0;  // key tiles that every row of the tile sees whole
+            if (x.t * kTile >= x.lo && x.t * kTile + kTile <= x.hi) {
+                full_from = (max(x.lo, x.t * kTile + kTile - g.window) + kTile - 1) / kTile;
+                full_to = x.t;
             }
-#pragma unroll
-            for (int k = 0; k < 64; ++k) p[k] = ex2_approx(p[k]);
-            if (j < full_from || j >= full_to) {
-                const int first = j * kTile + half * 64 - see;
-#pragma unroll
-                for (int k = 0; k < 64; ++k)
-                    if ((unsigned)(first + k) >= count) p[k] = 0.f;
-            }
-            if (!wait(&dp_full, i & 1)) break;
-            {
+            const size_t at = (((size_t)x.n * g.heads + x.h) * a.tiles + x.t) * kTile + row;
+            const float shift = a.shift[at], ndelta = a.ndelta[at];
+            const uint64_t shift2 = f32x2(shift, shift), ndelta2 = f32x2(ndelta, ndelta);
+            for (int i = 0; i < x.steps; ++i, ++gi) {
+                const int j = x.from + i;
+                float p[64];
                 uint32_t s[2][32], b[32];
+                if (!wait(&s_full[gi & 1u], (gi >> 1) & 1u)) break;
+                tmem_ld32(s_addr(gi) + mine, s[0]);
+                tmem_ld32(s_addr(gi) + mine + 32u, s[1]);
+                tmem_ld_wait();
+                probabilities(s, c2, [&](int) { return shift2; }, p);
+                if (j < full_from || j >= full_to) {
+                    const int first = j * kTile + half * 64 - see;
+#pragma unroll
+                    for (int e = 0; e < 64; ++e)
+                        if ((unsigned)(first + e) >= count) p[e] = 0.f;
+                }
+                if (!wait(&dp_full, gi & 1u)) break;
                 tmem_ld32(dp_t + mine, s[0]);
                 tmem_ld32(dp_t + mine + 32u, s[1]);
                 tmem_ld_wait();
-#pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                    const uint32_t* x = &s[k >> 4][(k & 15) * 2];
-                    float e, f;
-                    f32x2_split(f32x2_mul(f32x2(p[2 * k], p[2 * k + 1]), f32x2_add(f32x2(__uint_as_float(x[0]), __uint_as_float(x[1])), ndelta2)), e, f);
-                    b[k] = pack_bf16x2(e, f);
-                }
-                tmem_st32(s_addr(i) + mine, b);
+                score_grads(s, p, [&](int) { return ndelta2; }, b);
+                tmem_st32(s_addr(gi) + mine, b);
+                tmem_st_wait();
+                tell(&ds_full);
             }
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&ds_full);
-        }
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&all_done, 0, abortp));
-        tc_fence_after();
-        if (ok) {  // each half writes half of the columns
-#pragma unroll 1
-            for (int i = half * (D / 64); i < (half + 1) * (D / 64); ++i) {
-                float f[32];
-                if (steps > 0) {
-                    uint32_t o[32];
-                    tmem_ld32(dq_t + lanes + 32u * i, o);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) f[k] = live ? __uint_as_float(o[k]) * a.scale : 0.f;
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) f[k] = 0.f;
-                }
-                stage_row32(q_tile, row, i, f);
+            if (ok && x.steps > 0) wait(&acc_full, pieces & 1u);
+            if (!ok) break;
+            // each half writes half of the columns
+            const int64_t r = (int64_t)x.n * g.seq_len + pos;
+            write_row(dq_t + lanes, half * (D / 64), (half + 1) * (D / 64), x.steps > 0, live, a.scale, a.dq + r * a.ld_dq + x.h * g.head_dim,
+                      g.head_dim, a.wide_dq, pos < g.seq_len);
+            if (x.steps > 0) {
+                tell(&acc_empty);
+                ++pieces;
             }
-            fence_proxy_async_smem();
-        }
-        named_barrier(1, 256);
-        if (tid == 0 && !*abortp) {
-            store_tile<D>(&mdq, q_tile, g.head_dim, h, t * kTile, n);
-            bulk_commit();
-            bulk_wait_all<0>();
+            block = work_next(&queue, k, lane, abortp);
         }
     }
     tc_fence_before();
@@ -630,7 +832,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
 // ---- host -------------------------------------------------------------------------------------------------------
 
 struct Maps {
-    CUtensorMap q, k, v, dout, dq, dk, dv;
+    CUtensorMap q, k, v, dout;
 };
 
 template <int D>
@@ -639,8 +841,8 @@ cudaError_t launch_bwd(const Maps& m, const BwdArgs& a, cudaStream_t st) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_dq_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)DqCfg<D>::kSmem);
     if (e != cudaSuccess) return e;
     const unsigned nk = (unsigned)(a.g.n_seq * a.g.kv_heads), nh = (unsigned)(a.g.n_seq * a.g.heads);
-    attn_dkv_kernel<D><<<nk * (unsigned)a.tiles, kThreads, DkvCfg<D>::kSmem, st>>>(m.q, m.k, m.v, m.dout, m.dk, m.dv, a);
-    attn_dq_kernel<D><<<nh * (unsigned)a.tiles, kThreads, DqCfg<D>::kSmem, st>>>(m.q, m.k, m.v, m.dout, m.dq, a);
+    attn_dkv_kernel<D><<<nk * (unsigned)a.tiles, kThreads, DkvCfg<D>::kSmem, st>>>(m.q, m.k, m.v, m.dout, a);
+    attn_dq_kernel<D><<<nh * (unsigned)a.tiles, kThreads, DqCfg<D>::kSmem, st>>>(m.q, m.k, m.v, m.dout, a);
     return cudaGetLastError();
 }
 
@@ -707,9 +909,7 @@ extern "C" rapid_status_t rapid_attention_bwd(const rapid_attn_desc_t* desc, con
     if ((s = policy::check_device(&sms)) != RAPID_OK) return s;
     Maps m;
     if (!make_head_map(&m.q, q, d, d.n_heads, d.ld_q) || !make_head_map(&m.k, k, d, d.n_kv_heads, d.ld_k) ||
-        !make_head_map(&m.v, v, d, d.n_kv_heads, d.ld_v) || !make_head_map(&m.dout, dout, d, d.n_heads, d.ld_dout) ||
-        !make_head_map(&m.dq, dq, d, d.n_heads, d.ld_dq) || !make_head_map(&m.dk, dk, d, d.n_kv_heads, d.ld_dk) ||
-        !make_head_map(&m.dv, dv, d, d.n_kv_heads, d.ld_dv))
+        !make_head_map(&m.v, v, d, d.n_kv_heads, d.ld_v) || !make_head_map(&m.dout, dout, d, d.n_heads, d.ld_dout))
         return RAPID_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (policy::clear_stats(stats, st) != cudaSuccess) return RAPID_ERR_CUDA;
@@ -722,6 +922,15 @@ extern "C" rapid_status_t rapid_attention_bwd(const rapid_attn_desc_t* desc, con
     a.tiles = (d.seq_len + kTile - 1) / kTile;
     a.shift = shift;
     a.ndelta = ndelta;
+    a.dq = static_cast<uint16_t*>(dq);
+    a.dk = static_cast<uint16_t*>(dk);
+    a.dv = static_cast<uint16_t*>(dv);
+    a.ld_dq = d.ld_dq;
+    a.ld_dk = d.ld_dk;
+    a.ld_dv = d.ld_dv;
+    a.wide_dq = wide_rows(dq, d.ld_dq, d.head_dim);
+    a.wide_dk = wide_rows(dk, d.ld_dk, d.head_dim);
+    a.wide_dv = wide_rows(dv, d.ld_dv, d.head_dim);
     a.stats = stats;
     int lanes_log2 = 0;
     while ((8 << lanes_log2) < d.head_dim) ++lanes_log2;

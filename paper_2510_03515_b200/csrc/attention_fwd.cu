@@ -1,15 +1,15 @@
 // Causal attention, forward (tcgen05).
 //
-// A block takes two work items of one key head: an item is (query tile of 128 positions, query head of the group), items
+// A piece of work is two items of one key head: an item is (query tile of 128 positions, query head of the group), items
 // are numbered tile by tile, so the two usually share the tile and always the keys.  Warps 0-3 and 4-7 each run the
 // softmax of one item, a thread to a row, so row maximum and sum need no exchange; warp 8 issues the copies, warp 9 the
 // products:
-//     S_w = Q_w K_j^T into tensor memory -> softmax reads it, writes P_w (bf16) over it -> O_w += P_w V_j
-// P is the left operand straight from tensor memory, O stays there to the end.  While the softmax of one item works, the
-// tensor cores have the other item's products, so neither waits long.  O is rescaled only when a row's maximum has grown
-// by more than 2^8 since the last time (exponentials up to 2^8 are as exact in float and bf16 as those below 1), and the
-// warp that finds this does it itself: the barrier that says "S of this tile is there" also says that every earlier
-// product has ended.
+//     S_w = Q_w K_j^T into tensor memory -> softmax writes P_w (bf16) to tensor memory -> O_w += P_w V_j
+// P is the left operand straight from tensor memory, O stays there to the end.  At D = 128 P lies over S (tensor memory is
+// full): while the softmax of one item works, the tensor cores have the other item's products.  At D = 64 P has columns
+// of its own and the next S is formed as soon as the softmax has taken the last one into registers.  O is rescaled only
+// when a row's maximum has grown by more than 2^8 since the last time (exponentials up to 2^8 are as exact in float and
+// bf16 as those below 1), and the warp that finds this does it itself.
 #include <math.h>
 
 #include "attention.cuh"
@@ -18,72 +18,93 @@ namespace rapid {
 namespace attn {
 namespace {
 
-constexpr int kThreads = 320;
-
 struct FwdArgs {
     Geometry g;
     float scale_log2;  // scale * log2(e)
+    uint16_t* out;
+    int64_t ld_out;
+    bool wide;  // see store_row32
     float* lse;
     rapid_stats_t* stats;
-    int items, pairs;  // work items of a key head; blocks for them
+    int items, pairs;  // work items of a key head; pieces of work for them
 };
 
 template <int D>
 struct FwdCfg {
-    static constexpr int kStages = D == 128 ? 4 : 8;  // tiles of keys and values in flight
+    static constexpr uint32_t kStages = D == 128 ? 5 : 8;  // tiles in flight, keys and values alternating
+    static constexpr bool kOverlay = D == 128;        // P over S
+    static constexpr int kPoly = 4;                   // of 16 pairs of exponentials, those formed by polynomial
     static constexpr size_t kSmem = (size_t)(2 + kStages) * tile_bytes<D>() + 1024;
+};
+
+struct FwdWork {
+    int n, hk, lo, hi, jlo, jhi;
+    int t[2], h[2], from[2], to[2];
+    bool valid[2];
+
+    __device__ __forceinline__ FwdWork(const FwdArgs& a, int block) {
+        const Geometry& g = a.g;
+        // the longest rows first
+        const int pair = a.pairs - 1 - (int)((unsigned)block / (unsigned)(g.n_seq * g.kv_heads));
+        const int nk = (int)((unsigned)block % (unsigned)(g.n_seq * g.kv_heads));
+        n = nk / g.kv_heads;
+        hk = nk - n * g.kv_heads;
+        live_range(g, n, lo, hi);
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const int item = min(2 * pair + w, a.items - 1);
+            valid[w] = 2 * pair + w < a.items;
+            t[w] = item / g.group;
+            h[w] = hk * g.group + item - t[w] * g.group;
+            key_tiles(g, t[w], lo, hi, from[w], to[w]);
+            if (!valid[w]) from[w] = to[w] = 0;
+        }
+        // the tiles of either item: a contiguous range
+        jlo = jhi = 0;
+        if (to[0] > from[0]) jlo = from[0], jhi = to[0];
+        if (to[1] > from[1]) {
+            jlo = jhi > jlo ? min(jlo, from[1]) : from[1];
+            jhi = max(jhi, to[1]);
+        }
+    }
 };
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
-                const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mo, FwdArgs a) {
-    constexpr int kStages = FwdCfg<D>::kStages;
+                const __grid_constant__ CUtensorMap mv, const __grid_constant__ FwdArgs a) {
+    constexpr uint32_t kStages = FwdCfg<D>::kStages;
+    constexpr bool kOverlay = FwdCfg<D>::kOverlay;
     constexpr int TB = tile_bytes<D>();
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    __shared__ __align__(8) uint64_t q_full[2], s_full[2], p_full[2], o_full[2], kv_full[kStages], kv_empty[kStages], drain;
+    // [w]: of an item.  q_full, q_empty, o_empty count the items with keys; s_*, p_full, o_full count tiles.
+    __shared__ __align__(8) uint64_t q_full[2], q_empty[2], s_full[2], s_empty[2], p_full[2], o_full[2], o_empty[2],
+        kv_full[kStages], kv_empty[kStages], kv_raw[kStages], drain;
+    __shared__ WorkQueue queue;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     volatile int* abortp = &abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const Geometry& g = a.g;
 
-    // the longest rows first
-    const int pair = a.pairs - 1 - (int)(blockIdx.x / (unsigned)(g.n_seq * g.kv_heads));
-    const int nk = (int)(blockIdx.x % (unsigned)(g.n_seq * g.kv_heads));
-    const int n = nk / g.kv_heads, hk = nk - n * g.kv_heads;
-    int lo, hi;
-    live_range(g, n, lo, hi);
-    int t[2], h[2], from[2], to[2];
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        const int item = min(2 * pair + w, a.items - 1);
-        t[w] = item / g.group;
-        h[w] = hk * g.group + item - t[w] * g.group;
-        key_tiles(g, t[w], lo, hi, from[w], to[w]);
-        if (2 * pair + w >= a.items) from[w] = to[w] = 0;
-    }
-    // tiles of either item, a contiguous range
-    int jlo = 0, jhi = 0;
-    if (to[0] > from[0]) jlo = from[0], jhi = to[0];
-    if (to[1] > from[1]) {
-        jlo = jhi > jlo ? min(jlo, from[1]) : from[1];
-        jhi = max(jhi, to[1]);
-    }
-
     if (tid == 0) {
         for (int w = 0; w < 2; ++w) {
             mbar_init(&q_full[w], 1);
+            mbar_init(&q_empty[w], 1);
             mbar_init(&s_full[w], 1);
+            mbar_init(&s_empty[w], 4);
             mbar_init(&p_full[w], 4);
             mbar_init(&o_full[w], 1);
+            mbar_init(&o_empty[w], 4);
         }
-        for (int s = 0; s < kStages; ++s) {
+        for (uint32_t s = 0; s < kStages; ++s) {
             mbar_init(&kv_full[s], 1);
             mbar_init(&kv_empty[s], 1);
+            mbar_init(&kv_raw[s], 1);
         }
         mbar_init(&drain, 1);
+        work_init(&queue, 10);
         abort_flag = 0;
         mbar_init_fence();
     }
@@ -94,193 +115,264 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
     auto s_addr = [&](int w) { return tmem + (uint32_t)w * 128u; };
     auto o_addr = [&](int w) { return tmem + 256u + (uint32_t)w * D; };
-    auto kv_tile = [&](uint32_t it) { return smem + (size_t)(2 + it % kStages) * TB; };
+    auto p_addr = [&](int w) { return kOverlay ? s_addr(w) : tmem + 384u + (uint32_t)w * 64u; };
+    const uint32_t smem0 = smem_u32(smem);
+    auto kv_tile = [&](uint32_t s) { return smem + (size_t)(2 + s) * TB; };
+    auto kv_addr = [&](uint32_t s) { return smem0 + (2u + s) * (uint32_t)TB; };
 
+    if (warp >= 8) leave_registers();
     if (warp == 8) {
         // ------------------------------------ copies ------------------------------------------------------
         if (lane == 0) {
-#pragma unroll
-            for (int w = 0; w < 2; ++w)
-                if (to[w] > from[w]) {
-                    mbar_arrive_expect_tx(&q_full[w], TB);
-                    load_tile<D>(smem + (size_t)w * TB, &mq, h[w], t[w] * kTile, n, &q_full[w]);
-                }
-            uint32_t it = 0;
+            uint32_t it = 0, nq[2] = {0, 0}, k = 0, was_raw = 0;
+            RawParity raw;
+            Place<kStages> at;
             bool ok = true;
-            for (int j = jlo; j < jhi && ok; ++j)
-                for (int half = 0; half < 2; ++half, ++it) {
-                    const int s = it % kStages;
-                    const uint32_t use = it / kStages;
-                    if (use > 0 && !mbar_wait_bounded(&kv_empty[s], (use & 1u) ^ 1u, abortp)) {
-                        ok = false;
-                        break;
-                    }
-                    mbar_arrive_expect_tx(&kv_full[s], TB);
-                    load_tile<D>(kv_tile(it), half ? &mv : &mk, hk, j * kTile, n, &kv_full[s]);
-                }
-            if (!ok || *abortp) {  // gave up: let the copies land before the block's memory goes away
+            int block = (int)blockIdx.x;
+            while (block >= 0) {
+                const FwdWork x(a, block);
 #pragma unroll
                 for (int w = 0; w < 2; ++w)
-                    if (to[w] > from[w]) {
-                        const unsigned long long t0 = global_timer_ns();
-                        while (!mbar_try_wait(&q_full[w], 0))
-                            if (global_timer_ns() - t0 > kWaitLimitNs) break;
+                    if (ok && x.to[w] > x.from[w]) {
+                        if (nq[w] > 0) ok = wait_one(&q_empty[w], (nq[w] - 1u) & 1u, abortp);
+                        if (ok) {
+                            mbar_arrive_expect_tx(&q_full[w], TB);
+                            load_tile<D>(smem + (size_t)w * TB, &mq, x.h[w], x.t[w] * kTile, x.n, &q_full[w]);
+                            ++nq[w];
+                        }
                     }
-                for (uint32_t i = it > (uint32_t)kStages ? it - kStages : 0u; i < it; ++i) {
-                    const unsigned long long t0 = global_timer_ns();
-                    while (!mbar_try_wait(&kv_full[i % kStages], (i / kStages) & 1u))
-                        if (global_timer_ns() - t0 > kWaitLimitNs) break;
-                }
+                for (int j = x.jlo; j < x.jhi && ok; ++j)
+                    for (int half = 0; half < 2; ++half) {
+                        if (it >= kStages && !(ok = wait_one(&kv_empty[at.s], at.parity ^ 1u, abortp))) break;
+                        // dead keys are masked in the scores; dead values have to be zero
+                        const bool clean = half && dirty(j, x.lo, x.hi);
+                        uint64_t* bar = clean ? &kv_raw[at.s] : &kv_full[at.s];
+                        was_raw = clean ? was_raw | (1u << at.s) : was_raw & ~(1u << at.s);
+                        if (clean) raw.flip(at.s);
+                        mbar_arrive_expect_tx(bar, TB);
+                        load_tile<D>(kv_tile(at.s), half ? &mv : &mk, x.hk, j * kTile, x.n, bar);
+                        ++it;
+                        at.step();
+                    }
+                if (!ok || !(ok = work_ask(&queue, k, abortp))) break;
+                ++k;
+                if (!(ok = mbar_wait_bounded(&queue.full[(k - 1u) & 1u], ((k - 1u) >> 1) & 1u, abortp))) break;
+                block = work_read(&queue, k - 1u);
+                fence_proxy_async_smem();
             }
+            if (!ok || *abortp) {  // gave up: what is under way lands before the block's memory goes away
+#pragma unroll
+                for (int w = 0; w < 2; ++w)
+                    if (nq[w] > 0) wait_landed(&q_full[w], (nq[w] - 1u) & 1u);
+                for (uint32_t s = 0; s < kStages && s < it; ++s) {
+                    const bool now = s < at.s;  // this buffer's last use belongs to the current turn, or to the one before
+                    if ((was_raw >> s) & 1u) wait_landed(&kv_raw[s], ((raw.bits >> s) & 1u) ^ 1u);
+                    else wait_landed(&kv_full[s], now ? at.parity : at.parity ^ 1u);
+                }
+                if (k > 0) wait_landed(&queue.full[(k - 1u) & 1u], ((k - 1u) >> 1) & 1u);
+            }
+        }
+    } else if (warp == 10) {
+        // ------------------------------------ dead rows ---------------------------------------------------
+        RawParity raw;
+        Place<kStages> at;
+        bool ok = true;
+        int block = (int)blockIdx.x;
+        for (uint32_t k = 0; block >= 0 && ok; ++k) {
+            const FwdWork x(a, block);
+            for (int j = x.jlo; j < x.jhi && ok; ++j) {
+                at.step();  // past the keys
+                if (dirty(j, x.lo, x.hi)) {
+                    ok = wait_all(&kv_raw[at.s], raw.flip(at.s), abortp);
+                    if (ok) zero_rows_outside<D>(kv_tile(at.s), j * kTile, x.lo, x.hi, lane);
+                    if (ok && lane == 0) mbar_arrive(&kv_full[at.s]);
+                }
+                at.step();
+            }
+            if (ok) block = work_next(&queue, k, lane, abortp);
         }
     } else if (warp == 9) {
         // ------------------------------------ products ----------------------------------------------------
-        // All lanes walk the loop (they clear dead rows together); lane 0 issues.
-        bool ok = true;
-        uint32_t done[2] = {0, 0};  // tiles of P consumed
-        auto wait = [&](uint64_t* bar, uint32_t parity) {
-            ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abortp));
-            return ok;
-        };
-        for (int j = jlo; j <= jhi && jlo < jhi && ok; ++j) {
-            const uint32_t itk = 2u * (uint32_t)(j - jlo), itv = itk - 1u;  // ring numbers of K_j and V_{j-1}
-            if (j < jhi && !wait(&kv_full[itk % kStages], (itk / kStages) & 1u)) break;
-            if (j > jlo) {
-                if (!wait(&kv_full[itv % kStages], (itv / kStages) & 1u)) break;
-                zero_rows_outside<D>(kv_tile(itv), (j - 1) * kTile, lo, hi, lane);
-            }
-            tc_fence_after();
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                if (j - 1 >= from[w] && j - 1 < to[w]) {
-                    if (!wait(&p_full[w], done[w] & 1u)) break;
-                    tc_fence_after();
-                    if (lane == 0) {
-                        const uint32_t v = smem_u32(kv_tile(itv));
-#pragma unroll
-                        for (int ks = 0; ks < kTile / 16; ++ks)
-                            mma_f16_ts(o_addr(w), s_addr(w) + 8u * ks, desc_mn(v, ks), instr_desc(D, true), (done[w] | ks) ? 1u : 0u);
-                        mma_commit(&o_full[w]);
-                    }
-                    ++done[w];
-                }
-                if (j >= from[w] && j < to[w]) {
-                    if (j == from[w] && !wait(&q_full[w], 0)) break;
-                    tc_fence_after();
-                    if (lane == 0) {
-                        mma_ss<D>(s_addr(w), smem_u32(smem + (size_t)w * TB), smem_u32(kv_tile(itk)));
+        if (elect_one()) {
+            bool ok = true;
+            uint32_t nq[2] = {0, 0}, ns[2] = {0, 0}, np[2] = {0, 0};  // items; tiles of S, of P
+            Place<kStages> ka, va;  // the next tile of keys, of values
+            va.step();
+            auto wait = [&](uint64_t* bar, uint32_t parity) {
+                ok = wait_one(bar, parity, abortp);
+                tc_fence_after();
+                return ok;
+            };
+            int block = (int)blockIdx.x;
+            for (uint32_t k = 0; block >= 0 && ok; ++k) {
+                const FwdWork x(a, block);
+                for (int j = x.jlo; j <= x.jhi && x.jlo < x.jhi && ok; ++j) {
+                    auto scores = [&](int w) {  // S_w of tile j
+                        if (!ok || j < x.from[w] || j >= x.to[w]) return;
+                        if (j == x.from[w] && !wait(&q_full[w], nq[w] & 1u)) return;
+                        if (!kOverlay && ns[w] > 0 && !wait(&s_empty[w], (ns[w] - 1u) & 1u)) return;
+                        mma_rows<D>(s_addr(w), smem0 + (uint32_t)w * TB, kv_addr(ka.s));
                         mma_commit(&s_full[w]);
+                        if (j == x.to[w] - 1) mma_commit(&q_empty[w]);
+                        ++ns[w];
+                    };
+                    auto values = [&](int w) {  // O_w += P_w V of tile j - 1
+                        if (!ok || j - 1 < x.from[w] || j - 1 >= x.to[w]) return;
+                        if (j - 1 == x.from[w] && nq[w] > 0 && !wait(&o_empty[w], (nq[w] - 1u) & 1u)) return;
+                        if (!wait(&p_full[w], np[w] & 1u)) return;
+                        mma_sum<D>(o_addr(w), p_addr(w), 32u, kv_addr(va.s), j - 1 > x.from[w] ? 1u : 0u);
+                        mma_commit(&o_full[w]);
+                        ++np[w];
+                        if (j == x.to[w]) ++nq[w];
+                    };
+                    if (j < x.jhi && !wait(&kv_full[ka.s], ka.parity)) break;
+                    if (kOverlay) {
+                        if (j > x.jlo && !wait(&kv_full[va.s], va.parity)) break;
+                        values(0);
+                        scores(0);
+                        values(1);
+                        scores(1);
+                        if (!ok) break;
+                        if (j < x.jhi) mma_commit(&kv_empty[ka.s]);
+                        if (j > x.jlo) mma_commit(&kv_empty[va.s]);
+                    } else {
+                        scores(0);
+                        scores(1);
+                        if (!ok) break;
+                        if (j < x.jhi) mma_commit(&kv_empty[ka.s]);
+                        if (j > x.jlo && !wait(&kv_full[va.s], va.parity)) break;
+                        values(0);
+                        values(1);
+                        if (!ok) break;
+                        if (j > x.jlo) mma_commit(&kv_empty[va.s]);
                     }
+                    if (j < x.jhi) ka.step(2);
+                    if (j > x.jlo) va.step(2);
                 }
+                if (ok) block = work_next_one(&queue, k, abortp);
             }
-            if (!ok) break;
-            if (lane == 0) {
-                if (j < jhi) mma_commit(&kv_empty[itk % kStages]);
-                if (j > jlo) mma_commit(&kv_empty[itv % kStages]);
-            }
-        }
-        if (lane == 0) {  // every product has ended before tensor memory is given back
+            // every product has ended before tensor memory is given back
             mma_commit(&drain);
-            const unsigned long long t0 = global_timer_ns();
-            while (!mbar_try_wait(&drain, 0))
-                if (global_timer_ns() - t0 > kWaitLimitNs) {
-                    *abortp = 1;
-                    break;
-                }
+            wait_drained(&drain, abortp);
         }
-    } else {
+        __syncwarp();
+    } else if (warp < 8) {
         // ------------------------------------ softmax -----------------------------------------------------
+        take_registers();
         const int w = warp >> 2, row = (warp & 3) * 32 + lane;
-        const int tw = w ? t[1] : t[0], hw = w ? h[1] : h[0], fw = w ? from[1] : from[0], ew = w ? to[1] : to[0];
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t st = s_addr(w) + lanes, ot = o_addr(w) + lanes;
-        const int pos = tw * kTile + row;
-        const bool live = pos >= lo && pos < hi && ew > fw;
-        // keys [see, see + count) are visible to this row
-        const int see = max(lo, pos - g.window + 1);
-        const unsigned count = live ? (unsigned)(pos + 1 - see) : 0u;
-        // key tiles in [full_from, full_to) are visible to every row of this tile; the others are masked
-        int full_from = 1 << 30, full_to = 0;
-        if (tw * kTile >= lo && tw * kTile + kTile <= hi) {
-            full_from = (max(lo, tw * kTile + kTile - g.window) + kTile - 1) / kTile;
-            full_to = tw;
-        }
+        const uint32_t st = s_addr(w) + lanes, ot = o_addr(w) + lanes, pt = p_addr(w) + lanes;
         const float c = a.scale_log2;
-        float mref = -INFINITY, sum = 0.f;
+        const uint64_t c2 = f32x2(c, c);
+        uint32_t cnt = 0;  // tiles so far
         bool ok = true;
-        uint32_t it = 0;
-        for (int j = fw; j < ew; ++j, ++it) {
-            ok = __all_sync(0xffffffffu, mbar_wait_bounded(&s_full[w], it & 1u, abortp));
-            if (!ok) break;
-            tc_fence_after();
-            uint32_t s[4][32];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tmem_ld32(st + 32u * i, s[i]);
-            tmem_ld_wait();
-            if (j < full_from || j >= full_to) {
-                const int first = j * kTile - see;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int k = 0; k < 32; ++k)
-                        if ((unsigned)(first + 32 * i + k) >= count) s[i][k] = 0xff800000u;  // -infinity
+        int block = (int)blockIdx.x;
+        for (uint32_t k = 0; block >= 0; ++k) {
+            const FwdWork x(a, block);
+            const int tw = w ? x.t[1] : x.t[0], hw = w ? x.h[1] : x.h[0], fw = w ? x.from[1] : x.from[0], ew = w ? x.to[1] : x.to[0];
+            const int pos = tw * kTile + row;
+            const bool live = pos >= x.lo && pos < x.hi && ew > fw;
+            // keys [see, see + count) are visible to this row
+            const int see = max(x.lo, pos - g.window + 1);
+            const unsigned count = live ? (unsigned)(pos + 1 - see) : 0u;
+            // key tiles in [full_from, full_to) are visible to every row of this tile; the others are masked
+            int full_from = 1 << 30, full_to = 0;
+            if (tw * kTile >= x.lo && tw * kTile + kTile <= x.hi) {
+                full_from = (max(x.lo, tw * kTile + kTile - g.window) + kTile - 1) / kTile;
+                full_to = tw;
             }
-            float top = mref;
+            float mref = -INFINITY, sum = 0.f;
+            for (int j = fw; j < ew && ok; ++j, ++cnt) {
+                ok = wait_all(&s_full[w], cnt & 1u, abortp);
+                if (!ok) break;
+                tc_fence_after();
+                uint32_t s[4][32];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 4; ++i) tmem_ld32(st + 32u * i, s[i]);
+                tmem_ld_wait();
+                if (!kOverlay) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&s_empty[w]);
+                }
+                if (j < full_from || j >= full_to) {
+                    const int first = j * kTile - see;
 #pragma unroll
-                for (int k = 0; k < 32; ++k) top = fmaxf(top, __uint_as_float(s[i][k]));
-            const bool grown = (top - mref) * c > 8.f;  // false where both are -infinity
-            if (__any_sync(0xffffffffu, grown)) {
-                const float alpha = grown ? ex2_approx((mref - top) * c) : 1.f;
-                if (grown) mref = top;
-                sum *= alpha;
-                if (it > 0) {
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if ((unsigned)(first + 32 * i + e) >= count) s[i][e] = 0xff800000u;  // -infinity
+                }
+                float top4[4] = {mref, mref, mref, mref};
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top4[i] = fmaxf(top4[i], __uint_as_float(s[i][e]));
+                const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
+                // with P in columns of its own, the last product may still be reading them
+                if (!kOverlay && j > fw) {
+                    ok = wait_all(&o_full[w], (cnt - 1u) & 1u, abortp);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                const bool grown = (top - mref) * c > 8.f;  // false where both are -infinity
+                if (__any_sync(0xffffffffu, grown)) {
+                    const float alpha = grown ? ex2_approx((mref - top) * c) : 1.f;
+                    if (grown) mref = top;
+                    sum *= alpha;
+                    if (j > fw) {
 #pragma unroll 1
-                    for (int i = 0; i < D / 32; ++i) {
-                        uint32_t o[32];
-                        tmem_ld32(ot + 32u * i, o);
-                        tmem_ld_wait();
+                        for (int i = 0; i < D / 16; ++i) {
+                            uint32_t o[16];
+                            tmem_ld16(ot + 16u * i, o);
+                            tmem_ld_wait();
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
-                        tmem_st32(ot + 32u * i, o);
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                            tmem_st16(ot + 16u * i, o);
+                        }
                     }
                 }
-            }
-            const float shift = mref == -INFINITY ? 0.f : -mref * c;
-            const uint64_t c2 = f32x2(c, c), shift2 = f32x2(shift, shift);
-            uint64_t part = f32x2(0.f, 0.f);
+                const float shift = mref == -INFINITY ? 0.f : -mref * c;
+                const uint64_t shift2 = f32x2(shift, shift);
+                uint64_t part[2] = {f32x2(0.f, 0.f), f32x2(0.f, 0.f)};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t p[16];
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t p[16];
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    float x, y;
-                    f32x2_split(f32x2_fma(f32x2(__uint_as_float(s[i][2 * k]), __uint_as_float(s[i][2 * k + 1])), c2, shift2), x, y);
-                    x = ex2_approx(x);
-                    y = ex2_approx(y);
-                    part = f32x2_add(part, f32x2(x, y));
-                    p[k] = pack_bf16x2(x, y);
+                    for (int e = 0; e < 16; ++e) {
+                        const uint64_t z = f32x2_fma(f32x2(__uint_as_float(s[i][2 * e]), __uint_as_float(s[i][2 * e + 1])), c2, shift2);
+                        float u, v;
+                        if ((e & 3) == 3 && e / 4 < FwdCfg<D>::kPoly) {
+                            exp2_pair_poly(z, u, v);
+                        } else {
+                            f32x2_split(z, u, v);
+                            u = ex2_approx(u);
+                            v = ex2_approx(v);
+                        }
+                        part[e & 1] = f32x2_add(part[e & 1], f32x2(u, v));
+                        p[e] = pack_bf16x2(u, v);
+                    }
+                    tmem_st16(pt + 16u * i, p);
                 }
-                tmem_st16(st + 16u * i, p);
+                float u, v;
+                f32x2_split(f32x2_add(part[0], part[1]), u, v);
+                sum += u + v;
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[w]);
             }
-            float x, y;
-            f32x2_split(part, x, y);
-            sum += x + y;
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&p_full[w]);
-        }
-        // out = O / sum, lse = max + log(sum).  The barrier is passed by all four warps whatever they have seen.
-        if (2 * pair + w < a.items) {
-            if (ew > fw && ok) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&o_full[w], (it - 1u) & 1u, abortp));
-            tc_fence_after();
-            uint8_t* stage = smem + (size_t)w * TB;  // the query tile has been read for the last time
-            if (ok) {
+            // out = O / sum, lse = max + log(sum)
+            if (ok && ew > fw) {
+                ok = wait_all(&o_full[w], (cnt - 1u) & 1u, abortp);
+                tc_fence_after();
+            }
+            if (ok && (w ? x.valid[1] : x.valid[0])) {
+                const bool mine = pos < g.seq_len;
+                uint16_t* dst = a.out + ((int64_t)x.n * g.seq_len + pos) * a.ld_out + hw * g.head_dim;
                 const float inv = live ? 1.f / sum : 0.f;
 #pragma unroll 1
                 for (int i = 0; i < D / 32; ++i) {
@@ -290,24 +382,24 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                         tmem_ld32(ot + 32u * i, o);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) f[k] = live ? __uint_as_float(o[k]) * inv : 0.f;
+                        for (int e = 0; e < 32; ++e) f[e] = live ? __uint_as_float(o[e]) * inv : 0.f;
                     } else {
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) f[k] = 0.f;
+                        for (int e = 0; e < 32; ++e) f[e] = 0.f;
                     }
-                    stage_row32(stage, row, i, f);
+                    if (mine) store_row32(dst, 32 * i, g.head_dim, a.wide, f);
                 }
-                if (a.lse && pos < g.seq_len)
-                    a.lse[((size_t)n * g.heads + hw) * g.seq_len + pos] =
+                if (ew > fw) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&o_empty[w]);
+                }
+                if (a.lse && mine)
+                    a.lse[((size_t)x.n * g.heads + hw) * g.seq_len + pos] =
                         live ? (float)(((double)mref * (double)c + (double)log2f(sum)) * kLn2D) : -INFINITY;
-                fence_proxy_async_smem();
             }
-            named_barrier(1 + w, 128);
-            if ((warp & 3) == 0 && lane == 0 && !*abortp) {
-                store_tile<D>(&mo, stage, g.head_dim, hw, tw * kTile, n);
-                bulk_commit();
-                bulk_wait_all<0>();
-            }
+            if (!ok) break;
+            block = work_next(&queue, k, lane, abortp);
         }
     }
     tc_fence_before();
@@ -320,12 +412,12 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
 }
 
 template <int D>
-cudaError_t launch_fwd(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mo, const FwdArgs& a,
-                       unsigned grid, cudaStream_t st) {
+cudaError_t launch_fwd(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const FwdArgs& a, unsigned grid,
+                       cudaStream_t st) {
     auto kern = attn_fwd_kernel<D>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FwdCfg<D>::kSmem);
     if (e != cudaSuccess) return e;
-    kern<<<grid, kThreads, FwdCfg<D>::kSmem, st>>>(mq, mk, mv, mo, a);
+    kern<<<grid, kThreads, FwdCfg<D>::kSmem, st>>>(mq, mk, mv, a);
     return cudaGetLastError();
 }
 
@@ -384,20 +476,23 @@ extern "C" rapid_status_t rapid_attention_fwd(const rapid_attn_desc_t* desc, con
         return RAPID_ERR_INVALID_ARG;
     int sms = 0;
     if ((s = policy::check_device(&sms)) != RAPID_OK) return s;
-    CUtensorMap mq, mk, mv, mo;
+    CUtensorMap mq, mk, mv;
     if (!make_head_map(&mq, q, d, d.n_heads, d.ld_q) || !make_head_map(&mk, k, d, d.n_kv_heads, d.ld_k) ||
-        !make_head_map(&mv, v, d, d.n_kv_heads, d.ld_v) || !make_head_map(&mo, out, d, d.n_heads, d.ld_out))
+        !make_head_map(&mv, v, d, d.n_kv_heads, d.ld_v))
         return RAPID_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (policy::clear_stats(stats, st) != cudaSuccess) return RAPID_ERR_CUDA;
     FwdArgs a;
     a.g = make_geometry(d, bounds);
     a.scale_log2 = (float)(d.scale * kLog2eD);
+    a.out = static_cast<uint16_t*>(out);
+    a.ld_out = d.ld_out;
+    a.wide = wide_rows(out, d.ld_out, d.head_dim);
     a.lse = lse;
     a.stats = stats;
     a.items = (d.seq_len + kTile - 1) / kTile * a.g.group;
     a.pairs = (a.items + 1) / 2;
     const unsigned grid = (unsigned)((int64_t)a.pairs * d.n_seq * d.n_kv_heads);
-    const cudaError_t e = d.head_dim <= 64 ? launch_fwd<64>(mq, mk, mv, mo, a, grid, st) : launch_fwd<128>(mq, mk, mv, mo, a, grid, st);
+    const cudaError_t e = d.head_dim <= 64 ? launch_fwd<64>(mq, mk, mv, a, grid, st) : launch_fwd<128>(mq, mk, mv, a, grid, st);
     return e == cudaSuccess ? RAPID_OK : RAPID_ERR_CUDA;
 }
