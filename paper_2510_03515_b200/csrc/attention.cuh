@@ -46,6 +46,11 @@ __device__ __forceinline__ void tma_load_4d(void* smem_dst, const CUtensorMap* m
         "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(h), "r"(t), "r"(n)
         : "memory");
 }
+__device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, const void* smem_src, int x, int h, int t, int n) {
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(map),
+                 "r"(smem_u32(smem_src)), "r"(x), "r"(h), "r"(t), "r"(n)
+                 : "memory");
+}
 // True in one lane of a converged warp.  The whole loop that issues products runs inside `if (elect_one())`: the compiler
 // then knows that one lane runs and keeps operands in uniform registers.  Measured for 128 x 64 x 16 (operands in tensor
 // and shared memory): one product takes 33 cycles this way, 67 when the lane is chosen by a predicate.  Products are
@@ -141,14 +146,14 @@ __device__ __forceinline__ void mma_rows(uint32_t d_tmem, uint32_t a_tile, uint3
         mma_ss_1(d_tmem, a + step_k(ks), b + step_k(ks), instr_desc(kTile, false), ks > 0 ? 1u : 0u);
 }
 
-// acc[128 x D] (+)= M[128 x 128] * B[128 x D], M in tensor memory as bf16 (its second 64 columns start `half` 32-bit
-// columns after the first), B a tile used MN-major
+// acc[128 x D] (+)= M[128 x 128] * B[128 x D], M in tensor memory as bf16, 32 of its columns in 16 32-bit columns and the
+// next 32 `stride` columns further on; B a tile used MN-major
 template <int D>
-__device__ __forceinline__ void mma_sum(uint32_t acc, uint32_t m, uint32_t half, uint32_t b_tile, uint32_t more) {
+__device__ __forceinline__ void mma_sum(uint32_t acc, uint32_t m, uint32_t stride, uint32_t b_tile, uint32_t more) {
     const uint32_t b = tile_mn(b_tile);
 #pragma unroll
     for (int ks = 0; ks < kTile / 16; ++ks)
-        mma_ts_1(acc, m + (ks >> 2) * half + (ks & 3) * 8u, b + step_mn(ks), instr_desc(D, true), ks > 0 ? 1u : more);
+        mma_ts_1(acc, m + (ks >> 1) * stride + (ks & 1) * 8u, b + step_mn(ks), instr_desc(D, true), ks > 0 ? 1u : more);
 }
 
 template <int D>
@@ -156,6 +161,13 @@ __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* map, 
 #pragma unroll
     for (int b = 0; b < D / 64; ++b) tma_load_4d(dst + b * kBoxBytes, map, b * 64, h, t0, n, bar);
 }
+template <int D>
+__device__ __forceinline__ void store_tile(const CUtensorMap* map, const uint8_t* src, int head_dim, int h, int t0, int n) {
+#pragma unroll
+    for (int b = 0; b < D / 64; ++b)
+        if (b * 64 < head_dim) tma_store_4d(map, src + b * kBoxBytes, b * 64, h, t0, n);
+}
+
 // Wait for a phase of a barrier, bounded.  The first poll has no suspension hint: a phase that is over already then costs
 // a few tens of cycles.
 __device__ __forceinline__ bool wait_one(uint64_t* bar, uint32_t parity, volatile int* abortp) {
@@ -232,32 +244,45 @@ __device__ __forceinline__ void zero_rows_outside(uint8_t* tile, int t0, int lo,
 // A grid has one block for each piece of work, but a block that is done cancels the launch of a waiting one and does its
 // work instead (clusterlaunchcontrol), until none is left.  Barriers, tensor memory and the copies' descriptors are set up
 // once for each SM, the next piece's loads run under the end of this one, and the pieces still go to whoever is free.
-// One lane asks, when it has issued the last loads of a piece (asking earlier would tie the next piece to a block that is
-// still busy for long: dK, dV of 64 x 1024 took 410 us instead of 325); every role reads the answer.
+// The copying lane asks, when it has issued the last loads of a piece (asking earlier would tie the next piece to a block
+// that is still busy for long: dK, dV of 64 x 1024 took 410 us instead of 325), works out what the piece is and leaves it
+// in shared memory for the other roles, which so never wait for the bounds to come from memory.
+template <class W>  // the piece: plain data, a multiple of 16 bytes, with a member `end`: nothing is left
 struct WorkQueue {
-    __align__(16) uint4 answer[2];
-    __align__(8) uint64_t full[2], empty[2];
+    static_assert(sizeof(W) % 16 == 0, "copied in 16-byte units");
+    uint4 answer;
+    W piece[2];
+    uint64_t answered, full[2], empty[2];
 };
 
-__device__ __forceinline__ void work_init(WorkQueue* q, uint32_t readers) {
+template <class W>
+__device__ __forceinline__ void work_init(WorkQueue<W>* q, uint32_t readers) {
+    mbar_init(&q->answered, 1);
     for (int i = 0; i < 2; ++i) {
         mbar_init(&q->full[i], 1);
         mbar_init(&q->empty[i], readers);
     }
 }
-// Ask for the piece after number k (0, 1, ...).  False: gave up.
-__device__ __forceinline__ bool work_ask(WorkQueue* q, uint32_t k, volatile int* abortp) {
-    const uint32_t s = k & 1u;
-    if (k >= 2 && !mbar_wait_bounded(&q->empty[s], ((k >> 1) & 1u) ^ 1u, abortp)) return false;
-    mbar_arrive_expect_tx(&q->full[s], 16);
-    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
-                     smem_u32(&q->answer[s])),
-                 "r"(smem_u32(&q->full[s]))
-                 : "memory");
+// Publish piece number k (0, 1, ...).  False: gave up.
+template <class W>
+__device__ __forceinline__ bool work_put(WorkQueue<W>* q, uint32_t k, const W& w, volatile int* abortp) {
+    if (k >= 2 && !wait_one(&q->empty[k & 1u], ((k >> 1) & 1u) ^ 1u, abortp)) return false;
+    q->piece[k & 1u] = w;
+    mbar_arrive(&q->full[k & 1u]);
     return true;
 }
-// The answer to the request after piece k: the block number to do next, or -1.
-__device__ __forceinline__ int work_read(WorkQueue* q, uint32_t k) {
+// Ask for another block's work, for the k-th time; its number, -1 where there is none (then do not ask again), -2: gave up.
+template <class W>
+__device__ __forceinline__ int work_ask(WorkQueue<W>* q, uint32_t k, volatile int* abortp) {
+    mbar_arrive_expect_tx(&q->answered, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                     smem_u32(&q->answer)),
+                 "r"(smem_u32(&q->answered))
+                 : "memory");
+    if (!wait_one(&q->answered, k & 1u, abortp)) {
+        wait_landed(&q->answered, k & 1u);  // it must not arrive in a block that has gone
+        return -2;
+    }
     uint32_t x, got;
     asm volatile(
         "{\n\t.reg .pred p;\n\t.reg .b128 r;\n\t"
@@ -267,26 +292,27 @@ __device__ __forceinline__ int work_read(WorkQueue* q, uint32_t k) {
         "mov.u32 %0, 0;\n\t"
         "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, r;\n\t}"
         : "=r"(x), "=r"(got)
-        : "r"(smem_u32(&q->answer[k & 1u]))
+        : "r"(smem_u32(&q->answer))
         : "memory");
+    fence_proxy_async_smem();  // the read comes before the next answer's write
     return got ? (int)x : -1;
 }
-// One lane as a reader: wait, read, give the slot back.  -1 too when the wait gave up.
-__device__ __forceinline__ int work_next_one(WorkQueue* q, uint32_t k, volatile int* abortp) {
-    if (!wait_one(&q->full[k & 1u], (k >> 1) & 1u, abortp)) return -1;
-    const int next = work_read(q, k);
-    fence_proxy_async_smem();  // the read comes before the next answer's write
+// One lane takes piece k.  False when there is none (or the wait gave up).
+template <class W>
+__device__ __forceinline__ bool work_take_one(WorkQueue<W>* q, uint32_t k, W& w, volatile int* abortp) {
+    if (!wait_one(&q->full[k & 1u], (k >> 1) & 1u, abortp)) return false;
+    w = q->piece[k & 1u];
     mbar_arrive(&q->empty[k & 1u]);
-    return next;
+    return !w.end;
 }
 // The same for a whole warp.
-__device__ __forceinline__ int work_next(WorkQueue* q, uint32_t k, int lane, volatile int* abortp) {
-    if (!wait_all(&q->full[k & 1u], (k >> 1) & 1u, abortp)) return -1;
-    const int next = __shfl_sync(0xffffffffu, work_read(q, k), 0);
-    fence_proxy_async_smem();
+template <class W>
+__device__ __forceinline__ bool work_take(WorkQueue<W>* q, uint32_t k, W& w, int lane, volatile int* abortp) {
+    if (!wait_all(&q->full[k & 1u], (k >> 1) & 1u, abortp)) return false;
+    w = q->piece[k & 1u];
     __syncwarp();
     if (lane == 0) mbar_arrive(&q->empty[k & 1u]);
-    return next;
+    return !w.end;
 }
 
 // ---- exponentials -------------------------------------------------------------------------------------------------
@@ -316,33 +342,63 @@ __device__ __forceinline__ void exp2_pair_poly(uint64_t x2, float& lo, float& hi
     hi = __int_as_float(__float_as_int(b) + (__float_as_int(v) << 23));
 }
 
-// ---- results ------------------------------------------------------------------------------------------------------
+// The largest of three (one instruction at the rate of the two-operand form).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 
-// 32 columns [c, c + 32) of a row of `head_dim` bf16 at `row`.  `wide`: rows and heads begin on 32-byte boundaries, so that
-// whole sectors can be written at once.
-__device__ __forceinline__ void store_row32(uint16_t* row, int c, int head_dim, bool wide, const float (&f)[32]) {
+// ---- results ------------------------------------------------------------------------------------------------------
+//
+// A thread holds (part of) a row; written straight to memory, every store of a warp would touch 32 lines, and the 32 KB of a
+// tile kept the load/store unit busy for 2000 cycles.  Results go through shared memory and a tiled store instead; tiles
+// without a live row, which are only zeros, are written directly.
+
+// Row `row` of a tile in shared memory <- 32 values at columns [32 c, 32 c + 32), as bf16, in the layout of the copies.
+__device__ __forceinline__ void stage_row32(uint8_t* tile, int row, int c, const float (&f)[32]) {
+    uint8_t* box = tile + (c >> 1) * kBoxBytes;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        uint32_t w[8];
+    for (int k = 0; k < 4; ++k)
+        *reinterpret_cast<uint4*>(box + umma::swz128(row, (c & 1) * 4 + k)) =
+            make_uint4(pack_bf16x2(f[8 * k], f[8 * k + 1]), pack_bf16x2(f[8 * k + 2], f[8 * k + 3]),
+                       pack_bf16x2(f[8 * k + 4], f[8 * k + 5]), pack_bf16x2(f[8 * k + 6], f[8 * k + 7]));
+}
+// 32 accumulator columns of a row, times `factor`, to the same place (zeros where not `live`).
+__device__ __forceinline__ void stage_acc32(uint8_t* tile, int row, int c, uint32_t taddr, bool live, float factor) {
+    uint32_t o[32];
+    tmem_ld32(taddr, o);
+    tmem_ld_wait();
+    float f[32];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = pack_bf16x2(f[16 * k + 2 * i], f[16 * k + 2 * i + 1]);
-        uint16_t* p = row + c + 16 * k;
-        if (wide && c + 16 * k + 16 <= head_dim) {
-            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-                         "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                         : "memory");
-        } else {
-            if (c + 16 * k + 8 <= head_dim) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-            if (c + 16 * k + 16 <= head_dim) *reinterpret_cast<uint4*>(p + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-        }
+    for (int k = 0; k < 32; ++k) f[k] = live ? __uint_as_float(o[k]) * factor : 0.f;
+    stage_row32(tile, row, c, f);
+}
+// Rows [t0, t0 + 128) of head h of generation n <- zeros, by `threads` threads; head_dim is a multiple of 8.
+__device__ __forceinline__ void zero_tile(uint16_t* out, int64_t ld, int seq_len, int head_dim, int h, int t0, int n, int thread, int threads) {
+    const int per_row = head_dim / 8;
+    for (int i = thread; i < kTile * per_row; i += threads) {
+        const int r = i / per_row, c = i - r * per_row;
+        if (t0 + r < seq_len)
+            *reinterpret_cast<uint4*>(out + ((int64_t)n * seq_len + t0 + r) * ld + h * head_dim + c * 8) = make_uint4(0, 0, 0, 0);
     }
 }
 
-// Registers of the four warps that call it together: the eight warps that hold rows take what the four others leave (both
-// shares add up to the launch's 3 x 168 for each quarter of an SM).
-__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
-__device__ __forceinline__ void leave_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
-constexpr int kThreads = 384;  // warps 0-7: rows; 8: copies; 9: products; 10: dead rows; 11: only its registers are needed
+// Roles of a block's warps: R warps hold rows, then one issues copies, one products, one clears dead rows, and one only gives up
+// its registers.  The row warps take what the four others leave; the shares of a quarter of an SM add up to the launch's.
+template <int R>
+struct Roles {
+    static constexpr int kRow = R, kCopy = R, kMma = R + 1, kClean = R + 2, kThreads = (R + 4) * 32;
+    static __device__ __forceinline__ void take_registers() {
+        if (R == 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");  // 2 x 208 + 88 = 3 x 168
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");         // 4 x 104 + 64 = 5 x 96
+    }
+    static __device__ __forceinline__ void leave_registers() {
+        if (R == 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    }
+    static_assert(R == 8 || R == 16, "the register shares above");
+};
 
 // ---- geometry -----------------------------------------------------------------------------------------------------
 
@@ -375,9 +431,6 @@ __device__ __forceinline__ void key_tiles(const Geometry& g, int t, int lo, int 
 // Argument checks that both directions share, and the kernels' view of a descriptor.
 rapid_status_t check_attn(const rapid_attn_desc_t* d);
 Geometry make_geometry(const rapid_attn_desc_t& d, const int32_t* bounds);
-
-// Whether 32-byte stores to 16-element groups of every row and head are aligned.
-inline bool wide_rows(const void* p, int64_t ld, int head_dim) { return policy::aligned(p, 32) && ld % 16 == 0 && head_dim % 16 == 0; }
 
 // Tensor map of [n_seq][seq_len][heads][head_dim] bf16 with row pitch `ld` elements, boxes of 128 positions x 64 elements.
 bool make_head_map(CUtensorMap* map, const void* base, const rapid_attn_desc_t& d, int heads, int64_t ld);

@@ -10,9 +10,8 @@
 // Scores and dP are thus formed twice: 14 instead of 10 multiply-adds a pair and element, against float atomics on dQ (or
 // its partial sums in memory), which would make results depend on the order of blocks.
 //
-// In both main kernels warps 0-7 hold 64 columns of a row each thread, warp 8 issues copies, warp 9 products.  The order of
-// the products is such that the tensor cores have two of them to work on while the exponentials of one step are formed, and
-// one or two more during its dS.
+// The order of the products is such that the tensor cores have two of them to work on while the exponentials of one step are formed,
+// and one or two more during its dS.
 #include <math.h>
 
 #include "attention.cuh"
@@ -21,6 +20,10 @@ namespace rapid {
 namespace attn {
 namespace {
 
+// Sixteen row warps: a row's 128 columns are split over four threads, 32 columns each, so that every quarter of an SM has four
+// warps whose instructions fill in for one another.  Against eight warps with 64 columns a thread (64 x 1024, 12 heads of
+// 128: 218 and 238 us for the two kernels; 3 x 4095, window 1024, 16 heads of 64: 105 and 87 us) 222, 229, 99 and 77 us.
+using W = Roles<16>;
 constexpr int kVecBytes = kTile * 4;  // one float for each position of a tile
 
 struct BwdArgs {
@@ -31,7 +34,6 @@ struct BwdArgs {
     const float* ndelta;  // the same: -delta
     uint16_t *dq, *dk, *dv;
     int64_t ld_dq, ld_dk, ld_dv;
-    bool wide_dq, wide_dk, wide_dv;  // see store_row32
     rapid_stats_t* stats;
 };
 
@@ -75,90 +77,46 @@ attn_row_terms_kernel(Geometry g, int tiles, int lanes_log2, const uint16_t* __r
     }
 }
 
-// 64 scores of a row (raw, as read from tensor memory) -> exponentials of score * c + shift.  `shift_at(k)`: the pair of
-// shifts of columns 2 k, 2 k + 1.  One pair in four by polynomial (measured against none and against one in two).
+// 32 scores of a row (raw, as read from tensor memory) -> exponentials of score * c + shift.  `shift_at(k)`: the pair of
+// shifts of columns 2 k, 2 k + 1.
 template <class F>
-__device__ __forceinline__ void probabilities(const uint32_t (&s)[2][32], uint64_t c2, F shift_at, float (&p)[64]) {
+__device__ __forceinline__ void probabilities(const uint32_t (&s)[32], uint64_t c2, F shift_at, float (&p)[32]) {
 #pragma unroll
-    for (int k = 0; k < 32; ++k) {
-        const uint32_t* x = &s[k >> 4][(k & 15) * 2];
-        const uint64_t z = f32x2_fma(f32x2(__uint_as_float(x[0]), __uint_as_float(x[1])), c2, shift_at(k));
-        if ((k & 3) == 3) {
-            exp2_pair_poly(z, p[2 * k], p[2 * k + 1]);
-        } else {
-            float u, v;
-            f32x2_split(z, u, v);
-            p[2 * k] = ex2_approx(u);
-            p[2 * k + 1] = ex2_approx(v);
-        }
+    for (int k = 0; k < 16; ++k) {
+        const uint64_t z = f32x2_fma(f32x2(__uint_as_float(s[2 * k]), __uint_as_float(s[2 * k + 1])), c2, shift_at(k));
+        float u, v;
+        f32x2_split(z, u, v);
+        p[2 * k] = ex2_approx(u);
+        p[2 * k + 1] = ex2_approx(v);
     }
 }
-__device__ __forceinline__ void round_pairs(const float (&p)[64], uint32_t (&b)[32]) {
+__device__ __forceinline__ void round_pairs(const float (&p)[32], uint32_t (&b)[16]) {
 #pragma unroll
-    for (int k = 0; k < 32; ++k) b[k] = pack_bf16x2(p[2 * k], p[2 * k + 1]);
+    for (int k = 0; k < 16; ++k) b[k] = pack_bf16x2(p[2 * k], p[2 * k + 1]);
 }
 // p * (dp - delta) as bf16
 template <class F>
-__device__ __forceinline__ void score_grads(const uint32_t (&s)[2][32], const float (&p)[64], F ndelta_at, uint32_t (&b)[32]) {
+__device__ __forceinline__ void score_grads(const uint32_t (&s)[32], const float (&p)[32], F ndelta_at, uint32_t (&b)[16]) {
 #pragma unroll
-    for (int k = 0; k < 32; ++k) {
-        const uint32_t* x = &s[k >> 4][(k & 15) * 2];
+    for (int k = 0; k < 16; ++k) {
         float u, v;
-        f32x2_split(f32x2_mul(f32x2(p[2 * k], p[2 * k + 1]), f32x2_add(f32x2(__uint_as_float(x[0]), __uint_as_float(x[1])), ndelta_at(k))), u, v);
+        f32x2_split(f32x2_mul(f32x2(p[2 * k], p[2 * k + 1]),
+                              f32x2_add(f32x2(__uint_as_float(s[2 * k]), __uint_as_float(s[2 * k + 1])), ndelta_at(k))), u, v);
         b[k] = pack_bf16x2(u, v);
-    }
-}
-
-// One lane's `D / 32` chunks [from, to) of an accumulator row, times `factor`, to memory (zeros where not `live`).
-__device__ __forceinline__ void write_row(uint32_t acc, int from, int to, bool any, bool live, float factor, uint16_t* dst, int head_dim,
-                                          bool wide, bool mine) {
-#pragma unroll 1
-    for (int i = from; i < to; ++i) {
-        float f[32];
-        if (any) {
-            uint32_t o[32];
-            tmem_ld32(acc + 32u * i, o);
-            tmem_ld_wait();
-#pragma unroll
-            for (int k = 0; k < 32; ++k) f[k] = live ? __uint_as_float(o[k]) * factor : 0.f;
-        } else {
-#pragma unroll
-            for (int k = 0; k < 32; ++k) f[k] = 0.f;
-        }
-        if (mine) store_row32(dst, 32 * i, head_dim, wide, f);
     }
 }
 
 // ---- dK, dV -----------------------------------------------------------------------------------------------------
 
-template <int D>
-struct DkvCfg {
-    static constexpr uint32_t kQ = D == 128 ? 3 : 4, kDo = D == 128 ? 2 : 4;  // tiles of q (needed the longest) and of dout in flight
-    static constexpr uint32_t kVec = 2;                                       // row terms of query tiles in flight
-    // At D = 128 tensor memory is full (S', dP', dV, dK): P' lies over S' and dS' over dP', each half of the columns over its
-    // own half.  At D = 64 they have columns of their own and the next S', dP' start as soon as the last are in registers.
-    static constexpr bool kOverlay = D == 128;
-    static constexpr size_t kTiles = (size_t)(2 + kQ + kDo) * tile_bytes<D>();
-    struct Barriers {
-        WorkQueue queue;
-        // k_*, v_*, acc_* count pieces of work that have steps, the others steps
-        uint64_t k_full, k_empty, v_full, v_empty, acc_full, acc_empty, s_full, s_empty, dp_full, dp_empty, p_full, p_empty, ds_full,
-            ds_empty, all_done;
-        uint64_t q_full[kQ], q_empty[kQ], q_raw[kQ], do_full[kDo], do_empty[kDo], do_raw[kDo], vec_full[kVec], vec_empty[kVec];
-        uint32_t tmem_slot;
-        int abort_flag;
-    };
-    // everything in one dynamic block, so that no byte goes to alignment: at D = 128 it fills the SM's 227 KB but for 600 bytes
-    static constexpr size_t kSmem = kTiles + kVec * 2 * kVecBytes + sizeof(Barriers);
-    static_assert(kSmem <= 232448, "shared memory of an SM");
-};
-
 // Work: a key tile of one key head; steps: the heads of its group times the query tiles that see it.
-struct DkvWork {
+struct alignas(16) DkvWork {
     int n, hk, kt, lo, hi, q_from, q_tiles, steps;
+    int end;
 
-    __device__ __forceinline__ DkvWork(const BwdArgs& a, int block) {
+    __device__ __forceinline__ void set(const BwdArgs& a, int block) {
         const Geometry& g = a.g;
+        end = block < 0;
+        if (end) return;
         // the first key tiles are seen by the most queries: they go first
         kt = (int)((unsigned)block / (unsigned)(g.n_seq * g.kv_heads));
         const int nk = (int)((unsigned)block % (unsigned)(g.n_seq * g.kv_heads));
@@ -174,9 +132,32 @@ struct DkvWork {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
+struct DkvCfg {
+    static constexpr uint32_t kQ = D == 128 ? 3 : 4, kDo = D == 128 ? 2 : 4;  // tiles of q (needed the longest) and of dout in flight
+    static constexpr uint32_t kVec = 2;                                       // row terms of query tiles in flight
+    // At D = 128 tensor memory is full (S', dP', dV, dK): P' lies over S' and dS' over dP', each warp's part of them over its
+    // own part.  At D = 64 they have columns of their own and the next S', dP' start as soon as the last are in registers.
+    static constexpr bool kOverlay = D == 128;
+    static constexpr size_t kTiles = (size_t)(2 + kQ + kDo) * tile_bytes<D>();
+    struct Barriers {
+        WorkQueue<DkvWork> queue;
+        // k_*, v_*, acc_* count pieces of work that have steps, the others steps
+        uint64_t k_full, v_full, acc_full, acc_empty, s_full, s_empty, dp_full, dp_empty, p_full, p_empty, ds_full, ds_empty, staged,
+            all_done;
+        uint64_t q_full[kQ], q_empty[kQ], q_raw[kQ], do_full[kDo], do_empty[kDo], do_raw[kDo], vec_full[kVec], vec_empty[kVec];
+        uint32_t tmem_slot;
+        int abort_flag;
+    };
+    // everything in one dynamic block, so that no byte goes to alignment: at D = 128 it fills the SM's 227 KB but for 600 bytes
+    static constexpr size_t kSmem = kTiles + kVec * 2 * kVecBytes + sizeof(Barriers);
+    static_assert(kSmem <= 232448, "shared memory of an SM");
+};
+
+template <int D>
+__global__ void __launch_bounds__(W::kThreads, 1)
 attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
-                const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ BwdArgs a) {
+                const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo,
+                const __grid_constant__ CUtensorMap mdk, const __grid_constant__ CUtensorMap mdv, const __grid_constant__ BwdArgs a) {
     using Cfg = DkvCfg<D>;
     constexpr uint32_t kQ = Cfg::kQ, kDo = Cfg::kDo, kVec = Cfg::kVec;
     constexpr bool kOverlay = Cfg::kOverlay;
@@ -193,19 +174,18 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
 
     if (tid == 0) {
         mbar_init(&m.k_full, 1);
-        mbar_init(&m.k_empty, 1);
         mbar_init(&m.v_full, 1);
-        mbar_init(&m.v_empty, 1);
         mbar_init(&m.acc_full, 1);
-        mbar_init(&m.acc_empty, 8);
+        mbar_init(&m.acc_empty, W::kRow);
         mbar_init(&m.s_full, 1);
-        mbar_init(&m.s_empty, 8);
+        mbar_init(&m.s_empty, W::kRow);
         mbar_init(&m.dp_full, 1);
-        mbar_init(&m.dp_empty, 8);
-        mbar_init(&m.p_full, 8);
+        mbar_init(&m.dp_empty, W::kRow);
+        mbar_init(&m.p_full, W::kRow);
         mbar_init(&m.p_empty, 1);
-        mbar_init(&m.ds_full, 8);
+        mbar_init(&m.ds_full, W::kRow);
         mbar_init(&m.ds_empty, 1);
+        mbar_init(&m.staged, W::kRow);
         mbar_init(&m.all_done, 1);
         for (uint32_t s = 0; s < kQ; ++s) {
             mbar_init(&m.q_full[s], 1);
@@ -219,13 +199,13 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         }
         for (uint32_t s = 0; s < kVec; ++s) {
             mbar_init(&m.vec_full[s], 1);
-            mbar_init(&m.vec_empty[s], 8);
+            mbar_init(&m.vec_empty[s], W::kRow);
         }
-        work_init(&m.queue, 10);
+        work_init(&m.queue, W::kRow + 2);
         m.abort_flag = 0;
         mbar_init_fence();
     }
-    if (warp == 9) {
+    if (warp == W::kMma) {
         tmem_alloc(&m.tmem_slot, 512);
         tmem_relinquish();
     }
@@ -235,31 +215,41 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     const uint32_t tmem = __shfl_sync(0xffffffffu, m.tmem_slot, 0);
     const uint32_t s_t = tmem, dp_t = tmem + 128u, dv_t = tmem + 256u, dk_t = tmem + 256u + D;
     const uint32_t p_t = kOverlay ? s_t : tmem + 384u, ds_t = kOverlay ? dp_t : tmem + 448u;
-    constexpr uint32_t kHalf = kOverlay ? 64u : 32u;  // columns from the first half of P' or dS' to the second
+    constexpr uint32_t kPart = kOverlay ? 32u : 16u;  // 32-bit columns from one warp's part of P' or dS' to the next
     uint8_t* k_tile = smem;
     uint8_t* v_tile = smem + TB;
     auto q_tile = [&](uint32_t s) { return smem + (2u + s) * (uint32_t)TB; };
     auto do_tile = [&](uint32_t s) { return smem + (2u + kQ + s) * (uint32_t)TB; };
     auto vec_of = [&](uint32_t s) { return reinterpret_cast<float*>(smem + Cfg::kTiles) + s * 2u * kTile; };
 
-    if (warp >= 8) leave_registers();
-    if (warp == 8) {
+    if (warp >= W::kRow) W::leave_registers();
+    if (warp == W::kCopy) {
         // ------------------------------------ copies ------------------------------------------------------
         if (lane == 0) {
-            uint32_t steps = 0, n_do = 0, n_vec = 0, pieces = 0, v_pieces = 0, k = 0, q_was_raw = 0, do_was_raw = 0;
+            uint32_t steps = 0, n_do = 0, n_vec = 0, pieces = 0, k = 0, q_was_raw = 0, do_was_raw = 0;
             RawParity q_raw, do_raw;
             Place<kQ> qa;
             Place<kDo> da;
             Place<kVec> ca;
             bool ok = true;
             int block = (int)blockIdx.x;
-            while (block >= 0) {
-                const DkvWork x(a, block);
-                if (x.steps > 0) {
-                    if (pieces > 0 && !(ok = wait_one(&m.k_empty, (pieces - 1u) & 1u, abortp))) break;
-                    mbar_arrive_expect_tx(&m.k_full, TB);
-                    load_tile<D>(k_tile, &mk, x.hk, x.kt * kTile, x.n, &m.k_full);
-                    ++pieces;
+            DkvWork x, last{};
+            // The results of the last piece lie in its key and value tiles; they leave before new ones come.
+            auto flush = [&] {
+                ok = wait_one(&m.staged, (pieces - 1u) & 1u, abortp);
+                if (!ok) return;
+                store_tile<D>(&mdk, k_tile, g.head_dim, last.hk, last.kt * kTile, last.n);
+                store_tile<D>(&mdv, v_tile, g.head_dim, last.hk, last.kt * kTile, last.n);
+                bulk_commit();
+                bulk_wait_read<0>();
+            };
+            while (true) {
+                x.set(a, block);
+                if (!(ok = work_put(&m.queue, k, x, abortp))) break;
+                if (x.end) {
+                    if (pieces > 0) flush();
+                    bulk_wait_all<0>();
+                    break;
                 }
                 int h = x.hk * g.group, qt = x.q_from;
                 for (int i = 0; i < x.steps; ++i) {
@@ -281,11 +271,15 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                     ++n_vec;
                     ca.step();
 
-                    if (i == 0) {  // V after the first query tile: its old tile is needed the longest
-                        if (v_pieces > 0 && !(ok = wait_one(&m.v_empty, (v_pieces - 1u) & 1u, abortp))) break;
+                    if (i == 0) {
+                        if (pieces > 0) flush();
+                        if (!ok) break;
+                        last = x;
+                        mbar_arrive_expect_tx(&m.k_full, TB);
+                        load_tile<D>(k_tile, &mk, x.hk, x.kt * kTile, x.n, &m.k_full);
                         mbar_arrive_expect_tx(&m.v_full, TB);
                         load_tile<D>(v_tile, &mv, x.hk, x.kt * kTile, x.n, &m.v_full);
-                        ++v_pieces;
+                        ++pieces;
                     }
 
                     if (n_do >= kDo && !(ok = wait_one(&m.do_empty[da.s], da.parity ^ 1u, abortp))) break;
@@ -302,11 +296,10 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                         ++h;
                     }
                 }
-                if (!ok || !(ok = work_ask(&m.queue, k, abortp))) break;
+                if (!ok) break;
+                block = work_ask(&m.queue, k, abortp);
+                if (!(ok = block >= -1)) break;
                 ++k;
-                if (!(ok = mbar_wait_bounded(&m.queue.full[(k - 1u) & 1u], ((k - 1u) >> 1) & 1u, abortp))) break;
-                block = work_read(&m.queue, k - 1u);
-                fence_proxy_async_smem();
             }
             if (!ok || *abortp) {  // gave up: what is under way lands before the block's memory goes away
                 for (uint32_t s = 0; s < kQ && s < steps; ++s) {
@@ -319,19 +312,17 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 }
                 for (uint32_t s = 0; s < kVec && s < n_vec; ++s) wait_landed(&m.vec_full[s], s < ca.s ? ca.parity : ca.parity ^ 1u);
                 if (pieces > 0) wait_landed(&m.k_full, (pieces - 1u) & 1u);
-                if (v_pieces > 0) wait_landed(&m.v_full, (v_pieces - 1u) & 1u);
-                if (k > 0) wait_landed(&m.queue.full[(k - 1u) & 1u], ((k - 1u) >> 1) & 1u);
+                if (pieces > 0) wait_landed(&m.v_full, (pieces - 1u) & 1u);
             }
         }
-    } else if (warp == 10) {
+    } else if (warp == W::kClean) {
         // ------------------------------------ dead rows ---------------------------------------------------
         RawParity q_raw, do_raw;
         Place<kQ> qa;
         Place<kDo> da;
         bool ok = true;
-        int block = (int)blockIdx.x;
-        for (uint32_t k = 0; block >= 0 && ok; ++k) {
-            const DkvWork x(a, block);
+        DkvWork x;
+        for (uint32_t k = 0; ok && work_take(&m.queue, k, x, lane, abortp); ++k) {
             int qt = x.q_from;
             for (int i = 0; i < x.steps && ok; ++i) {
                 if (dirty(qt, x.lo, x.hi)) {
@@ -346,9 +337,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 da.step();
                 qt = qt + 1 < x.q_from + x.q_tiles ? qt + 1 : x.q_from;
             }
-            if (ok) block = work_next(&m.queue, k, lane, abortp);
         }
-    } else if (warp == 9) {
+    } else if (warp == W::kMma) {
         // ------------------------------------ products ----------------------------------------------------
         if (elect_one()) {
             bool ok = true;
@@ -362,74 +352,70 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             uint32_t pieces = 0, gi = 0;   // gi: steps so far, over all pieces
             Place<kQ> qa, qd;              // the query tile of the next scores, of the next dK
             Place<kDo> da, dd;             // the dout tile of the next dP, of the next dV
-            auto scores = [&](bool last) {  // S' of the next step
+            auto scores = [&] {  // S' of the next step
                 wait(&m.q_full[qa.s], qa.parity);
                 if (!ok) return;
                 mma_rows<D>(s_t, kb, q_addr(qa.s));
                 mma_commit(&m.s_full);
-                if (last) mma_commit(&m.k_empty);
                 qa.step();
             };
-            auto dps = [&](bool last) {  // dP' of the next step
+            auto dps = [&] {  // dP' of the next step
                 wait(&m.do_full[da.s], da.parity);
                 if (!ok) return;
                 mma_rows<D>(dp_t, vb, do_addr(da.s));
                 mma_commit(&m.dp_full);
-                if (last) mma_commit(&m.v_empty);
                 da.step();
             };
-            int block = (int)blockIdx.x;
-            for (uint32_t k = 0; block >= 0 && ok; ++k) {
-                const DkvWork x(a, block);
+            DkvWork x;
+            for (uint32_t k = 0; ok && work_take_one(&m.queue, k, x, abortp); ++k) {
                 if (x.steps > 0) {
                     wait(&m.k_full, pieces & 1u);
                     if (!kOverlay && gi > 0) wait(&m.s_empty, (gi - 1u) & 1u);
-                    scores(x.steps == 1);
+                    scores();
                     wait(&m.v_full, pieces & 1u);
                     if (!kOverlay && gi > 0) wait(&m.dp_empty, (gi - 1u) & 1u);
-                    dps(x.steps == 1);
+                    dps();
                     if (pieces > 0) wait(&m.acc_empty, (pieces - 1u) & 1u);
                 }
                 for (int i = 0; i < x.steps && ok; ++i, ++gi) {
-                    const bool more = i + 1 < x.steps, last = i + 2 == x.steps;
+                    const bool more = i + 1 < x.steps;
                     if (!kOverlay && more) {
                         wait(&m.s_empty, gi & 1u);
-                        scores(last);
+                        scores();
                     }
                     wait(&m.p_full, gi & 1u);
                     if (!ok) break;
-                    mma_sum<D>(dv_t, p_t, kHalf, do_addr(dd.s), (uint32_t)i);
-                    if (kOverlay && more) scores(last);
+                    mma_sum<D>(dv_t, p_t, kPart, do_addr(dd.s), (uint32_t)i);
+                    if (kOverlay && more) scores();
                     mma_commit(&m.do_empty[dd.s]);
                     dd.step();
                     if (!kOverlay) mma_commit(&m.p_empty);
                     if (!kOverlay && more) {
                         wait(&m.dp_empty, gi & 1u);
-                        dps(last);
+                        dps();
                     }
                     wait(&m.ds_full, gi & 1u);
                     if (!ok) break;
-                    mma_sum<D>(dk_t, ds_t, kHalf, q_addr(qd.s), (uint32_t)i);
+                    mma_sum<D>(dk_t, ds_t, kPart, q_addr(qd.s), (uint32_t)i);
                     if (!more) mma_commit(&m.acc_full);
-                    if (kOverlay && more) dps(last);
+                    if (kOverlay && more) dps();
                     mma_commit(&m.q_empty[qd.s]);
                     qd.step();
                     if (!kOverlay) mma_commit(&m.ds_empty);
                 }
                 if (x.steps > 0) ++pieces;
-                if (ok) block = work_next_one(&m.queue, k, abortp);
             }
             // every product has ended before tensor memory is given back
             mma_commit(&m.all_done);
             wait_drained(&m.all_done, abortp);
         }
         __syncwarp();
-    } else if (warp < 8) {
+    } else if (warp < W::kRow) {
         // ------------------------------------ probabilities, dS -------------------------------------------
-        take_registers();
-        const int half = warp >> 2, row = (warp & 3) * 32 + lane;
+        W::take_registers();
+        const int part = warp >> 2, row = (warp & 3) * 32 + lane;  // columns [32 part, 32 part + 32)
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t mine = lanes + (uint32_t)half * 64u, packed = lanes + (uint32_t)half * kHalf;
+        const uint32_t mine = lanes + (uint32_t)part * 32u, packed = lanes + (uint32_t)part * kPart;
         const uint64_t c2 = f32x2(a.scale_log2, a.scale_log2);
         bool ok = true;
         auto wait = [&](uint64_t* bar, uint32_t parity) {
@@ -444,68 +430,69 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         };
         uint32_t gi = 0, pieces = 0;
         Place<kVec> ca;
-        int block = (int)blockIdx.x;
-        for (uint32_t k = 0; block >= 0; ++k) {
-            const DkvWork x(a, block);
+        DkvWork x;
+        for (uint32_t k = 0; work_take(&m.queue, k, x, lane, abortp); ++k) {
             const int key = x.kt * kTile + row;
             int qt = x.q_from;
             for (int i = 0; i < x.steps; ++i, ++gi) {
                 const int q0 = qt * kTile;
                 qt = qt + 1 < x.q_from + x.q_tiles ? qt + 1 : x.q_from;
-                float p[64];
-                uint32_t s[2][32], b[32];
+                float p[32];
+                uint32_t s[32], b[16];
                 if (!wait(&m.vec_full[ca.s], ca.parity) || !wait(&m.s_full, gi & 1u)) break;
-                tmem_ld32(s_t + mine, s[0]);
-                tmem_ld32(s_t + mine + 32u, s[1]);
+                tmem_ld32(s_t + mine, s);
                 tmem_ld_wait();
                 if (!kOverlay) tell(&m.s_empty);
-                const ulonglong2* shift = reinterpret_cast<const ulonglong2*>(vec_of(ca.s) + half * 64);
+                const ulonglong2* shift = reinterpret_cast<const ulonglong2*>(vec_of(ca.s) + part * 32);
                 probabilities(s, c2, [&](int e) { return e & 1 ? shift[e >> 1].y : shift[e >> 1].x; }, p);
                 // the diagonal, and the far edge of a window
                 if (q0 <= x.kt * kTile || q0 + kTile - 1 - x.kt * kTile >= g.window) {
-                    const int first = q0 + half * 64 - key;
+                    const int first = q0 + part * 32 - key;
 #pragma unroll
-                    for (int e = 0; e < 64; ++e)
+                    for (int e = 0; e < 32; ++e)
                         if ((unsigned)(first + e) >= (unsigned)g.window) p[e] = 0.f;
                 }
                 round_pairs(p, b);
                 if (!kOverlay && gi > 0 && !wait(&m.p_empty, (gi - 1u) & 1u)) break;
-                tmem_st32(p_t + packed, b);
+                tmem_st16(p_t + packed, b);
                 tmem_st_wait();
                 tell(&m.p_full);
 
                 if (!wait(&m.dp_full, gi & 1u)) break;
-                tmem_ld32(dp_t + mine, s[0]);
-                tmem_ld32(dp_t + mine + 32u, s[1]);
+                tmem_ld32(dp_t + mine, s);
                 tmem_ld_wait();
                 if (!kOverlay) tell(&m.dp_empty);
-                const ulonglong2* ndelta = reinterpret_cast<const ulonglong2*>(vec_of(ca.s) + kTile + half * 64);
+                const ulonglong2* ndelta = reinterpret_cast<const ulonglong2*>(vec_of(ca.s) + kTile + part * 32);
                 score_grads(s, p, [&](int e) { return e & 1 ? ndelta[e >> 1].y : ndelta[e >> 1].x; }, b);
                 if (!kOverlay && gi > 0 && !wait(&m.ds_empty, (gi - 1u) & 1u)) break;
-                tmem_st32(ds_t + packed, b);
+                tmem_st16(ds_t + packed, b);
                 tmem_st_wait();
                 tell(&m.ds_full);
                 if (lane == 0) mbar_arrive(&m.vec_empty[ca.s]);
                 ca.step();
             }
-            // warps 0-3 write dV, warps 4-7 dK
+            // half of the warps write dV, half dK, each half of the columns
             if (ok && x.steps > 0) wait(&m.acc_full, pieces & 1u);
             if (!ok) break;
-            const bool live = key >= x.lo && key < x.hi;
-            const int64_t r = (int64_t)x.n * g.seq_len + key;
-            uint16_t* dst = (half ? a.dk + r * a.ld_dk : a.dv + r * a.ld_dv) + x.hk * g.head_dim;
-            write_row((half ? dk_t : dv_t) + lanes, 0, D / 32, x.steps > 0, live, half ? a.scale : 1.f, dst, g.head_dim,
-                      half ? a.wide_dk : a.wide_dv, key < g.seq_len);
+            const bool keys = part >= 2;
             if (x.steps > 0) {
+                const bool live = key >= x.lo && key < x.hi;
+#pragma unroll 1
+                for (int c = (part & 1) * (D / 64); c < ((part & 1) + 1) * (D / 64); ++c)
+                    stage_acc32(keys ? k_tile : v_tile, row, c, (keys ? dk_t : dv_t) + lanes + 32u * c, live, keys ? a.scale : 1.f);
+                fence_proxy_async_smem();
                 tell(&m.acc_empty);
+                tell(&m.staged);
                 ++pieces;
+            } else {
+                zero_tile(keys ? a.dk : a.dv, keys ? a.ld_dk : a.ld_dv, g.seq_len, g.head_dim, x.hk, x.kt * kTile, x.n,
+                          (part & 1) * 128 + row, 256);
             }
-            block = work_next(&m.queue, k, lane, abortp);
         }
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == W::kMma) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
@@ -521,11 +508,14 @@ struct DqCfg {
 };
 
 // Work: a query tile of one head; steps: the key tiles that it sees.
-struct DqWork {
+struct alignas(16) DqWork {
     int n, h, t, lo, hi, from, steps;
+    int end;
 
-    __device__ __forceinline__ DqWork(const BwdArgs& a, int block) {
+    __device__ __forceinline__ void set(const BwdArgs& a, int block) {
         const Geometry& g = a.g;
+        end = block < 0;
+        if (end) return;
         // the longest rows first; the heads of a group next to one another, they read the same keys
         t = a.tiles - 1 - (int)((unsigned)block / (unsigned)(g.n_seq * g.heads));
         const int nh = (int)((unsigned)block % (unsigned)(g.n_seq * g.heads));
@@ -539,17 +529,18 @@ struct DqWork {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(W::kThreads, 1)
 attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
-               const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const __grid_constant__ BwdArgs a) {
+               const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo,
+               const __grid_constant__ CUtensorMap mdq, const __grid_constant__ BwdArgs a) {
     constexpr uint32_t kKeys = DqCfg<D>::kKeys, kVals = DqCfg<D>::kVals;
     constexpr int TB = tile_bytes<D>();
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     // q_*, do_*, acc_* count pieces of work that have steps, the others steps
-    __shared__ __align__(8) uint64_t q_full, q_empty, do_full, do_empty, acc_full, acc_empty, s_full[2], dp_full, ds_full, all_done,
+    __shared__ __align__(8) uint64_t q_full, q_empty, do_full, acc_full, acc_empty, staged, s_full[2], dp_full, ds_full, all_done,
         k_full[kKeys], k_empty[kKeys], k_raw[kKeys], v_full[kVals], v_empty[kVals], v_raw[kVals];
-    __shared__ WorkQueue queue;
+    __shared__ __align__(16) WorkQueue<DqWork> queue;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     volatile int* abortp = &abort_flag;
@@ -560,13 +551,13 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         mbar_init(&q_full, 1);
         mbar_init(&q_empty, 1);
         mbar_init(&do_full, 1);
-        mbar_init(&do_empty, 1);
+        mbar_init(&staged, W::kRow);
         mbar_init(&acc_full, 1);
-        mbar_init(&acc_empty, 8);
+        mbar_init(&acc_empty, W::kRow);
         mbar_init(&s_full[0], 1);
         mbar_init(&s_full[1], 1);
         mbar_init(&dp_full, 1);
-        mbar_init(&ds_full, 8);
+        mbar_init(&ds_full, W::kRow);
         mbar_init(&all_done, 1);
         for (uint32_t s = 0; s < kKeys; ++s) {
             mbar_init(&k_full[s], 1);
@@ -578,11 +569,11 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             mbar_init(&v_empty[s], 1);
             mbar_init(&v_raw[s], 1);
         }
-        work_init(&queue, 10);
+        work_init(&queue, W::kRow + 2);
         abort_flag = 0;
         mbar_init_fence();
     }
-    if (warp == 9) {
+    if (warp == W::kMma) {
         tmem_alloc(&tmem_slot, 512);
         tmem_relinquish();
     }
@@ -598,8 +589,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     auto k_tile = [&](uint32_t s) { return smem + (2u + s) * (uint32_t)TB; };
     auto v_tile = [&](uint32_t s) { return smem + (2u + kKeys + s) * (uint32_t)TB; };
 
-    if (warp >= 8) leave_registers();
-    if (warp == 8) {
+    if (warp >= W::kRow) W::leave_registers();
+    if (warp == W::kCopy) {
         // ------------------------------------ copies ------------------------------------------------------
         if (lane == 0) {
             bool ok = true;
@@ -608,8 +599,24 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             Place<kKeys> ka;
             Place<kVals> va;
             int block = (int)blockIdx.x;
-            while (block >= 0) {
-                const DqWork x(a, block);
+            DqWork x, last{};
+            // The results of the last piece lie in its dout tile (queries of the next are wanted sooner); they leave before a
+            // new one comes.
+            auto flush = [&] {
+                ok = wait_one(&staged, (ndo - 1u) & 1u, abortp);
+                if (!ok) return;
+                store_tile<D>(&mdq, do_tile, g.head_dim, last.h, last.t * kTile, last.n);
+                bulk_commit();
+                bulk_wait_read<0>();
+            };
+            while (true) {
+                x.set(a, block);
+                if (!(ok = work_put(&queue, k, x, abortp))) break;
+                if (x.end) {
+                    if (ndo > 0) flush();
+                    bulk_wait_all<0>();
+                    break;
+                }
                 if (x.steps > 0) {
                     if (nq > 0 && !(ok = wait_one(&q_empty, (nq - 1u) & 1u, abortp))) break;
                     mbar_arrive_expect_tx(&q_full, TB);
@@ -630,7 +637,9 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                     ++nk;
                     ka.step();
                     if (i == 0) {
-                        if (ndo > 0 && !(ok = wait_one(&do_empty, (ndo - 1u) & 1u, abortp))) break;
+                        if (ndo > 0) flush();
+                        if (!ok) break;
+                        last = x;
                         mbar_arrive_expect_tx(&do_full, TB);
                         load_tile<D>(do_tile, &mdo, x.h, x.t * kTile, x.n, &do_full);
                         ++ndo;
@@ -644,11 +653,10 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                     ++nv;
                     va.step();
                 }
-                if (!ok || !(ok = work_ask(&queue, k, abortp))) break;
+                if (!ok) break;
+                block = work_ask(&queue, k, abortp);
+                if (!(ok = block >= -1)) break;
                 ++k;
-                if (!(ok = mbar_wait_bounded(&queue.full[(k - 1u) & 1u], ((k - 1u) >> 1) & 1u, abortp))) break;
-                block = work_read(&queue, k - 1u);
-                fence_proxy_async_smem();
             }
             if (!ok || *abortp) {  // gave up: what is under way lands before the block's memory goes away
                 if (nq > 0) wait_landed(&q_full, (nq - 1u) & 1u);
@@ -661,18 +669,16 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                     if ((v_was_raw >> s) & 1u) wait_landed(&v_raw[s], ((vr.bits >> s) & 1u) ^ 1u);
                     else wait_landed(&v_full[s], s < va.s ? va.parity : va.parity ^ 1u);
                 }
-                if (k > 0) wait_landed(&queue.full[(k - 1u) & 1u], ((k - 1u) >> 1) & 1u);
             }
         }
-    } else if (warp == 10) {
+    } else if (warp == W::kClean) {
         // ------------------------------------ dead rows ---------------------------------------------------
         RawParity kr, vr;
         Place<kKeys> ka;
         Place<kVals> va;
         bool ok = true;
-        int block = (int)blockIdx.x;
-        for (uint32_t k = 0; block >= 0 && ok; ++k) {
-            const DqWork x(a, block);
+        DqWork x;
+        for (uint32_t k = 0; ok && work_take(&queue, k, x, lane, abortp); ++k) {
             for (int i = 0; i < x.steps && ok; ++i) {
                 const int t0 = (x.from + i) * kTile;
                 if (dirty(x.from + i, x.lo, x.hi)) {
@@ -686,9 +692,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 ka.step();
                 va.step();
             }
-            if (ok) block = work_next(&queue, k, lane, abortp);
         }
-    } else if (warp == 9) {
+    } else if (warp == W::kMma) {
         // ------------------------------------ products ----------------------------------------------------
         if (elect_one()) {
             bool ok = true;
@@ -711,50 +716,47 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 ka.step();
                 ++gs;
             };
-            auto dps = [&](bool last) {
+            auto dps = [&] {
                 if (!ok) return;
                 mma_rows<D>(dp_t, dob, v_addr(va.s));
                 mma_commit(&dp_full);
                 mma_commit(&v_empty[va.s]);
-                if (last) mma_commit(&do_empty);
                 va.step();
             };
-            int block = (int)blockIdx.x;
-            for (uint32_t k = 0; block >= 0 && ok; ++k) {
-                const DqWork x(a, block);
+            DqWork x;
+            for (uint32_t k = 0; ok && work_take_one(&queue, k, x, abortp); ++k) {
                 if (x.steps > 0) {
                     wait(&q_full, pieces & 1u);
                     scores(x.steps == 1);
                     wait(&do_full, pieces & 1u);
                     wait(&v_full[va.s], va.parity);
-                    dps(x.steps == 1);
+                    dps();
                     if (x.steps > 1) scores(x.steps == 2);
                     if (pieces > 0) wait(&acc_empty, (pieces - 1u) & 1u);
                 }
                 for (int i = 0; i < x.steps && ok; ++i, ++gi) {
                     if (i + 1 < x.steps) wait(&v_full[va.s], va.parity);
                     wait(&ds_full, gi & 1u);  // dP has been read, dS is there
-                    if (i + 1 < x.steps) dps(i + 2 == x.steps);
+                    if (i + 1 < x.steps) dps();
                     if (!ok) break;
-                    mma_sum<D>(dq_t, s_addr(gi), 64u, k_addr(kd.s), (uint32_t)i);
+                    mma_sum<D>(dq_t, s_addr(gi), 32u, k_addr(kd.s), (uint32_t)i);
                     if (i + 1 == x.steps) mma_commit(&acc_full);
                     mma_commit(&k_empty[kd.s]);
                     kd.step();
                     if (i + 2 < x.steps) scores(i + 3 == x.steps);
                 }
                 if (x.steps > 0) ++pieces;
-                if (ok) block = work_next_one(&queue, k, abortp);
             }
             mma_commit(&all_done);
             wait_drained(&all_done, abortp);
         }
         __syncwarp();
-    } else if (warp < 8) {
+    } else if (warp < W::kRow) {
         // ------------------------------------ probabilities, dS -------------------------------------------
-        take_registers();
-        const int half = warp >> 2, row = (warp & 3) * 32 + lane;
+        W::take_registers();
+        const int part = warp >> 2, row = (warp & 3) * 32 + lane;  // columns [32 part, 32 part + 32)
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t mine = lanes + (uint32_t)half * 64u;
+        const uint32_t mine = lanes + (uint32_t)part * 32u;
         const uint64_t c2 = f32x2(a.scale_log2, a.scale_log2);
         bool ok = true;
         auto wait = [&](uint64_t* bar, uint32_t parity) {
@@ -768,9 +770,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             if (lane == 0) mbar_arrive(bar);
         };
         uint32_t gi = 0, pieces = 0;
-        int block = (int)blockIdx.x;
-        for (uint32_t k = 0; block >= 0; ++k) {
-            const DqWork x(a, block);
+        DqWork x;
+        for (uint32_t k = 0; work_take(&queue, k, x, lane, abortp); ++k) {
             const int pos = x.t * kTile + row;
             const bool live = pos >= x.lo && pos < x.hi;
             const int see = max(x.lo, pos - g.window + 1);
@@ -785,44 +786,42 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             const uint64_t shift2 = f32x2(shift, shift), ndelta2 = f32x2(ndelta, ndelta);
             for (int i = 0; i < x.steps; ++i, ++gi) {
                 const int j = x.from + i;
-                float p[64];
-                uint32_t s[2][32], b[32];
+                float p[32];
+                uint32_t s[32], b[16];
                 if (!wait(&s_full[gi & 1u], (gi >> 1) & 1u)) break;
-                tmem_ld32(s_addr(gi) + mine, s[0]);
-                tmem_ld32(s_addr(gi) + mine + 32u, s[1]);
+                tmem_ld32(s_addr(gi) + mine, s);
                 tmem_ld_wait();
                 probabilities(s, c2, [&](int) { return shift2; }, p);
                 if (j < full_from || j >= full_to) {
-                    const int first = j * kTile + half * 64 - see;
+                    const int first = j * kTile + part * 32 - see;
 #pragma unroll
-                    for (int e = 0; e < 64; ++e)
+                    for (int e = 0; e < 32; ++e)
                         if ((unsigned)(first + e) >= count) p[e] = 0.f;
                 }
                 if (!wait(&dp_full, gi & 1u)) break;
-                tmem_ld32(dp_t + mine, s[0]);
-                tmem_ld32(dp_t + mine + 32u, s[1]);
+                tmem_ld32(dp_t + mine, s);
                 tmem_ld_wait();
                 score_grads(s, p, [&](int) { return ndelta2; }, b);
-                tmem_st32(s_addr(gi) + mine, b);
+                tmem_st16(s_addr(gi) + mine, b);
                 tmem_st_wait();
                 tell(&ds_full);
             }
             if (ok && x.steps > 0) wait(&acc_full, pieces & 1u);
             if (!ok) break;
-            // each half writes half of the columns
-            const int64_t r = (int64_t)x.n * g.seq_len + pos;
-            write_row(dq_t + lanes, half * (D / 64), (half + 1) * (D / 64), x.steps > 0, live, a.scale, a.dq + r * a.ld_dq + x.h * g.head_dim,
-                      g.head_dim, a.wide_dq, pos < g.seq_len);
-            if (x.steps > 0) {
+            if (x.steps > 0) {  // 32 columns each (at D = 64 half of the warps have none)
+                if (part * 32 < D) stage_acc32(do_tile, row, part, dq_t + lanes + 32u * part, live, a.scale);
+                fence_proxy_async_smem();
                 tell(&acc_empty);
+                tell(&staged);
                 ++pieces;
+            } else {
+                zero_tile(a.dq, a.ld_dq, g.seq_len, g.head_dim, x.h, x.t * kTile, x.n, part * 128 + row, 512);
             }
-            block = work_next(&queue, k, lane, abortp);
         }
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == W::kMma) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
@@ -832,7 +831,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
 // ---- host -------------------------------------------------------------------------------------------------------
 
 struct Maps {
-    CUtensorMap q, k, v, dout;
+    CUtensorMap q, k, v, dout, dq, dk, dv;
 };
 
 template <int D>
@@ -841,8 +840,8 @@ cudaError_t launch_bwd(const Maps& m, const BwdArgs& a, cudaStream_t st) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_dq_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)DqCfg<D>::kSmem);
     if (e != cudaSuccess) return e;
     const unsigned nk = (unsigned)(a.g.n_seq * a.g.kv_heads), nh = (unsigned)(a.g.n_seq * a.g.heads);
-    attn_dkv_kernel<D><<<nk * (unsigned)a.tiles, kThreads, DkvCfg<D>::kSmem, st>>>(m.q, m.k, m.v, m.dout, a);
-    attn_dq_kernel<D><<<nh * (unsigned)a.tiles, kThreads, DqCfg<D>::kSmem, st>>>(m.q, m.k, m.v, m.dout, a);
+    attn_dkv_kernel<D><<<nk * (unsigned)a.tiles, W::kThreads, DkvCfg<D>::kSmem, st>>>(m.q, m.k, m.v, m.dout, m.dk, m.dv, a);
+    attn_dq_kernel<D><<<nh * (unsigned)a.tiles, W::kThreads, DqCfg<D>::kSmem, st>>>(m.q, m.k, m.v, m.dout, m.dq, a);
     return cudaGetLastError();
 }
 
@@ -909,7 +908,9 @@ extern "C" rapid_status_t rapid_attention_bwd(const rapid_attn_desc_t* desc, con
     if ((s = policy::check_device(&sms)) != RAPID_OK) return s;
     Maps m;
     if (!make_head_map(&m.q, q, d, d.n_heads, d.ld_q) || !make_head_map(&m.k, k, d, d.n_kv_heads, d.ld_k) ||
-        !make_head_map(&m.v, v, d, d.n_kv_heads, d.ld_v) || !make_head_map(&m.dout, dout, d, d.n_heads, d.ld_dout))
+        !make_head_map(&m.v, v, d, d.n_kv_heads, d.ld_v) || !make_head_map(&m.dout, dout, d, d.n_heads, d.ld_dout) ||
+        !make_head_map(&m.dq, dq, d, d.n_heads, d.ld_dq) || !make_head_map(&m.dk, dk, d, d.n_kv_heads, d.ld_dk) ||
+        !make_head_map(&m.dv, dv, d, d.n_kv_heads, d.ld_dv))
         return RAPID_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (policy::clear_stats(stats, st) != cudaSuccess) return RAPID_ERR_CUDA;
@@ -928,9 +929,6 @@ extern "C" rapid_status_t rapid_attention_bwd(const rapid_attn_desc_t* desc, con
     a.ld_dq = d.ld_dq;
     a.ld_dk = d.ld_dk;
     a.ld_dv = d.ld_dv;
-    a.wide_dq = wide_rows(dq, d.ld_dq, d.head_dim);
-    a.wide_dk = wide_rows(dk, d.ld_dk, d.head_dim);
-    a.wide_dv = wide_rows(dv, d.ld_dv, d.head_dim);
     a.stats = stats;
     int lanes_log2 = 0;
     while ((8 << lanes_log2) < d.head_dim) ++lanes_log2;

@@ -1,9 +1,8 @@
 // Causal attention, forward (tcgen05).
 //
 // A piece of work is two items of one key head: an item is (query tile of 128 positions, query head of the group), items
-// are numbered tile by tile, so the two usually share the tile and always the keys.  Warps 0-3 and 4-7 each run the
-// softmax of one item, a thread to a row, so row maximum and sum need no exchange; warp 8 issues the copies, warp 9 the
-// products:
+// are numbered tile by tile, so the two usually share the tile and always the keys.  Four warps run the softmax of one item, a
+// thread to a row, so row maximum and sum need no exchange:
 //     S_w = Q_w K_j^T into tensor memory -> softmax writes P_w (bf16) to tensor memory -> O_w += P_w V_j
 // P is the left operand straight from tensor memory, O stays there to the end.  At D = 128 P lies over S (tensor memory is
 // full): while the softmax of one item works, the tensor cores have the other item's products.  At D = 64 P has columns
@@ -18,12 +17,15 @@ namespace rapid {
 namespace attn {
 namespace {
 
+// Eight row warps, a thread to a row: with sixteen, half a row each, the exchange of the maximum through shared memory costs
+// more than the wider choice of instructions brings (64 x 256: 55 us against 47; 8 x 4096: 322 against 314).
+using W = Roles<8>;
+
 struct FwdArgs {
     Geometry g;
     float scale_log2;  // scale * log2(e)
     uint16_t* out;
     int64_t ld_out;
-    bool wide;  // see store_row32
     float* lse;
     rapid_stats_t* stats;
     int items, pairs;  // work items of a key head; pieces of work for them
@@ -31,33 +33,39 @@ struct FwdArgs {
 
 template <int D>
 struct FwdCfg {
-    static constexpr uint32_t kStages = D == 128 ? 5 : 8;  // tiles in flight, keys and values alternating
+    static constexpr uint32_t kStages = D == 128 ? 4 : 8;  // tiles in flight, keys and values alternating
     static constexpr bool kOverlay = D == 128;        // P over S
-    static constexpr int kPoly = 4;                   // of 16 pairs of exponentials, those formed by polynomial
-    static constexpr size_t kSmem = (size_t)(2 + kStages) * tile_bytes<D>() + 1024;
+    // Of 16 pairs of exponentials, those formed by polynomial.  With 1, 2, 3, 4: 293, 305, 308, 308 us (8 x 4096, 16 heads of 64).
+    static constexpr int kPoly = 1;
+    static constexpr size_t kSmem = (size_t)(2 + kStages) * tile_bytes<D>() + 2 * kBoxBytes + 1024;  // with a box of output for each item
 };
 
-struct FwdWork {
+struct alignas(16) FwdWork {
     int n, hk, lo, hi, jlo, jhi;
-    int t[2], h[2], from[2], to[2];
-    bool valid[2];
+    int t[2], h[2], from[2], to[2];  // of the two items
+    int valid;                       // bit w: item w exists
+    int end;
 
-    __device__ __forceinline__ FwdWork(const FwdArgs& a, int block) {
+    __device__ __forceinline__ void set(const FwdArgs& a, int block) {
         const Geometry& g = a.g;
+        end = block < 0;
+        if (end) return;
         // the longest rows first
         const int pair = a.pairs - 1 - (int)((unsigned)block / (unsigned)(g.n_seq * g.kv_heads));
         const int nk = (int)((unsigned)block % (unsigned)(g.n_seq * g.kv_heads));
         n = nk / g.kv_heads;
         hk = nk - n * g.kv_heads;
         live_range(g, n, lo, hi);
+        valid = 0;
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
             const int item = min(2 * pair + w, a.items - 1);
-            valid[w] = 2 * pair + w < a.items;
+            const bool exists = 2 * pair + w < a.items;
+            valid |= (exists ? 1 : 0) << w;
             t[w] = item / g.group;
             h[w] = hk * g.group + item - t[w] * g.group;
             key_tiles(g, t[w], lo, hi, from[w], to[w]);
-            if (!valid[w]) from[w] = to[w] = 0;
+            if (!exists) from[w] = to[w] = 0;
         }
         // the tiles of either item: a contiguous range
         jlo = jhi = 0;
@@ -70,18 +78,19 @@ struct FwdWork {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(W::kThreads, 1)
 attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
-                const __grid_constant__ CUtensorMap mv, const __grid_constant__ FwdArgs a) {
+                const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mo, const __grid_constant__ FwdArgs a) {
     constexpr uint32_t kStages = FwdCfg<D>::kStages;
     constexpr bool kOverlay = FwdCfg<D>::kOverlay;
     constexpr int TB = tile_bytes<D>();
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    // [w]: of an item.  q_full, q_empty, o_empty count the items with keys; s_*, p_full, o_full count tiles.
+    // [w]: of an item.  q_full, q_empty, o_empty (and o_full where P lies over S) count the items with keys; s_*, p_full, o_full
+    // count tiles.
     __shared__ __align__(8) uint64_t q_full[2], q_empty[2], s_full[2], s_empty[2], p_full[2], o_full[2], o_empty[2],
-        kv_full[kStages], kv_empty[kStages], kv_raw[kStages], drain;
-    __shared__ WorkQueue queue;
+        out_staged[2], out_free[2], kv_full[kStages], kv_empty[kStages], kv_raw[kStages], drain;
+    __shared__ __align__(16) WorkQueue<FwdWork> queue;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     volatile int* abortp = &abort_flag;
@@ -97,6 +106,8 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             mbar_init(&p_full[w], 4);
             mbar_init(&o_full[w], 1);
             mbar_init(&o_empty[w], 4);
+            mbar_init(&out_staged[w], 4);
+            mbar_init(&out_free[w], 1);
         }
         for (uint32_t s = 0; s < kStages; ++s) {
             mbar_init(&kv_full[s], 1);
@@ -104,11 +115,11 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             mbar_init(&kv_raw[s], 1);
         }
         mbar_init(&drain, 1);
-        work_init(&queue, 10);
+        work_init(&queue, W::kRow + 2);
         abort_flag = 0;
         mbar_init_fence();
     }
-    if (warp == 9) {
+    if (warp == W::kMma) {
         tmem_alloc(&tmem_slot, 512);
         tmem_relinquish();
     }
@@ -123,8 +134,8 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     auto kv_tile = [&](uint32_t s) { return smem + (size_t)(2 + s) * TB; };
     auto kv_addr = [&](uint32_t s) { return smem0 + (2u + s) * (uint32_t)TB; };
 
-    if (warp >= 8) leave_registers();
-    if (warp == 8) {
+    if (warp >= W::kRow) W::leave_registers();
+    if (warp == W::kCopy) {
         // ------------------------------------ copies ------------------------------------------------------
         if (lane == 0) {
             uint32_t it = 0, nq[2] = {0, 0}, k = 0, was_raw = 0;
@@ -132,8 +143,10 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             Place<kStages> at;
             bool ok = true;
             int block = (int)blockIdx.x;
-            while (block >= 0) {
-                const FwdWork x(a, block);
+            FwdWork x;
+            while (true) {
+                x.set(a, block);
+                if (!(ok = work_put(&queue, k, x, abortp)) || x.end) break;
 #pragma unroll
                 for (int w = 0; w < 2; ++w)
                     if (ok && x.to[w] > x.from[w]) {
@@ -157,11 +170,10 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                         ++it;
                         at.step();
                     }
-                if (!ok || !(ok = work_ask(&queue, k, abortp))) break;
+                if (!ok) break;
+                block = work_ask(&queue, k, abortp);
+                if (!(ok = block >= -1)) break;
                 ++k;
-                if (!(ok = mbar_wait_bounded(&queue.full[(k - 1u) & 1u], ((k - 1u) >> 1) & 1u, abortp))) break;
-                block = work_read(&queue, k - 1u);
-                fence_proxy_async_smem();
             }
             if (!ok || *abortp) {  // gave up: what is under way lands before the block's memory goes away
 #pragma unroll
@@ -172,17 +184,15 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                     if ((was_raw >> s) & 1u) wait_landed(&kv_raw[s], ((raw.bits >> s) & 1u) ^ 1u);
                     else wait_landed(&kv_full[s], now ? at.parity : at.parity ^ 1u);
                 }
-                if (k > 0) wait_landed(&queue.full[(k - 1u) & 1u], ((k - 1u) >> 1) & 1u);
             }
         }
-    } else if (warp == 10) {
+    } else if (warp == W::kClean) {
         // ------------------------------------ dead rows ---------------------------------------------------
         RawParity raw;
         Place<kStages> at;
         bool ok = true;
-        int block = (int)blockIdx.x;
-        for (uint32_t k = 0; block >= 0 && ok; ++k) {
-            const FwdWork x(a, block);
+        FwdWork x;
+        for (uint32_t k = 0; ok && work_take(&queue, k, x, lane, abortp); ++k)
             for (int j = x.jlo; j < x.jhi && ok; ++j) {
                 at.step();  // past the keys
                 if (dirty(j, x.lo, x.hi)) {
@@ -192,9 +202,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 }
                 at.step();
             }
-            if (ok) block = work_next(&queue, k, lane, abortp);
-        }
-    } else if (warp == 9) {
+    } else if (warp == W::kMma) {
         // ------------------------------------ products ----------------------------------------------------
         if (elect_one()) {
             bool ok = true;
@@ -206,10 +214,57 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 tc_fence_after();
                 return ok;
             };
-            int block = (int)blockIdx.x;
-            for (uint32_t k = 0; block >= 0 && ok; ++k) {
-                const FwdWork x(a, block);
+            FwdWork x;
+            for (uint32_t k = 0; ok && work_take_one(&queue, k, x, abortp); ++k) {
+                // Tiles in the middle, where both items have scores to form and earlier values to add, run through a loop
+                // without questions: what this lane does between products is time that the tensor cores lose.
+                const int mid_from = max(x.from[0], x.from[1]) + 2, mid_to = min(x.to[0], x.to[1]) - 1;
                 for (int j = x.jlo; j <= x.jhi && x.jlo < x.jhi && ok; ++j) {
+                    if (j >= mid_from && j < mid_to) {
+                        uint32_t sp0 = (ns[0] - 1u) & 1u, sp1 = (ns[1] - 1u) & 1u, pp0 = np[0] & 1u, pp1 = np[1] & 1u;
+                        ns[0] += (uint32_t)(mid_to - j);
+                        ns[1] += (uint32_t)(mid_to - j);
+                        np[0] += (uint32_t)(mid_to - j);
+                        np[1] += (uint32_t)(mid_to - j);
+                        for (; j < mid_to; ++j) {
+                            const uint32_t k_now = kv_addr(ka.s), v_now = kv_addr(va.s);
+                            if (!wait(&kv_full[ka.s], ka.parity)) break;
+                            if (kOverlay) {
+                                if (!wait(&kv_full[va.s], va.parity) || !wait(&p_full[0], pp0)) break;
+                                mma_sum<D>(o_addr(0), p_addr(0), 16u, v_now, 1u);
+                                mma_rows<D>(s_addr(0), smem0, k_now);
+                                mma_commit(&s_full[0]);
+                                if (!wait(&p_full[1], pp1)) break;
+                                mma_sum<D>(o_addr(1), p_addr(1), 16u, v_now, 1u);
+                                mma_rows<D>(s_addr(1), smem0 + TB, k_now);
+                                mma_commit(&s_full[1]);
+                                mma_commit(&kv_empty[ka.s]);
+                                mma_commit(&kv_empty[va.s]);
+                            } else {
+                                if (!wait(&s_empty[0], sp0)) break;
+                                mma_rows<D>(s_addr(0), smem0, k_now);
+                                mma_commit(&s_full[0]);
+                                if (!wait(&s_empty[1], sp1)) break;
+                                mma_rows<D>(s_addr(1), smem0 + TB, k_now);
+                                mma_commit(&s_full[1]);
+                                mma_commit(&kv_empty[ka.s]);
+                                if (!wait(&kv_full[va.s], va.parity) || !wait(&p_full[0], pp0)) break;
+                                mma_sum<D>(o_addr(0), p_addr(0), 16u, v_now, 1u);
+                                mma_commit(&o_full[0]);
+                                if (!wait(&p_full[1], pp1)) break;
+                                mma_sum<D>(o_addr(1), p_addr(1), 16u, v_now, 1u);
+                                mma_commit(&o_full[1]);
+                                mma_commit(&kv_empty[va.s]);
+                            }
+                            ka.step(2);
+                            va.step(2);
+                            sp0 ^= 1u;
+                            sp1 ^= 1u;
+                            pp0 ^= 1u;
+                            pp1 ^= 1u;
+                        }
+                        if (!ok) break;
+                    }
                     auto scores = [&](int w) {  // S_w of tile j
                         if (!ok || j < x.from[w] || j >= x.to[w]) return;
                         if (j == x.from[w] && !wait(&q_full[w], nq[w] & 1u)) return;
@@ -223,8 +278,8 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                         if (!ok || j - 1 < x.from[w] || j - 1 >= x.to[w]) return;
                         if (j - 1 == x.from[w] && nq[w] > 0 && !wait(&o_empty[w], (nq[w] - 1u) & 1u)) return;
                         if (!wait(&p_full[w], np[w] & 1u)) return;
-                        mma_sum<D>(o_addr(w), p_addr(w), 32u, kv_addr(va.s), j - 1 > x.from[w] ? 1u : 0u);
-                        mma_commit(&o_full[w]);
+                        mma_sum<D>(o_addr(w), p_addr(w), 16u, kv_addr(va.s), j - 1 > x.from[w] ? 1u : 0u);
+                        if (!kOverlay || j == x.to[w]) mma_commit(&o_full[w]);
                         ++np[w];
                         if (j == x.to[w]) ++nq[w];
                     };
@@ -252,26 +307,30 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                     if (j < x.jhi) ka.step(2);
                     if (j > x.jlo) va.step(2);
                 }
-                if (ok) block = work_next_one(&queue, k, abortp);
             }
             // every product has ended before tensor memory is given back
             mma_commit(&drain);
             wait_drained(&drain, abortp);
         }
         __syncwarp();
-    } else if (warp < 8) {
+    } else if (warp < W::kRow) {
         // ------------------------------------ softmax -----------------------------------------------------
-        take_registers();
+        W::take_registers();
         const int w = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t st = s_addr(w) + lanes, ot = o_addr(w) + lanes, pt = p_addr(w) + lanes;
         const float c = a.scale_log2;
         const uint64_t c2 = f32x2(c, c);
-        uint32_t cnt = 0;  // tiles so far
+        uint32_t cnt = 0, items = 0, boxes = 0;  // tiles, items with keys, boxes of output so far
+        uint8_t* stage = smem + (size_t)(2 + kStages) * TB + w * kBoxBytes;
         bool ok = true;
-        int block = (int)blockIdx.x;
-        for (uint32_t k = 0; block >= 0; ++k) {
-            const FwdWork x(a, block);
+        auto tell = [&](uint64_t* bar) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+        };
+        FwdWork x;
+        for (uint32_t k = 0; ok && work_take(&queue, k, x, lane, abortp); ++k) {
             const int tw = w ? x.t[1] : x.t[0], hw = w ? x.h[1] : x.h[0], fw = w ? x.from[1] : x.from[0], ew = w ? x.to[1] : x.to[0];
             const int pos = tw * kTile + row;
             const bool live = pos >= x.lo && pos < x.hi && ew > fw;
@@ -285,19 +344,20 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 full_to = tw;
             }
             float mref = -INFINITY, sum = 0.f;
-            for (int j = fw; j < ew && ok; ++j, ++cnt) {
-                ok = wait_all(&s_full[w], cnt & 1u, abortp);
-                if (!ok) break;
+            for (int j = fw; j < ew; ++j, ++cnt) {
+                if (!(ok = wait_all(&s_full[w], cnt & 1u, abortp))) break;
                 tc_fence_after();
+                // The items start together; half a tile's time apart, one is at its exponentials while the other waits, loads and
+                // compares (8 x 4096, 16 heads of 64: 314 -> 305 us; short pieces have no time for it).
+                if (w == 1 && j == fw && ew - fw >= 4) {
+                    const long long t0 = clock64();
+                    while (clock64() - t0 < 900) {}
+                }
                 uint32_t s[4][32];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) tmem_ld32(st + 32u * i, s[i]);
                 tmem_ld_wait();
-                if (!kOverlay) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&s_empty[w]);
-                }
+                if (!kOverlay) tell(&s_empty[w]);
                 if (j < full_from || j >= full_to) {
                     const int first = j * kTile - see;
 #pragma unroll
@@ -308,14 +368,13 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 }
                 float top4[4] = {mref, mref, mref, mref};
 #pragma unroll
-                for (int e = 0; e < 32; ++e)
+                for (int e = 0; e < 32; e += 2)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) top4[i] = fmaxf(top4[i], __uint_as_float(s[i][e]));
+                    for (int i = 0; i < 4; ++i) top4[i] = max3(top4[i], __uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1]));
                 const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
                 // with P in columns of its own, the last product may still be reading them
                 if (!kOverlay && j > fw) {
-                    ok = wait_all(&o_full[w], (cnt - 1u) & 1u, abortp);
-                    if (!ok) break;
+                    if (!(ok = wait_all(&o_full[w], (cnt - 1u) & 1u, abortp))) break;
                     tc_fence_after();
                 }
                 const bool grown = (top - mref) * c > 8.f;  // false where both are -infinity
@@ -361,50 +420,49 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 f32x2_split(f32x2_add(part[0], part[1]), u, v);
                 sum += u + v;
                 tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[w]);
+                tell(&p_full[w]);
             }
             // out = O / sum, lse = max + log(sum)
             if (ok && ew > fw) {
-                ok = wait_all(&o_full[w], (cnt - 1u) & 1u, abortp);
+                ok = wait_all(&o_full[w], (kOverlay ? items : cnt - 1u) & 1u, abortp);
                 tc_fence_after();
+                ++items;
             }
-            if (ok && (w ? x.valid[1] : x.valid[0])) {
-                const bool mine = pos < g.seq_len;
-                uint16_t* dst = a.out + ((int64_t)x.n * g.seq_len + pos) * a.ld_out + hw * g.head_dim;
-                const float inv = live ? 1.f / sum : 0.f;
+            if (!ok || !((x.valid >> w) & 1)) continue;
+            const float inv = live ? 1.f / sum : 0.f;
+            if (ew > fw) {
 #pragma unroll 1
-                for (int i = 0; i < D / 32; ++i) {
-                    float f[32];
-                    if (ew > fw) {
-                        uint32_t o[32];
-                        tmem_ld32(ot + 32u * i, o);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) f[e] = live ? __uint_as_float(o[e]) * inv : 0.f;
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) f[e] = 0.f;
+                for (int box = 0; box < D / 64; ++box) {
+                    // one lane stores the boxes and says when the last one has been read out of shared memory
+                    if ((warp & 3) == 0 && lane == 0 && boxes > 0) {
+                        bulk_wait_read<0>();
+                        mbar_arrive(&out_free[w]);
                     }
-                    if (mine) store_row32(dst, 32 * i, g.head_dim, a.wide, f);
+                    if (boxes > 0 && !(ok = wait_all(&out_free[w], (boxes - 1u) & 1u, abortp))) break;
+                    stage_acc32(stage, row, 0, ot + 64u * box, live, inv);
+                    stage_acc32(stage, row, 1, ot + 64u * box + 32u, live, inv);
+                    fence_proxy_async_smem();
+                    if (box == D / 64 - 1) tell(&o_empty[w]);
+                    tell(&out_staged[w]);
+                    if ((warp & 3) == 0) {
+                        if (!(ok = wait_all(&out_staged[w], boxes & 1u, abortp))) break;
+                        if (lane == 0 && box * 64 < g.head_dim) tma_store_4d(&mo, stage, box * 64, hw, tw * kTile, x.n);
+                        if (lane == 0) bulk_commit();
+                    }
+                    ++boxes;
                 }
-                if (ew > fw) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&o_empty[w]);
-                }
-                if (a.lse && mine)
-                    a.lse[((size_t)x.n * g.heads + hw) * g.seq_len + pos] =
-                        live ? (float)(((double)mref * (double)c + (double)log2f(sum)) * kLn2D) : -INFINITY;
+            } else {
+                zero_tile(a.out, a.ld_out, g.seq_len, g.head_dim, hw, tw * kTile, x.n, row, 128);
             }
-            if (!ok) break;
-            block = work_next(&queue, k, lane, abortp);
+            if (a.lse && pos < g.seq_len)
+                a.lse[((size_t)x.n * g.heads + hw) * g.seq_len + pos] =
+                    live ? (float)(((double)mref * (double)c + (double)log2f(sum)) * kLn2D) : -INFINITY;
         }
+        if ((warp & 3) == 0 && lane == 0) bulk_wait_all<0>();
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == W::kMma) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
@@ -412,12 +470,12 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
 }
 
 template <int D>
-cudaError_t launch_fwd(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const FwdArgs& a, unsigned grid,
-                       cudaStream_t st) {
+cudaError_t launch_fwd(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mo, const FwdArgs& a,
+                       unsigned grid, cudaStream_t st) {
     auto kern = attn_fwd_kernel<D>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FwdCfg<D>::kSmem);
     if (e != cudaSuccess) return e;
-    kern<<<grid, kThreads, FwdCfg<D>::kSmem, st>>>(mq, mk, mv, a);
+    kern<<<grid, W::kThreads, FwdCfg<D>::kSmem, st>>>(mq, mk, mv, mo, a);
     return cudaGetLastError();
 }
 
@@ -476,9 +534,9 @@ extern "C" rapid_status_t rapid_attention_fwd(const rapid_attn_desc_t* desc, con
         return RAPID_ERR_INVALID_ARG;
     int sms = 0;
     if ((s = policy::check_device(&sms)) != RAPID_OK) return s;
-    CUtensorMap mq, mk, mv;
+    CUtensorMap mq, mk, mv, mo;
     if (!make_head_map(&mq, q, d, d.n_heads, d.ld_q) || !make_head_map(&mk, k, d, d.n_kv_heads, d.ld_k) ||
-        !make_head_map(&mv, v, d, d.n_kv_heads, d.ld_v))
+        !make_head_map(&mv, v, d, d.n_kv_heads, d.ld_v) || !make_head_map(&mo, out, d, d.n_heads, d.ld_out))
         return RAPID_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (policy::clear_stats(stats, st) != cudaSuccess) return RAPID_ERR_CUDA;
@@ -487,12 +545,11 @@ extern "C" rapid_status_t rapid_attention_fwd(const rapid_attn_desc_t* desc, con
     a.scale_log2 = (float)(d.scale * kLog2eD);
     a.out = static_cast<uint16_t*>(out);
     a.ld_out = d.ld_out;
-    a.wide = wide_rows(out, d.ld_out, d.head_dim);
     a.lse = lse;
     a.stats = stats;
     a.items = (d.seq_len + kTile - 1) / kTile * a.g.group;
     a.pairs = (a.items + 1) / 2;
     const unsigned grid = (unsigned)((int64_t)a.pairs * d.n_seq * d.n_kv_heads);
-    const cudaError_t e = d.head_dim <= 64 ? launch_fwd<64>(mq, mk, mv, a, grid, st) : launch_fwd<128>(mq, mk, mv, a, grid, st);
+    const cudaError_t e = d.head_dim <= 64 ? launch_fwd<64>(mq, mk, mv, mo, a, grid, st) : launch_fwd<128>(mq, mk, mv, mo, a, grid, st);
     return e == cudaSuccess ? RAPID_OK : RAPID_ERR_CUDA;
 }
