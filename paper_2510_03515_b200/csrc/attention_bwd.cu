@@ -538,7 +538,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     // q_*, do_*, acc_* count pieces of work that have steps, the others steps
-    __shared__ __align__(8) uint64_t q_full, q_empty, do_full, acc_full, acc_empty, staged, s_full[2], dp_full, ds_full, all_done,
+    __shared__ __align__(8) uint64_t q_full, q_empty, do_full, do_empty, acc_full, acc_empty, s_full[2], dp_full, ds_full, all_done, staged[kKeys],
         k_full[kKeys], k_empty[kKeys], k_raw[kKeys], v_full[kVals], v_empty[kVals], v_raw[kVals];
     __shared__ __align__(16) WorkQueue<DqWork> queue;
     __shared__ uint32_t tmem_slot;
@@ -551,7 +551,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         mbar_init(&q_full, 1);
         mbar_init(&q_empty, 1);
         mbar_init(&do_full, 1);
-        mbar_init(&staged, W::kRow);
+        mbar_init(&do_empty, 1);
         mbar_init(&acc_full, 1);
         mbar_init(&acc_empty, W::kRow);
         mbar_init(&s_full[0], 1);
@@ -563,6 +563,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             mbar_init(&k_full[s], 1);
             mbar_init(&k_empty[s], 1);
             mbar_init(&k_raw[s], 1);
+            mbar_init(&staged[s], W::kRow);
         }
         for (uint32_t s = 0; s < kVals; ++s) {
             mbar_init(&v_full[s], 1);
@@ -599,13 +600,22 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             Place<kKeys> ka;
             Place<kVals> va;
             int block = (int)blockIdx.x;
-            DqWork x, last{};
-            // The results of the last piece lie in its dout tile (queries of the next are wanted sooner); they leave before a
-            // new one comes.
-            auto flush = [&] {
-                ok = wait_one(&staged, (ndo - 1u) & 1u, abortp);
+            DqWork x;
+            // The results of a piece are left in the place of its last key tile, the buffer that is wanted again last: they
+            // leave when a new tile is to go there, or at the end.
+            RawParity staged_at;
+            uint32_t pending = 0;  // buffers that hold results
+            int held[kKeys][3];    // whose
+            auto flush = [&](uint32_t s) {
+                if (!((pending >> s) & 1u)) return;
+                pending &= ~(1u << s);
+                ok = wait_one(&staged[s], staged_at.flip(s), abortp);
                 if (!ok) return;
-                store_tile<D>(&mdq, do_tile, g.head_dim, last.h, last.t * kTile, last.n);
+                int h = 0, t = 0, n = 0;
+#pragma unroll
+                for (uint32_t i = 0; i < kKeys; ++i)
+                    if (i == s) h = held[i][0], t = held[i][1], n = held[i][2];
+                store_tile<D>(&mdq, k_tile(s), g.head_dim, h, t * kTile, n);
                 bulk_commit();
                 bulk_wait_read<0>();
             };
@@ -613,7 +623,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 x.set(a, block);
                 if (!(ok = work_put(&queue, k, x, abortp))) break;
                 if (x.end) {
-                    if (ndo > 0) flush();
+                    for (uint32_t i = 0; i < kKeys && ok; ++i, ka.step()) flush(ka.s);  // the oldest first
                     bulk_wait_all<0>();
                     break;
                 }
@@ -629,6 +639,14 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                     const int t0 = (x.from + i) * kTile;
                     const bool clean = dirty(x.from + i, x.lo, x.hi);
                     if (nk >= kKeys && !(ok = wait_one(&k_empty[ka.s], ka.parity ^ 1u, abortp))) break;
+                    flush(ka.s);
+                    if (!ok) break;
+                    if (i + 1 == x.steps) {
+                        pending |= 1u << ka.s;
+#pragma unroll
+                        for (uint32_t b = 0; b < kKeys; ++b)
+                            if (b == ka.s) held[b][0] = x.h, held[b][1] = x.t, held[b][2] = x.n;
+                    }
                     uint64_t* bar = clean ? &k_raw[ka.s] : &k_full[ka.s];
                     k_was_raw = clean ? k_was_raw | (1u << ka.s) : k_was_raw & ~(1u << ka.s);
                     if (clean) kr.flip(ka.s);
@@ -637,9 +655,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                     ++nk;
                     ka.step();
                     if (i == 0) {
-                        if (ndo > 0) flush();
-                        if (!ok) break;
-                        last = x;
+                        if (ndo > 0 && !(ok = wait_one(&do_empty, (ndo - 1u) & 1u, abortp))) break;
                         mbar_arrive_expect_tx(&do_full, TB);
                         load_tile<D>(do_tile, &mdo, x.h, x.t * kTile, x.n, &do_full);
                         ++ndo;
@@ -716,11 +732,12 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 ka.step();
                 ++gs;
             };
-            auto dps = [&] {
+            auto dps = [&](bool last) {
                 if (!ok) return;
                 mma_rows<D>(dp_t, dob, v_addr(va.s));
                 mma_commit(&dp_full);
                 mma_commit(&v_empty[va.s]);
+                if (last) mma_commit(&do_empty);
                 va.step();
             };
             DqWork x;
@@ -730,14 +747,14 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                     scores(x.steps == 1);
                     wait(&do_full, pieces & 1u);
                     wait(&v_full[va.s], va.parity);
-                    dps();
+                    dps(x.steps == 1);
                     if (x.steps > 1) scores(x.steps == 2);
                     if (pieces > 0) wait(&acc_empty, (pieces - 1u) & 1u);
                 }
                 for (int i = 0; i < x.steps && ok; ++i, ++gi) {
                     if (i + 1 < x.steps) wait(&v_full[va.s], va.parity);
                     wait(&ds_full, gi & 1u);  // dP has been read, dS is there
-                    if (i + 1 < x.steps) dps();
+                    if (i + 1 < x.steps) dps(i + 2 == x.steps);
                     if (!ok) break;
                     mma_sum<D>(dq_t, s_addr(gi), 32u, k_addr(kd.s), (uint32_t)i);
                     if (i + 1 == x.steps) mma_commit(&acc_full);
@@ -770,6 +787,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             if (lane == 0) mbar_arrive(bar);
         };
         uint32_t gi = 0, pieces = 0;
+        Place<kKeys> kc;  // the key tile of this step
+        uint32_t key_buf = 0;
         DqWork x;
         for (uint32_t k = 0; work_take(&queue, k, x, lane, abortp); ++k) {
             const int pos = x.t * kTile + row;
@@ -786,6 +805,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             const uint64_t shift2 = f32x2(shift, shift), ndelta2 = f32x2(ndelta, ndelta);
             for (int i = 0; i < x.steps; ++i, ++gi) {
                 const int j = x.from + i;
+                key_buf = kc.s;
+                kc.step();
                 float p[32];
                 uint32_t s[32], b[16];
                 if (!wait(&s_full[gi & 1u], (gi >> 1) & 1u)) break;
@@ -809,10 +830,10 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             if (ok && x.steps > 0) wait(&acc_full, pieces & 1u);
             if (!ok) break;
             if (x.steps > 0) {  // 32 columns each (at D = 64 half of the warps have none)
-                if (part * 32 < D) stage_acc32(do_tile, row, part, dq_t + lanes + 32u * part, live, a.scale);
+                if (part * 32 < D) stage_acc32(k_tile(key_buf), row, part, dq_t + lanes + 32u * part, live, a.scale);
                 fence_proxy_async_smem();
                 tell(&acc_empty);
-                tell(&staged);
+                tell(&staged[key_buf]);
                 ++pieces;
             } else {
                 zero_tile(a.dq, a.ld_dq, g.seq_len, g.head_dim, x.h, x.t * kTile, x.n, part * 128 + row, 512);
