@@ -39,41 +39,57 @@ struct BwdArgs {
 
 // ---- row terms --------------------------------------------------------------------------------------------------
 
-// `lanes` = 2^lanes_log2 lanes take one head of one position, 8 elements each.
+// A block takes kTermRows positions of one generation with all their heads; 2^lanes_log2 lanes take one head of one position,
+// 8 elements each, and have four of them in flight.
+constexpr int kTermRows = 16;
+
 __global__ void __launch_bounds__(256)
 attn_row_terms_kernel(Geometry g, int tiles, int lanes_log2, const uint16_t* __restrict__ out, int64_t ld_out,
                       const uint16_t* __restrict__ dout, int64_t ld_dout, const float* __restrict__ lse, float* __restrict__ shift,
                       float* __restrict__ ndelta) {
-    const int64_t padded = (int64_t)tiles * kTile;
-    const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> lanes_log2;
-    const int u = threadIdx.x & ((1 << lanes_log2) - 1);
-    const int64_t row = unit / g.heads;  // n * padded + t
-    const int h = (int)(unit - row * g.heads);
-    const int n = (int)(row / padded), t = (int)(row - n * padded);
-    bool live = n < g.n_seq && t < g.seq_len;
-    if (live) {
-        int lo, hi;
-        live_range(g, n, lo, hi);
-        live = t >= lo && t < hi;
-    }
-    float sum = 0.f;
-    if (live && u * 8 < g.head_dim) {
-        const int64_t r = (int64_t)n * g.seq_len + t;
-        policy::Vec8<uint16_t> a, b;
-        a.load(out + r * ld_out + h * g.head_dim + u * 8);
-        b.load(dout + r * ld_dout + h * g.head_dim + u * 8);
-        float x[8], y[8];
-        a.get(x);
-        b.get(y);
+    constexpr int kAhead = 4;
+    const int padded = tiles * kTile, blocks = padded / kTermRows;
+    const int n = (int)(blockIdx.x / (unsigned)blocks), t0 = (int)(blockIdx.x % (unsigned)blocks) * kTermRows;
+    int lo, hi;
+    live_range(g, n, lo, hi);
+    const int lane = threadIdx.x & ((1 << lanes_log2) - 1), groups = 256 >> lanes_log2;
+    const int units = kTermRows * g.heads;
+    for (int u0 = 0; u0 < units; u0 += groups * kAhead) {
+        const int first = u0 + (int)(threadIdx.x >> lanes_log2);
+        policy::Vec8<uint16_t> x[kAhead], y[kAhead];
+        int t[kAhead], h[kAhead];
+        bool live[kAhead];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum += x[j] * y[j];
-    }
-    for (int o = 1; o < (1 << lanes_log2); o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (u == 0 && n < g.n_seq) {
-        const int64_t at = ((int64_t)n * g.heads + h) * padded + t;
-        // double: lse * log2(e) in float would shift every score of the row by its own rounding
-        shift[at] = live ? (float)((double)lse[((int64_t)n * g.heads + h) * g.seq_len + t] * -kLog2eD) : -INFINITY;
-        ndelta[at] = -sum;
+        for (int k = 0; k < kAhead; ++k) {
+            const int u = first + k * groups;
+            t[k] = u / g.heads;
+            h[k] = u - t[k] * g.heads;
+            t[k] += t0;
+            live[k] = u < units && t[k] >= lo && t[k] < hi;
+            if (live[k] && lane * 8 < g.head_dim) {
+                const int64_t r = (int64_t)n * g.seq_len + t[k];
+                x[k].load(out + r * ld_out + h[k] * g.head_dim + lane * 8);
+                y[k].load(dout + r * ld_dout + h[k] * g.head_dim + lane * 8);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            float sum = 0.f;
+            if (live[k] && lane * 8 < g.head_dim) {
+                float a[8], b[8];
+                x[k].get(a);
+                y[k].get(b);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum += a[j] * b[j];
+            }
+            for (int o = 1; o < (1 << lanes_log2); o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (lane == 0 && first + k * groups < units) {
+                const int64_t at = ((int64_t)n * g.heads + h[k]) * padded + t[k];
+                // double: lse * log2(e) in float would shift every score of the row by its own rounding
+                shift[at] = live[k] ? (float)((double)lse[((int64_t)n * g.heads + h[k]) * g.seq_len + t[k]] * -kLog2eD) : -INFINITY;
+                ndelta[at] = -sum;
+            }
+        }
     }
 }
 
@@ -953,7 +969,7 @@ extern "C" rapid_status_t rapid_attention_bwd(const rapid_attn_desc_t* desc, con
     a.stats = stats;
     int lanes_log2 = 0;
     while ((8 << lanes_log2) < d.head_dim) ++lanes_log2;
-    const int64_t blocks = (((int64_t)terms << lanes_log2) + 255) / 256;
+    const int64_t blocks = (int64_t)d.n_seq * a.tiles * (kTile / kTermRows);
     if (blocks > 0x7fffffffll) return RAPID_ERR_UNSUPPORTED;
     attn_row_terms_kernel<<<(unsigned)blocks, 256, 0, st>>>(a.g, a.tiles, lanes_log2, static_cast<const uint16_t*>(out), d.ld_out,
                                                             static_cast<const uint16_t*>(dout), d.ld_dout, lse, shift, ndelta);
