@@ -7,6 +7,7 @@ There is no fallback: if the shared library is missing the first call raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 import os
 from dataclasses import dataclass
@@ -380,27 +381,22 @@ def _dtype_code(dtype: torch.dtype) -> int:
     raise TypeError(f"float32 or bfloat16 expected, got {dtype}")
 
 
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise ValueError(what)
-
-
-def _one_device(*tensors: Optional[torch.Tensor]) -> torch.device:
-    """The CUDA device that all the tensors lie on."""
-    dev = None
-    for t in tensors:
-        if t is None:
-            continue
-        _need(t.is_cuda, "tensors must be CUDA tensors")
-        _need(dev is None or t.device == dev, "tensors lie on different devices")
-        dev = t.device
-    return dev
+def _one_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
+    """Number of the CUDA device that all the tensors lie on."""
+    index = first.get_device()
+    if index < 0:
+        raise ValueError("tensors must be CUDA tensors")
+    for t in others:
+        if t is not None and t.get_device() != index:
+            raise ValueError("tensors must be CUDA tensors of one device")
+    return index
 
 
 def _vector(t: Optional[torch.Tensor], n: int, dtype, name: str) -> None:
     if t is None:
         return
-    _need(t.numel() == n and t.is_contiguous(), f"{name}: {n} contiguous elements expected")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: {n} contiguous elements expected")
     if t.dtype != dtype:
         raise TypeError(f"{name}: {dtype} expected, got {t.dtype}")
 
@@ -416,22 +412,27 @@ def _mask8(mask: Optional[torch.Tensor], n: int) -> Optional[torch.Tensor]:
 
 def _pitch(t: torch.Tensor, name: str) -> int:
     """Row pitch of a matrix [rows, cols] or of rows of heads [rows, heads, head_dim]."""
-    inner = t.stride(-1) == 1 or t.shape[-1] == 1
-    if t.dim() == 3:
-        inner = inner and (t.shape[1] == 1 or t.stride(1) == t.shape[2])
-    width = t.shape[-1] * (t.shape[1] if t.dim() == 3 else 1)
-    _need(inner, f"{name}: the elements of a row must lie side by side")
-    if t.shape[0] == 1:  # one row has no pitch: the narrowest that 16-byte rows allow
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 3:
+        rows, heads, dim = shape
+        inner = (stride[2] == 1 or dim == 1) and (stride[1] == dim or heads == 1)
+        width = heads * dim
+    else:
+        rows, width = shape
+        inner = stride[1] == 1 or width == 1
+    if not inner:
+        raise ValueError(f"{name}: the elements of a row must lie side by side")
+    if rows == 1:  # one row has no pitch: the narrowest that 16-byte rows allow
         step = 16 // t.element_size()
         return -(-width // step) * step
-    return t.stride(0)
+    return stride[0]
 
 
 def _matrix(rows: int, cols: int, dtype, device) -> torch.Tensor:
     """An uninitialised [rows, cols] whose rows begin on 16-byte boundaries."""
-    step = 16 // torch.empty(0, dtype=dtype).element_size()
+    step = 16 // dtype.itemsize
     pitch = -(-cols // step) * step
-    buf = torch.empty(rows, pitch, dtype=dtype, device=device)
+    buf = torch.empty((rows, pitch), dtype=dtype, device=device)
     return buf if pitch == cols else buf[:, :cols]
 
 
@@ -439,17 +440,18 @@ def _like(out: Optional[torch.Tensor], x: torch.Tensor, name: str) -> torch.Tens
     """`out`, or a contiguous tensor of x's shape and type where there is none."""
     if out is None:
         return torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _need(out.shape == x.shape, f"{name}: shape {tuple(x.shape)} expected")
+    if out.shape != x.shape:
+        raise ValueError(f"{name}: shape {tuple(x.shape)} expected")
     if out.dtype != x.dtype:
         raise TypeError(f"{name}: {x.dtype} expected, got {out.dtype}")
     return out
 
 
 class _on:
-    """Make `device` current for the calls inside (nothing to do when it is already)."""
+    """Make device number `index` current for the calls inside (nothing to do when it is already)."""
 
-    def __init__(self, device: torch.device):
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    def __init__(self, index: int):
+        self.guard = None if index == torch.cuda.current_device() else torch.cuda.device(index)
 
     def __enter__(self):
         if self.guard is not None:
@@ -460,6 +462,48 @@ class _on:
             self.guard.__exit__(*exc)
 
 
+# torch.cuda.current_stream() builds an object for each call, 3 us; torch's own generated code asks for the bare handle.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_here() -> int:
+    """Handle of the current device's current stream."""
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
+
+
+def _addr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _workspace(query, desc, where: str) -> int:
+    n = C.c_size_t(0)
+    _check(query(C.byref(desc), C.byref(n)), where)
+    return int(n.value)
+
+
+# Descriptors by their values, with the workspace size where one is needed: shapes repeat from call to call, and building a
+# descriptor of 17 fields takes longer than a small kernel.  Only the convenience functions use these, and never change them.
+
+@functools.lru_cache(maxsize=512)
+def _embed_plan(n_rows, vocab, dim, dtype, ld_table, ld_rows, scale, flags, bwd):
+    desc = make_embed_desc(n_rows, vocab, dim, dtype, ld_table, ld_rows, scale, flags)
+    return desc, rapid_embedding_bwd_workspace_bytes(desc) if bwd else 0
+
+
+@functools.lru_cache(maxsize=512)
+def _qk_plan(n_seq, seq_len, hq, hk, hd, dtype, rot, pitches, eps, flags, bwd):
+    desc = make_qk_desc(n_seq, seq_len, hq, hk, hd, dtype, rot, *pitches, eps=eps, flags=flags)
+    return desc, rapid_qk_norm_rope_bwd_workspace_bytes(desc) if bwd and not flags & QK_NO_NORM else 0
+
+
+@functools.lru_cache(maxsize=512)
+def _attn_plan(n_seq, seq_len, h, hk, hd, window, scale, pitches, bwd):
+    desc = make_attn_desc(n_seq, seq_len, h, hk, hd, window, scale, *pitches)
+    return desc, rapid_attention_bwd_workspace_bytes(desc) if bwd else 0
+
+
 def make_embed_desc(n_rows: int, vocab: int, dim: int, dtype: torch.dtype, ld_table: Optional[int] = None,
                     ld_rows: Optional[int] = None, scale: float = 1.0, flags: int = 0) -> EmbedDesc:
     return EmbedDesc(n_rows, vocab, dim, dim if ld_table is None else ld_table, dim if ld_rows is None else ld_rows,
@@ -468,37 +512,37 @@ def make_embed_desc(n_rows: int, vocab: int, dim: int, dtype: torch.dtype, ld_ta
 
 def rapid_embedding_fwd(desc: EmbedDesc, tokens: torch.Tensor, mask: Optional[torch.Tensor], table: torch.Tensor,
                         out: torch.Tensor, stats: Optional[torch.Tensor]) -> None:
-    _check(lib().rapid_embedding_fwd(C.byref(desc), _ptr(tokens), _ptr(mask), _ptr(table), _ptr(out), _ptr(stats),
-                                     _stream()), "rapid_embedding_fwd")
+    _check(lib().rapid_embedding_fwd(C.byref(desc), _addr(tokens), _addr(mask), _addr(table), _addr(out), _addr(stats),
+                                     _stream_here()), "rapid_embedding_fwd")
 
 
 def rapid_embedding_bwd_workspace_bytes(desc: EmbedDesc) -> int:
-    n = C.c_size_t(0)
-    _check(lib().rapid_embedding_bwd_workspace_bytes(C.byref(desc), C.byref(n)), "rapid_embedding_bwd_workspace_bytes")
-    return int(n.value)
+    return _workspace(lib().rapid_embedding_bwd_workspace_bytes, desc, "rapid_embedding_bwd_workspace_bytes")
 
 
 def rapid_embedding_bwd(desc: EmbedDesc, tokens: torch.Tensor, mask: Optional[torch.Tensor], dout: torch.Tensor,
                         dtable: torch.Tensor, workspace: torch.Tensor) -> None:
-    _check(lib().rapid_embedding_bwd(C.byref(desc), _ptr(tokens), _ptr(mask), _ptr(dout), _ptr(dtable), _ptr(workspace),
-                                     workspace.numel(), _stream()), "rapid_embedding_bwd")
+    _check(lib().rapid_embedding_bwd(C.byref(desc), _addr(tokens), _addr(mask), _addr(dout), _addr(dtable), _addr(workspace),
+                                     workspace.numel(), _stream_here()), "rapid_embedding_bwd")
 
 
 def embedding(table: torch.Tensor, tokens: torch.Tensor, mask: Optional[torch.Tensor] = None, scale: float = 1.0,
               stats: Optional[torch.Tensor] = None) -> torch.Tensor:
     """scale * table[tokens], [T, D] in the table's type; rows that are masked or whose token is no row of the table are
     zeros.  tokens [T] int32, table [V, D] (rows on 16-byte boundaries)."""
-    _need(table.dim() == 2, "table: a matrix [V, D] expected")
+    if table.dim() != 2:
+        raise ValueError("table: a matrix [V, D] expected")
     T, (V, D) = tokens.numel(), table.shape
     mask = _mask8(mask, T)
     _vector(tokens, T, torch.int32, "tokens")
     dev = _one_device(table, tokens, mask, stats)
-    if T == 0:
-        return _matrix(0, D, table.dtype, dev)
     with _on(dev):
-        out = _matrix(T, D, table.dtype, dev)
-        desc = make_embed_desc(T, V, D, table.dtype, _pitch(table, "table"), _pitch(out, "out"), scale)
-        rapid_embedding_fwd(desc, tokens, mask, table, out, stats)
+        out = _matrix(T, D, table.dtype, table.device)
+        if T:
+            desc, _ = _embed_plan(T, V, D, table.dtype, _pitch(table, "table"), _pitch(out, "out"), scale, 0, False)
+            rapid_embedding_fwd(desc, tokens, mask, table, out, stats)
+        elif stats is not None:
+            stats.zero_()
     return out
 
 
@@ -506,13 +550,15 @@ def embedding_grad(dout: torch.Tensor, tokens: torch.Tensor, mask: Optional[torc
                    dtable_dtype: torch.dtype = torch.float32, dtable: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The gradient of embedding() with respect to its table: [vocab, D] in `dtable_dtype`, or added to `dtable`, which
     is then returned (its type counts, not `dtable_dtype`)."""
-    _need(dout.dim() == 2, "dout: a matrix [T, D] expected")
+    if dout.dim() != 2:
+        raise ValueError("dout: a matrix [T, D] expected")
     T, D = dout.shape
     mask = _mask8(mask, T)
     _vector(tokens, T, torch.int32, "tokens")
     flags = 0
     if dtable is not None:
-        _need(tuple(dtable.shape) == (vocab, D), "dtable: [vocab, D] expected")
+        if tuple(dtable.shape) != (vocab, D):
+            raise ValueError("dtable: [vocab, D] expected")
         dtable_dtype, flags = dtable.dtype, EMBED_ACCUMULATE
     if _dtype_code(dtable_dtype) == RAPID_BF16:
         if dout.dtype != torch.bfloat16:
@@ -521,10 +567,10 @@ def embedding_grad(dout: torch.Tensor, tokens: torch.Tensor, mask: Optional[torc
     dev = _one_device(dout, tokens, mask, dtable)
     with _on(dev):
         if T == 0:
-            return torch.zeros(vocab, D, dtype=dtable_dtype, device=dev) if dtable is None else dtable
-        out = _matrix(vocab, D, dtable_dtype, dev) if dtable is None else dtable
-        desc = make_embed_desc(T, vocab, D, dout.dtype, _pitch(out, "dtable"), _pitch(dout, "dout"), scale, flags)
-        ws = torch.empty(rapid_embedding_bwd_workspace_bytes(desc), dtype=torch.uint8, device=dev)
+            return torch.zeros(vocab, D, dtype=dtable_dtype, device=dout.device) if dtable is None else dtable
+        out = _matrix(vocab, D, dtable_dtype, dout.device) if dtable is None else dtable
+        desc, ws_bytes = _embed_plan(T, vocab, D, dout.dtype, _pitch(out, "dtable"), _pitch(dout, "dout"), scale, flags, True)
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dout.device)
         rapid_embedding_bwd(desc, tokens, mask, dout, out, ws)
     return out
 
@@ -542,15 +588,13 @@ def make_qk_desc(n_seq: int, seq_len: int, n_q_heads: int, n_k_heads: int, head_
 def rapid_qk_norm_rope_fwd(desc: QkDesc, q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Tensor],
                            k_weight: Optional[torch.Tensor], inv_freq: torch.Tensor, positions: Optional[torch.Tensor],
                            mask: Optional[torch.Tensor], q_out: torch.Tensor, k_out: torch.Tensor) -> None:
-    _check(lib().rapid_qk_norm_rope_fwd(C.byref(desc), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq),
-                                        _ptr(positions), _ptr(mask), _ptr(q_out), _ptr(k_out), _stream()),
+    _check(lib().rapid_qk_norm_rope_fwd(C.byref(desc), _addr(q), _addr(k), _addr(q_weight), _addr(k_weight), _addr(inv_freq),
+                                        _addr(positions), _addr(mask), _addr(q_out), _addr(k_out), _stream_here()),
            "rapid_qk_norm_rope_fwd")
 
 
 def rapid_qk_norm_rope_bwd_workspace_bytes(desc: QkDesc) -> int:
-    n = C.c_size_t(0)
-    _check(lib().rapid_qk_norm_rope_bwd_workspace_bytes(C.byref(desc), C.byref(n)), "rapid_qk_norm_rope_bwd_workspace_bytes")
-    return int(n.value)
+    return _workspace(lib().rapid_qk_norm_rope_bwd_workspace_bytes, desc, "rapid_qk_norm_rope_bwd_workspace_bytes")
 
 
 def rapid_qk_norm_rope_bwd(desc: QkDesc, q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Tensor],
@@ -559,22 +603,22 @@ def rapid_qk_norm_rope_bwd(desc: QkDesc, q: torch.Tensor, k: torch.Tensor, q_wei
                            dk: torch.Tensor, dq_weight: Optional[torch.Tensor], dk_weight: Optional[torch.Tensor],
                            workspace: Optional[torch.Tensor]) -> None:
     _check(lib().rapid_qk_norm_rope_bwd(
-        C.byref(desc), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq), _ptr(positions), _ptr(mask),
-        _ptr(dq_out), _ptr(dk_out), _ptr(dq), _ptr(dk), _ptr(dq_weight), _ptr(dk_weight), _ptr(workspace),
-        0 if workspace is None else workspace.numel(), _stream()), "rapid_qk_norm_rope_bwd")
+        C.byref(desc), _addr(q), _addr(k), _addr(q_weight), _addr(k_weight), _addr(inv_freq), _addr(positions), _addr(mask),
+        _addr(dq_out), _addr(dk_out), _addr(dq), _addr(dk), _addr(dq_weight), _addr(dk_weight), _addr(workspace),
+        0 if workspace is None else workspace.numel(), _stream_here()), "rapid_qk_norm_rope_bwd")
 
 
 def _qk_args(q, k, q_weight, k_weight, inv_freq, n_seq, seq_len, positions, mask, flags):
     T = n_seq * seq_len
-    _need(q.dim() == 3 and k.dim() == 3 and q.shape[0] == T and k.shape[0] == T and q.shape[2] == k.shape[2],
-          "q, k: [n_seq * seq_len, heads, head_dim] expected")
+    if q.dim() != 3 or k.dim() != 3 or q.shape[0] != T or k.shape[0] != T or q.shape[2] != k.shape[2]:
+        raise ValueError("q, k: [n_seq * seq_len, heads, head_dim] expected")
     if q.dtype != k.dtype:
         raise TypeError("q and k must have one type")
     hd = q.shape[2]
     if flags & QK_NO_NORM:
         q_weight = k_weight = None
-    else:
-        _need(q_weight is not None and k_weight is not None, "weights are needed unless QK_NO_NORM is set")
+    elif q_weight is None or k_weight is None:
+        raise ValueError("weights are needed unless QK_NO_NORM is set")
     _vector(q_weight, hd, torch.float32, "q_weight")
     _vector(k_weight, hd, torch.float32, "k_weight")
     _vector(inv_freq, inv_freq.numel(), torch.float32, "inv_freq")
@@ -590,12 +634,11 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Tens
     q_weight, k_weight, mask = _qk_args(q, k, q_weight, k_weight, inv_freq, n_seq, seq_len, positions, mask, flags)
     dev = _one_device(q, k, q_weight, k_weight, inv_freq, positions, mask)
     with _on(dev):
-        q_out, k_out = torch.empty(q.shape, dtype=q.dtype, device=dev), torch.empty(k.shape, dtype=k.dtype, device=dev)
-        if q.shape[0] == 0:
-            return q_out, k_out
-        desc = make_qk_desc(n_seq, seq_len, q.shape[1], k.shape[1], q.shape[2], q.dtype, 2 * inv_freq.numel(), _pitch(q, "q"),
-                            _pitch(k, "k"), eps=eps, flags=flags)
-        rapid_qk_norm_rope_fwd(desc, q, k, q_weight, k_weight, inv_freq, positions, mask, q_out, k_out)
+        q_out, k_out = torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        if q.shape[0]:
+            desc, _ = _qk_plan(n_seq, seq_len, q.shape[1], k.shape[1], q.shape[2], q.dtype, 2 * inv_freq.numel(),
+                               (_pitch(q, "q"), _pitch(k, "k")), eps, flags, False)
+            rapid_qk_norm_rope_fwd(desc, q, k, q_weight, k_weight, inv_freq, positions, mask, q_out, k_out)
     return q_out, k_out
 
 
@@ -614,7 +657,8 @@ def qk_norm_rope_grad(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch
     """The gradient of qk_norm_rope() from its inputs and the gradients of its outputs.  dq and dk may be given (slices of the
     gradient of one projection, say, or dq_out and dk_out themselves)."""
     q_weight, k_weight, mask = _qk_args(q, k, q_weight, k_weight, inv_freq, n_seq, seq_len, positions, mask, flags)
-    _need(dq_out.shape == q.shape and dk_out.shape == k.shape, "dq_out, dk_out: the shapes of q and k expected")
+    if dq_out.shape != q.shape or dk_out.shape != k.shape:
+        raise ValueError("dq_out, dk_out: the shapes of q and k expected")
     if dq_out.dtype != q.dtype or dk_out.dtype != k.dtype:
         raise TypeError("dq_out and dk_out must have the type of q and k")
     dev = _one_device(q, k, q_weight, k_weight, inv_freq, positions, mask, dq_out, dk_out, dq, dk)
@@ -622,15 +666,17 @@ def qk_norm_rope_grad(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch
         T, hq, hd = q.shape
         hk = k.shape[1]
         dq, dk = _like(dq, q, "dq"), _like(dk, k, "dk")
-        norm = not flags & QK_NO_NORM
-        dw = torch.empty(2, hd, device=dev) if norm else (None, None)
+        dw = (None, None) if flags & QK_NO_NORM else torch.empty((2, hd), dtype=torch.float32, device=q.device).unbind(0)
         if T == 0:
-            return QkGrads(dq, dk, *(x.zero_() for x in dw)) if norm else QkGrads(dq, dk, None, None)
-        desc = make_qk_desc(n_seq, seq_len, hq, hk, hd, q.dtype, 2 * inv_freq.numel(), _pitch(q, "q"), _pitch(k, "k"),
-                            _pitch(dq_out, "dq_out"), _pitch(dk_out, "dk_out"), _pitch(dq, "dq"), _pitch(dk, "dk"), eps, flags)
-        ws = torch.empty(rapid_qk_norm_rope_bwd_workspace_bytes(desc), dtype=torch.uint8, device=dev) if norm else None
+            for x in dw:
+                if x is not None:
+                    x.zero_()
+            return QkGrads(dq, dk, *dw)
+        pitches = (_pitch(q, "q"), _pitch(k, "k"), _pitch(dq_out, "dq_out"), _pitch(dk_out, "dk_out"), _pitch(dq, "dq"), _pitch(dk, "dk"))
+        desc, ws_bytes = _qk_plan(n_seq, seq_len, hq, hk, hd, q.dtype, 2 * inv_freq.numel(), pitches, eps, flags, True)
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device) if ws_bytes else None
         rapid_qk_norm_rope_bwd(desc, q, k, q_weight, k_weight, inv_freq, positions, mask, dq_out, dk_out, dq, dk, dw[0], dw[1], ws)
-    return QkGrads(dq, dk, dw[0], dw[1])
+    return QkGrads(dq, dk, *dw)
 
 
 def make_attn_desc(n_seq: int, seq_len: int, n_heads: int, n_kv_heads: int, head_dim: int, window: int = 0,
@@ -647,28 +693,26 @@ def make_attn_desc(n_seq: int, seq_len: int, n_heads: int, n_kv_heads: int, head
 
 def rapid_attention_fwd(desc: AttnDesc, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, bounds: Optional[torch.Tensor],
                         out: torch.Tensor, lse: Optional[torch.Tensor], stats: Optional[torch.Tensor]) -> None:
-    _check(lib().rapid_attention_fwd(C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(bounds), _ptr(out), _ptr(lse), _ptr(stats),
-                                     _stream()), "rapid_attention_fwd")
+    _check(lib().rapid_attention_fwd(C.byref(desc), _addr(q), _addr(k), _addr(v), _addr(bounds), _addr(out), _addr(lse), _addr(stats),
+                                     _stream_here()), "rapid_attention_fwd")
 
 
 def rapid_attention_bwd_workspace_bytes(desc: AttnDesc) -> int:
-    n = C.c_size_t(0)
-    _check(lib().rapid_attention_bwd_workspace_bytes(C.byref(desc), C.byref(n)), "rapid_attention_bwd_workspace_bytes")
-    return int(n.value)
+    return _workspace(lib().rapid_attention_bwd_workspace_bytes, desc, "rapid_attention_bwd_workspace_bytes")
 
 
 def rapid_attention_bwd(desc: AttnDesc, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, bounds: Optional[torch.Tensor],
                         out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor,
                         dv: torch.Tensor, stats: Optional[torch.Tensor], workspace: torch.Tensor) -> None:
     _check(lib().rapid_attention_bwd(
-        C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(bounds), _ptr(out), _ptr(lse), _ptr(dout), _ptr(dq), _ptr(dk), _ptr(dv),
-        _ptr(stats), _ptr(workspace), workspace.numel(), _stream()), "rapid_attention_bwd")
+        C.byref(desc), _addr(q), _addr(k), _addr(v), _addr(bounds), _addr(out), _addr(lse), _addr(dout), _addr(dq), _addr(dk), _addr(dv),
+        _addr(stats), _addr(workspace), workspace.numel(), _stream_here()), "rapid_attention_bwd")
 
 
 def _attn_args(q, k, v, n_seq, seq_len, bounds):
     T = n_seq * seq_len
-    _need(q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and q.shape[0] == T and k.shape[0] == T and q.shape[2] == k.shape[2],
-          "q: [n_seq * seq_len, heads, head_dim], k, v: [n_seq * seq_len, kv_heads, head_dim] expected")
+    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or q.shape[0] != T or k.shape[0] != T or q.shape[2] != k.shape[2]:
+        raise ValueError("q: [n_seq * seq_len, heads, head_dim], k, v: [n_seq * seq_len, kv_heads, head_dim] expected")
     if not q.dtype == k.dtype == v.dtype == torch.bfloat16:
         raise TypeError("q, k and v must be bfloat16")
     _vector(bounds, 2 * n_seq, torch.int32, "bounds")
@@ -682,13 +726,14 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_seq: int, seq
     _attn_args(q, k, v, n_seq, seq_len, bounds)
     dev = _one_device(q, k, v, bounds, stats)
     with _on(dev):
-        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-        lse = torch.empty(n_seq, q.shape[1], seq_len, device=dev)
-        if q.shape[0] == 0:
-            return out, lse
-        desc = make_attn_desc(n_seq, seq_len, q.shape[1], k.shape[1], q.shape[2], window, scale, _pitch(q, "q"), _pitch(k, "k"),
-                              _pitch(v, "v"))
-        rapid_attention_fwd(desc, q, k, v, bounds, out, lse, stats)
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        lse = torch.empty((n_seq, q.shape[1], seq_len), dtype=torch.float32, device=q.device)
+        if q.shape[0]:
+            desc, _ = _attn_plan(n_seq, seq_len, q.shape[1], k.shape[1], q.shape[2], window, scale,
+                                 (_pitch(q, "q"), _pitch(k, "k"), _pitch(v, "v")), False)
+            rapid_attention_fwd(desc, q, k, v, bounds, out, lse, stats)
+        elif stats is not None:
+            stats.zero_()
     return out, lse
 
 
@@ -706,18 +751,20 @@ def attention_grad(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch
     """The gradient of attention() from its inputs, its outputs out and lse, and the gradient of out.  dq, dk and dv may be
     given (slices of the gradient of one projection, say)."""
     _attn_args(q, k, v, n_seq, seq_len, bounds)
-    _need(out.shape == q.shape and dout.shape == q.shape, "out, dout: the shape of q expected")
+    if out.shape != q.shape or dout.shape != q.shape:
+        raise ValueError("out, dout: the shape of q expected")
     if not out.dtype == dout.dtype == torch.bfloat16:
         raise TypeError("out and dout must be bfloat16")
     _vector(lse, q.shape[0] * q.shape[1], torch.float32, "lse")
     dev = _one_device(q, k, v, out, lse, dout, bounds, stats, dq, dk, dv)
     with _on(dev):
         dq, dk, dv = _like(dq, q, "dq"), _like(dk, k, "dk"), _like(dv, v, "dv")
-        if q.shape[0] == 0:
-            return AttnGrads(dq, dk, dv)
-        desc = make_attn_desc(n_seq, seq_len, q.shape[1], k.shape[1], q.shape[2], window, scale, _pitch(q, "q"), _pitch(k, "k"),
-                              _pitch(v, "v"), _pitch(out, "out"), _pitch(dout, "dout"), _pitch(dq, "dq"), _pitch(dk, "dk"),
-                              _pitch(dv, "dv"))
-        ws = torch.empty(rapid_attention_bwd_workspace_bytes(desc), dtype=torch.uint8, device=dev)
-        rapid_attention_bwd(desc, q, k, v, bounds, out, lse, dout, dq, dk, dv, stats, ws)
+        if q.shape[0]:
+            pitches = (_pitch(q, "q"), _pitch(k, "k"), _pitch(v, "v"), _pitch(out, "out"), _pitch(dout, "dout"), _pitch(dq, "dq"),
+                       _pitch(dk, "dk"), _pitch(dv, "dv"))
+            desc, ws_bytes = _attn_plan(n_seq, seq_len, q.shape[1], k.shape[1], q.shape[2], window, scale, pitches, True)
+            ws = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+            rapid_attention_bwd(desc, q, k, v, bounds, out, lse, dout, dq, dk, dv, stats, ws)
+        elif stats is not None:
+            stats.zero_()
     return AttnGrads(dq, dk, dv)
