@@ -55,7 +55,7 @@ typedef struct rapid_embed_desc {
 rapid_status_t rapid_embedding_fwd(const rapid_embed_desc_t* desc, const int32_t* tokens, const uint8_t* mask,
                                    const void* table, void* out, rapid_stats_t* stats, void* stream);
 
-/* Scratch of rapid_embedding_bwd: 16 bytes a row, four bytes per 32 elements of dout, and a few hundred KB. */
+/* Scratch of rapid_embedding_bwd: 32 bytes a row at most, 4 bytes a token, 4 bytes per 32 elements of dout, and 128 KB. */
 rapid_status_t rapid_embedding_bwd_workspace_bytes(const rapid_embed_desc_t* desc, size_t* bytes);
 
 /*

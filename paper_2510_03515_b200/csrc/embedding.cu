@@ -7,11 +7,13 @@
 // token with a stable radix sort (9-bit digits, written here), so a token's rows lie next to each other in row order, and
 // every sum has a fixed order.  Frequent tokens (a few per cent of all rows each) would keep one warp busy for long, so any
 // 32 sorted positions [32 j, 32 j + 32) that hold one token are summed first, by a warp of their own; a row of dtable
-// is then at most 31 rows + the pieces + 31 rows.  Rows of dtable are dealt out interleaved over the blocks because the
-// frequent tokens have neighbouring numbers in most vocabularies.
+// is then at most 31 rows + the pieces + 31 rows.  The last kernel writes dtable: most of its rows belong to tokens that do
+// not occur, and one warp of each block writes those as bulk copies of zeros out of shared memory, which needs no registers
+// and hardly an instruction, while the other warps sum.
 #include <math.h>
 
 #include "policy_ops.cuh"
+#include "tma_pipe.cuh"
 
 namespace rapid {
 namespace policy {
@@ -73,8 +75,9 @@ embed_fwd_kernel(int64_t n_rows, int segs, int vocab, int dim, int64_t ld_table,
 
 constexpr int kRadixBits = 9, kBins = 1 << kRadixBits;
 constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;  // one thread a digit value
-constexpr int kMaxSortBlocks = 128;
-constexpr int kMinSortRows = 512;
+constexpr int kMaxSortBlocks = 64;  // every block reads the histograms of all
+constexpr int kMinSortRows = 1024;
+constexpr int64_t kOneBlockRows = 16384;
 
 // The rows of block b are [b * per_block, (b + 1) * per_block); within it warp w has a run of per_block / 16 of them.
 struct SortShape {
@@ -86,7 +89,7 @@ inline SortShape sort_shape(int64_t n_rows, int32_t vocab) {
     SortShape s;
     s.n_rows = n_rows;
     // one block does not need the histograms of others and finishes in one launch
-    const int64_t want = n_rows <= 4096 ? 1 : (n_rows + kMinSortRows - 1) / kMinSortRows;
+    const int64_t want = n_rows <= kOneBlockRows ? 1 : (n_rows + kMinSortRows - 1) / kMinSortRows;
     s.blocks = (int)(want < kMaxSortBlocks ? want : kMaxSortBlocks);
     s.per_block = (n_rows + s.blocks - 1) / s.blocks;
     s.per_block = (s.per_block + kSortThreads - 1) / kSortThreads * kSortThreads;  // whole warps' runs
@@ -106,6 +109,7 @@ struct SortArgs {
     uint32_t* key_out;
     uint32_t* row_out;
     uint32_t* hist;  // [blocks][kBins]
+    uint32_t* used;  // counter of the tokens that occur, cleared by the first launch
     int shift;
 };
 
@@ -118,6 +122,7 @@ __device__ __forceinline__ uint32_t sort_key(const SortArgs& a, int64_t i) {
 
 __global__ void __launch_bounds__(kSortThreads) sort_hist_kernel(SortArgs a, SortShape s) {
     __shared__ uint32_t bins[kBins];
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.used = 0;
     bins[threadIdx.x] = 0;
     __syncthreads();
     const int64_t lo = (int64_t)blockIdx.x * s.per_block, hi = min(lo + s.per_block, s.n_rows);
@@ -203,6 +208,7 @@ __global__ void __launch_bounds__(kSortThreads)
 sort_one_block_kernel(SortArgs a, SortShape s, uint32_t* key_a, uint32_t* row_a, uint32_t* key_b, uint32_t* row_b) {
     __shared__ uint32_t cnt[kSortWarps][kBins];
     __shared__ uint32_t scan[kSortWarps];
+    if (threadIdx.x == 0) *a.used = 0;
     for (int p = 0; p < s.passes; ++p) {
         a.shift = p * kRadixBits;
         a.key_in = p == 0 ? nullptr : (p & 1) ? key_a : key_b;
@@ -216,26 +222,29 @@ sort_one_block_kernel(SortArgs a, SortShape s, uint32_t* key_a, uint32_t* row_a,
 
 // ---- sums over a token's rows -------------------------------------------------------------------------------
 
-constexpr int kPiece = 32;       // sorted positions of a piece
-constexpr int kVecs = 2;         // vectors of 8 columns a lane sums
-constexpr int kSeg = kVecs * 256;  // columns a warp sums
-constexpr int kRowsPerBlock = 8;   // rows of dtable a block writes
-constexpr int kAhead = 4;          // rows of dout in flight
+constexpr int kPiece = 32;  // sorted positions of a piece
+constexpr int kAhead = 8;   // rows of dout in flight
+
+// columns a warp sums: two vectors of 8 a lane in bf16, one in float (the loads in flight take the same registers)
+template <class T>
+constexpr int kVecs = sizeof(T) == 2 ? 2 : 1;
+template <class T>
+constexpr int kSeg = kVecs<T> * 256;
 
 // acc += rows of dout at sorted positions [lo, hi), in order
 template <class T>
-__device__ __forceinline__ void add_rows(float (&acc)[kVecs][8], const uint32_t* __restrict__ rows, int64_t lo, int64_t hi,
+__device__ __forceinline__ void add_rows(float (&acc)[kVecs<T>][8], const uint32_t* __restrict__ rows, int64_t lo, int64_t hi,
                                          const T* __restrict__ dout, int64_t ld, int c0, int dim, int lane) {
     for (int64_t i0 = lo; i0 < hi; i0 += 32) {
         const int n = (int)min((int64_t)32, hi - i0);
         const uint32_t mine = lane < n ? rows[i0 + lane] : 0u;
         for (int i = 0; i < n; i += kAhead) {
-            Vec8<T> v[kAhead][kVecs];
+            Vec8<T> v[kAhead][kVecs<T>];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const T* src = dout + (int64_t)__shfl_sync(0xffffffffu, mine, min(i + u, n - 1)) * ld;
 #pragma unroll
-                for (int k = 0; k < kVecs; ++k) {
+                for (int k = 0; k < kVecs<T>; ++k) {
                     const int c = c0 + k * 256;
                     if (i + u < n && c + 8 <= dim) v[u][k].load(src + c);
                 }
@@ -245,7 +254,7 @@ __device__ __forceinline__ void add_rows(float (&acc)[kVecs][8], const uint32_t*
                 const T* src = dout + (int64_t)__shfl_sync(0xffffffffu, mine, min(i + u, n - 1)) * ld;
                 if (i + u < n) {
 #pragma unroll
-                    for (int k = 0; k < kVecs; ++k) {
+                    for (int k = 0; k < kVecs<T>; ++k) {
                         const int c = c0 + k * 256;
                         if (c + 8 <= dim) {
                             float f[8];
@@ -264,69 +273,128 @@ __device__ __forceinline__ void add_rows(float (&acc)[kVecs][8], const uint32_t*
     }
 }
 
-template <class T>
-__global__ void __launch_bounds__(256)
-embed_pieces_kernel(int64_t n_rows, int segs, int dim, int64_t ld, int vocab, const uint32_t* __restrict__ keys,
-                    const uint32_t* __restrict__ rows, const T* __restrict__ dout, float* __restrict__ pieces, int64_t ldp) {
-    const int lane = threadIdx.x & 31;
-    const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int64_t piece = unit / segs;
-    const int64_t lo = piece * kPiece, hi = lo + kPiece;
-    if (hi > n_rows) return;  // whole pieces only
-    const uint32_t key = keys[lo];
-    if (key != keys[hi - 1] || key >= (uint32_t)vocab) return;
-    const int c0 = (int)(unit - piece * segs) * kSeg + lane * 8;
-    float acc[kVecs][8] = {};
-    add_rows(acc, rows, lo, hi, dout, ld, c0, dim, lane);
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k)
-        if (c0 + k * 256 < dim) Vec8<float>::store(pieces + piece * ldp + c0 + k * 256, acc[k]);
-}
+// A token that occurs: its rows are at sorted positions [lo, hi).
+struct __align__(16) Used {
+    uint32_t token, lo, hi, pad;
+};
 
-__device__ __forceinline__ int64_t lower_bound(const uint32_t* __restrict__ keys, int64_t n, uint32_t v) {
-    int64_t lo = 0, hi = n;
+struct GradArgs {
+    int64_t n_rows;
+    int segs, dim, vocab;
+    int64_t ld, ldp, ld_table;
+    float scale;
+    bool accumulate;
+    const uint32_t *keys, *rows;
+    uint32_t* start;  // [vocab + 1]: first sorted position of each token
+    uint32_t* used;   // how many tokens occur
+    Used* list;       // which, in any order
+    float* pieces;    // [n_rows / kPiece][ldp]
+};
+
+__device__ __forceinline__ uint32_t lower_bound(const uint32_t* __restrict__ keys, uint32_t n, uint32_t v) {
+    uint32_t lo = 0, hi = n;
     while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
+        const uint32_t mid = lo + ((hi - lo) >> 1);
         if (keys[mid] < v) lo = mid + 1;
         else hi = mid;
     }
     return lo;
 }
 
-template <class T, class G>
-__global__ void __launch_bounds__(256, 2)
-embed_rows_kernel(int64_t n_rows, int segs, int dim, int64_t ld, int vocab, float scale, bool accumulate,
-                  const uint32_t* __restrict__ keys, const uint32_t* __restrict__ rows, const T* __restrict__ dout,
-                  const float* __restrict__ pieces, int64_t ldp, G* __restrict__ dtable, int64_t ld_table) {
-    __shared__ int64_t bound[kRowsPerBlock][2];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (threadIdx.x < 2 * kRowsPerBlock) {
-        const int64_t v = (int64_t)(threadIdx.x >> 1) * gridDim.x + blockIdx.x;
-        bound[threadIdx.x >> 1][threadIdx.x & 1] = v < vocab ? lower_bound(keys, n_rows, (uint32_t)v + (threadIdx.x & 1)) : 0;
+// Blocks [0, token_blocks): where each token's rows begin, and the list of the tokens that occur.  The others: sums of whole
+// pieces, a warp for each piece and segment.
+template <class T>
+__global__ void __launch_bounds__(256) embed_prepare_kernel(GradArgs a, int token_blocks, const T* __restrict__ dout) {
+    const int lane = threadIdx.x & 31;
+    if ((int)blockIdx.x < token_blocks) {
+        __shared__ uint32_t first[257];
+        const uint32_t v0 = blockIdx.x * 256u;
+        const uint32_t n = (uint32_t)a.n_rows;
+        if (v0 + threadIdx.x <= (uint32_t)a.vocab) first[threadIdx.x] = lower_bound(a.keys, n, v0 + threadIdx.x);
+        if (threadIdx.x == 0 && v0 + 256u <= (uint32_t)a.vocab) first[256] = lower_bound(a.keys, n, v0 + 256u);
+        __syncthreads();
+        const uint32_t v = v0 + threadIdx.x;
+        const bool in = v < (uint32_t)a.vocab;
+        const uint32_t lo = in ? first[threadIdx.x] : 0u, hi = in ? first[threadIdx.x + 1] : 0u;
+        if (v <= (uint32_t)a.vocab) a.start[v] = first[threadIdx.x];
+        const unsigned some = __ballot_sync(0xffffffffu, hi > lo);
+        uint32_t at = 0;
+        if (lane == 0 && some) at = atomicAdd(a.used, (uint32_t)__popc(some));
+        at = __shfl_sync(0xffffffffu, at, 0) + __popc(some & ((1u << lane) - 1u));
+        if (hi > lo) a.list[at] = Used{v, lo, hi, 0u};
+        return;
     }
-    __syncthreads();
-    for (int item = warp; item < kRowsPerBlock * segs; item += 8) {
-        const int j = item / segs;
-        const int64_t v = (int64_t)j * gridDim.x + blockIdx.x;
-        const int64_t lo = bound[j][0], hi = bound[j][1];
-        if (v >= vocab || (accumulate && lo == hi)) continue;
-        const int c0 = (item - j * segs) * kSeg + lane * 8;
-        float acc[kVecs][8] = {};
+    const int64_t unit = (int64_t)(blockIdx.x - token_blocks) * 8 + (threadIdx.x >> 5);
+    const int64_t piece = unit / a.segs;
+    const int64_t lo = piece * kPiece, hi = lo + kPiece;
+    if (hi > a.n_rows) return;  // whole pieces only
+    const uint32_t key = a.keys[lo];
+    if (key != a.keys[hi - 1] || key >= (uint32_t)a.vocab) return;
+    const int c0 = (int)(unit - piece * a.segs) * kSeg<T> + lane * 8;
+    float acc[kVecs<T>][8] = {};
+    add_rows(acc, a.rows, lo, hi, dout, a.ld, c0, a.dim, lane);
+#pragma unroll
+    for (int k = 0; k < kVecs<T>; ++k)
+        if (c0 + k * 256 < a.dim) Vec8<float>::store(a.pieces + piece * a.ldp + c0 + k * 256, acc[k]);
+}
+
+constexpr int kZeroBytes = 8192;
+
+// Warp 7 of a block: rows of dtable whose token does not occur, the rows of tokens [from, to).
+template <class G>
+__device__ __forceinline__ void write_zeros(const GradArgs& a, uint8_t* zeros, int64_t from, int64_t to, G* __restrict__ dtable, int lane) {
+    for (int i = lane; i < kZeroBytes / 16; i += 32) reinterpret_cast<uint4*>(zeros)[i] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+    __syncwarp();
+    const uint32_t bytes = (uint32_t)((int64_t)a.dim * sizeof(G) / 16 * 16);  // the rest of a row is less than a vector
+    for (int64_t v0 = from; v0 < to; v0 += 32) {
+        const int64_t v = v0 + lane;
+        const bool empty = v < to && a.start[v] == a.start[v + 1];
+        if (empty) {
+            G* row = dtable + v * a.ld_table;
+            for (uint32_t at = 0; at < bytes; at += kZeroBytes)
+                bulk_store(reinterpret_cast<uint8_t*>(row) + at, zeros, min(bytes - at, (uint32_t)kZeroBytes));
+            for (int c = (int)(bytes / sizeof(G)); c < a.dim; ++c) from_float(row + c, 0.f);
+        }
+        bulk_commit();
+        bulk_wait_all<4>();
+    }
+    bulk_wait_all<0>();
+}
+
+template <class T, class G>
+__global__ void __launch_bounds__(256, 2) embed_rows_kernel(GradArgs a, const T* __restrict__ dout, G* __restrict__ dtable) {
+    __shared__ __align__(16) uint8_t zeros[kZeroBytes];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (warp == 7) {
+        if (a.accumulate) return;
+        const int64_t share = (a.vocab + gridDim.x - 1) / gridDim.x, from = (int64_t)blockIdx.x * share;
+        write_zeros(a, zeros, from, min(from + share, (int64_t)a.vocab), dtable, lane);
+        return;
+    }
+    const uint32_t items = *a.used;
+    const int64_t units = (int64_t)items * a.segs, stride = (int64_t)gridDim.x * 7;
+    for (int64_t unit = (int64_t)blockIdx.x * 7 + warp; unit < units; unit += stride) {
+        const int64_t which = unit / a.segs;
+        const Used u = a.list[which];
+        const int64_t lo = u.lo, hi = u.hi;
+        const int c0 = (int)(unit - which * a.segs) * kSeg<T> + lane * 8;
+        float acc[kVecs<T>][8] = {};
         // rows before the first whole piece, the pieces, rows after the last one (all rows first when there is no piece)
-        int64_t a = (lo + kPiece - 1) / kPiece, b = hi / kPiece;
-        const bool whole = a < b;
+        const int64_t first = (lo + kPiece - 1) / kPiece, last = hi / kPiece;
+        const bool whole = first < last;
 #pragma unroll 1
         for (int part = 0; part < 2; ++part) {
-            const int64_t from = part == 0 ? lo : whole ? b * kPiece : hi, to = part == 0 && whole ? a * kPiece : hi;
-            add_rows(acc, rows, from, to, dout, ld, c0, dim, lane);
+            const int64_t from = part == 0 ? lo : whole ? last * kPiece : hi, to = part == 0 && whole ? first * kPiece : hi;
+            add_rows(acc, a.rows, from, to, dout, a.ld, c0, a.dim, lane);
             if (part == 0 && whole) {
-#pragma unroll 2
-                for (int64_t p = a; p < b; ++p) {
+#pragma unroll 4
+                for (int64_t p = first; p < last; ++p) {
 #pragma unroll
-                    for (int k = 0; k < kVecs; ++k)
-                        if (c0 + k * 256 < dim) {
+                    for (int k = 0; k < kVecs<T>; ++k)
+                        if (c0 + k * 256 < a.dim) {
                             Vec8<float> x;
-                            x.load(pieces + p * ldp + c0 + k * 256);
+                            x.load(a.pieces + p * a.ldp + c0 + k * 256);
                             float f[8];
                             x.get(f);
 #pragma unroll
@@ -335,14 +403,14 @@ embed_rows_kernel(int64_t n_rows, int segs, int dim, int64_t ld, int vocab, floa
                 }
             }
         }
-        G* dst = dtable + v * ld_table;
+        G* dst = dtable + (int64_t)u.token * a.ld_table;
 #pragma unroll
-        for (int k = 0; k < kVecs; ++k) {
+        for (int k = 0; k < kVecs<T>; ++k) {
             const int c = c0 + k * 256;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) acc[k][i] *= scale;
-            if (c + 8 <= dim) {
-                if (accumulate) {
+            for (int i = 0; i < 8; ++i) acc[k][i] *= a.scale;
+            if (c + 8 <= a.dim) {
+                if (a.accumulate) {
                     Vec8<G> x;
                     x.load(dst + c);
                     float f[8];
@@ -354,7 +422,7 @@ embed_rows_kernel(int64_t n_rows, int segs, int dim, int64_t ld, int vocab, floa
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (c + i < dim) from_float(dst + c + i, accumulate ? acc[k][i] + to_float(dst[c + i]) : acc[k][i]);
+                    if (c + i < a.dim) from_float(dst + c + i, a.accumulate ? acc[k][i] + to_float(dst[c + i]) : acc[k][i]);
             }
         }
     }
@@ -363,7 +431,8 @@ embed_rows_kernel(int64_t n_rows, int segs, int dim, int64_t ld, int vocab, floa
 // ---- host side ------------------------------------------------------------------------------------------------
 
 struct EmbedScratch {
-    uint32_t *key_a, *row_a, *key_b, *row_b, *hist;
+    uint32_t *key_a, *row_a, *key_b, *row_b, *hist, *start, *used;
+    Used* list;
     float* pieces;  // [n_rows / kPiece][ldp]
     int64_t ldp;
 };
@@ -383,6 +452,9 @@ size_t carve_embed(const rapid_embed_desc_t& d, void* base, EmbedScratch* out) {
     s.key_b = reinterpret_cast<uint32_t*>(take(n * 4));
     s.row_b = reinterpret_cast<uint32_t*>(take(n * 4));
     s.hist = reinterpret_cast<uint32_t*>(take((size_t)kMaxSortBlocks * kBins * 4));
+    s.start = reinterpret_cast<uint32_t*>(take(((size_t)d.vocab + 1) * 4));
+    s.used = reinterpret_cast<uint32_t*>(take(4));
+    s.list = reinterpret_cast<Used*>(take((n < (size_t)d.vocab ? n : (size_t)d.vocab) * sizeof(Used)));
     s.ldp = (int64_t)align_up((size_t)d.dim, 8);
     s.pieces = reinterpret_cast<float*>(take(n / kPiece * (size_t)s.ldp * 4));
     if (out) *out = s;
@@ -413,16 +485,34 @@ bool blocks_of_8(int64_t units, unsigned* grid) {
 
 template <class T, class G>
 rapid_status_t run_bwd(const rapid_embed_desc_t& d, const int32_t* tokens, const uint8_t* mask, const T* dout, G* dtable,
-                       const EmbedScratch& w, cudaStream_t st) {
+                       const EmbedScratch& w, int sms, cudaStream_t st) {
     const SortShape s = sort_shape(d.n_rows, d.vocab);
+    GradArgs g{};
+    g.n_rows = d.n_rows;
+    g.segs = (d.dim + kSeg<T> - 1) / kSeg<T>;
+    g.dim = d.dim;
+    g.vocab = d.vocab;
+    g.ld = d.ld_rows;
+    g.ldp = w.ldp;
+    g.ld_table = d.ld_table;
+    g.scale = d.scale;
+    g.accumulate = (d.flags & RAPID_EMBED_ACCUMULATE) != 0;
+    g.keys = (s.passes & 1) ? w.key_a : w.key_b;
+    g.rows = (s.passes & 1) ? w.row_a : w.row_b;
+    g.start = w.start;
+    g.used = w.used;
+    g.list = w.list;
+    g.pieces = w.pieces;
+    const int64_t token_blocks = (d.vocab + 256) / 256;  // vocab + 1 bounds
+    const int64_t prepare = token_blocks + (d.n_rows / kPiece * g.segs + 7) / 8;
+    if (prepare > 0x7fffffffll) return RAPID_ERR_UNSUPPORTED;
+
     SortArgs a{};
     a.tokens = tokens;
     a.mask = mask;
     a.vocab = d.vocab;
     a.hist = w.hist;
-    const int segs = (d.dim + kSeg - 1) / kSeg;
-    unsigned piece_grid = 0;
-    if (!blocks_of_8(d.n_rows / kPiece * segs, &piece_grid)) return RAPID_ERR_UNSUPPORTED;
+    a.used = w.used;
     if (s.blocks == 1) {
         sort_one_block_kernel<<<1, kSortThreads, 0, st>>>(a, s, w.key_a, w.row_a, w.key_b, w.row_b);
     } else {
@@ -436,14 +526,8 @@ rapid_status_t run_bwd(const rapid_embed_desc_t& d, const int32_t* tokens, const
             sort_scatter_kernel<<<s.blocks, kSortThreads, 0, st>>>(a, s);
         }
     }
-    const uint32_t* keys = (s.passes & 1) ? w.key_a : w.key_b;
-    const uint32_t* rows = (s.passes & 1) ? w.row_a : w.row_b;
-    if (piece_grid)
-        embed_pieces_kernel<T><<<piece_grid, 256, 0, st>>>(d.n_rows, segs, d.dim, d.ld_rows, d.vocab, keys, rows, dout,
-                                                           w.pieces, w.ldp);
-    embed_rows_kernel<T, G><<<(unsigned)((d.vocab + kRowsPerBlock - 1) / kRowsPerBlock), 256, 0, st>>>(
-        d.n_rows, segs, d.dim, d.ld_rows, d.vocab, d.scale, (d.flags & RAPID_EMBED_ACCUMULATE) != 0, keys, rows, dout, w.pieces,
-        w.ldp, dtable, d.ld_table);
+    embed_prepare_kernel<T><<<(unsigned)prepare, 256, 0, st>>>(g, (int)token_blocks, dout);
+    embed_rows_kernel<T, G><<<2 * sms, 256, 0, st>>>(g, dout, dtable);
     return cudaGetLastError() == cudaSuccess ? RAPID_OK : RAPID_ERR_CUDA;
 }
 
@@ -505,8 +589,8 @@ extern "C" rapid_status_t rapid_embedding_bwd(const rapid_embed_desc_t* desc, co
     if ((s = check_device(&sms)) != RAPID_OK) return s;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (d.dtype == RAPID_F32)
-        return run_bwd(d, tokens, mask, static_cast<const float*>(dout), static_cast<float*>(dtable), w, st);
+        return run_bwd(d, tokens, mask, static_cast<const float*>(dout), static_cast<float*>(dtable), w, sms, st);
     if (grad_bf16)
-        return run_bwd(d, tokens, mask, static_cast<const uint16_t*>(dout), static_cast<uint16_t*>(dtable), w, st);
-    return run_bwd(d, tokens, mask, static_cast<const uint16_t*>(dout), static_cast<float*>(dtable), w, st);
+        return run_bwd(d, tokens, mask, static_cast<const uint16_t*>(dout), static_cast<uint16_t*>(dtable), w, sms, st);
+    return run_bwd(d, tokens, mask, static_cast<const uint16_t*>(dout), static_cast<float*>(dtable), w, sms, st);
 }
