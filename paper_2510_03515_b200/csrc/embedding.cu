@@ -109,7 +109,7 @@ struct SortArgs {
     uint32_t* key_out;
     uint32_t* row_out;
     uint32_t* hist;  // [blocks][kBins]
-    uint32_t* used;  // counter of the tokens that occur, cleared by the first launch
+    uint32_t* used;  // counters of the tokens that occur, cleared by the first launch
     int shift;
 };
 
@@ -122,7 +122,7 @@ __device__ __forceinline__ uint32_t sort_key(const SortArgs& a, int64_t i) {
 
 __global__ void __launch_bounds__(kSortThreads) sort_hist_kernel(SortArgs a, SortShape s) {
     __shared__ uint32_t bins[kBins];
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.used = 0;
+    if (blockIdx.x == 0 && threadIdx.x < 2) a.used[threadIdx.x] = 0;
     bins[threadIdx.x] = 0;
     __syncthreads();
     const int64_t lo = (int64_t)blockIdx.x * s.per_block, hi = min(lo + s.per_block, s.n_rows);
@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kSortThreads)
 sort_one_block_kernel(SortArgs a, SortShape s, uint32_t* key_a, uint32_t* row_a, uint32_t* key_b, uint32_t* row_b) {
     __shared__ uint32_t cnt[kSortWarps][kBins];
     __shared__ uint32_t scan[kSortWarps];
-    if (threadIdx.x == 0) *a.used = 0;
+    if (threadIdx.x < 2) a.used[threadIdx.x] = 0;
     for (int p = 0; p < s.passes; ++p) {
         a.shift = p * kRadixBits;
         a.key_in = p == 0 ? nullptr : (p & 1) ? key_a : key_b;
@@ -223,28 +223,33 @@ sort_one_block_kernel(SortArgs a, SortShape s, uint32_t* key_a, uint32_t* row_a,
 // ---- sums over a token's rows -------------------------------------------------------------------------------
 
 constexpr int kPiece = 32;  // sorted positions of a piece
-constexpr int kAhead = 8;   // rows of dout in flight
 
-// columns a warp sums: two vectors of 8 a lane in bf16, one in float (the loads in flight take the same registers)
-template <class T>
-constexpr int kVecs = sizeof(T) == 2 ? 2 : 1;
-template <class T>
-constexpr int kSeg = kVecs<T> * 256;
+// A warp sums K vectors of 8 columns a lane, 256 K columns, with kAhead rows of dout in flight.  Most tokens occur once or
+// twice: what is in flight is then the width, so their rows are taken whole (WIDE).  Frequent tokens take a narrower segment
+// with more rows in flight.
+template <class T, bool WIDE>
+struct Seg {
+    static constexpr int K = (WIDE ? 6 : 2) / (sizeof(T) == 2 ? 1 : 2);
+    static constexpr int kAhead = WIDE ? 2 : 8;
+    static constexpr int kColumns = K * 256;
+};
+constexpr uint32_t kFrequent = 8;  // tokens that occur more often are summed by a whole block
 
 // acc += rows of dout at sorted positions [lo, hi), in order
-template <class T>
-__device__ __forceinline__ void add_rows(float (&acc)[kVecs<T>][8], const uint32_t* __restrict__ rows, int64_t lo, int64_t hi,
+template <class T, bool WIDE>
+__device__ __forceinline__ void add_rows(float (&acc)[Seg<T, WIDE>::K][8], const uint32_t* __restrict__ rows, int64_t lo, int64_t hi,
                                          const T* __restrict__ dout, int64_t ld, int c0, int dim, int lane) {
+    constexpr int K = Seg<T, WIDE>::K, kAhead = Seg<T, WIDE>::kAhead;
     for (int64_t i0 = lo; i0 < hi; i0 += 32) {
         const int n = (int)min((int64_t)32, hi - i0);
         const uint32_t mine = lane < n ? rows[i0 + lane] : 0u;
         for (int i = 0; i < n; i += kAhead) {
-            Vec8<T> v[kAhead][kVecs<T>];
+            Vec8<T> v[kAhead][K];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const T* src = dout + (int64_t)__shfl_sync(0xffffffffu, mine, min(i + u, n - 1)) * ld;
 #pragma unroll
-                for (int k = 0; k < kVecs<T>; ++k) {
+                for (int k = 0; k < K; ++k) {
                     const int c = c0 + k * 256;
                     if (i + u < n && c + 8 <= dim) v[u][k].load(src + c);
                 }
@@ -254,7 +259,7 @@ __device__ __forceinline__ void add_rows(float (&acc)[kVecs<T>][8], const uint32
                 const T* src = dout + (int64_t)__shfl_sync(0xffffffffu, mine, min(i + u, n - 1)) * ld;
                 if (i + u < n) {
 #pragma unroll
-                    for (int k = 0; k < kVecs<T>; ++k) {
+                    for (int k = 0; k < K; ++k) {
                         const int c = c0 + k * 256;
                         if (c + 8 <= dim) {
                             float f[8];
@@ -280,14 +285,15 @@ struct __align__(16) Used {
 
 struct GradArgs {
     int64_t n_rows;
-    int segs, dim, vocab;
+    int segs, wide_segs, dim, vocab;  // segments of a row for frequent tokens (and pieces), for the others
     int64_t ld, ldp, ld_table;
     float scale;
     bool accumulate;
     const uint32_t *keys, *rows;
     uint32_t* start;  // [vocab + 1]: first sorted position of each token
-    uint32_t* used;   // how many tokens occur
-    Used* list;       // which, in any order
+    uint32_t* used;   // how many tokens occur seldom, how many often
+    Used* list;       // which, in any order: the former from the front, the latter from the back
+    uint32_t room;    // of the list
     float* pieces;    // [n_rows / kPiece][ldp]
 };
 
@@ -301,27 +307,47 @@ __device__ __forceinline__ uint32_t lower_bound(const uint32_t* __restrict__ key
     return lo;
 }
 
+constexpr int kTokensPerBlock = 1024;
+
 // Blocks [0, token_blocks): where each token's rows begin, and the list of the tokens that occur.  The others: sums of whole
 // pieces, a warp for each piece and segment.
 template <class T>
 __global__ void __launch_bounds__(256) embed_prepare_kernel(GradArgs a, int token_blocks, const T* __restrict__ dout) {
+    constexpr int K = Seg<T, false>::K;
     const int lane = threadIdx.x & 31;
     if ((int)blockIdx.x < token_blocks) {
-        __shared__ uint32_t first[257];
-        const uint32_t v0 = blockIdx.x * 256u;
-        const uint32_t n = (uint32_t)a.n_rows;
-        if (v0 + threadIdx.x <= (uint32_t)a.vocab) first[threadIdx.x] = lower_bound(a.keys, n, v0 + threadIdx.x);
-        if (threadIdx.x == 0 && v0 + 256u <= (uint32_t)a.vocab) first[256] = lower_bound(a.keys, n, v0 + 256u);
+        __shared__ uint32_t first[kTokensPerBlock + 1];
+        const uint32_t v0 = blockIdx.x * (uint32_t)kTokensPerBlock, n = (uint32_t)a.n_rows;
+        // four searches of a thread side by side: each step is one trip to L2
+        uint32_t lo[4] = {0, 0, 0, 0}, hi[4] = {n, n, n, n};
+        for (uint32_t width = n; width > 0; width >>= 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (lo[i] < hi[i]) {
+                    const uint32_t mid = lo[i] + ((hi[i] - lo[i]) >> 1);
+                    if (a.keys[mid] < v0 + threadIdx.x + 256u * i) lo[i] = mid + 1;
+                    else hi[i] = mid;
+                }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) first[threadIdx.x + 256 * i] = lo[i];
+        if (threadIdx.x == 0) first[kTokensPerBlock] = lower_bound(a.keys, n, v0 + kTokensPerBlock);
         __syncthreads();
-        const uint32_t v = v0 + threadIdx.x;
-        const bool in = v < (uint32_t)a.vocab;
-        const uint32_t lo = in ? first[threadIdx.x] : 0u, hi = in ? first[threadIdx.x + 1] : 0u;
-        if (v <= (uint32_t)a.vocab) a.start[v] = first[threadIdx.x];
-        const unsigned some = __ballot_sync(0xffffffffu, hi > lo);
-        uint32_t at = 0;
-        if (lane == 0 && some) at = atomicAdd(a.used, (uint32_t)__popc(some));
-        at = __shfl_sync(0xffffffffu, at, 0) + __popc(some & ((1u << lane) - 1u));
-        if (hi > lo) a.list[at] = Used{v, lo, hi, 0u};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t at_v = threadIdx.x + 256u * i, v = v0 + at_v;
+            const uint32_t from = first[at_v], to = first[at_v + 1];
+            if (v <= (uint32_t)a.vocab) a.start[v] = from;
+            const uint32_t count = v < (uint32_t)a.vocab ? to - from : 0u;
+#pragma unroll
+            for (int often = 0; often < 2; ++often) {
+                const bool mine = often ? count > kFrequent : count > 0 && count <= kFrequent;
+                const unsigned which = __ballot_sync(0xffffffffu, mine);
+                uint32_t at = 0;
+                if (lane == 0 && which) at = atomicAdd(a.used + often, (uint32_t)__popc(which));
+                at = __shfl_sync(0xffffffffu, at, 0) + __popc(which & ((1u << lane) - 1u));
+                if (mine) a.list[often ? a.room - 1u - at : at] = Used{v, from, to, 0u};
+            }
+        }
         return;
     }
     const int64_t unit = (int64_t)(blockIdx.x - token_blocks) * 8 + (threadIdx.x >> 5);
@@ -330,11 +356,11 @@ __global__ void __launch_bounds__(256) embed_prepare_kernel(GradArgs a, int toke
     if (hi > a.n_rows) return;  // whole pieces only
     const uint32_t key = a.keys[lo];
     if (key != a.keys[hi - 1] || key >= (uint32_t)a.vocab) return;
-    const int c0 = (int)(unit - piece * a.segs) * kSeg<T> + lane * 8;
-    float acc[kVecs<T>][8] = {};
-    add_rows(acc, a.rows, lo, hi, dout, a.ld, c0, a.dim, lane);
+    const int c0 = (int)(unit - piece * a.segs) * (K * 256) + lane * 8;
+    float acc[K][8] = {};
+    add_rows<T, false>(acc, a.rows, lo, hi, dout, a.ld, c0, a.dim, lane);
 #pragma unroll
-    for (int k = 0; k < kVecs<T>; ++k)
+    for (int k = 0; k < K; ++k)
         if (c0 + k * 256 < a.dim) Vec8<float>::store(a.pieces + piece * a.ldp + c0 + k * 256, acc[k]);
 }
 
@@ -362,69 +388,106 @@ __device__ __forceinline__ void write_zeros(const GradArgs& a, uint8_t* zeros, i
     bulk_wait_all<0>();
 }
 
+// `n` sums (n = 4 or 8) of columns [c, c + n) of a token's row to dtable, or onto what is there.
+template <int N, class G>
+__device__ __forceinline__ void put(const GradArgs& a, G* row, int c, float (&f)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] *= a.scale;
+    if (a.accumulate) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (c + i < a.dim) f[i] += to_float(row[c + i]);
+    }
+    if (N == 8 && c + N <= a.dim) {
+        float g[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] = f[i % N];
+        Vec8<G>::store(row + c, g);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (c + i < a.dim) from_float(row + c + i, f[i]);
+    }
+}
+
+constexpr int kSumWarps = 7;
+
+// A frequent token's segment, by all summing warps of a block: each takes a run of the rows before the first whole piece, of
+// the pieces, and of the rows after the last one; the warps' sums are added in order.
+template <class T, class G>
+__device__ __forceinline__ void sum_frequent(const GradArgs& a, const Used& u, int seg, const T* __restrict__ dout, G* __restrict__ dtable,
+                                             float (*part)[Seg<T, false>::kColumns], int warp, int lane) {
+    constexpr int K = Seg<T, false>::K, kColumns = Seg<T, false>::kColumns;
+    const int c0 = seg * kColumns + lane * 8;
+    const int64_t lo = u.lo, hi = u.hi;
+    int64_t first = (lo + kPiece - 1) / kPiece, last = hi / kPiece;
+    const bool whole = first < last;
+    if (!whole) first = last = 0;
+    float acc[K][8] = {};
+    auto share = [&](int64_t from, int64_t to, int w) { return from + (to - from) * w / kSumWarps; };
+#pragma unroll 1
+    for (int side = 0; side < 2; ++side) {
+        const int64_t from = side == 0 ? lo : whole ? last * kPiece : hi, to = side == 0 && whole ? first * kPiece : hi;
+        add_rows<T, false>(acc, a.rows, share(from, to, warp), share(from, to, warp + 1), dout, a.ld, c0, a.dim, lane);
+    }
+#pragma unroll 4
+    for (int64_t p = share(first, last, warp); p < share(first, last, warp + 1); ++p) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (c0 + k * 256 < a.dim) {
+                Vec8<float> x;
+                x.load(a.pieces + p * a.ldp + c0 + k * 256);
+                float f[8];
+                x.get(f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[k][i] += f[i];
+            }
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) Vec8<float>::store(part[warp] + k * 256 + lane * 8, acc[k]);
+    asm volatile("bar.sync 1, %0;" ::"n"(kSumWarps * 32) : "memory");
+    for (int c = threadIdx.x * 4; c < kColumns; c += kSumWarps * 128) {
+        if (seg * kColumns + c >= a.dim) break;
+        float f[4] = {};
+        for (int w = 0; w < kSumWarps; ++w) {
+            const float4 x = *reinterpret_cast<const float4*>(part[w] + c);
+            f[0] += x.x, f[1] += x.y, f[2] += x.z, f[3] += x.w;
+        }
+        put(a, dtable + (int64_t)u.token * a.ld_table, seg * kColumns + c, f);
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(kSumWarps * 32) : "memory");
+}
+
 template <class T, class G>
 __global__ void __launch_bounds__(256, 2) embed_rows_kernel(GradArgs a, const T* __restrict__ dout, G* __restrict__ dtable) {
     __shared__ __align__(16) uint8_t zeros[kZeroBytes];
+    __shared__ __align__(16) float part[kSumWarps][Seg<T, false>::kColumns];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (warp == 7) {
+    if (warp == kSumWarps) {
         if (a.accumulate) return;
         const int64_t share = (a.vocab + gridDim.x - 1) / gridDim.x, from = (int64_t)blockIdx.x * share;
         write_zeros(a, zeros, from, min(from + share, (int64_t)a.vocab), dtable, lane);
         return;
     }
-    const uint32_t items = *a.used;
-    const int64_t units = (int64_t)items * a.segs, stride = (int64_t)gridDim.x * 7;
-    for (int64_t unit = (int64_t)blockIdx.x * 7 + warp; unit < units; unit += stride) {
+    const int64_t often = (int64_t)a.used[1] * a.segs;
+    for (int64_t unit = blockIdx.x; unit < often; unit += gridDim.x) {
         const int64_t which = unit / a.segs;
-        const Used u = a.list[which];
-        const int64_t lo = u.lo, hi = u.hi;
-        const int c0 = (int)(unit - which * a.segs) * kSeg<T> + lane * 8;
-        float acc[kVecs<T>][8] = {};
-        // rows before the first whole piece, the pieces, rows after the last one (all rows first when there is no piece)
-        const int64_t first = (lo + kPiece - 1) / kPiece, last = hi / kPiece;
-        const bool whole = first < last;
-#pragma unroll 1
-        for (int part = 0; part < 2; ++part) {
-            const int64_t from = part == 0 ? lo : whole ? last * kPiece : hi, to = part == 0 && whole ? first * kPiece : hi;
-            add_rows(acc, a.rows, from, to, dout, a.ld, c0, a.dim, lane);
-            if (part == 0 && whole) {
-#pragma unroll 4
-                for (int64_t p = first; p < last; ++p) {
+        sum_frequent<T, G>(a, a.list[a.room - 1u - (uint32_t)which], (int)(unit - which * a.segs), dout, dtable, part, warp, lane);
+    }
+    constexpr int K = Seg<T, true>::K;
+    const int64_t units = (int64_t)a.used[0] * a.wide_segs, stride = (int64_t)gridDim.x * kSumWarps;
+    // blocks with one frequent segment less begin first
+    const int64_t turn = (int64_t)((blockIdx.x + gridDim.x - (uint32_t)(often % gridDim.x)) % gridDim.x) * kSumWarps + warp;
+    Used next{};
+    if (turn < units) next = a.list[turn / a.wide_segs];
+    for (int64_t unit = turn; unit < units; unit += stride) {
+        const Used u = next;
+        if (unit + stride < units) next = a.list[(unit + stride) / a.wide_segs];
+        const int c0 = (int)(unit % a.wide_segs) * (K * 256) + lane * 8;
+        float acc[K][8] = {};
+        add_rows<T, true>(acc, a.rows, u.lo, u.hi, dout, a.ld, c0, a.dim, lane);
 #pragma unroll
-                    for (int k = 0; k < kVecs<T>; ++k)
-                        if (c0 + k * 256 < a.dim) {
-                            Vec8<float> x;
-                            x.load(a.pieces + p * a.ldp + c0 + k * 256);
-                            float f[8];
-                            x.get(f);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) acc[k][i] += f[i];
-                        }
-                }
-            }
-        }
-        G* dst = dtable + (int64_t)u.token * a.ld_table;
-#pragma unroll
-        for (int k = 0; k < kVecs<T>; ++k) {
-            const int c = c0 + k * 256;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) acc[k][i] *= a.scale;
-            if (c + 8 <= a.dim) {
-                if (a.accumulate) {
-                    Vec8<G> x;
-                    x.load(dst + c);
-                    float f[8];
-                    x.get(f);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[k][i] += f[i];
-                }
-                Vec8<G>::store(dst + c, acc[k]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (c + i < a.dim) from_float(dst + c + i, a.accumulate ? acc[k][i] + to_float(dst[c + i]) : acc[k][i]);
-            }
-        }
+        for (int k = 0; k < K; ++k) put(a, dtable + (int64_t)u.token * a.ld_table, c0 + k * 256, acc[k]);
     }
 }
 
@@ -453,7 +516,7 @@ size_t carve_embed(const rapid_embed_desc_t& d, void* base, EmbedScratch* out) {
     s.row_b = reinterpret_cast<uint32_t*>(take(n * 4));
     s.hist = reinterpret_cast<uint32_t*>(take((size_t)kMaxSortBlocks * kBins * 4));
     s.start = reinterpret_cast<uint32_t*>(take(((size_t)d.vocab + 1) * 4));
-    s.used = reinterpret_cast<uint32_t*>(take(4));
+    s.used = reinterpret_cast<uint32_t*>(take(8));
     s.list = reinterpret_cast<Used*>(take((n < (size_t)d.vocab ? n : (size_t)d.vocab) * sizeof(Used)));
     s.ldp = (int64_t)align_up((size_t)d.dim, 8);
     s.pieces = reinterpret_cast<float*>(take(n / kPiece * (size_t)s.ldp * 4));
@@ -489,7 +552,9 @@ rapid_status_t run_bwd(const rapid_embed_desc_t& d, const int32_t* tokens, const
     const SortShape s = sort_shape(d.n_rows, d.vocab);
     GradArgs g{};
     g.n_rows = d.n_rows;
-    g.segs = (d.dim + kSeg<T> - 1) / kSeg<T>;
+    g.segs = (d.dim + Seg<T, false>::kColumns - 1) / Seg<T, false>::kColumns;
+    g.wide_segs = (d.dim + Seg<T, true>::kColumns - 1) / Seg<T, true>::kColumns;
+    g.room = (uint32_t)(d.n_rows < d.vocab ? d.n_rows : d.vocab);
     g.dim = d.dim;
     g.vocab = d.vocab;
     g.ld = d.ld_rows;
@@ -503,7 +568,7 @@ rapid_status_t run_bwd(const rapid_embed_desc_t& d, const int32_t* tokens, const
     g.used = w.used;
     g.list = w.list;
     g.pieces = w.pieces;
-    const int64_t token_blocks = (d.vocab + 256) / 256;  // vocab + 1 bounds
+    const int64_t token_blocks = d.vocab / kTokensPerBlock + 1;  // vocab + 1 bounds
     const int64_t prepare = token_blocks + (d.n_rows / kPiece * g.segs + 7) / 8;
     if (prepare > 0x7fffffffll) return RAPID_ERR_UNSUPPORTED;
 
