@@ -77,6 +77,7 @@ constexpr int kRadixBits = 9, kBins = 1 << kRadixBits;
 constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;  // one thread a digit value
 constexpr int kMaxSortBlocks = 64;  // every block reads the histograms of all
 constexpr int kMinSortRows = 1024;
+constexpr int kSortAhead = 8;
 constexpr int64_t kOneBlockRows = 16384;
 
 // The rows of block b are [b * per_block, (b + 1) * per_block); within it warp w has a run of per_block / 16 of them.
@@ -139,7 +140,15 @@ __device__ __forceinline__ void sort_scatter(const SortArgs& a, const SortShape&
     __syncthreads();
     const int64_t run = s.per_block / kSortWarps;  // a multiple of 32
     const int64_t lo = (int64_t)blockIdx.x * s.per_block + warp * run, hi = min(lo + run, s.n_rows);
-    for (int64_t i = lo + lane; i < hi; i += 32) atomicAdd(&cnt[warp][(sort_key(a, i) >> a.shift) & (kBins - 1)], 1u);
+    // kSortAhead turns of 32 rows are loaded before the first is used
+    for (int64_t i0 = lo; i0 < hi; i0 += 32 * kSortAhead) {
+        uint32_t key[kSortAhead];
+#pragma unroll
+        for (int t = 0; t < kSortAhead; ++t) key[t] = i0 + 32 * t + lane < hi ? sort_key(a, i0 + 32 * t + lane) : 0u;
+#pragma unroll
+        for (int t = 0; t < kSortAhead; ++t)
+            if (i0 + 32 * t + lane < hi) atomicAdd(&cnt[warp][(key[t] >> a.shift) & (kBins - 1)], 1u);
+    }
     // this thread's digit: how many rows lie in blocks before this one, and how many in all
     uint32_t before = 0, total = 0;
     if (!alone) {
@@ -175,24 +184,33 @@ __device__ __forceinline__ void sort_scatter(const SortArgs& a, const SortShape&
     }
     __syncthreads();
     // in row order, 32 rows at a time: a row's place is the digit's next one plus the equal digits in lower lanes
-    for (int64_t i0 = lo; i0 < hi; i0 += 32) {
-        const int64_t i = i0 + lane;
-        const bool on = i < hi;
-        const uint32_t key = on ? sort_key(a, i) : 0u;
-        const uint32_t digit = on ? (key >> a.shift) & (kBins - 1) : (uint32_t)kBins;
-        const unsigned peers = __match_any_sync(0xffffffffu, digit);
-        const int first = __ffs(peers) - 1;
-        uint32_t place = 0;
-        if (on && lane == first) {
-            place = cnt[warp][digit];
-            cnt[warp][digit] = place + __popc(peers);
+    for (int64_t i0 = lo; i0 < hi; i0 += 32 * kSortAhead) {
+        uint32_t key[kSortAhead], row[kSortAhead];
+#pragma unroll
+        for (int t = 0; t < kSortAhead; ++t) {
+            const int64_t i = i0 + 32 * t + lane;
+            key[t] = i < hi ? sort_key(a, i) : 0u;
+            row[t] = i < hi && a.row_in ? a.row_in[i] : (uint32_t)i;
         }
-        place = __shfl_sync(0xffffffffu, place, first) + __popc(peers & ((1u << lane) - 1u));
-        if (on) {
-            a.key_out[place] = key;
-            a.row_out[place] = a.row_in ? a.row_in[i] : (uint32_t)i;
+#pragma unroll
+        for (int t = 0; t < kSortAhead; ++t) {
+            if (i0 + 32 * t >= hi) break;
+            const bool on = i0 + 32 * t + lane < hi;
+            const uint32_t digit = on ? (key[t] >> a.shift) & (kBins - 1) : (uint32_t)kBins;
+            const unsigned peers = __match_any_sync(0xffffffffu, digit);
+            const int first = __ffs(peers) - 1;
+            uint32_t place = 0;
+            if (on && lane == first) {
+                place = cnt[warp][digit];
+                cnt[warp][digit] = place + __popc(peers);
+            }
+            place = __shfl_sync(0xffffffffu, place, first) + __popc(peers & ((1u << lane) - 1u));
+            if (on) {
+                a.key_out[place] = key[t];
+                a.row_out[place] = row[t];
+            }
+            __syncwarp();
         }
-        __syncwarp();
     }
 }
 
