@@ -3,10 +3,13 @@
 //
 // A lane holds 16 elements of a head as two vectors of 8 whose elements form rotation pairs with one another (halves: 8 at
 // i and 8 at i + rot_dim / 2; interleaved: 16 neighbours), so a rotation needs no exchange between lanes; the lanes of
-// a head (head_dim / 16 rounded up to a power of two) exchange only the sums of the norm.  A group of lanes stays on one
-// row and walks its heads, so the 8 angles of a lane are formed once for all heads.  Angles are products in double,
-// reduced to a fraction of a turn in double (a float angle at position 100 000 is off by 4e-3), then sine and cosine in
-// float.
+// a head (head_dim / 16 rounded up to a power of two: a group) exchange only the sums of the norm.  A group stays on one row
+// and takes every few of its heads, up to four of them in flight.  What has to be saved here is instructions: with a division
+// for each head and one float operation at a time the forward kernel took 145 us on 64 x 1024 rows of 14 heads, half of all
+// issue slots, at 2.6 TB/s; so rows and pointers are worked out once for each group, the arithmetic is on packed pairs of
+// floats, and a row's angles are formed once for all its heads, in shared memory, while the first loads are under way.
+// Angles are products in double, reduced to a fraction of a turn in double (a float angle at position 100 000 is off by
+// 4e-3), then sine and cosine in float.
 #include <math.h>
 
 #include "policy_ops.cuh"
@@ -18,13 +21,16 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxHeadDim = 256;
 
+constexpr int kAhead = 4;     // heads of a group in flight, at most
+
 struct QkArgs {
     int64_t n_rows;
     int seq_len, heads_q, heads, head_dim, rot_dim;  // heads = queries and keys together
     int lanes_log2;                                  // lanes of a head
-    int parts, per_part;                             // a row's heads are split over `parts` groups
+    int per_row[2];                                  // groups on one row; backward: of queries, of keys
+    int q_blocks;                                    // backward: blocks that take queries
     uint32_t flags;
-    float eps;
+    float eps, inv_dim;
     int64_t ld_q, ld_k, ld_q_out, ld_k_out, ld_dq, ld_dk;
     const float *q_weight, *k_weight, *inv_freq;
     const int32_t* positions;
@@ -52,38 +58,90 @@ __device__ __forceinline__ Place place_of(const QkArgs& p, int u) {
     return x;
 }
 
-__device__ __forceinline__ void angles(const QkArgs& p, const Place& x, int64_t r, float (&cs)[8], float (&sn)[8]) {
-    if (x.angle < 0) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) cs[j] = 1.f, sn[j] = 0.f;
-        return;
-    }
-    const double pos = (double)(p.positions ? p.positions[r] : (int32_t)(r % p.seq_len));
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        double t = pos * (double)p.inv_freq[x.angle + j] * 0.15915494309189533577;  // turns: angle / (2 pi)
+// What a block keeps in shared memory: the factors of the norm, and its rows' angles.
+struct Shared {
+    float weight[2][kMaxHeadDim];  // queries, keys
+    // [row of the tile][rot_dim / 2]; a group of lanes has at most 8 angles a lane, a block kThreads lanes
+    float cs[kThreads * 8], sn[kThreads * 8];
+};
+
+__device__ __forceinline__ bool row_live(const QkArgs& p, int64_t r) { return r < p.n_rows && (p.mask == nullptr || p.mask[r] != 0); }
+
+// Sines and cosines of rows [r0, r0 + rows), by the whole block.
+__device__ __forceinline__ void angles(const QkArgs& p, Shared& sm, int64_t r0, int rows) {
+    const int n = p.rot_dim / 2, at_once = kThreads / n;  // n <= 128
+    const int first = threadIdx.x / n, k = threadIdx.x - first * n;
+    if (first >= at_once) return;
+    const double f = (double)p.inv_freq[k] * 0.15915494309189533577;  // turns a position: 1 / (2 pi)
+    for (int row = first; row < rows; row += at_once) {
+        const int64_t r = r0 + row;
+        if (!row_live(p, r)) continue;
+        double t = (double)(p.positions ? p.positions[r] : (int32_t)(r % p.seq_len)) * f;
         t -= rint(t);
-        sincospif((float)(2.0 * t), &sn[j], &cs[j]);
+        sincospif((float)(2.0 * t), &sm.sn[row * n + k], &sm.cs[row * n + k]);
     }
 }
 
-// (a_i, b_i) -> (a_i c - b_i s, a_i s + b_i c) over the lane's 8 pairs; halves: a and b, interleaved: neighbours
-__device__ __forceinline__ void rotate(bool interleaved, float (&a)[8], float (&b)[8], const float (&cs)[8], const float (&sn)[8]) {
-    if (interleaved) {
+// Eight floats as four packed pairs.
+struct Pairs {
+    uint64_t v[4];
+    __device__ __forceinline__ void zero() {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float a0 = a[2 * j], a1 = a[2 * j + 1], b0 = b[2 * j], b1 = b[2 * j + 1];
-            a[2 * j] = a0 * cs[j] - a1 * sn[j];
-            a[2 * j + 1] = a0 * sn[j] + a1 * cs[j];
-            b[2 * j] = b0 * cs[4 + j] - b1 * sn[4 + j];
-            b[2 * j + 1] = b0 * sn[4 + j] + b1 * cs[4 + j];
-        }
+        for (int j = 0; j < 4; ++j) v[j] = 0;
+    }
+    __device__ __forceinline__ void from(const float* src) {  // shared memory, 16-byte aligned
+        const ulonglong2 x = reinterpret_cast<const ulonglong2*>(src)[0], y = reinterpret_cast<const ulonglong2*>(src)[1];
+        v[0] = x.x, v[1] = x.y, v[2] = y.x, v[3] = y.y;
+    }
+    template <class T>
+    __device__ __forceinline__ void from(const Vec8<T>& x) {
+        float f[8];
+        x.get(f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = f32x2(f[2 * j], f[2 * j + 1]);
+    }
+    template <class T>
+    __device__ __forceinline__ void store(T* p) const {
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f32x2_split(v[j], f[2 * j], f[2 * j + 1]);
+        Vec8<T>::store(p, f);
+    }
+    __device__ __forceinline__ void times(const Pairs& o) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = f32x2_mul(v[j], o.v[j]);
+    }
+    __device__ __forceinline__ void times(float x) {
+        const uint64_t y = f32x2(x, x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = f32x2_mul(v[j], y);
+    }
+};
+__device__ __forceinline__ uint64_t negated(uint64_t x) { return x ^ 0x8000000080000000ull; }
+
+// (a_i, b_i) -> (a_i c - b_i s, a_i s + b_i c) over the lane's 8 pairs; halves: a and b, interleaved: neighbours
+template <bool INTER>
+__device__ __forceinline__ void rotate(Pairs& a, Pairs& b, const Pairs& cs, const Pairs& sn) {
+    if (INTER) {
+        auto turn = [](Pairs& x, uint64_t c0, uint64_t s0, uint64_t c1, uint64_t s1) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float u, v, ca, cb, sa, sb;
+                f32x2_split(x.v[j], u, v);
+                f32x2_split(j < 2 ? c0 : c1, ca, cb);
+                f32x2_split(j < 2 ? s0 : s1, sa, sb);
+                const float c = j & 1 ? cb : ca, s = j & 1 ? sb : sa;
+                x.v[j] = f32x2(u * c - v * s, u * s + v * c);
+            }
+        };
+        turn(a, cs.v[0], sn.v[0], cs.v[1], sn.v[1]);
+        turn(b, cs.v[2], sn.v[2], cs.v[3], sn.v[3]);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float x = a[j], y = b[j];
-            a[j] = x * cs[j] - y * sn[j];
-            b[j] = x * sn[j] + y * cs[j];
+        for (int j = 0; j < 4; ++j) {
+            const uint64_t x = a.v[j], y = b.v[j];
+            a.v[j] = f32x2_fma(x, cs.v[j], f32x2_mul(y, negated(sn.v[j])));
+            b.v[j] = f32x2_fma(x, sn.v[j], f32x2_mul(y, cs.v[j]));
         }
     }
 }
@@ -92,222 +150,237 @@ __device__ __forceinline__ float group_sum(float v, int lanes_log2) {
     for (int o = 1; o < (1 << lanes_log2); o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
+// sum over the lane's 16 elements of x * y
+__device__ __forceinline__ float dot16(const Pairs& xa, const Pairs& xb, const Pairs& ya, const Pairs& yb) {
+    uint64_t s = f32x2_mul(xa.v[0], ya.v[0]), t = f32x2_mul(xb.v[0], yb.v[0]);
+#pragma unroll
+    for (int j = 1; j < 4; ++j) {
+        s = f32x2_fma(xa.v[j], ya.v[j], s);
+        t = f32x2_fma(xb.v[j], yb.v[j], t);
+    }
+    float u, v;
+    f32x2_split(f32x2_add(s, t), u, v);
+    return u + v;
+}
 
-// The factors of the two norms, in shared memory: [0] queries, [1] keys.
-__device__ __forceinline__ void load_weights(const QkArgs& p, float (*w)[kMaxHeadDim]) {
+__device__ __forceinline__ void load_weights(const QkArgs& p, Shared& sm) {
     const float add = (p.flags & RAPID_QK_UNIT_OFFSET) ? 1.f : 0.f;
-    if (!(p.flags & RAPID_QK_NO_NORM))
-        for (int i = threadIdx.x; i < p.head_dim; i += kThreads) {
-            w[0][i] = p.q_weight[i] + add;
-            w[1][i] = p.k_weight[i] + add;
-        }
-    __syncthreads();
+    for (int i = threadIdx.x; i < p.head_dim; i += kThreads) {
+        sm.weight[0][i] = p.q_weight[i] + add;
+        sm.weight[1][i] = p.k_weight[i] + add;
+    }
 }
 
-constexpr int kHeadsAhead = 4;  // heads whose loads are in flight together
-
-template <class T>
-__global__ void __launch_bounds__(kThreads)
+template <class T, bool INTER, bool NORM>
+__global__ void __launch_bounds__(kThreads, 2)
 qk_fwd_kernel(QkArgs p, const T* q, const T* k, T* q_out, T* k_out) {
-    __shared__ float w[2][kMaxHeadDim];
-    load_weights(p, w);
-    const int lane = threadIdx.x & 31;
-    const int64_t group = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> p.lanes_log2;
-    const bool norm = !(p.flags & RAPID_QK_NO_NORM), inter = (p.flags & RAPID_QK_INTERLEAVED) != 0;
-    const int64_t r = group / p.parts;
-    const int h0 = (int)(group - r * p.parts) * p.per_part;
-    const bool row = r < p.n_rows;
-    const int h1 = row ? min(h0 + p.per_part, p.heads) : h0;
-    const bool live = row && (p.mask == nullptr || p.mask[r] != 0);
-    const Place x = place_of(p, lane & ((1 << p.lanes_log2) - 1));
-    float cs[8], sn[8];
-    if (live && x.on) angles(p, x, r, cs, sn);
-    // the same number of turns in every lane of the warp: the sums exchange over whole warps
-    for (int hh = 0; hh < p.per_part; hh += kHeadsAhead) {
-        Vec8<T> va[kHeadsAhead], vb[kHeadsAhead];
+    __shared__ __align__(16) Shared sm;
+    const int lanes = 1 << p.lanes_log2, groups = kThreads >> p.lanes_log2, group = threadIdx.x >> p.lanes_log2;
+    const int per_row = p.per_row[0], rows = groups / per_row;
+    const int row = group / per_row, h0 = group - row * per_row;
+    const int64_t r0 = (int64_t)blockIdx.x * rows, r = r0 + row;
+    const Place x = place_of(p, threadIdx.x & (lanes - 1));
+    const bool have = row < rows && r < p.n_rows && x.on, live = have && row_live(p, r);
+    const T *qr = q + r * p.ld_q, *kr = k + r * p.ld_k - (int64_t)p.heads_q * p.head_dim;
+    T *qo = q_out + r * p.ld_q_out, *ko = k_out + r * p.ld_k_out - (int64_t)p.heads_q * p.head_dim;
+    Pairs cs, sn;
+    bool angled = false;
+    // the same number of turns in every lane: the sums exchange over whole warps
+#pragma unroll 1
+    for (int turn = 0; turn * per_row * kAhead < p.heads; ++turn) {
+        Vec8<T> va[kAhead], vb[kAhead];
 #pragma unroll
-        for (int u = 0; u < kHeadsAhead; ++u) {
-            const int h = h0 + hh + u;
-            if (hh + u < p.per_part && h < h1 && live && x.on) {
-                const T* src = h < p.heads_q ? q + r * p.ld_q + h * p.head_dim : k + r * p.ld_k + (h - p.heads_q) * p.head_dim;
-                va[u].load(src + x.a);
-                vb[u].load(src + x.b);
+        for (int i = 0; i < kAhead; ++i) {
+            const int h = h0 + (turn * kAhead + i) * per_row;
+            if (live && h < p.heads) {
+                const T* src = (h < p.heads_q ? qr : kr) + h * p.head_dim;
+                va[i].load(src + x.a);
+                vb[i].load(src + x.b);
+            }
+        }
+        if (!angled) {
+            if (NORM) load_weights(p, sm);
+            angles(p, sm, r0, rows);
+            __syncthreads();
+            angled = true;
+            if (live && x.angle >= 0) {
+                cs.from(sm.cs + row * (p.rot_dim / 2) + x.angle);
+                sn.from(sm.sn + row * (p.rot_dim / 2) + x.angle);
             }
         }
 #pragma unroll
-        for (int u = 0; u < kHeadsAhead; ++u) {
-            const int h = h0 + hh + u;
-            const bool have = hh + u < p.per_part && h < h1 && x.on;
-            float a[8], b[8];
-            if (have && live) {
-                va[u].get(a);
-                vb[u].get(b);
+        for (int i = 0; i < kAhead; ++i) {
+            const int h = h0 + (turn * kAhead + i) * per_row;
+            if ((turn * kAhead + i) * per_row >= p.heads) break;  // the same for all lanes
+            const bool mine = have && h < p.heads;
+            Pairs a, b;
+            if (live && mine) {
+                a.from(va[i]);
+                b.from(vb[i]);
             } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) a[j] = b[j] = 0.f;
+                a.zero();
+                b.zero();
             }
-            if (norm) {
-                float sq = 0.f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sq += a[j] * a[j] + b[j] * b[j];
-                sq = group_sum(sq, p.lanes_log2);
-                const float rstd = 1.f / sqrtf(sq / (float)p.head_dim + p.eps);
-                const float* wt = w[h < p.heads_q ? 0 : 1];
-                if (have && live) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        a[j] *= rstd * wt[x.a + j];
-                        b[j] *= rstd * wt[x.b + j];
-                    }
+            if (NORM) {
+                const float sq = group_sum(dot16(a, b, a, b), p.lanes_log2);
+                const float rstd = rsqrtf(sq * p.inv_dim + p.eps);
+                if (live && mine) {
+                    const float* w = sm.weight[h < p.heads_q ? 0 : 1];
+                    Pairs wa, wb;
+                    wa.from(w + x.a);
+                    wb.from(w + x.b);
+                    wa.times(rstd);
+                    wb.times(rstd);
+                    a.times(wa);
+                    b.times(wb);
                 }
             }
-            if (have) {
-                if (live && x.angle >= 0) rotate(inter, a, b, cs, sn);
-                T* dst = h < p.heads_q ? q_out + r * p.ld_q_out + h * p.head_dim
-                                       : k_out + r * p.ld_k_out + (h - p.heads_q) * p.head_dim;
-                Vec8<T>::store(dst + x.a, a);
-                Vec8<T>::store(dst + x.b, b);
+            if (mine) {
+                if (live && x.angle >= 0) rotate<INTER>(a, b, cs, sn);
+                T* dst = (h < p.heads_q ? qo : ko) + h * p.head_dim;
+                a.store(dst + x.a);
+                b.store(dst + x.b);
             }
         }
     }
 }
 
-// The gradient.  A group takes rows group, group + groups, ... and keeps its lanes' share of the two weight gradients in
-// registers; a block adds its groups in order and leaves one partial sum, which qk_weight_grad_kernel adds in order.
-template <class T>
-__global__ void __launch_bounds__(kThreads)
+// The gradient.  A block takes tiles of rows of queries, or of keys (so that a lane keeps one set of 16 sums of the weight
+// gradient in registers); it adds its groups in order at the end and leaves one partial sum, which qk_weight_grad_kernel adds
+// in order.
+template <class T, bool INTER, bool NORM>
+__global__ void __launch_bounds__(kThreads, 2)
 qk_bwd_kernel(QkArgs p, const T* q, const T* k, const T* dq_out, const T* dk_out, T* dq, T* dk, float* __restrict__ partial) {
-    __shared__ float w[2][kMaxHeadDim];
+    constexpr int kTurn = sizeof(T) == 2 ? 2 : 1;  // heads of a group in flight, each of two matrices
+    __shared__ __align__(16) Shared sm;
     __shared__ float part[kThreads][17];
-    load_weights(p, w);
-    const int lane = threadIdx.x & 31;
-    const int lanes = 1 << p.lanes_log2;
-    const int64_t groups = (int64_t)gridDim.x * (kThreads >> p.lanes_log2);
-    const int64_t group = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> p.lanes_log2;
-    const bool norm = !(p.flags & RAPID_QK_NO_NORM), inter = (p.flags & RAPID_QK_INTERLEAVED) != 0;
-    const Place x = place_of(p, lane & (lanes - 1));
-    float dw[2][16] = {};
-    const int64_t units = p.n_rows * p.parts;
-    const int64_t turns = (units + groups - 1) / groups;
-    for (int64_t turn = 0; turn < turns; ++turn) {
-        const int64_t unit = group + turn * groups;
-        const int64_t r = unit / p.parts;
-        const int h0 = (int)(unit - r * p.parts) * p.per_part;
-        const bool row = unit < units;
-        const int h1 = row ? min(h0 + p.per_part, p.heads) : h0;
-        const bool live = row && (p.mask == nullptr || p.mask[r] != 0);
-        float cs[8], sn[8];
-        if (live && x.on) {
-            angles(p, x, r, cs, sn);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sn[j] = -sn[j];  // rotate back
-        }
-#pragma unroll
-        for (int kind = 0; kind < 2; ++kind) {  // queries, keys: the sums of the weight gradients stay in registers
-            const int from = kind == 0 ? 0 : p.heads_q, to = kind == 0 ? p.heads_q : p.heads;
+    const int kind = (int)blockIdx.x < p.q_blocks ? 0 : 1;
+    const int heads = kind ? p.heads - p.heads_q : p.heads_q, per_row = p.per_row[kind];
+    const int block = kind ? blockIdx.x - p.q_blocks : blockIdx.x, blocks = kind ? gridDim.x - p.q_blocks : p.q_blocks;
+    const int64_t ld = kind ? p.ld_k : p.ld_q, ld_g = kind ? p.ld_k_out : p.ld_q_out, ld_out = kind ? p.ld_dk : p.ld_dq;
+    const int lanes = 1 << p.lanes_log2, groups = kThreads >> p.lanes_log2, group = threadIdx.x >> p.lanes_log2;
+    const int rows = groups / per_row, row = group / per_row, h0 = group - row * per_row;
+    const Place x = place_of(p, threadIdx.x & (lanes - 1));
+    if (NORM) load_weights(p, sm);
+    Pairs dwa, dwb;
+    dwa.zero();
+    dwb.zero();
+    for (int64_t r0 = (int64_t)block * rows; r0 < p.n_rows; r0 += (int64_t)blocks * rows) {
+        const int64_t r = r0 + row;
+        const bool have = row < rows && r < p.n_rows && x.on, live = have && row_live(p, r);
+        const T *in = (kind ? k : q) + r * ld, *gin = (kind ? dk_out : dq_out) + r * ld_g;
+        T* out = (kind ? dk : dq) + r * ld_out;
+        Pairs cs, sn;
+        bool angled = false;
 #pragma unroll 1
-            for (int hh = 0; hh < p.per_part; hh += 2) {
-                // whole warps skip turns that hold no head of this kind
-                const bool any = h0 + hh < min(h1, to) && h0 + hh + 1 >= from;
-                if (!__any_sync(0xffffffffu, any)) continue;
-                Vec8<T> xa[2], xb[2], ya[2], yb[2];
+        for (int turn = 0; turn * per_row * kTurn < heads; ++turn) {
+            Vec8<T> xa[kTurn], xb[kTurn], ya[kTurn], yb[kTurn];
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int h = h0 + hh + u;
-                    if (hh + u < p.per_part && h >= from && h < min(h1, to) && live && x.on) {
-                        const T* src = kind == 0 ? q + r * p.ld_q + h * p.head_dim : k + r * p.ld_k + (h - from) * p.head_dim;
-                        const T* g = kind == 0 ? dq_out + r * p.ld_q_out + h * p.head_dim
-                                               : dk_out + r * p.ld_k_out + (h - from) * p.head_dim;
-                        if (norm) {
-                            xa[u].load(src + x.a);
-                            xb[u].load(src + x.b);
-                        }
-                        ya[u].load(g + x.a);
-                        yb[u].load(g + x.b);
+            for (int i = 0; i < kTurn; ++i) {
+                const int h = h0 + (turn * kTurn + i) * per_row;
+                if (live && h < heads) {
+                    const T *src = in + h * p.head_dim, *g = gin + h * p.head_dim;
+                    if (NORM) {
+                        xa[i].load(src + x.a);
+                        xb[i].load(src + x.b);
+                    }
+                    ya[i].load(g + x.a);
+                    yb[i].load(g + x.b);
+                }
+            }
+            if (!angled) {
+                __syncthreads();  // the last tile's angles have been read
+                angles(p, sm, r0, rows);
+                __syncthreads();
+                angled = true;
+                if (live && x.angle >= 0) {
+                    cs.from(sm.cs + row * (p.rot_dim / 2) + x.angle);
+                    sn.from(sm.sn + row * (p.rot_dim / 2) + x.angle);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sn.v[j] = negated(sn.v[j]);  // rotate back
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kTurn; ++i) {
+                const int h = h0 + (turn * kTurn + i) * per_row;
+                if ((turn * kTurn + i) * per_row >= heads) break;  // the same for all lanes
+                const bool mine = have && h < heads;
+                Pairs a, b, ga, gb;
+                a.zero();
+                b.zero();
+                ga.zero();
+                gb.zero();
+                if (live && mine) {
+                    ga.from(ya[i]);
+                    gb.from(yb[i]);
+                    if (x.angle >= 0) rotate<INTER>(ga, gb, cs, sn);
+                    if (NORM) {
+                        a.from(xa[i]);
+                        b.from(xb[i]);
                     }
                 }
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int h = h0 + hh + u;
-                    const bool have = hh + u < p.per_part && h >= from && h < min(h1, to) && x.on;
-                    const bool on = have && live;
-                    float a[8], b[8], ga[8], gb[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) a[j] = b[j] = ga[j] = gb[j] = 0.f;
-                    if (on) {
-                        ya[u].get(ga);
-                        yb[u].get(gb);
-                        if (x.angle >= 0) rotate(inter, ga, gb, cs, sn);
+                if (NORM) {
+                    // both sums go round together: x . x, and (w y') . x, of which xh = x * rstd needs rstd more
+                    Pairs wa, wb;
+                    wa.from(sm.weight[kind] + (x.on ? x.a : 0));
+                    wb.from(sm.weight[kind] + (x.on ? x.b : 0));
+                    wa.times(ga);
+                    wb.times(gb);
+                    float sq = dot16(a, b, a, b), dot = dot16(wa, wb, a, b);
+                    for (int o = 1; o < lanes; o <<= 1) {
+                        sq += __shfl_xor_sync(0xffffffffu, sq, o);
+                        dot += __shfl_xor_sync(0xffffffffu, dot, o);
                     }
-                    if (norm) {
-                        if (on) {
-                            xa[u].get(a);
-                            xb[u].get(b);
-                        }
-                        float sq = 0.f;
+                    if (live && mine) {
+                        const float rstd = rsqrtf(sq * p.inv_dim + p.eps);
+                        // dx = rstd (w y' - xh mean(w y' xh)) = rstd w y' - x rstd^3 (w y' . x) / head_dim
+                        const float back = -dot * p.inv_dim * rstd * rstd * rstd;
+                        const uint64_t r2 = f32x2(rstd, rstd), b2 = f32x2(back, back);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) sq += a[j] * a[j] + b[j] * b[j];
-                        sq = group_sum(sq, p.lanes_log2);
-                        const float rstd = 1.f / sqrtf(sq / (float)p.head_dim + p.eps);
-                        float dot = 0.f;
-                        if (on) {
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                a[j] *= rstd;
-                                b[j] *= rstd;
-                                dw[kind][j] += ga[j] * a[j];
-                                dw[kind][8 + j] += gb[j] * b[j];
-                                ga[j] *= w[kind][x.a + j];
-                                gb[j] *= w[kind][x.b + j];
-                                dot += ga[j] * a[j] + gb[j] * b[j];
-                            }
-                        }
-                        dot = group_sum(dot, p.lanes_log2) / (float)p.head_dim;
-                        if (on) {
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                ga[j] = (ga[j] - a[j] * dot) * rstd;
-                                gb[j] = (gb[j] - b[j] * dot) * rstd;
-                            }
+                        for (int j = 0; j < 4; ++j) {
+                            dwa.v[j] = f32x2_fma(ga.v[j], f32x2_mul(a.v[j], r2), dwa.v[j]);
+                            dwb.v[j] = f32x2_fma(gb.v[j], f32x2_mul(b.v[j], r2), dwb.v[j]);
+                            ga.v[j] = f32x2_fma(a.v[j], b2, f32x2_mul(wa.v[j], r2));
+                            gb.v[j] = f32x2_fma(b.v[j], b2, f32x2_mul(wb.v[j], r2));
                         }
                     }
-                    if (have) {
-                        T* dst = kind == 0 ? dq + r * p.ld_dq + h * p.head_dim : dk + r * p.ld_dk + (h - from) * p.head_dim;
-                        Vec8<T>::store(dst + x.a, ga);
-                        Vec8<T>::store(dst + x.b, gb);
-                    }
+                }
+                if (mine) {
+                    T* dst = out + h * p.head_dim;
+                    ga.store(dst + x.a);
+                    gb.store(dst + x.b);
                 }
             }
         }
     }
-    if (!norm) return;
+    if (!NORM) return;
 #pragma unroll
-    for (int kind = 0; kind < 2; ++kind) {
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 16; ++j) part[threadIdx.x][j] = dw[kind][j];
-        __syncthreads();
-        // thread (lane u of a group, element j): the sum over the block's groups
-        for (int i = threadIdx.x; i < lanes * 16; i += kThreads) {
-            const int u = i >> 4, j = i & 15;
-            const Place y = place_of(p, u);
-            if (!y.on) continue;
-            float sum = 0.f;
-            for (int g = 0; g < (kThreads >> p.lanes_log2); ++g) sum += part[g * lanes + u][j];
-            partial[((size_t)blockIdx.x * 2 + kind) * kMaxHeadDim + (j < 8 ? y.a + j : y.b + j - 8)] = sum;
-        }
+    for (int j = 0; j < 4; ++j) {
+        f32x2_split(dwa.v[j], part[threadIdx.x][2 * j], part[threadIdx.x][2 * j + 1]);
+        f32x2_split(dwb.v[j], part[threadIdx.x][8 + 2 * j], part[threadIdx.x][9 + 2 * j]);
+    }
+    __syncthreads();
+    // thread (lane u of a group, element j): the sum over the block's groups
+    for (int i = threadIdx.x; i < lanes * 16; i += kThreads) {
+        const int u = i >> 4, j = i & 15;
+        const Place y = place_of(p, u);
+        if (!y.on) continue;
+        float sum = 0.f;
+        for (int g = 0; g < groups; ++g) sum += part[g * lanes + u][j];
+        partial[(size_t)blockIdx.x * kMaxHeadDim + (j < 8 ? y.a + j : y.b + j - 8)] = sum;
     }
 }
 
 // One block for each kind and 8 columns: 32 threads a column each add every 32nd partial sum, then the 32 sums in order.
 __global__ void __launch_bounds__(256)
-qk_weight_grad_kernel(int blocks, int head_dim, const float* __restrict__ partial, float* __restrict__ dq_weight,
+qk_weight_grad_kernel(int q_blocks, int blocks, const float* __restrict__ partial, float* __restrict__ dq_weight,
                       float* __restrict__ dk_weight) {
     __shared__ double part[8][33];
     const int kind = blockIdx.y, col = threadIdx.x & 7, slice = threadIdx.x >> 3;
     const int c = blockIdx.x * 8 + col;
+    const int from = kind ? q_blocks : 0, to = kind ? blocks : q_blocks;
     double sum = 0.0;
-    for (int b = slice; b < blocks; b += 32) sum += (double)partial[((size_t)b * 2 + kind) * kMaxHeadDim + c];
+    for (int b = from + slice; b < to; b += 32) sum += (double)partial[(size_t)b * kMaxHeadDim + c];
     part[col][slice] = sum;
     __syncthreads();
     if (threadIdx.x < 8) {
@@ -346,7 +419,7 @@ rapid_status_t check_qk(const rapid_qk_desc_t* d, bool bwd) {
 }
 
 QkArgs make_args(const rapid_qk_desc_t& d, const float* q_weight, const float* k_weight, const float* inv_freq,
-                 const int32_t* positions, const uint8_t* mask, int sms) {
+                 const int32_t* positions, const uint8_t* mask) {
     QkArgs p{};
     p.n_rows = (int64_t)d.n_seq * d.seq_len;
     p.seq_len = d.seq_len;
@@ -355,14 +428,9 @@ QkArgs make_args(const rapid_qk_desc_t& d, const float* q_weight, const float* k
     p.head_dim = d.head_dim;
     p.rot_dim = d.rot_dim;
     while ((16 << p.lanes_log2) < d.head_dim) ++p.lanes_log2;
-    // Few rows: split a row's heads over groups until there are about 16 warps for each SM.
-    const int64_t groups = (int64_t)sms * 16 * (32 >> p.lanes_log2);
-    int64_t parts = (groups + p.n_rows - 1) / p.n_rows;
-    if (parts > p.heads) parts = p.heads;
-    p.per_part = (int)((p.heads + parts - 1) / parts);
-    p.parts = (p.heads + p.per_part - 1) / p.per_part;
     p.flags = d.flags;
     p.eps = d.eps;
+    p.inv_dim = 1.f / (float)d.head_dim;
     p.ld_q = d.ld_q;
     p.ld_k = d.ld_k;
     p.ld_q_out = d.ld_q_out;
@@ -377,17 +445,31 @@ QkArgs make_args(const rapid_qk_desc_t& d, const float* q_weight, const float* k
     return p;
 }
 
-int64_t blocks_for(const QkArgs& p) {
-    const int64_t per_block = kThreads >> p.lanes_log2;
-    return (p.n_rows * p.parts + per_block - 1) / per_block;
+// Groups on one row, so that each has up to `ahead` heads to take; with few rows more, for about `blocks` blocks.
+int groups_per_row(const QkArgs& p, int heads, int ahead, int64_t blocks) {
+    const int groups = kThreads >> p.lanes_log2, most = heads < groups ? heads : groups;
+    int per_row = (heads + ahead - 1) / ahead;
+    while (per_row < most && p.n_rows * per_row < blocks * groups) per_row *= 2;
+    return per_row < most ? per_row : most;
+}
+int tile_rows(const QkArgs& p, int per_row) { return (kThreads >> p.lanes_log2) / per_row; }
+
+template <class T>
+void run_fwd(const QkArgs& p, unsigned grid, const void* q, const void* k, void* q_out, void* k_out, cudaStream_t st) {
+    const bool inter = (p.flags & RAPID_QK_INTERLEAVED) != 0, norm = !(p.flags & RAPID_QK_NO_NORM);
+    auto kern = inter ? (norm ? qk_fwd_kernel<T, true, true> : qk_fwd_kernel<T, true, false>)
+                      : (norm ? qk_fwd_kernel<T, false, true> : qk_fwd_kernel<T, false, false>);
+    kern<<<grid, kThreads, 0, st>>>(p, static_cast<const T*>(q), static_cast<const T*>(k), static_cast<T*>(q_out), static_cast<T*>(k_out));
 }
 
 template <class T>
 void run_bwd(const QkArgs& p, int grid, const void* q, const void* k, const void* dq_out, const void* dk_out, void* dq, void* dk,
              float* partial, cudaStream_t st) {
-    qk_bwd_kernel<T><<<grid, kThreads, 0, st>>>(p, static_cast<const T*>(q), static_cast<const T*>(k),
-                                                static_cast<const T*>(dq_out), static_cast<const T*>(dk_out),
-                                                static_cast<T*>(dq), static_cast<T*>(dk), partial);
+    const bool inter = (p.flags & RAPID_QK_INTERLEAVED) != 0, norm = !(p.flags & RAPID_QK_NO_NORM);
+    auto kern = inter ? (norm ? qk_bwd_kernel<T, true, true> : qk_bwd_kernel<T, true, false>)
+                      : (norm ? qk_bwd_kernel<T, false, true> : qk_bwd_kernel<T, false, false>);
+    kern<<<grid, kThreads, 0, st>>>(p, static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(dq_out),
+                                    static_cast<const T*>(dk_out), static_cast<T*>(dq), static_cast<T*>(dk), partial);
 }
 
 }  // namespace
@@ -417,16 +499,12 @@ extern "C" rapid_status_t rapid_qk_norm_rope_fwd(const rapid_qk_desc_t* desc, co
         return RAPID_ERR_INVALID_ARG;
     int sms = 0;
     if ((s = check_device(&sms)) != RAPID_OK) return s;
-    const QkArgs p = make_args(d, q_weight, k_weight, inv_freq, positions, mask, sms);
-    const int64_t grid = blocks_for(p);
-    if (grid > 0x7fffffffll) return RAPID_ERR_UNSUPPORTED;
+    QkArgs p = make_args(d, q_weight, k_weight, inv_freq, positions, mask);
+    p.per_row[0] = groups_per_row(p, p.heads, kAhead, 2 * sms);
+    const int64_t rows = tile_rows(p, p.per_row[0]), grid = (p.n_rows + rows - 1) / rows;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (d.dtype == RAPID_BF16)
-        qk_fwd_kernel<uint16_t><<<(unsigned)grid, kThreads, 0, st>>>(p, static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k),
-                                                                    static_cast<uint16_t*>(q_out), static_cast<uint16_t*>(k_out));
-    else
-        qk_fwd_kernel<float><<<(unsigned)grid, kThreads, 0, st>>>(p, static_cast<const float*>(q), static_cast<const float*>(k),
-                                                                 static_cast<float*>(q_out), static_cast<float*>(k_out));
+    if (d.dtype == RAPID_BF16) run_fwd<uint16_t>(p, (unsigned)grid, q, k, q_out, k_out, st);
+    else run_fwd<float>(p, (unsigned)grid, q, k, q_out, k_out, st);
     return cudaGetLastError() == cudaSuccess ? RAPID_OK : RAPID_ERR_CUDA;
 }
 
@@ -434,7 +512,7 @@ extern "C" rapid_status_t rapid_qk_norm_rope_bwd_workspace_bytes(const rapid_qk_
     if (!bytes) return RAPID_ERR_INVALID_ARG;
     rapid_status_t s = check_qk(desc, true);
     if (s != RAPID_OK) return s;
-    *bytes = (size_t)kMaxBwdBlocks * 2 * kMaxHeadDim * sizeof(float);
+    *bytes = (size_t)(kMaxBwdBlocks + 1) * kMaxHeadDim * sizeof(float);
     return RAPID_OK;
 }
 
@@ -467,16 +545,25 @@ extern "C" rapid_status_t rapid_qk_norm_rope_bwd(const rapid_qk_desc_t* desc, co
     if (norm && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return RAPID_ERR_WORKSPACE;
     int sms = 0;
     if ((s = check_device(&sms)) != RAPID_OK) return s;
-    const QkArgs p = make_args(d, q_weight, k_weight, inv_freq, positions, mask, sms);
-    int64_t grid = blocks_for(p);
-    int64_t most = (int64_t)sms * 2 * 2;  // two resident blocks an SM, twice over
-    if (most > kMaxBwdBlocks) most = kMaxBwdBlocks;
-    if (grid > most) grid = most;
+    QkArgs p = make_args(d, q_weight, k_weight, inv_freq, positions, mask);
+    const int most = 2 * sms < kMaxBwdBlocks ? 2 * sms : kMaxBwdBlocks;  // two blocks are resident on an SM
+    // queries and keys share the blocks by their heads; no block without a tile
+    int64_t blocks[2];
+    for (int kind = 0; kind < 2; ++kind) {
+        const int heads = kind ? d.n_k_heads : d.n_q_heads;
+        int64_t part = (int64_t)most * heads / p.heads;
+        if (part < 1) part = 1;
+        p.per_row[kind] = groups_per_row(p, heads, kAhead, part);
+        const int64_t rows = tile_rows(p, p.per_row[kind]), tiles = (p.n_rows + rows - 1) / rows;
+        blocks[kind] = tiles < part ? tiles : part;
+    }
+    p.q_blocks = (int)blocks[0];
+    const int64_t grid = blocks[0] + blocks[1];
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     float* partial = static_cast<float*>(workspace);
     if (d.dtype == RAPID_BF16) run_bwd<uint16_t>(p, (int)grid, q, k, dq_out, dk_out, dq, dk, partial, st);
     else run_bwd<float>(p, (int)grid, q, k, dq_out, dk_out, dq, dk, partial, st);
     if (norm)
-        qk_weight_grad_kernel<<<dim3((unsigned)(d.head_dim / 8), 2), 256, 0, st>>>((int)grid, d.head_dim, partial, dq_weight, dk_weight);
+        qk_weight_grad_kernel<<<dim3((unsigned)(d.head_dim / 8), 2), 256, 0, st>>>(p.q_blocks, (int)grid, partial, dq_weight, dk_weight);
     return cudaGetLastError() == cudaSuccess ? RAPID_OK : RAPID_ERR_CUDA;
 }
