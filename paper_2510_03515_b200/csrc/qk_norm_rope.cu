@@ -26,9 +26,8 @@ constexpr int kAhead = 4;     // heads of a group in flight, at most
 struct QkArgs {
     int64_t n_rows;
     int seq_len, heads_q, heads, head_dim, rot_dim;  // heads = queries and keys together
-    int lanes_log2;                                  // lanes of a head
-    int per_row[2];                                  // groups on one row; backward: of queries, of keys
-    int q_blocks;                                    // backward: blocks that take queries
+    int lanes_log2;  // lanes of a head (a template argument of the kernels): 2, 3 or 4
+    int per_row;     // groups on one row
     uint32_t flags;
     float eps, inv_dim;
     int64_t ld_q, ld_k, ld_q_out, ld_k_out, ld_dq, ld_dk;
@@ -118,6 +117,14 @@ struct Pairs {
     }
 };
 __device__ __forceinline__ uint64_t negated(uint64_t x) { return x ^ 0x8000000080000000ull; }
+template <bool INTER>
+__device__ __forceinline__ void rotate(Pairs& a, Pairs& b, const Pairs& cs, const Pairs& sn);
+template <bool INTER>
+__device__ __forceinline__ void rotate_back(Pairs& a, Pairs& b, const Pairs& cs, Pairs sn) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sn.v[j] = negated(sn.v[j]);
+    rotate<INTER>(a, b, cs, sn);
+}
 
 // (a_i, b_i) -> (a_i c - b_i s, a_i s + b_i c) over the lane's 8 pairs; halves: a and b, interleaved: neighbours
 template <bool INTER>
@@ -146,8 +153,10 @@ __device__ __forceinline__ void rotate(Pairs& a, Pairs& b, const Pairs& cs, cons
     }
 }
 
-__device__ __forceinline__ float group_sum(float v, int lanes_log2) {
-    for (int o = 1; o < (1 << lanes_log2); o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+template <int LANES_LOG2>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+    for (int o = 1; o < (1 << LANES_LOG2); o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
 // sum over the lane's 16 elements of x * y
@@ -171,18 +180,28 @@ __device__ __forceinline__ void load_weights(const QkArgs& p, Shared& sm) {
     }
 }
 
-template <class T, bool INTER, bool NORM>
+// a lane's part of a row's head that has nothing in it
+template <class T>
+__device__ __forceinline__ void store_zeros(T* dst, const Place& x) {
+    const float z[8] = {};
+    Vec8<T>::store(dst + x.a, z);
+    Vec8<T>::store(dst + x.b, z);
+}
+
+template <class T, int LANES_LOG2, bool INTER, bool NORM>
 __global__ void __launch_bounds__(kThreads, 2)
 qk_fwd_kernel(QkArgs p, const T* q, const T* k, T* q_out, T* k_out) {
     __shared__ __align__(16) Shared sm;
-    const int lanes = 1 << p.lanes_log2, groups = kThreads >> p.lanes_log2, group = threadIdx.x >> p.lanes_log2;
-    const int per_row = p.per_row[0], rows = groups / per_row;
+    constexpr int lanes = 1 << LANES_LOG2, groups = kThreads >> LANES_LOG2;
+    const int group = threadIdx.x >> LANES_LOG2;
+    const int per_row = p.per_row, rows = groups / per_row;
     const int row = group / per_row, h0 = group - row * per_row;
     const int64_t r0 = (int64_t)blockIdx.x * rows, r = r0 + row;
     const Place x = place_of(p, threadIdx.x & (lanes - 1));
     const bool have = row < rows && r < p.n_rows && x.on, live = have && row_live(p, r);
     const T *qr = q + r * p.ld_q, *kr = k + r * p.ld_k - (int64_t)p.heads_q * p.head_dim;
     T *qo = q_out + r * p.ld_q_out, *ko = k_out + r * p.ld_k_out - (int64_t)p.heads_q * p.head_dim;
+    const bool warp_live = __any_sync(0xffffffffu, live);
     Pairs cs, sn;
     bool angled = false;
     // the same number of turns in every lane: the sums exchange over whole warps
@@ -213,6 +232,11 @@ qk_fwd_kernel(QkArgs p, const T* q, const T* k, T* q_out, T* k_out) {
             const int h = h0 + (turn * kAhead + i) * per_row;
             if ((turn * kAhead + i) * per_row >= p.heads) break;  // the same for all lanes
             const bool mine = have && h < p.heads;
+            T* dst = (h < p.heads_q ? qo : ko) + h * p.head_dim;
+            if (!warp_live) {
+                if (mine) store_zeros(dst, x);
+                continue;
+            }
             Pairs a, b;
             if (live && mine) {
                 a.from(va[i]);
@@ -222,22 +246,21 @@ qk_fwd_kernel(QkArgs p, const T* q, const T* k, T* q_out, T* k_out) {
                 b.zero();
             }
             if (NORM) {
-                const float sq = group_sum(dot16(a, b, a, b), p.lanes_log2);
+                const float sq = group_sum<LANES_LOG2>(dot16(a, b, a, b));
                 const float rstd = rsqrtf(sq * p.inv_dim + p.eps);
                 if (live && mine) {
                     const float* w = sm.weight[h < p.heads_q ? 0 : 1];
                     Pairs wa, wb;
                     wa.from(w + x.a);
                     wb.from(w + x.b);
-                    wa.times(rstd);
-                    wb.times(rstd);
                     a.times(wa);
                     b.times(wb);
+                    a.times(rstd);
+                    b.times(rstd);
                 }
             }
             if (mine) {
                 if (live && x.angle >= 0) rotate<INTER>(a, b, cs, sn);
-                T* dst = (h < p.heads_q ? qo : ko) + h * p.head_dim;
                 a.store(dst + x.a);
                 b.store(dst + x.b);
             }
@@ -245,142 +268,151 @@ qk_fwd_kernel(QkArgs p, const T* q, const T* k, T* q_out, T* k_out) {
     }
 }
 
-// The gradient.  A block takes tiles of rows of queries, or of keys (so that a lane keeps one set of 16 sums of the weight
-// gradient in registers); it adds its groups in order at the end and leaves one partial sum, which qk_weight_grad_kernel adds
-// in order.
-template <class T, bool INTER, bool NORM>
+// The gradient.  A lane keeps its 16 sums of either weight gradient in registers, a block adds its groups in order at the
+// end and leaves one partial sum, which qk_weight_grad_kernel adds in order.
+template <class T, int LANES_LOG2, bool INTER, bool NORM>
 __global__ void __launch_bounds__(kThreads, 2)
 qk_bwd_kernel(QkArgs p, const T* q, const T* k, const T* dq_out, const T* dk_out, T* dq, T* dk, float* __restrict__ partial) {
     constexpr int kTurn = sizeof(T) == 2 ? 2 : 1;  // heads of a group in flight, each of two matrices
     __shared__ __align__(16) Shared sm;
     __shared__ float part[kThreads][17];
-    const int kind = (int)blockIdx.x < p.q_blocks ? 0 : 1;
-    const int heads = kind ? p.heads - p.heads_q : p.heads_q, per_row = p.per_row[kind];
-    const int block = kind ? blockIdx.x - p.q_blocks : blockIdx.x, blocks = kind ? gridDim.x - p.q_blocks : p.q_blocks;
-    const int64_t ld = kind ? p.ld_k : p.ld_q, ld_g = kind ? p.ld_k_out : p.ld_q_out, ld_out = kind ? p.ld_dk : p.ld_dq;
-    const int lanes = 1 << p.lanes_log2, groups = kThreads >> p.lanes_log2, group = threadIdx.x >> p.lanes_log2;
-    const int rows = groups / per_row, row = group / per_row, h0 = group - row * per_row;
+    constexpr int lanes = 1 << LANES_LOG2, groups = kThreads >> LANES_LOG2;
+    const int group = threadIdx.x >> LANES_LOG2;
+    const int per_row = p.per_row, rows = groups / per_row, row = group / per_row, h0 = group - row * per_row;
     const Place x = place_of(p, threadIdx.x & (lanes - 1));
     if (NORM) load_weights(p, sm);
-    Pairs dwa, dwb;
-    dwa.zero();
-    dwb.zero();
-    for (int64_t r0 = (int64_t)block * rows; r0 < p.n_rows; r0 += (int64_t)blocks * rows) {
+    Pairs dwa[2], dwb[2];
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+        dwa[kind].zero();
+        dwb[kind].zero();
+    }
+    for (int64_t r0 = (int64_t)blockIdx.x * rows; r0 < p.n_rows; r0 += (int64_t)gridDim.x * rows) {
         const int64_t r = r0 + row;
         const bool have = row < rows && r < p.n_rows && x.on, live = have && row_live(p, r);
-        const T *in = (kind ? k : q) + r * ld, *gin = (kind ? dk_out : dq_out) + r * ld_g;
-        T* out = (kind ? dk : dq) + r * ld_out;
-        Pairs cs, sn;
+        const bool warp_live = __any_sync(0xffffffffu, live);
         bool angled = false;
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind) {
+            const int heads = kind ? p.heads - p.heads_q : p.heads_q;
+            const T *in = (kind ? k : q) + r * (kind ? p.ld_k : p.ld_q), *gin = (kind ? dk_out : dq_out) + r * (kind ? p.ld_k_out : p.ld_q_out);
+            T* out = (kind ? dk : dq) + r * (kind ? p.ld_dk : p.ld_dq);
 #pragma unroll 1
-        for (int turn = 0; turn * per_row * kTurn < heads; ++turn) {
-            Vec8<T> xa[kTurn], xb[kTurn], ya[kTurn], yb[kTurn];
+            for (int turn = 0; turn * per_row * kTurn < heads; ++turn) {
+                Vec8<T> xa[kTurn], xb[kTurn], ya[kTurn], yb[kTurn];
 #pragma unroll
-            for (int i = 0; i < kTurn; ++i) {
-                const int h = h0 + (turn * kTurn + i) * per_row;
-                if (live && h < heads) {
-                    const T *src = in + h * p.head_dim, *g = gin + h * p.head_dim;
-                    if (NORM) {
-                        xa[i].load(src + x.a);
-                        xb[i].load(src + x.b);
-                    }
-                    ya[i].load(g + x.a);
-                    yb[i].load(g + x.b);
-                }
-            }
-            if (!angled) {
-                __syncthreads();  // the last tile's angles have been read
-                angles(p, sm, r0, rows);
-                __syncthreads();
-                angled = true;
-                if (live && x.angle >= 0) {
-                    cs.from(sm.cs + row * (p.rot_dim / 2) + x.angle);
-                    sn.from(sm.sn + row * (p.rot_dim / 2) + x.angle);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) sn.v[j] = negated(sn.v[j]);  // rotate back
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kTurn; ++i) {
-                const int h = h0 + (turn * kTurn + i) * per_row;
-                if ((turn * kTurn + i) * per_row >= heads) break;  // the same for all lanes
-                const bool mine = have && h < heads;
-                Pairs a, b, ga, gb;
-                a.zero();
-                b.zero();
-                ga.zero();
-                gb.zero();
-                if (live && mine) {
-                    ga.from(ya[i]);
-                    gb.from(yb[i]);
-                    if (x.angle >= 0) rotate<INTER>(ga, gb, cs, sn);
-                    if (NORM) {
-                        a.from(xa[i]);
-                        b.from(xb[i]);
+                for (int i = 0; i < kTurn; ++i) {
+                    const int h = h0 + (turn * kTurn + i) * per_row;
+                    if (live && h < heads) {
+                        const T *src = in + h * p.head_dim, *g = gin + h * p.head_dim;
+                        if (NORM) {
+                            xa[i].load(src + x.a);
+                            xb[i].load(src + x.b);
+                        }
+                        ya[i].load(g + x.a);
+                        yb[i].load(g + x.b);
                     }
                 }
-                if (NORM) {
-                    // both sums go round together: x . x, and (w y') . x, of which xh = x * rstd needs rstd more
-                    Pairs wa, wb;
-                    wa.from(sm.weight[kind] + (x.on ? x.a : 0));
-                    wb.from(sm.weight[kind] + (x.on ? x.b : 0));
-                    wa.times(ga);
-                    wb.times(gb);
-                    float sq = dot16(a, b, a, b), dot = dot16(wa, wb, a, b);
-                    for (int o = 1; o < lanes; o <<= 1) {
-                        sq += __shfl_xor_sync(0xffffffffu, sq, o);
-                        dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                if (!angled) {
+                    __syncthreads();  // the last tile's angles have been read
+                    angles(p, sm, r0, rows);
+                    __syncthreads();
+                    angled = true;
+                }
+#pragma unroll
+                for (int i = 0; i < kTurn; ++i) {
+                    const int h = h0 + (turn * kTurn + i) * per_row;
+                    if ((turn * kTurn + i) * per_row >= heads) break;  // the same for all lanes
+                    const bool mine = have && h < heads;
+                    T* dst = out + h * p.head_dim;
+                    if (!warp_live) {
+                        if (mine) store_zeros(dst, x);
+                        continue;
                     }
+                    Pairs a, b, ga, gb;
+                    a.zero();
+                    b.zero();
+                    ga.zero();
+                    gb.zero();
                     if (live && mine) {
-                        const float rstd = rsqrtf(sq * p.inv_dim + p.eps);
-                        // dx = rstd (w y' - xh mean(w y' xh)) = rstd w y' - x rstd^3 (w y' . x) / head_dim
-                        const float back = -dot * p.inv_dim * rstd * rstd * rstd;
-                        const uint64_t r2 = f32x2(rstd, rstd), b2 = f32x2(back, back);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            dwa.v[j] = f32x2_fma(ga.v[j], f32x2_mul(a.v[j], r2), dwa.v[j]);
-                            dwb.v[j] = f32x2_fma(gb.v[j], f32x2_mul(b.v[j], r2), dwb.v[j]);
-                            ga.v[j] = f32x2_fma(a.v[j], b2, f32x2_mul(wa.v[j], r2));
-                            gb.v[j] = f32x2_fma(b.v[j], b2, f32x2_mul(wb.v[j], r2));
+                        ga.from(ya[i]);
+                        gb.from(yb[i]);
+                        if (x.angle >= 0) {
+                            Pairs cs, sn;
+                            cs.from(sm.cs + row * (p.rot_dim / 2) + x.angle);
+                            sn.from(sm.sn + row * (p.rot_dim / 2) + x.angle);
+                            rotate_back<INTER>(ga, gb, cs, sn);
+                        }
+                        if (NORM) {
+                            a.from(xa[i]);
+                            b.from(xb[i]);
                         }
                     }
-                }
-                if (mine) {
-                    T* dst = out + h * p.head_dim;
-                    ga.store(dst + x.a);
-                    gb.store(dst + x.b);
+                    if (NORM) {
+                        // both sums go round together: x . x, and (w y') . x, of which xh = x * rstd needs rstd more
+                        Pairs wa, wb;
+                        wa.from(sm.weight[kind] + (x.on ? x.a : 0));
+                        wb.from(sm.weight[kind] + (x.on ? x.b : 0));
+                        wa.times(ga);
+                        wb.times(gb);
+                        float sq = dot16(a, b, a, b), dot = dot16(wa, wb, a, b);
+#pragma unroll
+                        for (int o = 1; o < lanes; o <<= 1) {
+                            sq += __shfl_xor_sync(0xffffffffu, sq, o);
+                            dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                        }
+                        if (live && mine) {
+                            const float rstd = rsqrtf(sq * p.inv_dim + p.eps);
+                            // dx = rstd (w y' - xh mean(w y' xh)) = rstd w y' - x rstd^3 (w y' . x) / head_dim
+                            const float back = -dot * p.inv_dim * rstd * rstd * rstd;
+                            const uint64_t r2 = f32x2(rstd, rstd), b2 = f32x2(back, back);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                dwa[kind].v[j] = f32x2_fma(ga.v[j], f32x2_mul(a.v[j], r2), dwa[kind].v[j]);
+                                dwb[kind].v[j] = f32x2_fma(gb.v[j], f32x2_mul(b.v[j], r2), dwb[kind].v[j]);
+                                ga.v[j] = f32x2_fma(a.v[j], b2, f32x2_mul(wa.v[j], r2));
+                                gb.v[j] = f32x2_fma(b.v[j], b2, f32x2_mul(wb.v[j], r2));
+                            }
+                        }
+                    }
+                    if (mine) {
+                        ga.store(dst + x.a);
+                        gb.store(dst + x.b);
+                    }
                 }
             }
         }
     }
     if (!NORM) return;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        f32x2_split(dwa.v[j], part[threadIdx.x][2 * j], part[threadIdx.x][2 * j + 1]);
-        f32x2_split(dwb.v[j], part[threadIdx.x][8 + 2 * j], part[threadIdx.x][9 + 2 * j]);
-    }
-    __syncthreads();
-    // thread (lane u of a group, element j): the sum over the block's groups
-    for (int i = threadIdx.x; i < lanes * 16; i += kThreads) {
-        const int u = i >> 4, j = i & 15;
-        const Place y = place_of(p, u);
-        if (!y.on) continue;
-        float sum = 0.f;
-        for (int g = 0; g < groups; ++g) sum += part[g * lanes + u][j];
-        partial[(size_t)blockIdx.x * kMaxHeadDim + (j < 8 ? y.a + j : y.b + j - 8)] = sum;
+    for (int kind = 0; kind < 2; ++kind) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            f32x2_split(dwa[kind].v[j], part[threadIdx.x][2 * j], part[threadIdx.x][2 * j + 1]);
+            f32x2_split(dwb[kind].v[j], part[threadIdx.x][8 + 2 * j], part[threadIdx.x][9 + 2 * j]);
+        }
+        __syncthreads();
+        // thread (lane u of a group, element j): the sum over the block's groups
+        for (int i = threadIdx.x; i < lanes * 16; i += kThreads) {
+            const int u = i >> 4, j = i & 15;
+            const Place y = place_of(p, u);
+            if (!y.on) continue;
+            float sum = 0.f;
+            for (int g = 0; g < groups; ++g) sum += part[g * lanes + u][j];
+            partial[((size_t)blockIdx.x * 2 + kind) * kMaxHeadDim + (j < 8 ? y.a + j : y.b + j - 8)] = sum;
+        }
     }
 }
 
 // One block for each kind and 8 columns: 32 threads a column each add every 32nd partial sum, then the 32 sums in order.
 __global__ void __launch_bounds__(256)
-qk_weight_grad_kernel(int q_blocks, int blocks, const float* __restrict__ partial, float* __restrict__ dq_weight,
-                      float* __restrict__ dk_weight) {
+qk_weight_grad_kernel(int blocks, const float* __restrict__ partial, float* __restrict__ dq_weight, float* __restrict__ dk_weight) {
     __shared__ double part[8][33];
     const int kind = blockIdx.y, col = threadIdx.x & 7, slice = threadIdx.x >> 3;
     const int c = blockIdx.x * 8 + col;
-    const int from = kind ? q_blocks : 0, to = kind ? blocks : q_blocks;
     double sum = 0.0;
-    for (int b = from + slice; b < to; b += 32) sum += (double)partial[(size_t)b * kMaxHeadDim + c];
+    for (int b = slice; b < blocks; b += 32) sum += (double)partial[((size_t)b * 2 + kind) * kMaxHeadDim + c];
     part[col][slice] = sum;
     __syncthreads();
     if (threadIdx.x < 8) {
@@ -427,7 +459,7 @@ QkArgs make_args(const rapid_qk_desc_t& d, const float* q_weight, const float* k
     p.heads = d.n_q_heads + d.n_k_heads;
     p.head_dim = d.head_dim;
     p.rot_dim = d.rot_dim;
-    while ((16 << p.lanes_log2) < d.head_dim) ++p.lanes_log2;
+    p.lanes_log2 = d.head_dim <= 64 ? 2 : d.head_dim <= 128 ? 3 : 4;
     p.flags = d.flags;
     p.eps = d.eps;
     p.inv_dim = 1.f / (float)d.head_dim;
@@ -454,22 +486,33 @@ int groups_per_row(const QkArgs& p, int heads, int ahead, int64_t blocks) {
 }
 int tile_rows(const QkArgs& p, int per_row) { return (kThreads >> p.lanes_log2) / per_row; }
 
+template <class T, int LANES_LOG2>
+void run_fwd_as(const QkArgs& p, unsigned grid, const T* q, const T* k, T* q_out, T* k_out, cudaStream_t st) {
+    const bool inter = (p.flags & RAPID_QK_INTERLEAVED) != 0, norm = !(p.flags & RAPID_QK_NO_NORM);
+    auto kern = inter ? (norm ? qk_fwd_kernel<T, LANES_LOG2, true, true> : qk_fwd_kernel<T, LANES_LOG2, true, false>)
+                      : (norm ? qk_fwd_kernel<T, LANES_LOG2, false, true> : qk_fwd_kernel<T, LANES_LOG2, false, false>);
+    kern<<<grid, kThreads, 0, st>>>(p, q, k, q_out, k_out);
+}
 template <class T>
 void run_fwd(const QkArgs& p, unsigned grid, const void* q, const void* k, void* q_out, void* k_out, cudaStream_t st) {
-    const bool inter = (p.flags & RAPID_QK_INTERLEAVED) != 0, norm = !(p.flags & RAPID_QK_NO_NORM);
-    auto kern = inter ? (norm ? qk_fwd_kernel<T, true, true> : qk_fwd_kernel<T, true, false>)
-                      : (norm ? qk_fwd_kernel<T, false, true> : qk_fwd_kernel<T, false, false>);
-    kern<<<grid, kThreads, 0, st>>>(p, static_cast<const T*>(q), static_cast<const T*>(k), static_cast<T*>(q_out), static_cast<T*>(k_out));
+    auto run = p.lanes_log2 == 2 ? run_fwd_as<T, 2> : p.lanes_log2 == 3 ? run_fwd_as<T, 3> : run_fwd_as<T, 4>;
+    run(p, grid, static_cast<const T*>(q), static_cast<const T*>(k), static_cast<T*>(q_out), static_cast<T*>(k_out), st);
 }
 
-template <class T>
-void run_bwd(const QkArgs& p, int grid, const void* q, const void* k, const void* dq_out, const void* dk_out, void* dq, void* dk,
-             float* partial, cudaStream_t st) {
+template <class T, int LANES_LOG2>
+void run_bwd_as(const QkArgs& p, unsigned grid, const T* q, const T* k, const T* dq_out, const T* dk_out, T* dq, T* dk, float* partial,
+                cudaStream_t st) {
     const bool inter = (p.flags & RAPID_QK_INTERLEAVED) != 0, norm = !(p.flags & RAPID_QK_NO_NORM);
-    auto kern = inter ? (norm ? qk_bwd_kernel<T, true, true> : qk_bwd_kernel<T, true, false>)
-                      : (norm ? qk_bwd_kernel<T, false, true> : qk_bwd_kernel<T, false, false>);
-    kern<<<grid, kThreads, 0, st>>>(p, static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(dq_out),
-                                    static_cast<const T*>(dk_out), static_cast<T*>(dq), static_cast<T*>(dk), partial);
+    auto kern = inter ? (norm ? qk_bwd_kernel<T, LANES_LOG2, true, true> : qk_bwd_kernel<T, LANES_LOG2, true, false>)
+                      : (norm ? qk_bwd_kernel<T, LANES_LOG2, false, true> : qk_bwd_kernel<T, LANES_LOG2, false, false>);
+    kern<<<grid, kThreads, 0, st>>>(p, q, k, dq_out, dk_out, dq, dk, partial);
+}
+template <class T>
+void run_bwd(const QkArgs& p, unsigned grid, const void* q, const void* k, const void* dq_out, const void* dk_out, void* dq, void* dk,
+             float* partial, cudaStream_t st) {
+    auto run = p.lanes_log2 == 2 ? run_bwd_as<T, 2> : p.lanes_log2 == 3 ? run_bwd_as<T, 3> : run_bwd_as<T, 4>;
+    run(p, grid, static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(dq_out), static_cast<const T*>(dk_out),
+        static_cast<T*>(dq), static_cast<T*>(dk), partial, st);
 }
 
 }  // namespace
@@ -500,8 +543,8 @@ extern "C" rapid_status_t rapid_qk_norm_rope_fwd(const rapid_qk_desc_t* desc, co
     int sms = 0;
     if ((s = check_device(&sms)) != RAPID_OK) return s;
     QkArgs p = make_args(d, q_weight, k_weight, inv_freq, positions, mask);
-    p.per_row[0] = groups_per_row(p, p.heads, kAhead, 2 * sms);
-    const int64_t rows = tile_rows(p, p.per_row[0]), grid = (p.n_rows + rows - 1) / rows;
+    p.per_row = groups_per_row(p, p.heads, kAhead, 2 * sms);
+    const int64_t rows = tile_rows(p, p.per_row), grid = (p.n_rows + rows - 1) / rows;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (d.dtype == RAPID_BF16) run_fwd<uint16_t>(p, (unsigned)grid, q, k, q_out, k_out, st);
     else run_fwd<float>(p, (unsigned)grid, q, k, q_out, k_out, st);
@@ -512,7 +555,7 @@ extern "C" rapid_status_t rapid_qk_norm_rope_bwd_workspace_bytes(const rapid_qk_
     if (!bytes) return RAPID_ERR_INVALID_ARG;
     rapid_status_t s = check_qk(desc, true);
     if (s != RAPID_OK) return s;
-    *bytes = (size_t)(kMaxBwdBlocks + 1) * kMaxHeadDim * sizeof(float);
+    *bytes = (size_t)kMaxBwdBlocks * 2 * kMaxHeadDim * sizeof(float);
     return RAPID_OK;
 }
 
@@ -547,23 +590,14 @@ extern "C" rapid_status_t rapid_qk_norm_rope_bwd(const rapid_qk_desc_t* desc, co
     if ((s = check_device(&sms)) != RAPID_OK) return s;
     QkArgs p = make_args(d, q_weight, k_weight, inv_freq, positions, mask);
     const int most = 2 * sms < kMaxBwdBlocks ? 2 * sms : kMaxBwdBlocks;  // two blocks are resident on an SM
-    // queries and keys share the blocks by their heads; no block without a tile
-    int64_t blocks[2];
-    for (int kind = 0; kind < 2; ++kind) {
-        const int heads = kind ? d.n_k_heads : d.n_q_heads;
-        int64_t part = (int64_t)most * heads / p.heads;
-        if (part < 1) part = 1;
-        p.per_row[kind] = groups_per_row(p, heads, kAhead, part);
-        const int64_t rows = tile_rows(p, p.per_row[kind]), tiles = (p.n_rows + rows - 1) / rows;
-        blocks[kind] = tiles < part ? tiles : part;
-    }
-    p.q_blocks = (int)blocks[0];
-    const int64_t grid = blocks[0] + blocks[1];
+    p.per_row = groups_per_row(p, d.n_q_heads, kAhead, most);
+    const int64_t rows = tile_rows(p, p.per_row), tiles = (p.n_rows + rows - 1) / rows;
+    const unsigned grid = (unsigned)(tiles < most ? tiles : most);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     float* partial = static_cast<float*>(workspace);
-    if (d.dtype == RAPID_BF16) run_bwd<uint16_t>(p, (int)grid, q, k, dq_out, dk_out, dq, dk, partial, st);
-    else run_bwd<float>(p, (int)grid, q, k, dq_out, dk_out, dq, dk, partial, st);
+    if (d.dtype == RAPID_BF16) run_bwd<uint16_t>(p, grid, q, k, dq_out, dk_out, dq, dk, partial, st);
+    else run_bwd<float>(p, grid, q, k, dq_out, dk_out, dq, dk, partial, st);
     if (norm)
-        qk_weight_grad_kernel<<<dim3((unsigned)(d.head_dim / 8), 2), 256, 0, st>>>(p.q_blocks, (int)grid, partial, dq_weight, dk_weight);
+        qk_weight_grad_kernel<<<dim3((unsigned)(d.head_dim / 8), 2), 256, 0, st>>>((int)grid, partial, dq_weight, dk_weight);
     return cudaGetLastError() == cudaSuccess ? RAPID_OK : RAPID_ERR_CUDA;
 }
