@@ -196,73 +196,76 @@ qk_fwd_kernel(QkArgs p, const T* q, const T* k, T* q_out, T* k_out) {
     const int group = threadIdx.x >> LANES_LOG2;
     const int per_row = p.per_row, rows = groups / per_row;
     const int row = group / per_row, h0 = group - row * per_row;
-    const int64_t r0 = (int64_t)blockIdx.x * rows, r = r0 + row;
     const Place x = place_of(p, threadIdx.x & (lanes - 1));
-    const bool have = row < rows && r < p.n_rows && x.on, live = have && row_live(p, r);
-    const T *qr = q + r * p.ld_q, *kr = k + r * p.ld_k - (int64_t)p.heads_q * p.head_dim;
-    T *qo = q_out + r * p.ld_q_out, *ko = k_out + r * p.ld_k_out - (int64_t)p.heads_q * p.head_dim;
-    const bool warp_live = __any_sync(0xffffffffu, live);
-    Pairs cs, sn;
-    bool angled = false;
-    // the same number of turns in every lane: the sums exchange over whole warps
+    if (NORM) load_weights(p, sm);
+    for (int64_t r0 = (int64_t)blockIdx.x * rows; r0 < p.n_rows; r0 += (int64_t)gridDim.x * rows) {
+        const int64_t r = r0 + row;
+        const bool have = row < rows && r < p.n_rows && x.on, live = have && row_live(p, r);
+        const T *qr = q + r * p.ld_q, *kr = k + r * p.ld_k - (int64_t)p.heads_q * p.head_dim;
+        T *qo = q_out + r * p.ld_q_out, *ko = k_out + r * p.ld_k_out - (int64_t)p.heads_q * p.head_dim;
+        const bool warp_live = __any_sync(0xffffffffu, live);
+        bool angled = false;
+        // the same number of turns in every lane: the sums exchange over whole warps
 #pragma unroll 1
-    for (int turn = 0; turn * per_row * kAhead < p.heads; ++turn) {
-        Vec8<T> va[kAhead], vb[kAhead];
+        for (int turn = 0; turn * per_row * kAhead < p.heads; ++turn) {
+            Vec8<T> va[kAhead], vb[kAhead];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int h = h0 + (turn * kAhead + i) * per_row;
-            if (live && h < p.heads) {
-                const T* src = (h < p.heads_q ? qr : kr) + h * p.head_dim;
-                va[i].load(src + x.a);
-                vb[i].load(src + x.b);
+            for (int i = 0; i < kAhead; ++i) {
+                const int h = h0 + (turn * kAhead + i) * per_row;
+                if (live && h < p.heads) {
+                    const T* src = (h < p.heads_q ? qr : kr) + h * p.head_dim;
+                    va[i].load(src + x.a);
+                    vb[i].load(src + x.b);
+                }
             }
-        }
-        if (!angled) {
-            if (NORM) load_weights(p, sm);
-            angles(p, sm, r0, rows);
-            __syncthreads();
-            angled = true;
+            if (!angled) {
+                __syncthreads();  // the last tile's angles have been read
+                angles(p, sm, r0, rows);
+                __syncthreads();
+                angled = true;
+            }
+            Pairs cs, sn;
             if (live && x.angle >= 0) {
                 cs.from(sm.cs + row * (p.rot_dim / 2) + x.angle);
                 sn.from(sm.sn + row * (p.rot_dim / 2) + x.angle);
             }
-        }
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int h = h0 + (turn * kAhead + i) * per_row;
-            if ((turn * kAhead + i) * per_row >= p.heads) break;  // the same for all lanes
-            const bool mine = have && h < p.heads;
-            T* dst = (h < p.heads_q ? qo : ko) + h * p.head_dim;
-            if (!warp_live) {
-                if (mine) store_zeros(dst, x);
-                continue;
-            }
-            Pairs a, b;
-            if (live && mine) {
-                a.from(va[i]);
-                b.from(vb[i]);
-            } else {
-                a.zero();
-                b.zero();
-            }
-            if (NORM) {
-                const float sq = group_sum<LANES_LOG2>(dot16(a, b, a, b));
-                const float rstd = rsqrtf(sq * p.inv_dim + p.eps);
-                if (live && mine) {
-                    const float* w = sm.weight[h < p.heads_q ? 0 : 1];
-                    Pairs wa, wb;
-                    wa.from(w + x.a);
-                    wb.from(w + x.b);
-                    a.times(wa);
-                    b.times(wb);
-                    a.times(rstd);
-                    b.times(rstd);
+            for (int i = 0; i < kAhead; ++i) {
+                const int h = h0 + (turn * kAhead + i) * per_row;
+                if ((turn * kAhead + i) * per_row >= p.heads) break;  // the same for all lanes
+                const bool mine = have && h < p.heads;
+                T* dst = (h < p.heads_q ? qo : ko) + h * p.head_dim;
+                if (!warp_live) {
+                    if (mine) store_zeros(dst, x);
+                    continue;
                 }
-            }
-            if (mine) {
-                if (live && x.angle >= 0) rotate<INTER>(a, b, cs, sn);
-                a.store(dst + x.a);
-                b.store(dst + x.b);
+                Pairs a, b;
+                if (live && mine) {
+                    a.from(va[i]);
+                    b.from(vb[i]);
+                } else {
+                    a.zero();
+                    b.zero();
+                }
+                if (NORM) {
+                    const float sq = group_sum<LANES_LOG2>(dot16(a, b, a, b));
+                    const float rstd = rsqrtf(sq * p.inv_dim + p.eps);
+                    if (live && mine) {
+                        const float* w = sm.weight[h < p.heads_q ? 0 : 1];
+                        Pairs wa, wb;
+                        wa.from(w + x.a);
+                        wb.from(w + x.b);
+                        a.times(wa);
+                        b.times(wb);
+                        a.times(rstd);
+                        b.times(rstd);
+                    }
+                }
+                if (mine) {
+                    if (live && x.angle >= 0) rotate<INTER>(a, b, cs, sn);
+                    a.store(dst + x.a);
+                    b.store(dst + x.b);
+                }
             }
         }
     }
@@ -544,10 +547,11 @@ extern "C" rapid_status_t rapid_qk_norm_rope_fwd(const rapid_qk_desc_t* desc, co
     if ((s = check_device(&sms)) != RAPID_OK) return s;
     QkArgs p = make_args(d, q_weight, k_weight, inv_freq, positions, mask);
     p.per_row = groups_per_row(p, p.heads, kAhead, 2 * sms);
-    const int64_t rows = tile_rows(p, p.per_row), grid = (p.n_rows + rows - 1) / rows;
+    const int64_t rows = tile_rows(p, p.per_row), tiles = (p.n_rows + rows - 1) / rows;
+    const unsigned grid = (unsigned)(tiles < 2 * sms ? tiles : 2 * sms);  // two blocks are resident on an SM
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (d.dtype == RAPID_BF16) run_fwd<uint16_t>(p, (unsigned)grid, q, k, q_out, k_out, st);
-    else run_fwd<float>(p, (unsigned)grid, q, k, q_out, k_out, st);
+    if (d.dtype == RAPID_BF16) run_fwd<uint16_t>(p, grid, q, k, q_out, k_out, st);
+    else run_fwd<float>(p, grid, q, k, q_out, k_out, st);
     return cudaGetLastError() == cudaSuccess ? RAPID_OK : RAPID_ERR_CUDA;
 }
 
