@@ -629,7 +629,7 @@ extern "C" rapid_status_t rapid_embedding_fwd(const rapid_embed_desc_t* desc, co
     if (!aligned(table, 16) || !aligned(out, 16) || !aligned(tokens, 4)) return RAPID_ERR_ALIGNMENT;
     const rapid_embed_desc_t& d = *desc;
     const size_t es = elem_size(d.dtype);
-    if (overlap(table, (size_t)d.vocab * d.ld_table * es, out, (size_t)d.n_rows * d.ld_rows * es)) return RAPID_ERR_INVALID_ARG;
+    if (overlap(table, extent(d.vocab, d.dim, d.ld_table, es), out, extent(d.n_rows, d.dim, d.ld_rows, es))) return RAPID_ERR_INVALID_ARG;
     const int segs = (d.dim + kFwdSeg - 1) / kFwdSeg;
     unsigned grid = 0;
     if (!blocks_of_8(d.n_rows * segs, &grid)) return RAPID_ERR_UNSUPPORTED;
@@ -663,7 +663,7 @@ extern "C" rapid_status_t rapid_embedding_bwd(const rapid_embed_desc_t* desc, co
     if (!aligned(dout, 16) || !aligned(dtable, 16) || !aligned(tokens, 4)) return RAPID_ERR_ALIGNMENT;
     const rapid_embed_desc_t& d = *desc;
     const bool grad_bf16 = (d.flags & RAPID_EMBED_DTABLE_BF16) != 0;
-    if (overlap(dout, (size_t)d.n_rows * d.ld_rows * elem_size(d.dtype), dtable, (size_t)d.vocab * d.ld_table * (grad_bf16 ? 2 : 4)))
+    if (overlap(dout, extent(d.n_rows, d.dim, d.ld_rows, elem_size(d.dtype)), dtable, extent(d.vocab, d.dim, d.ld_table, grad_bf16 ? 2 : 4)))
         return RAPID_ERR_INVALID_ARG;
     if (!workspace || !aligned(workspace, 256)) return RAPID_ERR_WORKSPACE;
     EmbedScratch w;

@@ -21,10 +21,13 @@ inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
     return x < y + nb && y < x + na;
 }
 
+// Bytes from the first element of `n` rows of `width` elements at pitch `ld` to the end of the last.
+inline size_t extent(int64_t n, int64_t width, int64_t ld, size_t es) { return ((size_t)(n - 1) * ld + width) * es; }
+
 // Rows of `width` elements at pitch `ld`: do the two matrices share an element?  Matrices of one pitch may lie side by
 // side in the same rows (queries, keys and values of one projection); of two pitches, they have to be apart altogether.
 inline bool rows_overlap(const void* a, int64_t wa, int64_t lda, const void* b, int64_t wb, int64_t ldb, int64_t n, size_t es) {
-    if (!overlap(a, ((size_t)(n - 1) * lda + wa) * es, b, ((size_t)(n - 1) * ldb + wb) * es)) return false;
+    if (!overlap(a, extent(n, wa, lda, es), b, extent(n, wb, ldb, es))) return false;
     if (lda != ldb) return true;
     const int64_t pitch = lda * (int64_t)es;
     int64_t off = ((int64_t)reinterpret_cast<uintptr_t>(b) - (int64_t)reinterpret_cast<uintptr_t>(a)) % pitch;

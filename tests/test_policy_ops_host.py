@@ -212,3 +212,16 @@ def test_wrappers_check_shapes_and_types_before_the_call():
         rb.attention(b, b, b, 2, 2, torch.zeros(2, 2))
     with pytest.raises(ValueError):
         rb.attention_grad(b, b, b, b, torch.zeros(3), b, 2, 2)
+
+
+@no_gpu
+def test_embedding_matrices_may_end_where_the_next_begins():
+    """The last row of a slice ends with its columns, not with its pitch."""
+    d = rb.make_embed_desc(2, 2, 16, BF, 64, 64)
+    end = FAKE + (64 + 16) * 2
+    assert _embed_fwd(d, table=FAKE, out=end) == rb.RAPID_ERR_CUDA
+    assert _embed_fwd(d, table=FAKE, out=end - 16) == INVALID
+    d = rb.make_embed_desc(2, 2, 16, BF, 64, 64, flags=rb.EMBED_DTABLE_BF16)
+    assert _embed_bwd(d, dout=end, dtable=FAKE) == rb.RAPID_ERR_CUDA
+    assert _embed_bwd(d, dout=FAKE, dtable=end) == rb.RAPID_ERR_CUDA
+    assert _embed_bwd(d, dout=FAKE, dtable=end - 16) == INVALID
