@@ -253,3 +253,42 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for a, b in zip(want, got):
         assert torch.equal(a.dq, b.dq) and torch.equal(a.dk, b.dk) and torch.equal(a.dv, b.dv)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_most_generations_empty(hd):
+    """Long runs of tiles without a live row, between tiles that have some: every block works through many of both."""
+    n, length, heads, kv, window = 300, 300, 2, 1, 70
+    g = torch.Generator().manual_seed(4)
+    qkv = torch.randn(n * length, heads + 2 * kv, hd, generator=g).to(BF)
+    lo = torch.randint(0, length, (n,), generator=g)
+    lens = torch.where(torch.rand(n, generator=g) < 0.1, torch.randint(1, length, (n,), generator=g), 0)
+    bounds = torch.stack([lo, (lo + lens).clamp_max(length)], 1).to(torch.int32)
+    t = torch.arange(length)
+    live = (t >= bounds[:, :1]) & (t < bounds[:, 1:])
+    split = lambda m: (m[:, :heads], m[:, heads:heads + kv], m[:, heads + kv:])  # noqa: E731
+    (q, k, v), dev = split(qkv), split(qkv.cuda())
+    stats = rb.alloc_stats()
+    out, lse = rb.attention(*dev, n, length, bounds.cuda(), window, stats=stats)
+    assert rb.read_stats(stats)["status"] == 0
+    dout = torch.randn(n * length, heads, hd, generator=g).to(BF)
+    r = rb.attention_grad(*dev, out, lse, dout.cuda(), n, length, bounds.cuda(), window, stats=stats)
+    assert rb.read_stats(stats)["status"] == 0
+    want = _reference_grads(q, k, v, out.cpu(), lse.cpu(), dout, n, length, window, live, hd ** -0.5)
+    dead = ~live.reshape(-1)
+    assert (out.cpu()[dead] == 0).all()
+    for name, got, (ref, tol) in zip(("dq", "dk", "dv"), (r.dq, r.dk, r.dv), want):
+        got = got.cpu().double()
+        assert (got[dead] == 0).all(), name
+        assert ((got - ref).abs() <= tol).all(), name
+
+
+@pytest.mark.parametrize("window", [0, 2 ** 31 - 1])
+def test_window_beyond_the_generation(window):
+    q, k, v = _make(2, 300, 2, 1, 64, "full", 6)[1]
+    want, lse = rb.attention(q, k, v, 2, 300, None, 300)
+    out, l = rb.attention(q, k, v, 2, 300, None, window)
+    assert torch.equal(out, want) and torch.equal(l, lse)
+    dout = torch.randn_like(out)
+    a, b = (rb.attention_grad(q, k, v, out, lse, dout, 2, 300, None, w) for w in (300, window))
+    assert torch.equal(a.dq, b.dq) and torch.equal(a.dk, b.dk) and torch.equal(a.dv, b.dv)
