@@ -10,11 +10,11 @@
 // 4e-3), then sine and cosine in float.
 //
 // What has to be saved here is instructions: rows and pointers are worked out once for each group, the arithmetic is on packed
-// pairs of floats, and lanes without a head run along instead of branching.  64 x 1024 rows of 16 heads of 128, bf16, part of
-// them masked: forward 145 us with a division for each head and one float operation at a time, 114 packed, 99 with
+// pairs of floats, and lanes without a head run along instead of branching.  64 x 1024 rows of 12 + 2 heads of 128, bf16, a
+// third of them masked: forward 145 us with a division for each head and one float operation at a time, 114 packed, 99 with
 // the grid walking its tiles, 95 without block barriers, 82 with eight heads in flight and no branches (4.7 TB/s); the
 // gradient 273, 154, 149 and, with queries and keys in blocks of their own, half the weight sums a lane and all groups
-// busy on the keys' few heads, 124 (4.3 TB/s).  Three blocks an SM spill registers: 112 and 200 us.
+// busy on the keys' few heads, 120 (4.4 TB/s).  Three blocks an SM spill registers: 112 and 200 us.
 #include <math.h>
 
 #include "policy_ops.cuh"
@@ -644,13 +644,13 @@ extern "C" rapid_status_t rapid_qk_norm_rope_bwd(const rapid_qk_desc_t* desc, co
     QkArgs p = make_args(d, q_weight, k_weight, inv_freq, positions, mask);
     const int most = 2 * sms < kMaxBwdBlocks ? 2 * sms : kMaxBwdBlocks;  // two blocks are resident on an SM
     QkBwdKinds both = {{{q, dq_out, dq, d.ld_q, d.ld_q_out, d.ld_dq, d.n_q_heads, 1, 0, 0}, {k, dk_out, dk, d.ld_k, d.ld_k_out, d.ld_dk, d.n_k_heads, 1, 0, 0}}};
-    // Blocks in proportion to the heads, a row's angles counted as one head more.
-    int share = (int)((int64_t)most * (d.n_k_heads + 1) / (p.heads + 2));
+    // Blocks in proportion to the heads, a row's angles counted as two heads more (one: 124 us, three: 127, two: 120, 64 x 1024).
+    int share = (int)((int64_t)most * (d.n_k_heads + 2) / (p.heads + 4));
     share = share < 1 ? 1 : share;
     for (int i = 0; i < 2; ++i) {
         QkBwdKind& m = both.kind[i];
         const int64_t room = i ? share : most - share;
-        m.per_row = groups_per_row(p, m.heads, 4, room);
+        m.per_row = groups_per_row(p, m.heads, 6, room);
         const int64_t rows = tile_rows(p, m.per_row), tiles = (p.n_rows + rows - 1) / rows;
         m.blocks = (int)(tiles < room ? tiles : room);
     }
