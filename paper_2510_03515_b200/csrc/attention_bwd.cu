@@ -805,8 +805,18 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         uint32_t gi = 0, pieces = 0;
         Place<kKeys> kc;  // the key tile of this step
         uint32_t key_buf = 0;
+        // A piece and its row's terms; the next one is taken, and its terms are asked for, before this one's dQ is waited for.
         DqWork x;
-        for (uint32_t k = 0; work_take(&queue, k, x, lane, abortp); ++k) {
+        float shift = 0.f, ndelta = 0.f;
+        auto take = [&](uint32_t k) {
+            if (!work_take(&queue, k, x, lane, abortp)) return false;
+            const size_t at = (((size_t)x.n * g.heads + x.h) * a.tiles + x.t) * kTile + row;
+            shift = a.shift[at];
+            ndelta = a.ndelta[at];
+            return true;
+        };
+        bool more = take(0);
+        for (uint32_t k = 1; more; ++k) {
             const int pos = x.t * kTile + row;
             const bool live = pos >= x.lo && pos < x.hi;
             const int see = max(x.lo, pos - g.window + 1);
@@ -816,8 +826,6 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 full_from = (max(x.lo, x.t * kTile + kTile - g.window) + kTile - 1) / kTile;
                 full_to = x.t;
             }
-            const size_t at = (((size_t)x.n * g.heads + x.h) * a.tiles + x.t) * kTile + row;
-            const float shift = a.shift[at], ndelta = a.ndelta[at];
             const uint64_t shift2 = f32x2(shift, shift), ndelta2 = f32x2(ndelta, ndelta);
             for (int i = 0; i < x.steps; ++i, ++gi) {
                 const int j = x.from + i;
@@ -843,16 +851,19 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 tmem_st_wait();
                 tell(&ds_full);
             }
-            if (ok && x.steps > 0) wait(&acc_full, pieces & 1u);
+            const int n = x.n, h = x.h, t = x.t;
+            const bool any = x.steps > 0;
             if (!ok) break;
-            if (x.steps > 0) {  // 32 columns each (at D = 64 half of the warps have none)
+            more = take(k);
+            if (any && !wait(&acc_full, pieces & 1u)) break;
+            if (any) {  // 32 columns each (at D = 64 half of the warps have none)
                 if (part * 32 < D) stage_acc32(k_tile(key_buf), row, part, dq_t + lanes + 32u * part, live, a.scale);
                 fence_proxy_async_smem();
                 tell(&acc_empty);
                 tell(&staged[key_buf]);
                 ++pieces;
             } else {
-                zero_tile(a.dq, a.ld_dq, g.seq_len, g.head_dim, x.h, x.t * kTile, x.n, part * 128 + row, 512);
+                zero_tile(a.dq, a.ld_dq, g.seq_len, g.head_dim, h, t * kTile, n, part * 128 + row, 512);
             }
         }
     }
