@@ -153,7 +153,7 @@ typedef struct rapid_attn_desc {
  *            outputs are then unspecified)
  * Rows outside the bounds may hold anything (infinities and NaN too) and influence nothing.  Rows inside must be finite.
  * The products run on the tensor cores in bf16 with float accumulation; scores, maximum and sum of the softmax are float;
- * the probabilities are rounded to bf16 for their product with v (relative error 2^-9, as independent roundings).
+ * the probabilities are rounded to bf16 for their product with v (half a step, a relative error of at most 2^-8 each).
  */
 rapid_status_t rapid_attention_fwd(const rapid_attn_desc_t* desc, const void* q, const void* k, const void* v,
                                    const int32_t* bounds, void* out, float* lse, rapid_stats_t* stats, void* stream);

@@ -12,6 +12,12 @@
 //
 // The order of the products is such that the tensor cores have two of them to work on while the exponentials of one step are formed,
 // and one or two more during its dS.
+//
+// Measured, 64 x 1024 positions at most, 12 heads of 128 over 2: 62 us (6.2 TB/s, the copy rate), about 205 and 190 us back to
+// back, 545 to 610 in all with cold caches and under the power cap.  In a step of dK, dV of 2950 cycles the tensor cores work for
+// 2048: the exponentials (1450 cycles), the product that reads them and the next scores follow one another.  Handing P' over
+// in halves, or forming the next S' in halves, brought nothing (460 and 464 us against 465), nor did letting half of the row
+// warps of dQ take every other step (476), or running its steps on across pieces (its kernel 211 instead of 203).
 #include <math.h>
 
 #include "attention.cuh"

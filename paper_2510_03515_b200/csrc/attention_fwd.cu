@@ -9,6 +9,10 @@
 // of its own and the next S is formed as soon as the softmax has taken the last one into registers.  O is rescaled only
 // when a row's maximum has grown by more than 2^8 since the last time (exponentials up to 2^8 are as exact in float and
 // bf16 as those below 1), and the warp that finds this does it itself.
+//
+// Measured: 8 x 4096 positions at most, 16 heads of 64: 300 us (670 TFLOP/s; up to 350 under the power cap), where the
+// exponentials alone take about 180; 64 x 256, 12 heads of 128: 47 us, of which the key tiles' work is a third and the rest the
+// beginnings and ends of pieces of one to three tiles.
 #include <math.h>
 
 #include "attention.cuh"
@@ -35,7 +39,7 @@ template <int D>
 struct FwdCfg {
     static constexpr uint32_t kStages = D == 128 ? 4 : 8;  // tiles in flight, keys and values alternating
     static constexpr bool kOverlay = D == 128;        // P over S
-    // Of 16 pairs of exponentials, those formed by polynomial.  With 1, 2, 3, 4: 293, 305, 308, 308 us (8 x 4096, 16 heads of 64).
+    // Of 16 pairs of exponentials, those formed by polynomial.  With 0, 1, 2, 3, 4: 302, 298, 305, 308, 308 us (8 x 4096, 16 heads of 64).
     static constexpr int kPoly = 1;
     static constexpr size_t kSmem = (size_t)(2 + kStages) * tile_bytes<D>() + 2 * kBoxBytes + 1024;  // with a box of output for each item
 };

@@ -10,6 +10,11 @@
 // is then at most 31 rows + the pieces + 31 rows.  The last kernel writes dtable: most of its rows belong to tokens that do
 // not occur, and one warp of each block writes those as bulk copies of zeros out of shared memory, which needs no registers
 // and hardly an instruction, while the other warps sum.
+//
+// Measured: 64 x 1024 tokens x 1536 bf16, over a third of them masked: forward 43 us (5.7 TB/s).  Gradient into 151936 rows of float:
+// 434 us with a warp a token and segment, 299 with the radix sort's wide digits, 248 with frequent tokens summed by blocks
+// and the others a whole row at a time, 244 (4.3 TB/s) with the sort's loads issued ahead; its last kernel takes 195 of them
+// at 5.4 TB/s, the sort and the lists before it the rest.
 #include <math.h>
 
 #include "policy_ops.cuh"

@@ -10,8 +10,8 @@
 // 4e-3), then sine and cosine in float.
 //
 // What has to be saved here is instructions: rows and pointers are worked out once for each group, the arithmetic is on packed
-// pairs of floats, and lanes without a head run along instead of branching.  64 x 1024 rows of 12 + 2 heads of 128, bf16, a
-// third of them masked: forward 145 us with a division for each head and one float operation at a time, 114 packed, 99 with
+// pairs of floats, and lanes without a head run along instead of branching.  64 x 1024 rows of 12 + 2 heads of 128, bf16, over
+// a third of them masked: forward 145 us with a division for each head and one float operation at a time, 114 packed, 99 with
 // the grid walking its tiles, 95 without block barriers, 82 with eight heads in flight and no branches (4.7 TB/s); the
 // gradient 273, 154, 149 and, with queries and keys in blocks of their own, half the weight sums a lane and all groups
 // busy on the keys' few heads, 120 (4.4 TB/s).  Three blocks an SM spill registers: 112 and 200 us.
