@@ -428,18 +428,23 @@ def _pitch(t: torch.Tensor, name: str) -> int:
     return stride[0]
 
 
-def _matrix(rows: int, cols: int, dtype, device) -> torch.Tensor:
-    """An uninitialised [rows, cols] whose rows begin on 16-byte boundaries."""
+def _matrix(rows: int, cols: int, dtype, like: torch.Tensor) -> torch.Tensor:
+    """An uninitialised [rows, cols] on like's device whose rows begin on 16-byte boundaries."""
     step = 16 // dtype.itemsize
     pitch = -(-cols // step) * step
-    buf = torch.empty((rows, pitch), dtype=dtype, device=device)
+    buf = like.new_empty((rows, pitch), dtype=dtype)
     return buf if pitch == cols else buf[:, :cols]
+
+
+def _new(x: torch.Tensor) -> torch.Tensor:
+    """A contiguous tensor of x's shape and type (half the time of torch.empty with a shape, a type and a device)."""
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
 
 
 def _like(out: Optional[torch.Tensor], x: torch.Tensor, name: str) -> torch.Tensor:
     """`out`, or a contiguous tensor of x's shape and type where there is none."""
     if out is None:
-        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        return _new(x)
     if out.shape != x.shape:
         raise ValueError(f"{name}: shape {tuple(x.shape)} expected")
     if out.dtype != x.dtype:
@@ -537,7 +542,7 @@ def embedding(table: torch.Tensor, tokens: torch.Tensor, mask: Optional[torch.Te
     _vector(tokens, T, torch.int32, "tokens")
     dev = _one_device(table, tokens, mask, stats)
     with _on(dev):
-        out = _matrix(T, D, table.dtype, table.device)
+        out = _matrix(T, D, table.dtype, table)
         if T:
             desc, _ = _embed_plan(T, V, D, table.dtype, _pitch(table, "table"), _pitch(out, "out"), scale, 0, False)
             rapid_embedding_fwd(desc, tokens, mask, table, out, stats)
@@ -568,9 +573,9 @@ def embedding_grad(dout: torch.Tensor, tokens: torch.Tensor, mask: Optional[torc
     with _on(dev):
         if T == 0:
             return torch.zeros(vocab, D, dtype=dtable_dtype, device=dout.device) if dtable is None else dtable
-        out = _matrix(vocab, D, dtable_dtype, dout.device) if dtable is None else dtable
+        out = _matrix(vocab, D, dtable_dtype, dout) if dtable is None else dtable
         desc, ws_bytes = _embed_plan(T, vocab, D, dout.dtype, _pitch(out, "dtable"), _pitch(dout, "dout"), scale, flags, True)
-        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dout.device)
+        ws = dout.new_empty(ws_bytes, dtype=torch.uint8)
         rapid_embedding_bwd(desc, tokens, mask, dout, out, ws)
     return out
 
@@ -634,7 +639,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Tens
     q_weight, k_weight, mask = _qk_args(q, k, q_weight, k_weight, inv_freq, n_seq, seq_len, positions, mask, flags)
     dev = _one_device(q, k, q_weight, k_weight, inv_freq, positions, mask)
     with _on(dev):
-        q_out, k_out = torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        q_out, k_out = _new(q), _new(k)
         if q.shape[0]:
             desc, _ = _qk_plan(n_seq, seq_len, q.shape[1], k.shape[1], q.shape[2], q.dtype, 2 * inv_freq.numel(),
                                (_pitch(q, "q"), _pitch(k, "k")), eps, flags, False)
@@ -646,7 +651,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Tens
 class QkGrads:
     dq: torch.Tensor                    # [T, Hq, D]
     dk: torch.Tensor                    # [T, Hk, D]
-    dq_weight: Optional[torch.Tensor]   # [D] float32; None with QK_NO_NORM
+    dq_weight: Optional[torch.Tensor]   # like q_weight; None with QK_NO_NORM
     dk_weight: Optional[torch.Tensor]
 
 
@@ -666,7 +671,7 @@ def qk_norm_rope_grad(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch
         T, hq, hd = q.shape
         hk = k.shape[1]
         dq, dk = _like(dq, q, "dq"), _like(dk, k, "dk")
-        dw = (None, None) if flags & QK_NO_NORM else torch.empty((2, hd), dtype=torch.float32, device=q.device).unbind(0)
+        dw = (None, None) if flags & QK_NO_NORM else (_new(q_weight), _new(k_weight))
         if T == 0:
             for x in dw:
                 if x is not None:
@@ -674,7 +679,7 @@ def qk_norm_rope_grad(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch
             return QkGrads(dq, dk, *dw)
         pitches = (_pitch(q, "q"), _pitch(k, "k"), _pitch(dq_out, "dq_out"), _pitch(dk_out, "dk_out"), _pitch(dq, "dq"), _pitch(dk, "dk"))
         desc, ws_bytes = _qk_plan(n_seq, seq_len, hq, hk, hd, q.dtype, 2 * inv_freq.numel(), pitches, eps, flags, True)
-        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device) if ws_bytes else None
+        ws = q.new_empty(ws_bytes, dtype=torch.uint8) if ws_bytes else None
         rapid_qk_norm_rope_bwd(desc, q, k, q_weight, k_weight, inv_freq, positions, mask, dq_out, dk_out, dq, dk, dw[0], dw[1], ws)
     return QkGrads(dq, dk, *dw)
 
@@ -726,8 +731,8 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_seq: int, seq
     _attn_args(q, k, v, n_seq, seq_len, bounds)
     dev = _one_device(q, k, v, bounds, stats)
     with _on(dev):
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty((n_seq, q.shape[1], seq_len), dtype=torch.float32, device=q.device)
+        out = _new(q)
+        lse = q.new_empty((n_seq, q.shape[1], seq_len), dtype=torch.float32)
         if q.shape[0]:
             desc, _ = _attn_plan(n_seq, seq_len, q.shape[1], k.shape[1], q.shape[2], window, scale,
                                  (_pitch(q, "q"), _pitch(k, "k"), _pitch(v, "v")), False)
@@ -763,7 +768,7 @@ def attention_grad(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch
             pitches = (_pitch(q, "q"), _pitch(k, "k"), _pitch(v, "v"), _pitch(out, "out"), _pitch(dout, "dout"), _pitch(dq, "dq"),
                        _pitch(dk, "dk"), _pitch(dv, "dv"))
             desc, ws_bytes = _attn_plan(n_seq, seq_len, q.shape[1], k.shape[1], q.shape[2], window, scale, pitches, True)
-            ws = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+            ws = q.new_empty(ws_bytes, dtype=torch.uint8)
             rapid_attention_bwd(desc, q, k, v, bounds, out, lse, dout, dq, dk, dv, stats, ws)
         elif stats is not None:
             stats.zero_()

@@ -14,7 +14,7 @@
 // and one or two more during its dS.
 //
 // Measured, 64 x 1024 positions at most, 12 heads of 128 over 2: 62 us (6.2 TB/s, the copy rate), about 205 and 190 us back to
-// back, 545 to 610 in all with cold caches and under the power cap.  In a step of dK, dV of 2950 cycles the tensor cores work for
+// back, 465 in all; 545 to 610 when run for long, at 1.6 instead of 1.97 GHz under the 1000 W cap.  In a step of dK, dV of 2950 cycles the tensor cores work for
 // 2048: the exponentials (1450 cycles), the product that reads them and the next scores follow one another.  Handing P' over
 // in halves, or forming the next S' in halves, brought nothing (460 and 464 us against 465), nor did letting half of the row
 // warps of dQ take every other step (476), or running its steps on across pieces (its kernel 211 instead of 203).
