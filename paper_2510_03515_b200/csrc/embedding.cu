@@ -13,8 +13,9 @@
 //
 // Measured: 64 x 1024 tokens x 1536 bf16, over a third of them masked: forward 43 us (5.7 TB/s).  Gradient into 151936 rows of float:
 // 434 us with a warp a token and segment, 299 with the radix sort's wide digits, 248 with frequent tokens summed by blocks
-// and the others a whole row at a time, 244 (4.3 TB/s) with the sort's loads issued ahead; its last kernel takes 195 of them
-// at 5.4 TB/s, the sort and the lists before it the rest.
+// , and the others a whole row at a time, 244 (4.3 TB/s) with the sort's loads issued ahead; its last kernel takes 200 of them,
+// the sort and the lists before it the rest.  16384 rows of 512 into 32000: 92 us, 53 with the sort over several blocks and
+// narrow rows eight at a time.
 #include <math.h>
 
 #include "policy_ops.cuh"
@@ -83,7 +84,9 @@ constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;  // one thread
 constexpr int kMaxSortBlocks = 64;  // every block reads the histograms of all
 constexpr int kMinSortRows = 1024;
 constexpr int kSortAhead = 8;
-constexpr int64_t kOneBlockRows = 16384;
+// Up to here one block sorts alone, without histograms and launches in between (151936 tokens, one block against several:
+// 2000 rows 9.3 and 9.4 us, 4000 13.6 and 15.4, 6000 19.3 and 16.1, 16000 44 and 15).
+constexpr int64_t kOneBlockRows = 5120;
 
 // The rows of block b are [b * per_block, (b + 1) * per_block); within it warp w has a run of per_block / 16 of them.
 struct SortShape {
@@ -481,6 +484,28 @@ __device__ __forceinline__ void sum_frequent(const GradArgs& a, const Used& u, i
     asm volatile("bar.sync 1, %0;" ::"n"(kSumWarps * 32) : "memory");
 }
 
+// The other tokens, a warp for each and segment.  Rows that fit a narrow segment take it, for the rows in flight.
+template <class T, class G, bool WIDE>
+__device__ __forceinline__ void sum_seldom(const GradArgs& a, int64_t often, const T* __restrict__ dout, G* __restrict__ dtable, int warp,
+                                           int lane) {
+    constexpr int K = Seg<T, WIDE>::K;
+    const int segs = WIDE ? a.wide_segs : 1;
+    const int64_t units = (int64_t)a.used[0] * segs, stride = (int64_t)gridDim.x * kSumWarps;
+    // blocks with one frequent segment less begin first
+    const int64_t turn = (int64_t)((blockIdx.x + gridDim.x - (uint32_t)(often % gridDim.x)) % gridDim.x) * kSumWarps + warp;
+    Used next{};
+    if (turn < units) next = a.list[turn / segs];
+    for (int64_t unit = turn; unit < units; unit += stride) {
+        const Used u = next;
+        if (unit + stride < units) next = a.list[(unit + stride) / segs];
+        const int c0 = (int)(unit % segs) * (K * 256) + lane * 8;
+        float acc[K][8] = {};
+        add_rows<T, WIDE>(acc, a.rows, u.lo, u.hi, dout, a.ld, c0, a.dim, lane);
+#pragma unroll
+        for (int k = 0; k < K; ++k) put(a, dtable + (int64_t)u.token * a.ld_table, c0 + k * 256, acc[k]);
+    }
+}
+
 template <class T, class G>
 __global__ void __launch_bounds__(256, 2) embed_rows_kernel(GradArgs a, const T* __restrict__ dout, G* __restrict__ dtable) {
     __shared__ __align__(16) uint8_t zeros[kZeroBytes];
@@ -497,21 +522,8 @@ __global__ void __launch_bounds__(256, 2) embed_rows_kernel(GradArgs a, const T*
         const int64_t which = unit / a.segs;
         sum_frequent<T, G>(a, a.list[a.room - 1u - (uint32_t)which], (int)(unit - which * a.segs), dout, dtable, part, warp, lane);
     }
-    constexpr int K = Seg<T, true>::K;
-    const int64_t units = (int64_t)a.used[0] * a.wide_segs, stride = (int64_t)gridDim.x * kSumWarps;
-    // blocks with one frequent segment less begin first
-    const int64_t turn = (int64_t)((blockIdx.x + gridDim.x - (uint32_t)(often % gridDim.x)) % gridDim.x) * kSumWarps + warp;
-    Used next{};
-    if (turn < units) next = a.list[turn / a.wide_segs];
-    for (int64_t unit = turn; unit < units; unit += stride) {
-        const Used u = next;
-        if (unit + stride < units) next = a.list[(unit + stride) / a.wide_segs];
-        const int c0 = (int)(unit % a.wide_segs) * (K * 256) + lane * 8;
-        float acc[K][8] = {};
-        add_rows<T, true>(acc, a.rows, u.lo, u.hi, dout, a.ld, c0, a.dim, lane);
-#pragma unroll
-        for (int k = 0; k < K; ++k) put(a, dtable + (int64_t)u.token * a.ld_table, c0 + k * 256, acc[k]);
-    }
+    if (a.segs == 1) sum_seldom<T, G, false>(a, often, dout, dtable, warp, lane);
+    else sum_seldom<T, G, true>(a, often, dout, dtable, warp, lane);
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------
