@@ -71,7 +71,9 @@ attn_row_terms_kernel(Geometry g, int tiles, int lanes_log2, const uint16_t* __r
             t[k] = u / g.heads;
             h[k] = u - t[k] * g.heads;
             t[k] += t0;
-            live[k] = u < units && t[k] >= lo && t[k] < hi;
+            int from = lo, to = hi;
+            row_range(g, n, t[k], from, to);
+            live[k] = u < units && t[k] >= from && t[k] < to;
             if (live[k] && lane * 8 < g.head_dim) {
                 const int64_t r = (int64_t)n * g.seq_len + t[k];
                 x[k].load(out + r * ld_out + h[k] * g.head_dim + lane * 8);
@@ -92,7 +94,7 @@ attn_row_terms_kernel(Geometry g, int tiles, int lanes_log2, const uint16_t* __r
             if (lane == 0 && first + k * groups < units) {
                 const int64_t at = ((int64_t)n * g.heads + h[k]) * padded + t[k];
                 // double: lse * log2(e) in float would shift every score of the row by its own rounding
-                shift[at] = live[k] ? (float)((double)lse[((int64_t)n * g.heads + h[k]) * g.seq_len + t[k]] * -kLog2eD) : -INFINITY;
+                shift[at] = live[k] ? (float)((double)lse[lse_at(g, n, h[k], t[k])] * -kLog2eD) : -INFINITY;
                 ndelta[at] = -sum;
             }
         }
@@ -275,7 +277,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 }
                 int h = x.hk * g.group, qt = x.q_from;
                 for (int i = 0; i < x.steps; ++i) {
-                    const bool clean = dirty(qt, x.lo, x.hi);
+                    const bool clean = dirty(g, qt, x.lo, x.hi);
                     if (steps >= kQ && !(ok = wait_one(&m.q_empty[qa.s], qa.parity ^ 1u, abortp))) break;
                     uint64_t* bar = clean ? &m.q_raw[qa.s] : &m.q_full[qa.s];
                     q_was_raw = clean ? q_was_raw | (1u << qa.s) : q_was_raw & ~(1u << qa.s);
@@ -347,12 +349,12 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         for (uint32_t k = 0; ok && work_take(&m.queue, k, x, lane, abortp); ++k) {
             int qt = x.q_from;
             for (int i = 0; i < x.steps && ok; ++i) {
-                if (dirty(qt, x.lo, x.hi)) {
+                if (dirty(g, qt, x.lo, x.hi)) {
                     ok = wait_all(&m.q_raw[qa.s], q_raw.flip(qa.s), abortp);
-                    if (ok) zero_rows_outside<D>(q_tile(qa.s), qt * kTile, x.lo, x.hi, lane);
+                    if (ok) zero_dead_rows<D>(g, q_tile(qa.s), x.n, qt * kTile, x.lo, x.hi, lane);
                     if (ok && lane == 0) mbar_arrive(&m.q_full[qa.s]);
                     ok = ok && wait_all(&m.do_raw[da.s], do_raw.flip(da.s), abortp);
-                    if (ok) zero_rows_outside<D>(do_tile(da.s), qt * kTile, x.lo, x.hi, lane);
+                    if (ok) zero_dead_rows<D>(g, do_tile(da.s), x.n, qt * kTile, x.lo, x.hi, lane);
                     if (ok && lane == 0) mbar_arrive(&m.do_full[da.s]);
                 }
                 qa.step();
@@ -455,6 +457,9 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         DkvWork x;
         for (uint32_t k = 0; work_take(&m.queue, k, x, lane, abortp); ++k) {
             const int key = x.kt * kTile + row;
+            int lo = x.lo, hi = x.hi;
+            row_range(g, x.n, key, lo, hi);
+            const unsigned seen_by = g.part == 0 ? (unsigned)g.window : (unsigned)max(0, min(g.window, hi - key));  // queries from `key` on
             int qt = x.q_from;
             for (int i = 0; i < x.steps; ++i, ++gi) {
                 const int q0 = qt * kTile;
@@ -472,7 +477,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                     const int first = q0 + part * 32 - key;
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
-                        if ((unsigned)(first + e) >= (unsigned)g.window) p[e] = 0.f;
+                        if ((unsigned)(first + e) >= seen_by) p[e] = 0.f;
                 }
                 round_pairs(p, b);
                 if (!kOverlay && gi > 0 && !wait(&m.p_empty, (gi - 1u) & 1u)) break;
@@ -498,7 +503,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             if (!ok) break;
             const bool keys = part >= 2;
             if (x.steps > 0) {
-                const bool live = key >= x.lo && key < x.hi;
+                const bool live = key >= lo && key < hi;
 #pragma unroll 1
                 for (int c = (part & 1) * (D / 64); c < ((part & 1) + 1) * (D / 64); ++c)
                     stage_acc32(keys ? k_tile : v_tile, row, c, (keys ? dk_t : dv_t) + lanes + 32u * c, live, keys ? a.scale : 1.f);
@@ -659,7 +664,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 const int hk = x.h / g.group;
                 for (int i = 0; i < x.steps; ++i) {
                     const int t0 = (x.from + i) * kTile;
-                    const bool clean = dirty(x.from + i, x.lo, x.hi);
+                    const bool clean = dirty(g, x.from + i, x.lo, x.hi);
                     if (nk >= kKeys && !(ok = wait_one(&k_empty[ka.s], ka.parity ^ 1u, abortp))) break;
                     flush(ka.s);
                     if (!ok) break;
@@ -719,12 +724,12 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         for (uint32_t k = 0; ok && work_take(&queue, k, x, lane, abortp); ++k) {
             for (int i = 0; i < x.steps && ok; ++i) {
                 const int t0 = (x.from + i) * kTile;
-                if (dirty(x.from + i, x.lo, x.hi)) {
+                if (dirty(g, x.from + i, x.lo, x.hi)) {
                     ok = wait_all(&k_raw[ka.s], kr.flip(ka.s), abortp);
-                    if (ok) zero_rows_outside<D>(k_tile(ka.s), t0, x.lo, x.hi, lane);
+                    if (ok) zero_dead_rows<D>(g, k_tile(ka.s), x.n, t0, x.lo, x.hi, lane);
                     if (ok && lane == 0) mbar_arrive(&k_full[ka.s]);
                     ok = ok && wait_all(&v_raw[va.s], vr.flip(va.s), abortp);
-                    if (ok) zero_rows_outside<D>(v_tile(va.s), t0, x.lo, x.hi, lane);
+                    if (ok) zero_dead_rows<D>(g, v_tile(va.s), x.n, t0, x.lo, x.hi, lane);
                     if (ok && lane == 0) mbar_arrive(&v_full[va.s]);
                 }
                 ka.step();
@@ -824,11 +829,13 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         bool more = take(0);
         for (uint32_t k = 1; more; ++k) {
             const int pos = x.t * kTile + row;
-            const bool live = pos >= x.lo && pos < x.hi;
-            const int see = max(x.lo, pos - g.window + 1);
+            int lo = x.lo, hi = x.hi;
+            row_range(g, x.n, pos, lo, hi);
+            const bool live = pos >= lo && pos < hi;
+            const int see = max(lo, pos - g.window + 1);
             const unsigned count = live ? (unsigned)(pos + 1 - see) : 0u;
             int full_from = 1 << 30, full_to = 0;  // key tiles that every row of the tile sees whole
-            if (x.t * kTile >= x.lo && x.t * kTile + kTile <= x.hi) {
+            if (g.part == 0 && x.t * kTile >= x.lo && x.t * kTile + kTile <= x.hi) {
                 full_from = (max(x.lo, x.t * kTile + kTile - g.window) + kTile - 1) / kTile;
                 full_to = x.t;
             }
@@ -960,36 +967,47 @@ extern "C" rapid_status_t rapid_attention_bwd(const rapid_attn_desc_t* desc, con
     if (!workspace || !policy::aligned(workspace, 256) || workspace_bytes < terms * 2 * sizeof(float)) return RAPID_ERR_WORKSPACE;
     int sms = 0;
     if ((s = policy::check_device(&sms)) != RAPID_OK) return s;
-    Maps m;
-    if (!make_head_map(&m.q, q, d, d.n_heads, d.ld_q) || !make_head_map(&m.k, k, d, d.n_kv_heads, d.ld_k) ||
-        !make_head_map(&m.v, v, d, d.n_kv_heads, d.ld_v) || !make_head_map(&m.dout, dout, d, d.n_heads, d.ld_dout) ||
-        !make_head_map(&m.dq, dq, d, d.n_heads, d.ld_dq) || !make_head_map(&m.dk, dk, d, d.n_kv_heads, d.ld_dk) ||
-        !make_head_map(&m.dv, dv, d, d.n_kv_heads, d.ld_dv))
-        return RAPID_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (policy::clear_stats(stats, st) != cudaSuccess) return RAPID_ERR_CUDA;
-    float* shift = static_cast<float*>(workspace);
-    float* ndelta = shift + terms;
-    BwdArgs a;
-    a.g = make_geometry(d, bounds);
-    a.scale = (float)d.scale;
-    a.scale_log2 = (float)(d.scale * kLog2eD);
-    a.tiles = (d.seq_len + kTile - 1) / kTile;
-    a.shift = shift;
-    a.ndelta = ndelta;
-    a.dq = static_cast<uint16_t*>(dq);
-    a.dk = static_cast<uint16_t*>(dk);
-    a.dv = static_cast<uint16_t*>(dv);
-    a.ld_dq = d.ld_dq;
-    a.ld_dk = d.ld_dk;
-    a.ld_dv = d.ld_dv;
-    a.stats = stats;
     int lanes_log2 = 0;
     while ((8 << lanes_log2) < d.head_dim) ++lanes_log2;
-    const int64_t blocks = (int64_t)d.n_seq * a.tiles * (kTile / kTermRows);
-    if (blocks > 0x7fffffffll) return RAPID_ERR_UNSUPPORTED;
-    attn_row_terms_kernel<<<(unsigned)blocks, 256, 0, st>>>(a.g, a.tiles, lanes_log2, static_cast<const uint16_t*>(out), d.ld_out,
-                                                            static_cast<const uint16_t*>(dout), d.ld_dout, lse, shift, ndelta);
-    const cudaError_t e = d.head_dim <= 64 ? launch_bwd<64>(m, a, st) : launch_bwd<128>(m, a, st);
+    Share shares[2];
+    const int count = make_shares(d, bounds, shares);
+    cudaError_t e = cudaSuccess;
+    for (int i = 0; i < count && e == cudaSuccess; ++i) {
+        const Share& c = shares[i];
+        const void *o_rows = rows_from(out, c.first_row, d.ld_out), *do_rows = rows_from(dout, c.first_row, d.ld_dout);
+        void *dq_rows = rows_from(dq, c.first_row, d.ld_dq), *dk_rows = rows_from(dk, c.first_row, d.ld_dk),
+             *dv_rows = rows_from(dv, c.first_row, d.ld_dv);
+        Maps m;
+        if (!make_head_map(&m.q, rows_from(q, c.first_row, d.ld_q), c.d, d.n_heads, d.ld_q) ||
+            !make_head_map(&m.k, rows_from(k, c.first_row, d.ld_k), c.d, d.n_kv_heads, d.ld_k) ||
+            !make_head_map(&m.v, rows_from(v, c.first_row, d.ld_v), c.d, d.n_kv_heads, d.ld_v) ||
+            !make_head_map(&m.dout, do_rows, c.d, d.n_heads, d.ld_dout) || !make_head_map(&m.dq, dq_rows, c.d, d.n_heads, d.ld_dq) ||
+            !make_head_map(&m.dk, dk_rows, c.d, d.n_kv_heads, d.ld_dk) || !make_head_map(&m.dv, dv_rows, c.d, d.n_kv_heads, d.ld_dv))
+            return RAPID_ERR_CUDA;
+        BwdArgs a;
+        a.g = c.g;
+        a.scale = (float)d.scale;
+        a.scale_log2 = (float)(d.scale * kLog2eD);
+        a.tiles = (c.d.seq_len + kTile - 1) / kTile;
+        // the second share's row terms take the place of the first's, which its kernels have read by then
+        a.shift = static_cast<float*>(workspace);
+        float* ndelta = static_cast<float*>(workspace) + terms;
+        a.ndelta = ndelta;
+        a.dq = static_cast<uint16_t*>(dq_rows);
+        a.dk = static_cast<uint16_t*>(dk_rows);
+        a.dv = static_cast<uint16_t*>(dv_rows);
+        a.ld_dq = d.ld_dq;
+        a.ld_dk = d.ld_dk;
+        a.ld_dv = d.ld_dv;
+        a.stats = stats;
+        const int64_t blocks = (int64_t)c.d.n_seq * a.tiles * (kTile / kTermRows);
+        if (blocks > 0x7fffffffll) return RAPID_ERR_UNSUPPORTED;
+        attn_row_terms_kernel<<<(unsigned)blocks, 256, 0, st>>>(a.g, a.tiles, lanes_log2, static_cast<const uint16_t*>(o_rows), d.ld_out,
+                                                                static_cast<const uint16_t*>(do_rows), d.ld_dout,
+                                                                lse + c.first_row * d.n_heads, static_cast<float*>(workspace), ndelta);
+        e = d.head_dim <= 64 ? launch_bwd<64>(m, a, st) : launch_bwd<128>(m, a, st);
+    }
     return e == cudaSuccess ? RAPID_OK : RAPID_ERR_CUDA;
 }

@@ -165,7 +165,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                     for (int half = 0; half < 2; ++half) {
                         if (it >= kStages && !(ok = wait_one(&kv_empty[at.s], at.parity ^ 1u, abortp))) break;
                         // dead keys are masked in the scores; dead values have to be zero
-                        const bool clean = half && dirty(j, x.lo, x.hi);
+                        const bool clean = half && dirty(g, j, x.lo, x.hi);
                         uint64_t* bar = clean ? &kv_raw[at.s] : &kv_full[at.s];
                         was_raw = clean ? was_raw | (1u << at.s) : was_raw & ~(1u << at.s);
                         if (clean) raw.flip(at.s);
@@ -199,9 +199,9 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         for (uint32_t k = 0; ok && work_take(&queue, k, x, lane, abortp); ++k)
             for (int j = x.jlo; j < x.jhi && ok; ++j) {
                 at.step();  // past the keys
-                if (dirty(j, x.lo, x.hi)) {
+                if (dirty(g, j, x.lo, x.hi)) {
                     ok = wait_all(&kv_raw[at.s], raw.flip(at.s), abortp);
-                    if (ok) zero_rows_outside<D>(kv_tile(at.s), j * kTile, x.lo, x.hi, lane);
+                    if (ok) zero_dead_rows<D>(g, kv_tile(at.s), x.n, j * kTile, x.lo, x.hi, lane);
                     if (ok && lane == 0) mbar_arrive(&kv_full[at.s]);
                 }
                 at.step();
@@ -337,13 +337,15 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         for (uint32_t k = 0; ok && work_take(&queue, k, x, lane, abortp); ++k) {
             const int tw = w ? x.t[1] : x.t[0], hw = w ? x.h[1] : x.h[0], fw = w ? x.from[1] : x.from[0], ew = w ? x.to[1] : x.to[0];
             const int pos = tw * kTile + row;
-            const bool live = pos >= x.lo && pos < x.hi && ew > fw;
+            int lo = x.lo, hi = x.hi;
+            row_range(g, x.n, pos, lo, hi);
+            const bool live = pos >= lo && pos < hi && ew > fw;
             // keys [see, see + count) are visible to this row
-            const int see = max(x.lo, pos - g.window + 1);
+            const int see = max(lo, pos - g.window + 1);
             const unsigned count = live ? (unsigned)(pos + 1 - see) : 0u;
             // key tiles in [full_from, full_to) are visible to every row of this tile; the others are masked
             int full_from = 1 << 30, full_to = 0;
-            if (tw * kTile >= x.lo && tw * kTile + kTile <= x.hi) {
+            if (g.part == 0 && tw * kTile >= x.lo && tw * kTile + kTile <= x.hi) {
                 full_from = (max(x.lo, tw * kTile + kTile - g.window) + kTile - 1) / kTile;
                 full_to = tw;
             }
@@ -459,7 +461,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 zero_tile(a.out, a.ld_out, g.seq_len, g.head_dim, hw, tw * kTile, x.n, row, 128);
             }
             if (a.lse && pos < g.seq_len)
-                a.lse[((size_t)x.n * g.heads + hw) * g.seq_len + pos] =
+                a.lse[lse_at(g, x.n, hw, pos)] =
                     live ? (float)(((double)mref * (double)c + (double)log2f(sum)) * kLn2D) : -INFINITY;
         }
         if ((warp & 3) == 0 && lane == 0) bulk_wait_all<0>();
@@ -514,8 +516,32 @@ Geometry make_geometry(const rapid_attn_desc_t& d, const int32_t* bounds) {
     g.group = d.n_heads / d.n_kv_heads;
     g.head_dim = d.head_dim;
     g.window = d.window == 0 || d.window > d.seq_len ? d.seq_len : d.window;
+    g.part = g.parts = 0;
     g.bounds = bounds;
     return g;
+}
+
+int make_shares(const rapid_attn_desc_t& d, const int32_t* bounds, Share (&shares)[2]) {
+    const int parts = kTile / d.seq_len < d.n_seq ? kTile / d.seq_len : d.n_seq;
+    if (parts < 2) {
+        shares[0] = Share{d, make_geometry(d, bounds), 0};
+        return 1;
+    }
+    int count = 0;
+    for (int first = 0; first < d.n_seq;) {
+        Share& s = shares[count++];
+        const int here = d.n_seq - first < parts ? d.n_seq - first : parts, sequences = (d.n_seq - first) / here;
+        s.d = d;
+        s.d.n_seq = sequences;
+        s.d.seq_len = here * d.seq_len;
+        s.g = make_geometry(s.d, bounds ? bounds + 2 * (int64_t)first : nullptr);
+        s.g.window = d.window == 0 || d.window > d.seq_len ? d.seq_len : d.window;
+        s.g.part = d.seq_len;
+        s.g.parts = here;
+        s.first_row = (int64_t)first * d.seq_len;
+        first += sequences * here;
+    }
+    return count;
 }
 
 }  // namespace attn
@@ -538,22 +564,31 @@ extern "C" rapid_status_t rapid_attention_fwd(const rapid_attn_desc_t* desc, con
         return RAPID_ERR_INVALID_ARG;
     int sms = 0;
     if ((s = policy::check_device(&sms)) != RAPID_OK) return s;
-    CUtensorMap mq, mk, mv, mo;
-    if (!make_head_map(&mq, q, d, d.n_heads, d.ld_q) || !make_head_map(&mk, k, d, d.n_kv_heads, d.ld_k) ||
-        !make_head_map(&mv, v, d, d.n_kv_heads, d.ld_v) || !make_head_map(&mo, out, d, d.n_heads, d.ld_out))
-        return RAPID_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (policy::clear_stats(stats, st) != cudaSuccess) return RAPID_ERR_CUDA;
-    FwdArgs a;
-    a.g = make_geometry(d, bounds);
-    a.scale_log2 = (float)(d.scale * kLog2eD);
-    a.out = static_cast<uint16_t*>(out);
-    a.ld_out = d.ld_out;
-    a.lse = lse;
-    a.stats = stats;
-    a.items = (d.seq_len + kTile - 1) / kTile * a.g.group;
-    a.pairs = (a.items + 1) / 2;
-    const unsigned grid = (unsigned)((int64_t)a.pairs * d.n_seq * d.n_kv_heads);
-    const cudaError_t e = d.head_dim <= 64 ? launch_fwd<64>(mq, mk, mv, mo, a, grid, st) : launch_fwd<128>(mq, mk, mv, mo, a, grid, st);
+    Share shares[2];
+    const int count = make_shares(d, bounds, shares);
+    cudaError_t e = cudaSuccess;
+    for (int i = 0; i < count && e == cudaSuccess; ++i) {
+        const Share& c = shares[i];
+        void* rows = rows_from(out, c.first_row, d.ld_out);
+        CUtensorMap mq, mk, mv, mo;
+        if (!make_head_map(&mq, rows_from(q, c.first_row, d.ld_q), c.d, d.n_heads, d.ld_q) ||
+            !make_head_map(&mk, rows_from(k, c.first_row, d.ld_k), c.d, d.n_kv_heads, d.ld_k) ||
+            !make_head_map(&mv, rows_from(v, c.first_row, d.ld_v), c.d, d.n_kv_heads, d.ld_v) ||
+            !make_head_map(&mo, rows, c.d, d.n_heads, d.ld_out))
+            return RAPID_ERR_CUDA;
+        FwdArgs a;
+        a.g = c.g;
+        a.scale_log2 = (float)(d.scale * kLog2eD);
+        a.out = static_cast<uint16_t*>(rows);
+        a.ld_out = d.ld_out;
+        a.lse = lse ? lse + c.first_row * d.n_heads : nullptr;
+        a.stats = stats;
+        a.items = (c.d.seq_len + kTile - 1) / kTile * a.g.group;
+        a.pairs = (a.items + 1) / 2;
+        const unsigned grid = (unsigned)((int64_t)a.pairs * c.d.n_seq * d.n_kv_heads);
+        e = d.head_dim <= 64 ? launch_fwd<64>(mq, mk, mv, mo, a, grid, st) : launch_fwd<128>(mq, mk, mv, mo, a, grid, st);
+    }
     return e == cudaSuccess ? RAPID_OK : RAPID_ERR_CUDA;
 }

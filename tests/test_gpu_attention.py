@@ -292,3 +292,39 @@ def test_window_beyond_the_generation(window):
     dout = torch.randn_like(out)
     a, b = (rb.attention_grad(q, k, v, out, lse, dout, 2, 300, None, w) for w in (300, window))
     assert torch.equal(a.dq, b.dq) and torch.equal(a.dk, b.dk) and torch.equal(a.dv, b.dv)
+
+
+# generations of at most 64 positions share tiles; the last tile may hold fewer of them
+SHORT = [(17, 8, 4, 2, 128, 3, "mixed"), (40, 33, 3, 1, 64, 0, "mixed"), (9, 64, 2, 2, 80, 0, "left"), (300, 1, 3, 1, 128, 0, "full"),
+         (129, 1, 2, 1, 64, 0, "mixed"), (3, 42, 6, 2, 128, 7, "right"), (256, 64, 2, 1, 64, 20, "mixed"), (5, 25, 1, 1, 8, 0, "full"),
+         (2, 64, 4, 4, 128, 1, "right"), (63, 5, 9, 3, 128, 0, "left")]
+
+
+@pytest.mark.parametrize("n,length,heads,kv,hd,window,kind", SHORT)
+def test_short_generations(n, length, heads, kv, hd, window, kind):
+    test_forward(n, length, heads, kv, hd, window, kind)
+    test_backward(n, length, heads, kv, hd, window, kind)
+
+
+def test_short_generations_do_not_influence_one_another():
+    """Generations that share a tile give the same bits whatever their neighbours hold.  (Not the bits of the generation in a tile
+    of its own: a key's place in the tile decides which partial sum its exponential goes to, and which form it takes.)"""
+    n, length, heads, kv, hd = 11, 21, 4, 2, 64
+    _, dev, b, _, out, _, lse, dout = _backward_inputs(n, length, heads, kv, hd, 0, "mixed", 8, pitch=8)
+    dout = dout.cuda()
+    r = rb.attention_grad(*dev, out, lse, dout, n, length, b)
+    kept = [x.contiguous().view(n, length, -1, hd) for x in (*dev, dout)]
+    other = [x.clone() for x in kept]
+    b2 = b.clone()
+    for x in other:
+        x[1::2] = torch.randn_like(x[1::2]) * 30
+        x[5] = float("nan")
+    b2[1::2] = torch.tensor([2, length - 1], dtype=torch.int32, device="cuda")
+    b2[5] = 0
+    q, k, v, do = [x.view(n * length, -1, hd) for x in other]
+    out2, lse2 = rb.attention(q, k, v, n, length, b2)
+    r2 = rb.attention_grad(q, k, v, out2, lse2, do, n, length, b2)
+    assert torch.equal(lse2[::2], lse[::2])
+    for x, y in ((out, out2), (r.dq, r2.dq), (r.dk, r2.dk), (r.dv, r2.dv)):
+        x, y = x.view(n, length, -1, hd), y.view(n, length, -1, hd)
+        assert torch.equal(x[::2], y[::2]) and (y[5] == 0).all() and y.isfinite().all()
