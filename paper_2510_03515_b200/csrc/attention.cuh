@@ -429,17 +429,18 @@ __device__ __forceinline__ size_t lse_at(const Geometry& g, int n, int h, int po
     const int gen = pos / g.part;
     return (((size_t)n * g.parts + gen) * g.heads + h) * g.part + (pos - gen * g.part);
 }
-__device__ __forceinline__ bool dirty(const Geometry& g, int tile, int lo, int hi) {
-    return g.part != 0 || tile * kTile < lo || tile * kTile + kTile > hi;
+template <bool SHARED>
+__device__ __forceinline__ bool dirty(int tile, int lo, int hi) {
+    return SHARED || tile * kTile < lo || tile * kTile + kTile > hi;
 }
 // Zero the dead rows of a tile, by one warp; the tile's first position is t0.
-template <int D>
+template <int D, bool SHARED>
 __device__ __forceinline__ void zero_dead_rows(const Geometry& g, uint8_t* tile, int n, int t0, int lo, int hi, int lane) {
     uint32_t dead[kTile / 32];
 #pragma unroll
     for (int k = 0; k < kTile / 32; ++k) {
         int a = lo, b = hi;
-        row_range(g, n, t0 + 32 * k + lane, a, b);
+        if (SHARED) row_range(g, n, t0 + 32 * k + lane, a, b);
         dead[k] = __ballot_sync(0xffffffffu, t0 + 32 * k + lane < a || t0 + 32 * k + lane >= b);
     }
 #pragma unroll

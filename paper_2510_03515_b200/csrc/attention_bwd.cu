@@ -49,6 +49,8 @@ struct BwdArgs {
 // 8 elements each, and have four of them in flight.
 constexpr int kTermRows = 16;
 
+// SHARED: generations share tiles.
+template <bool SHARED>
 __global__ void __launch_bounds__(256)
 attn_row_terms_kernel(Geometry g, int tiles, int lanes_log2, const uint16_t* __restrict__ out, int64_t ld_out,
                       const uint16_t* __restrict__ dout, int64_t ld_dout, const float* __restrict__ lse, float* __restrict__ shift,
@@ -72,7 +74,7 @@ attn_row_terms_kernel(Geometry g, int tiles, int lanes_log2, const uint16_t* __r
             h[k] = u - t[k] * g.heads;
             t[k] += t0;
             int from = lo, to = hi;
-            row_range(g, n, t[k], from, to);
+            if (SHARED) row_range(g, n, t[k], from, to);
             live[k] = u < units && t[k] >= from && t[k] < to;
             if (live[k] && lane * 8 < g.head_dim) {
                 const int64_t r = (int64_t)n * g.seq_len + t[k];
@@ -94,7 +96,7 @@ attn_row_terms_kernel(Geometry g, int tiles, int lanes_log2, const uint16_t* __r
             if (lane == 0 && first + k * groups < units) {
                 const int64_t at = ((int64_t)n * g.heads + h[k]) * padded + t[k];
                 // double: lse * log2(e) in float would shift every score of the row by its own rounding
-                shift[at] = live[k] ? (float)((double)lse[lse_at(g, n, h[k], t[k])] * -kLog2eD) : -INFINITY;
+                shift[at] = live[k] ? (float)((double)lse[SHARED ? lse_at(g, n, h[k], t[k]) : ((size_t)n * g.heads + h[k]) * g.seq_len + t[k]] * -kLog2eD) : -INFINITY;
                 ndelta[at] = -sum;
             }
         }
@@ -177,7 +179,7 @@ struct DkvCfg {
     static_assert(kSmem <= 232448, "shared memory of an SM");
 };
 
-template <int D>
+template <int D, bool SHARED>
 __global__ void __launch_bounds__(W::kThreads, 1)
 attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                 const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo,
@@ -277,7 +279,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 }
                 int h = x.hk * g.group, qt = x.q_from;
                 for (int i = 0; i < x.steps; ++i) {
-                    const bool clean = dirty(g, qt, x.lo, x.hi);
+                    const bool clean = dirty<SHARED>(qt, x.lo, x.hi);
                     if (steps >= kQ && !(ok = wait_one(&m.q_empty[qa.s], qa.parity ^ 1u, abortp))) break;
                     uint64_t* bar = clean ? &m.q_raw[qa.s] : &m.q_full[qa.s];
                     q_was_raw = clean ? q_was_raw | (1u << qa.s) : q_was_raw & ~(1u << qa.s);
@@ -349,12 +351,12 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         for (uint32_t k = 0; ok && work_take(&m.queue, k, x, lane, abortp); ++k) {
             int qt = x.q_from;
             for (int i = 0; i < x.steps && ok; ++i) {
-                if (dirty(g, qt, x.lo, x.hi)) {
+                if (dirty<SHARED>(qt, x.lo, x.hi)) {
                     ok = wait_all(&m.q_raw[qa.s], q_raw.flip(qa.s), abortp);
-                    if (ok) zero_dead_rows<D>(g, q_tile(qa.s), x.n, qt * kTile, x.lo, x.hi, lane);
+                    if (ok) zero_dead_rows<D, SHARED>(g, q_tile(qa.s), x.n, qt * kTile, x.lo, x.hi, lane);
                     if (ok && lane == 0) mbar_arrive(&m.q_full[qa.s]);
                     ok = ok && wait_all(&m.do_raw[da.s], do_raw.flip(da.s), abortp);
-                    if (ok) zero_dead_rows<D>(g, do_tile(da.s), x.n, qt * kTile, x.lo, x.hi, lane);
+                    if (ok) zero_dead_rows<D, SHARED>(g, do_tile(da.s), x.n, qt * kTile, x.lo, x.hi, lane);
                     if (ok && lane == 0) mbar_arrive(&m.do_full[da.s]);
                 }
                 qa.step();
@@ -458,8 +460,8 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         for (uint32_t k = 0; work_take(&m.queue, k, x, lane, abortp); ++k) {
             const int key = x.kt * kTile + row;
             int lo = x.lo, hi = x.hi;
-            row_range(g, x.n, key, lo, hi);
-            const unsigned seen_by = g.part == 0 ? (unsigned)g.window : (unsigned)max(0, min(g.window, hi - key));  // queries from `key` on
+            if (SHARED) row_range(g, x.n, key, lo, hi);
+            const unsigned seen_by = !SHARED ? (unsigned)g.window : (unsigned)max(0, min(g.window, hi - key));  // queries from `key` on
             int qt = x.q_from;
             for (int i = 0; i < x.steps; ++i, ++gi) {
                 const int q0 = qt * kTile;
@@ -555,7 +557,7 @@ struct alignas(16) DqWork {
     }
 };
 
-template <int D>
+template <int D, bool SHARED>
 __global__ void __launch_bounds__(W::kThreads, 1)
 attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo,
@@ -664,7 +666,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 const int hk = x.h / g.group;
                 for (int i = 0; i < x.steps; ++i) {
                     const int t0 = (x.from + i) * kTile;
-                    const bool clean = dirty(g, x.from + i, x.lo, x.hi);
+                    const bool clean = dirty<SHARED>(x.from + i, x.lo, x.hi);
                     if (nk >= kKeys && !(ok = wait_one(&k_empty[ka.s], ka.parity ^ 1u, abortp))) break;
                     flush(ka.s);
                     if (!ok) break;
@@ -724,12 +726,12 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         for (uint32_t k = 0; ok && work_take(&queue, k, x, lane, abortp); ++k) {
             for (int i = 0; i < x.steps && ok; ++i) {
                 const int t0 = (x.from + i) * kTile;
-                if (dirty(g, x.from + i, x.lo, x.hi)) {
+                if (dirty<SHARED>(x.from + i, x.lo, x.hi)) {
                     ok = wait_all(&k_raw[ka.s], kr.flip(ka.s), abortp);
-                    if (ok) zero_dead_rows<D>(g, k_tile(ka.s), x.n, t0, x.lo, x.hi, lane);
+                    if (ok) zero_dead_rows<D, SHARED>(g, k_tile(ka.s), x.n, t0, x.lo, x.hi, lane);
                     if (ok && lane == 0) mbar_arrive(&k_full[ka.s]);
                     ok = ok && wait_all(&v_raw[va.s], vr.flip(va.s), abortp);
-                    if (ok) zero_dead_rows<D>(g, v_tile(va.s), x.n, t0, x.lo, x.hi, lane);
+                    if (ok) zero_dead_rows<D, SHARED>(g, v_tile(va.s), x.n, t0, x.lo, x.hi, lane);
                     if (ok && lane == 0) mbar_arrive(&v_full[va.s]);
                 }
                 ka.step();
@@ -830,12 +832,12 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         for (uint32_t k = 1; more; ++k) {
             const int pos = x.t * kTile + row;
             int lo = x.lo, hi = x.hi;
-            row_range(g, x.n, pos, lo, hi);
+            if (SHARED) row_range(g, x.n, pos, lo, hi);
             const bool live = pos >= lo && pos < hi;
             const int see = max(lo, pos - g.window + 1);
             const unsigned count = live ? (unsigned)(pos + 1 - see) : 0u;
             int full_from = 1 << 30, full_to = 0;  // key tiles that every row of the tile sees whole
-            if (g.part == 0 && x.t * kTile >= x.lo && x.t * kTile + kTile <= x.hi) {
+            if (!SHARED && x.t * kTile >= x.lo && x.t * kTile + kTile <= x.hi) {
                 full_from = (max(x.lo, x.t * kTile + kTile - g.window) + kTile - 1) / kTile;
                 full_to = x.t;
             }
@@ -895,14 +897,14 @@ struct Maps {
     CUtensorMap q, k, v, dout, dq, dk, dv;
 };
 
-template <int D>
+template <int D, bool SHARED>
 cudaError_t launch_bwd(const Maps& m, const BwdArgs& a, cudaStream_t st) {
-    cudaError_t e = cudaFuncSetAttribute(attn_dkv_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)DkvCfg<D>::kSmem);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_dq_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)DqCfg<D>::kSmem);
+    cudaError_t e = cudaFuncSetAttribute(attn_dkv_kernel<D, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)DkvCfg<D>::kSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_dq_kernel<D, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)DqCfg<D>::kSmem);
     if (e != cudaSuccess) return e;
     const unsigned nk = (unsigned)(a.g.n_seq * a.g.kv_heads), nh = (unsigned)(a.g.n_seq * a.g.heads);
-    attn_dkv_kernel<D><<<nk * (unsigned)a.tiles, W::kThreads, DkvCfg<D>::kSmem, st>>>(m.q, m.k, m.v, m.dout, m.dk, m.dv, a);
-    attn_dq_kernel<D><<<nh * (unsigned)a.tiles, W::kThreads, DqCfg<D>::kSmem, st>>>(m.q, m.k, m.v, m.dout, m.dq, a);
+    attn_dkv_kernel<D, SHARED><<<nk * (unsigned)a.tiles, W::kThreads, DkvCfg<D>::kSmem, st>>>(m.q, m.k, m.v, m.dout, m.dk, m.dv, a);
+    attn_dq_kernel<D, SHARED><<<nh * (unsigned)a.tiles, W::kThreads, DqCfg<D>::kSmem, st>>>(m.q, m.k, m.v, m.dout, m.dq, a);
     return cudaGetLastError();
 }
 
@@ -1004,10 +1006,13 @@ extern "C" rapid_status_t rapid_attention_bwd(const rapid_attn_desc_t* desc, con
         a.stats = stats;
         const int64_t blocks = (int64_t)c.d.n_seq * a.tiles * (kTile / kTermRows);
         if (blocks > 0x7fffffffll) return RAPID_ERR_UNSUPPORTED;
-        attn_row_terms_kernel<<<(unsigned)blocks, 256, 0, st>>>(a.g, a.tiles, lanes_log2, static_cast<const uint16_t*>(o_rows), d.ld_out,
-                                                                static_cast<const uint16_t*>(do_rows), d.ld_dout,
-                                                                lse + c.first_row * d.n_heads, static_cast<float*>(workspace), ndelta);
-        e = d.head_dim <= 64 ? launch_bwd<64>(m, a, st) : launch_bwd<128>(m, a, st);
+        auto terms_kernel = c.g.part ? attn_row_terms_kernel<true> : attn_row_terms_kernel<false>;
+        terms_kernel<<<(unsigned)blocks, 256, 0, st>>>(a.g, a.tiles, lanes_log2, static_cast<const uint16_t*>(o_rows), d.ld_out,
+                                                       static_cast<const uint16_t*>(do_rows), d.ld_dout, lse + c.first_row * d.n_heads,
+                                                       static_cast<float*>(workspace), ndelta);
+        auto launch = d.head_dim <= 64 ? (c.g.part ? launch_bwd<64, true> : launch_bwd<64, false>)
+                                       : (c.g.part ? launch_bwd<128, true> : launch_bwd<128, false>);
+        e = launch(m, a, st);
     }
     return e == cudaSuccess ? RAPID_OK : RAPID_ERR_CUDA;
 }

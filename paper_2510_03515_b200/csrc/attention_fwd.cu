@@ -81,7 +81,7 @@ struct alignas(16) FwdWork {
     }
 };
 
-template <int D>
+template <int D, bool SHARED>
 __global__ void __launch_bounds__(W::kThreads, 1)
 attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                 const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mo, const __grid_constant__ FwdArgs a) {
@@ -165,7 +165,7 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                     for (int half = 0; half < 2; ++half) {
                         if (it >= kStages && !(ok = wait_one(&kv_empty[at.s], at.parity ^ 1u, abortp))) break;
                         // dead keys are masked in the scores; dead values have to be zero
-                        const bool clean = half && dirty(g, j, x.lo, x.hi);
+                        const bool clean = half && dirty<SHARED>(j, x.lo, x.hi);
                         uint64_t* bar = clean ? &kv_raw[at.s] : &kv_full[at.s];
                         was_raw = clean ? was_raw | (1u << at.s) : was_raw & ~(1u << at.s);
                         if (clean) raw.flip(at.s);
@@ -199,9 +199,9 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         for (uint32_t k = 0; ok && work_take(&queue, k, x, lane, abortp); ++k)
             for (int j = x.jlo; j < x.jhi && ok; ++j) {
                 at.step();  // past the keys
-                if (dirty(g, j, x.lo, x.hi)) {
+                if (dirty<SHARED>(j, x.lo, x.hi)) {
                     ok = wait_all(&kv_raw[at.s], raw.flip(at.s), abortp);
-                    if (ok) zero_dead_rows<D>(g, kv_tile(at.s), x.n, j * kTile, x.lo, x.hi, lane);
+                    if (ok) zero_dead_rows<D, SHARED>(g, kv_tile(at.s), x.n, j * kTile, x.lo, x.hi, lane);
                     if (ok && lane == 0) mbar_arrive(&kv_full[at.s]);
                 }
                 at.step();
@@ -338,14 +338,14 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             const int tw = w ? x.t[1] : x.t[0], hw = w ? x.h[1] : x.h[0], fw = w ? x.from[1] : x.from[0], ew = w ? x.to[1] : x.to[0];
             const int pos = tw * kTile + row;
             int lo = x.lo, hi = x.hi;
-            row_range(g, x.n, pos, lo, hi);
+            if (SHARED) row_range(g, x.n, pos, lo, hi);
             const bool live = pos >= lo && pos < hi && ew > fw;
             // keys [see, see + count) are visible to this row
             const int see = max(lo, pos - g.window + 1);
             const unsigned count = live ? (unsigned)(pos + 1 - see) : 0u;
             // key tiles in [full_from, full_to) are visible to every row of this tile; the others are masked
             int full_from = 1 << 30, full_to = 0;
-            if (g.part == 0 && tw * kTile >= x.lo && tw * kTile + kTile <= x.hi) {
+            if (!SHARED && tw * kTile >= x.lo && tw * kTile + kTile <= x.hi) {
                 full_from = (max(x.lo, tw * kTile + kTile - g.window) + kTile - 1) / kTile;
                 full_to = tw;
             }
@@ -475,10 +475,10 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     if (tid == 0 && abort_flag && a.stats) atomicMax(&a.stats->status, (int)RAPID_ERR_TIMEOUT);
 }
 
-template <int D>
+template <int D, bool SHARED>
 cudaError_t launch_fwd(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mo, const FwdArgs& a,
                        unsigned grid, cudaStream_t st) {
-    auto kern = attn_fwd_kernel<D>;
+    auto kern = attn_fwd_kernel<D, SHARED>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FwdCfg<D>::kSmem);
     if (e != cudaSuccess) return e;
     kern<<<grid, W::kThreads, FwdCfg<D>::kSmem, st>>>(mq, mk, mv, mo, a);
@@ -588,7 +588,9 @@ extern "C" rapid_status_t rapid_attention_fwd(const rapid_attn_desc_t* desc, con
         a.items = (c.d.seq_len + kTile - 1) / kTile * a.g.group;
         a.pairs = (a.items + 1) / 2;
         const unsigned grid = (unsigned)((int64_t)a.pairs * c.d.n_seq * d.n_kv_heads);
-        e = d.head_dim <= 64 ? launch_fwd<64>(mq, mk, mv, mo, a, grid, st) : launch_fwd<128>(mq, mk, mv, mo, a, grid, st);
+        auto launch = d.head_dim <= 64 ? (c.g.part ? launch_fwd<64, true> : launch_fwd<64, false>)
+                                       : (c.g.part ? launch_fwd<128, true> : launch_fwd<128, false>);
+        e = launch(mq, mk, mv, mo, a, grid, st);
     }
     return e == cudaSuccess ? RAPID_OK : RAPID_ERR_CUDA;
 }
