@@ -436,11 +436,20 @@ __device__ __forceinline__ bool dirty(int tile, int lo, int hi) {
 // Zero the dead rows of a tile, by one warp; the tile's first position is t0.
 template <int D, bool SHARED>
 __device__ __forceinline__ void zero_dead_rows(const Geometry& g, uint8_t* tile, int n, int t0, int lo, int hi, int lane) {
+    if (!SHARED) {  // as below, the gradient of 3 x 4095 positions took 212 us instead of 194
+        for (int i = lane; i < D / 64 * kTile * 8; i += 32) {
+            const int row = (i >> 3) & (kTile - 1);
+            if (t0 + row < lo || t0 + row >= hi) reinterpret_cast<uint4*>(tile)[i] = make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        return;
+    }
     uint32_t dead[kTile / 32];
 #pragma unroll
     for (int k = 0; k < kTile / 32; ++k) {
         int a = lo, b = hi;
-        if (SHARED) row_range(g, n, t0 + 32 * k + lane, a, b);
+        row_range(g, n, t0 + 32 * k + lane, a, b);
         dead[k] = __ballot_sync(0xffffffffu, t0 + 32 * k + lane < a || t0 + 32 * k + lane >= b);
     }
 #pragma unroll
