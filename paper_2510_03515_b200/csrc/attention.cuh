@@ -303,33 +303,6 @@ __device__ __forceinline__ bool work_take(WorkQueue<W>* q, uint32_t k, W& w, int
     return !w.end;
 }
 
-// ---- exponentials -------------------------------------------------------------------------------------------------
-//
-// The special-function unit forms 16 exponentials a cycle and SM, which is what bounds these kernels' inner loops (1024
-// cycles for a 128 x 128 tile against 512 for a product with D = 128).  So a part of them is formed by the multiply-add
-// units: 2^x = 2^n 2^f with n = round(x) and f in [-1/2, 1/2]; 2^f by the polynomial of degree 4 with the least maximal
-// relative error (2.6e-6; coefficients from a Remez iteration), 2^n by adding n to the exponent's bits.  Below 2^-126 the
-// result is not zero but some value below 1.2e-38.
-__device__ __forceinline__ void exp2_pair_poly(uint64_t x2, float& lo, float& hi) {
-    constexpr float kRound = 12582912.f;  // 1.5 * 2^23: adding it rounds to an integer, which lands in the low bits
-    float x, y;
-    f32x2_split(x2, x, y);
-    x2 = f32x2(fmaxf(x, -126.f), fmaxf(y, -126.f));
-    const uint64_t r = f32x2_add(x2, f32x2(kRound, kRound));
-    const uint64_t n = f32x2_add(r, f32x2(-kRound, -kRound));
-    const uint64_t f = f32x2_fma(n, f32x2(-1.f, -1.f), x2);
-    uint64_t p = f32x2(0.009570102207362652f, 0.009570102207362652f);
-    p = f32x2_fma(p, f, f32x2(0.05591785907745361f, 0.05591785907745361f));
-    p = f32x2_fma(p, f, f32x2(0.240247443318367f, 0.240247443318367f));
-    p = f32x2_fma(p, f, f32x2(0.6931217908859253f, 0.6931217908859253f));
-    p = f32x2_fma(p, f, f32x2(0.9999992847442627f, 0.9999992847442627f));
-    float a, b, u, v;
-    f32x2_split(p, a, b);
-    f32x2_split(r, u, v);
-    lo = __int_as_float(__float_as_int(a) + (__float_as_int(u) << 23));
-    hi = __int_as_float(__float_as_int(b) + (__float_as_int(v) << 23));
-}
-
 // The largest of three (one instruction at the rate of the two-operand form).
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;

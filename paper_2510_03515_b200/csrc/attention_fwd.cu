@@ -10,9 +10,11 @@
 // when a row's maximum has grown by more than 2^8 since the last time (exponentials up to 2^8 are as exact in float and
 // bf16 as those below 1), and the warp that finds this does it itself.
 //
-// Measured: 8 x 4096 positions at most, 16 heads of 64: 300 us (670 TFLOP/s; up to 350 under the power cap), where the
-// exponentials alone take about 180; 64 x 256, 12 heads of 128: 47 us, of which the key tiles' work is a third and the rest the
-// beginnings and ends of pieces of one to three tiles.
+// Measured: 8 x 4096 positions at most, 16 heads of 64: 292 us (690 TFLOP/s; up to 350 under the power cap), where the
+// exponentials alone take about 180 at 16 a cycle and SM; 64 x 256, 12 heads of 128: 48 us, of which the key tiles' work is a
+// third and the rest the beginnings and ends of pieces of one to three tiles.  All exponentials are the special-function unit's,
+// whose result for a masked score is exactly zero; one pair in 16 by a polynomial instead, with its result selected to zero there:
+// 293 and 49 us, and 195 against 191 for 64 x 1024, 12 heads of 128.
 #include <math.h>
 
 #include "attention.cuh"
@@ -39,8 +41,6 @@ template <int D>
 struct FwdCfg {
     static constexpr uint32_t kStages = D == 128 ? 4 : 8;  // tiles in flight, keys and values alternating
     static constexpr bool kOverlay = D == 128;        // P over S
-    // Of 16 pairs of exponentials, those formed by polynomial.  With 0, 1, 2, 3, 4: 302, 298, 305, 308, 308 us (8 x 4096, 16 heads of 64).
-    static constexpr int kPoly = 1;
     static constexpr size_t kSmem = (size_t)(2 + kStages) * tile_bytes<D>() + 2 * kBoxBytes + 1024;  // with a box of output for each item
 };
 
@@ -410,13 +410,9 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                     for (int e = 0; e < 16; ++e) {
                         const uint64_t z = f32x2_fma(f32x2(__uint_as_float(s[i][2 * e]), __uint_as_float(s[i][2 * e + 1])), c2, shift2);
                         float u, v;
-                        if ((e & 3) == 3 && e / 4 < FwdCfg<D>::kPoly) {
-                            exp2_pair_poly(z, u, v);
-                        } else {
-                            f32x2_split(z, u, v);
-                            u = ex2_approx(u);
-                            v = ex2_approx(v);
-                        }
+                        f32x2_split(z, u, v);
+                        u = ex2_approx(u);  // exactly zero for a masked score
+                        v = ex2_approx(v);
                         part[e & 1] = f32x2_add(part[e & 1], f32x2(u, v));
                         p[e] = pack_bf16x2(u, v);
                     }

@@ -1,0 +1,62 @@
+"""Pairs that do not see each other contribute exactly nothing to attention, however large the finite values on either side are."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from paper_2510_03515_b200 import binding as rb  # noqa: E402
+
+BF = torch.bfloat16
+HUGE = 3e38
+
+
+def _rows(n, length, heads, kv, hd, seed):
+    g = torch.Generator().manual_seed(seed)
+    mk = lambda h: torch.randn(n * length, h, hd, generator=g).to(BF).cuda()  # noqa: E731
+    return mk(heads), mk(kv), mk(kv)
+
+
+def _signs(x, seed):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randint(0, 2, x.shape, generator=g) * 2 - 1).to(BF).to(x.device) * HUGE
+
+
+# n_seq = 1: length, head_dim, window, first position with other values
+SEEN = [(100, 64, 0, 40), (300, 64, 0, 131), (300, 128, 0, 131), (700, 128, 0, 390), (700, 64, 0, 512), (130, 80, 0, 3)]
+WINDOWED = [(300, 64, 20, 131), (700, 128, 130, 257), (700, 64, 256, 300), (90, 128, 7, 40)]
+
+
+@pytest.mark.parametrize("what", ["k", "v"])
+@pytest.mark.parametrize("length,hd,window,s", SEEN)
+def test_later_keys(length, hd, window, s, what):
+    q, k, v = _rows(1, length, 4, 2, hd, 1)
+    out, lse = rb.attention(q, k, v, 1, length, None, window)
+    k2, v2 = k.clone(), v.clone()
+    (k2 if what == "k" else v2)[s:] = _signs(v[s:], 2)
+    out2, lse2 = rb.attention(q, k2, v2, 1, length, None, window)
+    assert torch.equal(out2[:s], out[:s]) and torch.equal(lse2[:, :, :s], lse[:, :, :s])
+
+
+@pytest.mark.parametrize("what", ["k", "v"])
+@pytest.mark.parametrize("length,hd,window,s", WINDOWED)
+def test_keys_before_the_window(length, hd, window, s, what):
+    q, k, v = _rows(1, length, 4, 2, hd, 3)
+    out, lse = rb.attention(q, k, v, 1, length, None, window)
+    k2, v2 = k.clone(), v.clone()
+    (k2 if what == "k" else v2)[:s] = _signs(v[:s], 4)
+    out2, lse2 = rb.attention(q, k2, v2, 1, length, None, window)
+    first = s + window - 1  # sees nothing before s
+    assert torch.equal(out2[first:], out[first:]) and torch.equal(lse2[:, :, first:], lse[:, :, first:])
+
+
+@pytest.mark.parametrize("n,length,hd", [(11, 21, 64), (40, 8, 128), (6, 64, 64), (130, 1, 128)])
+def test_live_neighbours_in_a_tile(n, length, hd):
+    """Short generations share tiles: what a live neighbour holds does not reach the others."""
+    q, k, v = _rows(n, length, 4, 2, hd, 9)
+    out, lse = rb.attention(q, k, v, n, length)
+    grid = lambda x: x.view(n, length, -1, hd)  # noqa: E731
+    for which in range(3):
+        x = [t.clone() for t in (q, k, v)]
+        grid(x[which])[1::2] = _signs(grid(x[which])[1::2], 10)
+        out2, lse2 = rb.attention(*x, n, length)
+        assert torch.equal(grid(out2)[::2], grid(out)[::2]) and torch.equal(lse2[::2], lse[::2]), which
