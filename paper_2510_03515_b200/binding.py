@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import math
+import operator
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -490,6 +491,15 @@ def _workspace(query, desc, where: str) -> int:
 
 # Descriptors by their values, with the workspace size where one is needed: shapes repeat from call to call, and building a
 # descriptor of 17 fields takes longer than a small kernel.  Only the convenience functions use these, and never change them.
+# Every number among the keys is a Python int or float by then: a tensor is found again by its identity, whatever it holds.
+
+def _int(x) -> int:
+    return x if type(x) is int else operator.index(x)
+
+
+def _float(x) -> float:
+    return x if type(x) is float else float(x)
+
 
 @functools.lru_cache(maxsize=512)
 def _embed_plan(n_rows, vocab, dim, dtype, ld_table, ld_rows, scale, flags, bwd):
@@ -537,6 +547,7 @@ def embedding(table: torch.Tensor, tokens: torch.Tensor, mask: Optional[torch.Te
     zeros.  tokens [T] int32, table [V, D] (rows on 16-byte boundaries)."""
     if table.dim() != 2:
         raise ValueError("table: a matrix [V, D] expected")
+    scale = _float(scale)
     T, (V, D) = tokens.numel(), table.shape
     mask = _mask8(mask, T)
     _vector(tokens, T, torch.int32, "tokens")
@@ -557,6 +568,7 @@ def embedding_grad(dout: torch.Tensor, tokens: torch.Tensor, mask: Optional[torc
     is then returned (its type counts, not `dtable_dtype`)."""
     if dout.dim() != 2:
         raise ValueError("dout: a matrix [T, D] expected")
+    vocab, scale = _int(vocab), _float(scale)
     T, D = dout.shape
     mask = _mask8(mask, T)
     _vector(tokens, T, torch.int32, "tokens")
@@ -636,6 +648,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Tens
                  mask: Optional[torch.Tensor] = None, eps: float = 1e-6, flags: int = 0):
     """Norm of every head of q [T, Hq, D] and k [T, Hk, D], then rotation by position (2 * inv_freq.numel() elements of a
     head); returns contiguous (q_out, k_out).  q and k may be slices of one projection's rows."""
+    n_seq, seq_len, eps, flags = _int(n_seq), _int(seq_len), _float(eps), _int(flags)
     q_weight, k_weight, mask = _qk_args(q, k, q_weight, k_weight, inv_freq, n_seq, seq_len, positions, mask, flags)
     dev = _one_device(q, k, q_weight, k_weight, inv_freq, positions, mask)
     with _on(dev):
@@ -661,6 +674,7 @@ def qk_norm_rope_grad(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch
                       flags: int = 0, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None) -> QkGrads:
     """The gradient of qk_norm_rope() from its inputs and the gradients of its outputs.  dq and dk may be given (slices of the
     gradient of one projection, say, or dq_out and dk_out themselves)."""
+    n_seq, seq_len, eps, flags = _int(n_seq), _int(seq_len), _float(eps), _int(flags)
     q_weight, k_weight, mask = _qk_args(q, k, q_weight, k_weight, inv_freq, n_seq, seq_len, positions, mask, flags)
     if dq_out.shape != q.shape or dk_out.shape != k.shape:
         raise ValueError("dq_out, dk_out: the shapes of q and k expected")
@@ -728,6 +742,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_seq: int, seq
     """Causal attention over the padded token grid, q [T, H, D], k and v [T, Hk, D] bfloat16 (rows may be slices of one
     projection); bounds [n_seq, 2] int32 gives each generation's live positions.  Returns out [T, H, D] and lse
     [n_seq, H, seq_len] float32.  The default scale is D ** -0.5."""
+    n_seq, seq_len, window, scale = _int(n_seq), _int(seq_len), _int(window), None if scale is None else _float(scale)
     _attn_args(q, k, v, n_seq, seq_len, bounds)
     dev = _one_device(q, k, v, bounds, stats)
     with _on(dev):
@@ -755,6 +770,7 @@ def attention_grad(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch
                    dv: Optional[torch.Tensor] = None) -> AttnGrads:
     """The gradient of attention() from its inputs, its outputs out and lse, and the gradient of out.  dq, dk and dv may be
     given (slices of the gradient of one projection, say)."""
+    n_seq, seq_len, window, scale = _int(n_seq), _int(seq_len), _int(window), None if scale is None else _float(scale)
     _attn_args(q, k, v, n_seq, seq_len, bounds)
     if out.shape != q.shape or dout.shape != q.shape:
         raise ValueError("out, dout: the shape of q expected")
