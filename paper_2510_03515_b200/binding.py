@@ -519,8 +519,18 @@ def _attn_plan(n_seq, seq_len, h, hk, hd, window, scale, pitches, bwd):
     return desc, rapid_attention_bwd_workspace_bytes(desc) if bwd else 0
 
 
+def _fits(flags: int, **numbers: int) -> None:
+    """A field of 32 bits would keep a larger number's low bits."""
+    for name, x in numbers.items():
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ValueError(f"{name}: {x} is not a number of 32 bits")
+    if not 0 <= flags < 2 ** 32:
+        raise ValueError(f"flags: {flags} is not a set of 32 bits")
+
+
 def make_embed_desc(n_rows: int, vocab: int, dim: int, dtype: torch.dtype, ld_table: Optional[int] = None,
                     ld_rows: Optional[int] = None, scale: float = 1.0, flags: int = 0) -> EmbedDesc:
+    _fits(flags, vocab=vocab, dim=dim)
     return EmbedDesc(n_rows, vocab, dim, dim if ld_table is None else ld_table, dim if ld_rows is None else ld_rows,
                      _dtype_code(dtype), flags, float(scale), 0)
 
@@ -596,6 +606,8 @@ def make_qk_desc(n_seq: int, seq_len: int, n_q_heads: int, n_k_heads: int, head_
                  rot_dim: Optional[int] = None, ld_q: Optional[int] = None, ld_k: Optional[int] = None,
                  ld_q_out: Optional[int] = None, ld_k_out: Optional[int] = None, ld_dq: Optional[int] = None,
                  ld_dk: Optional[int] = None, eps: float = 1e-6, flags: int = 0) -> QkDesc:
+    _fits(flags, n_seq=n_seq, seq_len=seq_len, n_q_heads=n_q_heads, n_k_heads=n_k_heads, head_dim=head_dim,
+          rot_dim=head_dim if rot_dim is None else rot_dim)
     wq, wk = n_q_heads * head_dim, n_k_heads * head_dim
     pitches = [w if ld is None else ld for w, ld in ((wq, ld_q), (wk, ld_k), (wq, ld_q_out), (wk, ld_k_out), (wq, ld_dq), (wk, ld_dk))]
     return QkDesc(n_seq, seq_len, n_q_heads, n_k_heads, head_dim, head_dim if rot_dim is None else rot_dim, *pitches,
@@ -703,6 +715,7 @@ def make_attn_desc(n_seq: int, seq_len: int, n_heads: int, n_kv_heads: int, head
                    ld_v: Optional[int] = None, ld_out: Optional[int] = None, ld_dout: Optional[int] = None,
                    ld_dq: Optional[int] = None, ld_dk: Optional[int] = None, ld_dv: Optional[int] = None,
                    dtype: torch.dtype = torch.bfloat16, flags: int = 0) -> AttnDesc:
+    _fits(flags, n_seq=n_seq, seq_len=seq_len, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, window=window)
     wq, wk = n_heads * head_dim, n_kv_heads * head_dim
     pitches = [w if ld is None else ld for w, ld in ((wq, ld_q), (wk, ld_k), (wk, ld_v), (wq, ld_out), (wq, ld_dout), (wq, ld_dq),
                                                      (wk, ld_dk), (wk, ld_dv))]

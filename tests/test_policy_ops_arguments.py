@@ -81,3 +81,21 @@ def test_a_changed_vocabulary_reaches_the_call(calls):
         vocab.fill_(want)
         assert rb.embedding_grad(torch.zeros(4, 8), torch.zeros(4, dtype=torch.int32), None, vocab).shape == (want, 8)
         assert calls[-1].vocab == want
+
+
+def test_numbers_beyond_32_bits_are_refused(calls):
+    """A field of the descriptor would keep their low bits: a window of 2^32 + 1 would become 1."""
+    x = _heads()
+    for window in (2 ** 32, 2 ** 32 + 1, 2 ** 31):
+        with pytest.raises(ValueError, match="window"):
+            rb.attention(x, x, x, 2, 3, window=window)
+        with pytest.raises(ValueError, match="window"):
+            rb.attention_grad(x, x, x, x, torch.zeros(12), x, 2, 3, window=window)
+    rb.attention(x, x, x, 2, 3, window=2 ** 31 - 1)
+    assert calls[-1].window == 2 ** 31 - 1
+    big = 2 ** 32 + 2
+    for make in (lambda: rb.make_embed_desc(4, big, 8, BF), lambda: rb.make_embed_desc(4, 5, big, BF), lambda: rb.make_qk_desc(big, 3, 2, 1, 16, BF),
+                 lambda: rb.make_qk_desc(2, 3, 2, 1, 16, BF, big), lambda: rb.make_attn_desc(2, big, 2, 1, 16), lambda: rb.make_attn_desc(2, 3, 2, 1, big),
+                 lambda: rb.make_attn_desc(2, 3, 2, 1, 16, flags=2 ** 32), lambda: rb.make_qk_desc(2, 3, 2, 1, 16, BF, flags=-1)):
+        with pytest.raises(ValueError, match="32 bits"):
+            make()
