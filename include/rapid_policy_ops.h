@@ -136,7 +136,8 @@ typedef struct rapid_attn_desc {
     int64_t ld_dq, ld_dk, ld_dv;  /* of the gradients (ld_dout too: rapid_attention_bwd only)                     */
     int32_t dtype;                /* RAPID_BF16                                                                   */
     uint32_t flags;               /* 0                                                                            */
-    double scale;                 /* factor of the scores, > 0 and finite (1 / sqrt(head_dim) as a rule)          */
+    double scale;                 /* factor of the scores, > 0 (1 / sqrt(head_dim) as a rule); it and its product with log2(e) */
+                                  /* are used as floats and have to be normal ones                                */
 } rapid_attn_desc_t;
 
 /*
@@ -151,7 +152,8 @@ typedef struct rapid_attn_desc {
  *   lse      [n_seq, n_heads, seq_len] float out, natural logarithm, -infinity outside the bounds; may be NULL
  *   stats    may be NULL; only status is meaningful: RAPID_OK, or RAPID_ERR_TIMEOUT when a bounded wait gave up (the
  *            outputs are then unspecified)
- * Rows outside the bounds may hold anything (infinities and NaN too) and influence nothing.  Rows inside must be finite.
+ * Rows outside the bounds may hold anything (infinities and NaN too) and influence nothing.  Rows inside must be finite, and so must be
+ * the scores of pairs that see each other, in float.
  * The products run on the tensor cores in bf16 with float accumulation; scores, maximum and sum of the softmax are float;
  * the probabilities are rounded to bf16 for their product with v (half a step, a relative error of at most 2^-8 each).
  */

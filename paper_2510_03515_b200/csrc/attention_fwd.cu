@@ -15,6 +15,7 @@
 // third and the rest the beginnings and ends of pieces of one to three tiles.  All exponentials are the special-function unit's,
 // whose result for a masked score is exactly zero; one pair in 16 by a polynomial instead, with its result selected to zero there:
 // 293 and 49 us, and 195 against 191 for 64 x 1024, 12 heads of 128.
+#include <float.h>
 #include <math.h>
 
 #include "attention.cuh"
@@ -487,7 +488,10 @@ rapid_status_t check_attn(const rapid_attn_desc_t* d) {
     if (!d || d->n_seq <= 0 || d->seq_len <= 0 || d->n_heads <= 0 || d->n_kv_heads <= 0 || d->head_dim <= 0 || d->window < 0)
         return RAPID_ERR_INVALID_ARG;
     if (d->dtype != RAPID_BF16 || d->flags != 0) return RAPID_ERR_INVALID_ARG;
-    if (d->n_heads % d->n_kv_heads != 0 || !(d->scale > 0.0) || !isfinite(d->scale)) return RAPID_ERR_INVALID_ARG;
+    if (d->n_heads % d->n_kv_heads != 0) return RAPID_ERR_INVALID_ARG;
+    // the kernels' factors; also false for NaN.  A factor of zero would turn the -infinity of a masked score into NaN.
+    const float scale = (float)d->scale, scale_log2 = (float)(d->scale * kLog2eD);
+    if (!(scale >= FLT_MIN && scale_log2 <= FLT_MAX)) return RAPID_ERR_INVALID_ARG;
     const int64_t wq = (int64_t)d->n_heads * d->head_dim, wk = (int64_t)d->n_kv_heads * d->head_dim;
     if (d->ld_q < wq || d->ld_out < wq || d->ld_k < wk || d->ld_v < wk) return RAPID_ERR_INVALID_ARG;
     if (d->head_dim % 8 != 0 || d->head_dim > 128) return RAPID_ERR_UNSUPPORTED;
