@@ -411,6 +411,11 @@ def _mask8(mask: Optional[torch.Tensor], n: int) -> Optional[torch.Tensor]:
     return mask
 
 
+def _stats_room(stats: Optional[torch.Tensor]) -> None:
+    if stats is not None and (stats.numel() * stats.element_size() < STATS_BYTES or not stats.is_contiguous() or stats.data_ptr() % 8):
+        raise ValueError(f"stats: {STATS_BYTES} bytes side by side on an 8-byte boundary expected (alloc_stats)")
+
+
 def _pitch(t: torch.Tensor, name: str) -> int:
     """Row pitch of a matrix [rows, cols] or of rows of heads [rows, heads, head_dim]."""
     shape, stride = t.shape, t.stride()
@@ -561,6 +566,7 @@ def embedding(table: torch.Tensor, tokens: torch.Tensor, mask: Optional[torch.Te
     T, (V, D) = tokens.numel(), table.shape
     mask = _mask8(mask, T)
     _vector(tokens, T, torch.int32, "tokens")
+    _stats_room(stats)
     dev = _one_device(table, tokens, mask, stats)
     with _on(dev):
         out = _matrix(T, D, table.dtype, table)
@@ -741,13 +747,14 @@ def rapid_attention_bwd(desc: AttnDesc, q: torch.Tensor, k: torch.Tensor, v: tor
         _addr(stats), _addr(workspace), workspace.numel(), _stream_here()), "rapid_attention_bwd")
 
 
-def _attn_args(q, k, v, n_seq, seq_len, bounds):
+def _attn_args(q, k, v, n_seq, seq_len, bounds, stats):
     T = n_seq * seq_len
     if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or q.shape[0] != T or k.shape[0] != T or q.shape[2] != k.shape[2]:
         raise ValueError("q: [n_seq * seq_len, heads, head_dim], k, v: [n_seq * seq_len, kv_heads, head_dim] expected")
     if not q.dtype == k.dtype == v.dtype == torch.bfloat16:
         raise TypeError("q, k and v must be bfloat16")
     _vector(bounds, 2 * n_seq, torch.int32, "bounds")
+    _stats_room(stats)
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_seq: int, seq_len: int, bounds: Optional[torch.Tensor] = None,
@@ -756,7 +763,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_seq: int, seq
     projection); bounds [n_seq, 2] int32 gives each generation's live positions.  Returns out [T, H, D] and lse
     [n_seq, H, seq_len] float32.  The default scale is D ** -0.5."""
     n_seq, seq_len, window, scale = _int(n_seq), _int(seq_len), _int(window), None if scale is None else _float(scale)
-    _attn_args(q, k, v, n_seq, seq_len, bounds)
+    _attn_args(q, k, v, n_seq, seq_len, bounds, stats)
     dev = _one_device(q, k, v, bounds, stats)
     with _on(dev):
         out = _new(q)
@@ -784,7 +791,7 @@ def attention_grad(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch
     """The gradient of attention() from its inputs, its outputs out and lse, and the gradient of out.  dq, dk and dv may be
     given (slices of the gradient of one projection, say)."""
     n_seq, seq_len, window, scale = _int(n_seq), _int(seq_len), _int(window), None if scale is None else _float(scale)
-    _attn_args(q, k, v, n_seq, seq_len, bounds)
+    _attn_args(q, k, v, n_seq, seq_len, bounds, stats)
     if out.shape != q.shape or dout.shape != q.shape:
         raise ValueError("out, dout: the shape of q expected")
     if not out.dtype == dout.dtype == torch.bfloat16:

@@ -99,3 +99,17 @@ def test_numbers_beyond_32_bits_are_refused(calls):
                  lambda: rb.make_attn_desc(2, 3, 2, 1, 16, flags=2 ** 32), lambda: rb.make_qk_desc(2, 3, 2, 1, 16, BF, flags=-1)):
         with pytest.raises(ValueError, match="32 bits"):
             make()
+
+
+@pytest.mark.parametrize("stats", [torch.zeros(rb.STATS_BYTES - 1, dtype=torch.uint8), torch.zeros(0, dtype=torch.uint8),
+                                   torch.zeros(2 * rb.STATS_BYTES, dtype=torch.uint8)[::2], torch.zeros(rb.STATS_BYTES + 8, dtype=torch.uint8)[4:],
+                                   torch.zeros(rb.STATS_BYTES // 8 - 1, dtype=torch.int64)])
+def test_stats_that_are_no_stats_are_refused(calls, stats):
+    """Too short, with gaps, or off an 8-byte boundary: the kernels write STATS_BYTES bytes with 8-byte accesses."""
+    x = _heads()
+    for call in (lambda s: rb.embedding(torch.zeros(5, 8), torch.zeros(4, dtype=torch.int32), stats=s), lambda s: rb.attention(x, x, x, 2, 3, stats=s),
+                 lambda s: rb.attention_grad(x, x, x, x, torch.zeros(12), x, 2, 3, stats=s)):
+        with pytest.raises(ValueError, match="stats"):
+            call(stats)
+        call(rb.alloc_stats("cpu"))
+    assert len(calls) == 3
