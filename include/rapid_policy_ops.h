@@ -12,6 +12,8 @@
  * the first launch and returned as a status; what only the device can see never traps.  Calls that use one workspace must
  * not overlap on the device.  No result depends on the order in which blocks run: the same inputs give the same bits.
  *
+ * Arrays of int32 and float lie on 4-byte boundaries, stats on 8-byte ones, matrices and pitches as each operator says.
+ *
  * Rows are those of the padded token grid: row r = n * seq_len + t is position t of generation n.
  */
 #ifndef RAPID_POLICY_OPS_H

@@ -969,6 +969,7 @@ extern "C" rapid_status_t rapid_attention_bwd(const rapid_attn_desc_t* desc, con
         if (!policy::aligned(p, 16)) return RAPID_ERR_ALIGNMENT;
     for (const void* p : grads)
         if (!policy::aligned(p, 16)) return RAPID_ERR_ALIGNMENT;
+    if (!policy::aligned(bounds, 4) || !policy::aligned(lse, 4) || !policy::aligned(stats, 8)) return RAPID_ERR_ALIGNMENT;
     const int64_t T = (int64_t)d.n_seq * d.seq_len, wq = (int64_t)d.n_heads * d.head_dim, wk = (int64_t)d.n_kv_heads * d.head_dim;
     const int64_t in_w[5] = {wq, wk, wk, wq, wq}, in_ld[5] = {d.ld_q, d.ld_k, d.ld_v, d.ld_out, d.ld_dout};
     const int64_t g_w[3] = {wq, wk, wk}, g_ld[3] = {d.ld_dq, d.ld_dk, d.ld_dv};

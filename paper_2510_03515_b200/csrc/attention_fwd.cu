@@ -556,7 +556,8 @@ extern "C" rapid_status_t rapid_attention_fwd(const rapid_attn_desc_t* desc, con
     if (s != RAPID_OK) return s;
     const rapid_attn_desc_t& d = *desc;
     if (!q || !k || !v || !out) return RAPID_ERR_INVALID_ARG;
-    if (!policy::aligned(q, 16) || !policy::aligned(k, 16) || !policy::aligned(v, 16) || !policy::aligned(out, 16))
+    if (!policy::aligned(q, 16) || !policy::aligned(k, 16) || !policy::aligned(v, 16) || !policy::aligned(out, 16) ||
+        !policy::aligned(bounds, 4) || !policy::aligned(lse, 4) || !policy::aligned(stats, 8))
         return RAPID_ERR_ALIGNMENT;
     const int64_t T = (int64_t)d.n_seq * d.seq_len, wq = (int64_t)d.n_heads * d.head_dim, wk = (int64_t)d.n_kv_heads * d.head_dim;
     if (policy::rows_overlap(out, wq, d.ld_out, q, wq, d.ld_q, T, 2) || policy::rows_overlap(out, wq, d.ld_out, k, wk, d.ld_k, T, 2) ||

@@ -643,7 +643,7 @@ extern "C" rapid_status_t rapid_embedding_fwd(const rapid_embed_desc_t* desc, co
     rapid_status_t s = check_embed(desc, false);
     if (s != RAPID_OK) return s;
     if (!tokens || !table || !out) return RAPID_ERR_INVALID_ARG;
-    if (!aligned(table, 16) || !aligned(out, 16) || !aligned(tokens, 4)) return RAPID_ERR_ALIGNMENT;
+    if (!aligned(table, 16) || !aligned(out, 16) || !aligned(tokens, 4) || !aligned(stats, 8)) return RAPID_ERR_ALIGNMENT;
     const rapid_embed_desc_t& d = *desc;
     const size_t es = elem_size(d.dtype);
     if (overlap(table, extent(d.vocab, d.dim, d.ld_table, es), out, extent(d.n_rows, d.dim, d.ld_rows, es))) return RAPID_ERR_INVALID_ARG;

@@ -583,7 +583,9 @@ extern "C" rapid_status_t rapid_qk_norm_rope_fwd(const rapid_qk_desc_t* desc, co
     const rapid_qk_desc_t& d = *desc;
     if (!q || !k || !inv_freq || !q_out || !k_out) return RAPID_ERR_INVALID_ARG;
     if (!(d.flags & RAPID_QK_NO_NORM) && (!q_weight || !k_weight)) return RAPID_ERR_INVALID_ARG;
-    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_out, 16) || !aligned(k_out, 16)) return RAPID_ERR_ALIGNMENT;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_out, 16) || !aligned(k_out, 16) || !aligned(inv_freq, 4) || !aligned(positions, 4))
+        return RAPID_ERR_ALIGNMENT;
+    if (!(d.flags & RAPID_QK_NO_NORM) && (!aligned(q_weight, 4) || !aligned(k_weight, 4))) return RAPID_ERR_ALIGNMENT;
     const int64_t n = (int64_t)d.n_seq * d.seq_len, wq = (int64_t)d.n_q_heads * d.head_dim, wk = (int64_t)d.n_k_heads * d.head_dim;
     const size_t es = elem_size(d.dtype);
     const bool q_in_place = q == q_out && d.ld_q == d.ld_q_out, k_in_place = k == k_out && d.ld_k == d.ld_k_out;
@@ -623,8 +625,10 @@ extern "C" rapid_status_t rapid_qk_norm_rope_bwd(const rapid_qk_desc_t* desc, co
     const bool norm = !(d.flags & RAPID_QK_NO_NORM);
     if (!q || !k || !inv_freq || !dq_out || !dk_out || !dq || !dk) return RAPID_ERR_INVALID_ARG;
     if (norm && (!q_weight || !k_weight || !dq_weight || !dk_weight)) return RAPID_ERR_INVALID_ARG;
-    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(dq_out, 16) || !aligned(dk_out, 16) || !aligned(dq, 16) || !aligned(dk, 16))
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(dq_out, 16) || !aligned(dk_out, 16) || !aligned(dq, 16) || !aligned(dk, 16) ||
+        !aligned(inv_freq, 4) || !aligned(positions, 4))
         return RAPID_ERR_ALIGNMENT;
+    if (norm && (!aligned(q_weight, 4) || !aligned(k_weight, 4) || !aligned(dq_weight, 4) || !aligned(dk_weight, 4))) return RAPID_ERR_ALIGNMENT;
     const int64_t n = (int64_t)d.n_seq * d.seq_len, wq = (int64_t)d.n_q_heads * d.head_dim, wk = (int64_t)d.n_k_heads * d.head_dim;
     const size_t es = elem_size(d.dtype);
     const bool q_in_place = dq == dq_out && d.ld_dq == d.ld_q_out, k_in_place = dk == dk_out && d.ld_dk == d.ld_k_out;

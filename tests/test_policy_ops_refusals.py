@@ -1,6 +1,8 @@
 """Policy-network operators, host side: calls whose numbers or addresses the kernels could not work with are refused before anything is
 enqueued (no GPU needed; what is accepted stops at the missing device)."""
 
+import ctypes as C
+
 import pytest
 import torch
 
@@ -31,3 +33,31 @@ def test_a_scale_that_is_no_float_is_refused(call, scale):
 @pytest.mark.parametrize("scale", [FLT_MAX / 1.45, FLT_MIN, 1.0, 64 ** -0.5])
 def test_any_other_scale_is_accepted(call, scale):
     assert call(_attn(scale=scale)) == rb.RAPID_ERR_CUDA
+
+
+# ---- arrays of numbers and stats off their boundaries ------------------------------------------------------------
+
+ODD = base.FAKE + base.FAR // 2 + 2
+
+
+@pytest.mark.parametrize("call,names", [(base._qk_fwd, ["qw", "kw", "freq", "pos"]), (base._qk_bwd, ["qw", "kw", "freq", "pos", "dqw", "dkw"])])
+def test_qk_arrays_off_a_boundary_are_refused(call, names):
+    d = rb.make_qk_desc(4, 8, 4, 2, 64, base.BF)
+    for name in names:
+        assert call(d, **{name: ODD}) == base.ALIGN, name
+
+
+@pytest.mark.parametrize("call", ATTENTION)
+def test_attention_arrays_off_a_boundary_are_refused(call):
+    for name in ("bounds", "lse"):
+        assert call(_attn(), **{name: ODD}) == base.ALIGN, name
+
+
+def test_stats_off_a_boundary_are_refused():
+    stats = base.FAKE + 90 * base.FAR + 4
+    a = base._args(["tokens", "mask", "table", "out"])
+    assert rb.lib().rapid_embedding_fwd(C.byref(rb.make_embed_desc(8, 100, 16, base.BF)), *a, stats, None) == base.ALIGN
+    a = base._args(["q", "k", "v", "bounds", "out", "lse"])
+    assert rb.lib().rapid_attention_fwd(C.byref(_attn()), *a, stats, None) == base.ALIGN
+    a = base._args(["q", "k", "v", "bounds", "out", "lse", "dout", "dq", "dk", "dv"])
+    assert rb.lib().rapid_attention_bwd(C.byref(_attn()), *a, stats, base.FAKE + 80 * base.FAR, 1 << 50, None) == base.ALIGN
