@@ -162,7 +162,10 @@ typedef struct rapid_attn_desc {
 rapid_status_t rapid_attention_fwd(const rapid_attn_desc_t* desc, const void* q, const void* k, const void* v,
                                    const int32_t* bounds, void* out, float* lse, rapid_stats_t* stats, void* stream);
 
-/* Scratch of rapid_attention_bwd: two floats for each row and head. */
+/*
+ * Scratch of rapid_attention_bwd: two floats for each head and position of the tiles, which are 128 positions of one generation or, where
+ * generations have at most 64 positions, as many whole generations as fit; each of the two arrays in whole 8 KB.
+ */
 rapid_status_t rapid_attention_bwd_workspace_bytes(const rapid_attn_desc_t* desc, size_t* bytes);
 
 /*

@@ -932,8 +932,17 @@ rapid_status_t check_attn_bwd(const rapid_attn_desc_t* d) {
     return RAPID_OK;
 }
 
-size_t row_terms(const rapid_attn_desc_t& d) {  // floats of one of the two arrays
-    return (size_t)((d.seq_len + kTile - 1) / kTile) * kTile * (size_t)d.n_seq * (size_t)d.n_heads;
+// Floats of one of the two arrays: what the larger share needs (they follow one another), in whole 8 KB.
+size_t row_terms(const rapid_attn_desc_t& d) {
+    Share shares[2];
+    const int count = make_shares(d, nullptr, shares);
+    size_t most = 0;
+    for (int i = 0; i < count; ++i) {
+        const rapid_attn_desc_t& s = shares[i].d;
+        const size_t floats = (size_t)((s.seq_len + kTile - 1) / kTile) * kTile * (size_t)s.n_seq * (size_t)s.n_heads;
+        most = floats > most ? floats : most;
+    }
+    return align_up(most, 2048);
 }
 
 }  // namespace

@@ -61,3 +61,24 @@ def test_stats_off_a_boundary_are_refused():
     assert rb.lib().rapid_attention_fwd(C.byref(_attn()), *a, stats, None) == base.ALIGN
     a = base._args(["q", "k", "v", "bounds", "out", "lse", "dout", "dq", "dk", "dv"])
     assert rb.lib().rapid_attention_bwd(C.byref(_attn()), *a, stats, base.FAKE + 80 * base.FAR, 1 << 50, None) == base.ALIGN
+
+
+# ---- scratch of the attention gradient -----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n,length,heads", [(65536, 1, 12), (4877, 8, 9), (1335, 40, 2), (1000, 64, 3), (300, 43, 4), (129, 1, 2), (7, 60, 12)])
+def test_scratch_follows_the_rows_of_short_generations(n, length, heads):
+    """Generations that share a tile share its scratch: at most half of a tile's places are empty, the last tile's aside."""
+    got = rb.rapid_attention_bwd_workspace_bytes(rb.make_attn_desc(n, length, heads, 1, 64))
+    assert got <= 2 * 4 * heads * (2 * n * length + 128) + 2 * 8192
+    # the generations that fill whole tiles at the least; those of the last tile come after them, in the same place
+    parts = min(128 // length, n)
+    assert got >= 2 * 4 * heads * (n // parts * parts) * length
+
+
+@pytest.mark.parametrize("n,length,heads", [(64, 1024, 12), (3, 4095, 16), (5, 65, 3), (1, 64, 1), (2, 127, 8)])
+def test_scratch_of_longer_generations(n, length, heads):
+    got = rb.rapid_attention_bwd_workspace_bytes(rb.make_attn_desc(n, length, heads, 1, 64))
+    need = 2 * 4 * heads * n * (-(-length // 128) * 128)
+    assert need <= got <= need + 2 * 8192
+    d = rb.make_attn_desc(n, length, heads, 1, 64)
+    assert base._attn_bwd(d, ws_bytes=got - 1) == base.WORK
