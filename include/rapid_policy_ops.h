@@ -175,6 +175,7 @@ rapid_status_t rapid_attention_bwd_workspace_bytes(const rapid_attn_desc_t* desc
  * share a key head).  Rows outside the bounds are written as zeros and read from nowhere.  p and ds are rounded to bf16 for
  * the last three products; the sums are float, each gradient is rounded once.
  *   dout [T, ld_dout], dq [T, ld_dq], dk [T, ld_dk], dv [T, ld_dv] bf16;  workspace 256-byte aligned
+ * Refused (RAPID_ERR_UNSUPPORTED): more than 2^20 pairs of a query tile of 128 positions that sees one key and a head that shares it.
  */
 rapid_status_t rapid_attention_bwd(const rapid_attn_desc_t* desc, const void* q, const void* k, const void* v,
                                    const int32_t* bounds, const void* out, const float* lse, const void* dout, void* dq,

@@ -929,6 +929,10 @@ rapid_status_t check_attn_bwd(const rapid_attn_desc_t* d) {
     if (d->ld_dout % 8 || d->ld_dq % 8 || d->ld_dk % 8 || d->ld_dv % 8) return RAPID_ERR_ALIGNMENT;
     const int64_t most = (1ll << 38) / d->seq_len < (1ll << 31) ? (1ll << 38) / d->seq_len : (1ll << 31);
     if (d->ld_dout > most || d->ld_dq > most || d->ld_dk > most || d->ld_dv > most) return RAPID_ERR_UNSUPPORTED;
+    // A piece of dK, dV is one key tile's walk over the query tiles that see it, for all heads of its group.  A warp that has no dead
+    // rows to clear in it waits for the next piece meanwhile; 2^20 steps of 1.5 us (2.3 at 1.3 GHz) stay below that wait's limit.
+    const int64_t tiles = (d->seq_len + kTile - 1) / kTile, in_window = d->window ? ((int64_t)d->window + kTile - 2) / kTile + 1 : tiles;
+    if ((in_window < tiles ? in_window : tiles) * (d->n_heads / d->n_kv_heads) > (1 << 20)) return RAPID_ERR_UNSUPPORTED;
     return RAPID_OK;
 }
 

@@ -82,3 +82,25 @@ def test_scratch_of_longer_generations(n, length, heads):
     assert need <= got <= need + 2 * 8192
     d = rb.make_attn_desc(n, length, heads, 1, 64)
     assert base._attn_bwd(d, ws_bytes=got - 1) == base.WORK
+
+
+# ---- work behind one wait --------------------------------------------------------------------------------------------
+
+def _long(length, h, hk, window=0):
+    return rb.make_attn_desc(1, length, h, hk, 8, window)
+
+
+def test_gradients_whose_waits_would_run_out_are_refused():
+    """One key tile's walk over all query tiles and heads of its group takes 1.5 us a step; a warp that has nothing to do in it waits
+    for the next one, at most 4 s."""
+    for d in (_long(1 << 24, 16, 1), _long(1 << 24, 64, 4), _long((1 << 23) + 1, 16, 1), _long(1 << 20, 256, 1), _long(1 << 24, 16, 1, 1 << 23)):
+        assert base._attn_bwd(d) == base.UNSUP
+    with pytest.raises(rb.RapidError):
+        rb.rapid_attention_bwd_workspace_bytes(_long(1 << 24, 16, 1))
+
+
+@base.no_gpu
+def test_long_gradients_with_short_walks_are_accepted():
+    for d in (_long(1 << 23, 16, 1), _long(1 << 24, 16, 2), _long(1 << 24, 16, 1, 4096), _long(1 << 20, 256, 2)):
+        assert base._attn_bwd(d) == rb.RAPID_ERR_CUDA
+    assert base._attn_fwd(_long(1 << 24, 16, 1)) == rb.RAPID_ERR_CUDA
