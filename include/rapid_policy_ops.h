@@ -52,7 +52,8 @@ typedef struct rapid_embed_desc {
  * outside [0, vocab), come out as zeros.
  *   tokens [T] int32;  mask [T] uint8, non-zero = live, NULL = all live;  table [V, ld_table];  out [T, ld_rows]
  *   stats  may be NULL; n_tokens = live rows with a valid token, n_bad_token = live rows with another; the rest zero
- * Row pitches are multiples of 16 bytes and bases are 16-byte aligned; columns >= dim are neither read nor written.
+ * Row pitches are multiples of 16 bytes and bases are 16-byte aligned; columns >= dim are neither read nor written, so matrices of
+ * one pitch (in bytes) may lie side by side in the same rows.  Other matrices have to be apart altogether.
  */
 rapid_status_t rapid_embedding_fwd(const rapid_embed_desc_t* desc, const int32_t* tokens, const uint8_t* mask,
                                    const void* table, void* out, rapid_stats_t* stats, void* stream);

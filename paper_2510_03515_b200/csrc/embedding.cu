@@ -645,8 +645,8 @@ extern "C" rapid_status_t rapid_embedding_fwd(const rapid_embed_desc_t* desc, co
     if (!tokens || !table || !out) return RAPID_ERR_INVALID_ARG;
     if (!aligned(table, 16) || !aligned(out, 16) || !aligned(tokens, 4) || !aligned(stats, 8)) return RAPID_ERR_ALIGNMENT;
     const rapid_embed_desc_t& d = *desc;
-    const size_t es = elem_size(d.dtype);
-    if (overlap(table, extent(d.vocab, d.dim, d.ld_table, es), out, extent(d.n_rows, d.dim, d.ld_rows, es))) return RAPID_ERR_INVALID_ARG;
+    const int64_t es = (int64_t)elem_size(d.dtype);
+    if (matrices_overlap(table, d.vocab, d.dim * es, d.ld_table * es, out, d.n_rows, d.dim * es, d.ld_rows * es)) return RAPID_ERR_INVALID_ARG;
     const int segs = (d.dim + kFwdSeg - 1) / kFwdSeg;
     unsigned grid = 0;
     if (!blocks_of_8(d.n_rows * segs, &grid)) return RAPID_ERR_UNSUPPORTED;
@@ -680,8 +680,8 @@ extern "C" rapid_status_t rapid_embedding_bwd(const rapid_embed_desc_t* desc, co
     if (!aligned(dout, 16) || !aligned(dtable, 16) || !aligned(tokens, 4)) return RAPID_ERR_ALIGNMENT;
     const rapid_embed_desc_t& d = *desc;
     const bool grad_bf16 = (d.flags & RAPID_EMBED_DTABLE_BF16) != 0;
-    if (overlap(dout, extent(d.n_rows, d.dim, d.ld_rows, elem_size(d.dtype)), dtable, extent(d.vocab, d.dim, d.ld_table, grad_bf16 ? 2 : 4)))
-        return RAPID_ERR_INVALID_ARG;
+    const int64_t es = (int64_t)elem_size(d.dtype), gs = grad_bf16 ? 2 : 4;
+    if (matrices_overlap(dout, d.n_rows, d.dim * es, d.ld_rows * es, dtable, d.vocab, d.dim * gs, d.ld_table * gs)) return RAPID_ERR_INVALID_ARG;
     if (!workspace || !aligned(workspace, 256)) return RAPID_ERR_WORKSPACE;
     EmbedScratch w;
     if (workspace_bytes < carve_embed(d, workspace, &w)) return RAPID_ERR_WORKSPACE;

@@ -24,15 +24,20 @@ inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 // Bytes from the first element of `n` rows of `width` elements at pitch `ld` to the end of the last.
 inline size_t extent(int64_t n, int64_t width, int64_t ld, size_t es) { return ((size_t)(n - 1) * ld + width) * es; }
 
-// Rows of `width` elements at pitch `ld`: do the two matrices share an element?  Matrices of one pitch may lie side by
-// side in the same rows (queries, keys and values of one projection); of two pitches, they have to be apart altogether.
+// Two matrices of `na` and `nb` rows, `wa` and `wb` bytes wide, at pitches of `pa` and `pb` bytes: do they share a byte?  Matrices of
+// one pitch may lie side by side in the same rows (queries, keys and values of one projection); of two pitches, they have to be
+// apart altogether.
+inline bool matrices_overlap(const void* a, int64_t na, int64_t wa, int64_t pa, const void* b, int64_t nb, int64_t wb, int64_t pb) {
+    if (!overlap(a, extent(na, wa, pa, 1), b, extent(nb, wb, pb, 1))) return false;
+    if (pa != pb) return true;
+    int64_t off = ((int64_t)reinterpret_cast<uintptr_t>(b) - (int64_t)reinterpret_cast<uintptr_t>(a)) % pa;
+    if (off < 0) off += pa;
+    return off < wa || off + wb > pa;
+}
+// The same for `n` rows each, widths and pitches in elements of `es` bytes.
 inline bool rows_overlap(const void* a, int64_t wa, int64_t lda, const void* b, int64_t wb, int64_t ldb, int64_t n, size_t es) {
-    if (!overlap(a, extent(n, wa, lda, es), b, extent(n, wb, ldb, es))) return false;
-    if (lda != ldb) return true;
-    const int64_t pitch = lda * (int64_t)es;
-    int64_t off = ((int64_t)reinterpret_cast<uintptr_t>(b) - (int64_t)reinterpret_cast<uintptr_t>(a)) % pitch;
-    if (off < 0) off += pitch;
-    return off < wa * (int64_t)es || off + wb * (int64_t)es > pitch;
+    const int64_t e = (int64_t)es;
+    return matrices_overlap(a, n, wa * e, lda * e, b, n, wb * e, ldb * e);
 }
 
 // sm_100 only.  Returns the SM count of the current device through *sm_count.

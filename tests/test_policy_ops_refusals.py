@@ -104,3 +104,31 @@ def test_long_gradients_with_short_walks_are_accepted():
     for d in (_long(1 << 23, 16, 1), _long(1 << 24, 16, 2), _long(1 << 24, 16, 1, 4096), _long(1 << 20, 256, 2)):
         assert base._attn_bwd(d) == rb.RAPID_ERR_CUDA
     assert base._attn_fwd(_long(1 << 24, 16, 1)) == rb.RAPID_ERR_CUDA
+
+
+# ---- embedding matrices side by side in the same rows ------------------------------------------------------------------
+
+@base.no_gpu
+@pytest.mark.parametrize("n,v", [(8, 100), (100, 8), (1, 100), (100, 1)])
+def test_embedding_matrices_may_share_rows(n, v):
+    """Column slices of one matrix: table and out, or dout and a bf16 dtable."""
+    d = rb.make_embed_desc(n, v, 16, base.BF, 48, 48)
+    assert base._embed_fwd(d, table=base.FAKE, out=base.FAKE + 32) == rb.RAPID_ERR_CUDA
+    assert base._embed_fwd(d, table=base.FAKE + 64, out=base.FAKE) == rb.RAPID_ERR_CUDA
+    d = rb.make_embed_desc(n, v, 16, base.BF, 48, 48, flags=rb.EMBED_DTABLE_BF16)
+    assert base._embed_bwd(d, dout=base.FAKE + 32, dtable=base.FAKE) == rb.RAPID_ERR_CUDA
+    # float columns beside bf16 ones, 160 bytes a row both ways
+    d = rb.make_embed_desc(n, v, 16, base.BF, 40, 80)
+    assert base._embed_bwd(d, dout=base.FAKE + 64, dtable=base.FAKE) == rb.RAPID_ERR_CUDA
+
+
+@pytest.mark.parametrize("n,v", [(8, 100), (100, 8)])
+def test_embedding_matrices_that_share_elements_are_refused(n, v):
+    d = rb.make_embed_desc(n, v, 16, base.BF, 48, 48)
+    for off in (0, 16, 80):  # the last: into the next row's first columns
+        assert base._embed_fwd(d, table=base.FAKE, out=base.FAKE + off) == base.INVALID, off
+        assert base._embed_fwd(d, table=base.FAKE + off, out=base.FAKE) == base.INVALID, off
+    d = rb.make_embed_desc(n, v, 16, base.BF, 48, 56, flags=rb.EMBED_DTABLE_BF16)  # other pitches: apart altogether
+    assert base._embed_bwd(d, dout=base.FAKE + 32, dtable=base.FAKE) == base.INVALID
+    d = rb.make_embed_desc(n, v, 16, base.BF, 48, 96)
+    assert base._embed_bwd(d, dout=base.FAKE + 48, dtable=base.FAKE) == base.INVALID
