@@ -567,7 +567,7 @@ rapid_status_t check_embed(const rapid_embed_desc_t* d, bool bwd) {
     if (!isfinite(d->scale) || d->ld_table < d->dim || d->ld_rows < d->dim) return RAPID_ERR_INVALID_ARG;
     if (d->n_rows > 0x7fffffffll || d->vocab > (1 << 27) - 2 || d->dim > (1 << 24)) return RAPID_ERR_UNSUPPORTED;
     // far beyond any device's memory; keeps every size below in 64 bits
-    if (d->ld_table > (1ll << 32) || d->ld_rows > (1ll << 32)) return RAPID_ERR_UNSUPPORTED;
+    if (d->ld_table > (1ll << 56) / d->vocab || d->ld_rows > (1ll << 56) / d->n_rows) return RAPID_ERR_UNSUPPORTED;
     const size_t rows = elem_size(d->dtype);
     const size_t table = !bwd ? rows : (d->flags & RAPID_EMBED_DTABLE_BF16) ? 2 : 4;
     if ((size_t)d->ld_rows * rows % 16 != 0 || (size_t)d->ld_table * table % 16 != 0) return RAPID_ERR_ALIGNMENT;

@@ -495,7 +495,8 @@ rapid_status_t check_qk(const rapid_qk_desc_t* d, bool bwd) {
     if ((int64_t)d->n_seq * d->seq_len > 0x7fffffffll) return RAPID_ERR_UNSUPPORTED;
     const int64_t wq = (int64_t)d->n_q_heads * d->head_dim, wk = (int64_t)d->n_k_heads * d->head_dim;
     if (d->ld_q < wq || d->ld_q_out < wq || d->ld_k < wk || d->ld_k_out < wk) return RAPID_ERR_INVALID_ARG;
-    const int64_t most = 1ll << 31;
+    // far beyond any device's memory; keeps every size below in 64 bits
+    const int64_t rows = (int64_t)d->n_seq * d->seq_len, most = (1ll << 56) / rows < (1ll << 31) ? (1ll << 56) / rows : 1ll << 31;
     if (d->ld_q > most || d->ld_k > most || d->ld_q_out > most || d->ld_k_out > most) return RAPID_ERR_UNSUPPORTED;
     const int64_t unit = 16 / (int64_t)elem_size(d->dtype);
     if (d->ld_q % unit || d->ld_k % unit || d->ld_q_out % unit || d->ld_k_out % unit) return RAPID_ERR_ALIGNMENT;

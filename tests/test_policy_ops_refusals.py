@@ -132,3 +132,19 @@ def test_embedding_matrices_that_share_elements_are_refused(n, v):
     assert base._embed_bwd(d, dout=base.FAKE + 32, dtable=base.FAKE) == base.INVALID
     d = rb.make_embed_desc(n, v, 16, base.BF, 48, 96)
     assert base._embed_bwd(d, dout=base.FAKE + 48, dtable=base.FAKE) == base.INVALID
+
+
+# ---- sizes beyond 64 bits ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("call", [base._embed_fwd, base._embed_bwd])
+def test_embedding_matrices_beyond_any_memory_are_refused(call):
+    """2^31 rows of 2^32 floats are 2^65 bytes; the overlap checks count bytes in 64 bits."""
+    for d in (rb.make_embed_desc(2 ** 31 - 1, 5, 8, torch.float32, 8, 2 ** 32), rb.make_embed_desc(2 ** 31 - 1, 5, 8, base.BF, 8, 2 ** 32),
+              rb.make_embed_desc(1, 2 ** 27 - 2, 8, torch.float32, 2 ** 32, 8)):
+        assert call(d) == base.UNSUP
+
+
+@pytest.mark.parametrize("call", [base._qk_fwd, base._qk_bwd])
+def test_qk_matrices_beyond_any_memory_are_refused(call):
+    for name in ("ld_q", "ld_k", "ld_q_out", "ld_k_out") + (("ld_dq", "ld_dk") if call is base._qk_bwd else ()):
+        assert call(rb.make_qk_desc(2 ** 31 - 1, 1, 1, 1, 16, torch.float32, **{name: 2 ** 31})) == base.UNSUP, name
