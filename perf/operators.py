@@ -214,7 +214,8 @@ def _own(s, c):
         return r.dq, r.dk, r.dq_weight, r.dk_weight
     if op == "attn_fwd":
         return rb.attention(s["q"], s["k"], s["v"], c["n_seq"], c["seq_len"], bounds=s["bounds"], window=c["window"])
-    r = rb.attention_grad(s["q"], s["k"], s["v"], s["out"], s["lse"], s["dout"], c["n_seq"], c["seq_len"], bounds=s["bounds"],
+    # with one generation the plain forward pass leaves out head by head; a row's heads have to lie side by side
+    r = rb.attention_grad(s["q"], s["k"], s["v"], s["out"].contiguous(), s["lse"], s["dout"], c["n_seq"], c["seq_len"], bounds=s["bounds"],
                           window=c["window"])
     return r.dq, r.dk, r.dv
 
