@@ -62,10 +62,13 @@ rapid_status_t rapid_embedding_fwd(const rapid_embed_desc_t* desc, const int32_t
 rapid_status_t rapid_embedding_bwd_workspace_bytes(const rapid_embed_desc_t* desc, size_t* bytes);
 
 /*
- * dtable[v, :] (+)= s * sum of dout[r, :] over the live rows r with tokens[r] == v.  The rows are sorted by token (stable)
- * and summed in row order in float, in pieces of 32 whose sums are added in order.  Masked rows of dout, and rows with a
- * token outside [0, vocab), are never read.  Without RAPID_EMBED_ACCUMULATE every row of dtable is written (zeros where a
- * token does not occur).
+ * dtable[v, :] (+)= s * sum of dout[r, :] over the live rows r with tokens[r] == v, summed in float.  The order of the additions
+ * is fixed by tokens and mask: the rows are sorted by token (stable); a token with at most 8 rows has them added in row order; of
+ * another, whole pieces (sorted positions 32 j .. 32 j + 31) are summed in row order first, then seven runs each add a seventh of the
+ * rows before the first whole piece, of those behind the last one, and of the pieces, and the seven sums are added in order.
+ * Where a piece begins depends on the rows of smaller tokens, so they can change a sum's last bits.  Masked rows of dout, and
+ * rows with a token outside [0, vocab), are never read.  Without RAPID_EMBED_ACCUMULATE every row of dtable is written (zeros
+ * where a token does not occur).
  *   dtable [V, ld_table] float (bf16 with RAPID_EMBED_DTABLE_BF16);  workspace 256-byte aligned
  */
 rapid_status_t rapid_embedding_bwd(const rapid_embed_desc_t* desc, const int32_t* tokens, const uint8_t* mask,
@@ -154,7 +157,7 @@ typedef struct rapid_attn_desc {
  *   out      rows outside the bounds are written as zeros
  *   lse      [n_seq, n_heads, seq_len] float out, natural logarithm, -infinity outside the bounds; may be NULL
  *   stats    may be NULL; only status is meaningful: RAPID_OK, or RAPID_ERR_TIMEOUT when a bounded wait gave up (the
- *            outputs are then unspecified)
+ *            outputs are then unspecified).  Nothing else reports that: without stats a call that gave up looks like any other
  * Rows outside the bounds may hold anything (infinities and NaN too) and influence nothing.  Rows inside must be finite, and so must be
  * the scores of pairs that see each other, in float.
  * The products run on the tensor cores in bf16 with float accumulation; scores, maximum and sum of the softmax are float;

@@ -761,7 +761,8 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_seq: int, seq
               window: int = 0, scale: Optional[float] = None, stats: Optional[torch.Tensor] = None):
     """Causal attention over the padded token grid, q [T, H, D], k and v [T, Hk, D] bfloat16 (rows may be slices of one
     projection); bounds [n_seq, 2] int32 gives each generation's live positions.  Returns out [T, H, D] and lse
-    [n_seq, H, seq_len] float32.  The default scale is D ** -0.5."""
+    [n_seq, H, seq_len] float32.  The default scale is D ** -0.5.  A wait that gives up is reported in stats (alloc_stats, read_stats)
+    and nowhere else."""
     n_seq, seq_len, window, scale = _int(n_seq), _int(seq_len), _int(window), None if scale is None else _float(scale)
     _attn_args(q, k, v, n_seq, seq_len, bounds, stats)
     dev = _one_device(q, k, v, bounds, stats)
@@ -789,7 +790,7 @@ def attention_grad(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch
                    stats: Optional[torch.Tensor] = None, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
                    dv: Optional[torch.Tensor] = None) -> AttnGrads:
     """The gradient of attention() from its inputs, its outputs out and lse, and the gradient of out.  dq, dk and dv may be
-    given (slices of the gradient of one projection, say)."""
+    given (slices of the gradient of one projection, say).  stats as in attention()."""
     n_seq, seq_len, window, scale = _int(n_seq), _int(seq_len), _int(window), None if scale is None else _float(scale)
     _attn_args(q, k, v, n_seq, seq_len, bounds, stats)
     if out.shape != q.shape or dout.shape != q.shape:

@@ -12,10 +12,12 @@
 // and hardly an instruction, while the other warps sum.
 //
 // Measured: 64 x 1024 tokens x 1536 bf16, over a third of them masked: forward 43 us (5.7 TB/s).  Gradient into 151936 rows of float:
-// 434 us with a warp a token and segment, 299 with the radix sort's wide digits, 248 with frequent tokens summed by blocks
-// , and the others a whole row at a time, 244 (4.3 TB/s) with the sort's loads issued ahead; its last kernel takes 200 of them,
-// the sort and the lists before it the rest.  16384 rows of 512 into 32000: 92 us, 53 with the sort over several blocks and
-// narrow rows eight at a time.
+// 434 us with a warp a token and segment, 299 with the radix sort's wide digits, 248 with frequent tokens summed by blocks and
+// the others a whole row at a time, 244 with the sort's loads issued ahead, 240 (4.4 TB/s) now; its last kernel takes 200 of
+// them, the sort and the lists before it the rest.  Into bf16 170, added to a table 154, 256 x 1024 rows of 512 172, 64 x 1024 of
+// 2048 into 128256 276.  16384 rows of 512 into 32000: 92 us, 53 with the sort over several blocks and narrow rows eight at a time.
+// The last kernel holds 48 sums and two rows of 24 registers in the 128 that two blocks an SM leave a thread: it spills 24 of them
+// (bf16 rows; 10 with float rows).
 #include <math.h>
 
 #include "policy_ops.cuh"

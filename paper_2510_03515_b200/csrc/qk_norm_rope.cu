@@ -14,7 +14,9 @@
 // a third of them masked: forward 145 us with a division for each head and one float operation at a time, 114 packed, 99 with
 // the grid walking its tiles, 95 without block barriers, 82 with eight heads in flight and no branches (4.7 TB/s); the
 // gradient 273, 154, 149 and, with queries and keys in blocks of their own, half the weight sums a lane and all groups
-// busy on the keys' few heads, 120 (4.4 TB/s).  Three blocks an SM spill registers: 112 and 200 us.
+// busy on the keys' few heads, 120 (4.4 TB/s).  Three blocks an SM spill registers: 112 and 200 us.  Now 45 % of the issue slots are
+// used, and what the 15 warps of an SM have in flight bounds both.  Float, 16 x 1024: 42 and 68 us; rotation alone, bf16, 64 x 1024: 72
+// and 82.
 #include <math.h>
 
 #include "policy_ops.cuh"
