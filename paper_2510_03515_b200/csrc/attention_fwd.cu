@@ -355,8 +355,9 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 if (!(ok = wait_all(&s_full[w], cnt & 1u, abortp))) break;
                 tc_fence_after();
                 // The items start together; half a tile's time apart, one is at its exponentials while the other waits, loads and
-                // compares (8 x 4096, 16 heads of 64: 314 -> 305 us; short pieces have no time for it).
-                if (w == 1 && j == fw && ew - fw >= 4) {
+                // compares (heads of 64, 8 x 4096: 324 -> 293 us; short pieces have no time for it).  Where P lies over S the order of
+                // the products keeps them apart anyway (heads of 128, 64 x 1024 with the wait 191 us, without 190; 8 x 4096 275 both).
+                if (!kOverlay && w == 1 && j == fw && ew - fw >= 4) {
                     const long long t0 = clock64();
                     while (clock64() - t0 < 900) {}
                 }
