@@ -1,5 +1,5 @@
-"""ctypes binding over librapid_pg.so: same names as the C ABI (include/rapid_pg.h and
-include/rapid_policy_ops.h), argument marshalling only.  Tensors are PyTorch CUDA tensors used purely as device memory; every step of
+"""ctypes binding over librapid_pg.so: same names as the C ABI (include/rapid_pg.h, include/rapid_policy_ops.h and
+include/rapid_losses.h), argument marshalling only.  Tensors are PyTorch CUDA tensors used purely as device memory; every step of
 the computation runs in the library's kernels on torch's current stream.
 
 There is no fallback: if the shared library is missing the first call raises.
@@ -48,6 +48,13 @@ QK_NO_NORM = 1
 QK_UNIT_OFFSET = 2
 QK_INTERLEAVED = 4
 
+LOSS_NORM_SEQ = 1
+LOSS_NORM_GIVEN = 2
+CLIP_ADV_TOKEN = 4
+PREF_HINGE = 16
+PREF_SQUARED = 32
+PREF_TOKEN_MEAN = 64
+
 # every symbol declared in include/
 EXPORTS = (
     "rapid_status_string", "rapid_version", "rapid_workspace_bytes", "rapid_group_advantage",
@@ -57,6 +64,8 @@ EXPORTS = (
     "rapid_embedding_fwd", "rapid_embedding_bwd_workspace_bytes", "rapid_embedding_bwd",
     "rapid_qk_norm_rope_fwd", "rapid_qk_norm_rope_bwd_workspace_bytes", "rapid_qk_norm_rope_bwd",
     "rapid_attention_fwd", "rapid_attention_bwd_workspace_bytes", "rapid_attention_bwd",
+    "rapid_clip_loss_workspace_bytes", "rapid_clip_loss", "rapid_preference_loss_workspace_bytes", "rapid_preference_loss",
+    "rapid_distill_loss_workspace_bytes", "rapid_distill_loss",
 )
 
 
@@ -93,6 +102,29 @@ class AttnDesc(C.Structure):
                 ("head_dim", C.c_int32), ("window", C.c_int32), ("ld_q", C.c_int64), ("ld_k", C.c_int64), ("ld_v", C.c_int64),
                 ("ld_out", C.c_int64), ("ld_dout", C.c_int64), ("ld_dq", C.c_int64), ("ld_dk", C.c_int64),
                 ("ld_dv", C.c_int64), ("dtype", C.c_int32), ("flags", C.c_uint32), ("scale", C.c_double)]
+
+
+class LossStats(C.Structure):
+    _fields_ = [("n_tokens", C.c_int64), ("n_clipped", C.c_int32), ("n_bad", C.c_int32), ("n_pairs", C.c_int32), ("status", C.c_int32),
+                ("mean_log_ratio", C.c_double), ("mean_kl", C.c_double), ("loss", C.c_double)]
+
+
+class ClipDesc(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("seq_len", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32), ("ld", C.c_int64),
+                ("ld_grad", C.c_int64), ("flags", C.c_uint32), ("reserved", C.c_int32), ("eps_low", C.c_double), ("eps_high", C.c_double),
+                ("kl_beta", C.c_double), ("scale", C.c_double), ("norm_z", C.c_double)]
+
+
+class PrefDesc(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("seq_len", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32), ("ld", C.c_int64),
+                ("ld_grad", C.c_int64), ("flags", C.c_uint32), ("n_pairs", C.c_int32), ("beta", C.c_double), ("margin", C.c_double),
+                ("label_smoothing", C.c_double), ("scale", C.c_double), ("norm_z", C.c_double)]
+
+
+class DistillDesc(C.Structure):
+    _fields_ = [("n_rows", C.c_int64), ("vocab", C.c_int32), ("k", C.c_int32), ("ld", C.c_int64), ("ld_grad", C.c_int64),
+                ("ld_top", C.c_int64), ("dtype", C.c_int32), ("flags", C.c_uint32), ("temperature", C.c_double), ("scale", C.c_double),
+                ("norm_z", C.c_double)]
 
 
 class RapidError(RuntimeError):
@@ -153,6 +185,12 @@ def lib():
             "rapid_attention_fwd": [ap] + [vp] * 8,
             "rapid_attention_bwd_workspace_bytes": [ap, C.POINTER(sz)],
             "rapid_attention_bwd": [ap] + [vp] * 12 + [sz, vp],
+            "rapid_clip_loss_workspace_bytes": [C.POINTER(ClipDesc), C.POINTER(sz)],
+            "rapid_clip_loss": [C.POINTER(ClipDesc)] + [vp] * 11 + [sz, vp],
+            "rapid_preference_loss_workspace_bytes": [C.POINTER(PrefDesc), C.POINTER(sz)],
+            "rapid_preference_loss": [C.POINTER(PrefDesc)] + [vp] * 11 + [sz, vp],
+            "rapid_distill_loss_workspace_bytes": [C.POINTER(DistillDesc), C.POINTER(sz)],
+            "rapid_distill_loss": [C.POINTER(DistillDesc)] + [vp] * 10 + [sz, vp],
         }.items():
             getattr(L, name).restype = C.c_int
             getattr(L, name).argtypes = argtypes
@@ -810,3 +848,224 @@ def attention_grad(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch
         elif stats is not None:
             stats.zero_()
     return AttnGrads(dq, dk, dv)
+
+
+# ---- further losses over the logits (include/rapid_losses.h) ------------------------------------------------------
+#
+# rapid_clip_loss(), rapid_preference_loss() and rapid_distill_loss() marshal the arguments of the C calls; clip_loss(),
+# preference_loss() and distill_loss() check shapes and types, allocate the outputs and the workspace and make one call.
+
+
+def read_loss_stats(stats: torch.Tensor) -> dict:
+    """Copy a device rapid_loss_stats_t (alloc_stats) to the host (synchronises) and return it as a dict."""
+    s = LossStats.from_buffer_copy(bytes(stats.cpu().numpy().tobytes())[:STATS_BYTES])
+    return {k: getattr(s, k) for k, _ in LossStats._fields_}
+
+
+def make_clip_desc(n_seq: int, seq_len: int, vocab: int, dtype: torch.dtype, ld: Optional[int] = None, ld_grad: Optional[int] = None,
+                   eps_low: float = 0.2, eps_high: float = 0.2, kl_beta: float = 0.0, scale: float = 1.0, flags: int = 0,
+                   norm_z: float = 0.0) -> ClipDesc:
+    _fits(flags, n_seq=n_seq, seq_len=seq_len, vocab=vocab)
+    ld = vocab if ld is None else ld
+    return ClipDesc(n_seq, seq_len, vocab, _dtype_code(dtype), ld, ld if ld_grad is None else ld_grad, flags, 0, float(eps_low), float(eps_high),
+                    float(kl_beta), float(scale), float(norm_z))
+
+
+def make_pref_desc(n_seq: int, seq_len: int, vocab: int, dtype: torch.dtype, n_pairs: int, ld: Optional[int] = None,
+                   ld_grad: Optional[int] = None, beta: float = 0.1, margin: float = 0.0, label_smoothing: float = 0.0, scale: float = 1.0,
+                   flags: int = 0, norm_z: float = 0.0) -> PrefDesc:
+    _fits(flags, n_seq=n_seq, seq_len=seq_len, vocab=vocab, n_pairs=n_pairs)
+    ld = vocab if ld is None else ld
+    return PrefDesc(n_seq, seq_len, vocab, _dtype_code(dtype), ld, ld if ld_grad is None else ld_grad, flags, n_pairs, float(beta), float(margin),
+                    float(label_smoothing), float(scale), float(norm_z))
+
+
+def make_distill_desc(n_rows: int, vocab: int, k: int, dtype: torch.dtype, ld: Optional[int] = None, ld_grad: Optional[int] = None,
+                      ld_top: Optional[int] = None, temperature: float = 1.0, scale: float = 1.0, flags: int = 0,
+                      norm_z: float = 0.0) -> DistillDesc:
+    _fits(flags, vocab=vocab, k=k)
+    ld = vocab if ld is None else ld
+    return DistillDesc(n_rows, vocab, k, ld, ld if ld_grad is None else ld_grad, k if ld_top is None else ld_top, _dtype_code(dtype), flags,
+                       float(temperature), float(scale), float(norm_z))
+
+
+def rapid_clip_loss_workspace_bytes(desc: ClipDesc) -> int:
+    return _workspace(lib().rapid_clip_loss_workspace_bytes, desc, "rapid_clip_loss_workspace_bytes")
+
+
+def rapid_clip_loss(desc: ClipDesc, logits: torch.Tensor, targets: torch.Tensor, mask: Optional[torch.Tensor], old_logp: torch.Tensor,
+                    ref_logp: Optional[torch.Tensor], adv: torch.Tensor, dlogits: Optional[torch.Tensor], loss: torch.Tensor,
+                    token_logp: Optional[torch.Tensor], stats: Optional[torch.Tensor], workspace: torch.Tensor) -> None:
+    _check(lib().rapid_clip_loss(C.byref(desc), _addr(logits), _addr(targets), _addr(mask), _addr(old_logp), _addr(ref_logp), _addr(adv),
+                                 _addr(dlogits), _addr(loss), _addr(token_logp), _addr(stats), _addr(workspace), workspace.numel(),
+                                 _stream_here()), "rapid_clip_loss")
+
+
+def rapid_preference_loss_workspace_bytes(desc: PrefDesc) -> int:
+    return _workspace(lib().rapid_preference_loss_workspace_bytes, desc, "rapid_preference_loss_workspace_bytes")
+
+
+def rapid_preference_loss(desc: PrefDesc, logits: torch.Tensor, targets: torch.Tensor, mask: Optional[torch.Tensor], pairs: torch.Tensor,
+                          ref_logp: Optional[torch.Tensor], dlogits: Optional[torch.Tensor], loss: torch.Tensor,
+                          margins: Optional[torch.Tensor], token_logp: Optional[torch.Tensor], stats: Optional[torch.Tensor],
+                          workspace: torch.Tensor) -> None:
+    _check(lib().rapid_preference_loss(C.byref(desc), _addr(logits), _addr(targets), _addr(mask), _addr(pairs), _addr(ref_logp),
+                                       _addr(dlogits), _addr(loss), _addr(margins), _addr(token_logp), _addr(stats), _addr(workspace),
+                                       workspace.numel(), _stream_here()), "rapid_preference_loss")
+
+
+def rapid_distill_loss_workspace_bytes(desc: DistillDesc) -> int:
+    return _workspace(lib().rapid_distill_loss_workspace_bytes, desc, "rapid_distill_loss_workspace_bytes")
+
+
+def rapid_distill_loss(desc: DistillDesc, logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch.Tensor,
+                       top_lse: Optional[torch.Tensor], mask: Optional[torch.Tensor], dlogits: Optional[torch.Tensor], loss: torch.Tensor,
+                       token_loss: Optional[torch.Tensor], stats: Optional[torch.Tensor], workspace: torch.Tensor) -> None:
+    _check(lib().rapid_distill_loss(C.byref(desc), _addr(logits), _addr(top_index), _addr(top_logit), _addr(top_lse), _addr(mask),
+                                    _addr(dlogits), _addr(loss), _addr(token_loss), _addr(stats), _addr(workspace), workspace.numel(),
+                                    _stream_here()), "rapid_distill_loss")
+
+
+@functools.lru_cache(maxsize=512)
+def _clip_plan(n_seq, seq_len, vocab, dtype, ld, ld_grad, eps_low, eps_high, kl_beta, scale, flags, norm_z):
+    desc = make_clip_desc(n_seq, seq_len, vocab, dtype, ld, ld_grad, eps_low, eps_high, kl_beta, scale, flags, norm_z)
+    return desc, rapid_clip_loss_workspace_bytes(desc)
+
+
+@functools.lru_cache(maxsize=512)
+def _pref_plan(n_seq, seq_len, vocab, dtype, n_pairs, ld, ld_grad, beta, margin, label_smoothing, scale, flags, norm_z):
+    desc = make_pref_desc(n_seq, seq_len, vocab, dtype, n_pairs, ld, ld_grad, beta, margin, label_smoothing, scale, flags, norm_z)
+    return desc, rapid_preference_loss_workspace_bytes(desc)
+
+
+@functools.lru_cache(maxsize=512)
+def _distill_plan(n_rows, vocab, k, dtype, ld, ld_grad, ld_top, temperature, scale, flags, norm_z):
+    desc = make_distill_desc(n_rows, vocab, k, dtype, ld, ld_grad, ld_top, temperature, scale, flags, norm_z)
+    return desc, rapid_distill_loss_workspace_bytes(desc)
+
+
+def _loss_args(logits, n_rows, mask, stats, want_grad, in_place):
+    if logits.dim() != 2 or logits.shape[0] != n_rows:
+        raise ValueError("logits: a matrix of one row for each position expected")
+    if n_rows <= 0 or logits.shape[1] <= 0:
+        raise ValueError("logits: at least one row and one column expected")
+    if in_place and not want_grad:
+        raise ValueError("in_place: there is no gradient to put in the place of the logits")
+    _stats_room(stats)
+    return _mask8(mask, n_rows)
+
+
+def _loss_grad(logits, want_grad, in_place):
+    return None if not want_grad else logits if in_place else _matrix(logits.shape[0], logits.shape[1], logits.dtype, logits)
+
+
+@dataclass
+class ClipResult:
+    loss: torch.Tensor               # [1] float32
+    dlogits: Optional[torch.Tensor]  # [T, V], None without want_grad
+    token_logp: torch.Tensor         # [T] float32
+
+
+def clip_loss(logits: torch.Tensor, targets: torch.Tensor, mask: Optional[torch.Tensor], old_logp: torch.Tensor, adv: torch.Tensor,
+              n_seq: int, seq_len: int, ref_logp: Optional[torch.Tensor] = None, eps_low: float = 0.2, eps_high: float = 0.2,
+              kl_beta: float = 0.0, scale: float = 1.0, flags: int = 0, norm_z: float = 0.0, want_grad: bool = True, in_place: bool = False,
+              stats: Optional[torch.Tensor] = None) -> ClipResult:
+    """Clipped policy loss over the token grid, logits [T, V], with a KL term to ref_logp where kl_beta > 0, and its gradient by the
+    logits.  adv holds an advantage for each generation, or (T of them) for each row.  Weights of the rows: one over their number,
+    or by LOSS_NORM_SEQ / LOSS_NORM_GIVEN in flags.  stats (alloc_stats, read_loss_stats) gets the side statistics."""
+    n_seq, seq_len, flags = _int(n_seq), _int(seq_len), _int(flags)
+    T = n_seq * seq_len
+    mask = _loss_args(logits, T, mask, stats, want_grad, in_place)
+    _vector(targets, T, torch.int32, "targets")
+    _vector(old_logp, T, torch.float32, "old_logp")
+    _vector(ref_logp, T, torch.float32, "ref_logp")
+    if adv.numel() not in (n_seq, T):
+        raise ValueError("adv: one element for each generation or for each row expected")
+    by_token = adv.numel() != n_seq or bool(flags & CLIP_ADV_TOKEN)
+    _vector(adv, T if by_token else n_seq, torch.float32, "adv")
+    flags |= CLIP_ADV_TOKEN if by_token else 0
+    dev = _one_device(logits, targets, mask, old_logp, ref_logp, adv, stats)
+    with _on(dev):
+        ld = _pitch(logits, "logits")
+        dlogits = _loss_grad(logits, want_grad, in_place)
+        desc, ws_bytes = _clip_plan(n_seq, seq_len, logits.shape[1], logits.dtype, ld, ld if dlogits is None else _pitch(dlogits, "dlogits"),
+                                    _float(eps_low), _float(eps_high), _float(kl_beta), _float(scale), flags, _float(norm_z))
+        loss, token_logp = old_logp.new_empty(1), _new(old_logp)
+        rapid_clip_loss(desc, logits, targets, mask, old_logp, ref_logp, adv, dlogits, loss, token_logp, stats,
+                        logits.new_empty(ws_bytes, dtype=torch.uint8))
+    return ClipResult(loss, dlogits, token_logp)
+
+
+@dataclass
+class PrefResult:
+    loss: torch.Tensor               # [1] float32
+    dlogits: Optional[torch.Tensor]  # [T, V], None without want_grad
+    margins: torch.Tensor            # [P] float32, h of every pair
+    token_logp: torch.Tensor         # [T] float32
+
+
+def preference_loss(logits: torch.Tensor, targets: torch.Tensor, mask: Optional[torch.Tensor], pairs: torch.Tensor, n_seq: int,
+                    seq_len: int, ref_logp: Optional[torch.Tensor] = None, beta: float = 0.1, margin: float = 0.0,
+                    label_smoothing: float = 0.0, scale: float = 1.0, flags: int = 0, norm_z: float = 0.0, want_grad: bool = True,
+                    in_place: bool = False, stats: Optional[torch.Tensor] = None) -> PrefResult:
+    """Preference loss over pairs [P, 2] int32 of generations (preferred, other) of the token grid, logits [T, V], and its gradient
+    by the logits.  flags: PREF_HINGE or PREF_SQUARED instead of the logistic form, PREF_TOKEN_MEAN, LOSS_NORM_GIVEN."""
+    n_seq, seq_len, flags = _int(n_seq), _int(seq_len), _int(flags)
+    T = n_seq * seq_len
+    mask = _loss_args(logits, T, mask, stats, want_grad, in_place)
+    _vector(targets, T, torch.int32, "targets")
+    _vector(ref_logp, T, torch.float32, "ref_logp")
+    if pairs.dim() != 2 or pairs.shape[1] != 2 or pairs.shape[0] == 0:
+        raise ValueError("pairs: [P, 2] expected")
+    P = pairs.shape[0]
+    _vector(pairs, 2 * P, torch.int32, "pairs")
+    dev = _one_device(logits, targets, mask, pairs, ref_logp, stats)
+    with _on(dev):
+        ld = _pitch(logits, "logits")
+        dlogits = _loss_grad(logits, want_grad, in_place)
+        desc, ws_bytes = _pref_plan(n_seq, seq_len, logits.shape[1], logits.dtype, P, ld, ld if dlogits is None else _pitch(dlogits, "dlogits"),
+                                    _float(beta), _float(margin), _float(label_smoothing), _float(scale), flags, _float(norm_z))
+        loss, margins, token_logp = (logits.new_empty(n, dtype=torch.float32) for n in (1, P, T))
+        rapid_preference_loss(desc, logits, targets, mask, pairs, ref_logp, dlogits, loss, margins, token_logp, stats,
+                              logits.new_empty(ws_bytes, dtype=torch.uint8))
+    return PrefResult(loss, dlogits, margins, token_logp)
+
+
+@dataclass
+class DistillResult:
+    loss: torch.Tensor               # [1] float32
+    dlogits: Optional[torch.Tensor]  # [T, V], None without want_grad
+    token_loss: torch.Tensor         # [T] float32
+
+
+def distill_loss(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch.Tensor, mask: Optional[torch.Tensor] = None,
+                 top_lse: Optional[torch.Tensor] = None, temperature: float = 1.0, scale: float = 1.0, flags: int = 0, norm_z: float = 0.0,
+                 want_grad: bool = True, in_place: bool = False, stats: Optional[torch.Tensor] = None) -> DistillResult:
+    """Divergence of the student's logits [T, V] from a teacher's top ones, top_index [T, K] int32 (negative: no entry) and top_logit
+    [T, K] float32, and its gradient by the logits.  With top_lse [T], the teacher's log-sum-exp of logits / temperature over its whole
+    vocabulary, the tokens outside the list are one outcome more; without it the list is all of the teacher's probability."""
+    flags = _int(flags)
+    T = logits.shape[0]
+    mask = _loss_args(logits, T, mask, stats, want_grad, in_place)
+    if top_index.dim() != 2 or top_index.shape != top_logit.shape or top_index.shape[0] != T or top_index.shape[1] == 0:
+        raise ValueError("top_index, top_logit: [T, K] expected")
+    if top_index.dtype != torch.int32 or top_logit.dtype != torch.float32:
+        raise TypeError("top_index must be int32 and top_logit float32")
+    K = top_index.shape[1]
+    for x, name in ((top_index, "top_index"), (top_logit, "top_logit")):
+        if K > 1 and x.stride(1) != 1:
+            raise ValueError(f"{name}: the elements of a row must lie side by side")
+    pitch = K if T == 1 else top_index.stride(0)
+    if T > 1 and top_logit.stride(0) != pitch:
+        raise ValueError("top_index and top_logit must have one row pitch")
+    _vector(top_lse, T, torch.float32, "top_lse")
+    dev = _one_device(logits, top_index, top_logit, top_lse, mask, stats)
+    with _on(dev):
+        ld = _pitch(logits, "logits")
+        dlogits = _loss_grad(logits, want_grad, in_place)
+        desc, ws_bytes = _distill_plan(T, logits.shape[1], K, logits.dtype, ld, ld if dlogits is None else _pitch(dlogits, "dlogits"), pitch,
+                                       _float(temperature), _float(scale), flags, _float(norm_z))
+        loss, token_loss = (logits.new_empty(n, dtype=torch.float32) for n in (1, T))
+        rapid_distill_loss(desc, logits, top_index, top_logit, top_lse, mask, dlogits, loss, token_loss, stats,
+                           logits.new_empty(ws_bytes, dtype=torch.uint8))
+    return DistillResult(loss, dlogits, token_loss)

@@ -1,0 +1,536 @@
+// What the losses of rapid_losses.h share: the scratch, the statistics of a row of logits and the gradient of a row.
+//
+// All three losses have the same shape.  A row r of logits z gives a log-sum-exp of z / tau; an operator turns it, together with
+// a few chosen columns of the row, into a factor a_r and values for those columns; the gradient is
+//     dz[v] = a_r softmax(z / tau)_v  everywhere else,   dz[column_j] = value_j.
+// An operator says what the chosen columns are (the sampled token, or a teacher's list) and computes the factor and the values,
+// in double, with one warp; this file and loss_rows.cu do the rest.
+//
+// Logarithms are base 2 inside: x_v = z_v log2(e) / tau, lse2 = log2 sum_v 2^(x_v).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "rapid_common.cuh"
+#include "rapid_losses.h"
+
+namespace rapid {
+namespace losses {
+
+static_assert(sizeof(rapid_clip_desc_t) == 80 && sizeof(rapid_pref_desc_t) == 80 && sizeof(rapid_distill_desc_t) == 72 &&
+                  sizeof(rapid_loss_stats_t) == 48,
+              "bindings rely on these");
+
+constexpr int kMaxList = 256;      // entries of a distillation list
+constexpr int kPrepBlocks = 256;   // blocks of a preparing kernel, at most
+constexpr int kSumBlocks = 1024;   // blocks of a summing kernel, at most
+
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+inline size_t elem_size(int32_t dtype) { return dtype == RAPID_BF16 ? 2 : 4; }
+
+// ---- scratch ------------------------------------------------------------------------------------------------
+
+struct Header {
+    unsigned int ticket;  // rows handed out
+    unsigned int done;    // blocks of the summing kernel that are through
+    int32_t status;       // RAPID_ERR_TIMEOUT when a wait gave up
+    int32_t pad;
+};
+
+struct Scratch {
+    Header* head;
+    int2* counts;         // [kPrepBlocks] rows that count, rows that are not valid
+    double* sums;         // [kSumBlocks][8] partial sums
+    double* lse2;         // [T]
+    double* value;        // [T] log-probability of the token, or the row's loss
+    float* row_max;       // [T]
+    uint8_t* state;       // [T] ROW_*
+    int32_t* seq_rows;    // [N] rows that count
+    double* seq_sum;      // [N] s_n
+    double* seq_coef;     // [N] g_n
+    double* pair_slope;   // [P]
+    double* teacher_lse2; // [T]
+};
+
+enum : int { NEED_SEQ = 1, NEED_PAIRS = 2, NEED_TEACHER = 4 };
+
+// Carve `base` (256-byte aligned); returns the bytes used.
+inline size_t carve(int64_t T, int64_t N, int64_t P, int need, void* base, Scratch* out) {
+    size_t off = 0;
+    char* p = static_cast<char*>(base);
+    auto take = [&](size_t bytes) {
+        char* q = p ? p + off : nullptr;
+        off = align_up(off + bytes, 256);
+        return q;
+    };
+    Scratch s{};
+    s.head = reinterpret_cast<Header*>(take(sizeof(Header)));
+    s.counts = reinterpret_cast<int2*>(take(kPrepBlocks * sizeof(int2)));
+    s.sums = reinterpret_cast<double*>(take((size_t)kSumBlocks * 64));
+    s.lse2 = reinterpret_cast<double*>(take((size_t)T * 8));
+    s.value = reinterpret_cast<double*>(take((size_t)T * 8));
+    s.row_max = reinterpret_cast<float*>(take((size_t)T * 4));
+    s.state = reinterpret_cast<uint8_t*>(take((size_t)T));
+    if (need & NEED_SEQ) s.seq_rows = reinterpret_cast<int32_t*>(take((size_t)N * 4));
+    if (need & NEED_PAIRS) {
+        s.seq_sum = reinterpret_cast<double*>(take((size_t)N * 8));
+        s.seq_coef = reinterpret_cast<double*>(take((size_t)N * 8));
+        s.pair_slope = reinterpret_cast<double*>(take((size_t)P * 8));
+    }
+    if (need & NEED_TEACHER) s.teacher_lse2 = reinterpret_cast<double*>(take((size_t)T * 8));
+    if (out) *out = s;
+    return off;
+}
+
+// ---- host checks that all three share --------------------------------------------------------------------------
+
+// Do two matrices of `n` rows, `width` bytes wide at pitches of pa and pb bytes, share a byte?  Matrices of one pitch may lie side
+// by side in the same rows; of two pitches, they have to be apart altogether.
+inline bool matrices_overlap(const void* a, int64_t pa, const void* b, int64_t pb, int64_t n, int64_t width) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    const size_t ea = (size_t)(n - 1) * pa + width, eb = (size_t)(n - 1) * pb + width;
+    if (x >= y + eb || y >= x + ea) return false;
+    if (pa != pb) return true;
+    int64_t off = ((int64_t)y - (int64_t)x) % pa;
+    if (off < 0) off += pa;
+    return off < width || off + width > pa;
+}
+
+inline rapid_status_t check_shape(int64_t T, int32_t vocab, int32_t dtype, int64_t ld, int64_t ld_grad, uint32_t flags, uint32_t known,
+                                  double scale, double norm_z) {
+    if (T <= 0 || vocab <= 0 || ld < vocab || ld_grad < vocab) return RAPID_ERR_INVALID_ARG;
+    if (dtype != RAPID_F32 && dtype != RAPID_BF16) return RAPID_ERR_INVALID_ARG;
+    if ((flags & ~known) || !isfinite(scale)) return RAPID_ERR_INVALID_ARG;
+    if ((flags & RAPID_LOSS_NORM_GIVEN) && !(norm_z > 0.0 && isfinite(norm_z))) return RAPID_ERR_INVALID_ARG;
+    // 2^56 elements are far beyond any device's memory; keeps every size below in 64 bits
+    if (T > 0x7fffffffll || vocab > (1 << 30) || ld > (1ll << 56) / T || ld_grad > (1ll << 56) / T) return RAPID_ERR_UNSUPPORTED;
+    const size_t es = elem_size(dtype);
+    if ((size_t)ld * es % 16 != 0 || (size_t)ld_grad * es % 16 != 0) return RAPID_ERR_ALIGNMENT;
+    return RAPID_OK;
+}
+
+inline rapid_status_t check_matrices(const void* logits, const void* dlogits, int64_t T, int32_t vocab, int32_t dtype, int64_t ld,
+                                     int64_t ld_grad) {
+    if (!logits) return RAPID_ERR_INVALID_ARG;
+    if (!aligned(logits, 16) || !aligned(dlogits, 16)) return RAPID_ERR_ALIGNMENT;
+    if (!dlogits) return RAPID_OK;
+    const int64_t es = (int64_t)elem_size(dtype);
+    if (logits == dlogits) return ld == ld_grad || T == 1 ? RAPID_OK : RAPID_ERR_INVALID_ARG;
+    return matrices_overlap(logits, ld * es, dlogits, ld_grad * es, T, vocab * es) ? RAPID_ERR_INVALID_ARG : RAPID_OK;
+}
+
+// sm_100 only.  Returns the SM count of the current device through *sm_count.
+inline rapid_status_t check_device(int* sm_count) {
+    int dev = 0, major = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return RAPID_ERR_CUDA;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(sm_count, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        return RAPID_ERR_CUDA;
+    return major == 10 ? RAPID_OK : RAPID_ERR_UNSUPPORTED;
+}
+
+// ---- a row's statistics -----------------------------------------------------------------------------------------
+
+// log2(e) / tau, as a sum of two floats: k1 has 16 significant bits, so that its product with a bf16 logit (8 bits) is exact, and
+// k2 > 0 carries the next 24 (k2 is never 0, or -inf * k2 would be NaN).  k is the nearest float.
+struct Factor {
+    double kd;
+    float k1, k2, k;
+};
+inline Factor make_factor(double tau) {
+    Factor f;
+    f.kd = kLog2eD / tau;
+    int e = 0;
+    const double m = frexp(f.kd, &e);  // in [1/2, 1)
+    f.k1 = (float)ldexp(floor(ldexp(m, 16)), e - 16);
+    f.k2 = (float)(f.kd - (double)f.k1);
+    if (!(f.k2 > 0.f)) f.k2 = 1e-30f;
+    f.k = (float)f.kd;
+    return f;
+}
+
+#ifdef __CUDACC__
+
+template <int DT>
+struct Elem;
+template <>
+struct Elem<RAPID_BF16> {
+    using T = uint16_t;
+    static constexpr int kPer = 8;  // elements of a 16-byte vector
+    __device__ static __forceinline__ float get(T x) { return __uint_as_float((uint32_t)x << 16); }
+    __device__ static __forceinline__ T put(float x) { return (T)(pack_bf16x2(x, 0.f) & 0xffffu); }
+    __device__ static __forceinline__ float largest(const uint4& q) {
+        const uint32_t m = bf16x2_max(bf16x2_max(q.x, q.y), bf16x2_max(q.z, q.w));
+        return fmaxf(bf16_lo(m), bf16_hi(m));
+    }
+    // the i-th pair of elements
+    __device__ static __forceinline__ uint64_t pair(const uint4& q, int i) {
+        const uint32_t w = i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w;
+        return f32x2(bf16_lo(w), bf16_hi(w));
+    }
+};
+template <>
+struct Elem<RAPID_F32> {
+    using T = float;
+    static constexpr int kPer = 4;
+    __device__ static __forceinline__ float get(T x) { return x; }
+    __device__ static __forceinline__ T put(float x) { return x; }
+    __device__ static __forceinline__ float largest(const uint4& q) {
+        return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
+    }
+    __device__ static __forceinline__ uint64_t pair(const uint4& q, int i) {
+        return i == 0 ? f32x2(__uint_as_float(q.x), __uint_as_float(q.y)) : f32x2(__uint_as_float(q.z), __uint_as_float(q.w));
+    }
+};
+
+// Mean relative error of the hardware exponential over the fraction of its argument (errors lie in [-1.44e-7, +0.63e-7]; measured
+// over all 2^23 fractions): a sum of many terms carries it and is divided by 1 + kEx2Mean.
+constexpr float kEx2Mean = -4.95e-8f;
+constexpr float kNothing = -1.0e38f;  // at or below: -inf or the lowest finite value, a masked part of the vocabulary
+
+// One thread's part of a row: the largest logit m, the shift sh that its exponentials are taken against, and sum_v 2^(x_v - sh)
+// with the rounding errors of its additions beside it.  sh = ceil(m k) + off is used as it stands, here and where the parts meet,
+// so no rounding of m k enters; `off`, a 16-bit fraction, is one for a warp (the parts of its lanes differ by exact powers of two)
+// and another for each warp, so that the errors of the exponentials of equal logits do not all have one sign.
+struct Part {
+    float m = -INFINITY, sh = 0.f, s = 0.f, c = 0.f;
+
+    __device__ __forceinline__ void see(float bm, float off, const Factor& f) {
+        if (bm > m) {
+            m = bm;
+            if (bm > kNothing) {
+                const float now = ceilf(bm * f.k) + off;
+                const float by = ex2_approx(sh - now);  // an exact power of two; of an empty part, whatever: its sum is 0
+                if (s > 0.f) {
+                    s *= by;
+                    c *= by;
+                }
+                sh = now;
+            }
+        }
+    }
+    __device__ __forceinline__ void add(float b) {  // Fast2Sum wants the larger one first
+        const float hi = fmaxf(s, b), lo = fminf(s, b);
+        const float t = hi + lo;
+        c += (hi - t) + lo;
+        s = t;
+    }
+    __device__ __forceinline__ float term(float z, const Factor& f) const { return ex2_approx(fmaf(z, f.k2, fmaf(z, f.k1, -sh))); }
+
+    // U vectors: the exponentials are summed from zero, in as many partial sums as a vector has elements, and then added
+    template <int DT, int U>
+    __device__ __forceinline__ void vectors(const uint4 (&q)[U], float off, const Factor& f) {
+        constexpr int P = Elem<DT>::kPer / 2;
+        float bm = Elem<DT>::largest(q[0]);
+#pragma unroll
+        for (int j = 1; j < U; ++j) bm = fmaxf(bm, Elem<DT>::largest(q[j]));
+        see(bm, off, f);
+        const uint64_t k1 = f32x2(f.k1, f.k1), k2 = f32x2(f.k2, f.k2), nsh = f32x2(-sh, -sh);
+        uint64_t a[P];
+#pragma unroll
+        for (int i = 0; i < P; ++i) a[i] = f32x2(0.f, 0.f);
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const uint64_t z = Elem<DT>::pair(q[j], i);
+                float x0, x1;
+                f32x2_split(f32x2_fma(z, k2, f32x2_fma(z, k1, nsh)), x0, x1);
+                a[i] = f32x2_add(a[i], f32x2(ex2_approx(x0), ex2_approx(x1)));
+            }
+        }
+#pragma unroll
+        for (int n = P / 2; n > 0; n /= 2)
+#pragma unroll
+            for (int i = 0; i < n; ++i) a[i] = f32x2_add(a[i], a[i + n]);
+        float s0, s1;
+        f32x2_split(a[0], s0, s1);
+        add(s0 + s1);
+    }
+    __device__ __forceinline__ void scalar(float z, float off, const Factor& f) {
+        see(z, off, f);
+        if (z > kNothing) add(term(z, f));
+    }
+};
+
+// A warp's part, the same in all lanes: its largest logit, its shift, and the sum WITHOUT the largest logit's term, which may carry
+// nearly all of the row's probability and is put back exactly, in double, where the warps' parts meet.
+struct WarpPart {
+    float m, sh;
+    double s;
+};
+__device__ __forceinline__ WarpPart warp_part(const Part& p, const Factor& f) {
+    WarpPart w;
+    w.m = warp_max(p.m);
+    w.sh = warp_max(p.s > 0.f ? p.sh : -INFINITY);
+    double s = (double)p.s + (double)p.c;
+    const unsigned top = __ballot_sync(0xffffffffu, p.m == w.m && w.m > kNothing);
+    if (top && (threadIdx.x & 31) == __ffs(top) - 1) s -= (double)p.term(p.m, f);
+    if (p.s > 0.f) s *= (double)ex2_approx(p.sh - w.sh);  // an exact power of two
+    else s = 0.0;
+    w.s = warp_sum(s);
+    return w;
+}
+
+struct RowStat {
+    double lse2;  // -inf when no logit is left
+    float max;
+};
+// The warps' parts together, by one warp: lane i holds warp i's part (sh = -inf where there is none).
+__device__ __forceinline__ RowStat join_parts(const WarpPart& p, const Factor& f) {
+    RowStat r;
+    r.max = warp_max(p.m);
+    const float sh = warp_max(p.sh);
+    double s = 0.0;
+    if (p.m > kNothing)
+        s = p.s / (1.0 + (double)kEx2Mean) * exp2((double)p.sh - (double)sh) + exp2((double)p.m * f.kd - (double)sh);
+    s = warp_sum(s);
+    r.lse2 = s > 0.0 ? (double)sh + log2(s) : -INFINITY;
+    return r;
+}
+
+__device__ __forceinline__ float shift_fraction(int warp) { return (float)(((unsigned)warp * 40503u) & 0xffffu) * (1.f / 65536.f); }
+
+// ---- a row's gradient --------------------------------------------------------------------------------------------
+
+// dz_v = a 2^(x_v - lse2).  bf16: |a| goes into the exponent, one multiply-add and one exponential an element.  float: the largest
+// logit is taken off first, which keeps the argument small and so its rounding below the result's; a is multiplied at the end.
+template <int DT>
+struct Grad;
+template <>
+struct Grad<RAPID_BF16> {
+    float k, c;
+    uint32_t sign;  // of a, on both halves of a pair
+    __device__ __forceinline__ void set(double a, double lse2, float, const Factor& f) {
+        k = f.k;
+        c = a != 0.0 ? (float)(log2(fabs(a)) - lse2) : -INFINITY;
+        sign = a < 0.0 ? 0x80008000u : 0u;
+    }
+    __device__ __forceinline__ uint4 vector(const uint4& q) const {
+        const uint32_t in[4] = {q.x, q.y, q.z, q.w};
+        uint32_t out[4];
+        const uint64_t k2 = f32x2(k, k), c2 = f32x2(c, c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x0, x1;
+            f32x2_split(f32x2_fma(f32x2(bf16_lo(in[i]), bf16_hi(in[i])), k2, c2), x0, x1);
+            out[i] = pack_bf16x2(ex2_approx(x0), ex2_approx(x1)) ^ sign;
+        }
+        return make_uint4(out[0], out[1], out[2], out[3]);
+    }
+    __device__ __forceinline__ uint16_t one(uint16_t z) const {
+        return (uint16_t)(Elem<RAPID_BF16>::put(ex2_approx(fmaf(Elem<RAPID_BF16>::get(z), k, c))) ^ (uint16_t)sign);
+    }
+};
+template <>
+struct Grad<RAPID_F32> {
+    float k, m, c, a;
+    __device__ __forceinline__ void set(double a_, double lse2, float max, const Factor& f) {
+        k = f.k;
+        m = max > kNothing ? max : 0.f;
+        c = (float)((double)m * f.kd - lse2);
+        a = (float)a_;
+    }
+    __device__ __forceinline__ float one(float z) const { return a * ex2_approx(fmaf(z - m, k, c)); }
+    __device__ __forceinline__ uint4 vector(const uint4& q) const {
+        return make_uint4(__float_as_uint(one(__uint_as_float(q.x))), __float_as_uint(one(__uint_as_float(q.y))),
+                          __float_as_uint(one(__uint_as_float(q.z))), __float_as_uint(one(__uint_as_float(q.w))));
+    }
+};
+
+// The factor and the chosen columns' values of one row.
+struct RowGrad {
+    double a, lse2;
+};
+
+// Rows that count, from the preparing kernel's blocks; by one warp.
+__device__ __forceinline__ long long rows_that_count(const int2* counts, int blocks) {
+    long long n = 0;
+    for (int i = threadIdx.x & 31; i < blocks; i += 32) n += counts[i].x;
+    return warp_sum(n);
+}
+
+#endif  // __CUDACC__
+
+// ---- what an operator brings to the rows ----------------------------------------------------------------------------
+
+struct RowsArgs {
+    const void* logits;
+    void* grad;  // may be logits, may be NULL
+    int64_t ld, ld_grad, n_rows;
+    int vocab, dtype;
+    int known;   // the statistics are in the scratch already: gradient only
+    Factor f;
+    Scratch w;
+};
+
+struct ClipOp {
+    const int32_t* targets;
+    const float *old_logp, *ref_logp, *adv;
+    const int32_t* seq_rows;  // with RAPID_LOSS_NORM_SEQ
+    const int2* counts;
+    int count_blocks, n_seq, seq_len;
+    uint32_t flags;
+    double low, high, beta, scale, norm_z;
+};
+struct PrefOp {  // first reading: the token's log-probability; second: the gradient, from the generation's coefficient
+    const int32_t* targets;
+    const double* seq_coef;
+    int seq_len;
+};
+struct DistillOp {
+    const int32_t* index;
+    const float* logit;
+    const double* teacher_lse2;
+    const int2* counts;
+    int64_t ld;
+    int k, tail, count_blocks;
+    uint32_t flags;
+    double inv_tau, scale, norm_z, kd;
+};
+
+cudaError_t launch_rows(const RowsArgs& a, const ClipOp& op, int sm_count, cudaStream_t stream);
+cudaError_t launch_rows(const RowsArgs& a, const PrefOp& op, int sm_count, cudaStream_t stream);
+cudaError_t launch_rows(const RowsArgs& a, const DistillOp& op, int sm_count, cudaStream_t stream);
+
+// State of every row from mask and token, their numbers, and (where asked for) those of every generation; clears the header.
+cudaError_t launch_prepare_tokens(int n_seq, int seq_len, int vocab, const int32_t* targets, const uint8_t* mask, const Scratch& w,
+                                  int by_seq, int* blocks, cudaStream_t stream);
+
+#ifdef __CUDACC__
+
+// The clipped loss of one row and its slope by the log-probability, sign turned: loss' = -slope.
+struct ClipTerms {
+    double loss, slope, kl;
+    bool cut;
+};
+__device__ __forceinline__ ClipTerms clip_terms(const ClipOp& op, int64_t r, double lp) {
+    ClipTerms t;
+    const double A = (double)op.adv[(op.flags & RAPID_CLIP_ADV_TOKEN) ? r : r / op.seq_len];
+    const double rho = exp(lp - (double)op.old_logp[r]);
+    const double u = A != 0.0 ? rho * A : 0.0;  // A = 0 leaves nothing, even of an infinite ratio
+    const double v = A != 0.0 ? fmin(fmax(rho, 1.0 - op.low), 1.0 + op.high) * A : 0.0;
+    t.cut = v < u;
+    t.loss = t.cut ? -v : -u;
+    t.slope = t.cut ? 0.0 : u;
+    t.kl = 0.0;
+    if (op.ref_logp) {
+        const double d = (double)op.ref_logp[r] - lp, e = expm1(d);
+        t.kl = isinf(e) ? e : e - d;
+        if (op.beta != 0.0) {
+            t.loss += op.beta * t.kl;
+            t.slope += op.beta * e;
+        }
+    }
+    return t;
+}
+// Weight of row r: `rows` is the number of rows that count.
+__device__ __forceinline__ double clip_weight(const ClipOp& op, int64_t r, long long rows) {
+    if (op.flags & RAPID_LOSS_NORM_SEQ) {
+        const double n = (op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)op.n_seq;
+        return op.scale / (n * (double)op.seq_rows[r / op.seq_len]);
+    }
+    return op.scale / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows);
+}
+
+// finish(): by one warp, once a row's log-sum-exp is there (without the chosen columns where exclude() says so).  z[j] are the
+// chosen columns' logits, value[j] becomes their gradient.  Writes what the operator keeps of the row to the scratch.
+__device__ __forceinline__ int list_size(const ClipOp&) { return 1; }
+__device__ __forceinline__ int list_size(const PrefOp&) { return 1; }
+__device__ __forceinline__ int list_size(const DistillOp& op) { return op.k; }
+__device__ __forceinline__ const int2* op_counts(const ClipOp& op) { return op.counts; }
+__device__ __forceinline__ const int2* op_counts(const PrefOp&) { return nullptr; }
+__device__ __forceinline__ const int2* op_counts(const DistillOp& op) { return op.counts; }
+__device__ __forceinline__ int op_blocks(const ClipOp& op) { return op.count_blocks; }
+__device__ __forceinline__ int op_blocks(const PrefOp&) { return 0; }
+__device__ __forceinline__ int op_blocks(const DistillOp& op) { return op.count_blocks; }
+__device__ __forceinline__ bool exclude(const ClipOp&) { return false; }
+__device__ __forceinline__ bool exclude(const PrefOp&) { return false; }
+__device__ __forceinline__ bool exclude(const DistillOp& op) { return op.tail != 0; }
+__device__ __forceinline__ int column(const ClipOp& op, int64_t r, int) { return op.targets[r]; }
+__device__ __forceinline__ int column(const PrefOp& op, int64_t r, int) { return op.targets[r]; }
+__device__ __forceinline__ int column(const DistillOp& op, int64_t r, int j) { return op.index[r * op.ld + j]; }
+
+__device__ __forceinline__ RowGrad finish(const ClipOp& op, const RowsArgs& a, int64_t r, const RowStat& st, const float* z, float* value,
+                                          long long rows) {
+    const double lp = ((double)z[0] * a.f.kd - st.lse2) * kLn2D;
+    RowGrad g;
+    g.lse2 = st.lse2;
+    g.a = 0.0;
+    if (a.grad) {
+        g.a = clip_weight(op, r, rows) * clip_terms(op, r, lp).slope;
+        if ((threadIdx.x & 31) == 0) value[0] = (float)(g.a * expm1(lp));
+    }
+    if ((threadIdx.x & 31) == 0) a.w.value[r] = lp;
+    return g;
+}
+
+__device__ __forceinline__ RowGrad finish(const PrefOp& op, const RowsArgs& a, int64_t r, const RowStat& st, const float* z, float* value,
+                                          long long) {
+    const double lp = ((double)z[0] * a.f.kd - st.lse2) * kLn2D;
+    RowGrad g;
+    g.lse2 = st.lse2;
+    g.a = 0.0;
+    if (a.known) {
+        g.a = op.seq_coef[r / op.seq_len];
+        if ((threadIdx.x & 31) == 0) value[0] = (float)(g.a * expm1(lp));
+    } else if ((threadIdx.x & 31) == 0) {
+        a.w.value[r] = lp;
+        a.w.lse2[r] = st.lse2;
+        a.w.row_max[r] = st.max;
+    }
+    return g;
+}
+
+__device__ __forceinline__ RowGrad finish(const DistillOp& op, const RowsArgs& a, int64_t r, const RowStat& st, const float* z, float* value,
+                                          long long rows) {
+    const int lane = threadIdx.x & 31;
+    const double teacher = op.teacher_lse2[r];
+    // the student's log-sum-exp over the whole vocabulary
+    double lse2 = st.lse2;
+    if (op.tail) {
+        double top = lse2;
+        for (int j = lane; j < op.k; j += 32)
+            if (column(op, r, j) >= 0) top = fmax(top, (double)z[j] * op.kd);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, o));
+        double s = 0.0;
+        if (top > -INFINITY) {
+            if (lane == 0) s = exp2(lse2 - top);
+            for (int j = lane; j < op.k; j += 32)
+                if (column(op, r, j) >= 0) s += exp2((double)z[j] * op.kd - top);
+        }
+        s = warp_sum(s);
+        lse2 = s > 0.0 ? top + log2(s) : -INFINITY;
+    }
+    const double w = op.scale * op.inv_tau / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows);
+    double loss = 0.0, mass = 0.0;
+    for (int j = lane; j < op.k; j += 32) {
+        if (column(op, r, j) < 0) continue;
+        const double lt = (double)op.logit[r * op.ld + j] * op.kd - teacher, lq = (double)z[j] * op.kd - lse2;
+        const double p = exp2(lt);
+        if (p > 0.0) loss += p * (lt - lq);
+        mass += p;
+        if (a.grad) value[j] = (float)(w * (exp2(lq) - p));
+    }
+    loss = warp_sum(loss);
+    RowGrad g;
+    g.lse2 = lse2;
+    g.a = w;
+    if (op.tail) {
+        const double p0 = 1.0 - warp_sum(mass), l0 = st.lse2 - lse2;
+        if (p0 > 0.0) {
+            loss += p0 * (log2(p0) - l0);
+            if (st.lse2 > -INFINITY) g.a = w * (1.0 - exp2(log2(p0) - l0));
+        }
+    }
+    if (lane == 0) a.w.value[r] = loss * kLn2D;
+    return g;
+}
+
+#endif  // __CUDACC__
+
+}  // namespace losses
+}  // namespace rapid

@@ -1,0 +1,504 @@
+// The losses of rapid_losses.h around their rows: states and numbers of the rows before them, sums over rows, pairs and
+// generations after them, and the C calls.  All of it is double and touches a few values a row, so a call's time beside the rows
+// is that of the launches.
+#include "loss_rows.cuh"
+
+namespace rapid {
+namespace losses {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+
+// Sum over the block, the same in all threads; the order depends on the block's size alone.
+template <class T>
+__device__ __forceinline__ T block_sum(T v, T* sh) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    v = warp_sum(v);
+    __syncthreads();
+    if (lane == 0) sh[warp] = v;
+    __syncthreads();
+    T t = 0;
+    for (int w = 0; w < warps; ++w) t += sh[w];
+    return t;
+}
+
+// ---- before the rows -------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void clear_header(const Scratch& w) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *w.head = Header{0u, 0u, RAPID_OK, 0};
+}
+
+__global__ void __launch_bounds__(kThreads)
+prepare_tokens_kernel(int64_t n_rows, int vocab, const int32_t* __restrict__ targets, const uint8_t* __restrict__ mask, Scratch w) {
+    __shared__ int sh[kWarps];
+    clear_header(w);
+    int live = 0, bad = 0;
+    for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < n_rows; r += (int64_t)gridDim.x * kThreads) {
+        uint8_t st = ROW_MASKED;
+        if (!mask || mask[r]) {
+            const int32_t y = targets[r];
+            st = (y >= 0 && y < vocab) ? ROW_OK : ROW_BAD_TOKEN;
+        }
+        w.state[r] = st;
+        live += st == ROW_OK;
+        bad += st == ROW_BAD_TOKEN;
+    }
+    live = block_sum(live, sh);
+    bad = block_sum(bad, sh);
+    if (threadIdx.x == 0) w.counts[blockIdx.x] = make_int2(live, bad);
+}
+
+// Rows that count of every generation: one block of 32 or 256 threads each.
+__global__ void __launch_bounds__(kThreads) count_by_seq_kernel(int seq_len, Scratch w) {
+    __shared__ int sh[kWarps];
+    const uint8_t* st = w.state + (int64_t)blockIdx.x * seq_len;
+    int n = 0;
+    for (int t = threadIdx.x; t < seq_len; t += blockDim.x) n += st[t] == ROW_OK;
+    n = block_sum(n, sh);
+    if (threadIdx.x == 0) w.seq_rows[blockIdx.x] = n;
+}
+
+// A warp for each row: whether its list is valid, and the teacher's log-sum-exp in base 2.
+__global__ void __launch_bounds__(kThreads)
+prepare_lists_kernel(int64_t n_rows, int vocab, int k, int64_t ld, double kd, const int32_t* __restrict__ index,
+                     const float* __restrict__ logit, const float* __restrict__ top_lse, const uint8_t* __restrict__ mask, Scratch w) {
+    constexpr int R = kMaxList / 32;
+    __shared__ int sh[kWarps];
+    clear_header(w);
+    const int lane = threadIdx.x & 31;
+    int live = 0, bad = 0;
+    for (int64_t r = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); r < n_rows; r += (int64_t)gridDim.x * kWarps) {
+        uint8_t st = ROW_MASKED;
+        if (!mask || mask[r]) {
+            int v[R];
+            float t[R], top = -INFINITY;
+            bool some = false, wrong = false;
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const int j = 32 * i + lane;
+                v[i] = -1;
+                t[i] = -INFINITY;
+                if (j < k) {
+                    v[i] = index[r * ld + j];
+                    if (v[i] >= 0) {
+                        t[i] = logit[r * ld + j];
+                        some = true;
+                        wrong |= v[i] >= vocab || !(t[i] < INFINITY);
+                        top = fmaxf(top, t[i]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                if (32 * i >= k) break;
+                for (int l = 0; l < 32; ++l) {
+                    const int x = __shfl_sync(0xffffffffu, v[i], l);
+                    if (x < 0) continue;
+#pragma unroll
+                    for (int i2 = i; i2 < R; ++i2) wrong |= v[i2] == x && 32 * i2 + lane > 32 * i + l;
+                }
+            }
+            some = __any_sync(0xffffffffu, some);
+            top = warp_max(top);
+            double lse2;
+            if (top_lse) {
+                const float l = top_lse[r];
+                wrong |= !isfinite(l);
+                lse2 = (double)l * kLog2eD;
+            } else {
+                some = some && top > -INFINITY;
+                double s = 0.0;
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+                    if (t[i] > -INFINITY) s += exp2(((double)t[i] - (double)top) * kd);
+                lse2 = (double)top * kd + log2(warp_sum(s));
+            }
+            wrong = __any_sync(0xffffffffu, wrong);
+            st = wrong ? ROW_BAD_TOKEN : some ? ROW_OK : ROW_MASKED;
+            if (lane == 0) w.teacher_lse2[r] = lse2;
+        }
+        if (lane == 0) {
+            w.state[r] = st;
+            live += st == ROW_OK;
+            bad += st == ROW_BAD_TOKEN;
+        }
+    }
+    live = block_sum(live, sh);
+    bad = block_sum(bad, sh);
+    if (threadIdx.x == 0) w.counts[blockIdx.x] = make_int2(live, bad);
+}
+
+// ---- after the rows --------------------------------------------------------------------------------------------
+
+// The last block of a summing kernel adds up the blocks' sums, in their order.  Returns whether this is it; `total` then holds
+// the sums, in all threads.
+template <int N>
+__device__ __forceinline__ bool last_block_sums(const double (&mine)[N], const Scratch& w, double (&total)[N]) {
+    __shared__ double sh[kWarps];
+    __shared__ bool last;
+    double block[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) block[i] = block_sum(mine[i], sh);
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w.sums[(size_t)blockIdx.x * 8 + i] = block[i];
+        __threadfence();
+        last = atomicAdd(&w.head->done, 1u) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last) return false;
+    __threadfence();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        double t = 0.0;
+        for (unsigned b = threadIdx.x; b < gridDim.x; b += kThreads) t += __ldcg(w.sums + (size_t)b * 8 + i);
+        total[i] = block_sum(t, sh);
+    }
+    return true;
+}
+
+__device__ __forceinline__ void counts_of(const int2* counts, int blocks, long long& live, int& bad) {
+    live = 0;
+    bad = 0;
+    for (int i = threadIdx.x & 31; i < blocks; i += 32) {
+        live += counts[i].x;
+        bad += counts[i].y;
+    }
+    live = warp_sum(live);
+    bad = warp_sum(bad);
+}
+
+__global__ void __launch_bounds__(kThreads)
+clip_sum_kernel(ClipOp op, int64_t n_rows, float* __restrict__ token_logp, float* __restrict__ loss, rapid_loss_stats_t* stats, Scratch w) {
+    long long rows;
+    int bad;
+    counts_of(op.counts, op.count_blocks, rows, bad);
+    double mine[4] = {0.0, 0.0, 0.0, 0.0}, total[4];
+    for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < n_rows; r += (int64_t)gridDim.x * kThreads) {
+        double lp = 0.0;
+        if (w.state[r] == ROW_OK) {
+            lp = w.value[r];
+            const ClipTerms t = clip_terms(op, r, lp);
+            mine[0] += clip_weight(op, r, rows) * t.loss;
+            mine[1] += lp - (double)op.old_logp[r];
+            mine[2] += t.kl;
+            mine[3] += t.cut ? 1.0 : 0.0;
+        }
+        if (token_logp) token_logp[r] = (float)lp;
+    }
+    if (!last_block_sums(mine, w, total) || threadIdx.x != 0) return;
+    *loss = (float)total[0];
+    if (stats) {
+        const double n = rows > 0 ? (double)rows : 1.0;
+        *stats = rapid_loss_stats_t{rows, (int32_t)total[3], bad, 0, w.head->status, total[1] / n, total[2] / n, total[0]};
+    }
+}
+
+__global__ void __launch_bounds__(kThreads)
+distill_sum_kernel(DistillOp op, int64_t n_rows, float* __restrict__ token_loss, float* __restrict__ loss, rapid_loss_stats_t* stats,
+                   Scratch w) {
+    double mine[1] = {0.0}, total[1];
+    for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < n_rows; r += (int64_t)gridDim.x * kThreads) {
+        const double v = w.state[r] == ROW_OK ? w.value[r] : 0.0;
+        mine[0] += v;
+        if (token_loss) token_loss[r] = (float)v;
+    }
+    if (!last_block_sums(mine, w, total)) return;
+    long long rows;
+    int bad;
+    counts_of(op.counts, op.count_blocks, rows, bad);
+    if (threadIdx.x != 0) return;
+    const double z = (op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows;
+    const double l = rows > 0 ? op.scale * total[0] / z : 0.0;
+    *loss = (float)l;
+    if (stats) *stats = rapid_loss_stats_t{rows, 0, bad, 0, w.head->status, 0.0, 0.0, l};
+}
+
+// One block for each generation: its sum of log-ratios.
+__global__ void __launch_bounds__(kThreads)
+pref_seq_kernel(int seq_len, uint32_t flags, const float* __restrict__ ref_logp, float* __restrict__ token_logp, Scratch w) {
+    __shared__ double sh[kWarps];
+    __shared__ int shi[kWarps];
+    const int64_t base = (int64_t)blockIdx.x * seq_len;
+    double s = 0.0;
+    int n = 0;
+    for (int t = threadIdx.x; t < seq_len; t += kThreads) {
+        const int64_t r = base + t;
+        double lp = 0.0;
+        if (w.state[r] == ROW_OK) {
+            lp = w.value[r];
+            s += ref_logp ? lp - (double)ref_logp[r] : lp;
+            n += 1;
+        }
+        if (token_logp) token_logp[r] = (float)lp;
+    }
+    s = block_sum(s, sh);
+    n = block_sum(n, shi);
+    if (threadIdx.x == 0) {
+        w.seq_rows[blockIdx.x] = n;
+        w.seq_sum[blockIdx.x] = (flags & RAPID_PREF_TOKEN_MEAN) && n > 0 ? s / (double)n : s;
+    }
+}
+
+struct PairArgs {
+    const int32_t* pairs;
+    int n_pairs, n_seq;
+    uint32_t flags;
+    double beta, margin, smoothing, scale, norm_z;
+};
+__device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
+
+// One block: every pair's loss and slope, and their sums.
+constexpr int kPairThreads = 1024;
+__global__ void __launch_bounds__(kPairThreads)
+pref_pairs_kernel(PairArgs a, int count_blocks, float* __restrict__ margins, float* __restrict__ loss, rapid_loss_stats_t* stats, Scratch w) {
+    __shared__ double sh[kPairThreads / 32];
+    __shared__ int shi[kPairThreads / 32];
+    double sum = 0.0, sum_h = 0.0;
+    int valid = 0, won = 0;
+    for (int p = threadIdx.x; p < a.n_pairs; p += kPairThreads) {
+        const int i = a.pairs[2 * p], j = a.pairs[2 * p + 1];
+        double h = NAN, slope = 0.0;
+        if (i >= 0 && i < a.n_seq && j >= 0 && j < a.n_seq) {
+            h = a.beta * (w.seq_sum[i] - w.seq_sum[j]) - a.margin;
+            double f;
+            if (a.flags & RAPID_PREF_HINGE) {
+                f = fmax(1.0 - h, 0.0);
+                slope = h < 1.0 ? -1.0 : 0.0;
+            } else if (a.flags & RAPID_PREF_SQUARED) {
+                f = (h - 0.5) * (h - 0.5);
+                slope = 2.0 * (h - 0.5);
+            } else {
+                f = (1.0 - a.smoothing) * softplus(-h) + a.smoothing * softplus(h);
+                slope = 1.0 / (1.0 + exp(-h)) - (1.0 - a.smoothing);
+            }
+            sum += f;
+            sum_h += h;
+            valid += 1;
+            won += h > 0.0;
+        }
+        w.pair_slope[p] = slope;
+        if (margins) margins[p] = (float)h;
+    }
+    sum = block_sum(sum, sh);
+    sum_h = block_sum(sum_h, sh);
+    valid = block_sum(valid, shi);
+    won = block_sum(won, shi);
+    long long rows;
+    int bad;
+    counts_of(w.counts, count_blocks, rows, bad);
+    if (threadIdx.x != 0) return;
+    const double z = (a.flags & RAPID_LOSS_NORM_GIVEN) ? a.norm_z : (double)valid;
+    const double l = valid > 0 ? a.scale * sum / z : 0.0;
+    w.sums[0] = valid > 0 ? a.scale * a.beta / z : 0.0;  // what the slopes are multiplied by
+    *loss = (float)l;
+    if (stats) {
+        const double n = valid > 0 ? (double)valid : 1.0;
+        *stats = rapid_loss_stats_t{rows, 0, bad, valid, w.head->status, sum_h / n, (double)won / n, l};
+    }
+}
+
+// A warp for each generation: minus the loss's slope by the sum of its log-probabilities, over the pairs that it is in.
+__global__ void __launch_bounds__(kThreads) pref_coef_kernel(PairArgs a, Scratch w) {
+    const int n = blockIdx.x * kWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (n >= a.n_seq) return;
+    double s = 0.0;
+    for (int p = lane; p < a.n_pairs; p += 32) {
+        const int i = a.pairs[2 * p], j = a.pairs[2 * p + 1];
+        if (i == j) continue;
+        if (i == n) s -= w.pair_slope[p];
+        if (j == n) s += w.pair_slope[p];
+    }
+    s = warp_sum(s) * w.sums[0];
+    if (lane == 0) {
+        const int rows = w.seq_rows[n];
+        w.seq_coef[n] = (a.flags & RAPID_PREF_TOKEN_MEAN) && rows > 0 ? s / (double)rows : s;
+    }
+}
+
+unsigned sum_blocks(int64_t T) {
+    const int64_t b = (T + kThreads - 1) / kThreads;
+    return (unsigned)(b < kSumBlocks ? b : kSumBlocks);
+}
+
+}  // namespace
+
+cudaError_t launch_prepare_tokens(int n_seq, int seq_len, int vocab, const int32_t* targets, const uint8_t* mask, const Scratch& w,
+                                  int by_seq, int* blocks, cudaStream_t stream) {
+    const int64_t T = (int64_t)n_seq * seq_len, b = (T + 1023) / 1024;
+    *blocks = (int)(b < kPrepBlocks ? b : kPrepBlocks);
+    prepare_tokens_kernel<<<*blocks, kThreads, 0, stream>>>(T, vocab, targets, mask, w);
+    if (by_seq) count_by_seq_kernel<<<n_seq, seq_len > 2048 ? kThreads : 32, 0, stream>>>(seq_len, w);
+    return cudaGetLastError();
+}
+
+}  // namespace losses
+}  // namespace rapid
+
+using namespace rapid;
+using namespace rapid::losses;
+
+namespace {
+
+rapid_status_t check_scratch(const void* ws, size_t bytes, size_t need) {
+    return !ws || !aligned(ws, 256) || bytes < need ? RAPID_ERR_WORKSPACE : RAPID_OK;
+}
+inline bool arrays_aligned(const void* a, const void* b, const void* c, const void* d, const void* e, const void* f, const void* stats) {
+    return aligned(a, 4) && aligned(b, 4) && aligned(c, 4) && aligned(d, 4) && aligned(e, 4) && aligned(f, 4) && aligned(stats, 8);
+}
+
+rapid_status_t check_clip(const rapid_clip_desc_t* d) {
+    if (!d || d->n_seq <= 0 || d->seq_len <= 0 || d->reserved != 0) return RAPID_ERR_INVALID_ARG;
+    if (!(d->eps_low >= 0.0) || !(d->eps_high >= 0.0) || !(d->kl_beta >= 0.0) || !isfinite(d->kl_beta)) return RAPID_ERR_INVALID_ARG;
+    return check_shape((int64_t)d->n_seq * d->seq_len, d->vocab, d->dtype, d->ld, d->ld_grad, d->flags,
+                       RAPID_LOSS_NORM_SEQ | RAPID_LOSS_NORM_GIVEN | RAPID_CLIP_ADV_TOKEN, d->scale, d->norm_z);
+}
+size_t carve_clip(const rapid_clip_desc_t& d, void* base, Scratch* w) {
+    return carve((int64_t)d.n_seq * d.seq_len, d.n_seq, 0, (d.flags & RAPID_LOSS_NORM_SEQ) ? NEED_SEQ : 0, base, w);
+}
+
+rapid_status_t check_pref(const rapid_pref_desc_t* d) {
+    if (!d || d->n_seq <= 0 || d->seq_len <= 0 || d->n_pairs <= 0) return RAPID_ERR_INVALID_ARG;
+    if (!(d->beta > 0.0) || !isfinite(d->beta) || !isfinite(d->margin)) return RAPID_ERR_INVALID_ARG;
+    if (!(d->label_smoothing >= 0.0 && d->label_smoothing <= 0.5)) return RAPID_ERR_INVALID_ARG;
+    const uint32_t form = d->flags & (RAPID_PREF_HINGE | RAPID_PREF_SQUARED);
+    if (form == (RAPID_PREF_HINGE | RAPID_PREF_SQUARED) || (form && d->label_smoothing != 0.0)) return RAPID_ERR_INVALID_ARG;
+    const rapid_status_t s = check_shape((int64_t)d->n_seq * d->seq_len, d->vocab, d->dtype, d->ld, d->ld_grad, d->flags,
+                                         RAPID_LOSS_NORM_GIVEN | RAPID_PREF_HINGE | RAPID_PREF_SQUARED | RAPID_PREF_TOKEN_MEAN, d->scale,
+                                         d->norm_z);
+    if (s != RAPID_OK) return s;
+    return d->n_pairs > (1 << 20) ? RAPID_ERR_UNSUPPORTED : RAPID_OK;
+}
+size_t carve_pref(const rapid_pref_desc_t& d, void* base, Scratch* w) {
+    return carve((int64_t)d.n_seq * d.seq_len, d.n_seq, d.n_pairs, NEED_SEQ | NEED_PAIRS, base, w);
+}
+
+rapid_status_t check_distill(const rapid_distill_desc_t* d) {
+    if (!d || d->k <= 0 || d->ld_top < d->k) return RAPID_ERR_INVALID_ARG;
+    if (!(d->temperature > 0.0) || !isfinite(d->temperature)) return RAPID_ERR_INVALID_ARG;
+    const rapid_status_t s = check_shape(d->n_rows, d->vocab, d->dtype, d->ld, d->ld_grad, d->flags, RAPID_LOSS_NORM_GIVEN, d->scale, d->norm_z);
+    if (s != RAPID_OK) return s;
+    if (d->k > kMaxList || d->ld_top > (1ll << 56) / d->n_rows) return RAPID_ERR_UNSUPPORTED;
+    return d->temperature < 1e-3 || d->temperature > 1e3 ? RAPID_ERR_UNSUPPORTED : RAPID_OK;
+}
+size_t carve_distill(const rapid_distill_desc_t& d, void* base, Scratch* w) { return carve(d.n_rows, 0, 0, NEED_TEACHER, base, w); }
+
+inline rapid_status_t cuda_status(cudaError_t e) { return e == cudaSuccess ? RAPID_OK : RAPID_ERR_CUDA; }
+
+}  // namespace
+
+extern "C" {
+
+rapid_status_t rapid_clip_loss_workspace_bytes(const rapid_clip_desc_t* desc, size_t* bytes) {
+    if (!bytes) return RAPID_ERR_INVALID_ARG;
+    const rapid_status_t s = check_clip(desc);
+    if (s == RAPID_OK) *bytes = carve_clip(*desc, nullptr, nullptr);
+    return s;
+}
+
+rapid_status_t rapid_clip_loss(const rapid_clip_desc_t* desc, const void* logits, const int32_t* targets, const uint8_t* mask,
+                               const float* old_logp, const float* ref_logp, const float* adv, void* dlogits, float* loss,
+                               float* token_logp, rapid_loss_stats_t* stats, void* workspace, size_t workspace_bytes, void* stream) {
+    rapid_status_t s = check_clip(desc);
+    if (s != RAPID_OK) return s;
+    const rapid_clip_desc_t& d = *desc;
+    const int64_t T = (int64_t)d.n_seq * d.seq_len;
+    if (!targets || !old_logp || !adv || !loss || (!ref_logp && d.kl_beta != 0.0)) return RAPID_ERR_INVALID_ARG;
+    if ((s = check_matrices(logits, dlogits, T, d.vocab, d.dtype, d.ld, d.ld_grad)) != RAPID_OK) return s;
+    if (!arrays_aligned(targets, old_logp, ref_logp, adv, loss, token_logp, stats)) return RAPID_ERR_ALIGNMENT;
+    if ((s = check_scratch(workspace, workspace_bytes, carve_clip(d, nullptr, nullptr))) != RAPID_OK) return s;
+    Scratch w;
+    carve_clip(d, workspace, &w);
+    int sms = 0;
+    if ((s = check_device(&sms)) != RAPID_OK) return s;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int blocks = 0;
+    if (launch_prepare_tokens(d.n_seq, d.seq_len, d.vocab, targets, mask, w, (d.flags & RAPID_LOSS_NORM_SEQ) != 0, &blocks, st) != cudaSuccess)
+        return RAPID_ERR_CUDA;
+    const ClipOp op{targets, old_logp, ref_logp, adv, w.seq_rows, w.counts, blocks, d.n_seq, d.seq_len, d.flags, d.eps_low, d.eps_high,
+                    d.kl_beta, d.scale, d.norm_z};
+    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, 0, make_factor(1.0), w};
+    if (launch_rows(a, op, sms, st) != cudaSuccess) return RAPID_ERR_CUDA;
+    clip_sum_kernel<<<sum_blocks(T), kThreads, 0, st>>>(op, T, token_logp, loss, stats, w);
+    return cuda_status(cudaGetLastError());
+}
+
+rapid_status_t rapid_preference_loss_workspace_bytes(const rapid_pref_desc_t* desc, size_t* bytes) {
+    if (!bytes) return RAPID_ERR_INVALID_ARG;
+    const rapid_status_t s = check_pref(desc);
+    if (s == RAPID_OK) *bytes = carve_pref(*desc, nullptr, nullptr);
+    return s;
+}
+
+rapid_status_t rapid_preference_loss(const rapid_pref_desc_t* desc, const void* logits, const int32_t* targets, const uint8_t* mask,
+                                     const int32_t* pairs, const float* ref_logp, void* dlogits, float* loss, float* margins,
+                                     float* token_logp, rapid_loss_stats_t* stats, void* workspace, size_t workspace_bytes,
+                                     void* stream) {
+    rapid_status_t s = check_pref(desc);
+    if (s != RAPID_OK) return s;
+    const rapid_pref_desc_t& d = *desc;
+    const int64_t T = (int64_t)d.n_seq * d.seq_len;
+    if (!targets || !pairs || !loss) return RAPID_ERR_INVALID_ARG;
+    if ((s = check_matrices(logits, dlogits, T, d.vocab, d.dtype, d.ld, d.ld_grad)) != RAPID_OK) return s;
+    if (!arrays_aligned(targets, pairs, ref_logp, loss, margins, token_logp, stats)) return RAPID_ERR_ALIGNMENT;
+    if ((s = check_scratch(workspace, workspace_bytes, carve_pref(d, nullptr, nullptr))) != RAPID_OK) return s;
+    Scratch w;
+    carve_pref(d, workspace, &w);
+    int sms = 0;
+    if ((s = check_device(&sms)) != RAPID_OK) return s;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int blocks = 0;
+    if (launch_prepare_tokens(d.n_seq, d.seq_len, d.vocab, targets, mask, w, 0, &blocks, st) != cudaSuccess) return RAPID_ERR_CUDA;
+    const PrefOp op{targets, w.seq_coef, d.seq_len};
+    RowsArgs a{logits, nullptr, d.ld, d.ld_grad, T, d.vocab, d.dtype, 0, make_factor(1.0), w};
+    if (launch_rows(a, op, sms, st) != cudaSuccess) return RAPID_ERR_CUDA;
+    const PairArgs pa{pairs, d.n_pairs, d.n_seq, d.flags, d.beta, d.margin, d.label_smoothing, d.scale, d.norm_z};
+    pref_seq_kernel<<<d.n_seq, kThreads, 0, st>>>(d.seq_len, d.flags, ref_logp, token_logp, w);
+    pref_pairs_kernel<<<1, kPairThreads, 0, st>>>(pa, blocks, margins, loss, stats, w);
+    if (cudaGetLastError() != cudaSuccess) return RAPID_ERR_CUDA;
+    if (!dlogits) return RAPID_OK;
+    pref_coef_kernel<<<(unsigned)(((int64_t)d.n_seq + kWarps - 1) / kWarps), kThreads, 0, st>>>(pa, w);
+    if (cudaGetLastError() != cudaSuccess) return RAPID_ERR_CUDA;
+    a.grad = dlogits;
+    a.known = 1;
+    return cuda_status(launch_rows(a, op, sms, st));
+}
+
+rapid_status_t rapid_distill_loss_workspace_bytes(const rapid_distill_desc_t* desc, size_t* bytes) {
+    if (!bytes) return RAPID_ERR_INVALID_ARG;
+    const rapid_status_t s = check_distill(desc);
+    if (s == RAPID_OK) *bytes = carve_distill(*desc, nullptr, nullptr);
+    return s;
+}
+
+rapid_status_t rapid_distill_loss(const rapid_distill_desc_t* desc, const void* logits, const int32_t* top_index, const float* top_logit,
+                                  const float* top_lse, const uint8_t* mask, void* dlogits, float* loss, float* token_loss,
+                                  rapid_loss_stats_t* stats, void* workspace, size_t workspace_bytes, void* stream) {
+    rapid_status_t s = check_distill(desc);
+    if (s != RAPID_OK) return s;
+    const rapid_distill_desc_t& d = *desc;
+    if (!top_index || !top_logit || !loss) return RAPID_ERR_INVALID_ARG;
+    if ((s = check_matrices(logits, dlogits, d.n_rows, d.vocab, d.dtype, d.ld, d.ld_grad)) != RAPID_OK) return s;
+    if (!arrays_aligned(top_index, top_logit, top_lse, loss, token_loss, nullptr, stats)) return RAPID_ERR_ALIGNMENT;
+    if ((s = check_scratch(workspace, workspace_bytes, carve_distill(d, nullptr, nullptr))) != RAPID_OK) return s;
+    Scratch w;
+    carve_distill(d, workspace, &w);
+    int sms = 0;
+    if ((s = check_device(&sms)) != RAPID_OK) return s;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const Factor f = make_factor(d.temperature);
+    const int64_t b = (d.n_rows + 4 * kWarps - 1) / (4 * kWarps);
+    const int blocks = (int)(b < kPrepBlocks ? b : kPrepBlocks);
+    prepare_lists_kernel<<<blocks, kThreads, 0, st>>>(d.n_rows, d.vocab, d.k, d.ld_top, f.kd, top_index, top_logit, top_lse, mask, w);
+    if (cudaGetLastError() != cudaSuccess) return RAPID_ERR_CUDA;
+    const DistillOp op{top_index, top_logit, w.teacher_lse2, w.counts, d.ld_top, d.k, top_lse != nullptr, blocks, d.flags, 1.0 / d.temperature,
+                       d.scale, d.norm_z, f.kd};
+    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, d.n_rows, d.vocab, d.dtype, 0, f, w};
+    if (launch_rows(a, op, sms, st) != cudaSuccess) return RAPID_ERR_CUDA;
+    distill_sum_kernel<<<sum_blocks(d.n_rows), kThreads, 0, st>>>(op, d.n_rows, token_loss, loss, stats, w);
+    return cuda_status(cudaGetLastError());
+}
+
+}  // extern "C"
