@@ -1,125 +1,431 @@
-// The rows of the losses of rapid_losses.h: one block for each row, which reads it twice and writes its gradient.
+// The rows of the losses of rapid_losses.h, where a row is long: a block holds a whole row on its SM.
+//
+// Roles of a block: one producer warp draws rows from a counter and streams them into a ring of shared-memory stages with bulk
+// copies (rows that do not count it fills with zeros itself); kWarps consumer warps read the stages; one warp does what is done once
+// a row: it gathers the chosen columns' logits ahead of time, joins the consumers' sums and computes the row's factor in double.
+//
+// A row's first reading takes its maximum and sum of exponentials chunk by chunk.  What fits stays: the first kKeep chunks in the
+// consumers' registers, the last ones in their stages, so that the second reading, which writes the gradient, needs no memory
+// traffic and hands its stages to the next row's loads as it goes.  Only of rows that are longer still are the chunks in between
+// loaded again.
+//
+// Every wait on a barrier is bounded; a wait that gives up raises RAPID_ERR_TIMEOUT in the scratch and never traps.
 #include "loss_rows.cuh"
+#include "tma_pipe.cuh"
 
 namespace rapid {
 namespace losses {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kVecs = 2;         // 16-byte vectors of a thread in a chunk
+constexpr int kMaxStages = 32;
+constexpr int kQueue = kMaxStages + 4;  // rows that are known to the block at a time, at most
 
-template <int DT, class Op>
-__global__ void __launch_bounds__(kThreads) rows_kernel(RowsArgs a, Op op) {
+struct RingShape {
+    int stages;   // of kWarps KB each
+    int chunks;   // of a row
+    int again;    // chunks of a row that are loaded a second time
+    int batch;    // rows drawn at a time
+    int list;     // chosen columns of a row, rounded up
+    unsigned long long stride;
+};
+
+// Shared memory of one row's chosen columns: column, key, logit, value.
+struct Slot {
+    int *col, *key;
+    float *z, *x;
+};
+__device__ __forceinline__ Slot slot_at(uint8_t* base, int list) {
+    int* p = reinterpret_cast<int*>(base);
+    return Slot{p, p + list, reinterpret_cast<float*>(p + 2 * list), reinterpret_cast<float*>(p + 3 * list)};
+}
+
+__device__ __forceinline__ void bulk_load_once(void* smem_dst, const void* gsrc, uint32_t bytes, uint64_t* bar, uint64_t policy) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(smem_u32(smem_dst)),
+                 "l"(gsrc), "r"(bytes), "r"(smem_u32(bar)), "l"(policy)
+                 : "memory");
+}
+__device__ __forceinline__ uint64_t policy_first() {
+    uint64_t p;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+
+// By a whole warp; the lanes agree, so that all of them stay or all leave.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag));
+}
+
+template <int DT, class Op, int kWarps, int kKeep, int kBlocks>
+__global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsArgs a, Op op, RingShape sh) {
     using E = Elem<DT>;
     using T = typename E::T;
-    extern __shared__ uint32_t left_out[];  // a bit for each column that the sum leaves out
-    __shared__ WarpPart parts[kThreads / 32];
-    __shared__ float z[kMaxList], value[kMaxList];
-    __shared__ RowGrad grad;
-    __shared__ float row_max;
+    constexpr int kLanes = kWarps * 32;          // consumer threads
+    constexpr int kChunkVecs = kLanes * kVecs;   // vectors of a chunk
+    constexpr int kChunk = kChunkVecs * 16;
+    extern __shared__ __align__(128) uint8_t dyn[];
+    __shared__ __align__(8) uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], row_bar[kQueue], list_bar[2], parts_bar[2], grad_bar[2];
+    __shared__ long long row_q[kQueue];
+    __shared__ WarpPart parts[2][kWarps];
+    __shared__ RowGrad grads[2];
+    __shared__ float maxima[2];
+    __shared__ int abort_flag;
+    uint8_t* ring = dyn;
+    uint8_t* slots = dyn + (size_t)sh.stages * kChunk;
+    const int slot_bytes = sh.list * 16;
+
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const bool ex = exclude(op) && !a.known;
-    const int nvec = a.vocab / E::kPer;
-    long long rows = 0;
-    if (warp == 0 && op_counts(op)) rows = rows_that_count(op_counts(op), op_blocks(op));
-    if (ex)
-        for (int i = tid; i < (a.vocab + 31) / 32; i += kThreads) left_out[i] = 0;
-    for (int64_t r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
-        const T* row = static_cast<const T*>(a.logits) + r * a.ld;
-        T* out = static_cast<T*>(a.grad) + r * a.ld_grad;
-        if (a.w.state[r] != ROW_OK) {
-            if (a.grad)
-                for (int v = tid; v < a.vocab; v += kThreads) out[v] = E::put(0.f);
-            if (!a.known && tid == 0) a.w.value[r] = 0.0;
-            continue;
+    if (tid == 0) {
+        for (int s = 0; s < sh.stages; ++s) {
+            mbar_init(&full_bar[s], 1);
+            mbar_init(&empty_bar[s], kWarps);
         }
-        const int n_list = list_size(op);
-        __syncthreads();
-        for (int j = tid; j < n_list; j += kThreads) {
-            const int v = column(op, r, j);
-            if (v >= 0) {
-                z[j] = E::get(row[v]);
-                if (ex) atomicOr(&left_out[v >> 5], 1u << (v & 31));
+        for (int q = 0; q < kQueue; ++q) mbar_init(&row_bar[q], 1);
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&list_bar[s], 1);
+            mbar_init(&parts_bar[s], kWarps);
+            mbar_init(&grad_bar[s], 1);
+        }
+        abort_flag = 0;
+        mbar_init_fence();
+    }
+    __syncthreads();
+    volatile int* abortp = &abort_flag;
+
+    const bool stats = !a.known, grad = a.grad != nullptr;
+    const int readings = stats && grad ? 2 : 1;
+    const int nvec = a.vocab / E::kPer, rest = a.vocab - nvec * E::kPer;
+    const int keep = readings == 2 ? kKeep : 0;  // chunks that stay in registers
+
+    if (warp == kWarps) {
+        // ------------------------------- producer -------------------------------------------
+        const int load_bytes = (nvec + (rest ? 1 : 0)) * 16;  // inside the row: its pitch is a multiple of 16 bytes
+        const uint64_t first = policy_first();
+        uint32_t it = 0, q = 0;
+        bool ok = true;
+        auto load = [&](const uint8_t* src, int c) {  // chunk c into the next stage
+            const int s = it % sh.stages;
+            const uint32_t use = it / sh.stages;
+            if (use > 0 && !warp_wait(&empty_bar[s], (use & 1u) ^ 1u, abortp)) return false;
+            if (lane == 0) {
+                const int bytes = min(kChunk, load_bytes - c * kChunk);
+                mbar_arrive_expect_tx(&full_bar[s], (uint32_t)bytes);
+                bulk_load_once(ring + (size_t)s * kChunk, src + (size_t)c * kChunk, (uint32_t)bytes, &full_bar[s], first);
             }
-        }
-        __syncthreads();
-        RowStat st;
-        if (!a.known) {
-            const float off = shift_fraction(warp);
-            Part p;
-            for (int v = tid; v < nvec; v += kThreads) {
-                uint4 q[1] = {reinterpret_cast<const uint4*>(row)[v]};
-                if (ex) {
-                    T* e = reinterpret_cast<T*>(q);
-                    const uint32_t bits = left_out[v * E::kPer >> 5] >> (v * E::kPer & 31);
-#pragma unroll
-                    for (int i = 0; i < E::kPer; ++i)
-                        if (bits >> i & 1u) e[i] = E::put(-INFINITY);
+            ++it;
+            return true;
+        };
+        auto publish = [&](long long r) {
+            if (lane == 0) {
+                row_q[q % kQueue] = r;
+                mbar_arrive(&row_bar[q % kQueue]);
+            }
+            ++q;
+        };
+        while (ok) {
+            unsigned int t = 0;
+            if (lane == 0) t = atomicAdd(&a.w.head->ticket, 1u);
+            t = __shfl_sync(0xffffffffu, t, 0);
+            const int64_t d = (int64_t)t * sh.batch;
+            if (d >= a.n_rows) break;
+            int64_t mine = -1;
+            uint8_t st = ROW_MASKED;
+            if (lane < sh.batch && d + lane < a.n_rows) {
+                mine = (int64_t)(((unsigned long long)(d + lane) * sh.stride) % (unsigned long long)a.n_rows);
+                st = a.w.state[mine];
+            }
+            for (int i = 0; i < sh.batch && ok; ++i) {
+                const int64_t r = __shfl_sync(0xffffffffu, mine, i);
+                const int state = __shfl_sync(0xffffffffu, (int)st, i);
+                if (r < 0) break;
+                if (state != ROW_OK) {  // nobody reads this row
+                    if (grad) {
+                        T* out = static_cast<T*>(a.grad) + r * a.ld_grad;
+                        for (int v = lane; v < nvec; v += 32) st_stream(reinterpret_cast<uint4*>(out) + v, make_uint4(0, 0, 0, 0));
+                        if (lane < rest) out[nvec * E::kPer + lane] = E::put(0.f);
+                    }
+                    if (stats && lane == 0) a.w.value[r] = 0.0;
+                    continue;
                 }
-                p.template vectors<DT, 1>(q, off, a.f);
+                const uint8_t* src = static_cast<const uint8_t*>(a.logits) + (size_t)r * a.ld * sizeof(T);
+                publish(r);
+                for (int c = 0; c < sh.chunks && ok; ++c) ok = load(src, c);
+                for (int c = keep; c < keep + sh.again && ok; ++c) ok = load(src, c);
             }
-            const int e = nvec * E::kPer + tid;
-            if (e < a.vocab && !(ex && (left_out[e >> 5] >> (e & 31) & 1u))) p.scalar(E::get(row[e]), off, a.f);
-            const WarpPart w = warp_part(p, a.f);
-            if (lane == 0) parts[warp] = w;
-            __syncthreads();
-            if (warp == 0) {
+        }
+        if (ok) publish(-1);
+        __syncwarp();
+        if (!ok || *abortp) {  // gave up: let the copies already issued land before the block's memory goes away
+            const uint32_t from = it > (uint32_t)sh.stages ? it - sh.stages : 0u;
+            for (uint32_t j = from; j < it; ++j) {
+                const unsigned long long t0 = global_timer_ns();
+                while (!mbar_try_wait(&full_bar[j % sh.stages], (j / sh.stages) & 1u))
+                    if (global_timer_ns() - t0 > kWaitLimitNs) break;
+            }
+        }
+    } else if (warp == kWarps + 1) {
+        // ------------------------------- once a row -----------------------------------------
+        const long long rows = op_counts(op) ? rows_that_count(op_counts(op), op_blocks(op)) : 0;
+        const int n = list_size(op);
+        for (uint32_t jq = 0;; ++jq) {
+            if (!warp_wait(&row_bar[jq % kQueue], (jq / kQueue) & 1u, abortp)) break;
+            const int64_t r = row_q[jq % kQueue];
+            if (r < 0) break;
+            const int s = jq & 1;
+            const uint32_t ph = (jq >> 1) & 1u;
+            // the consumers are through with this slot's last row, the one before the last: with sums to join, all of them have
+            // begun the last row, whose sums are in; without, they say so
+            if (!stats && jq >= 2 && !warp_wait(&parts_bar[s], ph ^ 1u, abortp)) break;
+            const Slot slot = slot_at(slots + s * slot_bytes, sh.list);
+            const T* row = static_cast<const T*>(a.logits) + r * a.ld;
+            for (int j = lane; j < sh.list; j += 32) {
+                const int v = j < n ? column(op, r, j) : -1;
+                int key = -1;
+                if (v >= 0) {
+                    const int vec = v / E::kPer;
+                    key = vec / kChunkVecs * kWarps + vec % kLanes / 32;
+                    slot.z[j] = E::get(row[v]);
+                    slot.x[j] = entry(op, r, j);
+                }
+                slot.col[j] = v;
+                slot.key[j] = key;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&list_bar[s]);
+            const auto ahead = look(op, a, r, rows);
+            RowStat st = known_stat(ahead);
+            if (stats) {
+                if (!warp_wait(&parts_bar[s], ph, abortp)) break;
                 WarpPart mine{-INFINITY, -INFINITY, 0.0};
-                if (lane < kThreads / 32) mine = parts[lane];
+                if (lane < kWarps) mine = parts[s][lane];
                 st = join_parts(mine, a.f);
             }
-        } else {
-            st.lse2 = a.w.lse2[r];
-            st.max = a.w.row_max[r];
-        }
-        if (warp == 0) {
-            const RowGrad g = finish(op, a, r, st, z, value, rows);
+            const RowGrad g = finish(op, a, r, ahead, st, slot.col, slot.z, slot.x);
             if (lane == 0) {
-                grad = g;
-                row_max = st.max;
+                grads[s] = g;
+                maxima[s] = st.max;
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&grad_bar[s]);
         }
-        __syncthreads();
-        if (ex)
-            for (int j = tid; j < n_list; j += kThreads) {
-                const int v = column(op, r, j);
-                if (v >= 0) left_out[v >> 5] = 0;
+    } else {
+        // ------------------------------- consumers ------------------------------------------
+        const float off = shift_fraction(warp);
+        const bool ex = exclude(op) && stats;
+        int st = 0;
+        uint32_t ph = 0;
+        auto next_stage = [&]() {
+            if (++st == sh.stages) {
+                st = 0;
+                ph ^= 1u;
             }
-        if (a.grad) {
+        };
+        auto give_back = [&](int s) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&empty_bar[s]);
+        };
+        // this thread's vectors of chunk c from stage s; columns behind the last read as -inf
+        auto read = [&](int c, int s, uint4 (&v)[kVecs]) {
+            const uint4* sv = reinterpret_cast<const uint4*>(ring + (size_t)s * kChunk) + tid;
+            const int v0 = c * kChunkVecs + tid;
+            if ((c + 1) * kChunkVecs <= nvec) {
+#pragma unroll
+                for (int j = 0; j < kVecs; ++j) v[j] = sv[j * kLanes];
+            } else {
+#pragma unroll
+                for (int j = 0; j < kVecs; ++j) {
+                    constexpr uint32_t kNone = DT == RAPID_BF16 ? 0xff80ff80u : 0xff800000u;
+                    v[j] = make_uint4(kNone, kNone, kNone, kNone);
+                    const int at = v0 + j * kLanes;
+                    if (at < nvec) v[j] = sv[j * kLanes];
+                    else if (at == nvec && rest) {
+                        const T* e = reinterpret_cast<const T*>(sv + j * kLanes);
+                        uint32_t w[4] = {kNone, kNone, kNone, kNone};
+#pragma unroll
+                        for (int i = 0; i < E::kPer; ++i) {
+                            if (i >= rest) continue;
+                            if constexpr (DT == RAPID_BF16) {
+                                const uint32_t b = e[i];
+                                w[i / 2] = (i & 1) ? ((w[i / 2] & 0xffffu) | (b << 16)) : ((w[i / 2] & 0xffff0000u) | b);
+                            } else {
+                                w[i] = __float_as_uint(e[i]);
+                            }
+                        }
+                        v[j] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+            }
+        };
+        for (uint32_t jq = 0;; ++jq) {
+            if (!warp_wait(&row_bar[jq % kQueue], (jq / kQueue) & 1u, abortp)) break;
+            const int64_t r = row_q[jq % kQueue];
+            if (r < 0) break;
+            const int slot_i = jq & 1;
+            const uint32_t sph = (jq >> 1) & 1u;
+            const Slot slot = slot_at(slots + slot_i * slot_bytes, sh.list);
+            bool ok = true;
+            if (ex) ok = warp_wait(&list_bar[slot_i], sph, abortp);
+            uint4 kept[kKeep > 0 ? kKeep : 1][kVecs];
+            int held = 0;  // stage of the first chunk that stays
+            Part p;
+            // first reading of chunk c
+            auto first = [&](int c, uint4 (&v)[kVecs], bool stays) {
+                const int s = st;
+                if (!warp_wait(&full_bar[s], ph, abortp)) return false;
+                next_stage();
+                if (ex) {  // the list's columns are left out of the sum
+                    T* e = reinterpret_cast<T*>(ring + (size_t)s * kChunk);
+                    bool wrote = false;
+                    for (int j = lane; j < sh.list; j += 32)
+                        if (slot.key[j] == c * kWarps + warp) {
+                            e[slot.col[j] - c * kChunkVecs * E::kPer] = E::put(-INFINITY);
+                            wrote = true;
+                        }
+                    if (wrote) fence_proxy_async_smem();  // a bulk copy writes this stage next
+                    __syncwarp();
+                }
+                read(c, s, v);
+                if (!stays) give_back(s);
+                p.template vectors<DT, kVecs>(v, off, a.f);
+                return true;
+            };
+            const int held_from = grad ? keep + sh.again : sh.chunks;  // chunks from here on stay in their stages
+            if (stats && ok) {
+                if (keep) {
+#pragma unroll
+                    for (int c = 0; c < kKeep; ++c)
+                        if (ok) ok = first(c, kept[c], false);
+                }
+                for (int c = keep; c < sh.chunks && ok; ++c) {
+                    uint4 v[kVecs];
+                    if (c == held_from) held = st;
+                    ok = first(c, v, c >= held_from);
+                }
+                if (!ok) break;
+                const WarpPart w = warp_part(p, a.f);
+                // two rows ago's sums have been read
+                if (!grad && jq >= 2 && !warp_wait(&grad_bar[slot_i], sph ^ 1u, abortp)) break;
+                if (lane == 0) {
+                    parts[slot_i][warp] = w;
+                    mbar_arrive(&parts_bar[slot_i]);
+                }
+            }
+            if (!ok) break;
+            if (!grad) continue;
+            if (!warp_wait(&grad_bar[slot_i], sph, abortp)) break;
             Grad<DT> gr;
-            gr.set(grad.a, grad.lse2, row_max, a.f);
-            for (int v = tid; v < nvec; v += kThreads)
-                reinterpret_cast<uint4*>(out)[v] = gr.vector(reinterpret_cast<const uint4*>(row)[v]);
-            const int e = nvec * E::kPer + tid;
-            if (e < a.vocab) out[e] = gr.one(row[e]);
-            __syncthreads();
-            for (int j = tid; j < n_list; j += kThreads) {
-                const int v = column(op, r, j);
-                if (v >= 0) out[v] = E::put(value[j]);
+            gr.set(grads[slot_i].a, grads[slot_i].lse2, maxima[slot_i], a.f);
+            T* out = static_cast<T*>(a.grad) + r * a.ld_grad;
+            // second reading: the gradient of chunk c, then the chosen columns over it
+            auto second = [&](int c, const uint4 (&v)[kVecs]) {
+                uint4* ov = reinterpret_cast<uint4*>(out) + c * kChunkVecs + tid;
+                if ((c + 1) * kChunkVecs <= nvec) {
+#pragma unroll
+                    for (int j = 0; j < kVecs; ++j) st_stream(ov + j * kLanes, gr.vector(v[j]));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kVecs; ++j) {
+                        const int at = c * kChunkVecs + tid + j * kLanes;
+                        if (at < nvec) st_stream(ov + j * kLanes, gr.vector(v[j]));
+                        else if (at == nvec && rest) {
+                            const uint4 y = gr.vector(v[j]);
+                            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                            for (int i = 0; i < E::kPer; ++i) {
+                                if (i >= rest) continue;
+                                if constexpr (DT == RAPID_BF16) out[nvec * E::kPer + i] = (T)(w[i / 2] >> (16 * (i & 1)));
+                                else out[nvec * E::kPer + i] = __uint_as_float(w[i]);
+                            }
+                        }
+                    }
+                }
+                __syncwarp();  // the vectors first
+                for (int j = lane; j < sh.list; j += 32)
+                    if (slot.key[j] == c * kWarps + warp) out[slot.col[j]] = E::put(slot.x[j]);
+            };
+            if (stats) {
+                for (int c = held_from; c < sh.chunks; ++c) {
+                    uint4 v[kVecs];
+                    read(c, held, v);
+                    give_back(held);
+                    if (++held == sh.stages) held = 0;
+                    second(c, v);
+                }
+                if (keep) {
+#pragma unroll
+                    for (int c = 0; c < kKeep; ++c) second(c, kept[c]);
+                }
+            }
+            const int from = stats ? keep : 0, to = stats ? keep + sh.again : sh.chunks;
+            for (int c = from; c < to; ++c) {
+                const int s = st;
+                ok = warp_wait(&full_bar[s], ph, abortp);
+                if (!ok) break;
+                next_stage();
+                uint4 v[kVecs];
+                read(c, s, v);
+                give_back(s);
+                second(c, v);
+            }
+            if (!ok) break;
+            if (!stats) {  // the slot is free
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&parts_bar[slot_i]);
             }
         }
+    }
+    __syncthreads();
+    if (tid == 0 && abort_flag) {
+        atomicMax(&a.w.head->status, (int)RAPID_ERR_TIMEOUT);
+        if (a.stats) atomicMax(&a.stats->status, (int)RAPID_ERR_TIMEOUT);
     }
 }
 
 template <class Op>
-cudaError_t launch(const RowsArgs& a, const Op& op, bool ex, int sm_count, cudaStream_t stream) {
-    const size_t smem = ex ? (size_t)(a.vocab + 31) / 32 * 4 : 0;
-    const int64_t grid = a.n_rows < 8ll * sm_count ? a.n_rows : 8ll * sm_count;
-    auto go = [&](auto kern) -> cudaError_t {
+cudaError_t launch(const RowsArgs& a, const Op& op, int list, int sm_count, cudaStream_t stream) {
+    const size_t es = elem_size(a.dtype);
+    const int64_t row_bytes = ((int64_t)a.vocab * es + 15) / 16 * 16;
+    auto go = [&](auto kern, int warps, int keep, int blocks) -> cudaError_t {
+        RingShape sh{};
+        const int chunk = warps * 32 * kVecs * 16;
+        sh.list = (list + 3) / 4 * 4;
+        const size_t extra = 2 * (size_t)sh.list * 16;
+        // 228 KB an SM; of every block 1 KB is the system's and up to 2 KB are barriers and queues
+        const size_t room = (size_t)228 * 1024 / blocks - 3072 - extra;
+        sh.stages = (int)(room / chunk);
+        if (sh.stages > kMaxStages) sh.stages = kMaxStages;
+        sh.chunks = (int)((row_bytes + chunk - 1) / chunk);
+        const bool both = !a.known && a.grad;
+        sh.again = both && sh.chunks > keep + sh.stages ? sh.chunks - keep - sh.stages : 0;
+        const size_t smem = (size_t)sh.stages * chunk + extra;
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
-        kern<<<(unsigned)grid, kThreads, smem, stream>>>(a, op);
+        int64_t grid = (int64_t)sm_count * blocks;
+        sh.batch = (int)(a.n_rows / (grid * 4));
+        if (sh.batch < 1 || chunk >= 16384) sh.batch = 1;
+        if (sh.batch > 8) sh.batch = 8;
+        if (grid > a.n_rows) grid = a.n_rows;
+        sh.stride = scatter_stride(a.n_rows);
+        kern<<<(unsigned)grid, (warps + 2) * 32, smem, stream>>>(a, op, sh);
         return cudaGetLastError();
     };
-    return a.dtype == RAPID_BF16 ? go(rows_kernel<RAPID_BF16, Op>) : go(rows_kernel<RAPID_F32, Op>);
+    auto by_type = [&](auto dt) -> cudaError_t {
+        constexpr int DT = decltype(dt)::value;
+        if (row_bytes <= 16384) return go(ring_kernel<DT, Op, 4, 0, 5>, 4, 0, 5);
+        if (row_bytes <= 65536) return go(ring_kernel<DT, Op, 8, 0, 2>, 8, 0, 2);
+        if (!a.known && a.grad && row_bytes > 10 * 16384) return go(ring_kernel<DT, Op, 16, 6, 1>, 16, 6, 1);
+        return go(ring_kernel<DT, Op, 16, 0, 1>, 16, 0, 1);
+    };
+    return a.dtype == RAPID_BF16 ? by_type(std::integral_constant<int, RAPID_BF16>{}) : by_type(std::integral_constant<int, RAPID_F32>{});
 }
 
 }  // namespace
 
-cudaError_t launch_rows(const RowsArgs& a, const ClipOp& op, int sm_count, cudaStream_t stream) { return launch(a, op, false, sm_count, stream); }
-cudaError_t launch_rows(const RowsArgs& a, const PrefOp& op, int sm_count, cudaStream_t stream) { return launch(a, op, false, sm_count, stream); }
+cudaError_t launch_rows(const RowsArgs& a, const ClipOp& op, int sm_count, cudaStream_t stream) { return launch(a, op, 1, sm_count, stream); }
+cudaError_t launch_rows(const RowsArgs& a, const PrefOp& op, int sm_count, cudaStream_t stream) { return launch(a, op, 1, sm_count, stream); }
 cudaError_t launch_rows(const RowsArgs& a, const DistillOp& op, int sm_count, cudaStream_t stream) {
-    return launch(a, op, op.tail != 0 && !a.known, sm_count, stream);
+    return launch(a, op, op.k, sm_count, stream);
 }
 
 }  // namespace losses

@@ -364,6 +364,7 @@ struct RowsArgs {
     int known;   // the statistics are in the scratch already: gradient only
     Factor f;
     Scratch w;
+    rapid_loss_stats_t* stats;  // written before the rows: a wait that gives up is reported here too (may be NULL)
 };
 
 struct ClipOp {
@@ -402,22 +403,28 @@ cudaError_t launch_prepare_tokens(int n_seq, int seq_len, int vocab, const int32
 #ifdef __CUDACC__
 
 // The clipped loss of one row and its slope by the log-probability, sign turned: loss' = -slope.
+struct ClipIn {
+    double A, old, ref;
+};
 struct ClipTerms {
     double loss, slope, kl;
     bool cut;
 };
-__device__ __forceinline__ ClipTerms clip_terms(const ClipOp& op, int64_t r, double lp) {
+__device__ __forceinline__ ClipIn clip_in(const ClipOp& op, int64_t r) {
+    return ClipIn{(double)op.adv[(op.flags & RAPID_CLIP_ADV_TOKEN) ? r : r / op.seq_len], (double)op.old_logp[r],
+                  op.ref_logp ? (double)op.ref_logp[r] : 0.0};
+}
+__device__ __forceinline__ ClipTerms clip_terms(const ClipOp& op, const ClipIn& in, double lp) {
     ClipTerms t;
-    const double A = (double)op.adv[(op.flags & RAPID_CLIP_ADV_TOKEN) ? r : r / op.seq_len];
-    const double rho = exp(lp - (double)op.old_logp[r]);
-    const double u = A != 0.0 ? rho * A : 0.0;  // A = 0 leaves nothing, even of an infinite ratio
-    const double v = A != 0.0 ? fmin(fmax(rho, 1.0 - op.low), 1.0 + op.high) * A : 0.0;
+    const double rho = exp(lp - in.old);
+    const double u = in.A != 0.0 ? rho * in.A : 0.0;  // A = 0 leaves nothing, even of an infinite ratio
+    const double v = in.A != 0.0 ? fmin(fmax(rho, 1.0 - op.low), 1.0 + op.high) * in.A : 0.0;
     t.cut = v < u;
     t.loss = t.cut ? -v : -u;
     t.slope = t.cut ? 0.0 : u;
     t.kl = 0.0;
     if (op.ref_logp) {
-        const double d = (double)op.ref_logp[r] - lp, e = expm1(d);
+        const double d = in.ref - lp, e = expm1(d);
         t.kl = isinf(e) ? e : e - d;
         if (op.beta != 0.0) {
             t.loss += op.beta * t.kl;
@@ -435,8 +442,10 @@ __device__ __forceinline__ double clip_weight(const ClipOp& op, int64_t r, long 
     return op.scale / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows);
 }
 
-// finish(): by one warp, once a row's log-sum-exp is there (without the chosen columns where exclude() says so).  z[j] are the
-// chosen columns' logits, value[j] becomes their gradient.  Writes what the operator keeps of the row to the scratch.
+// What an operator does with a row, by one warp.  look() loads what it needs of the row beside its logits, ahead of time; finish()
+// is called once the row's log-sum-exp is there (without the chosen columns where exclude() says so).  col[j] and z[j] are the chosen
+// columns and their logits; x[j], for distillation the teacher's logits, become the columns' gradient.  finish() writes what is
+// kept of the row to the scratch.
 __device__ __forceinline__ int list_size(const ClipOp&) { return 1; }
 __device__ __forceinline__ int list_size(const PrefOp&) { return 1; }
 __device__ __forceinline__ int list_size(const DistillOp& op) { return op.k; }
@@ -452,78 +461,98 @@ __device__ __forceinline__ bool exclude(const DistillOp& op) { return op.tail !=
 __device__ __forceinline__ int column(const ClipOp& op, int64_t r, int) { return op.targets[r]; }
 __device__ __forceinline__ int column(const PrefOp& op, int64_t r, int) { return op.targets[r]; }
 __device__ __forceinline__ int column(const DistillOp& op, int64_t r, int j) { return op.index[r * op.ld + j]; }
+__device__ __forceinline__ float entry(const ClipOp&, int64_t, int) { return 0.f; }
+__device__ __forceinline__ float entry(const PrefOp&, int64_t, int) { return 0.f; }
+__device__ __forceinline__ float entry(const DistillOp& op, int64_t r, int j) { return op.logit[r * op.ld + j]; }
 
-__device__ __forceinline__ RowGrad finish(const ClipOp& op, const RowsArgs& a, int64_t r, const RowStat& st, const float* z, float* value,
-                                          long long rows) {
+struct ClipRow {
+    ClipIn in;
+    double w;
+};
+__device__ __forceinline__ ClipRow look(const ClipOp& op, const RowsArgs&, int64_t r, long long rows) {
+    return ClipRow{clip_in(op, r), clip_weight(op, r, rows)};
+}
+struct PrefRow {
+    double a;
+    RowStat st;
+};
+__device__ __forceinline__ PrefRow look(const PrefOp& op, const RowsArgs& a, int64_t r, long long) {
+    PrefRow p{0.0, {0.0, 0.f}};
+    if (a.known) p = PrefRow{op.seq_coef[r / op.seq_len], {a.w.lse2[r], a.w.row_max[r]}};
+    return p;
+}
+struct DistillRow {
+    double teacher, w;
+};
+__device__ __forceinline__ DistillRow look(const DistillOp& op, const RowsArgs&, int64_t r, long long rows) {
+    return DistillRow{op.teacher_lse2[r], op.scale * op.inv_tau / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows)};
+}
+__device__ __forceinline__ RowStat known_stat(const ClipRow&) { return RowStat{0.0, 0.f}; }
+__device__ __forceinline__ RowStat known_stat(const PrefRow& p) { return p.st; }
+__device__ __forceinline__ RowStat known_stat(const DistillRow&) { return RowStat{0.0, 0.f}; }
+
+__device__ __forceinline__ RowGrad finish(const ClipOp& op, const RowsArgs& a, int64_t r, const ClipRow& row, const RowStat& st, const int*,
+                                          const float* z, float* x) {
     const double lp = ((double)z[0] * a.f.kd - st.lse2) * kLn2D;
-    RowGrad g;
-    g.lse2 = st.lse2;
-    g.a = 0.0;
+    RowGrad g{0.0, st.lse2};
     if (a.grad) {
-        g.a = clip_weight(op, r, rows) * clip_terms(op, r, lp).slope;
-        if ((threadIdx.x & 31) == 0) value[0] = (float)(g.a * expm1(lp));
+        g.a = row.w * clip_terms(op, row.in, lp).slope;
+        if ((threadIdx.x & 31) == 0) x[0] = (float)(g.a * expm1(lp));
     }
     if ((threadIdx.x & 31) == 0) a.w.value[r] = lp;
     return g;
 }
 
-__device__ __forceinline__ RowGrad finish(const PrefOp& op, const RowsArgs& a, int64_t r, const RowStat& st, const float* z, float* value,
-                                          long long) {
+__device__ __forceinline__ RowGrad finish(const PrefOp& op, const RowsArgs& a, int64_t r, const PrefRow& row, const RowStat& st, const int*,
+                                          const float* z, float* x) {
     const double lp = ((double)z[0] * a.f.kd - st.lse2) * kLn2D;
-    RowGrad g;
-    g.lse2 = st.lse2;
-    g.a = 0.0;
     if (a.known) {
-        g.a = op.seq_coef[r / op.seq_len];
-        if ((threadIdx.x & 31) == 0) value[0] = (float)(g.a * expm1(lp));
+        if ((threadIdx.x & 31) == 0) x[0] = (float)(row.a * expm1(lp));
     } else if ((threadIdx.x & 31) == 0) {
         a.w.value[r] = lp;
         a.w.lse2[r] = st.lse2;
         a.w.row_max[r] = st.max;
     }
-    return g;
+    return RowGrad{row.a, st.lse2};
 }
 
-__device__ __forceinline__ RowGrad finish(const DistillOp& op, const RowsArgs& a, int64_t r, const RowStat& st, const float* z, float* value,
-                                          long long rows) {
+__device__ __forceinline__ RowGrad finish(const DistillOp& op, const RowsArgs& a, int64_t r, const DistillRow& row, const RowStat& st,
+                                          const int* col, const float* z, float* x) {
     const int lane = threadIdx.x & 31;
-    const double teacher = op.teacher_lse2[r];
     // the student's log-sum-exp over the whole vocabulary
     double lse2 = st.lse2;
     if (op.tail) {
         double top = lse2;
         for (int j = lane; j < op.k; j += 32)
-            if (column(op, r, j) >= 0) top = fmax(top, (double)z[j] * op.kd);
+            if (col[j] >= 0) top = fmax(top, (double)z[j] * op.kd);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, o));
         double s = 0.0;
         if (top > -INFINITY) {
             if (lane == 0) s = exp2(lse2 - top);
             for (int j = lane; j < op.k; j += 32)
-                if (column(op, r, j) >= 0) s += exp2((double)z[j] * op.kd - top);
+                if (col[j] >= 0) s += exp2((double)z[j] * op.kd - top);
         }
         s = warp_sum(s);
         lse2 = s > 0.0 ? top + log2(s) : -INFINITY;
     }
-    const double w = op.scale * op.inv_tau / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows);
     double loss = 0.0, mass = 0.0;
     for (int j = lane; j < op.k; j += 32) {
-        if (column(op, r, j) < 0) continue;
-        const double lt = (double)op.logit[r * op.ld + j] * op.kd - teacher, lq = (double)z[j] * op.kd - lse2;
+        if (col[j] < 0) continue;
+        const double lt = (double)x[j] * op.kd - row.teacher, lq = (double)z[j] * op.kd - lse2;
         const double p = exp2(lt);
         if (p > 0.0) loss += p * (lt - lq);
         mass += p;
-        if (a.grad) value[j] = (float)(w * (exp2(lq) - p));
+        x[j] = (float)(row.w * (exp2(lq) - p));
     }
     loss = warp_sum(loss);
-    RowGrad g;
-    g.lse2 = lse2;
-    g.a = w;
+    RowGrad g{row.w, lse2};
     if (op.tail) {
         const double p0 = 1.0 - warp_sum(mass), l0 = st.lse2 - lse2;
         if (p0 > 0.0) {
-            loss += p0 * (log2(p0) - l0);
-            if (st.lse2 > -INFINITY) g.a = w * (1.0 - exp2(log2(p0) - l0));
+            const double lp0 = log2(p0);
+            loss += p0 * (lp0 - l0);
+            if (st.lse2 > -INFINITY) g.a = row.w * (1.0 - exp2(lp0 - l0));
         }
     }
     if (lane == 0) a.w.value[r] = loss * kLn2D;

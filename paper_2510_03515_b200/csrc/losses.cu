@@ -180,9 +180,10 @@ clip_sum_kernel(ClipOp op, int64_t n_rows, float* __restrict__ token_logp, float
         double lp = 0.0;
         if (w.state[r] == ROW_OK) {
             lp = w.value[r];
-            const ClipTerms t = clip_terms(op, r, lp);
+            const ClipIn in = clip_in(op, r);
+            const ClipTerms t = clip_terms(op, in, lp);
             mine[0] += clip_weight(op, r, rows) * t.loss;
-            mine[1] += lp - (double)op.old_logp[r];
+            mine[1] += lp - in.old;
             mine[2] += t.kl;
             mine[3] += t.cut ? 1.0 : 0.0;
         }
@@ -293,6 +294,7 @@ pref_pairs_kernel(PairArgs a, int count_blocks, float* __restrict__ margins, flo
     const double z = (a.flags & RAPID_LOSS_NORM_GIVEN) ? a.norm_z : (double)valid;
     const double l = valid > 0 ? a.scale * sum / z : 0.0;
     w.sums[0] = valid > 0 ? a.scale * a.beta / z : 0.0;  // what the slopes are multiplied by
+    w.head->ticket = 0;  // the rows are handed out once more
     *loss = (float)l;
     if (stats) {
         const double n = valid > 0 ? (double)valid : 1.0;
@@ -419,7 +421,7 @@ rapid_status_t rapid_clip_loss(const rapid_clip_desc_t* desc, const void* logits
         return RAPID_ERR_CUDA;
     const ClipOp op{targets, old_logp, ref_logp, adv, w.seq_rows, w.counts, blocks, d.n_seq, d.seq_len, d.flags, d.eps_low, d.eps_high,
                     d.kl_beta, d.scale, d.norm_z};
-    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, 0, make_factor(1.0), w};
+    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, 0, make_factor(1.0), w, nullptr};
     if (launch_rows(a, op, sms, st) != cudaSuccess) return RAPID_ERR_CUDA;
     clip_sum_kernel<<<sum_blocks(T), kThreads, 0, st>>>(op, T, token_logp, loss, stats, w);
     return cuda_status(cudaGetLastError());
@@ -452,7 +454,7 @@ rapid_status_t rapid_preference_loss(const rapid_pref_desc_t* desc, const void* 
     int blocks = 0;
     if (launch_prepare_tokens(d.n_seq, d.seq_len, d.vocab, targets, mask, w, 0, &blocks, st) != cudaSuccess) return RAPID_ERR_CUDA;
     const PrefOp op{targets, w.seq_coef, d.seq_len};
-    RowsArgs a{logits, nullptr, d.ld, d.ld_grad, T, d.vocab, d.dtype, 0, make_factor(1.0), w};
+    RowsArgs a{logits, nullptr, d.ld, d.ld_grad, T, d.vocab, d.dtype, 0, make_factor(1.0), w, nullptr};
     if (launch_rows(a, op, sms, st) != cudaSuccess) return RAPID_ERR_CUDA;
     const PairArgs pa{pairs, d.n_pairs, d.n_seq, d.flags, d.beta, d.margin, d.label_smoothing, d.scale, d.norm_z};
     pref_seq_kernel<<<d.n_seq, kThreads, 0, st>>>(d.seq_len, d.flags, ref_logp, token_logp, w);
@@ -463,6 +465,7 @@ rapid_status_t rapid_preference_loss(const rapid_pref_desc_t* desc, const void* 
     if (cudaGetLastError() != cudaSuccess) return RAPID_ERR_CUDA;
     a.grad = dlogits;
     a.known = 1;
+    a.stats = stats;
     return cuda_status(launch_rows(a, op, sms, st));
 }
 
@@ -495,7 +498,7 @@ rapid_status_t rapid_distill_loss(const rapid_distill_desc_t* desc, const void* 
     if (cudaGetLastError() != cudaSuccess) return RAPID_ERR_CUDA;
     const DistillOp op{top_index, top_logit, w.teacher_lse2, w.counts, d.ld_top, d.k, top_lse != nullptr, blocks, d.flags, 1.0 / d.temperature,
                        d.scale, d.norm_z, f.kd};
-    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, d.n_rows, d.vocab, d.dtype, 0, f, w};
+    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, d.n_rows, d.vocab, d.dtype, 0, f, w, nullptr};
     if (launch_rows(a, op, sms, st) != cudaSuccess) return RAPID_ERR_CUDA;
     distill_sum_kernel<<<sum_blocks(d.n_rows), kThreads, 0, st>>>(op, d.n_rows, token_loss, loss, stats, w);
     return cuda_status(cudaGetLastError());
