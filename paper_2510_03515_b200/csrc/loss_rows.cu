@@ -18,12 +18,12 @@ namespace losses {
 
 namespace {
 
-constexpr int kVecs = 2;         // 16-byte vectors of a thread in a chunk
+constexpr int kVecs = 4;         // 16-byte vectors of a thread in a chunk
 constexpr int kMaxStages = 32;
 constexpr int kQueue = kMaxStages + 4;  // rows that are known to the block at a time, at most
 
 struct RingShape {
-    int stages;   // of kWarps KB each
+    int stages;   // of 2 kWarps KB each
     int chunks;   // of a row
     int again;    // chunks of a row that are loaded a second time
     int batch;    // rows drawn at a time
@@ -225,37 +225,27 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
             __syncwarp();
             if (lane == 0) mbar_arrive(&empty_bar[s]);
         };
-        // this thread's vectors of chunk c from stage s; columns behind the last read as -inf
-        auto read = [&](int c, int s, uint4 (&v)[kVecs]) {
-            const uint4* sv = reinterpret_cast<const uint4*>(ring + (size_t)s * kChunk) + tid;
-            const int v0 = c * kChunkVecs + tid;
-            if ((c + 1) * kChunkVecs <= nvec) {
+        // vector `at` of the row from place `sv`; columns behind the last read as -inf
+        auto read_edge = [&](const uint4* sv, int at) {
+            constexpr uint32_t kNone = DT == RAPID_BF16 ? 0xff80ff80u : 0xff800000u;
+            uint4 v = make_uint4(kNone, kNone, kNone, kNone);
+            if (at < nvec) v = *sv;
+            else if (at == nvec && rest) {
+                const T* e = reinterpret_cast<const T*>(sv);
+                uint32_t w[4] = {kNone, kNone, kNone, kNone};
 #pragma unroll
-                for (int j = 0; j < kVecs; ++j) v[j] = sv[j * kLanes];
-            } else {
-#pragma unroll
-                for (int j = 0; j < kVecs; ++j) {
-                    constexpr uint32_t kNone = DT == RAPID_BF16 ? 0xff80ff80u : 0xff800000u;
-                    v[j] = make_uint4(kNone, kNone, kNone, kNone);
-                    const int at = v0 + j * kLanes;
-                    if (at < nvec) v[j] = sv[j * kLanes];
-                    else if (at == nvec && rest) {
-                        const T* e = reinterpret_cast<const T*>(sv + j * kLanes);
-                        uint32_t w[4] = {kNone, kNone, kNone, kNone};
-#pragma unroll
-                        for (int i = 0; i < E::kPer; ++i) {
-                            if (i >= rest) continue;
-                            if constexpr (DT == RAPID_BF16) {
-                                const uint32_t b = e[i];
-                                w[i / 2] = (i & 1) ? ((w[i / 2] & 0xffffu) | (b << 16)) : ((w[i / 2] & 0xffff0000u) | b);
-                            } else {
-                                w[i] = __float_as_uint(e[i]);
-                            }
-                        }
-                        v[j] = make_uint4(w[0], w[1], w[2], w[3]);
+                for (int i = 0; i < E::kPer; ++i) {
+                    if (i >= rest) continue;
+                    if constexpr (DT == RAPID_BF16) {
+                        const uint32_t b = e[i];
+                        w[i / 2] = (i & 1) ? ((w[i / 2] & 0xffffu) | (b << 16)) : ((w[i / 2] & 0xffff0000u) | b);
+                    } else {
+                        w[i] = __float_as_uint(e[i]);
                     }
                 }
+                v = make_uint4(w[0], w[1], w[2], w[3]);
             }
+            return v;
         };
         for (uint32_t jq = 0;; ++jq) {
             if (!warp_wait(&row_bar[jq % kQueue], (jq / kQueue) & 1u, abortp)) break;
@@ -265,7 +255,20 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
             const uint32_t sph = (jq >> 1) & 1u;
             const Slot slot = slot_at(slots + slot_i * slot_bytes, sh.list);
             bool ok = true;
-            if (ex) ok = warp_wait(&list_bar[slot_i], sph, abortp);
+            // chunks in which this warp has chosen columns, a bit each (the last one for all from 63 on)
+            uint64_t chosen = 0;
+            auto find_chosen = [&]() {
+                uint64_t m = 0;
+                for (int j = lane; j < sh.list; j += 32) {
+                    const int key = slot.key[j];
+                    if (key >= 0 && key % kWarps == warp) m |= 1ull << min(key / kWarps, 63);
+                }
+                chosen = (uint64_t)__reduce_or_sync(0xffffffffu, (unsigned)(m >> 32)) << 32 | __reduce_or_sync(0xffffffffu, (unsigned)m);
+            };
+            if (ex) {
+                ok = warp_wait(&list_bar[slot_i], sph, abortp);
+                if (ok) find_chosen();
+            }
             uint4 kept[kKeep > 0 ? kKeep : 1][kVecs];
             int held = 0;  // stage of the first chunk that stays
             Part p;
@@ -274,20 +277,29 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
                 const int s = st;
                 if (!warp_wait(&full_bar[s], ph, abortp)) return false;
                 next_stage();
-                if (ex) {  // the list's columns are left out of the sum
+                if (ex && (chosen >> min(c, 63) & 1u)) {  // the list's columns are left out of the sum
                     T* e = reinterpret_cast<T*>(ring + (size_t)s * kChunk);
-                    bool wrote = false;
                     for (int j = lane; j < sh.list; j += 32)
-                        if (slot.key[j] == c * kWarps + warp) {
-                            e[slot.col[j] - c * kChunkVecs * E::kPer] = E::put(-INFINITY);
-                            wrote = true;
-                        }
-                    if (wrote) fence_proxy_async_smem();  // a bulk copy writes this stage next
+                        if (slot.key[j] == c * kWarps + warp) e[slot.col[j] - c * kChunkVecs * E::kPer] = E::put(-INFINITY);
+                    fence_proxy_async_smem();  // a bulk copy writes this stage next
                     __syncwarp();
                 }
-                read(c, s, v);
-                if (!stays) give_back(s);
-                p.template vectors<DT, kVecs>(v, off, a.f);
+                const uint4* sv = reinterpret_cast<const uint4*>(ring + (size_t)s * kChunk) + tid;
+                if ((c + 1) * kChunkVecs <= nvec) {
+#pragma unroll
+                    for (int j = 0; j < kVecs; ++j) v[j] = sv[j * kLanes];
+                    if (!stays) give_back(s);
+                    p.template vectors<DT, kVecs>(v, off, a.f);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kVecs; ++j) {
+                        const int at = c * kChunkVecs + j * kLanes + tid;
+                        if (at - lane > nvec) break;  // nothing of this warp's any more
+                        uint4 q[1] = {read_edge(sv + j * kLanes, at)};
+                        p.template vectors<DT, 1>(q, off, a.f);
+                    }
+                    if (!stays) give_back(s);
+                }
                 return true;
             };
             const int held_from = grad ? keep + sh.again : sh.chunks;  // chunks from here on stay in their stages
@@ -314,43 +326,58 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
             if (!ok) break;
             if (!grad) continue;
             if (!warp_wait(&grad_bar[slot_i], sph, abortp)) break;
+            if (!ex) find_chosen();
             Grad<DT> gr;
             gr.set(grads[slot_i].a, grads[slot_i].lse2, maxima[slot_i], a.f);
             T* out = static_cast<T*>(a.grad) + r * a.ld_grad;
-            // second reading: the gradient of chunk c, then the chosen columns over it
+            auto over = [&](int c) {  // the chosen columns over the vectors
+                if (chosen >> min(c, 63) & 1u) {
+                    __syncwarp();  // the vectors first
+                    for (int j = lane; j < sh.list; j += 32)
+                        if (slot.key[j] == c * kWarps + warp) out[slot.col[j]] = E::put(slot.x[j]);
+                }
+            };
+            // second reading: the gradient of a whole chunk
             auto second = [&](int c, const uint4 (&v)[kVecs]) {
                 uint4* ov = reinterpret_cast<uint4*>(out) + c * kChunkVecs + tid;
+#pragma unroll
+                for (int j = 0; j < kVecs; ++j) st_stream(ov + j * kLanes, gr.vector(v[j]));
+                over(c);
+            };
+            // and of chunk c in stage s, which is then given back
+            auto second_at = [&](int c, int s) {
+                const uint4* sv = reinterpret_cast<const uint4*>(ring + (size_t)s * kChunk) + tid;
                 if ((c + 1) * kChunkVecs <= nvec) {
+                    uint4 v[kVecs];
 #pragma unroll
-                    for (int j = 0; j < kVecs; ++j) st_stream(ov + j * kLanes, gr.vector(v[j]));
-                } else {
+                    for (int j = 0; j < kVecs; ++j) v[j] = sv[j * kLanes];
+                    give_back(s);
+                    second(c, v);
+                    return;
+                }
 #pragma unroll
-                    for (int j = 0; j < kVecs; ++j) {
-                        const int at = c * kChunkVecs + tid + j * kLanes;
-                        if (at < nvec) st_stream(ov + j * kLanes, gr.vector(v[j]));
-                        else if (at == nvec && rest) {
-                            const uint4 y = gr.vector(v[j]);
-                            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+                for (int j = 0; j < kVecs; ++j) {
+                    const int at = c * kChunkVecs + j * kLanes + tid;
+                    if (at - lane > nvec) break;
+                    const uint4 y = gr.vector(read_edge(sv + j * kLanes, at));
+                    if (at < nvec) st_stream(reinterpret_cast<uint4*>(out) + at, y);
+                    else if (at == nvec && rest) {
+                        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-                            for (int i = 0; i < E::kPer; ++i) {
-                                if (i >= rest) continue;
-                                if constexpr (DT == RAPID_BF16) out[nvec * E::kPer + i] = (T)(w[i / 2] >> (16 * (i & 1)));
-                                else out[nvec * E::kPer + i] = __uint_as_float(w[i]);
-                            }
+                        for (int i = 0; i < E::kPer; ++i) {
+                            if (i >= rest) continue;
+                            if constexpr (DT == RAPID_BF16) out[nvec * E::kPer + i] = (T)(w[i / 2] >> (16 * (i & 1)));
+                            else out[nvec * E::kPer + i] = __uint_as_float(w[i]);
                         }
                     }
                 }
-                __syncwarp();  // the vectors first
-                for (int j = lane; j < sh.list; j += 32)
-                    if (slot.key[j] == c * kWarps + warp) out[slot.col[j]] = E::put(slot.x[j]);
+                give_back(s);
+                over(c);
             };
             if (stats) {
                 for (int c = held_from; c < sh.chunks; ++c) {
-                    uint4 v[kVecs];
-                    read(c, held, v);
-                    give_back(held);
+                    second_at(c, held);
                     if (++held == sh.stages) held = 0;
-                    second(c, v);
                 }
                 if (keep) {
 #pragma unroll
@@ -363,10 +390,7 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
                 ok = warp_wait(&full_bar[s], ph, abortp);
                 if (!ok) break;
                 next_stage();
-                uint4 v[kVecs];
-                read(c, s, v);
-                give_back(s);
-                second(c, v);
+                second_at(c, s);
             }
             if (!ok) break;
             if (!stats) {  // the slot is free
@@ -412,9 +436,9 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, int sm_count, cuda
     };
     auto by_type = [&](auto dt) -> cudaError_t {
         constexpr int DT = decltype(dt)::value;
-        if (row_bytes <= 16384) return go(ring_kernel<DT, Op, 4, 0, 5>, 4, 0, 5);
+        if (row_bytes <= 16384) return go(ring_kernel<DT, Op, 4, 0, 4>, 4, 0, 4);
         if (row_bytes <= 65536) return go(ring_kernel<DT, Op, 8, 0, 2>, 8, 0, 2);
-        if (!a.known && a.grad && row_bytes > 10 * 16384) return go(ring_kernel<DT, Op, 16, 6, 1>, 16, 6, 1);
+        if (!a.known && a.grad && row_bytes > 5 * 32768) return go(ring_kernel<DT, Op, 16, 3, 1>, 16, 3, 1);
         return go(ring_kernel<DT, Op, 16, 0, 1>, 16, 0, 1);
     };
     return a.dtype == RAPID_BF16 ? by_type(std::integral_constant<int, RAPID_BF16>{}) : by_type(std::integral_constant<int, RAPID_F32>{});
