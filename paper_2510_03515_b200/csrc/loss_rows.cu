@@ -18,12 +18,12 @@ namespace losses {
 
 namespace {
 
-constexpr int kVecs = 4;         // 16-byte vectors of a thread in a chunk
 constexpr int kMaxStages = 32;
 constexpr int kQueue = kMaxStages + 4;  // rows that are known to the block at a time, at most
+constexpr int kZeroQueue = 8;           // rows that wait for their zeros
 
 struct RingShape {
-    int stages;   // of 2 kWarps KB each
+    int stages;   // of a chunk each
     int chunks;   // of a row
     int again;    // chunks of a row that are loaded a second time
     int batch;    // rows drawn at a time
@@ -53,23 +53,28 @@ __device__ __forceinline__ uint64_t policy_first() {
 }
 
 // By a whole warp; the lanes agree, so that all of them stay or all leave.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+__device__ __noinline__ bool warp_wait_long(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
     return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag));
 }
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    return warp_wait_long(bar, parity, abort_flag);
+}
 
-template <int DT, class Op, int kWarps, int kKeep, int kBlocks>
-__global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsArgs a, Op op, RingShape sh) {
+// kWarps consumer warps, kVecs 16-byte vectors of a thread in a chunk, kKeep chunks in registers, kBlocks blocks on an SM
+template <int DT, class Op, int kWarps, int kVecs, int kKeep, int kBlocks>
+__global__ void __launch_bounds__((kWarps + 3) * 32, kBlocks) ring_kernel(RowsArgs a, Op op, RingShape sh) {
     using E = Elem<DT>;
     using T = typename E::T;
     constexpr int kLanes = kWarps * 32;          // consumer threads
     constexpr int kChunkVecs = kLanes * kVecs;   // vectors of a chunk
     constexpr int kChunk = kChunkVecs * 16;
     extern __shared__ __align__(128) uint8_t dyn[];
-    __shared__ __align__(8) uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], row_bar[kQueue], list_bar[2], parts_bar[2], grad_bar[2];
-    __shared__ long long row_q[kQueue];
+    __shared__ __align__(8) uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], row_bar[kQueue];
+    __shared__ __align__(8) uint64_t list_bar[2], parts_bar[2], grad_bar[2], value_bar[2], zero_full[kZeroQueue], zero_empty[kZeroQueue];
+    __shared__ long long row_q[kQueue], zero_q[kZeroQueue];
     __shared__ WarpPart parts[2][kWarps];
-    __shared__ RowGrad grads[2];
-    __shared__ float maxima[2];
+    __shared__ GradConst grads[2];
     __shared__ int abort_flag;
     uint8_t* ring = dyn;
     uint8_t* slots = dyn + (size_t)sh.stages * kChunk;
@@ -82,10 +87,15 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
             mbar_init(&empty_bar[s], kWarps);
         }
         for (int q = 0; q < kQueue; ++q) mbar_init(&row_bar[q], 1);
+        for (int q = 0; q < kZeroQueue; ++q) {
+            mbar_init(&zero_full[q], 1);
+            mbar_init(&zero_empty[q], 1);
+        }
         for (int s = 0; s < 2; ++s) {
             mbar_init(&list_bar[s], 1);
             mbar_init(&parts_bar[s], kWarps);
             mbar_init(&grad_bar[s], 1);
+            mbar_init(&value_bar[s], 1);
         }
         abort_flag = 0;
         mbar_init_fence();
@@ -94,15 +104,14 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
     volatile int* abortp = &abort_flag;
 
     const bool stats = !a.known, grad = a.grad != nullptr;
-    const int readings = stats && grad ? 2 : 1;
     const int nvec = a.vocab / E::kPer, rest = a.vocab - nvec * E::kPer;
-    const int keep = readings == 2 ? kKeep : 0;  // chunks that stay in registers
+    const int keep = stats && grad ? kKeep : 0;  // chunks that stay in registers
 
     if (warp == kWarps) {
         // ------------------------------- producer -------------------------------------------
         const int load_bytes = (nvec + (rest ? 1 : 0)) * 16;  // inside the row: its pitch is a multiple of 16 bytes
         const uint64_t first = policy_first();
-        uint32_t it = 0, q = 0;
+        uint32_t it = 0, q = 0, zq = 0;
         bool ok = true;
         auto load = [&](const uint8_t* src, int c) {  // chunk c into the next stage
             const int s = it % sh.stages;
@@ -123,6 +132,16 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
             }
             ++q;
         };
+        auto zero = [&](long long r) {
+            const uint32_t use = zq / kZeroQueue;
+            if (use > 0 && !warp_wait(&zero_empty[zq % kZeroQueue], (use & 1u) ^ 1u, abortp)) return false;
+            if (lane == 0) {
+                zero_q[zq % kZeroQueue] = r;
+                mbar_arrive(&zero_full[zq % kZeroQueue]);
+            }
+            ++zq;
+            return true;
+        };
         while (ok) {
             unsigned int t = 0;
             if (lane == 0) t = atomicAdd(&a.w.head->ticket, 1u);
@@ -140,12 +159,7 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
                 const int state = __shfl_sync(0xffffffffu, (int)st, i);
                 if (r < 0) break;
                 if (state != ROW_OK) {  // nobody reads this row
-                    if (grad) {
-                        T* out = static_cast<T*>(a.grad) + r * a.ld_grad;
-                        for (int v = lane; v < nvec; v += 32) st_stream(reinterpret_cast<uint4*>(out) + v, make_uint4(0, 0, 0, 0));
-                        if (lane < rest) out[nvec * E::kPer + lane] = E::put(0.f);
-                    }
-                    if (stats && lane == 0) a.w.value[r] = 0.0;
+                    if (grad) ok = zero(r);
                     continue;
                 }
                 const uint8_t* src = static_cast<const uint8_t*>(a.logits) + (size_t)r * a.ld * sizeof(T);
@@ -155,6 +169,7 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
             }
         }
         if (ok) publish(-1);
+        if (ok) zero(-1);
         __syncwarp();
         if (!ok || *abortp) {  // gave up: let the copies already issued land before the block's memory goes away
             const uint32_t from = it > (uint32_t)sh.stages ? it - sh.stages : 0u;
@@ -163,6 +178,19 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
                 while (!mbar_try_wait(&full_bar[j % sh.stages], (j / sh.stages) & 1u))
                     if (global_timer_ns() - t0 > kWaitLimitNs) break;
             }
+        }
+    } else if (warp == kWarps + 2) {
+        // ------------------------------- zeros for the rows that do not count ----------------
+        for (uint32_t zq = 0;; ++zq) {
+            if (!warp_wait(&zero_full[zq % kZeroQueue], (zq / kZeroQueue) & 1u, abortp)) break;
+            const int64_t r = zero_q[zq % kZeroQueue];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&zero_empty[zq % kZeroQueue]);
+            if (r < 0) break;
+            T* out = static_cast<T*>(a.grad) + r * a.ld_grad;
+#pragma unroll 4
+            for (int v = lane; v < nvec; v += 32) st_stream(reinterpret_cast<uint4*>(out) + v, make_uint4(0, 0, 0, 0));
+            if (lane < rest) out[nvec * E::kPer + lane] = E::put(0.f);
         }
     } else if (warp == kWarps + 1) {
         // ------------------------------- once a row -----------------------------------------
@@ -193,26 +221,27 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&list_bar[s]);
-            const auto ahead = look(op, a, r, rows);
-            RowStat st = known_stat(ahead);
+            auto mine = look(op, a, r, rows, slot.col, slot.z, slot.x);
+            RowStat st = known_stat(mine);
             if (stats) {
                 if (!warp_wait(&parts_bar[s], ph, abortp)) break;
-                WarpPart mine{-INFINITY, -INFINITY, 0.0};
-                if (lane < kWarps) mine = parts[s][lane];
-                st = join_parts(mine, a.f);
+                st = join_parts(lane < kWarps ? parts[s][lane] : WarpPart{0.0, -INFINITY, kNoShift});
             }
-            const RowGrad g = finish(op, a, r, ahead, st, slot.col, slot.z, slot.x);
+            const RowGrad g = finish(op, a, mine, st, slot.col, slot.z, slot.x);
             if (lane == 0) {
-                grads[s] = g;
-                maxima[s] = st.max;
+                grads[s] = grad_const<DT>(g, st.max, a.f);
+                mbar_arrive(&grad_bar[s]);
             }
+            values(op, a, r, mine, g, st, slot.col, slot.z, slot.x);
             __syncwarp();
-            if (lane == 0) mbar_arrive(&grad_bar[s]);
+            if (lane == 0) mbar_arrive(&value_bar[s]);
         }
     } else {
         // ------------------------------- consumers ------------------------------------------
         const float off = shift_fraction(warp);
+        const double unit = warp_unit(off);
         const bool ex = exclude(op) && stats;
+        const int whole = nvec / kChunkVecs;  // whole chunks of a row; at most one more
         int st = 0;
         uint32_t ph = 0;
         auto next_stage = [&]() {
@@ -224,6 +253,12 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
         auto give_back = [&](int s) {
             __syncwarp();
             if (lane == 0) mbar_arrive(&empty_bar[s]);
+        };
+        const uint4* my_ring = reinterpret_cast<const uint4*>(ring) + tid;
+        auto read = [&](int s, uint4 (&v)[kVecs]) {
+            const uint4* sv = my_ring + s * kChunkVecs;
+#pragma unroll
+            for (int j = 0; j < kVecs; ++j) v[j] = sv[j * kLanes];
         };
         // vector `at` of the row from place `sv`; columns behind the last read as -inf
         auto read_edge = [&](const uint4* sv, int at) {
@@ -255,16 +290,17 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
             const uint32_t sph = (jq >> 1) & 1u;
             const Slot slot = slot_at(slots + slot_i * slot_bytes, sh.list);
             bool ok = true;
-            // chunks in which this warp has chosen columns, a bit each (the last one for all from 63 on)
-            uint64_t chosen = 0;
+            // chunks in which this warp has chosen columns, a bit each (the last one for all from 31 on)
+            uint32_t chosen = 0;
             auto find_chosen = [&]() {
-                uint64_t m = 0;
+                uint32_t m = 0;
                 for (int j = lane; j < sh.list; j += 32) {
                     const int key = slot.key[j];
-                    if (key >= 0 && key % kWarps == warp) m |= 1ull << min(key / kWarps, 63);
+                    if (key >= 0 && key % kWarps == warp) m |= 1u << min(key / kWarps, 31);
                 }
-                chosen = (uint64_t)__reduce_or_sync(0xffffffffu, (unsigned)(m >> 32)) << 32 | __reduce_or_sync(0xffffffffu, (unsigned)m);
+                chosen = __reduce_or_sync(0xffffffffu, m);
             };
+            auto has_chosen = [&](int c) { return (chosen >> min(c, 31) & 1u) != 0; };
             if (ex) {
                 ok = warp_wait(&list_bar[slot_i], sph, abortp);
                 if (ok) find_chosen();
@@ -272,33 +308,15 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
             uint4 kept[kKeep > 0 ? kKeep : 1][kVecs];
             int held = 0;  // stage of the first chunk that stays
             Part p;
-            // first reading of chunk c
-            auto first = [&](int c, uint4 (&v)[kVecs], bool stays) {
-                const int s = st;
-                if (!warp_wait(&full_bar[s], ph, abortp)) return false;
-                next_stage();
-                if (ex && (chosen >> min(c, 63) & 1u)) {  // the list's columns are left out of the sum
-                    T* e = reinterpret_cast<T*>(ring + (size_t)s * kChunk);
+            // the next stage, holding chunk c for its first reading
+            auto arrived = [&](int c) {
+                if (!warp_wait(&full_bar[st], ph, abortp)) return false;
+                if (ex && has_chosen(c)) {  // the list's columns are left out of the sum
+                    T* e = reinterpret_cast<T*>(ring + (size_t)st * kChunk);
                     for (int j = lane; j < sh.list; j += 32)
                         if (slot.key[j] == c * kWarps + warp) e[slot.col[j] - c * kChunkVecs * E::kPer] = E::put(-INFINITY);
                     fence_proxy_async_smem();  // a bulk copy writes this stage next
                     __syncwarp();
-                }
-                const uint4* sv = reinterpret_cast<const uint4*>(ring + (size_t)s * kChunk) + tid;
-                if ((c + 1) * kChunkVecs <= nvec) {
-#pragma unroll
-                    for (int j = 0; j < kVecs; ++j) v[j] = sv[j * kLanes];
-                    if (!stays) give_back(s);
-                    p.template vectors<DT, kVecs>(v, off, a.f);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < kVecs; ++j) {
-                        const int at = c * kChunkVecs + j * kLanes + tid;
-                        if (at - lane > nvec) break;  // nothing of this warp's any more
-                        uint4 q[1] = {read_edge(sv + j * kLanes, at)};
-                        p.template vectors<DT, 1>(q, off, a.f);
-                    }
-                    if (!stays) give_back(s);
                 }
                 return true;
             };
@@ -307,15 +325,36 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
                 if (keep) {
 #pragma unroll
                     for (int c = 0; c < kKeep; ++c)
-                        if (ok) ok = first(c, kept[c], false);
+                        if (ok && (ok = arrived(c))) {
+                            read(st, kept[c]);
+                            give_back(st);
+                            next_stage();
+                            p.template vectors<DT, kVecs>(kept[c], off, a.f);
+                        }
                 }
-                for (int c = keep; c < sh.chunks && ok; ++c) {
+                for (int c = keep; c < whole && ok; ++c) {
+                    if (!(ok = arrived(c))) break;
                     uint4 v[kVecs];
                     if (c == held_from) held = st;
-                    ok = first(c, v, c >= held_from);
+                    read(st, v);
+                    if (c < held_from) give_back(st);
+                    next_stage();
+                    p.template vectors<DT, kVecs>(v, off, a.f);
+                }
+                if (whole < sh.chunks && ok && (ok = arrived(whole))) {
+                    if (whole == held_from) held = st;
+#pragma unroll 1
+                    for (int j = 0; j < kVecs; ++j) {
+                        const int at = whole * kChunkVecs + j * kLanes + tid;
+                        if (at - lane > nvec) break;  // nothing of this warp's any more
+                        uint4 q[1] = {read_edge(my_ring + st * kChunkVecs + j * kLanes, at)};
+                        p.template vectors<DT, 1>(q, off, a.f);
+                    }
+                    if (whole < held_from) give_back(st);
+                    next_stage();
                 }
                 if (!ok) break;
-                const WarpPart w = warp_part(p, a.f);
+                const WarpPart w = warp_part(p, off, unit, a.f);
                 // two rows ago's sums have been read
                 if (!grad && jq >= 2 && !warp_wait(&grad_bar[slot_i], sph ^ 1u, abortp)) break;
                 if (lane == 0) {
@@ -326,40 +365,40 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
             if (!ok) break;
             if (!grad) continue;
             if (!warp_wait(&grad_bar[slot_i], sph, abortp)) break;
+            const Grad<DT> gr(grads[slot_i], a.f);
             if (!ex) find_chosen();
-            Grad<DT> gr;
-            gr.set(grads[slot_i].a, grads[slot_i].lse2, maxima[slot_i], a.f);
             T* out = static_cast<T*>(a.grad) + r * a.ld_grad;
-            auto over = [&](int c) {  // the chosen columns over the vectors
-                if (chosen >> min(c, 63) & 1u) {
-                    __syncwarp();  // the vectors first
-                    for (int j = lane; j < sh.list; j += 32)
-                        if (slot.key[j] == c * kWarps + warp) out[slot.col[j]] = E::put(slot.x[j]);
-                }
+            uint4* my_out = reinterpret_cast<uint4*>(out) + tid;
+            bool valued = false;
+            auto over = [&](int c) {  // the chosen columns over the vectors of chunk c
+                if (!has_chosen(c)) return;
+                if (!valued) ok = warp_wait(&value_bar[slot_i], sph, abortp);  // a wait that gives up: the values may be wrong, nothing else
+                valued = true;
+                __syncwarp();  // the vectors first
+                for (int j = lane; j < sh.list; j += 32)
+                    if (slot.key[j] == c * kWarps + warp) out[slot.col[j]] = E::put(slot.x[j]);
             };
             // second reading: the gradient of a whole chunk
-            auto second = [&](int c, const uint4 (&v)[kVecs]) {
-                uint4* ov = reinterpret_cast<uint4*>(out) + c * kChunkVecs + tid;
+            auto write = [&](int c, const uint4 (&v)[kVecs]) {
+                uint4* ov = my_out + c * kChunkVecs;
 #pragma unroll
                 for (int j = 0; j < kVecs; ++j) st_stream(ov + j * kLanes, gr.vector(v[j]));
                 over(c);
             };
-            // and of chunk c in stage s, which is then given back
-            auto second_at = [&](int c, int s) {
-                const uint4* sv = reinterpret_cast<const uint4*>(ring + (size_t)s * kChunk) + tid;
-                if ((c + 1) * kChunkVecs <= nvec) {
-                    uint4 v[kVecs];
-#pragma unroll
-                    for (int j = 0; j < kVecs; ++j) v[j] = sv[j * kLanes];
-                    give_back(s);
-                    second(c, v);
-                    return;
-                }
-#pragma unroll
+            // of a whole chunk c in stage s, which is then given back
+            auto write_from = [&](int c, int s) {
+                uint4 v[kVecs];
+                read(s, v);
+                give_back(s);
+                write(c, v);
+            };
+            // and of the last chunk, where that is not whole
+            auto write_edge = [&](int s) {
+#pragma unroll 1
                 for (int j = 0; j < kVecs; ++j) {
-                    const int at = c * kChunkVecs + j * kLanes + tid;
+                    const int at = whole * kChunkVecs + j * kLanes + tid;
                     if (at - lane > nvec) break;
-                    const uint4 y = gr.vector(read_edge(sv + j * kLanes, at));
+                    const uint4 y = gr.vector(read_edge(my_ring + s * kChunkVecs + j * kLanes, at));
                     if (at < nvec) st_stream(reinterpret_cast<uint4*>(out) + at, y);
                     else if (at == nvec && rest) {
                         const uint32_t w[4] = {y.x, y.y, y.z, y.w};
@@ -372,25 +411,26 @@ __global__ void __launch_bounds__((kWarps + 2) * 32, kBlocks) ring_kernel(RowsAr
                     }
                 }
                 give_back(s);
-                over(c);
+                over(whole);
             };
             if (stats) {
-                for (int c = held_from; c < sh.chunks; ++c) {
-                    second_at(c, held);
+                for (int c = held_from; c < whole; ++c) {
+                    write_from(c, held);
                     if (++held == sh.stages) held = 0;
                 }
+                if (whole < sh.chunks && whole >= held_from) write_edge(held);
                 if (keep) {
 #pragma unroll
-                    for (int c = 0; c < kKeep; ++c) second(c, kept[c]);
+                    for (int c = 0; c < kKeep; ++c) write(c, kept[c]);
                 }
             }
+            // chunks that are loaded for this reading
             const int from = stats ? keep : 0, to = stats ? keep + sh.again : sh.chunks;
-            for (int c = from; c < to; ++c) {
-                const int s = st;
-                ok = warp_wait(&full_bar[s], ph, abortp);
-                if (!ok) break;
+            for (int c = from; c < to && ok; ++c) {
+                if (!(ok = warp_wait(&full_bar[st], ph, abortp))) break;
+                if (c < whole) write_from(c, st);
+                else write_edge(st);
                 next_stage();
-                second_at(c, s);
             }
             if (!ok) break;
             if (!stats) {  // the slot is free
@@ -410,9 +450,9 @@ template <class Op>
 cudaError_t launch(const RowsArgs& a, const Op& op, int list, int sm_count, cudaStream_t stream) {
     const size_t es = elem_size(a.dtype);
     const int64_t row_bytes = ((int64_t)a.vocab * es + 15) / 16 * 16;
-    auto go = [&](auto kern, int warps, int keep, int blocks) -> cudaError_t {
+    auto go = [&](auto kern, int warps, int vecs, int keep, int blocks) -> cudaError_t {
         RingShape sh{};
-        const int chunk = warps * 32 * kVecs * 16;
+        const int chunk = warps * 32 * vecs * 16;
         sh.list = (list + 3) / 4 * 4;
         const size_t extra = 2 * (size_t)sh.list * 16;
         // 228 KB an SM; of every block 1 KB is the system's and up to 2 KB are barriers and queues
@@ -431,15 +471,15 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, int sm_count, cuda
         if (sh.batch > 8) sh.batch = 8;
         if (grid > a.n_rows) grid = a.n_rows;
         sh.stride = scatter_stride(a.n_rows);
-        kern<<<(unsigned)grid, (warps + 2) * 32, smem, stream>>>(a, op, sh);
+        kern<<<(unsigned)grid, (warps + 3) * 32, smem, stream>>>(a, op, sh);
         return cudaGetLastError();
     };
     auto by_type = [&](auto dt) -> cudaError_t {
         constexpr int DT = decltype(dt)::value;
-        if (row_bytes <= 16384) return go(ring_kernel<DT, Op, 4, 0, 4>, 4, 0, 4);
-        if (row_bytes <= 65536) return go(ring_kernel<DT, Op, 8, 0, 2>, 8, 0, 2);
-        if (!a.known && a.grad && row_bytes > 5 * 32768) return go(ring_kernel<DT, Op, 16, 3, 1>, 16, 3, 1);
-        return go(ring_kernel<DT, Op, 16, 0, 1>, 16, 0, 1);
+        if (row_bytes <= 16384) return go(ring_kernel<DT, Op, 4, 4, 0, 4>, 4, 4, 0, 4);
+        if (row_bytes <= 65536) return go(ring_kernel<DT, Op, 8, 4, 0, 2>, 8, 4, 0, 2);
+        if (!a.known && a.grad && row_bytes > 5 * 32768) return go(ring_kernel<DT, Op, 16, 4, 3, 1>, 16, 4, 3, 1);
+        return go(ring_kernel<DT, Op, 16, 4, 0, 1>, 16, 4, 0, 1);
     };
     return a.dtype == RAPID_BF16 ? by_type(std::integral_constant<int, RAPID_BF16>{}) : by_type(std::integral_constant<int, RAPID_F32>{});
 }

@@ -255,22 +255,41 @@ struct Part {
     }
 };
 
-// A warp's part, the same in all lanes: its largest logit, its shift, and the sum WITHOUT the largest logit's term, which may carry
-// nearly all of the row's probability and is put back exactly, in double, where the warps' parts meet.
+// Maximum over the warp of floats that are not NaN.
+__device__ __forceinline__ float warp_top(float v) {
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// A warp's part, the same in all lanes: its largest logit, and its sum as s 2^n.  The largest logit's term, which may carry nearly
+// all of the row's probability, is taken out of the sum again and put back exactly.
 struct WarpPart {
-    float m, sh;
     double s;
+    float m;
+    int n;
 };
-__device__ __forceinline__ WarpPart warp_part(const Part& p, const Factor& f) {
+// 2^off of a warp, for warp_part
+__device__ __forceinline__ double warp_unit(float off) { return exp2((double)off) / (1.0 + (double)kEx2Mean); }
+constexpr int kNoShift = -(1 << 20);
+__device__ __forceinline__ WarpPart warp_part(const Part& p, float off, double unit, const Factor& f) {
     WarpPart w;
-    w.m = warp_max(p.m);
-    w.sh = warp_max(p.s > 0.f ? p.sh : -INFINITY);
+    w.m = warp_top(p.m);
+    const float sh = warp_top(p.s > 0.f ? p.sh : -INFINITY);
     double s = (double)p.s + (double)p.c;
     const unsigned top = __ballot_sync(0xffffffffu, p.m == w.m && w.m > kNothing);
     if (top && (threadIdx.x & 31) == __ffs(top) - 1) s -= (double)p.term(p.m, f);
-    if (p.s > 0.f) s *= (double)ex2_approx(p.sh - w.sh);  // an exact power of two
+    if (p.s > 0.f) s *= (double)ex2_approx(p.sh - sh);  // an exact power of two
     else s = 0.0;
-    w.s = warp_sum(s);
+    w.n = kNoShift;
+    w.s = 0.0;
+    if (sh > -INFINITY) {
+        const float n = rintf(sh - off);
+        const double frac = (double)sh - (double)n;
+        if (frac != (double)off) unit = exp2(frac) / (1.0 + (double)kEx2Mean);  // a shift so large that the fraction was rounded
+        w.s = warp_sum(s) * unit + exp2((double)w.m * f.kd - (double)n);
+        w.n = (int)n;
+    }
     return w;
 }
 
@@ -278,16 +297,13 @@ struct RowStat {
     double lse2;  // -inf when no logit is left
     float max;
 };
-// The warps' parts together, by one warp: lane i holds warp i's part (sh = -inf where there is none).
-__device__ __forceinline__ RowStat join_parts(const WarpPart& p, const Factor& f) {
+// The warps' parts together, by one warp: lane i holds warp i's part (n = kNoShift where there is none).
+__device__ __forceinline__ RowStat join_parts(const WarpPart& p) {
     RowStat r;
-    r.max = warp_max(p.m);
-    const float sh = warp_max(p.sh);
-    double s = 0.0;
-    if (p.m > kNothing)
-        s = p.s / (1.0 + (double)kEx2Mean) * exp2((double)p.sh - (double)sh) + exp2((double)p.m * f.kd - (double)sh);
-    s = warp_sum(s);
-    r.lse2 = s > 0.0 ? (double)sh + log2(s) : -INFINITY;
+    r.max = warp_top(p.m);
+    const int n = __reduce_max_sync(0xffffffffu, p.n), down = n - p.n;
+    const double s = warp_sum(down < 1000 ? p.s * __hiloint2double((1023 - down) << 20, 0) : 0.0);
+    r.lse2 = s > 0.0 ? (double)n + log2(s) : -INFINITY;
     return r;
 }
 
@@ -297,17 +313,34 @@ __device__ __forceinline__ float shift_fraction(int warp) { return (float)(((uns
 
 // dz_v = a 2^(x_v - lse2).  bf16: |a| goes into the exponent, one multiply-add and one exponential an element.  float: the largest
 // logit is taken off first, which keeps the argument small and so its rounding below the result's; a is multiplied at the end.
+// The constants are formed once a row; they are floats, whose rounding (and that of log2f) is some 2^-18 of a probability at most.
+struct RowGrad {
+    double a, lse2;
+};
+struct GradConst {
+    float c, m, a;
+};
+template <int DT>
+__device__ __forceinline__ GradConst grad_const(const RowGrad& g, float max, const Factor& f) {
+    GradConst k;
+    k.a = (float)g.a;
+    if (DT == RAPID_BF16) {
+        k.m = 0.f;
+        k.c = (float)((double)log2f(fabsf(k.a)) - g.lse2);
+        if (k.a == 0.f) k.c = -INFINITY;
+    } else {
+        k.m = max > kNothing ? max : 0.f;
+        k.c = (float)((double)k.m * f.kd - g.lse2);
+    }
+    return k;
+}
 template <int DT>
 struct Grad;
 template <>
 struct Grad<RAPID_BF16> {
     float k, c;
     uint32_t sign;  // of a, on both halves of a pair
-    __device__ __forceinline__ void set(double a, double lse2, float, const Factor& f) {
-        k = f.k;
-        c = a != 0.0 ? (float)(log2(fabs(a)) - lse2) : -INFINITY;
-        sign = a < 0.0 ? 0x80008000u : 0u;
-    }
+    __device__ __forceinline__ Grad(const GradConst& g, const Factor& f) : k(f.k), c(g.c), sign(g.a < 0.f ? 0x80008000u : 0u) {}
     __device__ __forceinline__ uint4 vector(const uint4& q) const {
         const uint32_t in[4] = {q.x, q.y, q.z, q.w};
         uint32_t out[4];
@@ -320,29 +353,16 @@ struct Grad<RAPID_BF16> {
         }
         return make_uint4(out[0], out[1], out[2], out[3]);
     }
-    __device__ __forceinline__ uint16_t one(uint16_t z) const {
-        return (uint16_t)(Elem<RAPID_BF16>::put(ex2_approx(fmaf(Elem<RAPID_BF16>::get(z), k, c))) ^ (uint16_t)sign);
-    }
 };
 template <>
 struct Grad<RAPID_F32> {
     float k, m, c, a;
-    __device__ __forceinline__ void set(double a_, double lse2, float max, const Factor& f) {
-        k = f.k;
-        m = max > kNothing ? max : 0.f;
-        c = (float)((double)m * f.kd - lse2);
-        a = (float)a_;
-    }
+    __device__ __forceinline__ Grad(const GradConst& g, const Factor& f) : k(f.k), m(g.m), c(g.c), a(g.a) {}
     __device__ __forceinline__ float one(float z) const { return a * ex2_approx(fmaf(z - m, k, c)); }
     __device__ __forceinline__ uint4 vector(const uint4& q) const {
         return make_uint4(__float_as_uint(one(__uint_as_float(q.x))), __float_as_uint(one(__uint_as_float(q.y))),
                           __float_as_uint(one(__uint_as_float(q.z))), __float_as_uint(one(__uint_as_float(q.w))));
     }
-};
-
-// The factor and the chosen columns' values of one row.
-struct RowGrad {
-    double a, lse2;
 };
 
 // Rows that count, from the preparing kernel's blocks; by one warp.
@@ -442,10 +462,10 @@ __device__ __forceinline__ double clip_weight(const ClipOp& op, int64_t r, long 
     return op.scale / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows);
 }
 
-// What an operator does with a row, by one warp.  look() loads what it needs of the row beside its logits, ahead of time; finish()
-// is called once the row's log-sum-exp is there (without the chosen columns where exclude() says so).  col[j] and z[j] are the chosen
-// columns and their logits; x[j], for distillation the teacher's logits, become the columns' gradient.  finish() writes what is
-// kept of the row to the scratch.
+// What an operator does with a row, by one warp.  look() does, ahead of time, what needs no sums over the row; finish() gives the
+// factor once the row's log-sum-exp is there (without the chosen columns where exclude() says so), and is what the row's second
+// reading waits for; values() gives the chosen columns' gradient and writes what is kept of the row to the scratch.  col[j] and
+// z[j] are the chosen columns and their logits; x[j], for distillation the teacher's logits, become the columns' gradient.
 __device__ __forceinline__ int list_size(const ClipOp&) { return 1; }
 __device__ __forceinline__ int list_size(const PrefOp&) { return 1; }
 __device__ __forceinline__ int list_size(const DistillOp& op) { return op.k; }
@@ -467,96 +487,111 @@ __device__ __forceinline__ float entry(const DistillOp& op, int64_t r, int j) { 
 
 struct ClipRow {
     ClipIn in;
-    double w;
+    double w, lp;
 };
-__device__ __forceinline__ ClipRow look(const ClipOp& op, const RowsArgs&, int64_t r, long long rows) {
-    return ClipRow{clip_in(op, r), clip_weight(op, r, rows)};
+__device__ __forceinline__ ClipRow look(const ClipOp& op, const RowsArgs&, int64_t r, long long rows, const int*, const float*, const float*) {
+    return ClipRow{clip_in(op, r), clip_weight(op, r, rows), 0.0};
 }
 struct PrefRow {
-    double a;
+    double a, lp;
     RowStat st;
 };
-__device__ __forceinline__ PrefRow look(const PrefOp& op, const RowsArgs& a, int64_t r, long long) {
-    PrefRow p{0.0, {0.0, 0.f}};
-    if (a.known) p = PrefRow{op.seq_coef[r / op.seq_len], {a.w.lse2[r], a.w.row_max[r]}};
+__device__ __forceinline__ PrefRow look(const PrefOp& op, const RowsArgs& a, int64_t r, long long, const int*, const float*, const float*) {
+    PrefRow p{0.0, 0.0, {0.0, 0.f}};
+    if (a.known) p = PrefRow{op.seq_coef[r / op.seq_len], 0.0, {a.w.lse2[r], a.w.row_max[r]}};
     return p;
 }
 struct DistillRow {
     double teacher, w;
+    double p0, lp0;   // probability of the tokens beside the list, and its logarithm
+    double list_sum;  // this lane's share of the list's sum of 2^(x - top's x)
+    float top;        // the list's largest logit
 };
-__device__ __forceinline__ DistillRow look(const DistillOp& op, const RowsArgs&, int64_t r, long long rows) {
-    return DistillRow{op.teacher_lse2[r], op.scale * op.inv_tau / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows)};
+__device__ __forceinline__ DistillRow look(const DistillOp& op, const RowsArgs&, int64_t r, long long rows, const int* col, const float* z,
+                                           const float* x) {
+    const int lane = threadIdx.x & 31;
+    DistillRow row{op.teacher_lse2[r], op.scale * op.inv_tau / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows), 0.0, 0.0, 0.0,
+                   -INFINITY};
+    if (!op.tail) return row;
+    double mass = 0.0;
+    for (int j = lane; j < op.k; j += 32) {
+        if (col[j] < 0) continue;
+        row.top = fmaxf(row.top, z[j]);
+        mass += exp2((double)x[j] * op.kd - row.teacher);
+    }
+    row.top = warp_top(row.top);
+    row.p0 = 1.0 - warp_sum(mass);
+    if (row.p0 > 0.0) row.lp0 = log2(row.p0);
+    if (row.top > -INFINITY)
+        for (int j = lane; j < op.k; j += 32)
+            if (col[j] >= 0) row.list_sum += exp2(((double)z[j] - (double)row.top) * op.kd);
+    return row;
 }
 __device__ __forceinline__ RowStat known_stat(const ClipRow&) { return RowStat{0.0, 0.f}; }
 __device__ __forceinline__ RowStat known_stat(const PrefRow& p) { return p.st; }
 __device__ __forceinline__ RowStat known_stat(const DistillRow&) { return RowStat{0.0, 0.f}; }
 
-__device__ __forceinline__ RowGrad finish(const ClipOp& op, const RowsArgs& a, int64_t r, const ClipRow& row, const RowStat& st, const int*,
-                                          const float* z, float* x) {
-    const double lp = ((double)z[0] * a.f.kd - st.lse2) * kLn2D;
-    RowGrad g{0.0, st.lse2};
-    if (a.grad) {
-        g.a = row.w * clip_terms(op, row.in, lp).slope;
-        if ((threadIdx.x & 31) == 0) x[0] = (float)(g.a * expm1(lp));
-    }
-    if ((threadIdx.x & 31) == 0) a.w.value[r] = lp;
-    return g;
+__device__ __forceinline__ RowGrad finish(const ClipOp& op, const RowsArgs& a, ClipRow& row, const RowStat& st, const int*, const float* z,
+                                          const float*) {
+    row.lp = ((double)z[0] * a.f.kd - st.lse2) * kLn2D;
+    return RowGrad{a.grad ? row.w * clip_terms(op, row.in, row.lp).slope : 0.0, st.lse2};
+}
+__device__ __forceinline__ void values(const ClipOp&, const RowsArgs& a, int64_t r, const ClipRow& row, const RowGrad& g, const RowStat&,
+                                       const int*, const float*, float* x) {
+    if ((threadIdx.x & 31) != 0) return;
+    x[0] = (float)(g.a * expm1(row.lp));
+    a.w.value[r] = row.lp;
 }
 
-__device__ __forceinline__ RowGrad finish(const PrefOp& op, const RowsArgs& a, int64_t r, const PrefRow& row, const RowStat& st, const int*,
-                                          const float* z, float* x) {
-    const double lp = ((double)z[0] * a.f.kd - st.lse2) * kLn2D;
+__device__ __forceinline__ RowGrad finish(const PrefOp&, const RowsArgs& a, PrefRow& row, const RowStat& st, const int*, const float* z,
+                                          const float*) {
+    row.lp = ((double)z[0] * a.f.kd - st.lse2) * kLn2D;
+    return RowGrad{row.a, st.lse2};
+}
+__device__ __forceinline__ void values(const PrefOp&, const RowsArgs& a, int64_t r, const PrefRow& row, const RowGrad& g, const RowStat& st,
+                                       const int*, const float*, float* x) {
+    if ((threadIdx.x & 31) != 0) return;
     if (a.known) {
-        if ((threadIdx.x & 31) == 0) x[0] = (float)(row.a * expm1(lp));
-    } else if ((threadIdx.x & 31) == 0) {
-        a.w.value[r] = lp;
+        x[0] = (float)(g.a * expm1(row.lp));
+    } else {
+        a.w.value[r] = row.lp;
         a.w.lse2[r] = st.lse2;
         a.w.row_max[r] = st.max;
     }
-    return RowGrad{row.a, st.lse2};
 }
 
-__device__ __forceinline__ RowGrad finish(const DistillOp& op, const RowsArgs& a, int64_t r, const DistillRow& row, const RowStat& st,
-                                          const int* col, const float* z, float* x) {
+__device__ __forceinline__ RowGrad finish(const DistillOp& op, const RowsArgs&, DistillRow& row, const RowStat& st, const int* col, const float* z,
+                                          const float*) {
+    RowGrad g{row.w, st.lse2};
+    if (!op.tail) return g;
+    // the student's log-sum-exp over the whole vocabulary, in a sum against the larger of the rest's and the list's largest term
     const int lane = threadIdx.x & 31;
-    // the student's log-sum-exp over the whole vocabulary
-    double lse2 = st.lse2;
-    if (op.tail) {
-        double top = lse2;
-        for (int j = lane; j < op.k; j += 32)
-            if (col[j] >= 0) top = fmax(top, (double)z[j] * op.kd);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, o));
-        double s = 0.0;
-        if (top > -INFINITY) {
-            if (lane == 0) s = exp2(lse2 - top);
-            for (int j = lane; j < op.k; j += 32)
-                if (col[j] >= 0) s += exp2((double)z[j] * op.kd - top);
-        }
-        s = warp_sum(s);
-        lse2 = s > 0.0 ? top + log2(s) : -INFINITY;
+    const double x0 = row.top > -INFINITY ? (double)row.top * op.kd : -INFINITY;
+    const double top = fmax(st.lse2, x0);
+    double s = 0.0;
+    if (top > -INFINITY) {
+        s = row.list_sum * exp2(x0 - top);
+        if (lane == 0) s += exp2(st.lse2 - top);
     }
-    double loss = 0.0, mass = 0.0;
+    s = warp_sum(s);
+    g.lse2 = s > 0.0 ? top + log2(s) : -INFINITY;
+    if (row.p0 > 0.0 && st.lse2 > -INFINITY) g.a = row.w * (1.0 - exp2(row.lp0 - (st.lse2 - g.lse2)));
+    return g;
+}
+__device__ __forceinline__ void values(const DistillOp& op, const RowsArgs& a, int64_t r, const DistillRow& row, const RowGrad& g,
+                                       const RowStat& st, const int* col, const float* z, float* x) {
+    const int lane = threadIdx.x & 31;
+    double loss = 0.0;
     for (int j = lane; j < op.k; j += 32) {
         if (col[j] < 0) continue;
-        const double lt = (double)x[j] * op.kd - row.teacher, lq = (double)z[j] * op.kd - lse2;
+        const double lt = (double)x[j] * op.kd - row.teacher, lq = (double)z[j] * op.kd - g.lse2;
         const double p = exp2(lt);
         if (p > 0.0) loss += p * (lt - lq);
-        mass += p;
         x[j] = (float)(row.w * (exp2(lq) - p));
     }
     loss = warp_sum(loss);
-    RowGrad g{row.w, lse2};
-    if (op.tail) {
-        const double p0 = 1.0 - warp_sum(mass), l0 = st.lse2 - lse2;
-        if (p0 > 0.0) {
-            const double lp0 = log2(p0);
-            loss += p0 * (lp0 - l0);
-            if (st.lse2 > -INFINITY) g.a = row.w * (1.0 - exp2(lp0 - l0));
-        }
-    }
+    if (row.p0 > 0.0) loss += row.p0 * (row.lp0 - (st.lse2 - g.lse2));
     if (lane == 0) a.w.value[r] = loss * kLn2D;
-    return g;
 }
 
 #endif  // __CUDACC__
