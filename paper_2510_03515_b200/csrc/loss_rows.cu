@@ -10,6 +10,8 @@
 // loaded again.
 //
 // Every wait on a barrier is bounded; a wait that gives up raises RAPID_ERR_TIMEOUT in the scratch and never traps.
+#include <algorithm>
+
 #include "loss_rows.cuh"
 #include "tma_pipe.cuh"
 
@@ -18,9 +20,6 @@ namespace losses {
 
 namespace {
 
-constexpr int kMaxStages = 32;
-constexpr int kQueue = kMaxStages + 4;  // rows that are known to the block at a time, at most
-constexpr int kZeroQueue = 8;           // rows that wait for their zeros
 
 struct RingShape {
     int stages;   // of a chunk each
@@ -31,15 +30,30 @@ struct RingShape {
     unsigned long long stride;
 };
 
-// Shared memory of one row's chosen columns: column, key, logit, value.
+// Shared memory of one row's chosen columns: column, logit, value.
 struct Slot {
-    int *col, *key;
+    int* col;
     float *z, *x;
 };
+constexpr int kSlotEntry = 12;  // bytes of one of them
 __device__ __forceinline__ Slot slot_at(uint8_t* base, int list) {
-    int* p = reinterpret_cast<int*>(base);
-    return Slot{p, p + list, reinterpret_cast<float*>(p + 2 * list), reinterpret_cast<float*>(p + 3 * list)};
+    float* p = reinterpret_cast<float*>(base);
+    return Slot{reinterpret_cast<int*>(p), p + list, p + 2 * list};
 }
+
+// What the warps of a block tell each other, behind the stages in shared memory.
+template <int kWarps>
+struct Board {
+    static constexpr int kStages = kWarps >= 16 ? 8 : 16;  // at most
+    static constexpr int kQueue = kStages + 4;             // rows that are known to the block at a time, at most
+    static constexpr int kZeros = 4;                       // rows that wait for their zeros
+    uint64_t full[kStages], ready[kStages], empty[kStages], row[kQueue];
+    uint64_t list[2], parts_in[2], grad[2], value[2], zero_full[kZeros], zero_empty[kZeros];
+    long long row_q[kQueue], zero_q[kZeros];
+    WarpPart parts[2][kWarps];
+    GradConst grads[2];
+    int abort_flag;
+};
 
 __device__ __forceinline__ void bulk_load_once(void* smem_dst, const void* gsrc, uint32_t bytes, uint64_t* bar, uint64_t policy) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(smem_u32(smem_dst)),
@@ -63,45 +77,42 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
 
 // kWarps consumer warps, kVecs 16-byte vectors of a thread in a chunk, kKeep chunks in registers, kBlocks blocks on an SM
 template <int DT, class Op, int kWarps, int kVecs, int kKeep, int kBlocks>
-__global__ void __launch_bounds__((kWarps + 3) * 32, kBlocks) ring_kernel(RowsArgs a, Op op, RingShape sh) {
+__global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsArgs a, Op op, RingShape sh) {
     using E = Elem<DT>;
     using T = typename E::T;
     constexpr int kLanes = kWarps * 32;          // consumer threads
     constexpr int kChunkVecs = kLanes * kVecs;   // vectors of a chunk
     constexpr int kChunk = kChunkVecs * 16;
+    constexpr int kQueue = Board<kWarps>::kQueue, kZeros = Board<kWarps>::kZeros;
     extern __shared__ __align__(128) uint8_t dyn[];
-    __shared__ __align__(8) uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], row_bar[kQueue];
-    __shared__ __align__(8) uint64_t list_bar[2], parts_bar[2], grad_bar[2], value_bar[2], zero_full[kZeroQueue], zero_empty[kZeroQueue];
-    __shared__ long long row_q[kQueue], zero_q[kZeroQueue];
-    __shared__ WarpPart parts[2][kWarps];
-    __shared__ GradConst grads[2];
-    __shared__ int abort_flag;
     uint8_t* ring = dyn;
-    uint8_t* slots = dyn + (size_t)sh.stages * kChunk;
-    const int slot_bytes = sh.list * 16;
+    Board<kWarps>& bd = *reinterpret_cast<Board<kWarps>*>(dyn + (size_t)sh.stages * kChunk);
+    uint8_t* slots = dyn + (size_t)sh.stages * kChunk + sizeof(Board<kWarps>);
+    const int slot_bytes = sh.list * kSlotEntry;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
         for (int s = 0; s < sh.stages; ++s) {
-            mbar_init(&full_bar[s], 1);
-            mbar_init(&empty_bar[s], kWarps);
+            mbar_init(&bd.full[s], 1);
+            mbar_init(&bd.ready[s], 1);
+            mbar_init(&bd.empty[s], kWarps);
         }
-        for (int q = 0; q < kQueue; ++q) mbar_init(&row_bar[q], 1);
-        for (int q = 0; q < kZeroQueue; ++q) {
-            mbar_init(&zero_full[q], 1);
-            mbar_init(&zero_empty[q], 1);
+        for (int q = 0; q < kQueue; ++q) mbar_init(&bd.row[q], 1);
+        for (int q = 0; q < kZeros; ++q) {
+            mbar_init(&bd.zero_full[q], 1);
+            mbar_init(&bd.zero_empty[q], 1);
         }
         for (int s = 0; s < 2; ++s) {
-            mbar_init(&list_bar[s], 1);
-            mbar_init(&parts_bar[s], kWarps);
-            mbar_init(&grad_bar[s], 1);
-            mbar_init(&value_bar[s], 1);
+            mbar_init(&bd.list[s], 1);
+            mbar_init(&bd.parts_in[s], kWarps);
+            mbar_init(&bd.grad[s], 1);
+            mbar_init(&bd.value[s], 1);
         }
-        abort_flag = 0;
+        bd.abort_flag = 0;
         mbar_init_fence();
     }
     __syncthreads();
-    volatile int* abortp = &abort_flag;
+    volatile int* abortp = &bd.abort_flag;
 
     const bool stats = !a.known, grad = a.grad != nullptr;
     const int nvec = a.vocab / E::kPer, rest = a.vocab - nvec * E::kPer;
@@ -116,28 +127,28 @@ __global__ void __launch_bounds__((kWarps + 3) * 32, kBlocks) ring_kernel(RowsAr
         auto load = [&](const uint8_t* src, int c) {  // chunk c into the next stage
             const int s = it % sh.stages;
             const uint32_t use = it / sh.stages;
-            if (use > 0 && !warp_wait(&empty_bar[s], (use & 1u) ^ 1u, abortp)) return false;
+            if (use > 0 && !warp_wait(&bd.empty[s], (use & 1u) ^ 1u, abortp)) return false;
             if (lane == 0) {
                 const int bytes = min(kChunk, load_bytes - c * kChunk);
-                mbar_arrive_expect_tx(&full_bar[s], (uint32_t)bytes);
-                bulk_load_once(ring + (size_t)s * kChunk, src + (size_t)c * kChunk, (uint32_t)bytes, &full_bar[s], first);
+                mbar_arrive_expect_tx(&bd.full[s], (uint32_t)bytes);
+                bulk_load_once(ring + (size_t)s * kChunk, src + (size_t)c * kChunk, (uint32_t)bytes, &bd.full[s], first);
             }
             ++it;
             return true;
         };
         auto publish = [&](long long r) {
             if (lane == 0) {
-                row_q[q % kQueue] = r;
-                mbar_arrive(&row_bar[q % kQueue]);
+                bd.row_q[q % kQueue] = r;
+                mbar_arrive(&bd.row[q % kQueue]);
             }
             ++q;
         };
         auto zero = [&](long long r) {
-            const uint32_t use = zq / kZeroQueue;
-            if (use > 0 && !warp_wait(&zero_empty[zq % kZeroQueue], (use & 1u) ^ 1u, abortp)) return false;
+            const uint32_t use = zq / kZeros;
+            if (use > 0 && !warp_wait(&bd.zero_empty[zq % kZeros], (use & 1u) ^ 1u, abortp)) return false;
             if (lane == 0) {
-                zero_q[zq % kZeroQueue] = r;
-                mbar_arrive(&zero_full[zq % kZeroQueue]);
+                bd.zero_q[zq % kZeros] = r;
+                mbar_arrive(&bd.zero_full[zq % kZeros]);
             }
             ++zq;
             return true;
@@ -175,75 +186,107 @@ __global__ void __launch_bounds__((kWarps + 3) * 32, kBlocks) ring_kernel(RowsAr
             const uint32_t from = it > (uint32_t)sh.stages ? it - sh.stages : 0u;
             for (uint32_t j = from; j < it; ++j) {
                 const unsigned long long t0 = global_timer_ns();
-                while (!mbar_try_wait(&full_bar[j % sh.stages], (j / sh.stages) & 1u))
+                while (!mbar_try_wait(&bd.full[j % sh.stages], (j / sh.stages) & 1u))
                     if (global_timer_ns() - t0 > kWaitLimitNs) break;
             }
         }
     } else if (warp == kWarps + 2) {
         // ------------------------------- zeros for the rows that do not count ----------------
         for (uint32_t zq = 0;; ++zq) {
-            if (!warp_wait(&zero_full[zq % kZeroQueue], (zq / kZeroQueue) & 1u, abortp)) break;
-            const int64_t r = zero_q[zq % kZeroQueue];
+            if (!warp_wait(&bd.zero_full[zq % kZeros], (zq / kZeros) & 1u, abortp)) break;
+            const int64_t r = bd.zero_q[zq % kZeros];
             __syncwarp();
-            if (lane == 0) mbar_arrive(&zero_empty[zq % kZeroQueue]);
+            if (lane == 0) mbar_arrive(&bd.zero_empty[zq % kZeros]);
             if (r < 0) break;
             T* out = static_cast<T*>(a.grad) + r * a.ld_grad;
 #pragma unroll 4
             for (int v = lane; v < nvec; v += 32) st_stream(reinterpret_cast<uint4*>(out) + v, make_uint4(0, 0, 0, 0));
             if (lane < rest) out[nvec * E::kPer + lane] = E::put(0.f);
         }
+    } else if (warp == kWarps + 3) {
+        // ------------------------------- takes the list's columns out of the sum -------------
+        if (exclude(op) && stats) {
+            int st = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            for (uint32_t jq = 0; ok; ++jq) {
+                if (!warp_wait(&bd.row[jq % kQueue], (jq / kQueue) & 1u, abortp)) break;
+                if (bd.row_q[jq % kQueue] < 0) break;
+                if (!warp_wait(&bd.list[jq & 1], (jq >> 1) & 1u, abortp)) break;
+                const Slot slot = slot_at(slots + (jq & 1) * slot_bytes, sh.list);
+                // chunks loaded again come without: what is written for these columns is written over
+                for (int c = 0; c < sh.chunks + sh.again && ok; ++c) {
+                    if (!(ok = warp_wait(&bd.full[st], ph, abortp))) break;
+                    if (c < sh.chunks) {
+                        T* e = reinterpret_cast<T*>(ring + (size_t)st * kChunk);
+                        bool wrote = false;
+                        for (int j = lane; j < sh.list; j += 32) {
+                            const unsigned at = (unsigned)(slot.col[j] - c * kChunkVecs * E::kPer);
+                            if (at < (unsigned)(kChunkVecs * E::kPer)) {
+                                e[at] = E::put(-INFINITY);
+                                wrote = true;
+                            }
+                        }
+                        if (wrote) fence_proxy_async_smem();  // a bulk copy writes this stage next
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&bd.ready[st]);
+                    }
+                    if (++st == sh.stages) {
+                        st = 0;
+                        ph ^= 1u;
+                    }
+                }
+            }
+        }
     } else if (warp == kWarps + 1) {
         // ------------------------------- once a row -----------------------------------------
         const long long rows = op_counts(op) ? rows_that_count(op_counts(op), op_blocks(op)) : 0;
         const int n = list_size(op);
+        const float off = shift_fraction(lane);  // of consumer warp `lane`
+        const double unit = part_unit(off);
         for (uint32_t jq = 0;; ++jq) {
-            if (!warp_wait(&row_bar[jq % kQueue], (jq / kQueue) & 1u, abortp)) break;
-            const int64_t r = row_q[jq % kQueue];
+            if (!warp_wait(&bd.row[jq % kQueue], (jq / kQueue) & 1u, abortp)) break;
+            const int64_t r = bd.row_q[jq % kQueue];
             if (r < 0) break;
             const int s = jq & 1;
             const uint32_t ph = (jq >> 1) & 1u;
             // the consumers are through with this slot's last row, the one before the last: with sums to join, all of them have
             // begun the last row, whose sums are in; without, they say so
-            if (!stats && jq >= 2 && !warp_wait(&parts_bar[s], ph ^ 1u, abortp)) break;
+            if (!stats && jq >= 2 && !warp_wait(&bd.parts_in[s], ph ^ 1u, abortp)) break;
             const Slot slot = slot_at(slots + s * slot_bytes, sh.list);
             const T* row = static_cast<const T*>(a.logits) + r * a.ld;
             for (int j = lane; j < sh.list; j += 32) {
                 const int v = j < n ? column(op, r, j) : -1;
-                int key = -1;
                 if (v >= 0) {
-                    const int vec = v / E::kPer;
-                    key = vec / kChunkVecs * kWarps + vec % kLanes / 32;
                     slot.z[j] = E::get(row[v]);
                     slot.x[j] = entry(op, r, j);
                 }
                 slot.col[j] = v;
-                slot.key[j] = key;
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(&list_bar[s]);
+            if (lane == 0) mbar_arrive(&bd.list[s]);
             auto mine = look(op, a, r, rows, slot.col, slot.z, slot.x);
             RowStat st = known_stat(mine);
             if (stats) {
-                if (!warp_wait(&parts_bar[s], ph, abortp)) break;
-                st = join_parts(lane < kWarps ? parts[s][lane] : WarpPart{0.0, -INFINITY, kNoShift});
+                if (!warp_wait(&bd.parts_in[s], ph, abortp)) break;
+                st = join_parts(lane < kWarps ? bd.parts[s][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, off, unit, a.f);
             }
             const RowGrad g = finish(op, a, mine, st, slot.col, slot.z, slot.x);
             if (lane == 0) {
-                grads[s] = grad_const<DT>(g, st.max, a.f);
-                mbar_arrive(&grad_bar[s]);
+                bd.grads[s] = grad_const<DT>(g, st.max, a.f);
+                mbar_arrive(&bd.grad[s]);
             }
             values(op, a, r, mine, g, st, slot.col, slot.z, slot.x);
             __syncwarp();
-            if (lane == 0) mbar_arrive(&value_bar[s]);
+            if (lane == 0) mbar_arrive(&bd.value[s]);
         }
     } else {
         // ------------------------------- consumers ------------------------------------------
         const float off = shift_fraction(warp);
-        const double unit = warp_unit(off);
         const bool ex = exclude(op) && stats;
         const int whole = nvec / kChunkVecs;  // whole chunks of a row; at most one more
         int st = 0;
-        uint32_t ph = 0;
+        uint32_t ph = 0, rph = 0;  // rph: a bit for each stage, as not every load into one is made ready
         auto next_stage = [&]() {
             if (++st == sh.stages) {
                 st = 0;
@@ -252,7 +295,7 @@ __global__ void __launch_bounds__((kWarps + 3) * 32, kBlocks) ring_kernel(RowsAr
         };
         auto give_back = [&](int s) {
             __syncwarp();
-            if (lane == 0) mbar_arrive(&empty_bar[s]);
+            if (lane == 0) mbar_arrive(&bd.empty[s]);
         };
         const uint4* my_ring = reinterpret_cast<const uint4*>(ring) + tid;
         auto read = [&](int s, uint4 (&v)[kVecs]) {
@@ -283,65 +326,41 @@ __global__ void __launch_bounds__((kWarps + 3) * 32, kBlocks) ring_kernel(RowsAr
             return v;
         };
         for (uint32_t jq = 0;; ++jq) {
-            if (!warp_wait(&row_bar[jq % kQueue], (jq / kQueue) & 1u, abortp)) break;
-            const int64_t r = row_q[jq % kQueue];
+            if (!warp_wait(&bd.row[jq % kQueue], (jq / kQueue) & 1u, abortp)) break;
+            const int64_t r = bd.row_q[jq % kQueue];
             if (r < 0) break;
             const int slot_i = jq & 1;
             const uint32_t sph = (jq >> 1) & 1u;
             const Slot slot = slot_at(slots + slot_i * slot_bytes, sh.list);
             bool ok = true;
-            // chunks in which this warp has chosen columns, a bit each (the last one for all from 31 on)
-            uint32_t chosen = 0;
-            auto find_chosen = [&]() {
-                uint32_t m = 0;
-                for (int j = lane; j < sh.list; j += 32) {
-                    const int key = slot.key[j];
-                    if (key >= 0 && key % kWarps == warp) m |= 1u << min(key / kWarps, 31);
-                }
-                chosen = __reduce_or_sync(0xffffffffu, m);
-            };
-            auto has_chosen = [&](int c) { return (chosen >> min(c, 31) & 1u) != 0; };
-            if (ex) {
-                ok = warp_wait(&list_bar[slot_i], sph, abortp);
-                if (ok) find_chosen();
-            }
             uint4 kept[kKeep > 0 ? kKeep : 1][kVecs];
             int held = 0;  // stage of the first chunk that stays
             Part p;
-            // the next stage, holding chunk c for its first reading
-            auto arrived = [&](int c) {
-                if (!warp_wait(&full_bar[st], ph, abortp)) return false;
-                if (ex && has_chosen(c)) {  // the list's columns are left out of the sum
-                    T* e = reinterpret_cast<T*>(ring + (size_t)st * kChunk);
-                    for (int j = lane; j < sh.list; j += 32)
-                        if (slot.key[j] == c * kWarps + warp) e[slot.col[j] - c * kChunkVecs * E::kPer] = E::put(-INFINITY);
-                    fence_proxy_async_smem();  // a bulk copy writes this stage next
-                    __syncwarp();
-                }
-                return true;
+            auto landed = [&]() {  // the next stage, for a first reading
+                return ex ? warp_wait(&bd.ready[st], rph >> st & 1u, abortp) && ((rph ^= 1u << st), true) : warp_wait(&bd.full[st], ph, abortp);
             };
             const int held_from = grad ? keep + sh.again : sh.chunks;  // chunks from here on stay in their stages
             if (stats && ok) {
                 if (keep) {
 #pragma unroll
                     for (int c = 0; c < kKeep; ++c)
-                        if (ok && (ok = arrived(c))) {
+                        if (ok && (ok = landed())) {
                             read(st, kept[c]);
+                            p.template vectors<DT, kVecs>(kept[c], off, a.f);
                             give_back(st);
                             next_stage();
-                            p.template vectors<DT, kVecs>(kept[c], off, a.f);
                         }
                 }
                 for (int c = keep; c < whole && ok; ++c) {
-                    if (!(ok = arrived(c))) break;
+                    if (!(ok = landed())) break;
                     uint4 v[kVecs];
                     if (c == held_from) held = st;
                     read(st, v);
+                    p.template vectors<DT, kVecs>(v, off, a.f);
                     if (c < held_from) give_back(st);
                     next_stage();
-                    p.template vectors<DT, kVecs>(v, off, a.f);
                 }
-                if (whole < sh.chunks && ok && (ok = arrived(whole))) {
+                if (whole < sh.chunks && ok && (ok = landed())) {
                     if (whole == held_from) held = st;
 #pragma unroll 1
                     for (int j = 0; j < kVecs; ++j) {
@@ -354,43 +373,32 @@ __global__ void __launch_bounds__((kWarps + 3) * 32, kBlocks) ring_kernel(RowsAr
                     next_stage();
                 }
                 if (!ok) break;
-                const WarpPart w = warp_part(p, off, unit, a.f);
+                const WarpPart w = warp_part(p, a.f);
                 // two rows ago's sums have been read
-                if (!grad && jq >= 2 && !warp_wait(&grad_bar[slot_i], sph ^ 1u, abortp)) break;
+                if (!grad && jq >= 2 && !warp_wait(&bd.grad[slot_i], sph ^ 1u, abortp)) break;
                 if (lane == 0) {
-                    parts[slot_i][warp] = w;
-                    mbar_arrive(&parts_bar[slot_i]);
+                    bd.parts[slot_i][warp] = w;
+                    mbar_arrive(&bd.parts_in[slot_i]);
                 }
             }
             if (!ok) break;
             if (!grad) continue;
-            if (!warp_wait(&grad_bar[slot_i], sph, abortp)) break;
-            const Grad<DT> gr(grads[slot_i], a.f);
-            if (!ex) find_chosen();
+            if (!warp_wait(&bd.grad[slot_i], sph, abortp)) break;
+            const Grad<DT> gr(bd.grads[slot_i], a.f);
             T* out = static_cast<T*>(a.grad) + r * a.ld_grad;
             uint4* my_out = reinterpret_cast<uint4*>(out) + tid;
-            bool valued = false;
-            auto over = [&](int c) {  // the chosen columns over the vectors of chunk c
-                if (!has_chosen(c)) return;
-                if (!valued) ok = warp_wait(&value_bar[slot_i], sph, abortp);  // a wait that gives up: the values may be wrong, nothing else
-                valued = true;
-                __syncwarp();  // the vectors first
-                for (int j = lane; j < sh.list; j += 32)
-                    if (slot.key[j] == c * kWarps + warp) out[slot.col[j]] = E::put(slot.x[j]);
-            };
             // second reading: the gradient of a whole chunk
             auto write = [&](int c, const uint4 (&v)[kVecs]) {
                 uint4* ov = my_out + c * kChunkVecs;
 #pragma unroll
                 for (int j = 0; j < kVecs; ++j) st_stream(ov + j * kLanes, gr.vector(v[j]));
-                over(c);
             };
             // of a whole chunk c in stage s, which is then given back
             auto write_from = [&](int c, int s) {
                 uint4 v[kVecs];
                 read(s, v);
-                give_back(s);
                 write(c, v);
+                give_back(s);
             };
             // and of the last chunk, where that is not whole
             auto write_edge = [&](int s) {
@@ -411,7 +419,6 @@ __global__ void __launch_bounds__((kWarps + 3) * 32, kBlocks) ring_kernel(RowsAr
                     }
                 }
                 give_back(s);
-                over(whole);
             };
             if (stats) {
                 for (int c = held_from; c < whole; ++c) {
@@ -427,38 +434,48 @@ __global__ void __launch_bounds__((kWarps + 3) * 32, kBlocks) ring_kernel(RowsAr
             // chunks that are loaded for this reading
             const int from = stats ? keep : 0, to = stats ? keep + sh.again : sh.chunks;
             for (int c = from; c < to && ok; ++c) {
-                if (!(ok = warp_wait(&full_bar[st], ph, abortp))) break;
+                if (!(ok = warp_wait(&bd.full[st], ph, abortp))) break;
                 if (c < whole) write_from(c, st);
                 else write_edge(st);
                 next_stage();
             }
             if (!ok) break;
+            // the chosen columns over the vectors that hold them, which this warp wrote
+            bool mine = false;
+            for (int j = lane; j < sh.list; j += 32) mine |= slot.col[j] >= 0 && slot.col[j] / E::kPer % kLanes / 32 == warp;
+            if (__any_sync(0xffffffffu, mine)) {
+                if (!warp_wait(&bd.value[slot_i], sph, abortp)) break;
+                __syncwarp();
+                for (int j = lane; j < sh.list; j += 32) {
+                    const int v = slot.col[j];
+                    if (v >= 0 && v / E::kPer % kLanes / 32 == warp) out[v] = E::put(slot.x[j]);
+                }
+            }
             if (!stats) {  // the slot is free
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&parts_bar[slot_i]);
+                if (lane == 0) mbar_arrive(&bd.parts_in[slot_i]);
             }
         }
     }
     __syncthreads();
-    if (tid == 0 && abort_flag) {
+    if (tid == 0 && bd.abort_flag) {
         atomicMax(&a.w.head->status, (int)RAPID_ERR_TIMEOUT);
         if (a.stats) atomicMax(&a.stats->status, (int)RAPID_ERR_TIMEOUT);
     }
 }
 
 template <class Op>
-cudaError_t launch(const RowsArgs& a, const Op& op, int list, int sm_count, cudaStream_t stream) {
+cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_count, cudaStream_t stream) {
     const size_t es = elem_size(a.dtype);
     const int64_t row_bytes = ((int64_t)a.vocab * es + 15) / 16 * 16;
-    auto go = [&](auto kern, int warps, int vecs, int keep, int blocks) -> cudaError_t {
+    auto go = [&](auto kern, int warps, int vecs, int keep, int blocks, size_t board, int most) -> cudaError_t {
         RingShape sh{};
         const int chunk = warps * 32 * vecs * 16;
         sh.list = (list + 3) / 4 * 4;
-        const size_t extra = 2 * (size_t)sh.list * 16;
-        // 228 KB an SM; of every block 1 KB is the system's and up to 2 KB are barriers and queues
-        const size_t room = (size_t)228 * 1024 / blocks - 3072 - extra;
-        sh.stages = (int)(room / chunk);
-        if (sh.stages > kMaxStages) sh.stages = kMaxStages;
+        const size_t extra = board + 2 * (size_t)sh.list * kSlotEntry;
+        // 228 KB an SM, of which 1 KB for each block is the system's; 227 KB a block
+        const size_t room = std::min((size_t)227 * 1024, (size_t)228 * 1024 / blocks - 1024) - extra;
+        sh.stages = std::min((int)(room / chunk), most);
         sh.chunks = (int)((row_bytes + chunk - 1) / chunk);
         const bool both = !a.known && a.grad;
         sh.again = both && sh.chunks > keep + sh.stages ? sh.chunks - keep - sh.stages : 0;
@@ -471,25 +488,26 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, int sm_count, cuda
         if (sh.batch > 8) sh.batch = 8;
         if (grid > a.n_rows) grid = a.n_rows;
         sh.stride = scatter_stride(a.n_rows);
-        kern<<<(unsigned)grid, (warps + 3) * 32, smem, stream>>>(a, op, sh);
+        kern<<<(unsigned)grid, (warps + (ex ? 4 : 3)) * 32, smem, stream>>>(a, op, sh);
         return cudaGetLastError();
     };
     auto by_type = [&](auto dt) -> cudaError_t {
         constexpr int DT = decltype(dt)::value;
-        if (row_bytes <= 16384) return go(ring_kernel<DT, Op, 4, 4, 0, 4>, 4, 4, 0, 4);
-        if (row_bytes <= 65536) return go(ring_kernel<DT, Op, 8, 4, 0, 2>, 8, 4, 0, 2);
-        if (!a.known && a.grad && row_bytes > 5 * 32768) return go(ring_kernel<DT, Op, 16, 4, 3, 1>, 16, 4, 3, 1);
-        return go(ring_kernel<DT, Op, 16, 4, 0, 1>, 16, 4, 0, 1);
+        constexpr size_t b4 = sizeof(Board<4>), b8 = sizeof(Board<8>), b16 = sizeof(Board<16>);
+        if (row_bytes <= 16384) return go(ring_kernel<DT, Op, 4, 4, 0, 3>, 4, 4, 0, 3, b4, Board<4>::kStages);
+        if (row_bytes <= 65536) return go(ring_kernel<DT, Op, 8, 4, 0, 2>, 8, 4, 0, 2, b8, Board<8>::kStages);
+        if (!a.known && a.grad && row_bytes > 5 * 32768) return go(ring_kernel<DT, Op, 16, 4, 3, 1>, 16, 4, 3, 1, b16, Board<16>::kStages);
+        return go(ring_kernel<DT, Op, 16, 4, 0, 1>, 16, 4, 0, 1, b16, Board<16>::kStages);
     };
     return a.dtype == RAPID_BF16 ? by_type(std::integral_constant<int, RAPID_BF16>{}) : by_type(std::integral_constant<int, RAPID_F32>{});
 }
 
 }  // namespace
 
-cudaError_t launch_rows(const RowsArgs& a, const ClipOp& op, int sm_count, cudaStream_t stream) { return launch(a, op, 1, sm_count, stream); }
-cudaError_t launch_rows(const RowsArgs& a, const PrefOp& op, int sm_count, cudaStream_t stream) { return launch(a, op, 1, sm_count, stream); }
+cudaError_t launch_rows(const RowsArgs& a, const ClipOp& op, int sm_count, cudaStream_t stream) { return launch(a, op, 1, false, sm_count, stream); }
+cudaError_t launch_rows(const RowsArgs& a, const PrefOp& op, int sm_count, cudaStream_t stream) { return launch(a, op, 1, false, sm_count, stream); }
 cudaError_t launch_rows(const RowsArgs& a, const DistillOp& op, int sm_count, cudaStream_t stream) {
-    return launch(a, op, op.k, sm_count, stream);
+    return launch(a, op, op.k, op.tail != 0 && !a.known, sm_count, stream);
 }
 
 }  // namespace losses

@@ -255,6 +255,25 @@ struct Part {
     }
 };
 
+// 2^y and log2(s) in double where a whole row waits for them: Taylor's series of e^t for |t| <= ln(2) / 2 to t^11 (the rest is below
+// 7e-15) evaluated in pairs, six dependent steps; the logarithm by one step of Newton's iteration from the hardware's.  2^y below
+// 2^-1020 is 0.
+__device__ __forceinline__ double exp2_short(double y) {
+    if (!(y > -1020.0 && y < 1020.0)) return y > 0.0 || y != y ? exp2(y) : 0.0;
+    const double n = rint(y), t = (y - n) * kLn2D, t2 = t * t, t4 = t2 * t2;
+    const double a0 = 1.0 + t, a1 = fma(t, 1.0 / 6, 0.5), a2 = fma(t, 1.0 / 120, 1.0 / 24), a3 = fma(t, 1.0 / 5040, 1.0 / 720);
+    const double a4 = fma(t, 1.0 / 362880, 1.0 / 40320), a5 = fma(t, 1.0 / 39916800, 1.0 / 3628800);
+    const double b0 = fma(a1, t2, a0), b1 = fma(a3, t2, a2), b2 = fma(a5, t2, a4);
+    return fma(b2, t4 * t4, fma(b1, t4, b0)) * __hiloint2double(((int)n + 1023) << 20, 0);
+}
+__device__ __forceinline__ double log2_short(double s) {  // s > 0, normal
+    const int e = (__double2hiint(s) >> 20) - 1023;
+    const double m = __hiloint2double(__double2hiint(s) - (e << 20), __double2loint(s));  // in [1, 2)
+    const double l = (double)__log2f((float)m);
+    const double r = fma(m, exp2_short(-l), -1.0);  // below 1e-6
+    return (double)e + fma(r * fma(r, -0.5, 1.0), kLog2eD, l);
+}
+
 // Maximum over the warp of floats that are not NaN.
 __device__ __forceinline__ float warp_top(float v) {
     float r;
@@ -262,34 +281,22 @@ __device__ __forceinline__ float warp_top(float v) {
     return r;
 }
 
-// A warp's part, the same in all lanes: its largest logit, and its sum as s 2^n.  The largest logit's term, which may carry nearly
-// all of the row's probability, is taken out of the sum again and put back exactly.
+// A warp's part, the same in all lanes: its largest logit, its shift, and its sum without that logit's term, which may carry nearly
+// all of the row's probability and is put back exactly where the parts meet.
 struct WarpPart {
     double s;
-    float m;
-    int n;
+    float m, sh;  // sh = -inf where there is nothing
 };
-// 2^off of a warp, for warp_part
-__device__ __forceinline__ double warp_unit(float off) { return exp2((double)off) / (1.0 + (double)kEx2Mean); }
-constexpr int kNoShift = -(1 << 20);
-__device__ __forceinline__ WarpPart warp_part(const Part& p, float off, double unit, const Factor& f) {
+__device__ __forceinline__ WarpPart warp_part(const Part& p, const Factor& f) {
     WarpPart w;
     w.m = warp_top(p.m);
-    const float sh = warp_top(p.s > 0.f ? p.sh : -INFINITY);
+    w.sh = warp_top(p.s > 0.f ? p.sh : -INFINITY);
     double s = (double)p.s + (double)p.c;
     const unsigned top = __ballot_sync(0xffffffffu, p.m == w.m && w.m > kNothing);
     if (top && (threadIdx.x & 31) == __ffs(top) - 1) s -= (double)p.term(p.m, f);
-    if (p.s > 0.f) s *= (double)ex2_approx(p.sh - sh);  // an exact power of two
+    if (p.s > 0.f) s *= (double)ex2_approx(p.sh - w.sh);  // an exact power of two
     else s = 0.0;
-    w.n = kNoShift;
-    w.s = 0.0;
-    if (sh > -INFINITY) {
-        const float n = rintf(sh - off);
-        const double frac = (double)sh - (double)n;
-        if (frac != (double)off) unit = exp2(frac) / (1.0 + (double)kEx2Mean);  // a shift so large that the fraction was rounded
-        w.s = warp_sum(s) * unit + exp2((double)w.m * f.kd - (double)n);
-        w.n = (int)n;
-    }
+    w.s = warp_sum(s);
     return w;
 }
 
@@ -297,13 +304,22 @@ struct RowStat {
     double lse2;  // -inf when no logit is left
     float max;
 };
-// The warps' parts together, by one warp: lane i holds warp i's part (n = kNoShift where there is none).
-__device__ __forceinline__ RowStat join_parts(const WarpPart& p) {
+// The warps' parts together, by one warp: lane i holds warp i's part, the fraction of its shift, and unit = 2^off / (1 + kEx2Mean).
+__device__ __forceinline__ double part_unit(float off) { return exp2((double)off) / (1.0 + (double)kEx2Mean); }
+__device__ __forceinline__ RowStat join_parts(const WarpPart& p, float off, double unit, const Factor& f) {
     RowStat r;
     r.max = warp_top(p.m);
-    const int n = __reduce_max_sync(0xffffffffu, p.n), down = n - p.n;
-    const double s = warp_sum(down < 1000 ? p.s * __hiloint2double((1023 - down) << 20, 0) : 0.0);
-    r.lse2 = s > 0.0 ? (double)n + log2(s) : -INFINITY;
+    const bool some = p.sh > -INFINITY;
+    const float n = some ? rintf(p.sh - off) : -INFINITY, top = warp_top(n);  // the whole part of the shift
+    double s = 0.0;
+    if (some) {
+        const double frac = (double)p.sh - (double)n;
+        if (frac != (double)off) unit = exp2(frac) / (1.0 + (double)kEx2Mean);  // a shift so large that its fraction was rounded
+        const int down = (int)fminf(top - n, 1000.f);
+        s = fma(p.s, unit, exp2_short((double)p.m * f.kd - (double)n)) * __hiloint2double((1023 - down) << 20, 0);
+    }
+    s = warp_sum(s);
+    r.lse2 = s > 0.0 ? (double)top + log2_short(s) : -INFINITY;
     return r;
 }
 
@@ -313,7 +329,8 @@ __device__ __forceinline__ float shift_fraction(int warp) { return (float)(((uns
 
 // dz_v = a 2^(x_v - lse2).  bf16: |a| goes into the exponent, one multiply-add and one exponential an element.  float: the largest
 // logit is taken off first, which keeps the argument small and so its rounding below the result's; a is multiplied at the end.
-// The constants are formed once a row; they are floats, whose rounding (and that of log2f) is some 2^-18 of a probability at most.
+// The constants are formed once a row; they are floats, whose rounding (and the error of the hardware's logarithm, 2^-22) is some
+// 2^-18 of a probability at most.
 struct RowGrad {
     double a, lse2;
 };
@@ -326,7 +343,7 @@ __device__ __forceinline__ GradConst grad_const(const RowGrad& g, float max, con
     k.a = (float)g.a;
     if (DT == RAPID_BF16) {
         k.m = 0.f;
-        k.c = (float)((double)log2f(fabsf(k.a)) - g.lse2);
+        k.c = (float)((double)__log2f(fabsf(k.a)) - g.lse2);
         if (k.a == 0.f) k.c = -INFINITY;
     } else {
         k.m = max > kNothing ? max : 0.f;
@@ -436,7 +453,7 @@ __device__ __forceinline__ ClipIn clip_in(const ClipOp& op, int64_t r) {
 }
 __device__ __forceinline__ ClipTerms clip_terms(const ClipOp& op, const ClipIn& in, double lp) {
     ClipTerms t;
-    const double rho = exp(lp - in.old);
+    const double rho = exp2_short((lp - in.old) * kLog2eD);
     const double u = in.A != 0.0 ? rho * in.A : 0.0;  // A = 0 leaves nothing, even of an infinite ratio
     const double v = in.A != 0.0 ? fmin(fmax(rho, 1.0 - op.low), 1.0 + op.high) * in.A : 0.0;
     t.cut = v < u;
@@ -444,8 +461,8 @@ __device__ __forceinline__ ClipTerms clip_terms(const ClipOp& op, const ClipIn& 
     t.slope = t.cut ? 0.0 : u;
     t.kl = 0.0;
     if (op.ref_logp) {
-        const double d = in.ref - lp, e = expm1(d);
-        t.kl = isinf(e) ? e : e - d;
+        const double d = in.ref - lp, e = exp2_short(d * kLog2eD) - 1.0;
+        t.kl = isinf(e) ? e : e - d;  // off by 1e-15
         if (op.beta != 0.0) {
             t.loss += op.beta * t.kl;
             t.slope += op.beta * e;
@@ -504,7 +521,7 @@ __device__ __forceinline__ PrefRow look(const PrefOp& op, const RowsArgs& a, int
 struct DistillRow {
     double teacher, w;
     double p0, lp0;   // probability of the tokens beside the list, and its logarithm
-    double list_sum;  // this lane's share of the list's sum of 2^(x - top's x)
+    double list_sum;  // the list's sum of 2^(x - top's x)
     float top;        // the list's largest logit
 };
 __device__ __forceinline__ DistillRow look(const DistillOp& op, const RowsArgs&, int64_t r, long long rows, const int* col, const float* z,
@@ -525,6 +542,7 @@ __device__ __forceinline__ DistillRow look(const DistillOp& op, const RowsArgs&,
     if (row.top > -INFINITY)
         for (int j = lane; j < op.k; j += 32)
             if (col[j] >= 0) row.list_sum += exp2(((double)z[j] - (double)row.top) * op.kd);
+    row.list_sum = warp_sum(row.list_sum);
     return row;
 }
 __device__ __forceinline__ RowStat known_stat(const ClipRow&) { return RowStat{0.0, 0.f}; }
@@ -565,17 +583,12 @@ __device__ __forceinline__ RowGrad finish(const DistillOp& op, const RowsArgs&, 
     RowGrad g{row.w, st.lse2};
     if (!op.tail) return g;
     // the student's log-sum-exp over the whole vocabulary, in a sum against the larger of the rest's and the list's largest term
-    const int lane = threadIdx.x & 31;
     const double x0 = row.top > -INFINITY ? (double)row.top * op.kd : -INFINITY;
     const double top = fmax(st.lse2, x0);
-    double s = 0.0;
-    if (top > -INFINITY) {
-        s = row.list_sum * exp2(x0 - top);
-        if (lane == 0) s += exp2(st.lse2 - top);
-    }
-    s = warp_sum(s);
-    g.lse2 = s > 0.0 ? top + log2(s) : -INFINITY;
-    if (row.p0 > 0.0 && st.lse2 > -INFINITY) g.a = row.w * (1.0 - exp2(row.lp0 - (st.lse2 - g.lse2)));
+    if (top == -INFINITY) return g;
+    // (the list's sum holds its largest term, 1, so neither logarithm's argument is small)
+    g.lse2 = top + log2_short(row.list_sum * exp2_short(x0 - top) + exp2_short(st.lse2 - top));
+    if (row.p0 > 0.0 && st.lse2 > -INFINITY) g.a = row.w * (1.0 - exp2_short(row.lp0 - (st.lse2 - g.lse2)));
     return g;
 }
 __device__ __forceinline__ void values(const DistillOp& op, const RowsArgs& a, int64_t r, const DistillRow& row, const RowGrad& g,
