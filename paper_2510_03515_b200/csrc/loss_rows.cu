@@ -464,6 +464,317 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
     }
 }
 
+// ---- shorter rows ----------------------------------------------------------------------------------------------
+
+// A group of G warps holds a whole row in its share of the SM's shared memory and does everything for it; as many groups as fit work
+// side by side on an SM and hide one another's latencies.  A row comes in kParts bulk copies; a part's place is loaded with the next
+// row as soon as the second reading is through with it.  Rows are drawn from a counter, two ahead.
+
+constexpr int kParts = 4;
+
+struct GroupShape {
+    int groups;          // of a block
+    int row_bytes;       // place of a row, whole parts
+    int group_bytes;     // of a group in shared memory
+    int part_vecs;       // vectors of a part, a multiple of the group's threads
+    int parts;           // of a row
+    int list;
+    unsigned long long stride;
+};
+
+struct GroupBoard {
+    uint64_t full[kParts];
+    WarpPart parts[2][8];
+    GradConst grad;
+    long long next[2];  // the next row, ~row when it does not count; of odd and even turns
+};
+
+// The warps of a group together, with the OR of what they say: after a wait that gave up all leave together.
+template <int G>
+__device__ __forceinline__ bool group_sync(int id, bool flag) {
+    if constexpr (G == 1) return __any_sync(0xffffffffu, flag);
+    uint32_t out;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 q, %1, 0;\n\t"
+        "barrier.cta.red.or.pred p, %2, %3, q;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(out)
+        : "r"((uint32_t)flag), "r"(id), "n"(G * 32)
+        : "memory");
+    return out != 0;
+}
+
+template <int DT, class Op, int G>
+__global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a, Op op, GroupShape sh) {
+    using E = Elem<DT>;
+    using T = typename E::T;
+    constexpr int kLanes = G * 32;
+    constexpr int U = 4;  // vectors of a thread at a time
+    extern __shared__ __align__(128) uint8_t dyn[];
+    __shared__ int abort_flag;
+    __shared__ long long count;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = warp / G, gw = warp % G, gt = threadIdx.x % kLanes;
+    uint8_t* place = dyn + (size_t)group * sh.group_bytes;
+    GroupBoard& bd = *reinterpret_cast<GroupBoard*>(place + sh.row_bytes);
+    const Slot slot = slot_at(place + sh.row_bytes + sizeof(GroupBoard), sh.list);
+    if (gt == 0) {
+        for (int p = 0; p < kParts; ++p) mbar_init(&bd.full[p], 1);
+        mbar_init_fence();
+    }
+    if (threadIdx.x == 0) abort_flag = 0;
+    if (warp == 0 && op_counts(op)) {
+        const long long n = rows_that_count(op_counts(op), op_blocks(op));
+        if (lane == 0) count = n;
+    }
+    __syncthreads();
+    volatile int* abortp = &abort_flag;
+    const long long rows = op_counts(op) ? count : 0;
+    const bool stats = !a.known, grad = a.grad != nullptr, ex = exclude(op) && stats;
+    const int nvec = a.vocab / E::kPer, rest = a.vocab - nvec * E::kPer, all = nvec + (rest ? 1 : 0);
+    const int n_list = list_size(op), id = group + 1;
+    const uint64_t once = policy_first();
+    const float off = shift_fraction(gw), unit_off = shift_fraction(lane);
+    const double unit = part_unit(unit_off);
+    const uint4* row_place = reinterpret_cast<const uint4*>(place);
+
+    auto row_of = [&](unsigned int t) -> int64_t { return (int64_t)(((unsigned long long)t * sh.stride) % (unsigned long long)a.n_rows); };
+    uint32_t issued = 0, phase_of = 0;  // a bit for each part: anything loaded, and the phase of its last load
+    auto load_part = [&](int64_t r, int p, uint32_t phase) {  // by the group's first thread
+        issued |= 1u << p;
+        phase_of = (phase_of & ~(1u << p)) | phase << p;
+        const int v = p * sh.part_vecs, bytes = min(sh.part_vecs, all - v) * 16;
+        mbar_arrive_expect_tx(&bd.full[p], (uint32_t)bytes);
+        bulk_load_once(place + (size_t)v * 16, static_cast<const uint8_t*>(a.logits) + (size_t)r * a.ld * sizeof(T) + (size_t)v * 16, (uint32_t)bytes,
+                       &bd.full[p], once);
+    };
+    auto state_of = [&](unsigned int t) -> int { return t < a.n_rows ? (int)a.w.state[row_of(t)] : ROW_MASKED; };
+
+    // draws: the first ones are dealt out, one to every group of the grid; gt == 0 is ahead by two
+    const unsigned int everyone = gridDim.x * sh.groups;
+    unsigned int t0 = group * gridDim.x + blockIdx.x, t1 = 0, t2 = 0;
+    int state1 = ROW_MASKED;
+    int64_t row = -1;  // this row; ~row when it does not count; n_rows when there are none left
+    bool live = false;
+    {
+        const int st = state_of(t0);
+        live = st == ROW_OK;
+        row = t0 < a.n_rows ? row_of(t0) : a.n_rows;
+        if (gt == 0) {
+            t1 = everyone + atomicAdd(&a.w.head->ticket, 1u);
+            if (live)
+                for (int p = 0; p < sh.parts; ++p) load_part(row, p, 0u);
+        }
+    }
+    uint32_t ph = 0;  // phase of the parts, that is of the rows that are read
+    bool ok = true;
+    for (uint32_t turn = 0; row < a.n_rows; ++turn) {
+        if (gt == 0) {
+            t2 = everyone + atomicAdd(&a.w.head->ticket, 1u);
+            state1 = state_of(t1);
+        }
+        auto announce = [&]() {  // the next row, to the group
+            if (gt == 0) {
+                const int64_t r = t1 < a.n_rows ? row_of(t1) : a.n_rows;
+                bd.next[turn & 1] = t1 < a.n_rows && state1 != ROW_OK ? ~r : r;
+                t1 = t2;
+            }
+        };
+        T* out = static_cast<T*>(a.grad) + row * a.ld_grad;
+        if (!live) {
+            if (grad) {
+                for (int v = gt; v < nvec; v += kLanes) st_stream(reinterpret_cast<uint4*>(out) + v, make_uint4(0, 0, 0, 0));
+                if (gt < rest) out[nvec * E::kPer + gt] = E::put(0.f);
+            }
+            announce();
+            if (group_sync<G>(id, !ok)) break;
+            const long long next = bd.next[turn & 1];
+            row = next < 0 ? ~next : next;
+            live = next >= 0 && next < a.n_rows;
+            if (gt == 0 && live)
+                for (int p = 0; p < sh.parts; ++p) load_part(row, p, ph);
+            continue;
+        }
+        // ---- the row's chosen columns, by the group's first warp ----
+        auto landed = [&](int p) { return ok && (ok = warp_wait(&bd.full[p], ph, abortp)); };
+        decltype(look(op, a, row, rows, slot.col, slot.z, slot.x)) mine{};
+        if (gw == 0) {
+            for (int j = lane; j < n_list; j += 32) {
+                const int v = column(op, row, j);
+                slot.col[j] = v;
+                if (v >= 0) slot.x[j] = entry(op, row, j);
+            }
+            if (ex) {  // they are taken out of the sum before anyone reads the row
+                for (int p = 0; p < sh.parts; ++p) landed(p);
+                if (ok)
+                    for (int j = lane; j < n_list; j += 32) {
+                        const int v = slot.col[j];
+                        if (v < 0) continue;
+                        T* e = reinterpret_cast<T*>(place) + v;
+                        slot.z[j] = E::get(*e);
+                        *e = E::put(-INFINITY);
+                    }
+                fence_proxy_async_smem();  // a bulk copy writes there next
+                __syncwarp();
+            }
+        }
+        if (G > 1 && ex && group_sync<G>(id, !ok)) break;
+        // vector `at` of the row; columns behind the last read as -inf
+        auto read = [&](int at) {
+            constexpr uint32_t kNone = DT == RAPID_BF16 ? 0xff80ff80u : 0xff800000u;
+            uint4 v = make_uint4(kNone, kNone, kNone, kNone);
+            if (at < nvec) v = row_place[at];
+            else if (at == nvec && rest) {
+                const T* e = reinterpret_cast<const T*>(row_place + at);
+                uint32_t w[4] = {kNone, kNone, kNone, kNone};
+#pragma unroll
+                for (int i = 0; i < E::kPer; ++i) {
+                    if (i >= rest) continue;
+                    if constexpr (DT == RAPID_BF16) {
+                        const uint32_t b = e[i];
+                        w[i / 2] = (i & 1) ? ((w[i / 2] & 0xffffu) | (b << 16)) : ((w[i / 2] & 0xffff0000u) | b);
+                    } else {
+                        w[i] = __float_as_uint(e[i]);
+                    }
+                }
+                v = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            return v;
+        };
+        bool left = false;
+        long long next = 0;
+        // part p has been read for the last time: the next row's comes there
+        auto hand_over = [&](int p) {
+            if (group_sync<G>(id, !ok)) {
+                left = true;
+                return;
+            }
+            if (p == 0) next = bd.next[turn & 1];  // announced before
+            if (gt == 0 && next >= 0 && next < a.n_rows) {
+                fence_proxy_async_smem();
+                load_part(next, p, ph ^ 1u);
+            }
+        };
+        RowStat st{0.0, 0.f};
+        if (stats) {
+            // ---- first reading ----
+            if (!grad) announce();
+            Part p;
+            for (int q = 0; q < sh.parts && !left; ++q) {
+                if (landed(q)) {
+                    const int end = min((q + 1) * sh.part_vecs, all);
+                    int v = q * sh.part_vecs + gt;
+                    for (; v - lane + (U - 1) * kLanes + 31 < min(end, nvec); v += U * kLanes) {
+                        uint4 w[U];
+#pragma unroll
+                        for (int j = 0; j < U; ++j) w[j] = row_place[v + j * kLanes];
+                        p.template vectors<DT, U>(w, off, a.f);
+                    }
+                    for (; v - lane < end; v += kLanes) {
+                        uint4 w[1] = {read(v)};
+                        p.template vectors<DT, 1>(w, off, a.f);
+                    }
+                }
+                if (!grad) {
+                    if (gw == 0 && !ex)  // before the part goes
+                        for (int j = lane; j < n_list; j += 32) {
+                            const int v = slot.col[j];
+                            if (v >= 0 && v / E::kPer / sh.part_vecs == q) slot.z[j] = E::get(reinterpret_cast<const T*>(place)[v]);
+                        }
+                    hand_over(q);
+                }
+            }
+            if (left) break;
+            const WarpPart w = warp_part(p, a.f);
+            if constexpr (G == 1) {
+                st = join_parts(lane == 0 ? w : WarpPart{0.0, -INFINITY, -INFINITY}, unit_off, unit, a.f);
+            } else {
+                if (lane == 0) bd.parts[turn & 1][gw] = w;
+                if (group_sync<G>(id, !ok)) break;
+                if (gw == 0) st = join_parts(lane < G ? bd.parts[turn & 1][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, unit_off, unit, a.f);
+            }
+            if (G == 1 && !ok) break;
+        } else if (gw == 0) {  // the first parts may come while the columns are looked up
+            for (int p = 0; p < sh.parts; ++p) landed(p);
+        }
+        RowGrad g{0.0, 0.0};
+        if (gw == 0 && ok) {
+            __syncwarp();
+            if (!ex && grad)
+                for (int j = lane; j < n_list; j += 32) {
+                    const int v = slot.col[j];
+                    if (v >= 0) slot.z[j] = E::get(reinterpret_cast<const T*>(place)[v]);
+                }
+            __syncwarp();
+            mine = look(op, a, row, rows, slot.col, slot.z, slot.x);
+            if (!stats) st = known_stat(mine);
+            g = finish(op, a, mine, st, slot.col, slot.z, slot.x);
+            if (lane == 0) bd.grad = grad_const<DT>(g, st.max, a.f);
+            if (grad) announce();
+        }
+        if (grad) {
+            // ---- second reading ----
+            if (group_sync<G>(id, !ok)) break;
+            const Grad<DT> gr(bd.grad, a.f);
+            for (int q = 0; q < sh.parts && !left; ++q) {
+                if (!stats) landed(q);
+                if (ok) {
+                    const int end = min((q + 1) * sh.part_vecs, all);
+                    int v = q * sh.part_vecs + gt;
+                    uint4* ov = reinterpret_cast<uint4*>(out);
+                    for (; v - lane + (U - 1) * kLanes + 31 < min(end, nvec); v += U * kLanes) {
+                        uint4 w[U];
+#pragma unroll
+                        for (int j = 0; j < U; ++j) w[j] = row_place[v + j * kLanes];
+#pragma unroll
+                        for (int j = 0; j < U; ++j) st_stream(ov + v + j * kLanes, gr.vector(w[j]));
+                    }
+                    for (; v - lane < end; v += kLanes) {
+                        const uint4 y = gr.vector(read(v));
+                        if (v < nvec) st_stream(ov + v, y);
+                        else if (v == nvec && rest) {
+                            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                            for (int i = 0; i < E::kPer; ++i) {
+                                if (i >= rest) continue;
+                                if constexpr (DT == RAPID_BF16) out[nvec * E::kPer + i] = (T)(w[i / 2] >> (16 * (i & 1)));
+                                else out[nvec * E::kPer + i] = __uint_as_float(w[i]);
+                            }
+                        }
+                    }
+                }
+                hand_over(q);
+            }
+            if (left) break;
+        }
+        if (gw == 0) {  // (after the group's last meeting: all vectors are written)
+            values(op, a, row, mine, g, st, slot.col, slot.z, slot.x);
+            __syncwarp();
+            if (grad)
+                for (int j = lane; j < n_list; j += 32) {
+                    const int v = slot.col[j];
+                    if (v >= 0) out[v] = E::put(slot.x[j]);
+                }
+            __syncwarp();
+        }
+        ph ^= 1u;
+        row = next < 0 ? ~next : next;
+        live = next >= 0 && next < a.n_rows;
+    }
+    if (gt == 0 && *abortp) {  // gave up: let the copies already issued land before the block's memory goes away
+        for (int p = 0; p < sh.parts; ++p) {
+            const unsigned long long t = global_timer_ns();
+            while ((issued >> p & 1u) && !mbar_try_wait(&bd.full[p], phase_of >> p & 1u))
+                if (global_timer_ns() - t > kWaitLimitNs) break;
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && abort_flag) {
+        atomicMax(&a.w.head->status, (int)RAPID_ERR_TIMEOUT);
+        if (a.stats) atomicMax(&a.stats->status, (int)RAPID_ERR_TIMEOUT);
+    }
+}
+
 template <class Op>
 cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_count, cudaStream_t stream) {
     const size_t es = elem_size(a.dtype);
@@ -491,11 +802,31 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
         kern<<<(unsigned)grid, (warps + (ex ? 4 : 3)) * 32, smem, stream>>>(a, op, sh);
         return cudaGetLastError();
     };
+    auto go_groups = [&](auto kern, int G) -> cudaError_t {
+        GroupShape sh{};
+        const int lanes = G * 32, all = (int)(row_bytes / 16);
+        sh.list = (list + 3) / 4 * 4;
+        sh.part_vecs = ((all + kParts - 1) / kParts + lanes - 1) / lanes * lanes;
+        if (sh.part_vecs > 4 * lanes) sh.part_vecs = (sh.part_vecs + 4 * lanes - 1) / (4 * lanes) * (4 * lanes);
+        sh.parts = (all + sh.part_vecs - 1) / sh.part_vecs;
+        sh.row_bytes = (int)row_bytes;
+        sh.group_bytes = (int)((row_bytes + sizeof(GroupBoard) + sh.list * kSlotEntry + 127) / 128 * 128);
+        sh.groups = std::min((227 * 1024 - 64) / sh.group_bytes, (G == 1 ? 24 : 16) / G);
+        const size_t smem = (size_t)sh.groups * sh.group_bytes;
+        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        const int64_t grid = std::min((int64_t)sm_count, a.n_rows);
+        sh.stride = scatter_stride(a.n_rows);
+        kern<<<(unsigned)grid, sh.groups * lanes, smem, stream>>>(a, op, sh);
+        return cudaGetLastError();
+    };
     auto by_type = [&](auto dt) -> cudaError_t {
         constexpr int DT = decltype(dt)::value;
-        constexpr size_t b4 = sizeof(Board<4>), b8 = sizeof(Board<8>), b16 = sizeof(Board<16>);
-        if (row_bytes <= 16384) return go(ring_kernel<DT, Op, 4, 4, 0, 3>, 4, 4, 0, 3, b4, Board<4>::kStages);
-        if (row_bytes <= 65536) return go(ring_kernel<DT, Op, 8, 4, 0, 2>, 8, 4, 0, 2, b8, Board<8>::kStages);
+        if (row_bytes <= 16384) return go_groups(group_kernel<DT, Op, 1>, 1);
+        if (row_bytes <= 32768) return go_groups(group_kernel<DT, Op, 2>, 2);
+        if (row_bytes <= 73728) return go_groups(group_kernel<DT, Op, 4>, 4);
+        if (row_bytes <= 110 * 1024) return go_groups(group_kernel<DT, Op, 8>, 8);
+        constexpr size_t b16 = sizeof(Board<16>);
         if (!a.known && a.grad && row_bytes > 5 * 32768) return go(ring_kernel<DT, Op, 16, 4, 3, 1>, 16, 4, 3, 1, b16, Board<16>::kStages);
         return go(ring_kernel<DT, Op, 16, 4, 0, 1>, 16, 4, 0, 1, b16, Board<16>::kStages);
     };
