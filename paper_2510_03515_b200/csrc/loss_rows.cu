@@ -114,9 +114,9 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
     __syncthreads();
     volatile int* abortp = &bd.abort_flag;
 
-    const bool stats = !a.known, grad = a.grad != nullptr;
+    const bool grad = a.grad != nullptr;
     const int nvec = a.vocab / E::kPer, rest = a.vocab - nvec * E::kPer;
-    const int keep = stats && grad ? kKeep : 0;  // chunks that stay in registers
+    const int keep = grad ? kKeep : 0;  // chunks that stay in registers
 
     if (warp == kWarps) {
         // ------------------------------- producer -------------------------------------------
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
         }
     } else if (warp == kWarps + 3) {
         // ------------------------------- takes the list's columns out of the sum -------------
-        if (exclude(op) && stats) {
+        if (exclude(op)) {
             int st = 0;
             uint32_t ph = 0;
             bool ok = true;
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
         }
     } else if (warp == kWarps + 1) {
         // ------------------------------- once a row -----------------------------------------
-        const long long rows = op_counts(op) ? rows_that_count(op_counts(op), op_blocks(op)) : 0;
+        const double shared = shared_weight(op, rows_that_count(op_counts(op), op_blocks(op)));
         const int n = list_size(op);
         const float off = shift_fraction(lane);  // of consumer warp `lane`
         const double unit = part_unit(off);
@@ -250,9 +250,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
             if (r < 0) break;
             const int s = jq & 1;
             const uint32_t ph = (jq >> 1) & 1u;
-            // the consumers are through with this slot's last row, the one before the last: with sums to join, all of them have
-            // begun the last row, whose sums are in; without, they say so
-            if (!stats && jq >= 2 && !warp_wait(&bd.parts_in[s], ph ^ 1u, abortp)) break;
+            // (the consumers are through with this slot's last row, the one before the last: the last row's sums are all in)
             const Slot slot = slot_at(slots + s * slot_bytes, sh.list);
             const T* row = static_cast<const T*>(a.logits) + r * a.ld;
             for (int j = lane; j < sh.list; j += 32) {
@@ -265,12 +263,9 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&bd.list[s]);
-            auto mine = look(op, a, r, rows, slot.col, slot.z, slot.x);
-            RowStat st = known_stat(mine);
-            if (stats) {
-                if (!warp_wait(&bd.parts_in[s], ph, abortp)) break;
-                st = join_parts(lane < kWarps ? bd.parts[s][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, off, unit, a.f);
-            }
+            auto mine = look(op, r, shared, slot.col, slot.z, slot.x);
+            if (!warp_wait(&bd.parts_in[s], ph, abortp)) break;
+            const RowStat st = join_parts(lane < kWarps ? bd.parts[s][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, off, unit, a.f);
             const RowGrad g = finish(op, a, mine, st, slot.col, slot.z, slot.x);
             if (lane == 0) {
                 bd.grads[s] = grad_const<DT>(g, st.max, a.f);
@@ -283,7 +278,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
     } else {
         // ------------------------------- consumers ------------------------------------------
         const float off = shift_fraction(warp);
-        const bool ex = exclude(op) && stats;
+        const bool ex = exclude(op);
         const int whole = nvec / kChunkVecs;  // whole chunks of a row; at most one more
         int st = 0;
         uint32_t ph = 0, rph = 0;  // rph: a bit for each stage, as not every load into one is made ready
@@ -340,7 +335,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
                 return ex ? warp_wait(&bd.ready[st], rph >> st & 1u, abortp) && ((rph ^= 1u << st), true) : warp_wait(&bd.full[st], ph, abortp);
             };
             const int held_from = grad ? keep + sh.again : sh.chunks;  // chunks from here on stay in their stages
-            if (stats && ok) {
+            if (ok) {
                 if (keep) {
 #pragma unroll
                     for (int c = 0; c < kKeep; ++c)
@@ -381,7 +376,6 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
                     mbar_arrive(&bd.parts_in[slot_i]);
                 }
             }
-            if (!ok) break;
             if (!grad) continue;
             if (!warp_wait(&bd.grad[slot_i], sph, abortp)) break;
             const Grad<DT> gr(bd.grads[slot_i], a.f);
@@ -420,20 +414,17 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
                 }
                 give_back(s);
             };
-            if (stats) {
-                for (int c = held_from; c < whole; ++c) {
-                    write_from(c, held);
-                    if (++held == sh.stages) held = 0;
-                }
-                if (whole < sh.chunks && whole >= held_from) write_edge(held);
-                if (keep) {
-#pragma unroll
-                    for (int c = 0; c < kKeep; ++c) write(c, kept[c]);
-                }
+            for (int c = held_from; c < whole; ++c) {
+                write_from(c, held);
+                if (++held == sh.stages) held = 0;
             }
-            // chunks that are loaded for this reading
-            const int from = stats ? keep : 0, to = stats ? keep + sh.again : sh.chunks;
-            for (int c = from; c < to && ok; ++c) {
+            if (whole < sh.chunks && whole >= held_from) write_edge(held);
+            if (keep) {
+#pragma unroll
+                for (int c = 0; c < kKeep; ++c) write(c, kept[c]);
+            }
+            // chunks that are loaded again
+            for (int c = keep; c < keep + sh.again && ok; ++c) {
                 if (!(ok = warp_wait(&bd.full[st], ph, abortp))) break;
                 if (c < whole) write_from(c, st);
                 else write_edge(st);
@@ -451,16 +442,11 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
                     if (v >= 0 && v / E::kPer % kLanes / 32 == warp) out[v] = E::put(slot.x[j]);
                 }
             }
-            if (!stats) {  // the slot is free
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bd.parts_in[slot_i]);
-            }
         }
     }
     __syncthreads();
     if (tid == 0 && bd.abort_flag) {
         atomicMax(&a.w.head->status, (int)RAPID_ERR_TIMEOUT);
-        if (a.stats) atomicMax(&a.stats->status, (int)RAPID_ERR_TIMEOUT);
     }
 }
 
@@ -479,7 +465,6 @@ struct GroupShape {
     int part_vecs;       // vectors of a part, a multiple of the group's threads
     int parts;           // of a row
     int list;
-    unsigned long long stride;
 };
 
 struct GroupBoard {
@@ -513,7 +498,7 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
     constexpr int U = 4;  // vectors of a thread at a time
     extern __shared__ __align__(128) uint8_t dyn[];
     __shared__ int abort_flag;
-    __shared__ long long count;
+    __shared__ double weight;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = warp / G, gw = warp % G, gt = threadIdx.x % kLanes;
     uint8_t* place = dyn + (size_t)group * sh.group_bytes;
     GroupBoard& bd = *reinterpret_cast<GroupBoard*>(place + sh.row_bytes);
@@ -523,22 +508,22 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
         mbar_init_fence();
     }
     if (threadIdx.x == 0) abort_flag = 0;
-    if (warp == 0 && op_counts(op)) {
-        const long long n = rows_that_count(op_counts(op), op_blocks(op));
-        if (lane == 0) count = n;
+    if (warp == 0) {
+        const double w = shared_weight(op, rows_that_count(op_counts(op), op_blocks(op)));
+        if (lane == 0) weight = w;
     }
     __syncthreads();
     volatile int* abortp = &abort_flag;
-    const long long rows = op_counts(op) ? count : 0;
-    const bool stats = !a.known, grad = a.grad != nullptr, ex = exclude(op) && stats;
+    const double shared = weight;
+    const bool grad = a.grad != nullptr, ex = exclude(op);
     const int nvec = a.vocab / E::kPer, rest = a.vocab - nvec * E::kPer, all = nvec + (rest ? 1 : 0);
     const int n_list = list_size(op), id = group + 1;
     const uint64_t once = policy_first();
     const float off = shift_fraction(gw), unit_off = shift_fraction(lane);
-    const double unit = part_unit(unit_off);
+    const double unit = part_unit(unit_off), unit0 = part_unit(off);
     const uint4* row_place = reinterpret_cast<const uint4*>(place);
 
-    auto row_of = [&](unsigned int t) -> int64_t { return (int64_t)(((unsigned long long)t * sh.stride) % (unsigned long long)a.n_rows); };
+    const unsigned int n_rows = (unsigned int)a.n_rows;
     uint32_t issued = 0, phase_of = 0;  // a bit for each part: anything loaded, and the phase of its last load
     auto load_part = [&](int64_t r, int p, uint32_t phase) {  // by the group's first thread
         issued |= 1u << p;
@@ -548,7 +533,7 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
         bulk_load_once(place + (size_t)v * 16, static_cast<const uint8_t*>(a.logits) + (size_t)r * a.ld * sizeof(T) + (size_t)v * 16, (uint32_t)bytes,
                        &bd.full[p], once);
     };
-    auto state_of = [&](unsigned int t) -> int { return t < a.n_rows ? (int)a.w.state[row_of(t)] : ROW_MASKED; };
+    auto state_of = [&](unsigned int t) -> int { return t < n_rows ? (int)a.w.state[t] : ROW_MASKED; };
 
     // draws: the first ones are dealt out, one to every group of the grid; gt == 0 is ahead by two
     const unsigned int everyone = gridDim.x * sh.groups;
@@ -559,7 +544,7 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
     {
         const int st = state_of(t0);
         live = st == ROW_OK;
-        row = t0 < a.n_rows ? row_of(t0) : a.n_rows;
+        row = t0 < n_rows ? (int64_t)t0 : a.n_rows;
         if (gt == 0) {
             t1 = everyone + atomicAdd(&a.w.head->ticket, 1u);
             if (live)
@@ -575,8 +560,8 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
         }
         auto announce = [&]() {  // the next row, to the group
             if (gt == 0) {
-                const int64_t r = t1 < a.n_rows ? row_of(t1) : a.n_rows;
-                bd.next[turn & 1] = t1 < a.n_rows && state1 != ROW_OK ? ~r : r;
+                const int64_t r = t1 < n_rows ? (int64_t)t1 : a.n_rows;
+                bd.next[turn & 1] = t1 < n_rows && state1 != ROW_OK ? ~r : r;
                 t1 = t2;
             }
         };
@@ -597,7 +582,7 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
         }
         // ---- the row's chosen columns, by the group's first warp ----
         auto landed = [&](int p) { return ok && (ok = warp_wait(&bd.full[p], ph, abortp)); };
-        decltype(look(op, a, row, rows, slot.col, slot.z, slot.x)) mine{};
+        decltype(look(op, row, shared, slot.col, slot.z, slot.x)) mine{};
         if (gw == 0) {
             for (int j = lane; j < n_list; j += 32) {
                 const int v = column(op, row, j);
@@ -656,7 +641,7 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
             }
         };
         RowStat st{0.0, 0.f};
-        if (stats) {
+        {
             // ---- first reading ----
             if (!grad) announce();
             Part p;
@@ -687,15 +672,13 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
             if (left) break;
             const WarpPart w = warp_part(p, a.f);
             if constexpr (G == 1) {
-                st = join_parts(lane == 0 ? w : WarpPart{0.0, -INFINITY, -INFINITY}, unit_off, unit, a.f);
+                st = one_part(w, off, unit0, a.f);
             } else {
                 if (lane == 0) bd.parts[turn & 1][gw] = w;
                 if (group_sync<G>(id, !ok)) break;
                 if (gw == 0) st = join_parts(lane < G ? bd.parts[turn & 1][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, unit_off, unit, a.f);
             }
             if (G == 1 && !ok) break;
-        } else if (gw == 0) {  // the first parts may come while the columns are looked up
-            for (int p = 0; p < sh.parts; ++p) landed(p);
         }
         RowGrad g{0.0, 0.0};
         if (gw == 0 && ok) {
@@ -706,8 +689,7 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
                     if (v >= 0) slot.z[j] = E::get(reinterpret_cast<const T*>(place)[v]);
                 }
             __syncwarp();
-            mine = look(op, a, row, rows, slot.col, slot.z, slot.x);
-            if (!stats) st = known_stat(mine);
+            mine = look(op, row, shared, slot.col, slot.z, slot.x);
             g = finish(op, a, mine, st, slot.col, slot.z, slot.x);
             if (lane == 0) bd.grad = grad_const<DT>(g, st.max, a.f);
             if (grad) announce();
@@ -717,7 +699,6 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
             if (group_sync<G>(id, !ok)) break;
             const Grad<DT> gr(bd.grad, a.f);
             for (int q = 0; q < sh.parts && !left; ++q) {
-                if (!stats) landed(q);
                 if (ok) {
                     const int end = min((q + 1) * sh.part_vecs, all);
                     int v = q * sh.part_vecs + gt;
@@ -771,7 +752,6 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
     __syncthreads();
     if (threadIdx.x == 0 && abort_flag) {
         atomicMax(&a.w.head->status, (int)RAPID_ERR_TIMEOUT);
-        if (a.stats) atomicMax(&a.stats->status, (int)RAPID_ERR_TIMEOUT);
     }
 }
 
@@ -788,8 +768,7 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
         const size_t room = std::min((size_t)227 * 1024, (size_t)228 * 1024 / blocks - 1024) - extra;
         sh.stages = std::min((int)(room / chunk), most);
         sh.chunks = (int)((row_bytes + chunk - 1) / chunk);
-        const bool both = !a.known && a.grad;
-        sh.again = both && sh.chunks > keep + sh.stages ? sh.chunks - keep - sh.stages : 0;
+        sh.again = a.grad && sh.chunks > keep + sh.stages ? sh.chunks - keep - sh.stages : 0;
         const size_t smem = (size_t)sh.stages * chunk + extra;
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
@@ -816,7 +795,6 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         const int64_t grid = std::min((int64_t)sm_count, a.n_rows);
-        sh.stride = scatter_stride(a.n_rows);
         kern<<<(unsigned)grid, sh.groups * lanes, smem, stream>>>(a, op, sh);
         return cudaGetLastError();
     };
@@ -827,7 +805,7 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
         if (row_bytes <= 73728) return go_groups(group_kernel<DT, Op, 4>, 4);
         if (row_bytes <= 110 * 1024) return go_groups(group_kernel<DT, Op, 8>, 8);
         constexpr size_t b16 = sizeof(Board<16>);
-        if (!a.known && a.grad && row_bytes > 5 * 32768) return go(ring_kernel<DT, Op, 16, 4, 3, 1>, 16, 4, 3, 1, b16, Board<16>::kStages);
+        if (a.grad && row_bytes > 5 * 32768) return go(ring_kernel<DT, Op, 16, 4, 3, 1>, 16, 4, 3, 1, b16, Board<16>::kStages);
         return go(ring_kernel<DT, Op, 16, 4, 0, 1>, 16, 4, 0, 1, b16, Board<16>::kStages);
     };
     return a.dtype == RAPID_BF16 ? by_type(std::integral_constant<int, RAPID_BF16>{}) : by_type(std::integral_constant<int, RAPID_F32>{});
@@ -836,9 +814,8 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
 }  // namespace
 
 cudaError_t launch_rows(const RowsArgs& a, const ClipOp& op, int sm_count, cudaStream_t stream) { return launch(a, op, 1, false, sm_count, stream); }
-cudaError_t launch_rows(const RowsArgs& a, const PrefOp& op, int sm_count, cudaStream_t stream) { return launch(a, op, 1, false, sm_count, stream); }
 cudaError_t launch_rows(const RowsArgs& a, const DistillOp& op, int sm_count, cudaStream_t stream) {
-    return launch(a, op, op.k, op.tail != 0 && !a.known, sm_count, stream);
+    return launch(a, op, op.k, op.tail != 0, sm_count, stream);
 }
 
 }  // namespace losses

@@ -48,6 +48,7 @@ struct Scratch {
     float* row_max;       // [T]
     uint8_t* state;       // [T] ROW_*
     int32_t* seq_rows;    // [N] rows that count
+    int32_t* seq_bad;     // [N] rows that are not valid
     double* seq_sum;      // [N] s_n
     double* seq_coef;     // [N] g_n
     double* pair_slope;   // [P]
@@ -75,6 +76,7 @@ inline size_t carve(int64_t T, int64_t N, int64_t P, int need, void* base, Scrat
     s.state = reinterpret_cast<uint8_t*>(take((size_t)T));
     if (need & NEED_SEQ) s.seq_rows = reinterpret_cast<int32_t*>(take((size_t)N * 4));
     if (need & NEED_PAIRS) {
+        s.seq_bad = reinterpret_cast<int32_t*>(take((size_t)N * 4));
         s.seq_sum = reinterpret_cast<double*>(take((size_t)N * 8));
         s.seq_coef = reinterpret_cast<double*>(take((size_t)N * 8));
         s.pair_slope = reinterpret_cast<double*>(take((size_t)P * 8));
@@ -323,6 +325,19 @@ __device__ __forceinline__ RowStat join_parts(const WarpPart& p, float off, doub
     return r;
 }
 
+// The same where one warp has the whole row.
+__device__ __forceinline__ RowStat one_part(const WarpPart& p, float off, double unit, const Factor& f) {
+    RowStat r{-INFINITY, p.m};
+    if (p.sh > -INFINITY) {
+        const float n = rintf(p.sh - off);
+        const double frac = (double)p.sh - (double)n;
+        if (frac != (double)off) unit = exp2(frac) / (1.0 + (double)kEx2Mean);
+        const double s = fma(p.s, unit, exp2_short((double)p.m * f.kd - (double)n));
+        if (s > 0.0) r.lse2 = (double)n + log2_short(s);
+    }
+    return r;
+}
+
 __device__ __forceinline__ float shift_fraction(int warp) { return (float)(((unsigned)warp * 40503u) & 0xffffu) * (1.f / 65536.f); }
 
 // ---- a row's gradient --------------------------------------------------------------------------------------------
@@ -370,6 +385,9 @@ struct Grad<RAPID_BF16> {
         }
         return make_uint4(out[0], out[1], out[2], out[3]);
     }
+    __device__ __forceinline__ uint16_t one(uint16_t z) const {
+        return (uint16_t)(Elem<RAPID_BF16>::put(ex2_approx(fmaf(Elem<RAPID_BF16>::get(z), k, c))) ^ (uint16_t)sign);
+    }
 };
 template <>
 struct Grad<RAPID_F32> {
@@ -398,10 +416,8 @@ struct RowsArgs {
     void* grad;  // may be logits, may be NULL
     int64_t ld, ld_grad, n_rows;
     int vocab, dtype;
-    int known;   // the statistics are in the scratch already: gradient only
     Factor f;
     Scratch w;
-    rapid_loss_stats_t* stats;  // written before the rows: a wait that gives up is reported here too (may be NULL)
 };
 
 struct ClipOp {
@@ -412,11 +428,6 @@ struct ClipOp {
     int count_blocks, n_seq, seq_len;
     uint32_t flags;
     double low, high, beta, scale, norm_z;
-};
-struct PrefOp {  // first reading: the token's log-probability; second: the gradient, from the generation's coefficient
-    const int32_t* targets;
-    const double* seq_coef;
-    int seq_len;
 };
 struct DistillOp {
     const int32_t* index;
@@ -430,14 +441,22 @@ struct DistillOp {
 };
 
 cudaError_t launch_rows(const RowsArgs& a, const ClipOp& op, int sm_count, cudaStream_t stream);
-cudaError_t launch_rows(const RowsArgs& a, const PrefOp& op, int sm_count, cudaStream_t stream);
 cudaError_t launch_rows(const RowsArgs& a, const DistillOp& op, int sm_count, cudaStream_t stream);
 
+// The statistics of every row, without a gradient: log-probability of the token, log-sum-exp, largest logit; the states too, and the
+// header.  The logits are read once.
+cudaError_t launch_token_stats(const RowsArgs& a, const int32_t* targets, const uint8_t* mask, cudaStream_t stream);
+// The gradient of rows whose statistics are known: coefficient coef[row / seq_len] times softmax less one at the token.
+cudaError_t launch_token_grads(const RowsArgs& a, const int32_t* targets, const double* coef, int seq_len, cudaStream_t stream);
+
 // State of every row from mask and token, their numbers, and (where asked for) those of every generation; clears the header.
+cudaError_t launch_count_by_seq(int n_seq, int seq_len, const Scratch& w, cudaStream_t stream);
 cudaError_t launch_prepare_tokens(int n_seq, int seq_len, int vocab, const int32_t* targets, const uint8_t* mask, const Scratch& w,
                                   int by_seq, int* blocks, cudaStream_t stream);
 
 #ifdef __CUDACC__
+
+__device__ __forceinline__ uint32_t sequence(int64_t r, int seq_len) { return (uint32_t)r / (uint32_t)seq_len; }  // rows fit 31 bits
 
 // The clipped loss of one row and its slope by the log-probability, sign turned: loss' = -slope.
 struct ClipIn {
@@ -448,7 +467,7 @@ struct ClipTerms {
     bool cut;
 };
 __device__ __forceinline__ ClipIn clip_in(const ClipOp& op, int64_t r) {
-    return ClipIn{(double)op.adv[(op.flags & RAPID_CLIP_ADV_TOKEN) ? r : r / op.seq_len], (double)op.old_logp[r],
+    return ClipIn{(double)op.adv[(op.flags & RAPID_CLIP_ADV_TOKEN) ? r : sequence(r, op.seq_len)], (double)op.old_logp[r],
                   op.ref_logp ? (double)op.ref_logp[r] : 0.0};
 }
 __device__ __forceinline__ ClipTerms clip_terms(const ClipOp& op, const ClipIn& in, double lp) {
@@ -470,13 +489,16 @@ __device__ __forceinline__ ClipTerms clip_terms(const ClipOp& op, const ClipIn& 
     }
     return t;
 }
-// Weight of row r: `rows` is the number of rows that count.
-__device__ __forceinline__ double clip_weight(const ClipOp& op, int64_t r, long long rows) {
-    if (op.flags & RAPID_LOSS_NORM_SEQ) {
-        const double n = (op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)op.n_seq;
-        return op.scale / (n * (double)op.seq_rows[r / op.seq_len]);
-    }
-    return op.scale / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows);
+// Weight of a row: what all rows share, once for a kernel (`rows`: how many count), and the rest.
+__device__ __forceinline__ double shared_weight(const ClipOp& op, long long rows) {
+    if (op.flags & RAPID_LOSS_NORM_GIVEN) return op.scale / op.norm_z;
+    return op.scale / ((op.flags & RAPID_LOSS_NORM_SEQ) ? (double)op.n_seq : (double)rows);
+}
+__device__ __forceinline__ double clip_weight(const ClipOp& op, int64_t r, double shared) {
+    return (op.flags & RAPID_LOSS_NORM_SEQ) ? shared / (double)op.seq_rows[sequence(r, op.seq_len)] : shared;
+}
+__device__ __forceinline__ double shared_weight(const DistillOp& op, long long rows) {
+    return op.scale * op.inv_tau / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows);
 }
 
 // What an operator does with a row, by one warp.  look() does, ahead of time, what needs no sums over the row; finish() gives the
@@ -484,39 +506,24 @@ __device__ __forceinline__ double clip_weight(const ClipOp& op, int64_t r, long 
 // reading waits for; values() gives the chosen columns' gradient and writes what is kept of the row to the scratch.  col[j] and
 // z[j] are the chosen columns and their logits; x[j], for distillation the teacher's logits, become the columns' gradient.
 __device__ __forceinline__ int list_size(const ClipOp&) { return 1; }
-__device__ __forceinline__ int list_size(const PrefOp&) { return 1; }
 __device__ __forceinline__ int list_size(const DistillOp& op) { return op.k; }
 __device__ __forceinline__ const int2* op_counts(const ClipOp& op) { return op.counts; }
-__device__ __forceinline__ const int2* op_counts(const PrefOp&) { return nullptr; }
 __device__ __forceinline__ const int2* op_counts(const DistillOp& op) { return op.counts; }
 __device__ __forceinline__ int op_blocks(const ClipOp& op) { return op.count_blocks; }
-__device__ __forceinline__ int op_blocks(const PrefOp&) { return 0; }
 __device__ __forceinline__ int op_blocks(const DistillOp& op) { return op.count_blocks; }
 __device__ __forceinline__ bool exclude(const ClipOp&) { return false; }
-__device__ __forceinline__ bool exclude(const PrefOp&) { return false; }
 __device__ __forceinline__ bool exclude(const DistillOp& op) { return op.tail != 0; }
 __device__ __forceinline__ int column(const ClipOp& op, int64_t r, int) { return op.targets[r]; }
-__device__ __forceinline__ int column(const PrefOp& op, int64_t r, int) { return op.targets[r]; }
 __device__ __forceinline__ int column(const DistillOp& op, int64_t r, int j) { return op.index[r * op.ld + j]; }
 __device__ __forceinline__ float entry(const ClipOp&, int64_t, int) { return 0.f; }
-__device__ __forceinline__ float entry(const PrefOp&, int64_t, int) { return 0.f; }
 __device__ __forceinline__ float entry(const DistillOp& op, int64_t r, int j) { return op.logit[r * op.ld + j]; }
 
 struct ClipRow {
     ClipIn in;
     double w, lp;
 };
-__device__ __forceinline__ ClipRow look(const ClipOp& op, const RowsArgs&, int64_t r, long long rows, const int*, const float*, const float*) {
-    return ClipRow{clip_in(op, r), clip_weight(op, r, rows), 0.0};
-}
-struct PrefRow {
-    double a, lp;
-    RowStat st;
-};
-__device__ __forceinline__ PrefRow look(const PrefOp& op, const RowsArgs& a, int64_t r, long long, const int*, const float*, const float*) {
-    PrefRow p{0.0, 0.0, {0.0, 0.f}};
-    if (a.known) p = PrefRow{op.seq_coef[r / op.seq_len], 0.0, {a.w.lse2[r], a.w.row_max[r]}};
-    return p;
+__device__ __forceinline__ ClipRow look(const ClipOp& op, int64_t r, double shared, const int*, const float*, const float*) {
+    return ClipRow{clip_in(op, r), clip_weight(op, r, shared), 0.0};
 }
 struct DistillRow {
     double teacher, w;
@@ -524,58 +531,35 @@ struct DistillRow {
     double list_sum;  // the list's sum of 2^(x - top's x)
     float top;        // the list's largest logit
 };
-__device__ __forceinline__ DistillRow look(const DistillOp& op, const RowsArgs&, int64_t r, long long rows, const int* col, const float* z,
-                                           const float* x) {
+__device__ __forceinline__ DistillRow look(const DistillOp& op, int64_t r, double shared, const int* col, const float* z, const float* x) {
     const int lane = threadIdx.x & 31;
-    DistillRow row{op.teacher_lse2[r], op.scale * op.inv_tau / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows), 0.0, 0.0, 0.0,
-                   -INFINITY};
+    DistillRow row{op.teacher_lse2[r], shared, 0.0, 0.0, 0.0, -INFINITY};
     if (!op.tail) return row;
     double mass = 0.0;
     for (int j = lane; j < op.k; j += 32) {
         if (col[j] < 0) continue;
         row.top = fmaxf(row.top, z[j]);
-        mass += exp2((double)x[j] * op.kd - row.teacher);
+        mass += exp2_short((double)x[j] * op.kd - row.teacher);
     }
     row.top = warp_top(row.top);
     row.p0 = 1.0 - warp_sum(mass);
-    if (row.p0 > 0.0) row.lp0 = log2(row.p0);
+    if (row.p0 > 0.0) row.lp0 = log2_short(row.p0);
     if (row.top > -INFINITY)
         for (int j = lane; j < op.k; j += 32)
-            if (col[j] >= 0) row.list_sum += exp2(((double)z[j] - (double)row.top) * op.kd);
+            if (col[j] >= 0) row.list_sum += exp2_short(((double)z[j] - (double)row.top) * op.kd);
     row.list_sum = warp_sum(row.list_sum);
     return row;
 }
-__device__ __forceinline__ RowStat known_stat(const ClipRow&) { return RowStat{0.0, 0.f}; }
-__device__ __forceinline__ RowStat known_stat(const PrefRow& p) { return p.st; }
-__device__ __forceinline__ RowStat known_stat(const DistillRow&) { return RowStat{0.0, 0.f}; }
-
 __device__ __forceinline__ RowGrad finish(const ClipOp& op, const RowsArgs& a, ClipRow& row, const RowStat& st, const int*, const float* z,
                                           const float*) {
     row.lp = ((double)z[0] * a.f.kd - st.lse2) * kLn2D;
-    return RowGrad{a.grad ? row.w * clip_terms(op, row.in, row.lp).slope : 0.0, st.lse2};
+    return RowGrad{row.w * clip_terms(op, row.in, row.lp).slope, st.lse2};
 }
 __device__ __forceinline__ void values(const ClipOp&, const RowsArgs& a, int64_t r, const ClipRow& row, const RowGrad& g, const RowStat&,
                                        const int*, const float*, float* x) {
     if ((threadIdx.x & 31) != 0) return;
-    x[0] = (float)(g.a * expm1(row.lp));
+    x[0] = (float)(g.a * (exp2_short(row.lp * kLog2eD) - 1.0));
     a.w.value[r] = row.lp;
-}
-
-__device__ __forceinline__ RowGrad finish(const PrefOp&, const RowsArgs& a, PrefRow& row, const RowStat& st, const int*, const float* z,
-                                          const float*) {
-    row.lp = ((double)z[0] * a.f.kd - st.lse2) * kLn2D;
-    return RowGrad{row.a, st.lse2};
-}
-__device__ __forceinline__ void values(const PrefOp&, const RowsArgs& a, int64_t r, const PrefRow& row, const RowGrad& g, const RowStat& st,
-                                       const int*, const float*, float* x) {
-    if ((threadIdx.x & 31) != 0) return;
-    if (a.known) {
-        x[0] = (float)(g.a * expm1(row.lp));
-    } else {
-        a.w.value[r] = row.lp;
-        a.w.lse2[r] = st.lse2;
-        a.w.row_max[r] = st.max;
-    }
 }
 
 __device__ __forceinline__ RowGrad finish(const DistillOp& op, const RowsArgs&, DistillRow& row, const RowStat& st, const int* col, const float* z,
@@ -598,9 +582,9 @@ __device__ __forceinline__ void values(const DistillOp& op, const RowsArgs& a, i
     for (int j = lane; j < op.k; j += 32) {
         if (col[j] < 0) continue;
         const double lt = (double)x[j] * op.kd - row.teacher, lq = (double)z[j] * op.kd - g.lse2;
-        const double p = exp2(lt);
+        const double p = exp2_short(lt);
         if (p > 0.0) loss += p * (lt - lq);
-        x[j] = (float)(row.w * (exp2(lq) - p));
+        x[j] = (float)(row.w * (exp2_short(lq) - p));
     }
     loss = warp_sum(loss);
     if (row.p0 > 0.0) loss += row.p0 * (row.lp0 - (st.lse2 - g.lse2));

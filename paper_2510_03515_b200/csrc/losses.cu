@@ -172,28 +172,31 @@ __device__ __forceinline__ void counts_of(const int2* counts, int blocks, long l
 
 __global__ void __launch_bounds__(kThreads)
 clip_sum_kernel(ClipOp op, int64_t n_rows, float* __restrict__ token_logp, float* __restrict__ loss, rapid_loss_stats_t* stats, Scratch w) {
-    long long rows;
-    int bad;
-    counts_of(op.counts, op.count_blocks, rows, bad);
-    double mine[4] = {0.0, 0.0, 0.0, 0.0}, total[4];
+    double mine[6] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0}, total[6];
+    const bool by_seq = (op.flags & RAPID_LOSS_NORM_SEQ) != 0;
     for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < n_rows; r += (int64_t)gridDim.x * kThreads) {
         double lp = 0.0;
-        if (w.state[r] == ROW_OK) {
+        const uint8_t st = w.state[r];
+        if (st == ROW_OK) {
             lp = w.value[r];
             const ClipIn in = clip_in(op, r);
             const ClipTerms t = clip_terms(op, in, lp);
-            mine[0] += clip_weight(op, r, rows) * t.loss;
+            mine[0] += by_seq ? t.loss / (double)op.seq_rows[sequence(r, op.seq_len)] : t.loss;
             mine[1] += lp - in.old;
             mine[2] += t.kl;
             mine[3] += t.cut ? 1.0 : 0.0;
+            mine[4] += 1.0;
         }
+        mine[5] += st == ROW_BAD_TOKEN ? 1.0 : 0.0;
         if (token_logp) token_logp[r] = (float)lp;
     }
     if (!last_block_sums(mine, w, total) || threadIdx.x != 0) return;
-    *loss = (float)total[0];
+    const long long rows = (long long)total[4];
+    const double l = rows > 0 ? shared_weight(op, rows) * total[0] : 0.0;
+    *loss = (float)l;
     if (stats) {
         const double n = rows > 0 ? (double)rows : 1.0;
-        *stats = rapid_loss_stats_t{rows, (int32_t)total[3], bad, 0, w.head->status, total[1] / n, total[2] / n, total[0]};
+        *stats = rapid_loss_stats_t{rows, (int32_t)total[3], (int32_t)total[5], 0, w.head->status, total[1] / n, total[2] / n, l};
     }
 }
 
@@ -217,53 +220,27 @@ distill_sum_kernel(DistillOp op, int64_t n_rows, float* __restrict__ token_loss,
     if (stats) *stats = rapid_loss_stats_t{rows, 0, bad, 0, w.head->status, 0.0, 0.0, l};
 }
 
-// One block for each generation: its sum of log-ratios.
-__global__ void __launch_bounds__(kThreads)
-pref_seq_kernel(int seq_len, uint32_t flags, const float* __restrict__ ref_logp, float* __restrict__ token_logp, Scratch w) {
-    __shared__ double sh[kWarps];
-    __shared__ int shi[kWarps];
-    const int64_t base = (int64_t)blockIdx.x * seq_len;
-    double s = 0.0;
-    int n = 0;
-    for (int t = threadIdx.x; t < seq_len; t += kThreads) {
-        const int64_t r = base + t;
-        double lp = 0.0;
-        if (w.state[r] == ROW_OK) {
-            lp = w.value[r];
-            s += ref_logp ? lp - (double)ref_logp[r] : lp;
-            n += 1;
-        }
-        if (token_logp) token_logp[r] = (float)lp;
-    }
-    s = block_sum(s, sh);
-    n = block_sum(n, shi);
-    if (threadIdx.x == 0) {
-        w.seq_rows[blockIdx.x] = n;
-        w.seq_sum[blockIdx.x] = (flags & RAPID_PREF_TOKEN_MEAN) && n > 0 ? s / (double)n : s;
-    }
-}
-
 struct PairArgs {
     const int32_t* pairs;
-    int n_pairs, n_seq;
+    int n_pairs, n_seq, seq_len;
     uint32_t flags;
     double beta, margin, smoothing, scale, norm_z;
+    float *margins, *loss;
+    rapid_loss_stats_t* stats;
 };
 __device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
 
-// One block: every pair's loss and slope, and their sums.
-constexpr int kPairThreads = 1024;
-__global__ void __launch_bounds__(kPairThreads)
-pref_pairs_kernel(PairArgs a, int count_blocks, float* __restrict__ margins, float* __restrict__ loss, rapid_loss_stats_t* stats, Scratch w) {
-    __shared__ double sh[kPairThreads / 32];
-    __shared__ int shi[kPairThreads / 32];
+// By one block: every pair's loss and slope, and their sums; returns what the slopes are multiplied by.
+__device__ double pairs_of(const PairArgs& a, const Scratch& w) {
+    __shared__ double sh[32];
+    __shared__ int shi[32];
     double sum = 0.0, sum_h = 0.0;
-    int valid = 0, won = 0;
-    for (int p = threadIdx.x; p < a.n_pairs; p += kPairThreads) {
+    int valid = 0, won = 0, rows = 0, bad = 0;
+    for (int p = threadIdx.x; p < a.n_pairs; p += blockDim.x) {
         const int i = a.pairs[2 * p], j = a.pairs[2 * p + 1];
         double h = NAN, slope = 0.0;
         if (i >= 0 && i < a.n_seq && j >= 0 && j < a.n_seq) {
-            h = a.beta * (w.seq_sum[i] - w.seq_sum[j]) - a.margin;
+            h = a.beta * (__ldcg(w.seq_sum + i) - __ldcg(w.seq_sum + j)) - a.margin;
             double f;
             if (a.flags & RAPID_PREF_HINGE) {
                 f = fmax(1.0 - h, 0.0);
@@ -281,31 +258,31 @@ pref_pairs_kernel(PairArgs a, int count_blocks, float* __restrict__ margins, flo
             won += h > 0.0;
         }
         w.pair_slope[p] = slope;
-        if (margins) margins[p] = (float)h;
+        if (a.margins) a.margins[p] = (float)h;
+    }
+    long long live = 0;
+    for (int n = threadIdx.x; n < a.n_seq; n += blockDim.x) {
+        live += __ldcg(w.seq_rows + n);
+        bad += __ldcg(w.seq_bad + n);
     }
     sum = block_sum(sum, sh);
     sum_h = block_sum(sum_h, sh);
+    live = (long long)block_sum((double)live, sh);
     valid = block_sum(valid, shi);
     won = block_sum(won, shi);
-    long long rows;
-    int bad;
-    counts_of(w.counts, count_blocks, rows, bad);
-    if (threadIdx.x != 0) return;
+    bad = block_sum(bad, shi);
     const double z = (a.flags & RAPID_LOSS_NORM_GIVEN) ? a.norm_z : (double)valid;
-    const double l = valid > 0 ? a.scale * sum / z : 0.0;
-    w.sums[0] = valid > 0 ? a.scale * a.beta / z : 0.0;  // what the slopes are multiplied by
-    w.head->ticket = 0;  // the rows are handed out once more
-    *loss = (float)l;
-    if (stats) {
-        const double n = valid > 0 ? (double)valid : 1.0;
-        *stats = rapid_loss_stats_t{rows, 0, bad, valid, w.head->status, sum_h / n, (double)won / n, l};
+    if (threadIdx.x == 0) {
+        const double l = valid > 0 ? a.scale * sum / z : 0.0, n = valid > 0 ? (double)valid : 1.0;
+        *a.loss = (float)l;
+        if (a.stats) *a.stats = rapid_loss_stats_t{live, 0, bad, valid, RAPID_OK, sum_h / n, (double)won / n, l};
     }
+    return valid > 0 ? a.scale * a.beta / z : 0.0;
 }
 
-// A warp for each generation: minus the loss's slope by the sum of its log-probabilities, over the pairs that it is in.
-__global__ void __launch_bounds__(kThreads) pref_coef_kernel(PairArgs a, Scratch w) {
-    const int n = blockIdx.x * kWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (n >= a.n_seq) return;
+// By one warp: minus the loss's slope by the sum of generation n's log-probabilities, over the pairs that it is in.
+__device__ __forceinline__ void coefficient(const PairArgs& a, const Scratch& w, int n, double by) {
+    const int lane = threadIdx.x & 31;
     double s = 0.0;
     for (int p = lane; p < a.n_pairs; p += 32) {
         const int i = a.pairs[2 * p], j = a.pairs[2 * p + 1];
@@ -313,11 +290,64 @@ __global__ void __launch_bounds__(kThreads) pref_coef_kernel(PairArgs a, Scratch
         if (i == n) s -= w.pair_slope[p];
         if (j == n) s += w.pair_slope[p];
     }
-    s = warp_sum(s) * w.sums[0];
+    s = warp_sum(s) * by;
     if (lane == 0) {
-        const int rows = w.seq_rows[n];
+        const int rows = __ldcg(w.seq_rows + n);
         w.seq_coef[n] = (a.flags & RAPID_PREF_TOKEN_MEAN) && rows > 0 ? s / (double)rows : s;
     }
+}
+
+// One block for each generation: its sum of log-ratios.  Where there is little to do (`all`) the last one goes on to the pairs and
+// the coefficients, which saves a call with few rows two launches.
+__global__ void __launch_bounds__(kThreads)
+pref_seq_kernel(PairArgs a, const float* __restrict__ ref_logp, float* __restrict__ token_logp, int all, Scratch w) {
+    __shared__ double sh[kWarps];
+    __shared__ int shi[kWarps];
+    __shared__ bool last;
+    const int64_t base = (int64_t)blockIdx.x * a.seq_len;
+    double s = 0.0;
+    int n = 0, bad = 0;
+    for (int t = threadIdx.x; t < a.seq_len; t += kThreads) {
+        const int64_t r = base + t;
+        const uint8_t st = w.state[r];
+        double lp = 0.0;
+        if (st == ROW_OK) {
+            lp = w.value[r];
+            s += ref_logp ? lp - (double)ref_logp[r] : lp;
+            n += 1;
+        }
+        bad += st == ROW_BAD_TOKEN;
+        if (token_logp) token_logp[r] = (float)lp;
+    }
+    s = block_sum(s, sh);
+    n = block_sum(n, shi);
+    bad = block_sum(bad, shi);
+    if (threadIdx.x == 0) {
+        w.seq_rows[blockIdx.x] = n;
+        w.seq_bad[blockIdx.x] = bad;
+        w.seq_sum[blockIdx.x] = (a.flags & RAPID_PREF_TOKEN_MEAN) && n > 0 ? s / (double)n : s;
+        if (all) {
+            __threadfence();
+            last = atomicAdd(&w.head->done, 1u) == gridDim.x - 1;
+        }
+    }
+    if (!all) return;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    const double by = pairs_of(a, w);
+    __syncthreads();
+    for (int i = threadIdx.x >> 5; i < a.n_seq; i += kWarps) coefficient(a, w, i, by);
+}
+
+constexpr int kPairThreads = 1024;
+__global__ void __launch_bounds__(kPairThreads) pref_pairs_kernel(PairArgs a, Scratch w) {
+    const double by = pairs_of(a, w);
+    if (threadIdx.x == 0) w.sums[0] = by;
+}
+__global__ void __launch_bounds__(kThreads) pref_coef_kernel(PairArgs a, Scratch w) {
+    const int n = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    if (n < a.n_seq) coefficient(a, w, n, w.sums[0]);
 }
 
 unsigned sum_blocks(int64_t T) {
@@ -327,13 +357,17 @@ unsigned sum_blocks(int64_t T) {
 
 }  // namespace
 
+cudaError_t launch_count_by_seq(int n_seq, int seq_len, const Scratch& w, cudaStream_t stream) {
+    count_by_seq_kernel<<<n_seq, seq_len > 2048 ? kThreads : 32, 0, stream>>>(seq_len, w);
+    return cudaGetLastError();
+}
+
 cudaError_t launch_prepare_tokens(int n_seq, int seq_len, int vocab, const int32_t* targets, const uint8_t* mask, const Scratch& w,
                                   int by_seq, int* blocks, cudaStream_t stream) {
     const int64_t T = (int64_t)n_seq * seq_len, b = (T + 1023) / 1024;
     *blocks = (int)(b < kPrepBlocks ? b : kPrepBlocks);
     prepare_tokens_kernel<<<*blocks, kThreads, 0, stream>>>(T, vocab, targets, mask, w);
-    if (by_seq) count_by_seq_kernel<<<n_seq, seq_len > 2048 ? kThreads : 32, 0, stream>>>(seq_len, w);
-    return cudaGetLastError();
+    return by_seq ? launch_count_by_seq(n_seq, seq_len, w, stream) : cudaGetLastError();
 }
 
 }  // namespace losses
@@ -416,13 +450,17 @@ rapid_status_t rapid_clip_loss(const rapid_clip_desc_t* desc, const void* logits
     int sms = 0;
     if ((s = check_device(&sms)) != RAPID_OK) return s;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool by_seq = (d.flags & RAPID_LOSS_NORM_SEQ) != 0;
+    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, make_factor(1.0), w};
     int blocks = 0;
-    if (launch_prepare_tokens(d.n_seq, d.seq_len, d.vocab, targets, mask, w, (d.flags & RAPID_LOSS_NORM_SEQ) != 0, &blocks, st) != cudaSuccess)
+    if (dlogits) {
+        if (launch_prepare_tokens(d.n_seq, d.seq_len, d.vocab, targets, mask, w, by_seq, &blocks, st) != cudaSuccess) return RAPID_ERR_CUDA;
+    } else if (launch_token_stats(a, targets, mask, st) != cudaSuccess || (by_seq && launch_count_by_seq(d.n_seq, d.seq_len, w, st) != cudaSuccess)) {
         return RAPID_ERR_CUDA;
+    }
     const ClipOp op{targets, old_logp, ref_logp, adv, w.seq_rows, w.counts, blocks, d.n_seq, d.seq_len, d.flags, d.eps_low, d.eps_high,
                     d.kl_beta, d.scale, d.norm_z};
-    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, 0, make_factor(1.0), w, nullptr};
-    if (launch_rows(a, op, sms, st) != cudaSuccess) return RAPID_ERR_CUDA;
+    if (dlogits && launch_rows(a, op, sms, st) != cudaSuccess) return RAPID_ERR_CUDA;
     clip_sum_kernel<<<sum_blocks(T), kThreads, 0, st>>>(op, T, token_logp, loss, stats, w);
     return cuda_status(cudaGetLastError());
 }
@@ -451,22 +489,17 @@ rapid_status_t rapid_preference_loss(const rapid_pref_desc_t* desc, const void* 
     int sms = 0;
     if ((s = check_device(&sms)) != RAPID_OK) return s;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    int blocks = 0;
-    if (launch_prepare_tokens(d.n_seq, d.seq_len, d.vocab, targets, mask, w, 0, &blocks, st) != cudaSuccess) return RAPID_ERR_CUDA;
-    const PrefOp op{targets, w.seq_coef, d.seq_len};
-    RowsArgs a{logits, nullptr, d.ld, d.ld_grad, T, d.vocab, d.dtype, 0, make_factor(1.0), w, nullptr};
-    if (launch_rows(a, op, sms, st) != cudaSuccess) return RAPID_ERR_CUDA;
-    const PairArgs pa{pairs, d.n_pairs, d.n_seq, d.flags, d.beta, d.margin, d.label_smoothing, d.scale, d.norm_z};
-    pref_seq_kernel<<<d.n_seq, kThreads, 0, st>>>(d.seq_len, d.flags, ref_logp, token_logp, w);
-    pref_pairs_kernel<<<1, kPairThreads, 0, st>>>(pa, blocks, margins, loss, stats, w);
+    RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, make_factor(1.0), w};
+    if (launch_token_stats(a, targets, mask, st) != cudaSuccess) return RAPID_ERR_CUDA;
+    const PairArgs pa{pairs, d.n_pairs, d.n_seq, d.seq_len, d.flags, d.beta, d.margin, d.label_smoothing, d.scale, d.norm_z, margins, loss, stats};
+    const int all = d.n_pairs <= 4096 && (int64_t)d.n_pairs * d.n_seq <= 1 << 16;  // some ten microseconds of one block at most
+    pref_seq_kernel<<<d.n_seq, kThreads, 0, st>>>(pa, ref_logp, token_logp, all, w);
+    if (!all) {
+        pref_pairs_kernel<<<1, kPairThreads, 0, st>>>(pa, w);
+        if (dlogits) pref_coef_kernel<<<(unsigned)(((int64_t)d.n_seq + kWarps - 1) / kWarps), kThreads, 0, st>>>(pa, w);
+    }
     if (cudaGetLastError() != cudaSuccess) return RAPID_ERR_CUDA;
-    if (!dlogits) return RAPID_OK;
-    pref_coef_kernel<<<(unsigned)(((int64_t)d.n_seq + kWarps - 1) / kWarps), kThreads, 0, st>>>(pa, w);
-    if (cudaGetLastError() != cudaSuccess) return RAPID_ERR_CUDA;
-    a.grad = dlogits;
-    a.known = 1;
-    a.stats = stats;
-    return cuda_status(launch_rows(a, op, sms, st));
+    return dlogits ? cuda_status(launch_token_grads(a, targets, w.seq_coef, d.seq_len, st)) : RAPID_OK;
 }
 
 rapid_status_t rapid_distill_loss_workspace_bytes(const rapid_distill_desc_t* desc, size_t* bytes) {
@@ -498,7 +531,7 @@ rapid_status_t rapid_distill_loss(const rapid_distill_desc_t* desc, const void* 
     if (cudaGetLastError() != cudaSuccess) return RAPID_ERR_CUDA;
     const DistillOp op{top_index, top_logit, w.teacher_lse2, w.counts, d.ld_top, d.k, top_lse != nullptr, blocks, d.flags, 1.0 / d.temperature,
                        d.scale, d.norm_z, f.kd};
-    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, d.n_rows, d.vocab, d.dtype, 0, f, w, nullptr};
+    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, d.n_rows, d.vocab, d.dtype, f, w};
     if (launch_rows(a, op, sms, st) != cudaSuccess) return RAPID_ERR_CUDA;
     distill_sum_kernel<<<sum_blocks(d.n_rows), kThreads, 0, st>>>(op, d.n_rows, token_loss, loss, stats, w);
     return cuda_status(cudaGetLastError());
