@@ -448,6 +448,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
     if (tid == 0 && bd.abort_flag) {
         atomicMax(&a.w.head->status, (int)RAPID_ERR_TIMEOUT);
     }
+    if (a.end.last_block) finish_rows(op, a.end, a.n_rows, a.w, reinterpret_cast<double*>(dyn));
 }
 
 // ---- shorter rows ----------------------------------------------------------------------------------------------
@@ -491,7 +492,7 @@ __device__ __forceinline__ bool group_sync(int id, bool flag) {
 }
 
 template <int DT, class Op, int G>
-__global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a, Op op, GroupShape sh) {
+__global__ void __launch_bounds__(768, 1) group_kernel(RowsArgs a, Op op, GroupShape sh) {
     using E = Elem<DT>;
     using T = typename E::T;
     constexpr int kLanes = G * 32;
@@ -753,6 +754,7 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
     if (threadIdx.x == 0 && abort_flag) {
         atomicMax(&a.w.head->status, (int)RAPID_ERR_TIMEOUT);
     }
+    if (a.end.last_block) finish_rows(op, a.end, a.n_rows, a.w, reinterpret_cast<double*>(dyn));
 }
 
 template <class Op>
@@ -785,12 +787,11 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
         GroupShape sh{};
         const int lanes = G * 32, all = (int)(row_bytes / 16);
         sh.list = (list + 3) / 4 * 4;
-        sh.part_vecs = ((all + kParts - 1) / kParts + lanes - 1) / lanes * lanes;
-        if (sh.part_vecs > 4 * lanes) sh.part_vecs = (sh.part_vecs + 4 * lanes - 1) / (4 * lanes) * (4 * lanes);
+        sh.part_vecs = ((all + kParts - 1) / kParts + 4 * lanes - 1) / (4 * lanes) * (4 * lanes);
         sh.parts = (all + sh.part_vecs - 1) / sh.part_vecs;
         sh.row_bytes = (int)row_bytes;
         sh.group_bytes = (int)((row_bytes + sizeof(GroupBoard) + sh.list * kSlotEntry + 127) / 128 * 128);
-        sh.groups = std::min((227 * 1024 - 64) / sh.group_bytes, (G == 1 ? 24 : 16) / G);
+        sh.groups = std::min((227 * 1024 - 64) / sh.group_bytes, 24 / G);
         const size_t smem = (size_t)sh.groups * sh.group_bytes;
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
@@ -801,7 +802,7 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
     auto by_type = [&](auto dt) -> cudaError_t {
         constexpr int DT = decltype(dt)::value;
         if (row_bytes <= 16384) return go_groups(group_kernel<DT, Op, 1>, 1);
-        if (row_bytes <= 32768) return go_groups(group_kernel<DT, Op, 2>, 2);
+        if (row_bytes <= 32768) return go_groups(group_kernel<DT, Op, 4>, 4);
         if (row_bytes <= 73728) return go_groups(group_kernel<DT, Op, 4>, 4);
         if (row_bytes <= 110 * 1024) return go_groups(group_kernel<DT, Op, 8>, 8);
         constexpr size_t b16 = sizeof(Board<16>);

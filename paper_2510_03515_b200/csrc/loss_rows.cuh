@@ -153,7 +153,22 @@ inline Factor make_factor(double tau) {
     return f;
 }
 
+// Division of a number below 2^31 by one that is known on the host: the high word of a product (Granlund and Montgomery).
+struct Divisor {
+    uint32_t by, times, shift;
+};
+inline Divisor make_divisor(int32_t d) {
+    Divisor v{(uint32_t)d, 0u, 0u};
+    while ((1ll << v.shift) < d) ++v.shift;
+    v.times = (uint32_t)(((1ull << (31 + v.shift)) + d - 1) / (uint64_t)d);  // below 2^32 for d >= 2, as 2^shift < 2 d
+    return v;
+}
+
 #ifdef __CUDACC__
+
+__device__ __forceinline__ uint32_t divide(int64_t n, const Divisor& d) {
+    return d.by == 1 ? (uint32_t)n : __umulhi((uint32_t)n, d.times) >> (d.shift - 1);
+}
 
 template <int DT>
 struct Elem;
@@ -262,16 +277,19 @@ struct Part {
 // 2^-1020 is 0.
 __device__ __forceinline__ double exp2_short(double y) {
     if (!(y > -1020.0 && y < 1020.0)) return y > 0.0 || y != y ? exp2(y) : 0.0;
-    const double n = rint(y), t = (y - n) * kLn2D, t2 = t * t, t4 = t2 * t2;
+    // the nearest whole number by adding 1.5 2^52, in whose low word it then stands: no conversion, which would be a slow one
+    const double up = y + 6755399441055744.0, n = up - 6755399441055744.0;
+    const double t = (y - n) * kLn2D, t2 = t * t, t4 = t2 * t2;
     const double a0 = 1.0 + t, a1 = fma(t, 1.0 / 6, 0.5), a2 = fma(t, 1.0 / 120, 1.0 / 24), a3 = fma(t, 1.0 / 5040, 1.0 / 720);
     const double a4 = fma(t, 1.0 / 362880, 1.0 / 40320), a5 = fma(t, 1.0 / 39916800, 1.0 / 3628800);
     const double b0 = fma(a1, t2, a0), b1 = fma(a3, t2, a2), b2 = fma(a5, t2, a4);
-    return fma(b2, t4 * t4, fma(b1, t4, b0)) * __hiloint2double(((int)n + 1023) << 20, 0);
+    return fma(b2, t4 * t4, fma(b1, t4, b0)) * __hiloint2double((__double2loint(up) + 1023) << 20, 0);
 }
 __device__ __forceinline__ double log2_short(double s) {  // s > 0, normal
     const int e = (__double2hiint(s) >> 20) - 1023;
     const double m = __hiloint2double(__double2hiint(s) - (e << 20), __double2loint(s));  // in [1, 2)
-    const double l = (double)__log2f((float)m);
+    const float near = __uint_as_float(0x3f800000u | ((uint32_t)__double2hiint(m) & 0xfffffu) << 3 | (uint32_t)__double2loint(m) >> 29);  // m cut to a float
+    const double l = (double)__log2f(near);
     const double r = fma(m, exp2_short(-l), -1.0);  // below 1e-6
     return (double)e + fma(r * fma(r, -0.5, 1.0), kLog2eD, l);
 }
@@ -411,6 +429,14 @@ __device__ __forceinline__ long long rows_that_count(const int2* counts, int blo
 
 // ---- what an operator brings to the rows ----------------------------------------------------------------------------
 
+// What is made of the rows at the end: the arguments of the summing kernels, or of the last block of the rows' own kernel.
+struct Totals {
+    float *token, *loss;  // token may be NULL
+    rapid_loss_stats_t* stats;
+    int last_block;       // few rows: the rows' kernel does it
+};
+constexpr int64_t kFewRows = 1024;
+
 struct RowsArgs {
     const void* logits;
     void* grad;  // may be logits, may be NULL
@@ -418,6 +444,7 @@ struct RowsArgs {
     int vocab, dtype;
     Factor f;
     Scratch w;
+    Totals end;
 };
 
 struct ClipOp {
@@ -425,7 +452,8 @@ struct ClipOp {
     const float *old_logp, *ref_logp, *adv;
     const int32_t* seq_rows;  // with RAPID_LOSS_NORM_SEQ
     const int2* counts;
-    int count_blocks, n_seq, seq_len;
+    int count_blocks, n_seq;
+    Divisor seq_len;
     uint32_t flags;
     double low, high, beta, scale, norm_z;
 };
@@ -447,7 +475,7 @@ cudaError_t launch_rows(const RowsArgs& a, const DistillOp& op, int sm_count, cu
 // header.  The logits are read once.
 cudaError_t launch_token_stats(const RowsArgs& a, const int32_t* targets, const uint8_t* mask, cudaStream_t stream);
 // The gradient of rows whose statistics are known: coefficient coef[row / seq_len] times softmax less one at the token.
-cudaError_t launch_token_grads(const RowsArgs& a, const int32_t* targets, const double* coef, int seq_len, cudaStream_t stream);
+cudaError_t launch_token_grads(const RowsArgs& a, const int32_t* targets, const double* coef, const Divisor& seq_len, cudaStream_t stream);
 
 // State of every row from mask and token, their numbers, and (where asked for) those of every generation; clears the header.
 cudaError_t launch_count_by_seq(int n_seq, int seq_len, const Scratch& w, cudaStream_t stream);
@@ -456,7 +484,6 @@ cudaError_t launch_prepare_tokens(int n_seq, int seq_len, int vocab, const int32
 
 #ifdef __CUDACC__
 
-__device__ __forceinline__ uint32_t sequence(int64_t r, int seq_len) { return (uint32_t)r / (uint32_t)seq_len; }  // rows fit 31 bits
 
 // The clipped loss of one row and its slope by the log-probability, sign turned: loss' = -slope.
 struct ClipIn {
@@ -467,7 +494,7 @@ struct ClipTerms {
     bool cut;
 };
 __device__ __forceinline__ ClipIn clip_in(const ClipOp& op, int64_t r) {
-    return ClipIn{(double)op.adv[(op.flags & RAPID_CLIP_ADV_TOKEN) ? r : sequence(r, op.seq_len)], (double)op.old_logp[r],
+    return ClipIn{(double)op.adv[(op.flags & RAPID_CLIP_ADV_TOKEN) ? r : divide(r, op.seq_len)], (double)op.old_logp[r],
                   op.ref_logp ? (double)op.ref_logp[r] : 0.0};
 }
 __device__ __forceinline__ ClipTerms clip_terms(const ClipOp& op, const ClipIn& in, double lp) {
@@ -495,7 +522,7 @@ __device__ __forceinline__ double shared_weight(const ClipOp& op, long long rows
     return op.scale / ((op.flags & RAPID_LOSS_NORM_SEQ) ? (double)op.n_seq : (double)rows);
 }
 __device__ __forceinline__ double clip_weight(const ClipOp& op, int64_t r, double shared) {
-    return (op.flags & RAPID_LOSS_NORM_SEQ) ? shared / (double)op.seq_rows[sequence(r, op.seq_len)] : shared;
+    return (op.flags & RAPID_LOSS_NORM_SEQ) ? shared / (double)op.seq_rows[divide(r, op.seq_len)] : shared;
 }
 __device__ __forceinline__ double shared_weight(const DistillOp& op, long long rows) {
     return op.scale * op.inv_tau / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows);
@@ -589,6 +616,96 @@ __device__ __forceinline__ void values(const DistillOp& op, const RowsArgs& a, i
     loss = warp_sum(loss);
     if (row.p0 > 0.0) loss += row.p0 * (row.lp0 - (st.lse2 - g.lse2));
     if (lane == 0) a.w.value[r] = loss * kLn2D;
+}
+
+// ---- sums over the rows -------------------------------------------------------------------------------------------
+
+// Sums over the block of N numbers at once, the same in all threads; the order depends on the block's size alone.  `sh` is room for
+// 32 N numbers in shared memory.
+template <int N>
+__device__ __forceinline__ void block_sums(double (&v)[N], double* sh) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
+    __syncthreads();
+    if (lane == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sh[warp * N + i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < warps ? sh[lane * N + i] : 0.0);
+}
+
+// The last block of a grid to come here, with what the others wrote visible to it.  `sh` is one bool in shared memory.
+__device__ __forceinline__ bool is_last_block(Header* head, bool* sh) {
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        *sh = atomicAdd(&head->done, 1u) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (*sh) __threadfence();
+    return *sh;
+}
+
+// loss, mean log-ratio, KL, rows cut, rows that count, rows that are not valid: of one row, added up
+constexpr int kClipSums = 6, kDistillSums = 3;
+__device__ __forceinline__ void add_row(const ClipOp& op, const Totals& t, int64_t r, const Scratch& w, double (&v)[kClipSums]) {
+    double lp = 0.0;
+    const uint8_t st = w.state[r];
+    if (st == ROW_OK) {
+        lp = __ldcg(w.value + r);
+        const ClipIn in = clip_in(op, r);
+        const ClipTerms c = clip_terms(op, in, lp);
+        v[0] += (op.flags & RAPID_LOSS_NORM_SEQ) ? c.loss / (double)op.seq_rows[divide(r, op.seq_len)] : c.loss;
+        v[1] += lp - in.old;
+        v[2] += c.kl;
+        v[3] += c.cut ? 1.0 : 0.0;
+        v[4] += 1.0;
+    }
+    v[5] += st == ROW_BAD_TOKEN ? 1.0 : 0.0;
+    if (t.token) t.token[r] = (float)lp;
+}
+__device__ __forceinline__ void add_row(const DistillOp&, const Totals& t, int64_t r, const Scratch& w, double (&v)[kDistillSums]) {
+    const uint8_t st = w.state[r];
+    const double l = st == ROW_OK ? __ldcg(w.value + r) : 0.0;
+    v[0] += l;
+    v[1] += st == ROW_OK ? 1.0 : 0.0;
+    v[2] += st == ROW_BAD_TOKEN ? 1.0 : 0.0;
+    if (t.token) t.token[r] = (float)l;
+}
+__device__ __forceinline__ void write_totals(const ClipOp& op, const Totals& t, const Scratch& w, const double (&v)[kClipSums]) {
+    const long long rows = (long long)v[4];
+    const double l = rows > 0 ? shared_weight(op, rows) * v[0] : 0.0, n = rows > 0 ? v[4] : 1.0;
+    *t.loss = (float)l;
+    if (t.stats) *t.stats = rapid_loss_stats_t{rows, (int32_t)v[3], (int32_t)v[5], 0, *(volatile int32_t*)&w.head->status, v[1] / n, v[2] / n, l};
+}
+__device__ __forceinline__ void write_totals(const DistillOp& op, const Totals& t, const Scratch& w, const double (&v)[kDistillSums]) {
+    const long long rows = (long long)v[1];
+    const double l = rows > 0 ? op.scale * v[0] / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : v[1]) : 0.0;
+    *t.loss = (float)l;
+    if (t.stats) *t.stats = rapid_loss_stats_t{rows, 0, (int32_t)v[2], 0, *(volatile int32_t*)&w.head->status, 0.0, 0.0, l};
+}
+template <class Op>
+struct SumsOf;
+template <>
+struct SumsOf<ClipOp> {
+    static constexpr int kN = kClipSums;
+};
+template <>
+struct SumsOf<DistillOp> {
+    static constexpr int kN = kDistillSums;
+};
+
+// By the last block of the rows' kernel, where there are few rows.
+// `sh`: 2 KB of shared memory.
+template <class Op>
+__device__ __noinline__ void finish_rows(const Op& op, const Totals& t, int64_t n_rows, const Scratch& w, double* sh) {
+    if (!is_last_block(w.head, reinterpret_cast<bool*>(sh + 32 * SumsOf<Op>::kN))) return;
+    double v[SumsOf<Op>::kN] = {};
+    for (int64_t r = threadIdx.x; r < n_rows; r += blockDim.x) add_row(op, t, r, w, v);
+    block_sums(v, sh);
+    if (threadIdx.x == 0) write_totals(op, t, w, v);
 }
 
 #endif  // __CUDACC__

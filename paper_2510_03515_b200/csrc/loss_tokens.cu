@@ -79,7 +79,7 @@ constexpr int kPiece = 16 * 32;
 
 template <int DT>
 __global__ void __launch_bounds__(kGradThreads)
-token_grads_kernel(RowsArgs a, const int32_t* __restrict__ targets, const double* __restrict__ coef, int seq_len, uint32_t pieces, uint32_t total) {
+token_grads_kernel(RowsArgs a, const int32_t* __restrict__ targets, const double* __restrict__ coef, Divisor seq_len, uint32_t pieces, uint32_t total) {
     using E = Elem<DT>;
     using T = typename E::T;
     constexpr int U = 8;
@@ -92,7 +92,7 @@ token_grads_kernel(RowsArgs a, const int32_t* __restrict__ targets, const double
     const bool last = first + kPiece >= nvec;
     T* out = static_cast<T*>(a.grad) + (int64_t)r * a.ld_grad;
     uint4* ov = reinterpret_cast<uint4*>(out);
-    const double g = a.w.state[r] == ROW_OK ? coef[sequence(r, seq_len)] : 0.0;
+    const double g = a.w.state[r] == ROW_OK ? coef[divide(r, seq_len)] : 0.0;
     const int e = nvec * E::kPer + lane;  // columns behind the last whole vector
     if (g == 0.0) {
 #pragma unroll 4
@@ -143,7 +143,7 @@ cudaError_t launch_token_stats(const RowsArgs& a, const int32_t* targets, const 
     return single ? go(token_stats_kernel<RAPID_F32, 1>) : go(token_stats_kernel<RAPID_F32, 4>);
 }
 
-cudaError_t launch_token_grads(const RowsArgs& a, const int32_t* targets, const double* coef, int seq_len, cudaStream_t stream) {
+cudaError_t launch_token_grads(const RowsArgs& a, const int32_t* targets, const double* coef, const Divisor& seq_len, cudaStream_t stream) {
     const int64_t nvec = a.vocab / (16 / (int64_t)elem_size(a.dtype));
     const int64_t pieces = std::max<int64_t>(1, (nvec + kPiece - 1) / kPiece), total = pieces * a.n_rows;
     if (total > 0x7fffffffll) return cudaErrorInvalidValue;  // 17 TB of gradient

@@ -11,28 +11,21 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 
-// Sum over the block, the same in all threads; the order depends on the block's size alone.
-template <class T>
-__device__ __forceinline__ T block_sum(T v, T* sh) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    v = warp_sum(v);
-    __syncthreads();
-    if (lane == 0) sh[warp] = v;
-    __syncthreads();
-    T t = 0;
-    for (int w = 0; w < warps; ++w) t += sh[w];
-    return t;
-}
-
 // ---- before the rows -------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ void clear_header(const Scratch& w) {
     if (blockIdx.x == 0 && threadIdx.x == 0) *w.head = Header{0u, 0u, RAPID_OK, 0};
 }
 
+__device__ __forceinline__ void write_counts(int live, int bad, const Scratch& w) {
+    __shared__ double sh[64];
+    double v[2] = {(double)live, (double)bad};
+    block_sums(v, sh);
+    if (threadIdx.x == 0) w.counts[blockIdx.x] = make_int2((int)v[0], (int)v[1]);
+}
+
 __global__ void __launch_bounds__(kThreads)
 prepare_tokens_kernel(int64_t n_rows, int vocab, const int32_t* __restrict__ targets, const uint8_t* __restrict__ mask, Scratch w) {
-    __shared__ int sh[kWarps];
     clear_header(w);
     int live = 0, bad = 0;
     for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < n_rows; r += (int64_t)gridDim.x * kThreads) {
@@ -45,179 +38,140 @@ prepare_tokens_kernel(int64_t n_rows, int vocab, const int32_t* __restrict__ tar
         live += st == ROW_OK;
         bad += st == ROW_BAD_TOKEN;
     }
-    live = block_sum(live, sh);
-    bad = block_sum(bad, sh);
-    if (threadIdx.x == 0) w.counts[blockIdx.x] = make_int2(live, bad);
+    write_counts(live, bad, w);
 }
 
 // Rows that count of every generation: one block of 32 or 256 threads each.
 __global__ void __launch_bounds__(kThreads) count_by_seq_kernel(int seq_len, Scratch w) {
-    __shared__ int sh[kWarps];
     const uint8_t* st = w.state + (int64_t)blockIdx.x * seq_len;
-    int n = 0;
-    for (int t = threadIdx.x; t < seq_len; t += blockDim.x) n += st[t] == ROW_OK;
-    n = block_sum(n, sh);
-    if (threadIdx.x == 0) w.seq_rows[blockIdx.x] = n;
+    __shared__ double sh[32];
+    double n[1] = {0.0};
+    for (int t = threadIdx.x; t < seq_len; t += blockDim.x) n[0] += st[t] == ROW_OK ? 1.0 : 0.0;
+    block_sums(n, sh);
+    if (threadIdx.x == 0) w.seq_rows[blockIdx.x] = (int)n[0];
 }
 
-// A warp for each row: whether its list is valid, and the teacher's log-sum-exp in base 2.
+// W lanes for each row, R entries a lane: whether the row's list is valid, and the teacher's log-sum-exp in base 2.
+template <int W, int R>
 __global__ void __launch_bounds__(kThreads)
 prepare_lists_kernel(int64_t n_rows, int vocab, int k, int64_t ld, double kd, const int32_t* __restrict__ index,
                      const float* __restrict__ logit, const float* __restrict__ top_lse, const uint8_t* __restrict__ mask, Scratch w) {
-    constexpr int R = kMaxList / 32;
-    __shared__ int sh[kWarps];
+    constexpr int kRows = kThreads / W;
     clear_header(w);
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x % W;
+    const unsigned group = W == 32 ? 0xffffffffu : ((1u << W) - 1) << (threadIdx.x & 31 & ~(W - 1));  // this row's lanes of the warp
     int live = 0, bad = 0;
-    for (int64_t r = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); r < n_rows; r += (int64_t)gridDim.x * kWarps) {
-        uint8_t st = ROW_MASKED;
-        if (!mask || mask[r]) {
-            int v[R];
-            float t[R], top = -INFINITY;
-            bool some = false, wrong = false;
+    for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < n_rows; r0 += (int64_t)gridDim.x * kRows) {  // the whole block at a time
+        const int64_t r = r0 + threadIdx.x / W;
+        const bool on = r < n_rows && (!mask || mask[r]);
+        int v[R];
+        float t[R], top = -INFINITY;
+        bool some = false, wrong = false;
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const int j = 32 * i + lane;
-                v[i] = -1;
-                t[i] = -INFINITY;
-                if (j < k) {
-                    v[i] = index[r * ld + j];
-                    if (v[i] >= 0) {
-                        t[i] = logit[r * ld + j];
-                        some = true;
-                        wrong |= v[i] >= vocab || !(t[i] < INFINITY);
-                        top = fmaxf(top, t[i]);
-                    }
+        for (int i = 0; i < R; ++i) {
+            const int j = W * i + lane;
+            v[i] = -1 - j;  // places without an entry differ from one another
+            t[i] = -INFINITY;
+            if (on && j < k) {
+                const int x = index[r * ld + j];
+                const float z = logit[r * ld + j];
+                if (x >= 0) {
+                    v[i] = x;
+                    t[i] = z;
+                    some = true;
+                    wrong |= x >= vocab || !(z < INFINITY);
+                    top = fmaxf(top, z);
                 }
             }
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                if (32 * i >= k) break;
-                for (int l = 0; l < 32; ++l) {
-                    const int x = __shfl_sync(0xffffffffu, v[i], l);
-                    if (x < 0) continue;
-#pragma unroll
-                    for (int i2 = i; i2 < R; ++i2) wrong |= v[i2] == x && 32 * i2 + lane > 32 * i + l;
-                }
-            }
-            some = __any_sync(0xffffffffu, some);
-            top = warp_max(top);
-            double lse2;
-            if (top_lse) {
-                const float l = top_lse[r];
-                wrong |= !isfinite(l);
-                lse2 = (double)l * kLog2eD;
-            } else {
-                some = some && top > -INFINITY;
-                double s = 0.0;
-#pragma unroll
-                for (int i = 0; i < R; ++i)
-                    if (t[i] > -INFINITY) s += exp2(((double)t[i] - (double)top) * kd);
-                lse2 = (double)top * kd + log2(warp_sum(s));
-            }
-            wrong = __any_sync(0xffffffffu, wrong);
-            st = wrong ? ROW_BAD_TOKEN : some ? ROW_OK : ROW_MASKED;
-            if (lane == 0) w.teacher_lse2[r] = lse2;
         }
-        if (lane == 0) {
+        // every pair of entries once: a lane against those up to half way round, and its own
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+#pragma unroll
+            for (int o = 1; o <= W / 2; ++o) wrong |= __shfl_sync(0xffffffffu, v[i], lane + o, W) == v[i];
+            if (R > 1) {
+#pragma unroll 4
+                for (int o = 0; o < W; ++o) {
+                    const int x = __shfl_sync(0xffffffffu, v[i], lane + o, W);
+#pragma unroll
+                    for (int i2 = i + 1; i2 < R; ++i2) wrong |= x == v[i2];
+                }
+            }
+        }
+#pragma unroll
+        for (int o = W / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        some = (__ballot_sync(0xffffffffu, some) & group) != 0;
+        double lse2;
+        if (top_lse) {
+            const float l = on ? top_lse[r] : 0.f;
+            wrong |= !isfinite(l);
+            lse2 = (double)l * kLog2eD;
+        } else {
+            some = some && top > -INFINITY;
+            double s = 0.0;
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (t[i] > -INFINITY && t[i] < INFINITY) s += exp2_short(((double)t[i] - (double)top) * kd);
+#pragma unroll
+            for (int o = W / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            lse2 = s > 0.0 ? (double)top * kd + log2_short(s) : 0.0;
+        }
+        wrong = (__ballot_sync(0xffffffffu, wrong) & group) != 0;
+        if (lane == 0 && r < n_rows) {
+            const uint8_t st = !on ? ROW_MASKED : wrong ? ROW_BAD_TOKEN : some ? ROW_OK : ROW_MASKED;
             w.state[r] = st;
+            w.teacher_lse2[r] = lse2;
             live += st == ROW_OK;
             bad += st == ROW_BAD_TOKEN;
         }
     }
-    live = block_sum(live, sh);
-    bad = block_sum(bad, sh);
-    if (threadIdx.x == 0) w.counts[blockIdx.x] = make_int2(live, bad);
+    write_counts(live, bad, w);
+}
+
+cudaError_t launch_prepare_lists(const rapid_distill_desc_t& d, double kd, const int32_t* index, const float* logit, const float* top_lse,
+                                 const uint8_t* mask, const Scratch& w, int* blocks, cudaStream_t st) {
+    auto go = [&](auto kern, int width) {
+        const int64_t b = (d.n_rows * width + kThreads - 1) / kThreads;
+        *blocks = (int)(b < kPrepBlocks ? b : kPrepBlocks);
+        kern<<<*blocks, kThreads, 0, st>>>(d.n_rows, d.vocab, d.k, d.ld_top, kd, index, logit, top_lse, mask, w);
+        return cudaGetLastError();
+    };
+    if (d.k <= 8) return go(prepare_lists_kernel<8, 1>, 8);
+    if (d.k <= 16) return go(prepare_lists_kernel<16, 1>, 16);
+    if (d.k <= 32) return go(prepare_lists_kernel<32, 1>, 32);
+    if (d.k <= 64) return go(prepare_lists_kernel<32, 2>, 32);
+    if (d.k <= 128) return go(prepare_lists_kernel<32, 4>, 32);
+    return go(prepare_lists_kernel<32, 8>, 32);
 }
 
 // ---- after the rows --------------------------------------------------------------------------------------------
 
-// The last block of a summing kernel adds up the blocks' sums, in their order.  Returns whether this is it; `total` then holds
-// the sums, in all threads.
-template <int N>
-__device__ __forceinline__ bool last_block_sums(const double (&mine)[N], const Scratch& w, double (&total)[N]) {
-    __shared__ double sh[kWarps];
+// Many rows: the sums by blocks, and by the last of them over all.
+template <class Op>
+__global__ void __launch_bounds__(kThreads) sum_rows_kernel(Op op, Totals t, int64_t n_rows, Scratch w) {
+    constexpr int N = SumsOf<Op>::kN;
     __shared__ bool last;
-    double block[N];
+    __shared__ double sh[32 * N];
+    double v[N] = {};
+    for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < n_rows; r += (int64_t)gridDim.x * kThreads) add_row(op, t, r, w, v);
+    block_sums(v, sh);
+    if (threadIdx.x == 0)
 #pragma unroll
-    for (int i = 0; i < N; ++i) block[i] = block_sum(mine[i], sh);
-    if (threadIdx.x == 0) {
+        for (int i = 0; i < N; ++i) w.sums[(size_t)blockIdx.x * 8 + i] = v[i];
+    if (!is_last_block(w.head, &last)) return;
 #pragma unroll
-        for (int i = 0; i < N; ++i) w.sums[(size_t)blockIdx.x * 8 + i] = block[i];
-        __threadfence();
-        last = atomicAdd(&w.head->done, 1u) == gridDim.x - 1;
-    }
-    __syncthreads();
-    if (!last) return false;
-    __threadfence();
+    for (int i = 0; i < N; ++i) v[i] = 0.0;
+    for (unsigned b = threadIdx.x; b < gridDim.x; b += kThreads)
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        double t = 0.0;
-        for (unsigned b = threadIdx.x; b < gridDim.x; b += kThreads) t += __ldcg(w.sums + (size_t)b * 8 + i);
-        total[i] = block_sum(t, sh);
-    }
-    return true;
+        for (int i = 0; i < N; ++i) v[i] += __ldcg(w.sums + (size_t)b * 8 + i);
+    block_sums(v, sh);
+    if (threadIdx.x == 0) write_totals(op, t, w, v);
 }
-
-__device__ __forceinline__ void counts_of(const int2* counts, int blocks, long long& live, int& bad) {
-    live = 0;
-    bad = 0;
-    for (int i = threadIdx.x & 31; i < blocks; i += 32) {
-        live += counts[i].x;
-        bad += counts[i].y;
-    }
-    live = warp_sum(live);
-    bad = warp_sum(bad);
-}
-
-__global__ void __launch_bounds__(kThreads)
-clip_sum_kernel(ClipOp op, int64_t n_rows, float* __restrict__ token_logp, float* __restrict__ loss, rapid_loss_stats_t* stats, Scratch w) {
-    double mine[6] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0}, total[6];
-    const bool by_seq = (op.flags & RAPID_LOSS_NORM_SEQ) != 0;
-    for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < n_rows; r += (int64_t)gridDim.x * kThreads) {
-        double lp = 0.0;
-        const uint8_t st = w.state[r];
-        if (st == ROW_OK) {
-            lp = w.value[r];
-            const ClipIn in = clip_in(op, r);
-            const ClipTerms t = clip_terms(op, in, lp);
-            mine[0] += by_seq ? t.loss / (double)op.seq_rows[sequence(r, op.seq_len)] : t.loss;
-            mine[1] += lp - in.old;
-            mine[2] += t.kl;
-            mine[3] += t.cut ? 1.0 : 0.0;
-            mine[4] += 1.0;
-        }
-        mine[5] += st == ROW_BAD_TOKEN ? 1.0 : 0.0;
-        if (token_logp) token_logp[r] = (float)lp;
-    }
-    if (!last_block_sums(mine, w, total) || threadIdx.x != 0) return;
-    const long long rows = (long long)total[4];
-    const double l = rows > 0 ? shared_weight(op, rows) * total[0] : 0.0;
-    *loss = (float)l;
-    if (stats) {
-        const double n = rows > 0 ? (double)rows : 1.0;
-        *stats = rapid_loss_stats_t{rows, (int32_t)total[3], (int32_t)total[5], 0, w.head->status, total[1] / n, total[2] / n, l};
-    }
-}
-
-__global__ void __launch_bounds__(kThreads)
-distill_sum_kernel(DistillOp op, int64_t n_rows, float* __restrict__ token_loss, float* __restrict__ loss, rapid_loss_stats_t* stats,
-                   Scratch w) {
-    double mine[1] = {0.0}, total[1];
-    for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < n_rows; r += (int64_t)gridDim.x * kThreads) {
-        const double v = w.state[r] == ROW_OK ? w.value[r] : 0.0;
-        mine[0] += v;
-        if (token_loss) token_loss[r] = (float)v;
-    }
-    if (!last_block_sums(mine, w, total)) return;
-    long long rows;
-    int bad;
-    counts_of(op.counts, op.count_blocks, rows, bad);
-    if (threadIdx.x != 0) return;
-    const double z = (op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows;
-    const double l = rows > 0 ? op.scale * total[0] / z : 0.0;
-    *loss = (float)l;
-    if (stats) *stats = rapid_loss_stats_t{rows, 0, bad, 0, w.head->status, 0.0, 0.0, l};
+template <class Op>
+cudaError_t launch_sums(const Op& op, const Totals& t, int64_t n_rows, const Scratch& w, cudaStream_t st) {
+    const int64_t b = (n_rows + kThreads - 1) / kThreads;
+    sum_rows_kernel<<<(unsigned)(b < kSumBlocks ? b : kSumBlocks), kThreads, 0, st>>>(op, t, n_rows, w);
+    return cudaGetLastError();
 }
 
 struct PairArgs {
@@ -232,10 +186,8 @@ __device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log
 
 // By one block: every pair's loss and slope, and their sums; returns what the slopes are multiplied by.
 __device__ double pairs_of(const PairArgs& a, const Scratch& w) {
-    __shared__ double sh[32];
-    __shared__ int shi[32];
-    double sum = 0.0, sum_h = 0.0;
-    int valid = 0, won = 0, rows = 0, bad = 0;
+    __shared__ double sh[32 * 6];
+    double v[6] = {};  // losses, margins, valid pairs, pairs won, rows, rows that are not valid
     for (int p = threadIdx.x; p < a.n_pairs; p += blockDim.x) {
         const int i = a.pairs[2 * p], j = a.pairs[2 * p + 1];
         double h = NAN, slope = 0.0;
@@ -252,32 +204,26 @@ __device__ double pairs_of(const PairArgs& a, const Scratch& w) {
                 f = (1.0 - a.smoothing) * softplus(-h) + a.smoothing * softplus(h);
                 slope = 1.0 / (1.0 + exp(-h)) - (1.0 - a.smoothing);
             }
-            sum += f;
-            sum_h += h;
-            valid += 1;
-            won += h > 0.0;
+            v[0] += f;
+            v[1] += h;
+            v[2] += 1.0;
+            v[3] += h > 0.0 ? 1.0 : 0.0;
         }
         w.pair_slope[p] = slope;
         if (a.margins) a.margins[p] = (float)h;
     }
-    long long live = 0;
     for (int n = threadIdx.x; n < a.n_seq; n += blockDim.x) {
-        live += __ldcg(w.seq_rows + n);
-        bad += __ldcg(w.seq_bad + n);
+        v[4] += (double)__ldcg(w.seq_rows + n);
+        v[5] += (double)__ldcg(w.seq_bad + n);
     }
-    sum = block_sum(sum, sh);
-    sum_h = block_sum(sum_h, sh);
-    live = (long long)block_sum((double)live, sh);
-    valid = block_sum(valid, shi);
-    won = block_sum(won, shi);
-    bad = block_sum(bad, shi);
-    const double z = (a.flags & RAPID_LOSS_NORM_GIVEN) ? a.norm_z : (double)valid;
+    block_sums(v, sh);
+    const double z = (a.flags & RAPID_LOSS_NORM_GIVEN) ? a.norm_z : v[2];
     if (threadIdx.x == 0) {
-        const double l = valid > 0 ? a.scale * sum / z : 0.0, n = valid > 0 ? (double)valid : 1.0;
+        const double l = v[2] > 0.0 ? a.scale * v[0] / z : 0.0, n = v[2] > 0.0 ? v[2] : 1.0;
         *a.loss = (float)l;
-        if (a.stats) *a.stats = rapid_loss_stats_t{live, 0, bad, valid, RAPID_OK, sum_h / n, (double)won / n, l};
+        if (a.stats) *a.stats = rapid_loss_stats_t{(long long)v[4], 0, (int32_t)v[5], (int32_t)v[2], RAPID_OK, v[1] / n, v[3] / n, l};
     }
-    return valid > 0 ? a.scale * a.beta / z : 0.0;
+    return v[2] > 0.0 ? a.scale * a.beta / z : 0.0;
 }
 
 // By one warp: minus the loss's slope by the sum of generation n's log-probabilities, over the pairs that it is in.
@@ -301,40 +247,29 @@ __device__ __forceinline__ void coefficient(const PairArgs& a, const Scratch& w,
 // the coefficients, which saves a call with few rows two launches.
 __global__ void __launch_bounds__(kThreads)
 pref_seq_kernel(PairArgs a, const float* __restrict__ ref_logp, float* __restrict__ token_logp, int all, Scratch w) {
-    __shared__ double sh[kWarps];
-    __shared__ int shi[kWarps];
     __shared__ bool last;
     const int64_t base = (int64_t)blockIdx.x * a.seq_len;
-    double s = 0.0;
-    int n = 0, bad = 0;
+    __shared__ double sh[32 * 3];
+    double v[3] = {};  // log-ratios, rows, rows that are not valid
     for (int t = threadIdx.x; t < a.seq_len; t += kThreads) {
         const int64_t r = base + t;
         const uint8_t st = w.state[r];
         double lp = 0.0;
         if (st == ROW_OK) {
             lp = w.value[r];
-            s += ref_logp ? lp - (double)ref_logp[r] : lp;
-            n += 1;
+            v[0] += ref_logp ? lp - (double)ref_logp[r] : lp;
+            v[1] += 1.0;
         }
-        bad += st == ROW_BAD_TOKEN;
+        v[2] += st == ROW_BAD_TOKEN ? 1.0 : 0.0;
         if (token_logp) token_logp[r] = (float)lp;
     }
-    s = block_sum(s, sh);
-    n = block_sum(n, shi);
-    bad = block_sum(bad, shi);
+    block_sums(v, sh);
     if (threadIdx.x == 0) {
-        w.seq_rows[blockIdx.x] = n;
-        w.seq_bad[blockIdx.x] = bad;
-        w.seq_sum[blockIdx.x] = (a.flags & RAPID_PREF_TOKEN_MEAN) && n > 0 ? s / (double)n : s;
-        if (all) {
-            __threadfence();
-            last = atomicAdd(&w.head->done, 1u) == gridDim.x - 1;
-        }
+        w.seq_rows[blockIdx.x] = (int)v[1];
+        w.seq_bad[blockIdx.x] = (int)v[2];
+        w.seq_sum[blockIdx.x] = (a.flags & RAPID_PREF_TOKEN_MEAN) && v[1] > 0.0 ? v[0] / v[1] : v[0];
     }
-    if (!all) return;
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
+    if (!all || !is_last_block(w.head, &last)) return;
     const double by = pairs_of(a, w);
     __syncthreads();
     for (int i = threadIdx.x >> 5; i < a.n_seq; i += kWarps) coefficient(a, w, i, by);
@@ -350,11 +285,6 @@ __global__ void __launch_bounds__(kThreads) pref_coef_kernel(PairArgs a, Scratch
     if (n < a.n_seq) coefficient(a, w, n, w.sums[0]);
 }
 
-unsigned sum_blocks(int64_t T) {
-    const int64_t b = (T + kThreads - 1) / kThreads;
-    return (unsigned)(b < kSumBlocks ? b : kSumBlocks);
-}
-
 }  // namespace
 
 cudaError_t launch_count_by_seq(int n_seq, int seq_len, const Scratch& w, cudaStream_t stream) {
@@ -364,7 +294,7 @@ cudaError_t launch_count_by_seq(int n_seq, int seq_len, const Scratch& w, cudaSt
 
 cudaError_t launch_prepare_tokens(int n_seq, int seq_len, int vocab, const int32_t* targets, const uint8_t* mask, const Scratch& w,
                                   int by_seq, int* blocks, cudaStream_t stream) {
-    const int64_t T = (int64_t)n_seq * seq_len, b = (T + 1023) / 1024;
+    const int64_t T = (int64_t)n_seq * seq_len, b = (T + kThreads - 1) / kThreads;
     *blocks = (int)(b < kPrepBlocks ? b : kPrepBlocks);
     prepare_tokens_kernel<<<*blocks, kThreads, 0, stream>>>(T, vocab, targets, mask, w);
     return by_seq ? launch_count_by_seq(n_seq, seq_len, w, stream) : cudaGetLastError();
@@ -451,18 +381,18 @@ rapid_status_t rapid_clip_loss(const rapid_clip_desc_t* desc, const void* logits
     if ((s = check_device(&sms)) != RAPID_OK) return s;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool by_seq = (d.flags & RAPID_LOSS_NORM_SEQ) != 0;
-    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, make_factor(1.0), w};
+    const Totals end{token_logp, loss, stats, dlogits && T <= kFewRows};
+    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, make_factor(1.0), w, end};
     int blocks = 0;
     if (dlogits) {
         if (launch_prepare_tokens(d.n_seq, d.seq_len, d.vocab, targets, mask, w, by_seq, &blocks, st) != cudaSuccess) return RAPID_ERR_CUDA;
     } else if (launch_token_stats(a, targets, mask, st) != cudaSuccess || (by_seq && launch_count_by_seq(d.n_seq, d.seq_len, w, st) != cudaSuccess)) {
         return RAPID_ERR_CUDA;
     }
-    const ClipOp op{targets, old_logp, ref_logp, adv, w.seq_rows, w.counts, blocks, d.n_seq, d.seq_len, d.flags, d.eps_low, d.eps_high,
+    const ClipOp op{targets, old_logp, ref_logp, adv, w.seq_rows, w.counts, blocks, d.n_seq, make_divisor(d.seq_len), d.flags, d.eps_low, d.eps_high,
                     d.kl_beta, d.scale, d.norm_z};
     if (dlogits && launch_rows(a, op, sms, st) != cudaSuccess) return RAPID_ERR_CUDA;
-    clip_sum_kernel<<<sum_blocks(T), kThreads, 0, st>>>(op, T, token_logp, loss, stats, w);
-    return cuda_status(cudaGetLastError());
+    return end.last_block ? RAPID_OK : cuda_status(launch_sums(op, end, T, w, st));
 }
 
 rapid_status_t rapid_preference_loss_workspace_bytes(const rapid_pref_desc_t* desc, size_t* bytes) {
@@ -489,7 +419,7 @@ rapid_status_t rapid_preference_loss(const rapid_pref_desc_t* desc, const void* 
     int sms = 0;
     if ((s = check_device(&sms)) != RAPID_OK) return s;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, make_factor(1.0), w};
+    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, make_factor(1.0), w, Totals{}};
     if (launch_token_stats(a, targets, mask, st) != cudaSuccess) return RAPID_ERR_CUDA;
     const PairArgs pa{pairs, d.n_pairs, d.n_seq, d.seq_len, d.flags, d.beta, d.margin, d.label_smoothing, d.scale, d.norm_z, margins, loss, stats};
     const int all = d.n_pairs <= 4096 && (int64_t)d.n_pairs * d.n_seq <= 1 << 16;  // some ten microseconds of one block at most
@@ -499,7 +429,7 @@ rapid_status_t rapid_preference_loss(const rapid_pref_desc_t* desc, const void* 
         if (dlogits) pref_coef_kernel<<<(unsigned)(((int64_t)d.n_seq + kWarps - 1) / kWarps), kThreads, 0, st>>>(pa, w);
     }
     if (cudaGetLastError() != cudaSuccess) return RAPID_ERR_CUDA;
-    return dlogits ? cuda_status(launch_token_grads(a, targets, w.seq_coef, d.seq_len, st)) : RAPID_OK;
+    return dlogits ? cuda_status(launch_token_grads(a, targets, w.seq_coef, make_divisor(d.seq_len), st)) : RAPID_OK;
 }
 
 rapid_status_t rapid_distill_loss_workspace_bytes(const rapid_distill_desc_t* desc, size_t* bytes) {
@@ -525,16 +455,14 @@ rapid_status_t rapid_distill_loss(const rapid_distill_desc_t* desc, const void* 
     if ((s = check_device(&sms)) != RAPID_OK) return s;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const Factor f = make_factor(d.temperature);
-    const int64_t b = (d.n_rows + 4 * kWarps - 1) / (4 * kWarps);
-    const int blocks = (int)(b < kPrepBlocks ? b : kPrepBlocks);
-    prepare_lists_kernel<<<blocks, kThreads, 0, st>>>(d.n_rows, d.vocab, d.k, d.ld_top, f.kd, top_index, top_logit, top_lse, mask, w);
-    if (cudaGetLastError() != cudaSuccess) return RAPID_ERR_CUDA;
+    int blocks = 0;
+    if (launch_prepare_lists(d, f.kd, top_index, top_logit, top_lse, mask, w, &blocks, st) != cudaSuccess) return RAPID_ERR_CUDA;
     const DistillOp op{top_index, top_logit, w.teacher_lse2, w.counts, d.ld_top, d.k, top_lse != nullptr, blocks, d.flags, 1.0 / d.temperature,
                        d.scale, d.norm_z, f.kd};
-    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, d.n_rows, d.vocab, d.dtype, f, w};
+    const Totals end{token_loss, loss, stats, d.n_rows <= kFewRows};
+    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, d.n_rows, d.vocab, d.dtype, f, w, end};
     if (launch_rows(a, op, sms, st) != cudaSuccess) return RAPID_ERR_CUDA;
-    distill_sum_kernel<<<sum_blocks(d.n_rows), kThreads, 0, st>>>(op, d.n_rows, token_loss, loss, stats, w);
-    return cuda_status(cudaGetLastError());
+    return end.last_block ? RAPID_OK : cuda_status(launch_sums(op, end, d.n_rows, w, st));
 }
 
 }  // extern "C"
