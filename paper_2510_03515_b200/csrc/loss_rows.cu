@@ -454,16 +454,22 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
 // ---- shorter rows ----------------------------------------------------------------------------------------------
 
 // A group of G warps holds a whole row in its share of the SM's shared memory and does everything for it; as many groups as fit work
-// side by side on an SM and hide one another's latencies.  A row comes in kParts bulk copies; a part's place is loaded with the next
-// row as soon as the second reading is through with it.  Rows are drawn from a counter, two ahead.
+// side by side on an SM and hide one another's latencies.  A row comes in kParts bulk copies; the last warp to have read a part for the
+// last time has the next row's part loaded in its place, so the warps meet only twice a row: to join their sums, and for the
+// factor.  Rows are drawn from a counter, two ahead.
 
-constexpr int kParts = 4;
+constexpr int kParts = 2;
+
+// Vectors of a thread at a time: eight hide more latency, where the registers are there for them (16384 rows of 16384 bf16 228 -> 220 us;
+// eight warps a row 314 -> 325, one 154 either way).
+template <int G>
+constexpr int kBatch = G == 2 || G == 4 ? 8 : 4;
 
 struct GroupShape {
     int groups;          // of a block
-    int row_bytes;       // place of a row, whole parts
+    int row_bytes;       // place of a row
     int group_bytes;     // of a group in shared memory
-    int part_vecs;       // vectors of a part, a multiple of the group's threads
+    int part_vecs;       // vectors of a part, whole batches of every thread
     int parts;           // of a row
     int list;
 };
@@ -472,7 +478,8 @@ struct GroupBoard {
     uint64_t full[kParts];
     WarpPart parts[2][8];
     GradConst grad;
-    long long next[2];  // the next row, ~row when it does not count; of odd and even turns
+    int read[kParts];    // warps that are through with a part
+    long long next[2];   // the next row, ~row when it does not count; of odd and even turns
 };
 
 // The warps of a group together, with the OR of what they say: after a wait that gave up all leave together.
@@ -492,20 +499,23 @@ __device__ __forceinline__ bool group_sync(int id, bool flag) {
 }
 
 template <int DT, class Op, int G>
-__global__ void __launch_bounds__(768, 1) group_kernel(RowsArgs a, Op op, GroupShape sh) {
+__global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a, Op op, GroupShape sh) {
     using E = Elem<DT>;
     using T = typename E::T;
     constexpr int kLanes = G * 32;
-    constexpr int U = 4;  // vectors of a thread at a time
+    constexpr int U = kBatch<G>;  // vectors of a thread at a time
     extern __shared__ __align__(128) uint8_t dyn[];
     __shared__ int abort_flag;
     __shared__ double weight;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = warp / G, gw = warp % G, gt = threadIdx.x % kLanes;
     uint8_t* place = dyn + (size_t)group * sh.group_bytes;
     GroupBoard& bd = *reinterpret_cast<GroupBoard*>(place + sh.row_bytes);
-    const Slot slot = slot_at(place + sh.row_bytes + sizeof(GroupBoard), sh.list);
+    uint8_t* slots = place + sh.row_bytes + sizeof(GroupBoard);
     if (gt == 0) {
-        for (int p = 0; p < kParts; ++p) mbar_init(&bd.full[p], 1);
+        for (int p = 0; p < kParts; ++p) {
+            mbar_init(&bd.full[p], 1);
+            bd.read[p] = 0;
+        }
         mbar_init_fence();
     }
     if (threadIdx.x == 0) abort_flag = 0;
@@ -519,14 +529,14 @@ __global__ void __launch_bounds__(768, 1) group_kernel(RowsArgs a, Op op, GroupS
     const bool grad = a.grad != nullptr, ex = exclude(op);
     const int nvec = a.vocab / E::kPer, rest = a.vocab - nvec * E::kPer, all = nvec + (rest ? 1 : 0);
     const int n_list = list_size(op), id = group + 1;
+    const unsigned int n_rows = (unsigned int)a.n_rows;
     const uint64_t once = policy_first();
     const float off = shift_fraction(gw), unit_off = shift_fraction(lane);
     const double unit = part_unit(unit_off), unit0 = part_unit(off);
     const uint4* row_place = reinterpret_cast<const uint4*>(place);
 
-    const unsigned int n_rows = (unsigned int)a.n_rows;
-    uint32_t issued = 0, phase_of = 0;  // a bit for each part: anything loaded, and the phase of its last load
-    auto load_part = [&](int64_t r, int p, uint32_t phase) {  // by the group's first thread
+    uint32_t issued = 0, phase_of = 0;  // a bit for each part: loaded by this thread, and the phase of its last load
+    auto load_part = [&](int64_t r, int p, uint32_t phase) {  // by one thread
         issued |= 1u << p;
         phase_of = (phase_of & ~(1u << p)) | phase << p;
         const int v = p * sh.part_vecs, bytes = min(sh.part_vecs, all - v) * 16;
@@ -536,24 +546,29 @@ __global__ void __launch_bounds__(768, 1) group_kernel(RowsArgs a, Op op, GroupS
     };
     auto state_of = [&](unsigned int t) -> int { return t < n_rows ? (int)a.w.state[t] : ROW_MASKED; };
 
-    // draws: the first ones are dealt out, one to every group of the grid; gt == 0 is ahead by two
+    // draws: the first ones are dealt out, one to every group of the grid; the group's first thread is ahead by two
     const unsigned int everyone = gridDim.x * sh.groups;
     unsigned int t0 = group * gridDim.x + blockIdx.x, t1 = 0, t2 = 0;
     int state1 = ROW_MASKED;
-    int64_t row = -1;  // this row; ~row when it does not count; n_rows when there are none left
-    bool live = false;
-    {
-        const int st = state_of(t0);
-        live = st == ROW_OK;
-        row = t0 < n_rows ? (int64_t)t0 : a.n_rows;
-        if (gt == 0) {
-            t1 = everyone + atomicAdd(&a.w.head->ticket, 1u);
-            if (live)
-                for (int p = 0; p < sh.parts; ++p) load_part(row, p, 0u);
-        }
+    int64_t row = t0 < n_rows ? (int64_t)t0 : a.n_rows;  // n_rows: there are none left
+    bool live = state_of(t0) == ROW_OK;
+    if (gt == 0) {
+        t1 = everyone + atomicAdd(&a.w.head->ticket, 1u);
+        if (live)
+            for (int p = 0; p < sh.parts; ++p) load_part(row, p, 0u);
     }
-    uint32_t ph = 0;  // phase of the parts, that is of the rows that are read
+    uint32_t ph = 0;         // phase of the parts, that is of the rows that are read
+    int64_t pending = -1;    // the row whose chosen columns are still to be written
     bool ok = true;
+    auto write_pending = [&]() {  // by the first warp, when the group has met since
+        const Slot old = slot_at(slots + (ph ^ 1u) * sh.list * kSlotEntry, sh.list);
+        T* out = static_cast<T*>(a.grad) + pending * a.ld_grad;
+        for (int j = lane; j < n_list; j += 32) {
+            const int v = old.col[j];
+            if (v >= 0) out[v] = E::put(old.x[j]);
+        }
+        pending = -1;
+    };
     for (uint32_t turn = 0; row < a.n_rows; ++turn) {
         if (gt == 0) {
             t2 = everyone + atomicAdd(&a.w.head->ticket, 1u);
@@ -574,6 +589,8 @@ __global__ void __launch_bounds__(768, 1) group_kernel(RowsArgs a, Op op, GroupS
             }
             announce();
             if (group_sync<G>(id, !ok)) break;
+            __syncwarp();
+            if (gw == 0 && pending >= 0) write_pending();
             const long long next = bd.next[turn & 1];
             row = next < 0 ? ~next : next;
             live = next >= 0 && next < a.n_rows;
@@ -581,30 +598,14 @@ __global__ void __launch_bounds__(768, 1) group_kernel(RowsArgs a, Op op, GroupS
                 for (int p = 0; p < sh.parts; ++p) load_part(row, p, ph);
             continue;
         }
-        // ---- the row's chosen columns, by the group's first warp ----
-        auto landed = [&](int p) { return ok && (ok = warp_wait(&bd.full[p], ph, abortp)); };
-        decltype(look(op, row, shared, slot.col, slot.z, slot.x)) mine{};
-        if (gw == 0) {
+        const Slot slot = slot_at(slots + ph * sh.list * kSlotEntry, sh.list);
+        if (gw == 0)
             for (int j = lane; j < n_list; j += 32) {
                 const int v = column(op, row, j);
                 slot.col[j] = v;
                 if (v >= 0) slot.x[j] = entry(op, row, j);
             }
-            if (ex) {  // they are taken out of the sum before anyone reads the row
-                for (int p = 0; p < sh.parts; ++p) landed(p);
-                if (ok)
-                    for (int j = lane; j < n_list; j += 32) {
-                        const int v = slot.col[j];
-                        if (v < 0) continue;
-                        T* e = reinterpret_cast<T*>(place) + v;
-                        slot.z[j] = E::get(*e);
-                        *e = E::put(-INFINITY);
-                    }
-                fence_proxy_async_smem();  // a bulk copy writes there next
-                __syncwarp();
-            }
-        }
-        if (G > 1 && ex && group_sync<G>(id, !ok)) break;
+        if (!grad) announce();
         // vector `at` of the row; columns behind the last read as -inf
         auto read = [&](int at) {
             constexpr uint32_t kNone = DT == RAPID_BF16 ? 0xff80ff80u : 0xff800000u;
@@ -627,63 +628,74 @@ __global__ void __launch_bounds__(768, 1) group_kernel(RowsArgs a, Op op, GroupS
             }
             return v;
         };
-        bool left = false;
         long long next = 0;
-        // part p has been read for the last time: the next row's comes there
+        // this warp has read part p for the last time; the last one to say so has the next row's loaded there
         auto hand_over = [&](int p) {
-            if (group_sync<G>(id, !ok)) {
-                left = true;
-                return;
-            }
-            if (p == 0) next = bd.next[turn & 1];  // announced before
-            if (gt == 0 && next >= 0 && next < a.n_rows) {
-                fence_proxy_async_smem();
-                load_part(next, p, ph ^ 1u);
-            }
-        };
-        RowStat st{0.0, 0.f};
-        {
-            // ---- first reading ----
-            if (!grad) announce();
-            Part p;
-            for (int q = 0; q < sh.parts && !left; ++q) {
-                if (landed(q)) {
-                    const int end = min((q + 1) * sh.part_vecs, all);
-                    int v = q * sh.part_vecs + gt;
-                    for (; v - lane + (U - 1) * kLanes + 31 < min(end, nvec); v += U * kLanes) {
-                        uint4 w[U];
-#pragma unroll
-                        for (int j = 0; j < U; ++j) w[j] = row_place[v + j * kLanes];
-                        p.template vectors<DT, U>(w, off, a.f);
-                    }
-                    for (; v - lane < end; v += kLanes) {
-                        uint4 w[1] = {read(v)};
-                        p.template vectors<DT, 1>(w, off, a.f);
-                    }
-                }
-                if (!grad) {
-                    if (gw == 0 && !ex)  // before the part goes
-                        for (int j = lane; j < n_list; j += 32) {
-                            const int v = slot.col[j];
-                            if (v >= 0 && v / E::kPer / sh.part_vecs == q) slot.z[j] = E::get(reinterpret_cast<const T*>(place)[v]);
-                        }
-                    hand_over(q);
-                }
-            }
-            if (left) break;
-            const WarpPart w = warp_part(p, a.f);
-            if constexpr (G == 1) {
-                st = one_part(w, off, unit0, a.f);
-            } else {
-                if (lane == 0) bd.parts[turn & 1][gw] = w;
-                if (group_sync<G>(id, !ok)) break;
-                if (gw == 0) st = join_parts(lane < G ? bd.parts[turn & 1][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, unit_off, unit, a.f);
-            }
-            if (G == 1 && !ok) break;
-        }
-        RowGrad g{0.0, 0.0};
-        if (gw == 0 && ok) {
             __syncwarp();
+            if (lane != 0) return;
+            if constexpr (G > 1) {
+                __threadfence_block();
+                if (atomicAdd(&bd.read[p], 1) != G - 1) return;
+                __threadfence_block();
+                bd.read[p] = 0;
+            }
+            if (next >= 0 && next < a.n_rows) load_part(next, p, ph ^ 1u);
+        };
+        // ---- first reading ----
+        if (!grad) {
+            if (G > 1 && group_sync<G>(id, !ok)) break;  // the announcement
+            __syncwarp();
+            next = bd.next[turn & 1];
+        }
+        Part p;
+        for (int q = 0; q < sh.parts && ok; ++q) {
+            if (!(ok = warp_wait(&bd.full[q], ph, abortp))) break;
+            const int from = q * sh.part_vecs, end = min(from + sh.part_vecs, all);
+            if (ex) {  // the list's columns of this warp's vectors: their logits are noted and leave the sum
+                bool wrote = false;
+                for (int j = lane; j < n_list; j += 32) {
+                    const int v = G == 1 ? slot.col[j] : column(op, row, j), at = v / E::kPer;
+                    if (v >= 0 && at >= from && at < end && (at - from) % kLanes / 32 == gw) {
+                        T* e = reinterpret_cast<T*>(place) + v;
+                        slot.z[j] = E::get(*e);
+                        *e = E::put(-INFINITY);
+                        wrote = true;
+                    }
+                }
+                if (wrote) fence_proxy_async_smem();  // a bulk copy writes there next
+                __syncwarp();
+            } else if (!grad && gw == 0) {  // before the part goes
+                for (int j = lane; j < n_list; j += 32) {
+                    const int v = slot.col[j], at = v / E::kPer;
+                    if (v >= 0 && at >= from && at < end) slot.z[j] = E::get(reinterpret_cast<const T*>(place)[v]);
+                }
+            }
+            int v = from + gt;
+            for (; v - lane + (U - 1) * kLanes + 31 < min(end, nvec); v += U * kLanes) {
+                uint4 w[U];
+#pragma unroll
+                for (int j = 0; j < U; ++j) w[j] = row_place[v + j * kLanes];
+                p.template vectors<DT, U>(w, off, a.f);
+            }
+            for (; v - lane < end; v += kLanes) {
+                uint4 w[1] = {read(v)};
+                p.template vectors<DT, 1>(w, off, a.f);
+            }
+            if (!grad) hand_over(q);
+        }
+        const WarpPart w = warp_part(p, a.f);
+        RowStat st{0.0, 0.f};
+        if constexpr (G == 1) {
+            if (!ok) break;
+            st = one_part(w, off, unit0, a.f);
+        } else {
+            if (lane == 0) bd.parts[ph][gw] = w;
+            if (group_sync<G>(id, !ok)) break;
+            if (gw == 0) st = join_parts(lane < G ? bd.parts[ph][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, unit_off, unit, a.f);
+        }
+        decltype(look(op, row, shared, slot.col, slot.z, slot.x)) mine{};
+        RowGrad g{0.0, 0.0};
+        if (gw == 0) {
             if (!ex && grad)
                 for (int j = lane; j < n_list; j += 32) {
                     const int v = slot.col[j];
@@ -698,52 +710,52 @@ __global__ void __launch_bounds__(768, 1) group_kernel(RowsArgs a, Op op, GroupS
         if (grad) {
             // ---- second reading ----
             if (group_sync<G>(id, !ok)) break;
+            __syncwarp();
+            next = bd.next[turn & 1];
+            if (gw == G - 1 && next >= 0 && next < a.n_rows) bring_near(op, next);
+            if (gw == 0 && pending >= 0) write_pending();
             const Grad<DT> gr(bd.grad, a.f);
-            for (int q = 0; q < sh.parts && !left; ++q) {
-                if (ok) {
-                    const int end = min((q + 1) * sh.part_vecs, all);
-                    int v = q * sh.part_vecs + gt;
-                    uint4* ov = reinterpret_cast<uint4*>(out);
-                    for (; v - lane + (U - 1) * kLanes + 31 < min(end, nvec); v += U * kLanes) {
-                        uint4 w[U];
+            uint4* ov = reinterpret_cast<uint4*>(out);
+            for (int q = 0; q < sh.parts; ++q) {
+                const int from = q * sh.part_vecs, end = min(from + sh.part_vecs, all);
+                int v = from + gt;
+                for (; v - lane + (U - 1) * kLanes + 31 < min(end, nvec); v += U * kLanes) {
+                    uint4 w[U];
 #pragma unroll
-                        for (int j = 0; j < U; ++j) w[j] = row_place[v + j * kLanes];
+                    for (int j = 0; j < U; ++j) w[j] = row_place[v + j * kLanes];
 #pragma unroll
-                        for (int j = 0; j < U; ++j) st_stream(ov + v + j * kLanes, gr.vector(w[j]));
-                    }
-                    for (; v - lane < end; v += kLanes) {
-                        const uint4 y = gr.vector(read(v));
-                        if (v < nvec) st_stream(ov + v, y);
-                        else if (v == nvec && rest) {
-                            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+                    for (int j = 0; j < U; ++j) st_stream(ov + v + j * kLanes, gr.vector(w[j]));
+                }
+                for (; v - lane < end; v += kLanes) {
+                    const uint4 y = gr.vector(read(v));
+                    if (v < nvec) st_stream(ov + v, y);
+                    else if (v == nvec && rest) {
+                        const uint32_t x[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-                            for (int i = 0; i < E::kPer; ++i) {
-                                if (i >= rest) continue;
-                                if constexpr (DT == RAPID_BF16) out[nvec * E::kPer + i] = (T)(w[i / 2] >> (16 * (i & 1)));
-                                else out[nvec * E::kPer + i] = __uint_as_float(w[i]);
-                            }
+                        for (int i = 0; i < E::kPer; ++i) {
+                            if (i >= rest) continue;
+                            if constexpr (DT == RAPID_BF16) out[nvec * E::kPer + i] = (T)(x[i / 2] >> (16 * (i & 1)));
+                            else out[nvec * E::kPer + i] = __uint_as_float(x[i]);
                         }
                     }
                 }
                 hand_over(q);
             }
-            if (left) break;
         }
-        if (gw == 0) {  // (after the group's last meeting: all vectors are written)
+        if (gw == 0) {
             values(op, a, row, mine, g, st, slot.col, slot.z, slot.x);
             __syncwarp();
-            if (grad)
-                for (int j = lane; j < n_list; j += 32) {
-                    const int v = slot.col[j];
-                    if (v >= 0) out[v] = E::put(slot.x[j]);
-                }
-            __syncwarp();
+            if (grad) pending = row;
         }
         ph ^= 1u;
         row = next < 0 ? ~next : next;
         live = next >= 0 && next < a.n_rows;
     }
-    if (gt == 0 && *abortp) {  // gave up: let the copies already issued land before the block's memory goes away
+    if (grad && !group_sync<G>(id, *abortp != 0)) {
+        __syncwarp();
+        if (gw == 0 && pending >= 0) write_pending();
+    }
+    if (lane == 0 && *abortp) {  // gave up: let the copies already issued land before the block's memory goes away
         for (int p = 0; p < sh.parts; ++p) {
             const unsigned long long t = global_timer_ns();
             while ((issued >> p & 1u) && !mbar_try_wait(&bd.full[p], phase_of >> p & 1u))
@@ -783,15 +795,18 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
         kern<<<(unsigned)grid, (warps + (ex ? 4 : 3)) * 32, smem, stream>>>(a, op, sh);
         return cudaGetLastError();
     };
-    auto go_groups = [&](auto kern, int G) -> cudaError_t {
+    auto go_groups = [&](auto kern, int G, int batch) -> cudaError_t {
         GroupShape sh{};
         const int lanes = G * 32, all = (int)(row_bytes / 16);
         sh.list = (list + 3) / 4 * 4;
-        sh.part_vecs = ((all + kParts - 1) / kParts + 4 * lanes - 1) / (4 * lanes) * (4 * lanes);
+        // a row in two parts, so that the next row's first half comes while the second is read; with one warp the others hide it, and
+        // one part costs less (65536 rows of 4096 bf16: 304 us, in two 314, in four 320)
+        const int want = G == 1 ? 1 : kParts, unit = lanes * batch;
+        sh.part_vecs = ((all + want - 1) / want + unit - 1) / unit * unit;
         sh.parts = (all + sh.part_vecs - 1) / sh.part_vecs;
         sh.row_bytes = (int)row_bytes;
-        sh.group_bytes = (int)((row_bytes + sizeof(GroupBoard) + sh.list * kSlotEntry + 127) / 128 * 128);
-        sh.groups = std::min((227 * 1024 - 64) / sh.group_bytes, 24 / G);
+        sh.group_bytes = (int)((row_bytes + sizeof(GroupBoard) + 2 * sh.list * kSlotEntry + 127) / 128 * 128);
+        sh.groups = std::min((227 * 1024 - 64) / sh.group_bytes, (G == 1 ? 24 : 16) / G);
         const size_t smem = (size_t)sh.groups * sh.group_bytes;
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
@@ -801,10 +816,12 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
     };
     auto by_type = [&](auto dt) -> cudaError_t {
         constexpr int DT = decltype(dt)::value;
-        if (row_bytes <= 16384) return go_groups(group_kernel<DT, Op, 1>, 1);
-        if (row_bytes <= 32768) return go_groups(group_kernel<DT, Op, 4>, 4);
-        if (row_bytes <= 73728) return go_groups(group_kernel<DT, Op, 4>, 4);
-        if (row_bytes <= 110 * 1024) return go_groups(group_kernel<DT, Op, 8>, 8);
+        // warps for a row: as many as leave at least two groups an SM and each thread two batches (16384 x 8192 bf16 in ones 285 us, in twos
+        // 246; 8192 x 32000 in fours 229, in eights 249)
+        if (row_bytes <= 8192) return go_groups(group_kernel<DT, Op, 1>, 1, kBatch<1>);
+        if (row_bytes <= 32768) return go_groups(group_kernel<DT, Op, 2>, 2, kBatch<2>);
+        if (row_bytes <= 73728) return go_groups(group_kernel<DT, Op, 4>, 4, kBatch<4>);
+        if (row_bytes <= 110 * 1024) return go_groups(group_kernel<DT, Op, 8>, 8, kBatch<8>);
         constexpr size_t b16 = sizeof(Board<16>);
         if (a.grad && row_bytes > 5 * 32768) return go(ring_kernel<DT, Op, 16, 4, 3, 1>, 16, 4, 3, 1, b16, Board<16>::kStages);
         return go(ring_kernel<DT, Op, 16, 4, 0, 1>, 16, 4, 0, 1, b16, Board<16>::kStages);

@@ -472,8 +472,8 @@ cudaError_t launch_rows(const RowsArgs& a, const ClipOp& op, int sm_count, cudaS
 cudaError_t launch_rows(const RowsArgs& a, const DistillOp& op, int sm_count, cudaStream_t stream);
 
 // The statistics of every row, without a gradient: log-probability of the token, log-sum-exp, largest logit; the states too, and the
-// header.  The logits are read once.
-cudaError_t launch_token_stats(const RowsArgs& a, const int32_t* targets, const uint8_t* mask, cudaStream_t stream);
+// header.  The logits are read once; `keep`: they will be read again.
+cudaError_t launch_token_stats(const RowsArgs& a, const int32_t* targets, const uint8_t* mask, bool keep, cudaStream_t stream);
 // The gradient of rows whose statistics are known: coefficient coef[row / seq_len] times softmax less one at the token.
 cudaError_t launch_token_grads(const RowsArgs& a, const int32_t* targets, const double* coef, const Divisor& seq_len, cudaStream_t stream);
 
@@ -487,27 +487,26 @@ cudaError_t launch_prepare_tokens(int n_seq, int seq_len, int vocab, const int32
 
 // The clipped loss of one row and its slope by the log-probability, sign turned: loss' = -slope.
 struct ClipIn {
-    double A, old, ref;
+    float A, old, ref;
 };
 struct ClipTerms {
     double loss, slope, kl;
     bool cut;
 };
 __device__ __forceinline__ ClipIn clip_in(const ClipOp& op, int64_t r) {
-    return ClipIn{(double)op.adv[(op.flags & RAPID_CLIP_ADV_TOKEN) ? r : divide(r, op.seq_len)], (double)op.old_logp[r],
-                  op.ref_logp ? (double)op.ref_logp[r] : 0.0};
+    return ClipIn{op.adv[(op.flags & RAPID_CLIP_ADV_TOKEN) ? r : divide(r, op.seq_len)], op.old_logp[r], op.ref_logp ? op.ref_logp[r] : 0.f};
 }
 __device__ __forceinline__ ClipTerms clip_terms(const ClipOp& op, const ClipIn& in, double lp) {
     ClipTerms t;
-    const double rho = exp2_short((lp - in.old) * kLog2eD);
-    const double u = in.A != 0.0 ? rho * in.A : 0.0;  // A = 0 leaves nothing, even of an infinite ratio
-    const double v = in.A != 0.0 ? fmin(fmax(rho, 1.0 - op.low), 1.0 + op.high) * in.A : 0.0;
+    const double rho = exp2_short((lp - (double)in.old) * kLog2eD), A = (double)in.A;
+    const double u = in.A != 0.f ? rho * A : 0.0;  // A = 0 leaves nothing, even of an infinite ratio
+    const double v = in.A != 0.f ? fmin(fmax(rho, 1.0 - op.low), 1.0 + op.high) * A : 0.0;
     t.cut = v < u;
     t.loss = t.cut ? -v : -u;
     t.slope = t.cut ? 0.0 : u;
     t.kl = 0.0;
     if (op.ref_logp) {
-        const double d = in.ref - lp, e = exp2_short(d * kLog2eD) - 1.0;
+        const double d = (double)in.ref - lp, e = exp2_short(d * kLog2eD) - 1.0;
         t.kl = isinf(e) ? e : e - d;  // off by 1e-15
         if (op.beta != 0.0) {
             t.loss += op.beta * t.kl;
@@ -516,13 +515,10 @@ __device__ __forceinline__ ClipTerms clip_terms(const ClipOp& op, const ClipIn& 
     }
     return t;
 }
-// Weight of a row: what all rows share, once for a kernel (`rows`: how many count), and the rest.
+// The part of the rows' weights that all share, once for a kernel; `rows`: how many count.
 __device__ __forceinline__ double shared_weight(const ClipOp& op, long long rows) {
     if (op.flags & RAPID_LOSS_NORM_GIVEN) return op.scale / op.norm_z;
     return op.scale / ((op.flags & RAPID_LOSS_NORM_SEQ) ? (double)op.n_seq : (double)rows);
-}
-__device__ __forceinline__ double clip_weight(const ClipOp& op, int64_t r, double shared) {
-    return (op.flags & RAPID_LOSS_NORM_SEQ) ? shared / (double)op.seq_rows[divide(r, op.seq_len)] : shared;
 }
 __device__ __forceinline__ double shared_weight(const DistillOp& op, long long rows) {
     return op.scale * op.inv_tau / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows);
@@ -547,10 +543,26 @@ __device__ __forceinline__ float entry(const DistillOp& op, int64_t r, int j) { 
 
 struct ClipRow {
     ClipIn in;
+    int seq_rows;
     double w, lp;
 };
 __device__ __forceinline__ ClipRow look(const ClipOp& op, int64_t r, double shared, const int*, const float*, const float*) {
-    return ClipRow{clip_in(op, r), clip_weight(op, r, shared), 0.0};
+    return ClipRow{clip_in(op, r), (op.flags & RAPID_LOSS_NORM_SEQ) ? op.seq_rows[divide(r, op.seq_len)] : 1, shared, 0.0};
+}
+// A row's arrays, other than its logits, brought near, by one warp a row ahead.
+__device__ __forceinline__ void near_line(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
+__device__ __forceinline__ void bring_near(const ClipOp& op, int64_t r) {
+    const int lane = threadIdx.x & 31;
+    const float* p = lane == 0 ? reinterpret_cast<const float*>(op.targets) : lane == 1 ? op.old_logp : lane == 2 ? op.ref_logp : op.adv;
+    if (lane < 3 + ((op.flags & RAPID_CLIP_ADV_TOKEN) ? 1 : 0) && p) near_line(p + r);
+}
+__device__ __forceinline__ void bring_near(const DistillOp& op, int64_t r) {
+    const int lane = threadIdx.x & 31;
+    if (32 * lane < op.k) {
+        near_line(op.index + r * op.ld + 32 * lane);
+        near_line(op.logit + r * op.ld + 32 * lane);
+    }
+    if (lane == 31) near_line(op.teacher_lse2 + r);
 }
 struct DistillRow {
     double teacher, w;
@@ -580,6 +592,7 @@ __device__ __forceinline__ DistillRow look(const DistillOp& op, int64_t r, doubl
 __device__ __forceinline__ RowGrad finish(const ClipOp& op, const RowsArgs& a, ClipRow& row, const RowStat& st, const int*, const float* z,
                                           const float*) {
     row.lp = ((double)z[0] * a.f.kd - st.lse2) * kLn2D;
+    if (op.flags & RAPID_LOSS_NORM_SEQ) row.w /= (double)row.seq_rows;
     return RowGrad{row.w * clip_terms(op, row.in, row.lp).slope, st.lse2};
 }
 __device__ __forceinline__ void values(const ClipOp&, const RowsArgs& a, int64_t r, const ClipRow& row, const RowGrad& g, const RowStat&,
@@ -658,7 +671,7 @@ __device__ __forceinline__ void add_row(const ClipOp& op, const Totals& t, int64
         const ClipIn in = clip_in(op, r);
         const ClipTerms c = clip_terms(op, in, lp);
         v[0] += (op.flags & RAPID_LOSS_NORM_SEQ) ? c.loss / (double)op.seq_rows[divide(r, op.seq_len)] : c.loss;
-        v[1] += lp - in.old;
+        v[1] += lp - (double)in.old;
         v[2] += c.kl;
         v[3] += c.cut ? 1.0 : 0.0;
         v[4] += 1.0;

@@ -14,7 +14,8 @@ namespace {
 // an SM cover one another's ends.
 constexpr int kStatThreads = 128;
 
-template <int DT, int kGroup>
+// With kKeep the logits stay in L2 as far as they fit, for the gradient's reading.
+template <int DT, int kGroup, bool kKeep>
 __global__ void __launch_bounds__(kStatThreads, 6)
 token_stats_kernel(RowsArgs a, const int32_t* __restrict__ targets, const uint8_t* __restrict__ mask) {
     using E = Elem<DT>;
@@ -37,19 +38,20 @@ token_stats_kernel(RowsArgs a, const int32_t* __restrict__ targets, const uint8_
     const uint4* rv = reinterpret_cast<const uint4*>(row);
     const int nvec = a.vocab / E::kPer;
     const float off = shift_fraction(kGroup == 1 ? 0 : warp);
+    auto load = [](const uint4* at) { return kKeep ? __ldg(at) : ld_stream(at); };
     Part p;
     int v = gt;
     for (; v + (U - 1) * kLanes < nvec; v += U * kLanes) {
         uint4 q[U];
 #pragma unroll
-        for (int j = 0; j < U; ++j) q[j] = ld_stream(rv + v + j * kLanes);
+        for (int j = 0; j < U; ++j) q[j] = load(rv + v + j * kLanes);
         p.template vectors<DT, U>(q, off, a.f);
     }
     if (v - lane < nvec) {  // what is left, up to eight vectors of a thread; behind the row: -inf
         constexpr uint32_t kNone = DT == RAPID_BF16 ? 0xff80ff80u : 0xff800000u;
         uint4 q[U];
 #pragma unroll
-        for (int j = 0; j < U; ++j) q[j] = v + j * kLanes < nvec ? ld_stream(rv + v + j * kLanes) : make_uint4(kNone, kNone, kNone, kNone);
+        for (int j = 0; j < U; ++j) q[j] = v + j * kLanes < nvec ? load(rv + v + j * kLanes) : make_uint4(kNone, kNone, kNone, kNone);
         p.template vectors<DT, U>(q, off, a.f);
     }
     const int e = nvec * E::kPer + gt;
@@ -83,8 +85,9 @@ token_grads_kernel(RowsArgs a, const int32_t* __restrict__ targets, const double
     using E = Elem<DT>;
     using T = typename E::T;
     constexpr int U = 8;
-    const uint32_t piece = blockIdx.x * (kGradThreads / 32) + (threadIdx.x >> 5);
+    uint32_t piece = blockIdx.x * (kGradThreads / 32) + (threadIdx.x >> 5);
     if (piece >= total) return;
+    piece = total - 1 - piece;  // from the end: what the first reading read last may still be in L2
     const int lane = threadIdx.x & 31;
     const uint32_t r = piece / pieces;
     const int first = (int)(piece - r * pieces) * kPiece;  // first vector
@@ -130,7 +133,7 @@ token_grads_kernel(RowsArgs a, const int32_t* __restrict__ targets, const double
 
 }  // namespace
 
-cudaError_t launch_token_stats(const RowsArgs& a, const int32_t* targets, const uint8_t* mask, cudaStream_t stream) {
+cudaError_t launch_token_stats(const RowsArgs& a, const int32_t* targets, const uint8_t* mask, bool keep, cudaStream_t stream) {
     const int64_t row_bytes = (int64_t)a.vocab * (int64_t)elem_size(a.dtype);
     // a warp for a row of up to 16 vectors a lane; longer ones keep four warps' loads in flight
     const bool single = row_bytes <= 8192;
@@ -139,8 +142,12 @@ cudaError_t launch_token_stats(const RowsArgs& a, const int32_t* targets, const 
         kern<<<grid, kStatThreads, 0, stream>>>(a, targets, mask);
         return cudaGetLastError();
     };
-    if (a.dtype == RAPID_BF16) return single ? go(token_stats_kernel<RAPID_BF16, 1>) : go(token_stats_kernel<RAPID_BF16, 4>);
-    return single ? go(token_stats_kernel<RAPID_F32, 1>) : go(token_stats_kernel<RAPID_F32, 4>);
+    auto by_type = [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (keep) return single ? go(token_stats_kernel<DT, 1, true>) : go(token_stats_kernel<DT, 4, true>);
+        return single ? go(token_stats_kernel<DT, 1, false>) : go(token_stats_kernel<DT, 4, false>);
+    };
+    return a.dtype == RAPID_BF16 ? by_type(std::integral_constant<int, RAPID_BF16>{}) : by_type(std::integral_constant<int, RAPID_F32>{});
 }
 
 cudaError_t launch_token_grads(const RowsArgs& a, const int32_t* targets, const double* coef, const Divisor& seq_len, cudaStream_t stream) {

@@ -386,7 +386,7 @@ rapid_status_t rapid_clip_loss(const rapid_clip_desc_t* desc, const void* logits
     int blocks = 0;
     if (dlogits) {
         if (launch_prepare_tokens(d.n_seq, d.seq_len, d.vocab, targets, mask, w, by_seq, &blocks, st) != cudaSuccess) return RAPID_ERR_CUDA;
-    } else if (launch_token_stats(a, targets, mask, st) != cudaSuccess || (by_seq && launch_count_by_seq(d.n_seq, d.seq_len, w, st) != cudaSuccess)) {
+    } else if (launch_token_stats(a, targets, mask, false, st) != cudaSuccess || (by_seq && launch_count_by_seq(d.n_seq, d.seq_len, w, st) != cudaSuccess)) {
         return RAPID_ERR_CUDA;
     }
     const ClipOp op{targets, old_logp, ref_logp, adv, w.seq_rows, w.counts, blocks, d.n_seq, make_divisor(d.seq_len), d.flags, d.eps_low, d.eps_high,
@@ -420,7 +420,7 @@ rapid_status_t rapid_preference_loss(const rapid_pref_desc_t* desc, const void* 
     if ((s = check_device(&sms)) != RAPID_OK) return s;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, make_factor(1.0), w, Totals{}};
-    if (launch_token_stats(a, targets, mask, st) != cudaSuccess) return RAPID_ERR_CUDA;
+    if (launch_token_stats(a, targets, mask, dlogits != nullptr, st) != cudaSuccess) return RAPID_ERR_CUDA;
     const PairArgs pa{pairs, d.n_pairs, d.n_seq, d.seq_len, d.flags, d.beta, d.margin, d.label_smoothing, d.scale, d.norm_z, margins, loss, stats};
     const int all = d.n_pairs <= 4096 && (int64_t)d.n_pairs * d.n_seq <= 1 << 16;  // some ten microseconds of one block at most
     pref_seq_kernel<<<d.n_seq, kThreads, 0, st>>>(pa, ref_logp, token_logp, all, w);
