@@ -448,7 +448,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
     if (tid == 0 && bd.abort_flag) {
         atomicMax(&a.w.head->status, (int)RAPID_ERR_TIMEOUT);
     }
-    if (a.end.last_block) finish_rows(op, a.end, a.n_rows, a.w, reinterpret_cast<double*>(dyn));
+    if (a.end.last_block) finish_rows(op, a, reinterpret_cast<double*>(dyn));
 }
 
 // ---- shorter rows ----------------------------------------------------------------------------------------------
@@ -766,7 +766,7 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
     if (threadIdx.x == 0 && abort_flag) {
         atomicMax(&a.w.head->status, (int)RAPID_ERR_TIMEOUT);
     }
-    if (a.end.last_block) finish_rows(op, a.end, a.n_rows, a.w, reinterpret_cast<double*>(dyn));
+    if (a.end.last_block) finish_rows(op, a, reinterpret_cast<double*>(dyn));
 }
 
 template <class Op>
@@ -823,7 +823,7 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
         if (row_bytes <= 73728) return go_groups(group_kernel<DT, Op, 4>, 4, kBatch<4>);
         if (row_bytes <= 110 * 1024) return go_groups(group_kernel<DT, Op, 8>, 8, kBatch<8>);
         constexpr size_t b16 = sizeof(Board<16>);
-        if (a.grad && row_bytes > 5 * 32768) return go(ring_kernel<DT, Op, 16, 4, 3, 1>, 16, 4, 3, 1, b16, Board<16>::kStages);
+        if (a.grad) return go(ring_kernel<DT, Op, 16, 4, 3, 1>, 16, 4, 3, 1, b16, Board<16>::kStages);
         return go(ring_kernel<DT, Op, 16, 4, 0, 1>, 16, 4, 0, 1, b16, Board<16>::kStages);
     };
     return a.dtype == RAPID_BF16 ? by_type(std::integral_constant<int, RAPID_BF16>{}) : by_type(std::integral_constant<int, RAPID_F32>{});

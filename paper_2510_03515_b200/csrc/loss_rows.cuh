@@ -39,6 +39,13 @@ struct Header {
     int32_t pad;
 };
 
+// A warp's part of a row: its largest logit, its shift, and its sum without that logit's term, which may carry nearly all of the
+// row's probability and is put back exactly where the parts meet.
+struct WarpPart {
+    double s;
+    float m, sh;  // sh = -inf where there is nothing
+};
+
 struct Scratch {
     Header* head;
     int2* counts;         // [kPrepBlocks] rows that count, rows that are not valid
@@ -53,12 +60,21 @@ struct Scratch {
     double* seq_coef;     // [N] g_n
     double* pair_slope;   // [P]
     double* teacher_lse2; // [T]
+    WarpPart* parts;      // [T][pieces] of rows that are read without a gradient
+    float* token_z;       // [T] the token's logit
 };
 
 enum : int { NEED_SEQ = 1, NEED_PAIRS = 2, NEED_TEACHER = 4 };
 
+// Warps that share a row that is read without a gradient: 1024 vectors for each at the least, four at most (with as many as there are
+// 1024 vectors, 19 on 151936 bf16 columns, 8192 rows take 896 us instead of 838).
+inline int stat_pieces(int32_t vocab, int32_t dtype) {
+    const int64_t n = (vocab / (16 / (int64_t)elem_size(dtype)) + 1023) / 1024;
+    return n < 1 ? 1 : n > 4 ? 4 : (int)n;
+}
+
 // Carve `base` (256-byte aligned); returns the bytes used.
-inline size_t carve(int64_t T, int64_t N, int64_t P, int need, void* base, Scratch* out) {
+inline size_t carve(int64_t T, int64_t N, int64_t P, int pieces, int need, void* base, Scratch* out) {
     size_t off = 0;
     char* p = static_cast<char*>(base);
     auto take = [&](size_t bytes) {
@@ -82,6 +98,10 @@ inline size_t carve(int64_t T, int64_t N, int64_t P, int need, void* base, Scrat
         s.pair_slope = reinterpret_cast<double*>(take((size_t)P * 8));
     }
     if (need & NEED_TEACHER) s.teacher_lse2 = reinterpret_cast<double*>(take((size_t)T * 8));
+    if (pieces > 0) {
+        s.parts = reinterpret_cast<WarpPart*>(take((size_t)T * pieces * sizeof(WarpPart)));
+        s.token_z = reinterpret_cast<float*>(take((size_t)T * 4));
+    }
     if (out) *out = s;
     return off;
 }
@@ -301,12 +321,6 @@ __device__ __forceinline__ float warp_top(float v) {
     return r;
 }
 
-// A warp's part, the same in all lanes: its largest logit, its shift, and its sum without that logit's term, which may carry nearly
-// all of the row's probability and is put back exactly where the parts meet.
-struct WarpPart {
-    double s;
-    float m, sh;  // sh = -inf where there is nothing
-};
 __device__ __forceinline__ WarpPart warp_part(const Part& p, const Factor& f) {
     WarpPart w;
     w.m = warp_top(p.m);
@@ -353,6 +367,28 @@ __device__ __forceinline__ RowStat one_part(const WarpPart& p, float off, double
         const double s = fma(p.s, unit, exp2_short((double)p.m * f.kd - (double)n));
         if (s > 0.0) r.lse2 = (double)n + log2_short(s);
     }
+    return r;
+}
+
+// And by one thread, from memory: piece p was taken with the fraction of warp p mod 32.
+__device__ __forceinline__ float shift_fraction(int warp);
+__device__ __forceinline__ RowStat stored_parts(const WarpPart* parts, int pieces, const Factor& f) {
+    RowStat r{-INFINITY, -INFINITY};
+    float top = -INFINITY;
+    for (int p = 0; p < pieces; ++p) {
+        r.max = fmaxf(r.max, parts[p].m);
+        if (parts[p].sh > -INFINITY) top = fmaxf(top, rintf(parts[p].sh - shift_fraction(p & 31)));
+    }
+    double s = 0.0;
+    for (int p = 0; p < pieces; ++p) {
+        const WarpPart q = parts[p];
+        if (!(q.sh > -INFINITY)) continue;
+        const float n = rintf(q.sh - shift_fraction(p & 31));
+        const int down = (int)fminf(top - n, 1000.f);
+        s += fma(q.s, exp2_short((double)q.sh - (double)n) * (1.0 / (1.0 + (double)kEx2Mean)), exp2_short((double)q.m * f.kd - (double)n)) *
+             __hiloint2double((1023 - down) << 20, 0);
+    }
+    if (s > 0.0) r.lse2 = (double)top + log2_short(s);
     return r;
 }
 
@@ -434,8 +470,9 @@ struct Totals {
     float *token, *loss;  // token may be NULL
     rapid_loss_stats_t* stats;
     int last_block;       // few rows: the rows' kernel does it
+    int pieces;           // the rows' statistics are still in so many parts each (0: they are not)
 };
-constexpr int64_t kFewRows = 1024;
+constexpr int64_t kFewRows = 2048;
 
 struct RowsArgs {
     const void* logits;
@@ -471,8 +508,8 @@ struct DistillOp {
 cudaError_t launch_rows(const RowsArgs& a, const ClipOp& op, int sm_count, cudaStream_t stream);
 cudaError_t launch_rows(const RowsArgs& a, const DistillOp& op, int sm_count, cudaStream_t stream);
 
-// The statistics of every row, without a gradient: log-probability of the token, log-sum-exp, largest logit; the states too, and the
-// header.  The logits are read once; `keep`: they will be read again.
+// The parts of every row's statistics and the token's logit, without a gradient; the states too, and the header.  The logits are read
+// once; `keep`: they will be read again.  token_row() makes the statistics of them.
 cudaError_t launch_token_stats(const RowsArgs& a, const int32_t* targets, const uint8_t* mask, bool keep, cudaStream_t stream);
 // The gradient of rows whose statistics are known: coefficient coef[row / seq_len] times softmax less one at the token.
 cudaError_t launch_token_grads(const RowsArgs& a, const int32_t* targets, const double* coef, const Divisor& seq_len, cudaStream_t stream);
@@ -631,6 +668,16 @@ __device__ __forceinline__ void values(const DistillOp& op, const RowsArgs& a, i
     if (lane == 0) a.w.value[r] = loss * kLn2D;
 }
 
+// A row's statistics and its token's log-probability from what the reading without a gradient left of it.
+__device__ __forceinline__ double token_row(const Scratch& w, int64_t r, int pieces, const Factor& f) {
+    const RowStat st = stored_parts(w.parts + r * pieces, pieces, f);
+    const double lp = ((double)w.token_z[r] * f.kd - st.lse2) * kLn2D;
+    w.value[r] = lp;
+    w.lse2[r] = st.lse2;
+    w.row_max[r] = st.max;
+    return lp;
+}
+
 // ---- sums over the rows -------------------------------------------------------------------------------------------
 
 // Sums over the block of N numbers at once, the same in all threads; the order depends on the block's size alone.  `sh` is room for
@@ -663,11 +710,11 @@ __device__ __forceinline__ bool is_last_block(Header* head, bool* sh) {
 
 // loss, mean log-ratio, KL, rows cut, rows that count, rows that are not valid: of one row, added up
 constexpr int kClipSums = 6, kDistillSums = 3;
-__device__ __forceinline__ void add_row(const ClipOp& op, const Totals& t, int64_t r, const Scratch& w, double (&v)[kClipSums]) {
+__device__ __forceinline__ void add_row(const ClipOp& op, const Totals& t, int64_t r, const Scratch& w, const Factor& f, double (&v)[kClipSums]) {
     double lp = 0.0;
     const uint8_t st = w.state[r];
     if (st == ROW_OK) {
-        lp = __ldcg(w.value + r);
+        lp = t.pieces ? token_row(w, r, t.pieces, f) : __ldcg(w.value + r);
         const ClipIn in = clip_in(op, r);
         const ClipTerms c = clip_terms(op, in, lp);
         v[0] += (op.flags & RAPID_LOSS_NORM_SEQ) ? c.loss / (double)op.seq_rows[divide(r, op.seq_len)] : c.loss;
@@ -679,7 +726,7 @@ __device__ __forceinline__ void add_row(const ClipOp& op, const Totals& t, int64
     v[5] += st == ROW_BAD_TOKEN ? 1.0 : 0.0;
     if (t.token) t.token[r] = (float)lp;
 }
-__device__ __forceinline__ void add_row(const DistillOp&, const Totals& t, int64_t r, const Scratch& w, double (&v)[kDistillSums]) {
+__device__ __forceinline__ void add_row(const DistillOp&, const Totals& t, int64_t r, const Scratch& w, const Factor&, double (&v)[kDistillSums]) {
     const uint8_t st = w.state[r];
     const double l = st == ROW_OK ? __ldcg(w.value + r) : 0.0;
     v[0] += l;
@@ -713,10 +760,12 @@ struct SumsOf<DistillOp> {
 // By the last block of the rows' kernel, where there are few rows.
 // `sh`: 2 KB of shared memory.
 template <class Op>
-__device__ __noinline__ void finish_rows(const Op& op, const Totals& t, int64_t n_rows, const Scratch& w, double* sh) {
+__device__ __noinline__ void finish_rows(const Op& op, const RowsArgs& a, double* sh) {
+    const Totals& t = a.end;
+    const Scratch& w = a.w;
     if (!is_last_block(w.head, reinterpret_cast<bool*>(sh + 32 * SumsOf<Op>::kN))) return;
     double v[SumsOf<Op>::kN] = {};
-    for (int64_t r = threadIdx.x; r < n_rows; r += blockDim.x) add_row(op, t, r, w, v);
+    for (int64_t r = threadIdx.x; r < a.n_rows; r += blockDim.x) add_row(op, t, r, w, a.f, v);
     block_sums(v, sh);
     if (threadIdx.x == 0) write_totals(op, t, w, v);
 }

@@ -10,68 +10,51 @@ namespace losses {
 namespace {
 
 // ---- log-probabilities -------------------------------------------------------------------------------------------
-// A row for each warp (kGroup = 1) or block of four (kGroup = 4), eight 16-byte loads of every thread in flight; some six blocks on
-// an SM cover one another's ends.
+// One to four warps for a row; each leaves its part of the row's statistics in memory and is done, without meeting the others.  Whoever needs the row joins the
+// parts, a row for each thread.  Eight 16-byte loads of every lane are in flight.
 constexpr int kStatThreads = 128;
 
 // With kKeep the logits stay in L2 as far as they fit, for the gradient's reading.
-template <int DT, int kGroup, bool kKeep>
+template <int DT, bool kKeep>
 __global__ void __launch_bounds__(kStatThreads, 6)
-token_stats_kernel(RowsArgs a, const int32_t* __restrict__ targets, const uint8_t* __restrict__ mask) {
+token_stats_kernel(RowsArgs a, const int32_t* __restrict__ targets, const uint8_t* __restrict__ mask, uint32_t pieces, uint32_t total) {
     using E = Elem<DT>;
     using T = typename E::T;
-    constexpr int U = 8, kLanes = kGroup * 32;
-    __shared__ WarpPart parts[4];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gt = threadIdx.x % kLanes;
+    constexpr int U = 8;
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.w.head = Header{0u, 0u, RAPID_OK, 0};
-    const int64_t r = (int64_t)blockIdx.x * (4 / kGroup) + warp / kGroup;
-    if (r >= a.n_rows) return;  // the whole block, or warps that meet nobody
+    const uint32_t piece = blockIdx.x * (kStatThreads / 32) + (threadIdx.x >> 5);
+    if (piece >= total) return;
+    const int lane = threadIdx.x & 31;
+    const uint32_t r = pieces == 1 ? piece : piece / pieces, at = piece - r * pieces;
     const int y = targets[r];
     const uint8_t state = mask && !mask[r] ? ROW_MASKED : y >= 0 && y < a.vocab ? ROW_OK : ROW_BAD_TOKEN;
-    if (gt == 0) {
-        a.w.state[r] = state;
-        if (state != ROW_OK) a.w.value[r] = 0.0;
-    }
+    if (at == 0 && lane == 0) a.w.state[r] = state;
     if (state != ROW_OK) return;
-    const T* row = static_cast<const T*>(a.logits) + r * a.ld;
-    const float z = E::get(row[y]);
+    const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.ld;
+    if (at == 0 && lane == 0) a.w.token_z[r] = E::get(row[y]);
     const uint4* rv = reinterpret_cast<const uint4*>(row);
-    const int nvec = a.vocab / E::kPer;
-    const float off = shift_fraction(kGroup == 1 ? 0 : warp);
-    auto load = [](const uint4* at) { return kKeep ? __ldg(at) : ld_stream(at); };
+    const int nvec = a.vocab / E::kPer, lanes = 32 * (int)pieces;  // the row's warps take turns of 32 vectors
+    const float off = shift_fraction(at & 31);
+    auto load = [](const uint4* p) { return kKeep ? __ldg(p) : ld_stream(p); };
     Part p;
-    int v = gt;
-    for (; v + (U - 1) * kLanes < nvec; v += U * kLanes) {
+    int v = (int)at * 32 + lane;
+    for (; v + (U - 1) * lanes < nvec; v += U * lanes) {
         uint4 q[U];
 #pragma unroll
-        for (int j = 0; j < U; ++j) q[j] = load(rv + v + j * kLanes);
+        for (int j = 0; j < U; ++j) q[j] = load(rv + v + j * lanes);
         p.template vectors<DT, U>(q, off, a.f);
     }
-    if (v - lane < nvec) {  // what is left, up to eight vectors of a thread; behind the row: -inf
+    if (v - lane < nvec) {  // what is left, up to eight vectors of a lane; behind the row: -inf
         constexpr uint32_t kNone = DT == RAPID_BF16 ? 0xff80ff80u : 0xff800000u;
         uint4 q[U];
 #pragma unroll
-        for (int j = 0; j < U; ++j) q[j] = v + j * kLanes < nvec ? load(rv + v + j * kLanes) : make_uint4(kNone, kNone, kNone, kNone);
+        for (int j = 0; j < U; ++j) q[j] = v + j * lanes < nvec ? load(rv + v + j * lanes) : make_uint4(kNone, kNone, kNone, kNone);
         p.template vectors<DT, U>(q, off, a.f);
     }
-    const int e = nvec * E::kPer + gt;
-    if (e < a.vocab) p.scalar(E::get(row[e]), off, a.f);
+    const int e = nvec * E::kPer + lane;  // fewer columns than a vector has, behind the last one
+    if (at == pieces - 1 && e < a.vocab) p.scalar(E::get(row[e]), off, a.f);
     const WarpPart w = warp_part(p, a.f);
-    RowStat st;
-    if constexpr (kGroup == 1) {
-        st = one_part(w, off, part_unit(off), a.f);
-    } else {
-        if (lane == 0) parts[warp] = w;
-        __syncthreads();
-        if (warp != 0) return;
-        const float off_l = shift_fraction(lane);
-        st = join_parts(lane < 4 ? parts[lane] : WarpPart{0.0, -INFINITY, -INFINITY}, off_l, part_unit(off_l), a.f);
-    }
-    if (lane == 0) {
-        a.w.value[r] = ((double)z * a.f.kd - st.lse2) * kLn2D;
-        a.w.lse2[r] = st.lse2;
-        a.w.row_max[r] = st.max;
-    }
+    if (lane == 0) a.w.parts[(size_t)r * pieces + at] = w;
 }
 
 // ---- gradients ----------------------------------------------------------------------------------------------------
@@ -134,20 +117,15 @@ token_grads_kernel(RowsArgs a, const int32_t* __restrict__ targets, const double
 }  // namespace
 
 cudaError_t launch_token_stats(const RowsArgs& a, const int32_t* targets, const uint8_t* mask, bool keep, cudaStream_t stream) {
-    const int64_t row_bytes = (int64_t)a.vocab * (int64_t)elem_size(a.dtype);
-    // a warp for a row of up to 16 vectors a lane; longer ones keep four warps' loads in flight
-    const bool single = row_bytes <= 8192;
-    const unsigned grid = (unsigned)(single ? (a.n_rows + 3) / 4 : a.n_rows);
+    const int64_t pieces = stat_pieces(a.vocab, a.dtype), total = pieces * a.n_rows;
+    if (total > 0x7fffffffll) return cudaErrorInvalidValue;  // 34 TB of logits
+    const unsigned grid = (unsigned)((total + kStatThreads / 32 - 1) / (kStatThreads / 32));
     auto go = [&](auto kern) {
-        kern<<<grid, kStatThreads, 0, stream>>>(a, targets, mask);
+        kern<<<grid, kStatThreads, 0, stream>>>(a, targets, mask, (uint32_t)pieces, (uint32_t)total);
         return cudaGetLastError();
     };
-    auto by_type = [&](auto dt) {
-        constexpr int DT = decltype(dt)::value;
-        if (keep) return single ? go(token_stats_kernel<DT, 1, true>) : go(token_stats_kernel<DT, 4, true>);
-        return single ? go(token_stats_kernel<DT, 1, false>) : go(token_stats_kernel<DT, 4, false>);
-    };
-    return a.dtype == RAPID_BF16 ? by_type(std::integral_constant<int, RAPID_BF16>{}) : by_type(std::integral_constant<int, RAPID_F32>{});
+    if (a.dtype == RAPID_BF16) return keep ? go(token_stats_kernel<RAPID_BF16, true>) : go(token_stats_kernel<RAPID_BF16, false>);
+    return keep ? go(token_stats_kernel<RAPID_F32, true>) : go(token_stats_kernel<RAPID_F32, false>);
 }
 
 cudaError_t launch_token_grads(const RowsArgs& a, const int32_t* targets, const double* coef, const Divisor& seq_len, cudaStream_t stream) {

@@ -41,6 +41,26 @@ prepare_tokens_kernel(int64_t n_rows, int vocab, const int32_t* __restrict__ tar
     write_counts(live, bad, w);
 }
 
+// The same, a generation for each block, whose rows that count are noted too.
+__global__ void __launch_bounds__(kThreads)
+prepare_by_seq_kernel(int seq_len, int vocab, const int32_t* __restrict__ targets, const uint8_t* __restrict__ mask, Scratch w) {
+    clear_header(w);
+    const int64_t base = (int64_t)blockIdx.x * seq_len;
+    int live = 0, bad = 0;
+    for (int t = threadIdx.x; t < seq_len; t += kThreads) {
+        uint8_t st = ROW_MASKED;
+        if (!mask || mask[base + t]) {
+            const int32_t y = targets[base + t];
+            st = (y >= 0 && y < vocab) ? ROW_OK : ROW_BAD_TOKEN;
+        }
+        w.state[base + t] = st;
+        live += st == ROW_OK;
+        bad += st == ROW_BAD_TOKEN;
+    }
+    write_counts(live, bad, w);
+    if (threadIdx.x == 0) w.seq_rows[blockIdx.x] = w.counts[blockIdx.x].x;
+}
+
 // Rows that count of every generation: one block of 32 or 256 threads each.
 __global__ void __launch_bounds__(kThreads) count_by_seq_kernel(int seq_len, Scratch w) {
     const uint8_t* st = w.state + (int64_t)blockIdx.x * seq_len;
@@ -148,12 +168,12 @@ cudaError_t launch_prepare_lists(const rapid_distill_desc_t& d, double kd, const
 
 // Many rows: the sums by blocks, and by the last of them over all.
 template <class Op>
-__global__ void __launch_bounds__(kThreads) sum_rows_kernel(Op op, Totals t, int64_t n_rows, Scratch w) {
+__global__ void __launch_bounds__(kThreads) sum_rows_kernel(Op op, Totals t, int64_t n_rows, Factor f, Scratch w) {
     constexpr int N = SumsOf<Op>::kN;
     __shared__ bool last;
     __shared__ double sh[32 * N];
     double v[N] = {};
-    for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < n_rows; r += (int64_t)gridDim.x * kThreads) add_row(op, t, r, w, v);
+    for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < n_rows; r += (int64_t)gridDim.x * kThreads) add_row(op, t, r, w, f, v);
     block_sums(v, sh);
     if (threadIdx.x == 0)
 #pragma unroll
@@ -168,9 +188,9 @@ __global__ void __launch_bounds__(kThreads) sum_rows_kernel(Op op, Totals t, int
     if (threadIdx.x == 0) write_totals(op, t, w, v);
 }
 template <class Op>
-cudaError_t launch_sums(const Op& op, const Totals& t, int64_t n_rows, const Scratch& w, cudaStream_t st) {
-    const int64_t b = (n_rows + kThreads - 1) / kThreads;
-    sum_rows_kernel<<<(unsigned)(b < kSumBlocks ? b : kSumBlocks), kThreads, 0, st>>>(op, t, n_rows, w);
+cudaError_t launch_sums(const Op& op, const RowsArgs& a, cudaStream_t st) {
+    const int64_t b = (a.n_rows + kThreads - 1) / kThreads;
+    sum_rows_kernel<<<(unsigned)(b < kSumBlocks ? b : kSumBlocks), kThreads, 0, st>>>(op, a.end, a.n_rows, a.f, a.w);
     return cudaGetLastError();
 }
 
@@ -246,7 +266,7 @@ __device__ __forceinline__ void coefficient(const PairArgs& a, const Scratch& w,
 // One block for each generation: its sum of log-ratios.  Where there is little to do (`all`) the last one goes on to the pairs and
 // the coefficients, which saves a call with few rows two launches.
 __global__ void __launch_bounds__(kThreads)
-pref_seq_kernel(PairArgs a, const float* __restrict__ ref_logp, float* __restrict__ token_logp, int all, Scratch w) {
+pref_seq_kernel(PairArgs a, const float* __restrict__ ref_logp, float* __restrict__ token_logp, int all, int pieces, Factor f, Scratch w) {
     __shared__ bool last;
     const int64_t base = (int64_t)blockIdx.x * a.seq_len;
     __shared__ double sh[32 * 3];
@@ -256,7 +276,7 @@ pref_seq_kernel(PairArgs a, const float* __restrict__ ref_logp, float* __restric
         const uint8_t st = w.state[r];
         double lp = 0.0;
         if (st == ROW_OK) {
-            lp = w.value[r];
+            lp = token_row(w, r, pieces, f);
             v[0] += ref_logp ? lp - (double)ref_logp[r] : lp;
             v[1] += 1.0;
         }
@@ -294,6 +314,11 @@ cudaError_t launch_count_by_seq(int n_seq, int seq_len, const Scratch& w, cudaSt
 
 cudaError_t launch_prepare_tokens(int n_seq, int seq_len, int vocab, const int32_t* targets, const uint8_t* mask, const Scratch& w,
                                   int by_seq, int* blocks, cudaStream_t stream) {
+    if (by_seq && n_seq <= kPrepBlocks) {  // one launch instead of two
+        *blocks = n_seq;
+        prepare_by_seq_kernel<<<n_seq, kThreads, 0, stream>>>(seq_len, vocab, targets, mask, w);
+        return cudaGetLastError();
+    }
     const int64_t T = (int64_t)n_seq * seq_len, b = (T + kThreads - 1) / kThreads;
     *blocks = (int)(b < kPrepBlocks ? b : kPrepBlocks);
     prepare_tokens_kernel<<<*blocks, kThreads, 0, stream>>>(T, vocab, targets, mask, w);
@@ -322,7 +347,7 @@ rapid_status_t check_clip(const rapid_clip_desc_t* d) {
                        RAPID_LOSS_NORM_SEQ | RAPID_LOSS_NORM_GIVEN | RAPID_CLIP_ADV_TOKEN, d->scale, d->norm_z);
 }
 size_t carve_clip(const rapid_clip_desc_t& d, void* base, Scratch* w) {
-    return carve((int64_t)d.n_seq * d.seq_len, d.n_seq, 0, (d.flags & RAPID_LOSS_NORM_SEQ) ? NEED_SEQ : 0, base, w);
+    return carve((int64_t)d.n_seq * d.seq_len, d.n_seq, 0, stat_pieces(d.vocab, d.dtype), (d.flags & RAPID_LOSS_NORM_SEQ) ? NEED_SEQ : 0, base, w);
 }
 
 rapid_status_t check_pref(const rapid_pref_desc_t* d) {
@@ -338,7 +363,7 @@ rapid_status_t check_pref(const rapid_pref_desc_t* d) {
     return d->n_pairs > (1 << 20) ? RAPID_ERR_UNSUPPORTED : RAPID_OK;
 }
 size_t carve_pref(const rapid_pref_desc_t& d, void* base, Scratch* w) {
-    return carve((int64_t)d.n_seq * d.seq_len, d.n_seq, d.n_pairs, NEED_SEQ | NEED_PAIRS, base, w);
+    return carve((int64_t)d.n_seq * d.seq_len, d.n_seq, d.n_pairs, stat_pieces(d.vocab, d.dtype), NEED_SEQ | NEED_PAIRS, base, w);
 }
 
 rapid_status_t check_distill(const rapid_distill_desc_t* d) {
@@ -349,7 +374,7 @@ rapid_status_t check_distill(const rapid_distill_desc_t* d) {
     if (d->k > kMaxList || d->ld_top > (1ll << 56) / d->n_rows) return RAPID_ERR_UNSUPPORTED;
     return d->temperature < 1e-3 || d->temperature > 1e3 ? RAPID_ERR_UNSUPPORTED : RAPID_OK;
 }
-size_t carve_distill(const rapid_distill_desc_t& d, void* base, Scratch* w) { return carve(d.n_rows, 0, 0, NEED_TEACHER, base, w); }
+size_t carve_distill(const rapid_distill_desc_t& d, void* base, Scratch* w) { return carve(d.n_rows, 0, 0, 0, NEED_TEACHER, base, w); }
 
 inline rapid_status_t cuda_status(cudaError_t e) { return e == cudaSuccess ? RAPID_OK : RAPID_ERR_CUDA; }
 
@@ -381,7 +406,7 @@ rapid_status_t rapid_clip_loss(const rapid_clip_desc_t* desc, const void* logits
     if ((s = check_device(&sms)) != RAPID_OK) return s;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool by_seq = (d.flags & RAPID_LOSS_NORM_SEQ) != 0;
-    const Totals end{token_logp, loss, stats, dlogits && T <= kFewRows};
+    const Totals end{token_logp, loss, stats, dlogits && T <= kFewRows, dlogits ? 0 : stat_pieces(d.vocab, d.dtype)};
     const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, make_factor(1.0), w, end};
     int blocks = 0;
     if (dlogits) {
@@ -392,7 +417,7 @@ rapid_status_t rapid_clip_loss(const rapid_clip_desc_t* desc, const void* logits
     const ClipOp op{targets, old_logp, ref_logp, adv, w.seq_rows, w.counts, blocks, d.n_seq, make_divisor(d.seq_len), d.flags, d.eps_low, d.eps_high,
                     d.kl_beta, d.scale, d.norm_z};
     if (dlogits && launch_rows(a, op, sms, st) != cudaSuccess) return RAPID_ERR_CUDA;
-    return end.last_block ? RAPID_OK : cuda_status(launch_sums(op, end, T, w, st));
+    return end.last_block ? RAPID_OK : cuda_status(launch_sums(op, a, st));
 }
 
 rapid_status_t rapid_preference_loss_workspace_bytes(const rapid_pref_desc_t* desc, size_t* bytes) {
@@ -423,7 +448,7 @@ rapid_status_t rapid_preference_loss(const rapid_pref_desc_t* desc, const void* 
     if (launch_token_stats(a, targets, mask, dlogits != nullptr, st) != cudaSuccess) return RAPID_ERR_CUDA;
     const PairArgs pa{pairs, d.n_pairs, d.n_seq, d.seq_len, d.flags, d.beta, d.margin, d.label_smoothing, d.scale, d.norm_z, margins, loss, stats};
     const int all = d.n_pairs <= 4096 && (int64_t)d.n_pairs * d.n_seq <= 1 << 16;  // some ten microseconds of one block at most
-    pref_seq_kernel<<<d.n_seq, kThreads, 0, st>>>(pa, ref_logp, token_logp, all, w);
+    pref_seq_kernel<<<d.n_seq, kThreads, 0, st>>>(pa, ref_logp, token_logp, all, stat_pieces(d.vocab, d.dtype), a.f, w);
     if (!all) {
         pref_pairs_kernel<<<1, kPairThreads, 0, st>>>(pa, w);
         if (dlogits) pref_coef_kernel<<<(unsigned)(((int64_t)d.n_seq + kWarps - 1) / kWarps), kThreads, 0, st>>>(pa, w);
@@ -459,10 +484,10 @@ rapid_status_t rapid_distill_loss(const rapid_distill_desc_t* desc, const void* 
     if (launch_prepare_lists(d, f.kd, top_index, top_logit, top_lse, mask, w, &blocks, st) != cudaSuccess) return RAPID_ERR_CUDA;
     const DistillOp op{top_index, top_logit, w.teacher_lse2, w.counts, d.ld_top, d.k, top_lse != nullptr, blocks, d.flags, 1.0 / d.temperature,
                        d.scale, d.norm_z, f.kd};
-    const Totals end{token_loss, loss, stats, d.n_rows <= kFewRows};
+    const Totals end{token_loss, loss, stats, d.n_rows <= kFewRows, 0};
     const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, d.n_rows, d.vocab, d.dtype, f, w, end};
     if (launch_rows(a, op, sms, st) != cudaSuccess) return RAPID_ERR_CUDA;
-    return end.last_block ? RAPID_OK : cuda_status(launch_sums(op, end, d.n_rows, w, st));
+    return end.last_block ? RAPID_OK : cuda_status(launch_sums(op, a, st));
 }
 
 }  // extern "C"
