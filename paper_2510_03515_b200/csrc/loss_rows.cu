@@ -30,25 +30,26 @@ struct RingShape {
     unsigned long long stride;
 };
 
-// Shared memory of one row's chosen columns: column, logit, value.
+// Shared memory of one row's chosen columns: column, and logit or later value.
 struct Slot {
     int* col;
-    float *z, *x;
+    float* z;
 };
-constexpr int kSlotEntry = 12;  // bytes of one of them
+constexpr int kSlotEntry = 8;  // bytes of one of them
 __device__ __forceinline__ Slot slot_at(uint8_t* base, int list) {
     float* p = reinterpret_cast<float*>(base);
-    return Slot{reinterpret_cast<int*>(p), p + list, p + 2 * list};
+    return Slot{reinterpret_cast<int*>(p), p + list};
 }
 
 // What the warps of a block tell each other, behind the stages in shared memory.
 template <int kWarps>
 struct Board {
-    static constexpr int kStages = kWarps >= 16 ? 8 : 16;  // at most
+    static constexpr int kStages = kWarps >= 16 ? 9 : 16;  // at most
     static constexpr int kQueue = kStages + 4;             // rows that are known to the block at a time, at most
     static constexpr int kZeros = 4;                       // rows that wait for their zeros
+    static constexpr int kSlots = 3;                       // rows whose chosen columns are held
     uint64_t full[kStages], ready[kStages], empty[kStages], row[kQueue];
-    uint64_t list[2], parts_in[2], grad[2], value[2], zero_full[kZeros], zero_empty[kZeros];
+    uint64_t list[kSlots], value[kSlots], parts_in[2], grad[2], zero_full[kZeros], zero_empty[kZeros];
     long long row_q[kQueue], zero_q[kZeros];
     WarpPart parts[2][kWarps];
     GradConst grads[2];
@@ -63,6 +64,12 @@ __device__ __forceinline__ void bulk_load_once(void* smem_dst, const void* gsrc,
 __device__ __forceinline__ uint64_t policy_first() {
     uint64_t p;
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+
+__device__ __forceinline__ uint64_t policy_normal() {
+    uint64_t p;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
     return p;
 }
 
@@ -83,7 +90,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
     constexpr int kLanes = kWarps * 32;          // consumer threads
     constexpr int kChunkVecs = kLanes * kVecs;   // vectors of a chunk
     constexpr int kChunk = kChunkVecs * 16;
-    constexpr int kQueue = Board<kWarps>::kQueue, kZeros = Board<kWarps>::kZeros;
+    constexpr int kQueue = Board<kWarps>::kQueue, kZeros = Board<kWarps>::kZeros, kSlots = Board<kWarps>::kSlots;
     extern __shared__ __align__(128) uint8_t dyn[];
     uint8_t* ring = dyn;
     Board<kWarps>& bd = *reinterpret_cast<Board<kWarps>*>(dyn + (size_t)sh.stages * kChunk);
@@ -103,9 +110,11 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
             mbar_init(&bd.zero_empty[q], 1);
         }
         for (int s = 0; s < 2; ++s) {
-            mbar_init(&bd.list[s], 1);
             mbar_init(&bd.parts_in[s], kWarps);
             mbar_init(&bd.grad[s], 1);
+        }
+        for (int s = 0; s < kSlots; ++s) {
+            mbar_init(&bd.list[s], 1);
             mbar_init(&bd.value[s], 1);
         }
         bd.abort_flag = 0;
@@ -121,17 +130,17 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
     if (warp == kWarps) {
         // ------------------------------- producer -------------------------------------------
         const int load_bytes = (nvec + (rest ? 1 : 0)) * 16;  // inside the row: its pitch is a multiple of 16 bytes
-        const uint64_t first = policy_first();
+        const uint64_t first = policy_first(), normal = policy_normal();
         uint32_t it = 0, q = 0, zq = 0;
         bool ok = true;
-        auto load = [&](const uint8_t* src, int c) {  // chunk c into the next stage
+        auto load = [&](const uint8_t* src, int c, bool more) {  // chunk c into the next stage; `more`: it will be read again
             const int s = it % sh.stages;
             const uint32_t use = it / sh.stages;
             if (use > 0 && !warp_wait(&bd.empty[s], (use & 1u) ^ 1u, abortp)) return false;
             if (lane == 0) {
                 const int bytes = min(kChunk, load_bytes - c * kChunk);
                 mbar_arrive_expect_tx(&bd.full[s], (uint32_t)bytes);
-                bulk_load_once(ring + (size_t)s * kChunk, src + (size_t)c * kChunk, (uint32_t)bytes, &bd.full[s], first);
+                bulk_load_once(ring + (size_t)s * kChunk, src + (size_t)c * kChunk, (uint32_t)bytes, &bd.full[s], more ? normal : first);
             }
             ++it;
             return true;
@@ -175,8 +184,8 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
                 }
                 const uint8_t* src = static_cast<const uint8_t*>(a.logits) + (size_t)r * a.ld * sizeof(T);
                 publish(r);
-                for (int c = 0; c < sh.chunks && ok; ++c) ok = load(src, c);
-                for (int c = keep; c < keep + sh.again && ok; ++c) ok = load(src, c);
+                for (int c = 0; c < sh.chunks && ok; ++c) ok = load(src, c, c >= keep && c < keep + sh.again);
+                for (int c = keep; c < keep + sh.again && ok; ++c) ok = load(src, c, false);
             }
         }
         if (ok) publish(-1);
@@ -204,76 +213,78 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
             if (lane < rest) out[nvec * E::kPer + lane] = E::put(0.f);
         }
     } else if (warp == kWarps + 3) {
-        // ------------------------------- takes the list's columns out of the sum -------------
-        if (exclude(op)) {
-            int st = 0;
-            uint32_t ph = 0;
-            bool ok = true;
-            for (uint32_t jq = 0; ok; ++jq) {
-                if (!warp_wait(&bd.row[jq % kQueue], (jq / kQueue) & 1u, abortp)) break;
-                if (bd.row_q[jq % kQueue] < 0) break;
-                if (!warp_wait(&bd.list[jq & 1], (jq >> 1) & 1u, abortp)) break;
-                const Slot slot = slot_at(slots + (jq & 1) * slot_bytes, sh.list);
-                // chunks loaded again come without: what is written for these columns is written over
-                for (int c = 0; c < sh.chunks + sh.again && ok; ++c) {
-                    if (!(ok = warp_wait(&bd.full[st], ph, abortp))) break;
-                    if (c < sh.chunks) {
-                        T* e = reinterpret_cast<T*>(ring + (size_t)st * kChunk);
-                        bool wrote = false;
-                        for (int j = lane; j < sh.list; j += 32) {
-                            const unsigned at = (unsigned)(slot.col[j] - c * kChunkVecs * E::kPer);
-                            if (at < (unsigned)(kChunkVecs * E::kPer)) {
-                                e[at] = E::put(-INFINITY);
-                                wrote = true;
-                            }
+        // ------------------------------- a row's chosen columns, ahead of the others --------
+        const int n = list_size(op);
+        const bool ex = exclude(op);
+        int st = 0;
+        uint32_t ph = 0;
+        bool ok = true;
+        for (uint32_t jq = 0; ok; ++jq) {
+            if (!warp_wait(&bd.row[jq % kQueue], (jq / kQueue) & 1u, abortp)) break;
+            const int64_t r = bd.row_q[jq % kQueue];
+            if (r < 0) break;
+            const int s = jq % kSlots;
+            // the row that had the slot, three ago, is done with: the values of the next one follow its sums, which the consumers give
+            // when they have left the row before
+            if (jq >= kSlots && !warp_wait(&bd.value[(jq - 2) % kSlots], (jq - 2) / kSlots & 1u, abortp)) break;
+            const Slot slot = slot_at(slots + s * slot_bytes, sh.list);
+            const T* row = static_cast<const T*>(a.logits) + r * a.ld;
+            for (int j = lane; j < sh.list; j += 32) {
+                const int v = j < n ? column(op, r, j) : -1;
+                if (v >= 0) slot.z[j] = E::get(row[v]);
+                slot.col[j] = v;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bd.list[s]);
+            if (!ex) continue;
+            // the list's columns are taken out of the sum; chunks loaded again come without: what is written for these columns is
+            // written over
+            for (int c = 0; c < sh.chunks + sh.again; ++c) {
+                if (!(ok = warp_wait(&bd.full[st], ph, abortp))) break;
+                if (c < sh.chunks) {
+                    T* e = reinterpret_cast<T*>(ring + (size_t)st * kChunk);
+                    bool wrote = false;
+                    for (int j = lane; j < sh.list; j += 32) {
+                        const unsigned at = (unsigned)(slot.col[j] - c * kChunkVecs * E::kPer);
+                        if (at < (unsigned)(kChunkVecs * E::kPer)) {
+                            e[at] = E::put(-INFINITY);
+                            wrote = true;
                         }
-                        if (wrote) fence_proxy_async_smem();  // a bulk copy writes this stage next
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&bd.ready[st]);
                     }
-                    if (++st == sh.stages) {
-                        st = 0;
-                        ph ^= 1u;
-                    }
+                    if (wrote) fence_proxy_async_smem();  // a bulk copy writes this stage next
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bd.ready[st]);
+                }
+                if (++st == sh.stages) {
+                    st = 0;
+                    ph ^= 1u;
                 }
             }
         }
     } else if (warp == kWarps + 1) {
         // ------------------------------- once a row -----------------------------------------
         const double shared = shared_weight(op, rows_that_count(op_counts(op), op_blocks(op)));
-        const int n = list_size(op);
         const float off = shift_fraction(lane);  // of consumer warp `lane`
         const double unit = part_unit(off);
         for (uint32_t jq = 0;; ++jq) {
             if (!warp_wait(&bd.row[jq % kQueue], (jq / kQueue) & 1u, abortp)) break;
             const int64_t r = bd.row_q[jq % kQueue];
             if (r < 0) break;
-            const int s = jq & 1;
+            const int s = jq & 1, slot_i = jq % kSlots;
             const uint32_t ph = (jq >> 1) & 1u;
-            // (the consumers are through with this slot's last row, the one before the last: the last row's sums are all in)
-            const Slot slot = slot_at(slots + s * slot_bytes, sh.list);
-            const T* row = static_cast<const T*>(a.logits) + r * a.ld;
-            for (int j = lane; j < sh.list; j += 32) {
-                const int v = j < n ? column(op, r, j) : -1;
-                if (v >= 0) {
-                    slot.z[j] = E::get(row[v]);
-                    slot.x[j] = entry(op, r, j);
-                }
-                slot.col[j] = v;
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bd.list[s]);
-            auto mine = look(op, r, shared, slot.col, slot.z, slot.x);
+            const Slot slot = slot_at(slots + slot_i * slot_bytes, sh.list);
+            if (!warp_wait(&bd.list[slot_i], jq / kSlots & 1u, abortp)) break;
+            auto mine = look(op, r, shared, slot.col, slot.z);
             if (!warp_wait(&bd.parts_in[s], ph, abortp)) break;
             const RowStat st = join_parts(lane < kWarps ? bd.parts[s][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, off, unit, a.f);
-            const RowGrad g = finish(op, a, mine, st, slot.col, slot.z, slot.x);
+            const RowGrad g = finish(op, a, mine, st, slot.col, slot.z);
             if (lane == 0) {
                 bd.grads[s] = grad_const<DT>(g, st.max, a.f);
                 mbar_arrive(&bd.grad[s]);
             }
-            values(op, a, r, mine, g, st, slot.col, slot.z, slot.x);
+            values(op, a, r, mine, g, st, slot.col, slot.z);
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bd.value[s]);
+            if (lane == 0) mbar_arrive(&bd.value[slot_i]);
         }
     } else {
         // ------------------------------- consumers ------------------------------------------
@@ -324,9 +335,9 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
             if (!warp_wait(&bd.row[jq % kQueue], (jq / kQueue) & 1u, abortp)) break;
             const int64_t r = bd.row_q[jq % kQueue];
             if (r < 0) break;
-            const int slot_i = jq & 1;
+            const int slot_i = jq & 1;  // of the sums and the factor
             const uint32_t sph = (jq >> 1) & 1u;
-            const Slot slot = slot_at(slots + slot_i * slot_bytes, sh.list);
+            const Slot slot = slot_at(slots + jq % kSlots * slot_bytes, sh.list);
             bool ok = true;
             uint4 kept[kKeep > 0 ? kKeep : 1][kVecs];
             int held = 0;  // stage of the first chunk that stays
@@ -435,11 +446,11 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
             bool mine = false;
             for (int j = lane; j < sh.list; j += 32) mine |= slot.col[j] >= 0 && slot.col[j] / E::kPer % kLanes / 32 == warp;
             if (__any_sync(0xffffffffu, mine)) {
-                if (!warp_wait(&bd.value[slot_i], sph, abortp)) break;
+                if (!warp_wait(&bd.value[jq % kSlots], jq / kSlots & 1u, abortp)) break;
                 __syncwarp();
                 for (int j = lane; j < sh.list; j += 32) {
                     const int v = slot.col[j];
-                    if (v >= 0 && v / E::kPer % kLanes / 32 == warp) out[v] = E::put(slot.x[j]);
+                    if (v >= 0 && v / E::kPer % kLanes / 32 == warp) out[v] = E::put(slot.z[j]);
                 }
             }
         }
@@ -565,7 +576,7 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
         T* out = static_cast<T*>(a.grad) + pending * a.ld_grad;
         for (int j = lane; j < n_list; j += 32) {
             const int v = old.col[j];
-            if (v >= 0) out[v] = E::put(old.x[j]);
+            if (v >= 0) out[v] = E::put(old.z[j]);
         }
         pending = -1;
     };
@@ -603,7 +614,6 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
             for (int j = lane; j < n_list; j += 32) {
                 const int v = column(op, row, j);
                 slot.col[j] = v;
-                if (v >= 0) slot.x[j] = entry(op, row, j);
             }
         if (!grad) announce();
         // vector `at` of the row; columns behind the last read as -inf
@@ -693,7 +703,7 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
             if (group_sync<G>(id, !ok)) break;
             if (gw == 0) st = join_parts(lane < G ? bd.parts[ph][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, unit_off, unit, a.f);
         }
-        decltype(look(op, row, shared, slot.col, slot.z, slot.x)) mine{};
+        decltype(look(op, row, shared, slot.col, slot.z)) mine{};
         RowGrad g{0.0, 0.0};
         if (gw == 0) {
             if (!ex && grad)
@@ -702,8 +712,8 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
                     if (v >= 0) slot.z[j] = E::get(reinterpret_cast<const T*>(place)[v]);
                 }
             __syncwarp();
-            mine = look(op, row, shared, slot.col, slot.z, slot.x);
-            g = finish(op, a, mine, st, slot.col, slot.z, slot.x);
+            mine = look(op, row, shared, slot.col, slot.z);
+            g = finish(op, a, mine, st, slot.col, slot.z);
             if (lane == 0) bd.grad = grad_const<DT>(g, st.max, a.f);
             if (grad) announce();
         }
@@ -712,7 +722,6 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
             if (group_sync<G>(id, !ok)) break;
             __syncwarp();
             next = bd.next[turn & 1];
-            if (gw == G - 1 && next >= 0 && next < a.n_rows) bring_near(op, next);
             if (gw == 0 && pending >= 0) write_pending();
             const Grad<DT> gr(bd.grad, a.f);
             uint4* ov = reinterpret_cast<uint4*>(out);
@@ -743,7 +752,7 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
             }
         }
         if (gw == 0) {
-            values(op, a, row, mine, g, st, slot.col, slot.z, slot.x);
+            values(op, a, row, mine, g, st, slot.col, slot.z);
             __syncwarp();
             if (grad) pending = row;
         }
@@ -777,7 +786,7 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
         RingShape sh{};
         const int chunk = warps * 32 * vecs * 16;
         sh.list = (list + 3) / 4 * 4;
-        const size_t extra = board + 2 * (size_t)sh.list * kSlotEntry;
+        const size_t extra = board + 3 * (size_t)sh.list * kSlotEntry;
         // 228 KB an SM, of which 1 KB for each block is the system's; 227 KB a block
         const size_t room = std::min((size_t)227 * 1024, (size_t)228 * 1024 / blocks - 1024) - extra;
         sh.stages = std::min((int)(room / chunk), most);
@@ -792,7 +801,7 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
         if (sh.batch > 8) sh.batch = 8;
         if (grid > a.n_rows) grid = a.n_rows;
         sh.stride = scatter_stride(a.n_rows);
-        kern<<<(unsigned)grid, (warps + (ex ? 4 : 3)) * 32, smem, stream>>>(a, op, sh);
+        kern<<<(unsigned)grid, (warps + 4) * 32, smem, stream>>>(a, op, sh);
         return cudaGetLastError();
     };
     auto go_groups = [&](auto kern, int G, int batch) -> cudaError_t {
@@ -823,7 +832,11 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
         if (row_bytes <= 73728) return go_groups(group_kernel<DT, Op, 4>, 4, kBatch<4>);
         if (row_bytes <= 110 * 1024) return go_groups(group_kernel<DT, Op, 8>, 8, kBatch<8>);
         constexpr size_t b16 = sizeof(Board<16>);
-        if (a.grad) return go(ring_kernel<DT, Op, 16, 4, 3, 1>, 16, 4, 3, 1, b16, Board<16>::kStages);
+        if (a.grad && row_bytes <= 172 * 1024) return go(ring_kernel<DT, Op, 8, 4, 2, 2>, 8, 4, 2, 2, sizeof(Board<8>), Board<8>::kStages);
+        // Lists need room beside the stages: chunks of 24 KB leave it, seven of 32 KB do not (16 x 512 rows of 151936 with 128 entries 844 us,
+        // with a chunk that has to be loaded again 1174); without lists 32 KB cost a little less (4096 rows: 462, 469).
+        constexpr int kV = std::is_same<Op, DistillOp>::value ? 3 : 4, kK = 7 - kV;
+        if (a.grad) return go(ring_kernel<DT, Op, 16, kV, kK, 1>, 16, kV, kK, 1, b16, Board<16>::kStages);
         return go(ring_kernel<DT, Op, 16, 4, 0, 1>, 16, 4, 0, 1, b16, Board<16>::kStages);
     };
     return a.dtype == RAPID_BF16 ? by_type(std::integral_constant<int, RAPID_BF16>{}) : by_type(std::integral_constant<int, RAPID_F32>{});

@@ -564,7 +564,7 @@ __device__ __forceinline__ double shared_weight(const DistillOp& op, long long r
 // What an operator does with a row, by one warp.  look() does, ahead of time, what needs no sums over the row; finish() gives the
 // factor once the row's log-sum-exp is there (without the chosen columns where exclude() says so), and is what the row's second
 // reading waits for; values() gives the chosen columns' gradient and writes what is kept of the row to the scratch.  col[j] and
-// z[j] are the chosen columns and their logits; x[j], for distillation the teacher's logits, become the columns' gradient.
+// z[j] are the chosen columns and their logits; z[j] become the columns' gradient.
 __device__ __forceinline__ int list_size(const ClipOp&) { return 1; }
 __device__ __forceinline__ int list_size(const DistillOp& op) { return op.k; }
 __device__ __forceinline__ const int2* op_counts(const ClipOp& op) { return op.counts; }
@@ -575,31 +575,14 @@ __device__ __forceinline__ bool exclude(const ClipOp&) { return false; }
 __device__ __forceinline__ bool exclude(const DistillOp& op) { return op.tail != 0; }
 __device__ __forceinline__ int column(const ClipOp& op, int64_t r, int) { return op.targets[r]; }
 __device__ __forceinline__ int column(const DistillOp& op, int64_t r, int j) { return op.index[r * op.ld + j]; }
-__device__ __forceinline__ float entry(const ClipOp&, int64_t, int) { return 0.f; }
-__device__ __forceinline__ float entry(const DistillOp& op, int64_t r, int j) { return op.logit[r * op.ld + j]; }
 
 struct ClipRow {
     ClipIn in;
     int seq_rows;
     double w, lp;
 };
-__device__ __forceinline__ ClipRow look(const ClipOp& op, int64_t r, double shared, const int*, const float*, const float*) {
+__device__ __forceinline__ ClipRow look(const ClipOp& op, int64_t r, double shared, const int*, const float*) {
     return ClipRow{clip_in(op, r), (op.flags & RAPID_LOSS_NORM_SEQ) ? op.seq_rows[divide(r, op.seq_len)] : 1, shared, 0.0};
-}
-// A row's arrays, other than its logits, brought near, by one warp a row ahead.
-__device__ __forceinline__ void near_line(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
-__device__ __forceinline__ void bring_near(const ClipOp& op, int64_t r) {
-    const int lane = threadIdx.x & 31;
-    const float* p = lane == 0 ? reinterpret_cast<const float*>(op.targets) : lane == 1 ? op.old_logp : lane == 2 ? op.ref_logp : op.adv;
-    if (lane < 3 + ((op.flags & RAPID_CLIP_ADV_TOKEN) ? 1 : 0) && p) near_line(p + r);
-}
-__device__ __forceinline__ void bring_near(const DistillOp& op, int64_t r) {
-    const int lane = threadIdx.x & 31;
-    if (32 * lane < op.k) {
-        near_line(op.index + r * op.ld + 32 * lane);
-        near_line(op.logit + r * op.ld + 32 * lane);
-    }
-    if (lane == 31) near_line(op.teacher_lse2 + r);
 }
 struct DistillRow {
     double teacher, w;
@@ -607,7 +590,7 @@ struct DistillRow {
     double list_sum;  // the list's sum of 2^(x - top's x)
     float top;        // the list's largest logit
 };
-__device__ __forceinline__ DistillRow look(const DistillOp& op, int64_t r, double shared, const int* col, const float* z, const float* x) {
+__device__ __forceinline__ DistillRow look(const DistillOp& op, int64_t r, double shared, const int* col, const float* z) {
     const int lane = threadIdx.x & 31;
     DistillRow row{op.teacher_lse2[r], shared, 0.0, 0.0, 0.0, -INFINITY};
     if (!op.tail) return row;
@@ -615,7 +598,7 @@ __device__ __forceinline__ DistillRow look(const DistillOp& op, int64_t r, doubl
     for (int j = lane; j < op.k; j += 32) {
         if (col[j] < 0) continue;
         row.top = fmaxf(row.top, z[j]);
-        mass += exp2_short((double)x[j] * op.kd - row.teacher);
+        mass += exp2_short((double)op.logit[r * op.ld + j] * op.kd - row.teacher);
     }
     row.top = warp_top(row.top);
     row.p0 = 1.0 - warp_sum(mass);
@@ -626,21 +609,19 @@ __device__ __forceinline__ DistillRow look(const DistillOp& op, int64_t r, doubl
     row.list_sum = warp_sum(row.list_sum);
     return row;
 }
-__device__ __forceinline__ RowGrad finish(const ClipOp& op, const RowsArgs& a, ClipRow& row, const RowStat& st, const int*, const float* z,
-                                          const float*) {
+__device__ __forceinline__ RowGrad finish(const ClipOp& op, const RowsArgs& a, ClipRow& row, const RowStat& st, const int*, const float* z) {
     row.lp = ((double)z[0] * a.f.kd - st.lse2) * kLn2D;
     if (op.flags & RAPID_LOSS_NORM_SEQ) row.w /= (double)row.seq_rows;
     return RowGrad{row.w * clip_terms(op, row.in, row.lp).slope, st.lse2};
 }
 __device__ __forceinline__ void values(const ClipOp&, const RowsArgs& a, int64_t r, const ClipRow& row, const RowGrad& g, const RowStat&,
-                                       const int*, const float*, float* x) {
+                                       const int*, float* z) {
     if ((threadIdx.x & 31) != 0) return;
-    x[0] = (float)(g.a * (exp2_short(row.lp * kLog2eD) - 1.0));
+    z[0] = (float)(g.a * (exp2_short(row.lp * kLog2eD) - 1.0));
     a.w.value[r] = row.lp;
 }
 
-__device__ __forceinline__ RowGrad finish(const DistillOp& op, const RowsArgs&, DistillRow& row, const RowStat& st, const int* col, const float* z,
-                                          const float*) {
+__device__ __forceinline__ RowGrad finish(const DistillOp& op, const RowsArgs&, DistillRow& row, const RowStat& st, const int*, const float*) {
     RowGrad g{row.w, st.lse2};
     if (!op.tail) return g;
     // the student's log-sum-exp over the whole vocabulary, in a sum against the larger of the rest's and the list's largest term
@@ -653,15 +634,15 @@ __device__ __forceinline__ RowGrad finish(const DistillOp& op, const RowsArgs&, 
     return g;
 }
 __device__ __forceinline__ void values(const DistillOp& op, const RowsArgs& a, int64_t r, const DistillRow& row, const RowGrad& g,
-                                       const RowStat& st, const int* col, const float* z, float* x) {
+                                       const RowStat& st, const int* col, float* z) {
     const int lane = threadIdx.x & 31;
     double loss = 0.0;
     for (int j = lane; j < op.k; j += 32) {
         if (col[j] < 0) continue;
-        const double lt = (double)x[j] * op.kd - row.teacher, lq = (double)z[j] * op.kd - g.lse2;
+        const double lt = (double)op.logit[r * op.ld + j] * op.kd - row.teacher, lq = (double)z[j] * op.kd - g.lse2;
         const double p = exp2_short(lt);
         if (p > 0.0) loss += p * (lt - lq);
-        x[j] = (float)(row.w * (exp2_short(lq) - p));
+        z[j] = (float)(row.w * (exp2_short(lq) - p));
     }
     loss = warp_sum(loss);
     if (row.p0 > 0.0) loss += row.p0 * (row.lp0 - (st.lse2 - g.lse2));
