@@ -1,8 +1,10 @@
-// The rows of the losses of rapid_losses.h, where a row is long: a block holds a whole row on its SM.
+// The rows of the losses of rapid_losses.h: every logit is read from memory once and its gradient written once, with the row held on
+// one SM in between.  Three kernels, by the row's length: two rows by a warp, a row by a group of warps, and this one, a row by a block.
 //
-// Roles of a block: one producer warp draws rows from a counter and streams them into a ring of shared-memory stages with bulk
-// copies (rows that do not count it fills with zeros itself); kWarps consumer warps read the stages; one warp does what is done once
-// a row: it gathers the chosen columns' logits ahead of time, joins the consumers' sums and computes the row's factor in double.
+// Roles of a block of the longest rows: one producer warp draws rows from a counter and streams them into a ring of shared-memory
+// stages with bulk copies; kWarps consumer warps read the stages; one warp gathers the chosen columns' logits ahead of time; one does
+// what is done once a row: it joins the consumers' sums and computes the row's factor in double; one writes the zeros of the rows
+// that do not count.
 //
 // A row's first reading takes its maximum and sum of exponentials chunk by chunk.  What fits stays: the first kKeep chunks in the
 // consumers' registers, the last ones in their stages, so that the second reading, which writes the gradient, needs no memory
@@ -20,12 +22,12 @@ namespace losses {
 
 namespace {
 
+// ---- the longest rows ------------------------------------------------------------------------------------------
 
 struct RingShape {
     int stages;   // of a chunk each
     int chunks;   // of a row
     int again;    // chunks of a row that are loaded a second time
-    int batch;    // rows drawn at a time
     int list;     // chosen columns of a row, rounded up
     unsigned long long stride;
 };
@@ -166,27 +168,16 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
             unsigned int t = 0;
             if (lane == 0) t = atomicAdd(&a.w.head->ticket, 1u);
             t = __shfl_sync(0xffffffffu, t, 0);
-            const int64_t d = (int64_t)t * sh.batch;
-            if (d >= a.n_rows) break;
-            int64_t mine = -1;
-            uint8_t st = ROW_MASKED;
-            if (lane < sh.batch && d + lane < a.n_rows) {
-                mine = (int64_t)(((unsigned long long)(d + lane) * sh.stride) % (unsigned long long)a.n_rows);
-                st = a.w.state[mine];
+            if ((int64_t)t >= a.n_rows) break;
+            const int64_t r = (int64_t)((unsigned long long)t * sh.stride % (unsigned long long)a.n_rows);
+            if (a.w.state[r] != ROW_OK) {  // nobody reads this row
+                if (grad) ok = zero(r);
+                continue;
             }
-            for (int i = 0; i < sh.batch && ok; ++i) {
-                const int64_t r = __shfl_sync(0xffffffffu, mine, i);
-                const int state = __shfl_sync(0xffffffffu, (int)st, i);
-                if (r < 0) break;
-                if (state != ROW_OK) {  // nobody reads this row
-                    if (grad) ok = zero(r);
-                    continue;
-                }
-                const uint8_t* src = static_cast<const uint8_t*>(a.logits) + (size_t)r * a.ld * sizeof(T);
-                publish(r);
-                for (int c = 0; c < sh.chunks && ok; ++c) ok = load(src, c, c >= keep && c < keep + sh.again);
-                for (int c = keep; c < keep + sh.again && ok; ++c) ok = load(src, c, false);
-            }
+            const uint8_t* src = static_cast<const uint8_t*>(a.logits) + (size_t)r * a.ld * sizeof(T);
+            publish(r);
+            for (int c = 0; c < sh.chunks && ok; ++c) ok = load(src, c, c >= keep && c < keep + sh.again);
+            for (int c = keep; c < keep + sh.again && ok; ++c) ok = load(src, c, false);
         }
         if (ok) publish(-1);
         if (ok) zero(-1);
@@ -274,7 +265,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
             const uint32_t ph = (jq >> 1) & 1u;
             const Slot slot = slot_at(slots + slot_i * slot_bytes, sh.list);
             if (!warp_wait(&bd.list[slot_i], jq / kSlots & 1u, abortp)) break;
-            auto mine = look(op, r, shared, slot.col, slot.z);
+            auto mine = look<32>(op, r, shared, slot.col, slot.z);
             if (!warp_wait(&bd.parts_in[s], ph, abortp)) break;
             const RowStat st = join_parts(lane < kWarps ? bd.parts[s][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, off, unit, a.f);
             const RowGrad g = finish(op, a, mine, st, slot.col, slot.z);
@@ -282,7 +273,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
                 bd.grads[s] = grad_const<DT>(g, st.max, a.f);
                 mbar_arrive(&bd.grad[s]);
             }
-            values(op, a, r, mine, g, st, slot.col, slot.z);
+            values<32>(op, a, r, mine, g, st, slot.col, slot.z, true);
             __syncwarp();
             if (lane == 0) mbar_arrive(&bd.value[slot_i]);
         }
@@ -472,9 +463,9 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
 constexpr int kParts = 2;
 
 // Vectors of a thread at a time: eight hide more latency, where the registers are there for them (16384 rows of 16384 bf16 228 -> 220 us;
-// eight warps a row 314 -> 325, one 154 either way).
+// eight warps a row 314 -> 325).
 template <int G>
-constexpr int kBatch = G == 2 || G == 4 ? 8 : 4;
+constexpr int kBatch = G < 8 ? 8 : 4;
 
 struct GroupShape {
     int groups;          // of a block
@@ -496,7 +487,6 @@ struct GroupBoard {
 // The warps of a group together, with the OR of what they say: after a wait that gave up all leave together.
 template <int G>
 __device__ __forceinline__ bool group_sync(int id, bool flag) {
-    if constexpr (G == 1) return __any_sync(0xffffffffu, flag);
     uint32_t out;
     asm volatile(
         "{\n\t.reg .pred p, q;\n\t"
@@ -510,7 +500,7 @@ __device__ __forceinline__ bool group_sync(int id, bool flag) {
 }
 
 template <int DT, class Op, int G>
-__global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a, Op op, GroupShape sh) {
+__global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupShape sh) {
     using E = Elem<DT>;
     using T = typename E::T;
     constexpr int kLanes = G * 32;
@@ -543,7 +533,7 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
     const unsigned int n_rows = (unsigned int)a.n_rows;
     const uint64_t once = policy_first();
     const float off = shift_fraction(gw), unit_off = shift_fraction(lane);
-    const double unit = part_unit(unit_off), unit0 = part_unit(off);
+    const double unit = part_unit(unit_off);
     const uint4* row_place = reinterpret_cast<const uint4*>(place);
 
     uint32_t issued = 0, phase_of = 0;  // a bit for each part: loaded by this thread, and the phase of its last load
@@ -643,17 +633,15 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
         auto hand_over = [&](int p) {
             __syncwarp();
             if (lane != 0) return;
-            if constexpr (G > 1) {
-                __threadfence_block();
-                if (atomicAdd(&bd.read[p], 1) != G - 1) return;
-                __threadfence_block();
-                bd.read[p] = 0;
-            }
+            __threadfence_block();
+            if (atomicAdd(&bd.read[p], 1) != G - 1) return;
+            __threadfence_block();
+            bd.read[p] = 0;
             if (next >= 0 && next < a.n_rows) load_part(next, p, ph ^ 1u);
         };
         // ---- first reading ----
         if (!grad) {
-            if (G > 1 && group_sync<G>(id, !ok)) break;  // the announcement
+            if (group_sync<G>(id, !ok)) break;  // the announcement
             __syncwarp();
             next = bd.next[turn & 1];
         }
@@ -664,7 +652,7 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
             if (ex) {  // the list's columns of this warp's vectors: their logits are noted and leave the sum
                 bool wrote = false;
                 for (int j = lane; j < n_list; j += 32) {
-                    const int v = G == 1 ? slot.col[j] : column(op, row, j), at = v / E::kPer;
+                    const int v = column(op, row, j), at = v / E::kPer;
                     if (v >= 0 && at >= from && at < end && (at - from) % kLanes / 32 == gw) {
                         T* e = reinterpret_cast<T*>(place) + v;
                         slot.z[j] = E::get(*e);
@@ -695,15 +683,10 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
         }
         const WarpPart w = warp_part(p, a.f);
         RowStat st{0.0, 0.f};
-        if constexpr (G == 1) {
-            if (!ok) break;
-            st = one_part(w, off, unit0, a.f);
-        } else {
-            if (lane == 0) bd.parts[ph][gw] = w;
-            if (group_sync<G>(id, !ok)) break;
-            if (gw == 0) st = join_parts(lane < G ? bd.parts[ph][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, unit_off, unit, a.f);
-        }
-        decltype(look(op, row, shared, slot.col, slot.z)) mine{};
+        if (lane == 0) bd.parts[ph][gw] = w;
+        if (group_sync<G>(id, !ok)) break;
+        if (gw == 0) st = join_parts(lane < G ? bd.parts[ph][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, unit_off, unit, a.f);
+        decltype(look<32>(op, row, shared, slot.col, slot.z)) mine{};
         RowGrad g{0.0, 0.0};
         if (gw == 0) {
             if (!ex && grad)
@@ -712,7 +695,7 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
                     if (v >= 0) slot.z[j] = E::get(reinterpret_cast<const T*>(place)[v]);
                 }
             __syncwarp();
-            mine = look(op, row, shared, slot.col, slot.z);
+            mine = look<32>(op, row, shared, slot.col, slot.z);
             g = finish(op, a, mine, st, slot.col, slot.z);
             if (lane == 0) bd.grad = grad_const<DT>(g, st.max, a.f);
             if (grad) announce();
@@ -752,7 +735,7 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
             }
         }
         if (gw == 0) {
-            values(op, a, row, mine, g, st, slot.col, slot.z);
+            values<32>(op, a, row, mine, g, st, slot.col, slot.z, true);
             __syncwarp();
             if (grad) pending = row;
         }
@@ -778,6 +761,235 @@ __global__ void __launch_bounds__(G == 1 ? 768 : 512, 1) group_kernel(RowsArgs a
     if (a.end.last_block) finish_rows(op, a, reinterpret_cast<double*>(dyn));
 }
 
+// ---- the shortest rows ------------------------------------------------------------------------------------------
+
+// Up to 8 KB a warp holds two rows at a time: it reads them one after the other, then does what is done once a row for both of them
+// at once, half a warp each, and writes them one after the other.  That arithmetic, one value a row in double, is a chain of some
+// thousands of cycles in which a warp that holds one row does nothing else: 65536 rows of 4096 bf16 with 8 entries take 240 us, with
+// one row a warp they took 300, and four rows, which leave six warps an SM, 297.
+constexpr int kTogether = 2;
+
+struct ShortShape {
+    int warps;       // of a block
+    int row_bytes;   // place of a row
+    int warp_bytes;  // of a warp in shared memory
+    int list;
+};
+
+struct ShortBoard {
+    uint64_t full[kTogether];
+    WarpPart parts[kTogether];
+    GradConst grads[kTogether];
+};
+
+template <int DT, class Op>
+__global__ void __launch_bounds__(512, 1) short_kernel(RowsArgs a, Op op, ShortShape sh) {
+    using E = Elem<DT>;
+    using T = typename E::T;
+    constexpr int U = 4, W = 32 / kTogether;
+    extern __shared__ __align__(128) uint8_t dyn[];
+    __shared__ int abort_flag;
+    __shared__ double weight;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint8_t* place = dyn + (size_t)warp * sh.warp_bytes;
+    ShortBoard& bd = *reinterpret_cast<ShortBoard*>(place + kTogether * sh.row_bytes);
+    uint8_t* slots = place + kTogether * sh.row_bytes + sizeof(ShortBoard);
+    if (lane == 0) {
+        for (int k = 0; k < kTogether; ++k) mbar_init(&bd.full[k], 1);
+        mbar_init_fence();
+    }
+    if (threadIdx.x == 0) abort_flag = 0;
+    if (warp == 0) {
+        const double w = shared_weight(op, rows_that_count(op_counts(op), op_blocks(op)));
+        if (lane == 0) weight = w;
+    }
+    __syncthreads();
+    volatile int* abortp = &abort_flag;
+    const double shared = weight;
+    const bool grad = a.grad != nullptr, ex = exclude(op);
+    const int nvec = a.vocab / E::kPer, rest = a.vocab - nvec * E::kPer, all = nvec + (rest ? 1 : 0);
+    const int n_list = list_size(op);
+    const unsigned int n_rows = (unsigned int)a.n_rows, n_sets = (n_rows + kTogether - 1) / kTogether;
+    const uint64_t once = policy_first();
+    const float off = shift_fraction(0);
+    const double unit = part_unit(off);
+
+    uint32_t issued = 0, phase_of = 0;  // a bit for each place: loaded by this lane, and the phase of its last load
+    uint32_t ph = 0;                    // phase of each place's next load, a bit each
+    auto load_row = [&](unsigned int r, int k) {  // by one lane, into place k
+        issued |= 1u << k;
+        phase_of = (phase_of & ~(1u << k)) | (ph & 1u << k);
+        mbar_arrive_expect_tx(&bd.full[k], (uint32_t)all * 16u);
+        bulk_load_once(place + (size_t)k * sh.row_bytes, static_cast<const uint8_t*>(a.logits) + (size_t)r * a.ld * sizeof(T), (uint32_t)all * 16u,
+                       &bd.full[k], once);
+    };
+    // rows of a set that count, a bit each
+    auto live_of = [&](unsigned int set) {
+        const unsigned int r = set * kTogether + lane;
+        return __ballot_sync(0xffffffffu, lane < kTogether && set < n_sets && r < n_rows && a.w.state[r] == ROW_OK);
+    };
+    // sets are dealt out first, one to every warp of the grid, then drawn, one ahead
+    const unsigned int everyone = gridDim.x * sh.warps;
+    unsigned int set = warp * gridDim.x + blockIdx.x, t1 = 0;
+    uint32_t live = live_of(set);
+    if (lane == 0) t1 = everyone + atomicAdd(&a.w.head->ticket, 1u);
+    for (int k = 0; k < kTogether; ++k)
+        if (lane == 0 && (live >> k & 1u)) load_row(set * kTogether + k, k);
+    bool ok = true;
+    while (set < n_sets && ok) {
+        const unsigned int row0 = set * kTogether, next = __shfl_sync(0xffffffffu, t1, 0);
+        if (lane == 0) t1 = everyone + atomicAdd(&a.w.head->ticket, 1u);
+        // the chosen columns of all rows
+        for (int i = lane; i < kTogether * n_list; i += 32) {
+            const int k = i / n_list, j = i - k * n_list;
+            slot_at(slots + k * sh.list * kSlotEntry, sh.list).col[j] = (live >> k & 1u) ? column(op, row0 + k, j) : -1;
+        }
+        const uint32_t live_next = live_of(next);
+        if (grad)
+            for (int k = 0; k < kTogether; ++k)
+                if (!(live >> k & 1u) && row0 + k < n_rows) {  // nobody reads this row
+                    T* out = static_cast<T*>(a.grad) + (int64_t)(row0 + k) * a.ld_grad;
+                    for (int v = lane; v < nvec; v += 32) st_stream(reinterpret_cast<uint4*>(out) + v, make_uint4(0, 0, 0, 0));
+                    if (lane < rest) out[nvec * E::kPer + lane] = E::put(0.f);
+                }
+        __syncwarp();
+        // vector `at` of the row at `p`; columns behind the last read as -inf
+        auto read = [&](const uint4* p, int at) {
+            constexpr uint32_t kNone = DT == RAPID_BF16 ? 0xff80ff80u : 0xff800000u;
+            uint4 v = make_uint4(kNone, kNone, kNone, kNone);
+            if (at < nvec) v = p[at];
+            else if (at == nvec && rest) {
+                const T* e = reinterpret_cast<const T*>(p + at);
+                uint32_t w[4] = {kNone, kNone, kNone, kNone};
+#pragma unroll
+                for (int i = 0; i < E::kPer; ++i) {
+                    if (i >= rest) continue;
+                    if constexpr (DT == RAPID_BF16) {
+                        const uint32_t b = e[i];
+                        w[i / 2] = (i & 1) ? ((w[i / 2] & 0xffffu) | (b << 16)) : ((w[i / 2] & 0xffff0000u) | b);
+                    } else {
+                        w[i] = __float_as_uint(e[i]);
+                    }
+                }
+                v = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            return v;
+        };
+        auto hand_over = [&](int k) {  // place k has been read for the last time
+            __syncwarp();
+            if (lane == 0 && (live_next >> k & 1u)) load_row(next * kTogether + k, k);
+        };
+        // ---- first reading ----
+#pragma unroll 1
+        for (int k = 0; k < kTogether && ok; ++k) {
+            if (!(live >> k & 1u)) continue;
+            if (!(ok = warp_wait(&bd.full[k], ph >> k & 1u, abortp))) break;
+            ph ^= 1u << k;
+            uint8_t* row = place + (size_t)k * sh.row_bytes;
+            const uint4* p = reinterpret_cast<const uint4*>(row);
+            const Slot slot = slot_at(slots + k * sh.list * kSlotEntry, sh.list);
+            bool wrote = false;
+            for (int j = lane; j < n_list; j += 32) {
+                const int v = slot.col[j];
+                if (v < 0) continue;
+                T* e = reinterpret_cast<T*>(row) + v;
+                slot.z[j] = E::get(*e);
+                if (ex) *e = E::put(-INFINITY);  // left out of the sum
+                wrote = ex;
+            }
+            if (wrote) fence_proxy_async_smem();  // a bulk copy writes there next
+            __syncwarp();
+            Part part;
+            int v = lane;
+            for (; v - lane + (U - 1) * 32 + 31 < nvec; v += U * 32) {
+                uint4 q[U];
+#pragma unroll
+                for (int j = 0; j < U; ++j) q[j] = p[v + j * 32];
+                part.template vectors<DT, U>(q, off, a.f);
+            }
+            for (; v - lane < all; v += 32) {
+                uint4 q[1] = {read(p, v)};
+                part.template vectors<DT, 1>(q, off, a.f);
+            }
+            const WarpPart w = warp_part(part, a.f);
+            if (lane == 0) bd.parts[k] = w;
+            if (!grad) hand_over(k);
+        }
+        if (!ok) break;
+        __syncwarp();
+        // ---- once a row, for all of them ----
+        {
+            const int k = lane / W;
+            const bool mine = live >> k & 1u;
+            const unsigned int r = min(row0 + k, n_rows - 1);
+            const Slot slot = slot_at(slots + k * sh.list * kSlotEntry, sh.list);
+            const RowStat st = one_part(mine ? bd.parts[k] : WarpPart{0.0, -INFINITY, -INFINITY}, off, unit, a.f);
+            auto row = look<W>(op, r, shared, slot.col, slot.z);
+            const RowGrad g = finish(op, a, row, st, slot.col, slot.z);
+            if (lane % W == 0) bd.grads[k] = grad_const<DT>(g, st.max, a.f);
+            values<W>(op, a, r, row, g, st, slot.col, slot.z, mine);
+        }
+        __syncwarp();
+        // ---- second reading ----
+        if (grad) {
+#pragma unroll 1
+            for (int k = 0; k < kTogether; ++k) {
+                if (!(live >> k & 1u)) {
+                    hand_over(k);
+                    continue;
+                }
+                const uint4* p = reinterpret_cast<const uint4*>(place + (size_t)k * sh.row_bytes);
+                const Slot slot = slot_at(slots + k * sh.list * kSlotEntry, sh.list);
+                const Grad<DT> gr(bd.grads[k], a.f);
+                T* out = static_cast<T*>(a.grad) + (int64_t)(row0 + k) * a.ld_grad;
+                uint4* ov = reinterpret_cast<uint4*>(out);
+                int v = lane;
+                for (; v - lane + (U - 1) * 32 + 31 < nvec; v += U * 32) {
+                    uint4 q[U];
+#pragma unroll
+                    for (int j = 0; j < U; ++j) q[j] = p[v + j * 32];
+#pragma unroll
+                    for (int j = 0; j < U; ++j) st_stream(ov + v + j * 32, gr.vector(q[j]));
+                }
+                for (; v - lane < all; v += 32) {
+                    const uint4 y = gr.vector(read(p, v));
+                    if (v < nvec) st_stream(ov + v, y);
+                    else if (v == nvec && rest) {
+                        const uint32_t x[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                        for (int i = 0; i < E::kPer; ++i) {
+                            if (i >= rest) continue;
+                            if constexpr (DT == RAPID_BF16) out[nvec * E::kPer + i] = (T)(x[i / 2] >> (16 * (i & 1)));
+                            else out[nvec * E::kPer + i] = __uint_as_float(x[i]);
+                        }
+                    }
+                }
+                hand_over(k);
+                for (int j = lane; j < n_list; j += 32) {  // the chosen columns over the vectors
+                    const int c = slot.col[j];
+                    if (c >= 0) out[c] = E::put(slot.z[j]);
+                }
+            }
+        } else {
+            for (int k = 0; k < kTogether; ++k)
+                if (!(live >> k & 1u)) hand_over(k);
+        }
+        __syncwarp();  // the slots have been read
+        set = next;
+        live = live_next;
+    }
+    if (lane == 0 && *abortp) {  // gave up: let the copies already issued land before the block's memory goes away
+        for (int k = 0; k < kTogether; ++k) {
+            const unsigned long long t = global_timer_ns();
+            while ((issued >> k & 1u) && !mbar_try_wait(&bd.full[k], phase_of >> k & 1u))
+                if (global_timer_ns() - t > kWaitLimitNs) break;
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && abort_flag) atomicMax(&a.w.head->status, (int)RAPID_ERR_TIMEOUT);
+    if (a.end.last_block) finish_rows(op, a, reinterpret_cast<double*>(dyn));
+}
+
 template <class Op>
 cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_count, cudaStream_t stream) {
     const size_t es = elem_size(a.dtype);
@@ -796,9 +1008,6 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         int64_t grid = (int64_t)sm_count * blocks;
-        sh.batch = (int)(a.n_rows / (grid * 4));
-        if (sh.batch < 1 || chunk >= 16384) sh.batch = 1;
-        if (sh.batch > 8) sh.batch = 8;
         if (grid > a.n_rows) grid = a.n_rows;
         sh.stride = scatter_stride(a.n_rows);
         kern<<<(unsigned)grid, (warps + 4) * 32, smem, stream>>>(a, op, sh);
@@ -808,14 +1017,13 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
         GroupShape sh{};
         const int lanes = G * 32, all = (int)(row_bytes / 16);
         sh.list = (list + 3) / 4 * 4;
-        // a row in two parts, so that the next row's first half comes while the second is read; with one warp the others hide it, and
-        // one part costs less (65536 rows of 4096 bf16: 304 us, in two 314, in four 320)
-        const int want = G == 1 ? 1 : kParts, unit = lanes * batch;
-        sh.part_vecs = ((all + want - 1) / want + unit - 1) / unit * unit;
+        // a row in two parts, so that the next row's first half comes while the second is read
+        const int unit = lanes * batch;
+        sh.part_vecs = ((all + kParts - 1) / kParts + unit - 1) / unit * unit;
         sh.parts = (all + sh.part_vecs - 1) / sh.part_vecs;
         sh.row_bytes = (int)row_bytes;
         sh.group_bytes = (int)((row_bytes + sizeof(GroupBoard) + 2 * sh.list * kSlotEntry + 127) / 128 * 128);
-        sh.groups = std::min((227 * 1024 - 64) / sh.group_bytes, (G == 1 ? 24 : 16) / G);
+        sh.groups = std::min((227 * 1024 - 64) / sh.group_bytes, 16 / G);
         const size_t smem = (size_t)sh.groups * sh.group_bytes;
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
@@ -823,11 +1031,24 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
         kern<<<(unsigned)grid, sh.groups * lanes, smem, stream>>>(a, op, sh);
         return cudaGetLastError();
     };
+    auto go_short = [&](auto kern) -> cudaError_t {
+        ShortShape sh{};
+        sh.list = (list + 3) / 4 * 4;
+        sh.row_bytes = (int)row_bytes;
+        sh.warp_bytes = (int)((kTogether * row_bytes + sizeof(ShortBoard) + kTogether * sh.list * kSlotEntry + 127) / 128 * 128);
+        sh.warps = std::min((227 * 1024 - 256) / sh.warp_bytes, 16);
+        const size_t smem = std::max((size_t)sh.warps * sh.warp_bytes, (size_t)2048);
+        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        const int64_t sets = (a.n_rows + kTogether - 1) / kTogether;
+        kern<<<(unsigned)std::min((int64_t)sm_count, sets), sh.warps * 32, smem, stream>>>(a, op, sh);
+        return cudaGetLastError();
+    };
     auto by_type = [&](auto dt) -> cudaError_t {
         constexpr int DT = decltype(dt)::value;
         // warps for a row: as many as leave at least two groups an SM and each thread two batches (16384 x 8192 bf16 in ones 285 us, in twos
         // 246; 8192 x 32000 in fours 229, in eights 249)
-        if (row_bytes <= 8192) return go_groups(group_kernel<DT, Op, 1>, 1, kBatch<1>);
+        if (row_bytes <= 8192) return go_short(short_kernel<DT, Op>);
         if (row_bytes <= 32768) return go_groups(group_kernel<DT, Op, 2>, 2, kBatch<2>);
         if (row_bytes <= 73728) return go_groups(group_kernel<DT, Op, 4>, 4, kBatch<4>);
         if (row_bytes <= 110 * 1024) return go_groups(group_kernel<DT, Op, 8>, 8, kBatch<8>);

@@ -314,6 +314,20 @@ __device__ __forceinline__ double log2_short(double s) {  // s > 0, normal
     return (double)e + fma(r * fma(r, -0.5, 1.0), kLog2eD, l);
 }
 
+// Sum and maximum over W neighbouring lanes; all of the warp comes here.
+template <int W>
+__device__ __forceinline__ double lanes_sum(double v) {
+#pragma unroll
+    for (int o = W / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+template <int W>
+__device__ __forceinline__ float lanes_top(float v) {
+#pragma unroll
+    for (int o = W / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+
 // Maximum over the warp of floats that are not NaN.
 __device__ __forceinline__ float warp_top(float v) {
     float r;
@@ -561,8 +575,8 @@ __device__ __forceinline__ double shared_weight(const DistillOp& op, long long r
     return op.scale * op.inv_tau / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows);
 }
 
-// What an operator does with a row, by one warp.  look() does, ahead of time, what needs no sums over the row; finish() gives the
-// factor once the row's log-sum-exp is there (without the chosen columns where exclude() says so), and is what the row's second
+// What an operator does with a row, by W lanes of a warp whose other lanes do the same for other rows.  look() does, ahead of time,
+// what needs no sums over the row; finish() gives the factor once the row's log-sum-exp is there (without the chosen columns where exclude() says so), and is what the row's second
 // reading waits for; values() gives the chosen columns' gradient and writes what is kept of the row to the scratch.  col[j] and
 // z[j] are the chosen columns and their logits; z[j] become the columns' gradient.
 __device__ __forceinline__ int list_size(const ClipOp&) { return 1; }
@@ -581,6 +595,7 @@ struct ClipRow {
     int seq_rows;
     double w, lp;
 };
+template <int W>
 __device__ __forceinline__ ClipRow look(const ClipOp& op, int64_t r, double shared, const int*, const float*) {
     return ClipRow{clip_in(op, r), (op.flags & RAPID_LOSS_NORM_SEQ) ? op.seq_rows[divide(r, op.seq_len)] : 1, shared, 0.0};
 }
@@ -590,23 +605,24 @@ struct DistillRow {
     double list_sum;  // the list's sum of 2^(x - top's x)
     float top;        // the list's largest logit
 };
+template <int W>
 __device__ __forceinline__ DistillRow look(const DistillOp& op, int64_t r, double shared, const int* col, const float* z) {
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x % W;
     DistillRow row{op.teacher_lse2[r], shared, 0.0, 0.0, 0.0, -INFINITY};
     if (!op.tail) return row;
     double mass = 0.0;
-    for (int j = lane; j < op.k; j += 32) {
+    for (int j = lane; j < op.k; j += W) {
         if (col[j] < 0) continue;
         row.top = fmaxf(row.top, z[j]);
         mass += exp2_short((double)op.logit[r * op.ld + j] * op.kd - row.teacher);
     }
-    row.top = warp_top(row.top);
-    row.p0 = 1.0 - warp_sum(mass);
+    row.top = lanes_top<W>(row.top);
+    row.p0 = 1.0 - lanes_sum<W>(mass);
     if (row.p0 > 0.0) row.lp0 = log2_short(row.p0);
     if (row.top > -INFINITY)
-        for (int j = lane; j < op.k; j += 32)
+        for (int j = lane; j < op.k; j += W)
             if (col[j] >= 0) row.list_sum += exp2_short(((double)z[j] - (double)row.top) * op.kd);
-    row.list_sum = warp_sum(row.list_sum);
+    row.list_sum = lanes_sum<W>(row.list_sum);
     return row;
 }
 __device__ __forceinline__ RowGrad finish(const ClipOp& op, const RowsArgs& a, ClipRow& row, const RowStat& st, const int*, const float* z) {
@@ -614,9 +630,10 @@ __device__ __forceinline__ RowGrad finish(const ClipOp& op, const RowsArgs& a, C
     if (op.flags & RAPID_LOSS_NORM_SEQ) row.w /= (double)row.seq_rows;
     return RowGrad{row.w * clip_terms(op, row.in, row.lp).slope, st.lse2};
 }
+template <int W>
 __device__ __forceinline__ void values(const ClipOp&, const RowsArgs& a, int64_t r, const ClipRow& row, const RowGrad& g, const RowStat&,
-                                       const int*, float* z) {
-    if ((threadIdx.x & 31) != 0) return;
+                                       const int*, float* z, bool live) {
+    if (threadIdx.x % W != 0 || !live) return;
     z[0] = (float)(g.a * (exp2_short(row.lp * kLog2eD) - 1.0));
     a.w.value[r] = row.lp;
 }
@@ -633,20 +650,21 @@ __device__ __forceinline__ RowGrad finish(const DistillOp& op, const RowsArgs&, 
     if (row.p0 > 0.0 && st.lse2 > -INFINITY) g.a = row.w * (1.0 - exp2_short(row.lp0 - (st.lse2 - g.lse2)));
     return g;
 }
+template <int W>
 __device__ __forceinline__ void values(const DistillOp& op, const RowsArgs& a, int64_t r, const DistillRow& row, const RowGrad& g,
-                                       const RowStat& st, const int* col, float* z) {
-    const int lane = threadIdx.x & 31;
+                                       const RowStat& st, const int* col, float* z, bool live) {
+    const int lane = threadIdx.x % W;
     double loss = 0.0;
-    for (int j = lane; j < op.k; j += 32) {
+    for (int j = lane; j < op.k; j += W) {
         if (col[j] < 0) continue;
         const double lt = (double)op.logit[r * op.ld + j] * op.kd - row.teacher, lq = (double)z[j] * op.kd - g.lse2;
         const double p = exp2_short(lt);
         if (p > 0.0) loss += p * (lt - lq);
         z[j] = (float)(row.w * (exp2_short(lq) - p));
     }
-    loss = warp_sum(loss);
+    loss = lanes_sum<W>(loss);
     if (row.p0 > 0.0) loss += row.p0 * (row.lp0 - (st.lse2 - g.lse2));
-    if (lane == 0) a.w.value[r] = loss * kLn2D;
+    if (lane == 0 && live) a.w.value[r] = loss * kLn2D;
 }
 
 // A row's statistics and its token's log-probability from what the reading without a gradient left of it.
