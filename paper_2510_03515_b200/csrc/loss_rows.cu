@@ -75,6 +75,13 @@ __device__ __forceinline__ uint64_t policy_normal() {
     return p;
 }
 
+// The next ticket.  (After atomicAdd() a warp waits for the result at once, some 1200 cycles.)
+__device__ __forceinline__ unsigned int draw_ticket(const Scratch& w) {
+    unsigned int t;
+    asm volatile("atom.relaxed.gpu.global.add.u32 %0, [%1], 1;" : "=r"(t) : "l"(&w.head->ticket) : "memory");
+    return t;
+}
+
 // By a whole warp; the lanes agree, so that all of them stay or all leave.
 __device__ __noinline__ bool warp_wait_long(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
     return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag));
@@ -166,7 +173,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
         };
         while (ok) {
             unsigned int t = 0;
-            if (lane == 0) t = atomicAdd(&a.w.head->ticket, 1u);
+            if (lane == 0) t = draw_ticket(a.w);
             t = __shfl_sync(0xffffffffu, t, 0);
             if ((int64_t)t >= a.n_rows) break;
             const int64_t r = (int64_t)((unsigned long long)t * sh.stride % (unsigned long long)a.n_rows);
@@ -265,7 +272,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
             const uint32_t ph = (jq >> 1) & 1u;
             const Slot slot = slot_at(slots + slot_i * slot_bytes, sh.list);
             if (!warp_wait(&bd.list[slot_i], jq / kSlots & 1u, abortp)) break;
-            auto mine = look<32>(op, r, shared, slot.col, slot.z);
+            auto mine = look<32>(op, head(op, r), shared, slot.col, slot.z, teacher(op, r));
             if (!warp_wait(&bd.parts_in[s], ph, abortp)) break;
             const RowStat st = join_parts(lane < kWarps ? bd.parts[s][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, off, unit, a.f);
             const RowGrad g = finish(op, a, mine, st, slot.col, slot.z);
@@ -273,7 +280,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
                 bd.grads[s] = grad_const<DT>(g, st.max, a.f);
                 mbar_arrive(&bd.grad[s]);
             }
-            values<32>(op, a, r, mine, g, st, slot.col, slot.z, true);
+            values<32>(op, a, r, mine, g, st, slot.col, slot.z, teacher(op, r), true);
             __syncwarp();
             if (lane == 0) mbar_arrive(&bd.value[slot_i]);
         }
@@ -554,7 +561,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
     int64_t row = t0 < n_rows ? (int64_t)t0 : a.n_rows;  // n_rows: there are none left
     bool live = state_of(t0) == ROW_OK;
     if (gt == 0) {
-        t1 = everyone + atomicAdd(&a.w.head->ticket, 1u);
+        t1 = everyone + draw_ticket(a.w);
         if (live)
             for (int p = 0; p < sh.parts; ++p) load_part(row, p, 0u);
     }
@@ -572,14 +579,14 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
     };
     for (uint32_t turn = 0; row < a.n_rows; ++turn) {
         if (gt == 0) {
-            t2 = everyone + atomicAdd(&a.w.head->ticket, 1u);
+            t2 = draw_ticket(a.w);
             state1 = state_of(t1);
         }
         auto announce = [&]() {  // the next row, to the group
             if (gt == 0) {
                 const int64_t r = t1 < n_rows ? (int64_t)t1 : a.n_rows;
                 bd.next[turn & 1] = t1 < n_rows && state1 != ROW_OK ? ~r : r;
-                t1 = t2;
+                t1 = everyone + t2;
             }
         };
         T* out = static_cast<T*>(a.grad) + row * a.ld_grad;
@@ -686,7 +693,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
         if (lane == 0) bd.parts[ph][gw] = w;
         if (group_sync<G>(id, !ok)) break;
         if (gw == 0) st = join_parts(lane < G ? bd.parts[ph][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, unit_off, unit, a.f);
-        decltype(look<32>(op, row, shared, slot.col, slot.z)) mine{};
+        decltype(look<32>(op, head(op, row), shared, slot.col, slot.z, teacher(op, row))) mine{};
         RowGrad g{0.0, 0.0};
         if (gw == 0) {
             if (!ex && grad)
@@ -695,7 +702,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
                     if (v >= 0) slot.z[j] = E::get(reinterpret_cast<const T*>(place)[v]);
                 }
             __syncwarp();
-            mine = look<32>(op, row, shared, slot.col, slot.z);
+            mine = look<32>(op, head(op, row), shared, slot.col, slot.z, teacher(op, row));
             g = finish(op, a, mine, st, slot.col, slot.z);
             if (lane == 0) bd.grad = grad_const<DT>(g, st.max, a.f);
             if (grad) announce();
@@ -735,7 +742,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
             }
         }
         if (gw == 0) {
-            values<32>(op, a, row, mine, g, st, slot.col, slot.z, true);
+            values<32>(op, a, row, mine, g, st, slot.col, slot.z, teacher(op, row), true);
             __syncwarp();
             if (grad) pending = row;
         }
@@ -774,7 +781,22 @@ struct ShortShape {
     int row_bytes;   // place of a row
     int warp_bytes;  // of a warp in shared memory
     int list;
+    int slot_bytes;  // of a row's chosen columns
 };
+
+__device__ __forceinline__ void copy_word(void* smem_dst, const void* gsrc) {  // comes on its own
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(smem_dst)), "l"(gsrc) : "memory");
+}
+// What is known of a row's chosen columns ahead of time, into its slot, by one warp.
+__device__ __forceinline__ void copy_list(const ClipOp& op, int64_t r, const Slot& slot, int) {
+    if ((threadIdx.x & 31) == 0) copy_word(slot.col, op.targets + r);
+}
+__device__ __forceinline__ void copy_list(const DistillOp& op, int64_t r, const Slot& slot, int list) {
+    for (int j = threadIdx.x & 31; j < op.k; j += 32) {
+        copy_word(slot.col + j, op.index + r * op.ld + j);
+        copy_word(slot.z + list + j, op.logit + r * op.ld + j);
+    }
+}
 
 struct ShortBoard {
     uint64_t full[kTogether];
@@ -823,28 +845,37 @@ __global__ void __launch_bounds__(512, 1) short_kernel(RowsArgs a, Op op, ShortS
         bulk_load_once(place + (size_t)k * sh.row_bytes, static_cast<const uint8_t*>(a.logits) + (size_t)r * a.ld * sizeof(T), (uint32_t)all * 16u,
                        &bd.full[k], once);
     };
-    // rows of a set that count, a bit each
-    auto live_of = [&](unsigned int set) {
+    auto state_of = [&](unsigned int set) -> int {  // of the set's row that is this lane's
         const unsigned int r = set * kTogether + lane;
-        return __ballot_sync(0xffffffffu, lane < kTogether && set < n_sets && r < n_rows && a.w.state[r] == ROW_OK);
+        return lane < kTogether && set < n_sets && r < n_rows ? (int)a.w.state[r] : ROW_MASKED;
     };
-    // sets are dealt out first, one to every warp of the grid, then drawn, one ahead
+    auto slot_of = [&](uint32_t turn, int k) { return slot_at(slots + ((turn & 1u) * kTogether + k) * sh.slot_bytes, sh.list); };
+    auto my_row = [&](unsigned int set) { return (int64_t)min(set * kTogether + lane / W, n_rows - 1); };
+    auto copy_lists = [&](unsigned int set, uint32_t live, uint32_t turn) {
+        for (int k = 0; k < kTogether; ++k)
+            if (live >> k & 1u) copy_list(op, set * kTogether + k, slot_of(turn, k), sh.list);
+    };
+    // Sets are dealt out first, one to every warp of the grid, then drawn.  A load that is issued behind a row's stores comes back when
+    // those have left the SM, thousands of cycles later; so what is needed of the next set is asked for before this one's are written.
     const unsigned int everyone = gridDim.x * sh.warps;
-    unsigned int set = warp * gridDim.x + blockIdx.x, t1 = 0;
-    uint32_t live = live_of(set);
-    if (lane == 0) t1 = everyone + atomicAdd(&a.w.head->ticket, 1u);
+    unsigned int set = warp * gridDim.x + blockIdx.x, next = 0, draw = 0;
+    if (lane == 0) {
+        next = draw_ticket(a.w);
+        draw = draw_ticket(a.w);
+    }
+    next = everyone + __shfl_sync(0xffffffffu, next, 0);
+    uint32_t live = __ballot_sync(0xffffffffu, state_of(set) == ROW_OK);
+    int state = state_of(next);
     for (int k = 0; k < kTogether; ++k)
         if (lane == 0 && (live >> k & 1u)) load_row(set * kTogether + k, k);
+    copy_lists(set, live, 0u);
+    auto in = head(op, my_row(set));
     bool ok = true;
-    while (set < n_sets && ok) {
-        const unsigned int row0 = set * kTogether, next = __shfl_sync(0xffffffffu, t1, 0);
-        if (lane == 0) t1 = everyone + atomicAdd(&a.w.head->ticket, 1u);
-        // the chosen columns of all rows
-        for (int i = lane; i < kTogether * n_list; i += 32) {
-            const int k = i / n_list, j = i - k * n_list;
-            slot_at(slots + k * sh.list * kSlotEntry, sh.list).col[j] = (live >> k & 1u) ? column(op, row0 + k, j) : -1;
-        }
-        const uint32_t live_next = live_of(next);
+    for (uint32_t turn = 0; set < n_sets && ok; ++turn) {
+        const unsigned int row0 = set * kTogether, later = everyone + __shfl_sync(0xffffffffu, draw, 0);
+        if (lane == 0) draw = draw_ticket(a.w);
+        const uint32_t live_next = __ballot_sync(0xffffffffu, state == ROW_OK);
+        asm volatile("cp.async.wait_all;" ::: "memory");  // this set's columns
         if (grad)
             for (int k = 0; k < kTogether; ++k)
                 if (!(live >> k & 1u) && row0 + k < n_rows) {  // nobody reads this row
@@ -887,7 +918,7 @@ __global__ void __launch_bounds__(512, 1) short_kernel(RowsArgs a, Op op, ShortS
             ph ^= 1u << k;
             uint8_t* row = place + (size_t)k * sh.row_bytes;
             const uint4* p = reinterpret_cast<const uint4*>(row);
-            const Slot slot = slot_at(slots + k * sh.list * kSlotEntry, sh.list);
+            const Slot slot = slot_of(turn, k);
             bool wrote = false;
             for (int j = lane; j < n_list; j += 32) {
                 const int v = slot.col[j];
@@ -921,15 +952,17 @@ __global__ void __launch_bounds__(512, 1) short_kernel(RowsArgs a, Op op, ShortS
         {
             const int k = lane / W;
             const bool mine = live >> k & 1u;
-            const unsigned int r = min(row0 + k, n_rows - 1);
-            const Slot slot = slot_at(slots + k * sh.list * kSlotEntry, sh.list);
+            const Slot slot = slot_of(turn, k);
             const RowStat st = one_part(mine ? bd.parts[k] : WarpPart{0.0, -INFINITY, -INFINITY}, off, unit, a.f);
-            auto row = look<W>(op, r, shared, slot.col, slot.z);
+            auto row = look<W>(op, in, shared, slot.col, slot.z, slot.z + sh.list);
             const RowGrad g = finish(op, a, row, st, slot.col, slot.z);
             if (lane % W == 0) bd.grads[k] = grad_const<DT>(g, st.max, a.f);
-            values<W>(op, a, r, row, g, st, slot.col, slot.z, mine);
+            values<W>(op, a, my_row(set), row, g, st, slot.col, slot.z, slot.z + sh.list, mine);
         }
         __syncwarp();
+        copy_lists(next, live_next, turn + 1);
+        in = head(op, my_row(next));
+        state = state_of(later);
         // ---- second reading ----
         if (grad) {
 #pragma unroll 1
@@ -939,7 +972,7 @@ __global__ void __launch_bounds__(512, 1) short_kernel(RowsArgs a, Op op, ShortS
                     continue;
                 }
                 const uint4* p = reinterpret_cast<const uint4*>(place + (size_t)k * sh.row_bytes);
-                const Slot slot = slot_at(slots + k * sh.list * kSlotEntry, sh.list);
+                const Slot slot = slot_of(turn, k);
                 const Grad<DT> gr(bd.grads[k], a.f);
                 T* out = static_cast<T*>(a.grad) + (int64_t)(row0 + k) * a.ld_grad;
                 uint4* ov = reinterpret_cast<uint4*>(out);
@@ -976,8 +1009,10 @@ __global__ void __launch_bounds__(512, 1) short_kernel(RowsArgs a, Op op, ShortS
         }
         __syncwarp();  // the slots have been read
         set = next;
+        next = later;
         live = live_next;
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     if (lane == 0 && *abortp) {  // gave up: let the copies already issued land before the block's memory goes away
         for (int k = 0; k < kTogether; ++k) {
             const unsigned long long t = global_timer_ns();
@@ -1035,7 +1070,8 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, bool ex, int sm_co
         ShortShape sh{};
         sh.list = (list + 3) / 4 * 4;
         sh.row_bytes = (int)row_bytes;
-        sh.warp_bytes = (int)((kTogether * row_bytes + sizeof(ShortBoard) + kTogether * sh.list * kSlotEntry + 127) / 128 * 128);
+        sh.slot_bytes = sh.list * 12;  // column, logit and the teacher's logit
+        sh.warp_bytes = (int)((kTogether * row_bytes + sizeof(ShortBoard) + 2 * kTogether * sh.slot_bytes + 127) / 128 * 128);
         sh.warps = std::min((227 * 1024 - 256) / sh.warp_bytes, 16);
         const size_t smem = std::max((size_t)sh.warps * sh.warp_bytes, (size_t)2048);
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);

@@ -575,10 +575,11 @@ __device__ __forceinline__ double shared_weight(const DistillOp& op, long long r
     return op.scale * op.inv_tau / ((op.flags & RAPID_LOSS_NORM_GIVEN) ? op.norm_z : (double)rows);
 }
 
-// What an operator does with a row, by W lanes of a warp whose other lanes do the same for other rows.  look() does, ahead of time,
-// what needs no sums over the row; finish() gives the factor once the row's log-sum-exp is there (without the chosen columns where exclude() says so), and is what the row's second
-// reading waits for; values() gives the chosen columns' gradient and writes what is kept of the row to the scratch.  col[j] and
-// z[j] are the chosen columns and their logits; z[j] become the columns' gradient.
+// What an operator does with a row, by W lanes of a warp whose other lanes do the same for other rows.  head() reads what there is to
+// read of the row in memory; look() does, ahead of time, what needs no sums over the row; finish() gives the factor once the row's
+// log-sum-exp is there (without the chosen columns where exclude() says so), and is what the row's second reading waits for; values()
+// gives the chosen columns' gradient and writes what is kept of the row to the scratch.  col[j] and z[j] are the chosen columns and
+// their logits, t[j] the teacher's; z[j] become the columns' gradient.
 __device__ __forceinline__ int list_size(const ClipOp&) { return 1; }
 __device__ __forceinline__ int list_size(const DistillOp& op) { return op.k; }
 __device__ __forceinline__ const int2* op_counts(const ClipOp& op) { return op.counts; }
@@ -590,14 +591,23 @@ __device__ __forceinline__ bool exclude(const DistillOp& op) { return op.tail !=
 __device__ __forceinline__ int column(const ClipOp& op, int64_t r, int) { return op.targets[r]; }
 __device__ __forceinline__ int column(const DistillOp& op, int64_t r, int j) { return op.index[r * op.ld + j]; }
 
-struct ClipRow {
+__device__ __forceinline__ const float* teacher(const ClipOp&, int64_t) { return nullptr; }
+__device__ __forceinline__ const float* teacher(const DistillOp& op, int64_t r) { return op.logit + r * op.ld; }
+
+struct ClipHead {
     ClipIn in;
     int seq_rows;
+};
+struct ClipRow {
+    ClipHead head;
     double w, lp;
 };
+__device__ __forceinline__ ClipHead head(const ClipOp& op, int64_t r) {
+    return ClipHead{clip_in(op, r), (op.flags & RAPID_LOSS_NORM_SEQ) ? op.seq_rows[divide(r, op.seq_len)] : 1};
+}
 template <int W>
-__device__ __forceinline__ ClipRow look(const ClipOp& op, int64_t r, double shared, const int*, const float*) {
-    return ClipRow{clip_in(op, r), (op.flags & RAPID_LOSS_NORM_SEQ) ? op.seq_rows[divide(r, op.seq_len)] : 1, shared, 0.0};
+__device__ __forceinline__ ClipRow look(const ClipOp&, const ClipHead& in, double shared, const int*, const float*, const float*) {
+    return ClipRow{in, shared, 0.0};
 }
 struct DistillRow {
     double teacher, w;
@@ -605,16 +615,17 @@ struct DistillRow {
     double list_sum;  // the list's sum of 2^(x - top's x)
     float top;        // the list's largest logit
 };
+__device__ __forceinline__ double head(const DistillOp& op, int64_t r) { return op.teacher_lse2[r]; }
 template <int W>
-__device__ __forceinline__ DistillRow look(const DistillOp& op, int64_t r, double shared, const int* col, const float* z) {
+__device__ __forceinline__ DistillRow look(const DistillOp& op, double lse2, double shared, const int* col, const float* z, const float* t) {
     const int lane = threadIdx.x % W;
-    DistillRow row{op.teacher_lse2[r], shared, 0.0, 0.0, 0.0, -INFINITY};
+    DistillRow row{lse2, shared, 0.0, 0.0, 0.0, -INFINITY};
     if (!op.tail) return row;
     double mass = 0.0;
     for (int j = lane; j < op.k; j += W) {
         if (col[j] < 0) continue;
         row.top = fmaxf(row.top, z[j]);
-        mass += exp2_short((double)op.logit[r * op.ld + j] * op.kd - row.teacher);
+        mass += exp2_short((double)t[j] * op.kd - row.teacher);
     }
     row.top = lanes_top<W>(row.top);
     row.p0 = 1.0 - lanes_sum<W>(mass);
@@ -627,12 +638,12 @@ __device__ __forceinline__ DistillRow look(const DistillOp& op, int64_t r, doubl
 }
 __device__ __forceinline__ RowGrad finish(const ClipOp& op, const RowsArgs& a, ClipRow& row, const RowStat& st, const int*, const float* z) {
     row.lp = ((double)z[0] * a.f.kd - st.lse2) * kLn2D;
-    if (op.flags & RAPID_LOSS_NORM_SEQ) row.w /= (double)row.seq_rows;
-    return RowGrad{row.w * clip_terms(op, row.in, row.lp).slope, st.lse2};
+    if (op.flags & RAPID_LOSS_NORM_SEQ) row.w /= (double)row.head.seq_rows;
+    return RowGrad{row.w * clip_terms(op, row.head.in, row.lp).slope, st.lse2};
 }
 template <int W>
 __device__ __forceinline__ void values(const ClipOp&, const RowsArgs& a, int64_t r, const ClipRow& row, const RowGrad& g, const RowStat&,
-                                       const int*, float* z, bool live) {
+                                       const int*, float* z, const float*, bool live) {
     if (threadIdx.x % W != 0 || !live) return;
     z[0] = (float)(g.a * (exp2_short(row.lp * kLog2eD) - 1.0));
     a.w.value[r] = row.lp;
@@ -652,12 +663,12 @@ __device__ __forceinline__ RowGrad finish(const DistillOp& op, const RowsArgs&, 
 }
 template <int W>
 __device__ __forceinline__ void values(const DistillOp& op, const RowsArgs& a, int64_t r, const DistillRow& row, const RowGrad& g,
-                                       const RowStat& st, const int* col, float* z, bool live) {
+                                       const RowStat& st, const int* col, float* z, const float* t, bool live) {
     const int lane = threadIdx.x % W;
     double loss = 0.0;
     for (int j = lane; j < op.k; j += W) {
         if (col[j] < 0) continue;
-        const double lt = (double)op.logit[r * op.ld + j] * op.kd - row.teacher, lq = (double)z[j] * op.kd - g.lse2;
+        const double lt = (double)t[j] * op.kd - row.teacher, lq = (double)z[j] * op.kd - g.lse2;
         const double p = exp2_short(lt);
         if (p > 0.0) loss += p * (lt - lq);
         z[j] = (float)(row.w * (exp2_short(lq) - p));
