@@ -262,8 +262,6 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
     } else if (warp == kWarps + 1) {
         // ------------------------------- once a row -----------------------------------------
         const double shared = shared_weight(op, rows_that_count(op_counts(op), op_blocks(op)));
-        const float off = shift_fraction(lane);  // of consumer warp `lane`
-        const double unit = part_unit(off);
         for (uint32_t jq = 0;; ++jq) {
             if (!warp_wait(&bd.row[jq % kQueue], (jq / kQueue) & 1u, abortp)) break;
             const int64_t r = bd.row_q[jq % kQueue];
@@ -274,7 +272,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
             if (!warp_wait(&bd.list[slot_i], jq / kSlots & 1u, abortp)) break;
             auto mine = look<32>(op, head(op, r), shared, slot.col, slot.z, teacher(op, r));
             if (!warp_wait(&bd.parts_in[s], ph, abortp)) break;
-            const RowStat st = join_parts(lane < kWarps ? bd.parts[s][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, off, unit, a.f);
+            const RowStat st = join_parts(lane < kWarps ? bd.parts[s][lane] : WarpPart{0.0, -INFINITY, -INFINITY});
             const RowGrad g = finish(op, a, mine, st, slot.col, slot.z);
             if (lane == 0) {
                 bd.grads[s] = grad_const<DT>(g, st.max, a.f);
@@ -539,8 +537,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
     const int n_list = list_size(op), id = group + 1;
     const unsigned int n_rows = (unsigned int)a.n_rows;
     const uint64_t once = policy_first();
-    const float off = shift_fraction(gw), unit_off = shift_fraction(lane);
-    const double unit = part_unit(unit_off);
+    const float off = shift_fraction(gw);
     const uint4* row_place = reinterpret_cast<const uint4*>(place);
 
     uint32_t issued = 0, phase_of = 0;  // a bit for each part: loaded by this thread, and the phase of its last load
@@ -692,7 +689,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
         RowStat st{0.0, 0.f};
         if (lane == 0) bd.parts[ph][gw] = w;
         if (group_sync<G>(id, !ok)) break;
-        if (gw == 0) st = join_parts(lane < G ? bd.parts[ph][lane] : WarpPart{0.0, -INFINITY, -INFINITY}, unit_off, unit, a.f);
+        if (gw == 0) st = join_parts(lane < G ? bd.parts[ph][lane] : WarpPart{0.0, -INFINITY, -INFINITY});
         decltype(look<32>(op, head(op, row), shared, slot.col, slot.z, teacher(op, row))) mine{};
         RowGrad g{0.0, 0.0};
         if (gw == 0) {
@@ -834,7 +831,6 @@ __global__ void __launch_bounds__(512, 1) short_kernel(RowsArgs a, Op op, ShortS
     const unsigned int n_rows = (unsigned int)a.n_rows, n_sets = (n_rows + kTogether - 1) / kTogether;
     const uint64_t once = policy_first();
     const float off = shift_fraction(0);
-    const double unit = part_unit(off);
 
     uint32_t issued = 0, phase_of = 0;  // a bit for each place: loaded by this lane, and the phase of its last load
     uint32_t ph = 0;                    // phase of each place's next load, a bit each
@@ -953,7 +949,7 @@ __global__ void __launch_bounds__(512, 1) short_kernel(RowsArgs a, Op op, ShortS
             const int k = lane / W;
             const bool mine = live >> k & 1u;
             const Slot slot = slot_of(turn, k);
-            const RowStat st = one_part(mine ? bd.parts[k] : WarpPart{0.0, -INFINITY, -INFINITY}, off, unit, a.f);
+            const RowStat st = one_part(mine ? bd.parts[k] : WarpPart{0.0, -INFINITY, -INFINITY});
             auto row = look<W>(op, in, shared, slot.col, slot.z, slot.z + sh.list);
             const RowGrad g = finish(op, a, row, st, slot.col, slot.z);
             if (lane % W == 0) bd.grads[k] = grad_const<DT>(g, st.max, a.f);
