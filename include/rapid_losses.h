@@ -84,7 +84,8 @@ typedef struct rapid_clip_desc {
     double norm_z;            /* > 0, finite with RAPID_LOSS_NORM_GIVEN; else ignored                                */
 } rapid_clip_desc_t;
 
-/* Scratch of rapid_clip_loss: 21 bytes a row, 64 bytes for each 256 rows, 4 bytes for each 1024 rows or generation, and 64 KB. */
+/* Scratch of rapid_clip_loss: 25 bytes a row and 16 for each begun 16 KB of its logits (up to four times), 4 a generation with           */
+/* RAPID_LOSS_NORM_SEQ, and 68 KB. */
 rapid_status_t rapid_clip_loss_workspace_bytes(const rapid_clip_desc_t* desc, size_t* bytes);
 
 /*
@@ -116,7 +117,7 @@ typedef struct rapid_pref_desc {
     double scale, norm_z;    /* as above                                                                             */
 } rapid_pref_desc_t;
 
-/* Scratch of rapid_preference_loss: 21 bytes a row, 64 bytes for each 256 rows, 48 a generation, 16 a pair, and 64 KB. */
+/* Scratch of rapid_preference_loss: that of rapid_clip_loss, 24 bytes a generation and 8 a pair. */
 rapid_status_t rapid_preference_loss_workspace_bytes(const rapid_pref_desc_t* desc, size_t* bytes);
 
 /*
@@ -151,7 +152,7 @@ typedef struct rapid_distill_desc {
     double scale, norm_z;
 } rapid_distill_desc_t;
 
-/* Scratch of rapid_distill_loss: 37 bytes a row, 64 bytes for each 256 rows, and 64 KB. */
+/* Scratch of rapid_distill_loss: 29 bytes a row and 68 KB. */
 rapid_status_t rapid_distill_loss_workspace_bytes(const rapid_distill_desc_t* desc, size_t* bytes);
 
 /*

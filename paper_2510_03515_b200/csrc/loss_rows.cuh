@@ -39,8 +39,7 @@ struct Header {
     int32_t pad;
 };
 
-// A warp's part of a row: its largest logit, its shift, and its sum without that logit's term, which may carry nearly all of the
-// row's probability and is put back exactly where the parts meet.
+// A warp's part of a row: its largest logit m, its shift sh and s, the sum of its 2^(x_v - sh).
 struct WarpPart {
     double s;
     float m, sh;  // sh = -inf where there is nothing

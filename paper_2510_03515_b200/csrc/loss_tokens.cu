@@ -10,8 +10,8 @@ namespace losses {
 namespace {
 
 // ---- log-probabilities -------------------------------------------------------------------------------------------
-// One to four warps for a row; each leaves its part of the row's statistics in memory and is done, without meeting the others.  Whoever needs the row joins the
-// parts, a row for each thread.  Eight 16-byte loads of every lane are in flight.
+// One to four warps for a row; each leaves its part of the row's statistics in memory and is done, without meeting the others.  Whoever
+// needs the row joins the parts, a row for each thread.  Eight 16-byte loads of every lane are in flight.
 constexpr int kStatThreads = 128;
 
 // With kKeep the logits stay in L2 as far as they fit, for the gradient's reading.

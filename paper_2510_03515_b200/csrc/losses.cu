@@ -288,6 +288,7 @@ pref_seq_kernel(PairArgs a, const float* __restrict__ ref_logp, float* __restric
         w.seq_rows[blockIdx.x] = (int)v[1];
         w.seq_bad[blockIdx.x] = (int)v[2];
         w.seq_sum[blockIdx.x] = (a.flags & RAPID_PREF_TOKEN_MEAN) && v[1] > 0.0 ? v[0] / v[1] : v[0];
+        w.seq_coef[blockIdx.x] = 0.0;  // all bits
     }
     if (!all || !is_last_block(w.head, &last)) return;
     const double by = pairs_of(a, w);
@@ -295,14 +296,51 @@ pref_seq_kernel(PairArgs a, const float* __restrict__ ref_logp, float* __restric
     for (int i = threadIdx.x >> 5; i < a.n_seq; i += kWarps) coefficient(a, w, i, by);
 }
 
+// Many pairs: every generation's slopes are added up as whole numbers, in which the order of the additions makes no difference, of
+// 2^-41 of the largest slope's power of two (2^20 pairs that all hold one generation come to 2^61 at most).  A warp for each generation
+// that goes through all pairs, as above, would be at 2^20 pairs of 2^20 generations for minutes.
 constexpr int kPairThreads = 1024;
+constexpr int kNotFinite = (int)0x80000000;  // in seq_bad, after its sum: the generation is in a pair whose slope is not finite
 __global__ void __launch_bounds__(kPairThreads) pref_pairs_kernel(PairArgs a, Scratch w) {
+    __shared__ unsigned long long top;
+    if (threadIdx.x == 0) top = 0;
     const double by = pairs_of(a, w);
-    if (threadIdx.x == 0) w.sums[0] = by;
+    __syncthreads();
+    for (int p = threadIdx.x; p < a.n_pairs; p += kPairThreads) {
+        const double x = fabs(w.pair_slope[p]);  // this thread's own
+        if (isfinite(x)) atomicMax(&top, (unsigned long long)__double_as_longlong(x));
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        int e = 0;
+        frexp(__longlong_as_double((long long)top), &e);
+        e = max(e, -900);
+        w.sums[0] = ldexp(1.0, 41 - e);
+        w.sums[1] = ldexp(by, e - 41);
+    }
+}
+__global__ void __launch_bounds__(kThreads) pref_slopes_kernel(PairArgs a, Scratch w) {
+    const int p = blockIdx.x * kThreads + threadIdx.x;
+    if (p >= a.n_pairs) return;
+    const int i = a.pairs[2 * p], j = a.pairs[2 * p + 1];
+    const double x = w.pair_slope[p];
+    if (i == j || x == 0.0) return;  // (a pair that is left out has a slope of 0)
+    if (!isfinite(x)) {
+        atomicOr(w.seq_bad + i, kNotFinite);
+        atomicOr(w.seq_bad + j, kNotFinite);
+        return;
+    }
+    const long long n = __double2ll_rn(x * w.sums[0]);
+    unsigned long long* sum = reinterpret_cast<unsigned long long*>(w.seq_coef);
+    atomicAdd(sum + i, (unsigned long long)-n);
+    atomicAdd(sum + j, (unsigned long long)n);
 }
 __global__ void __launch_bounds__(kThreads) pref_coef_kernel(PairArgs a, Scratch w) {
-    const int n = blockIdx.x * kWarps + (threadIdx.x >> 5);
-    if (n < a.n_seq) coefficient(a, w, n, w.sums[0]);
+    const int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (n >= a.n_seq) return;
+    const double s = w.seq_bad[n] < 0 ? (double)NAN : (double)__double_as_longlong(w.seq_coef[n]) * w.sums[1];
+    const int rows = w.seq_rows[n];
+    w.seq_coef[n] = (a.flags & RAPID_PREF_TOKEN_MEAN) && rows > 0 ? s / (double)rows : s;
 }
 
 }  // namespace
@@ -451,7 +489,10 @@ rapid_status_t rapid_preference_loss(const rapid_pref_desc_t* desc, const void* 
     pref_seq_kernel<<<d.n_seq, kThreads, 0, st>>>(pa, ref_logp, token_logp, all, stat_pieces(d.vocab, d.dtype), a.f, w);
     if (!all) {
         pref_pairs_kernel<<<1, kPairThreads, 0, st>>>(pa, w);
-        if (dlogits) pref_coef_kernel<<<(unsigned)(((int64_t)d.n_seq + kWarps - 1) / kWarps), kThreads, 0, st>>>(pa, w);
+        if (dlogits) {
+            pref_slopes_kernel<<<(unsigned)((d.n_pairs + kThreads - 1) / kThreads), kThreads, 0, st>>>(pa, w);
+            pref_coef_kernel<<<(unsigned)(((int64_t)d.n_seq + kThreads - 1) / kThreads), kThreads, 0, st>>>(pa, w);
+        }
     }
     if (cudaGetLastError() != cudaSuccess) return RAPID_ERR_CUDA;
     return dlogits ? cuda_status(launch_token_grads(a, targets, w.seq_coef, make_divisor(d.seq_len), st)) : RAPID_OK;

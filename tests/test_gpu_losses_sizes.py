@@ -71,7 +71,7 @@ def test_long_lists_with_a_bucket(n, length, v, dtype, k):
 
 
 @pytest.mark.parametrize("kind", ["sigmoid", "hinge", "squared"])
-@pytest.mark.parametrize("n,length,n_pairs", [(100, 3, 5000), (700, 4, 100), (2, 3, 4097), (300, 5, 4096)])
+@pytest.mark.parametrize("n,length,n_pairs", [(100, 3, 5000), (700, 4, 100), (2, 3, 4097), (300, 5, 4096), (5000, 2, 1 << 20)])
 def test_many_pairs(kind, n, length, n_pairs):
     """More pairs, or pairs times generations, than one block goes through."""
     v, dtype = 600, F32
@@ -92,6 +92,23 @@ def test_many_pairs(kind, n, length, n_pairs):
         lu.check(want, got, st, dtype, grad)
         assert st["n_pairs"] == want["valid"] and abs(st["mean_kl"] * max(1, want["valid"]) - want["won"]) < 1e-6
         assert torch.equal(got.margins.isnan(), want["margins"].isnan())
+
+
+def test_many_pairs_one_of_them_without_a_finite_slope():
+    """The token of one generation has no probability: its margins are not finite, and other generations keep their gradients."""
+    n, v = 400, 64
+    z, targets, _, g = lu.grid(n, 1, v, F32, seed=31)
+    pairs = torch.randint(0, n // 2, (5000, 2), generator=g, dtype=torch.int32).cuda()
+    z[n - 1, targets[n - 1].long()] = -math.inf
+    pairs[7] = torch.tensor([n - 1, n - 2], dtype=torch.int32)
+    keep = torch.ones(5000, dtype=torch.bool, device="cuda")
+    keep[7] = False
+    want = rb.preference_loss(z, targets, None, pairs[keep].contiguous(), n, 1, flags=rb.PREF_SQUARED | rb.LOSS_NORM_GIVEN, norm_z=5000)
+    got = rb.preference_loss(z, targets, None, pairs, n, 1, flags=rb.PREF_SQUARED)
+    assert math.isinf(float(got.margins[7])) and math.isinf(float(got.loss))
+    assert torch.equal(got.margins[keep], want.margins)
+    a, b = got.dlogits[: n // 2], want.dlogits[: n // 2]
+    assert bool(((a - b).abs() <= 2.0 ** -22 * b.abs() + 1e-12).all())  # the same slopes; a rounding of the coefficient and one of the result each
 
 
 @pytest.mark.parametrize("n,length,v,dtype", [(500, 5, 2048, BF), (6, 400, 61000, BF), (4, 600, 30001, BF)])
