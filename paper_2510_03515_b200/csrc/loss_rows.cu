@@ -530,13 +530,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
         mbar_init_fence();
     }
     if (threadIdx.x == 0) abort_flag = 0;
-    if (warp == 0) {
-        const double w = shared_weight(op, rows_that_count(op_counts(op), op_blocks(op)));
-        if (lane == 0) weight = w;
-    }
-    __syncthreads();
     volatile int* abortp = &abort_flag;
-    const double shared = weight;
     const bool grad = a.grad != nullptr, ex = exclude(op);
     const int nvec = a.vocab / E::kPer, rest = a.vocab - nvec * E::kPer, all = nvec + (rest ? 1 : 0);
     const int n_list = list_size(op), id = group + 1;
@@ -567,6 +561,12 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
         if (live)
             for (int p = 0; p < sh.parts; ++p) load_part(row, p, 0u);
     }
+    if (warp == 0) {  // while the first rows come
+        const double w = shared_weight(op, rows_that_count(op_counts(op), op_blocks(op)));
+        if (lane == 0) weight = w;
+    }
+    __syncthreads();
+    const double shared = weight;
     uint32_t ph = 0;         // phase of the parts, that is of the rows that are read
     int64_t pending = -1;    // the row whose chosen columns are still to be written
     bool ok = true;
@@ -1059,8 +1059,8 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, int sm_count, cuda
         sh.parts = (all + sh.part_vecs - 1) / sh.part_vecs;
         sh.row_bytes = (int)row_bytes;
         sh.group_bytes = (int)((row_bytes + sizeof(GroupBoard) + 2 * sh.list * kSlotEntry + 127) / 128 * 128);
-        sh.groups = std::min((227 * 1024 - 64) / sh.group_bytes, 16 / G);
-        const size_t smem = (size_t)sh.groups * sh.group_bytes;
+        sh.groups = std::min((227 * 1024 - 128) / sh.group_bytes, 16 / G);
+        const size_t smem = std::max((size_t)sh.groups * sh.group_bytes, kEndBytes);
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         const int64_t grid = std::min((int64_t)sm_count, a.n_rows);
@@ -1073,8 +1073,8 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, int sm_count, cuda
         sh.row_bytes = (int)row_bytes;
         sh.slot_bytes = sh.list * 12;  // column, logit and the teacher's logit
         sh.warp_bytes = (int)((kTogether * row_bytes + sizeof(ShortBoard) + 2 * kTogether * sh.slot_bytes + 127) / 128 * 128);
-        sh.warps = std::min((227 * 1024 - 256) / sh.warp_bytes, 16);
-        const size_t smem = std::max((size_t)sh.warps * sh.warp_bytes, (size_t)2048);
+        sh.warps = std::min((227 * 1024 - 128) / sh.warp_bytes, 16);
+        const size_t smem = std::max((size_t)sh.warps * sh.warp_bytes, kEndBytes);
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         const int64_t sets = (a.n_rows + kTogether - 1) / kTogether;
@@ -1085,6 +1085,12 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, int sm_count, cuda
         constexpr int DT = decltype(dt)::value;
         // warps for a row: as many as leave at least two groups an SM and each thread two batches (16384 x 8192 bf16 in ones 285 us, in twos
         // 246; 8192 x 32000 in fours 229, in eights 249)
+        // Few rows: as many warps for each as there are for all at once, 16 an SM (256 rows of 1000 bf16 21 -> 16 us, 512 of 4096 25 -> 18,
+        // 1024 of 4096 28 -> 21, 64 of 32000 21 -> 19; where the rows do not fit side by side it makes no difference).
+        const int64_t rows_sm = (a.n_rows + sm_count - 1) / sm_count;
+        if (row_bytes <= 110 * 1024 && rows_sm <= 2) return go_groups(group_kernel<DT, Op, 8>, 8, kBatch<8>);
+        if (row_bytes <= 55 * 1024 && rows_sm <= 4) return go_groups(group_kernel<DT, Op, 4>, 4, kBatch<4>);
+        if (row_bytes <= 27 * 1024 && rows_sm <= 8) return go_groups(group_kernel<DT, Op, 2>, 2, kBatch<2>);
         if (row_bytes <= 8192) return go_short(short_kernel<DT, Op>);
         if (row_bytes <= 32768) return go_groups(group_kernel<DT, Op, 2>, 2, kBatch<2>);
         if (row_bytes <= 73728) return go_groups(group_kernel<DT, Op, 4>, 4, kBatch<4>);

@@ -464,6 +464,8 @@ struct Totals {
     int pieces;           // the rows' statistics are still in so many parts each (0: they are not)
 };
 constexpr int64_t kFewRows = 2048;
+constexpr size_t kEndBytes = 2048;  // of shared memory that this takes: six sums of 32 warps, and a flag
+static_assert(kEndBytes >= 32 * 6 * sizeof(double) + 1, "");
 
 struct RowsArgs {
     const void* logits;
@@ -744,8 +746,7 @@ struct SumsOf<DistillOp> {
     static constexpr int kN = kDistillSums;
 };
 
-// By the last block of the rows' kernel, where there are few rows.
-// `sh`: 2 KB of shared memory.
+// By the last block of the rows' kernel, where there are few rows.  `sh`: kEndBytes of shared memory.
 template <class Op>
 __device__ __noinline__ void finish_rows(const Op& op, const RowsArgs& a, double* sh) {
     const Totals& t = a.end;
