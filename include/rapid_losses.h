@@ -85,7 +85,7 @@ typedef struct rapid_clip_desc {
 } rapid_clip_desc_t;
 
 /* Scratch of rapid_clip_loss: 25 bytes a row and 16 for each begun 16 KB of its logits (up to four times), 4 a generation with           */
-/* RAPID_LOSS_NORM_SEQ, and 68 KB. */
+/* RAPID_LOSS_NORM_SEQ, and 73 KB. */
 rapid_status_t rapid_clip_loss_workspace_bytes(const rapid_clip_desc_t* desc, size_t* bytes);
 
 /*
@@ -152,7 +152,7 @@ typedef struct rapid_distill_desc {
     double scale, norm_z;
 } rapid_distill_desc_t;
 
-/* Scratch of rapid_distill_loss: 29 bytes a row and 68 KB. */
+/* Scratch of rapid_distill_loss: 29 bytes a row and 73 KB. */
 rapid_status_t rapid_distill_loss_workspace_bytes(const rapid_distill_desc_t* desc, size_t* bytes);
 
 /*

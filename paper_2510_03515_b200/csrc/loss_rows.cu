@@ -42,6 +42,7 @@ struct Slot {
     float* z;
 };
 constexpr int kSlotEntry = 8;  // bytes of one of them
+constexpr int kSlotEntryT = 12;  // with the teacher's logit
 __device__ __forceinline__ Slot slot_at(uint8_t* base, int list) {
     float* p = reinterpret_cast<float*>(base);
     return Slot{reinterpret_cast<int*>(p), p + list};
@@ -571,7 +572,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
     int64_t pending = -1;    // the row whose chosen columns are still to be written
     bool ok = true;
     auto write_pending = [&]() {  // by the first warp, when the group has met since
-        const Slot old = slot_at(slots + (ph ^ 1u) * sh.list * kSlotEntry, sh.list);
+        const Slot old = slot_at(slots + (ph ^ 1u) * sh.list * kSlotEntryT, sh.list);
         T* out = static_cast<T*>(a.grad) + pending * a.ld_grad;
         for (int j = lane; j < n_list; j += 32) {
             const int v = old.col[j];
@@ -608,12 +609,14 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
                 for (int p = 0; p < sh.parts; ++p) load_part(row, p, ph);
             continue;
         }
-        const Slot slot = slot_at(slots + ph * sh.list * kSlotEntry, sh.list);
+        const Slot slot = slot_at(slots + ph * sh.list * kSlotEntryT, sh.list);
         if (gw == 0)
             for (int j = lane; j < n_list; j += 32) {
                 const int v = column(op, row, j);
+                if (teacher(op, row)) slot.z[sh.list + j] = teacher(op, row)[j];  // behind the slot's logits
                 slot.col[j] = v;
             }
+        const auto in = head(op, row);
         if (!grad) announce();
         // vector `at` of the row; columns behind the last read as -inf
         auto read = [&](int at) {
@@ -695,7 +698,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
         if (lane == 0) bd.parts[ph][gw] = w;
         if (group_sync<G>(id, !ok)) break;
         if (gw == 0) st = join_parts(lane < G ? bd.parts[ph][lane] : WarpPart{0.0, -INFINITY, -INFINITY});
-        decltype(look<32>(op, head(op, row), shared, slot.col, slot.z, teacher(op, row))) mine{};
+        decltype(look<32>(op, in, shared, slot.col, slot.z, slot.z)) mine{};
         RowGrad g{0.0, 0.0};
         if (gw == 0) {
             if (!ex && grad)
@@ -704,7 +707,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
                     if (v >= 0) slot.z[j] = E::get(reinterpret_cast<const T*>(place)[v]);
                 }
             __syncwarp();
-            mine = look<32>(op, head(op, row), shared, slot.col, slot.z, teacher(op, row));
+            mine = look<32>(op, in, shared, slot.col, slot.z, slot.z + sh.list);
             g = finish(op, a, mine, st, slot.col, slot.z);
             if (lane == 0) bd.grad = grad_const<DT>(g, st.max, a.f);
             if (grad) announce();
@@ -744,7 +747,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
             }
         }
         if (gw == 0) {
-            values<32>(op, a, row, mine, g, st, slot.col, slot.z, teacher(op, row), true);
+            values<32>(op, a, row, mine, g, st, slot.col, slot.z, slot.z + sh.list, true);
             __syncwarp();
             if (grad) pending = row;
         }
@@ -1058,7 +1061,7 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, int sm_count, cuda
         sh.part_vecs = ((all + kParts - 1) / kParts + unit - 1) / unit * unit;
         sh.parts = (all + sh.part_vecs - 1) / sh.part_vecs;
         sh.row_bytes = (int)row_bytes;
-        sh.group_bytes = (int)((row_bytes + sizeof(GroupBoard) + 2 * sh.list * kSlotEntry + 127) / 128 * 128);
+        sh.group_bytes = (int)((row_bytes + sizeof(GroupBoard) + 2 * sh.list * kSlotEntryT + 127) / 128 * 128);
         sh.groups = std::min((227 * 1024 - 128) / sh.group_bytes, 16 / G);
         const size_t smem = std::max((size_t)sh.groups * sh.group_bytes, kEndBytes);
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -1071,7 +1074,7 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, int sm_count, cuda
         ShortShape sh{};
         sh.list = (list + 3) / 4 * 4;
         sh.row_bytes = (int)row_bytes;
-        sh.slot_bytes = sh.list * 12;  // column, logit and the teacher's logit
+        sh.slot_bytes = sh.list * kSlotEntryT;
         sh.warp_bytes = (int)((kTogether * row_bytes + sizeof(ShortBoard) + 2 * kTogether * sh.slot_bytes + 127) / 128 * 128);
         sh.warps = std::min((227 * 1024 - 128) / sh.warp_bytes, 16);
         const size_t smem = std::max((size_t)sh.warps * sh.warp_bytes, kEndBytes);

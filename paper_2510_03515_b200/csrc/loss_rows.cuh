@@ -24,7 +24,7 @@ static_assert(sizeof(rapid_clip_desc_t) == 80 && sizeof(rapid_pref_desc_t) == 80
               "bindings rely on these");
 
 constexpr int kMaxList = 256;      // entries of a distillation list
-constexpr int kPrepBlocks = 256;   // blocks of a preparing kernel, at most
+constexpr int kPrepBlocks = 1024;  // blocks of a preparing kernel, at most
 constexpr int kSumBlocks = 1024;   // blocks of a summing kernel, at most
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -292,17 +292,21 @@ struct Part {
 };
 
 // 2^y and log2(s) in double where a whole row waits for them: Taylor's series of e^t for |t| <= ln(2) / 2 to t^11 (the rest is below
-// 7e-15) evaluated in pairs, six dependent steps; the logarithm by one step of Newton's iteration from the hardware's.  2^y below
-// 2^-1020 is 0.
+// 7e-15) evaluated in pairs, six dependent steps; the logarithm by one step of Newton's iteration from the hardware's.  No
+// branch for far arguments: the calls are inlined some ten times in a kernel whose warps are at different places of it, and what they
+// take in the instruction cache counts (with a call of exp2() for those 65536 x 4096 distillation rows took 215 us, without 194).
 __device__ __forceinline__ double exp2_short(double y) {
-    if (!(y > -1020.0 && y < 1020.0)) return y > 0.0 || y != y ? exp2(y) : 0.0;
+    const double in = y < -2100.0 ? -2100.0 : y > 2100.0 ? 2100.0 : y;
     // the nearest whole number by adding 1.5 2^52, in whose low word it then stands: no conversion, which would be a slow one
-    const double up = y + 6755399441055744.0, n = up - 6755399441055744.0;
-    const double t = (y - n) * kLn2D, t2 = t * t, t4 = t2 * t2;
+    const double up = in + 6755399441055744.0, n = up - 6755399441055744.0;
+    const double t = (in - n) * kLn2D, t2 = t * t, t4 = t2 * t2;
     const double a0 = 1.0 + t, a1 = fma(t, 1.0 / 6, 0.5), a2 = fma(t, 1.0 / 120, 1.0 / 24), a3 = fma(t, 1.0 / 5040, 1.0 / 720);
     const double a4 = fma(t, 1.0 / 362880, 1.0 / 40320), a5 = fma(t, 1.0 / 39916800, 1.0 / 3628800);
     const double b0 = fma(a1, t2, a0), b1 = fma(a3, t2, a2), b2 = fma(a5, t2, a4);
-    return fma(b2, t4 * t4, fma(b1, t4, b0)) * __hiloint2double((__double2loint(up) + 1023) << 20, 0);
+    // 2^n in two factors, the last of which overflows or underflows where the result does (of NaN, t is NaN)
+    const int e = __double2loint(up), half = e >> 1, rest = e - half;
+    const double lo = __hiloint2double((min(max(half, -1022), 1023) + 1023) << 20, 0), hi = __hiloint2double((min(max(rest, -1022), 1023) + 1023) << 20, 0);
+    return fma(b2, t4 * t4, fma(b1, t4, b0)) * lo * hi;
 }
 __device__ __forceinline__ double log2_short(double s) {  // s > 0, normal
     const int e = (__double2hiint(s) >> 20) - 1023;

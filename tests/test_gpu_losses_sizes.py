@@ -21,7 +21,7 @@ def _ragged(n, length, seed):
 # on both sides of every length at which rows go to another kernel (bytes of a row: 8, 32, 72, 110 and 172 KB)
 EDGES = [(b, d) for b in (8192, 32768, 73728, 112640, 176128) for d in (-16, 0, 16)]
 # more rows than one block sums, more generations than one block counts, rows enough for every warp to take several
-MANY = [(9, 300, 500, F32), (33, 70, 4096, BF), (700, 5, 1030, BF), (5, 501, 16390, BF), (4, 600, 30001, BF), (3, 701, 50257, BF),
+MANY = [(9, 300, 500, F32), (33, 70, 4096, BF), (700, 5, 1030, BF), (1100, 3, 500, F32), (5, 501, 16390, BF), (4, 600, 30001, BF), (3, 701, 50257, BF),
         (5, 430, 61000, BF), (3, 700, 33001, F32), (2, 1051, 90001, BF)]
 
 
