@@ -574,6 +574,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
     auto write_pending = [&]() {  // by the first warp, when the group has met since
         const Slot old = slot_at(slots + (ph ^ 1u) * sh.list * kSlotEntryT, sh.list);
         T* out = static_cast<T*>(a.grad) + pending * a.ld_grad;
+#pragma unroll 1
         for (int j = lane; j < n_list; j += 32) {
             const int v = old.col[j];
             if (v >= 0) out[v] = E::put(old.z[j]);
@@ -611,6 +612,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
         }
         const Slot slot = slot_at(slots + ph * sh.list * kSlotEntryT, sh.list);
         if (gw == 0)
+#pragma unroll 1
             for (int j = lane; j < n_list; j += 32) {
                 const int v = column(op, row, j);
                 if (teacher(op, row)) slot.z[sh.list + j] = teacher(op, row)[j];  // behind the slot's logits
@@ -663,6 +665,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
             const int from = q * sh.part_vecs, end = min(from + sh.part_vecs, all);
             if (ex) {  // the list's columns of this warp's vectors: their logits are noted and leave the sum
                 bool wrote = false;
+#pragma unroll 1
                 for (int j = lane; j < n_list; j += 32) {
                     const int v = column(op, row, j), at = v / E::kPer;
                     if (v >= 0 && at >= from && at < end && (at - from) % kLanes / 32 == gw) {
@@ -675,6 +678,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
                 if (wrote) fence_proxy_async_smem();  // a bulk copy writes there next
                 __syncwarp();
             } else if (!grad && gw == 0) {  // before the part goes
+#pragma unroll 1
                 for (int j = lane; j < n_list; j += 32) {
                     const int v = slot.col[j], at = v / E::kPer;
                     if (v >= 0 && at >= from && at < end) slot.z[j] = E::get(reinterpret_cast<const T*>(place)[v]);
@@ -687,6 +691,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
                 for (int j = 0; j < U; ++j) w[j] = row_place[v + j * kLanes];
                 p.template vectors<DT, U>(w, off, a.f);
             }
+#pragma unroll 1
             for (; v - lane < end; v += kLanes) {
                 uint4 w[1] = {read(v)};
                 p.template vectors<DT, 1>(w, off, a.f);
@@ -702,6 +707,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
         RowGrad g{0.0, 0.0};
         if (gw == 0) {
             if (!ex && grad)
+#pragma unroll 1
                 for (int j = lane; j < n_list; j += 32) {
                     const int v = slot.col[j];
                     if (v >= 0) slot.z[j] = E::get(reinterpret_cast<const T*>(place)[v]);
@@ -730,6 +736,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
 #pragma unroll
                     for (int j = 0; j < U; ++j) st_stream(ov + v + j * kLanes, gr.vector(w[j]));
                 }
+#pragma unroll 1
                 for (; v - lane < end; v += kLanes) {
                     const uint4 y = gr.vector(read(v));
                     if (v < nvec) st_stream(ov + v, y);
@@ -924,6 +931,7 @@ __global__ void __launch_bounds__(512, 1) short_kernel(RowsArgs a, Op op, ShortS
             const uint4* p = reinterpret_cast<const uint4*>(row);
             const Slot slot = slot_of(turn, k);
             bool wrote = false;
+#pragma unroll 1
             for (int j = lane; j < n_list; j += 32) {
                 const int v = slot.col[j];
                 if (v < 0) continue;
@@ -942,6 +950,7 @@ __global__ void __launch_bounds__(512, 1) short_kernel(RowsArgs a, Op op, ShortS
                 for (int j = 0; j < U; ++j) q[j] = p[v + j * 32];
                 part.template vectors<DT, U>(q, off, a.f);
             }
+#pragma unroll 1
             for (; v - lane < all; v += 32) {
                 uint4 q[1] = {read(p, v)};
                 part.template vectors<DT, 1>(q, off, a.f);
@@ -988,6 +997,7 @@ __global__ void __launch_bounds__(512, 1) short_kernel(RowsArgs a, Op op, ShortS
 #pragma unroll
                     for (int j = 0; j < U; ++j) st_stream(ov + v + j * 32, gr.vector(q[j]));
                 }
+#pragma unroll 1
                 for (; v - lane < all; v += 32) {
                     const uint4 y = gr.vector(read(p, v));
                     if (v < nvec) st_stream(ov + v, y);
@@ -1002,6 +1012,7 @@ __global__ void __launch_bounds__(512, 1) short_kernel(RowsArgs a, Op op, ShortS
                     }
                 }
                 hand_over(k);
+#pragma unroll 1
                 for (int j = lane; j < n_list; j += 32) {  // the chosen columns over the vectors
                     const int c = slot.col[j];
                     if (c >= 0) out[c] = E::put(slot.z[j]);

@@ -605,6 +605,7 @@ __device__ __forceinline__ DistillRow look(const DistillOp& op, double lse2, dou
     DistillRow row{lse2, shared, 0.0, 0.0, 0.0, -INFINITY};
     if (!op.tail) return row;
     double mass = 0.0;
+#pragma unroll 1
     for (int j = lane; j < op.k; j += W) {
         if (col[j] < 0) continue;
         row.top = fmaxf(row.top, z[j]);
@@ -614,6 +615,7 @@ __device__ __forceinline__ DistillRow look(const DistillOp& op, double lse2, dou
     row.p0 = 1.0 - lanes_sum<W>(mass);
     if (row.p0 > 0.0) row.lp0 = log2_short(row.p0);
     if (row.top > -INFINITY)
+#pragma unroll 1
         for (int j = lane; j < op.k; j += W)
             if (col[j] >= 0) row.list_sum += exp2_short(((double)z[j] - (double)row.top) * op.kd);
     row.list_sum = lanes_sum<W>(row.list_sum);
@@ -649,6 +651,7 @@ __device__ __forceinline__ void values(const DistillOp& op, const RowsArgs& a, i
                                        const RowStat& st, const int* col, float* z, const float* t, bool live) {
     const int lane = threadIdx.x % W;
     double loss = 0.0;
+#pragma unroll 1
     for (int j = lane; j < op.k; j += W) {
         if (col[j] < 0) continue;
         const double lt = (double)t[j] * op.kd - row.teacher, lq = (double)z[j] * op.kd - g.lse2;
