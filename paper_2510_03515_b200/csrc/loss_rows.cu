@@ -13,10 +13,11 @@
 //
 // Every wait on a barrier is bounded; a wait that gives up raises RAPID_ERR_TIMEOUT in the scratch and never traps.
 //
-// What bounds it: the bytes, at full length (8 x 1024 ragged rows of 151936 bf16: 645 us, 0.95 of a copy's rate; with lists of 64 and a
-// bucket 693, 0.89).  Where all rows count, the two sweeps do: an element costs two exponentials and some ten instructions (4096 rows
-// of 151936: 462 us, 0.83).
+// What bounds it: the bytes, at full length (8 x 1024 ragged rows of 151936 bf16: 640 us, 0.95 of a copy's rate; with lists of 64 and a
+// bucket 682, 0.90).  Where all rows count, the two sweeps do: an element costs two exponentials and some ten instructions (4096 rows
+// of 151936: 453 us, 0.85).
 #include <algorithm>
+#include <type_traits>
 
 #include "loss_rows.cuh"
 #include "tma_pipe.cuh"
@@ -42,7 +43,9 @@ struct Slot {
     float* z;
 };
 constexpr int kSlotEntry = 8;  // bytes of one of them
-constexpr int kSlotEntryT = 12;  // with the teacher's logit
+// With the teacher's logits behind them, where there is a teacher (12 bytes for all would cost clip at 16384 bf16 one of its seven groups).
+template <class Op>
+constexpr int kSlotEntryT = std::is_same<Op, DistillOp>::value ? 12 : 8;
 __device__ __forceinline__ Slot slot_at(uint8_t* base, int list) {
     float* p = reinterpret_cast<float*>(base);
     return Slot{reinterpret_cast<int*>(p), p + list};
@@ -469,7 +472,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
 // side by side on an SM and hide one another's latencies.  A row comes in kParts bulk copies; the last warp to have read a part for the
 // last time has the next row's part loaded in its place, so the warps meet only twice a row: to join their sums, and for the
 // factor.  Rows are drawn from a counter, two ahead.  An element's instructions, and the two meetings, bound it: 32768 rows of 8192
-// bf16 take 239 us (0.69 of a copy's rate), 16384 of 16384 209 (0.80), 8192 of 32000 231 (0.70), 8192 of 50000 317 (0.80).
+// bf16 take 230 us (0.72 of a copy's rate), 16384 of 16384 216 (0.77), 8192 of 32000 224 (0.72), 8192 of 50000 308 (0.82).
 
 constexpr int kParts = 2;
 
@@ -572,7 +575,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
     int64_t pending = -1;    // the row whose chosen columns are still to be written
     bool ok = true;
     auto write_pending = [&]() {  // by the first warp, when the group has met since
-        const Slot old = slot_at(slots + (ph ^ 1u) * sh.list * kSlotEntryT, sh.list);
+        const Slot old = slot_at(slots + (ph ^ 1u) * sh.list * kSlotEntryT<Op>, sh.list);
         T* out = static_cast<T*>(a.grad) + pending * a.ld_grad;
 #pragma unroll 1
         for (int j = lane; j < n_list; j += 32) {
@@ -610,7 +613,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
                 for (int p = 0; p < sh.parts; ++p) load_part(row, p, ph);
             continue;
         }
-        const Slot slot = slot_at(slots + ph * sh.list * kSlotEntryT, sh.list);
+        const Slot slot = slot_at(slots + ph * sh.list * kSlotEntryT<Op>, sh.list);
         if (gw == 0)
 #pragma unroll 1
             for (int j = lane; j < n_list; j += 32) {
@@ -784,8 +787,8 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
 
 // Up to 8 KB a warp holds two rows at a time: it reads them one after the other, then does what is done once a row for both of them
 // at once, half a warp each, and writes them one after the other.  That arithmetic, one value a row in double, is a chain of some
-// thousands of cycles in which a warp that holds one row does nothing else: 65536 rows of 4096 bf16 with 8 entries take 240 us, with
-// one row a warp they took 300, and four rows, which leave six warps an SM, 297.
+// thousands of cycles in which a warp that holds one row does nothing else: when 65536 rows of 4096 bf16 with 8 entries took 240 us so,
+// they took 300 with one row a warp, and 297 with four, which leave six warps an SM.  Now 208; floor 146.
 constexpr int kTogether = 2;
 
 struct ShortShape {
@@ -1072,7 +1075,7 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, int sm_count, cuda
         sh.part_vecs = ((all + kParts - 1) / kParts + unit - 1) / unit * unit;
         sh.parts = (all + sh.part_vecs - 1) / sh.part_vecs;
         sh.row_bytes = (int)row_bytes;
-        sh.group_bytes = (int)((row_bytes + sizeof(GroupBoard) + 2 * sh.list * kSlotEntryT + 127) / 128 * 128);
+        sh.group_bytes = (int)((row_bytes + sizeof(GroupBoard) + 2 * sh.list * kSlotEntryT<Op> + 127) / 128 * 128);
         sh.groups = std::min((227 * 1024 - 128) / sh.group_bytes, 16 / G);
         const size_t smem = std::max((size_t)sh.groups * sh.group_bytes, kEndBytes);
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -1085,7 +1088,7 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, int sm_count, cuda
         ShortShape sh{};
         sh.list = (list + 3) / 4 * 4;
         sh.row_bytes = (int)row_bytes;
-        sh.slot_bytes = sh.list * kSlotEntryT;
+        sh.slot_bytes = sh.list * kSlotEntryT<Op>;
         sh.warp_bytes = (int)((kTogether * row_bytes + sizeof(ShortBoard) + 2 * kTogether * sh.slot_bytes + 127) / 128 * 128);
         sh.warps = std::min((227 * 1024 - 128) / sh.warp_bytes, 16);
         const size_t smem = std::max((size_t)sh.warps * sh.warp_bytes, kEndBytes);
