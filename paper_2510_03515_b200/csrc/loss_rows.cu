@@ -146,7 +146,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
 
     if (warp == kWarps) {
         // ------------------------------- producer -------------------------------------------
-        const int load_bytes = (nvec + (rest ? 1 : 0)) * 16;  // inside the row: its pitch is a multiple of 16 bytes
+        const int all = nvec + (rest ? 1 : 0);  // vectors, inside the row: its pitch is a multiple of 16 bytes (which can be 4 GiB)
         const uint64_t first = policy_first(), normal = policy_normal();
         uint32_t it = 0, q = 0, zq = 0;
         bool ok = true;
@@ -155,7 +155,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
             const uint32_t use = it / sh.stages;
             if (use > 0 && !warp_wait(&bd.empty[s], (use & 1u) ^ 1u, abortp)) return false;
             if (lane == 0) {
-                const int bytes = min(kChunk, load_bytes - c * kChunk);
+                const int bytes = min(kChunkVecs, all - c * kChunkVecs) * 16;
                 mbar_arrive_expect_tx(&bd.full[s], (uint32_t)bytes);
                 bulk_load_once(ring + (size_t)s * kChunk, src + (size_t)c * kChunk, (uint32_t)bytes, &bd.full[s], more ? normal : first);
             }
