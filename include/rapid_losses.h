@@ -72,7 +72,7 @@ typedef struct rapid_loss_stats {
 /* ---- clipped policy loss ----------------------------------------------------------------------------------- */
 
 typedef struct rapid_clip_desc {
-    int32_t n_seq, seq_len;   /* N generations of L padded positions, T = N * L rows (at most 2^31 - 1)              */
+    int32_t n_seq, seq_len;   /* N generations of L padded positions, T = N * L rows (at most 2^31 - 1024)           */
     int32_t vocab;            /* V                                                                                   */
     int32_t dtype;            /* rapid_dtype_t of logits and dlogits                                                 */
     int64_t ld, ld_grad;      /* row pitches, in elements, of logits and dlogits, >= vocab                           */
@@ -141,7 +141,7 @@ rapid_status_t rapid_preference_loss(const rapid_pref_desc_t* desc, const void* 
 /* ---- distillation from a teacher's top logits --------------------------------------------------------------- */
 
 typedef struct rapid_distill_desc {
-    int64_t n_rows;      /* T, 1 .. 2^31 - 1                                                                         */
+    int64_t n_rows;      /* T, 1 .. 2^31 - 1024                                                                      */
     int32_t vocab;       /* V                                                                                        */
     int32_t k;           /* K, entries of a row's list, 1 .. 256                                                     */
     int64_t ld, ld_grad; /* as above                                                                                 */

@@ -26,6 +26,7 @@ static_assert(sizeof(rapid_clip_desc_t) == 80 && sizeof(rapid_pref_desc_t) == 80
 constexpr int kMaxList = 256;      // entries of a distillation list
 constexpr int kPrepBlocks = 1024;  // blocks of a preparing kernel, at most
 constexpr int kSumBlocks = 1024;   // blocks of a summing kernel, at most
+constexpr int64_t kMaxRows = 0x7fffffffll - 1023;  // a position plus a block's threads stays within 31 bits
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline size_t elem_size(int32_t dtype) { return dtype == RAPID_BF16 ? 2 : 4; }
@@ -125,8 +126,8 @@ inline rapid_status_t check_shape(int64_t T, int32_t vocab, int32_t dtype, int64
     if (dtype != RAPID_F32 && dtype != RAPID_BF16) return RAPID_ERR_INVALID_ARG;
     if ((flags & ~known) || !isfinite(scale)) return RAPID_ERR_INVALID_ARG;
     if ((flags & RAPID_LOSS_NORM_GIVEN) && !(norm_z > 0.0 && isfinite(norm_z))) return RAPID_ERR_INVALID_ARG;
-    // 2^56 elements are far beyond any device's memory; keeps every size below in 64 bits
-    if (T > 0x7fffffffll || vocab > (1 << 30) || ld > (1ll << 56) / T || ld_grad > (1ll << 56) / T) return RAPID_ERR_UNSUPPORTED;
+    // 2^56 elements are far beyond any device's memory; keeps every offset of an element in 64 bits
+    if (T > kMaxRows || vocab > (1 << 30) || ld > (1ll << 56) / T || ld_grad > (1ll << 56) / T) return RAPID_ERR_UNSUPPORTED;
     const size_t es = elem_size(dtype);
     if ((size_t)ld * es % 16 != 0 || (size_t)ld_grad * es % 16 != 0) return RAPID_ERR_ALIGNMENT;
     return RAPID_OK;

@@ -1,0 +1,25 @@
+"""Losses over the logits, host side: the largest sizes that are accepted and the first that are not (no GPU needed: a call that passes
+every check stops at the missing device)."""
+import pytest
+
+from paper_2510_03515_b200 import binding as rb
+from test_losses_host import KINDS, _call, _desc, no_gpu
+
+MOST = 2 ** 31 - 1024  # rows
+
+
+@no_gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_the_most_rows(kind):
+    for n, length in ((1, MOST), (1 << 10, MOST >> 10)):
+        d = _desc(kind, n=n, length=length, v=1, ld=8)
+        assert _call(kind, d, dlogits=None, logits=1 << 48) == rb.RAPID_ERR_CUDA
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_rows_whose_numbers_would_pass_31_bits_within_a_block(kind):
+    for n, length in ((1, MOST + 1), (1, 2 ** 31 - 1), ((2 ** 31 - 1) // 7, 7)):
+        d = _desc(kind, n=n, length=length, v=1, ld=8)
+        assert _call(kind, d, dlogits=None, logits=1 << 48) == rb.RAPID_ERR_UNSUPPORTED
+        with pytest.raises(rb.RapidError):
+            getattr(rb, f"rapid_{kind}_loss_workspace_bytes")(d)
