@@ -119,7 +119,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
         for (int s = 0; s < sh.stages; ++s) {
             mbar_init(&bd.full[s], 1);
             mbar_init(&bd.ready[s], 1);
-            mbar_init(&bd.empty[s], kWarps);
+            mbar_init(&bd.empty[s], kWarps + (exclude(op) ? 1 : 0));  // the list's warp waits for the stages too
         }
         for (int q = 0; q < kQueue; ++q) mbar_init(&bd.row[q], 1);
         for (int q = 0; q < kZeros; ++q) {
@@ -243,8 +243,8 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
             __syncwarp();
             if (lane == 0) mbar_arrive(&bd.list[s]);
             if (!ex) continue;
-            // the list's columns are taken out of the sum; chunks loaded again come without: what is written for these columns is
-            // written over
+            // The list's columns are taken out of the sum; chunks loaded again come without: what is written for these columns is
+            // written over.  Every stage is given back, those too: a wait for a stage's phase holds only until its next one.
             for (int c = 0; c < sh.chunks + sh.again; ++c) {
                 if (!(ok = warp_wait(&bd.full[st], ph, abortp))) break;
                 if (c < sh.chunks) {
@@ -261,6 +261,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bd.ready[st]);
                 }
+                if (lane == 0) mbar_arrive(&bd.empty[st]);
                 if (++st == sh.stages) {
                     st = 0;
                     ph ^= 1u;
