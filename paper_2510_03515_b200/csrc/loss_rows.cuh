@@ -227,6 +227,18 @@ struct Elem<RAPID_F32> {
 constexpr float kEx2Mean = -4.95e-8f;
 constexpr float kNothing = -1.0e38f;  // at or below: -inf or the lowest finite value, a masked part of the vocabulary
 
+// Both halves of a packed pair of bf16 values, each with a float added to it, in one instruction each.
+__device__ __forceinline__ uint64_t bf16x2_plus(uint32_t p, float b) {
+    float lo, hi;
+    asm("{\n\t.reg .b16 l, h;\n\t"
+        "mov.b32 {l, h}, %2;\n\t"
+        "add.rn.f32.bf16 %0, l, %3;\n\t"
+        "add.rn.f32.bf16 %1, h, %3;\n\t}"
+        : "=f"(lo), "=f"(hi)
+        : "r"(p), "f"(b));
+    return f32x2(lo, hi);
+}
+
 // One thread's part of a row: the largest logit m, the shift sh that its exponentials are taken against, and sum_v 2^(x_v - sh)
 // with the rounding errors of its additions beside it.  sh = ceil(m k) + off is used as it stands, here and where the parts meet,
 // so no rounding of m k enters; `off`, a 16-bit fraction, is one for a warp (the parts of its lanes differ by exact powers of two)
@@ -392,10 +404,10 @@ __device__ __forceinline__ float shift_fraction(int warp) { return (float)(((uns
 
 // ---- a row's gradient --------------------------------------------------------------------------------------------
 
-// dz_v = a 2^(x_v - lse2).  bf16: |a| goes into the exponent, one multiply-add and one exponential an element.  float: the largest
-// logit is taken off first, which keeps the argument small and so its rounding below the result's; a is multiplied at the end.
-// The constants are formed once a row; they are floats, whose rounding (and the error of the hardware's logarithm, 2^-22) is some
-// 2^-18 of a probability at most.
+// dz_v = a 2^(x_v - lse2).  The largest logit m is taken off first, which keeps the argument (z_v - m) k + c small whatever the logits'
+// size, and so its rounding below the result's: c is some 2^7 at most, so the argument is off by 2^-18 of a probability.  bf16: |a| goes
+// into c too, and an element costs an addition (which widens it as well), a multiply-add and an exponential.  float: a is multiplied at the
+// end.  The constants are formed once a row; the hardware's logarithm is off by 2^-22.
 struct RowGrad {
     double a, lse2;
 };
@@ -406,13 +418,13 @@ template <int DT>
 __device__ __forceinline__ GradConst grad_const(const RowGrad& g, float max, const Factor& f) {
     GradConst k;
     k.a = (float)g.a;
+    k.m = max > kNothing ? max : 0.f;
+    const double c = (double)k.m * f.kd - g.lse2;
     if (DT == RAPID_BF16) {
-        k.m = 0.f;
-        k.c = (float)((double)__log2f(fabsf(k.a)) - g.lse2);
+        k.c = (float)(c + (double)__log2f(fabsf(k.a)));
         if (k.a == 0.f) k.c = -INFINITY;
     } else {
-        k.m = max > kNothing ? max : 0.f;
-        k.c = (float)((double)k.m * f.kd - g.lse2);
+        k.c = (float)c;
     }
     return k;
 }
@@ -420,9 +432,9 @@ template <int DT>
 struct Grad;
 template <>
 struct Grad<RAPID_BF16> {
-    float k, c;
+    float k, c, nm;
     uint32_t sign;  // of a, on both halves of a pair
-    __device__ __forceinline__ Grad(const GradConst& g, const Factor& f) : k(f.k), c(g.c), sign(g.a < 0.f ? 0x80008000u : 0u) {}
+    __device__ __forceinline__ Grad(const GradConst& g, const Factor& f) : k(f.k), c(g.c), nm(-g.m), sign(g.a < 0.f ? 0x80008000u : 0u) {}
     __device__ __forceinline__ uint4 vector(const uint4& q) const {
         const uint32_t in[4] = {q.x, q.y, q.z, q.w};
         uint32_t out[4];
@@ -430,13 +442,13 @@ struct Grad<RAPID_BF16> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float x0, x1;
-            f32x2_split(f32x2_fma(f32x2(bf16_lo(in[i]), bf16_hi(in[i])), k2, c2), x0, x1);
+            f32x2_split(f32x2_fma(bf16x2_plus(in[i], nm), k2, c2), x0, x1);
             out[i] = pack_bf16x2(ex2_approx(x0), ex2_approx(x1)) ^ sign;
         }
         return make_uint4(out[0], out[1], out[2], out[3]);
     }
     __device__ __forceinline__ uint16_t one(uint16_t z) const {
-        return (uint16_t)(Elem<RAPID_BF16>::put(ex2_approx(fmaf(Elem<RAPID_BF16>::get(z), k, c))) ^ (uint16_t)sign);
+        return (uint16_t)(Elem<RAPID_BF16>::put(ex2_approx(fmaf(Elem<RAPID_BF16>::get(z) + nm, k, c))) ^ (uint16_t)sign);
     }
 };
 template <>
