@@ -608,7 +608,7 @@ __device__ __forceinline__ ClipRow look(const ClipOp&, const ClipHead& in, doubl
 struct DistillRow {
     double teacher, w;
     double p0, lp0;   // probability of the tokens beside the list, and its logarithm
-    double list_sum;  // the list's sum of 2^(x - top's x)
+    double list_sum;  // the list's sum of 2^(x - top's x); after finish() the student's log-sum-exp over the whole vocabulary
     float top;        // the list's largest logit
 };
 __device__ __forceinline__ double head(const DistillOp& op, int64_t r) { return op.teacher_lse2[r]; }
@@ -647,33 +647,45 @@ __device__ __forceinline__ void values(const ClipOp&, const RowsArgs& a, int64_t
     a.w.value[r] = row.lp;
 }
 
+// The columns outside the list: w (q_v - p_0 q_v / q_0).  Where the student has less mass there than the teacher, p_0 / q_0 is above one and
+// may be beyond any type (a student that is sure of the list, or whose other columns are masked by a large negative number), while
+// the gradient is not: it is then a factor w p_0 (q_0 / p_0 - 1) of the softmax over these columns alone, which st.lse2 belongs to.
 __device__ __forceinline__ RowGrad finish(const DistillOp& op, const RowsArgs&, DistillRow& row, const RowStat& st, const int*, const float*) {
     RowGrad g{row.w, st.lse2};
-    if (!op.tail) return g;
-    // the student's log-sum-exp over the whole vocabulary, in a sum against the larger of the rest's and the list's largest term
+    double& lse2 = row.list_sum;
+    if (!op.tail) {
+        lse2 = st.lse2;
+        return g;
+    }
+    // the student's log-sum-exp, in a sum against the larger of the rest's and the list's largest term
     const double x0 = row.top > -INFINITY ? (double)row.top * op.kd : -INFINITY;
     const double top = fmax(st.lse2, x0);
     if (top == -INFINITY) return g;
     // (the list's sum holds its largest term, 1, so neither logarithm's argument is small)
-    g.lse2 = top + log2_short(row.list_sum * exp2_short(x0 - top) + exp2_short(st.lse2 - top));
-    if (row.p0 > 0.0 && st.lse2 > -INFINITY) g.a = row.w * (1.0 - exp2_short(row.lp0 - (st.lse2 - g.lse2)));
+    lse2 = g.lse2 = top + log2_short(row.list_sum * exp2_short(x0 - top) + exp2_short(st.lse2 - top));
+    if (row.p0 > 0.0 && st.lse2 > -INFINITY) {
+        const double over = row.lp0 - (st.lse2 - lse2);  // log2 of p_0 / q_0
+        const double one = 1.0 - exp2_short(-fabs(over));
+        if (over > 0.0) g = RowGrad{-row.w * row.p0 * one, st.lse2};
+        else g.a = row.w * one;
+    }
     return g;
 }
 template <int W>
-__device__ __forceinline__ void values(const DistillOp& op, const RowsArgs& a, int64_t r, const DistillRow& row, const RowGrad& g,
+__device__ __forceinline__ void values(const DistillOp& op, const RowsArgs& a, int64_t r, const DistillRow& row, const RowGrad&,
                                        const RowStat& st, const int* col, float* z, const float* t, bool live) {
     const int lane = threadIdx.x % W;
     double loss = 0.0;
 #pragma unroll 1
     for (int j = lane; j < op.k; j += W) {
         if (col[j] < 0) continue;
-        const double lt = (double)t[j] * op.kd - row.teacher, lq = (double)z[j] * op.kd - g.lse2;
+        const double lt = (double)t[j] * op.kd - row.teacher, lq = (double)z[j] * op.kd - row.list_sum;
         const double p = exp2_short(lt);
         if (p > 0.0) loss += p * (lt - lq);
         z[j] = (float)(row.w * (exp2_short(lq) - p));
     }
     loss = lanes_sum<W>(loss);
-    if (row.p0 > 0.0) loss += row.p0 * (row.lp0 - (st.lse2 - g.lse2));
+    if (row.p0 > 0.0) loss += row.p0 * (row.lp0 - (st.lse2 - row.list_sum));
     if (lane == 0 && live) a.w.value[r] = loss * kLn2D;
 }
 
