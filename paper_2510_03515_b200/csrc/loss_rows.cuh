@@ -407,7 +407,8 @@ __device__ __forceinline__ float shift_fraction(int warp) { return (float)(((uns
 // dz_v = a 2^(x_v - lse2).  The largest logit m is taken off first, which keeps the argument (z_v - m) k + c small whatever the logits'
 // size, and so its rounding below the result's: c is some 2^7 at most, so the argument is off by 2^-18 of a probability.  bf16: |a| goes
 // into c too, and an element costs an addition (which widens it as well), a multiply-add and an exponential.  float: a is multiplied at the
-// end.  The constants are formed once a row; the hardware's logarithm is off by 2^-22.
+// end, but for powers of two above one, which go into c: a factor may be beyond the floats (a ratio of e^90) where its products with small
+// probabilities are not, and its product with none is 0.  The constants are formed once a row; the hardware's logarithm is off by 2^-22.
 struct RowGrad {
     double a, lse2;
 };
@@ -417,15 +418,14 @@ struct GradConst {
 template <int DT>
 __device__ __forceinline__ GradConst grad_const(const RowGrad& g, float max, const Factor& f) {
     GradConst k;
-    k.a = (float)g.a;
     k.m = max > kNothing ? max : 0.f;
-    const double c = (double)k.m * f.kd - g.lse2;
-    if (DT == RAPID_BF16) {
-        k.c = (float)(c + (double)__log2f(fabsf(k.a)));
-        if (k.a == 0.f) k.c = -INFINITY;
-    } else {
-        k.c = (float)c;
-    }
+    const double a = g.a > 1e300 ? 1e300 : g.a < -1e300 ? -1e300 : g.a;  // (NaN stays)
+    int e = ((__double2hiint(a) >> 20) & 0x7ff) - 1023;                  // |a| < 2^(e + 1)
+    if (DT == RAPID_F32 && e < 0) e = 0;
+    k.a = (float)(a * __hiloint2double(::max(1023 - e, 1) << 20, 0));      // a 2^-e
+    double c = (double)k.m * f.kd - g.lse2 + (double)e;
+    if (DT == RAPID_BF16) c += (double)__log2f(fabsf(k.a));  // of 0: -inf
+    k.c = (float)c;
     return k;
 }
 template <int DT>
