@@ -30,7 +30,8 @@
  * Bases of logits and dlogits are 16-byte aligned and their pitches multiples of 16 bytes; int32 and float arrays lie on 4-byte
  * boundaries, stats on an 8-byte one.  `scale` multiplies the loss and its gradient.
  *
- * Sums over the vocabulary are formed in float pieces that are added in double, everything of one value a row is double.
+ * Sums over the vocabulary are formed in float pieces that are added in double, everything of one value a row, a pair or a generation is
+ * double (sums over a generation's pairs, where there are many, whole numbers of 2^-83 of the largest of them).
  */
 #ifndef RAPID_LOSSES_H
 #define RAPID_LOSSES_H
@@ -117,7 +118,7 @@ typedef struct rapid_pref_desc {
     double scale, norm_z;    /* as above                                                                             */
 } rapid_pref_desc_t;
 
-/* Scratch of rapid_preference_loss: that of rapid_clip_loss, 24 bytes a generation and 8 a pair. */
+/* Scratch of rapid_preference_loss: that of rapid_clip_loss, 32 bytes a generation and 8 a pair. */
 rapid_status_t rapid_preference_loss_workspace_bytes(const rapid_pref_desc_t* desc, size_t* bytes);
 
 /*

@@ -58,6 +58,7 @@ struct Scratch {
     int32_t* seq_bad;     // [N] rows that are not valid
     double* seq_sum;      // [N] s_n
     double* seq_coef;     // [N] g_n
+    unsigned long long* seq_top;  // [N] the largest slope of its pairs, where there are many
     double* pair_slope;   // [P]
     double* teacher_lse2; // [T]
     WarpPart* parts;      // [T][pieces] of rows that are read without a gradient
@@ -95,6 +96,7 @@ inline size_t carve(int64_t T, int64_t N, int64_t P, int pieces, int need, void*
         s.seq_bad = reinterpret_cast<int32_t*>(take((size_t)N * 4));
         s.seq_sum = reinterpret_cast<double*>(take((size_t)N * 8));
         s.seq_coef = reinterpret_cast<double*>(take((size_t)N * 8));
+        s.seq_top = reinterpret_cast<unsigned long long*>(take((size_t)N * 8));
         s.pair_slope = reinterpret_cast<double*>(take((size_t)P * 8));
     }
     if (need & NEED_TEACHER) s.teacher_lse2 = reinterpret_cast<double*>(take((size_t)T * 8));

@@ -289,6 +289,7 @@ pref_seq_kernel(PairArgs a, const float* __restrict__ ref_logp, float* __restric
         w.seq_bad[blockIdx.x] = (int)v[2];
         w.seq_sum[blockIdx.x] = (a.flags & RAPID_PREF_TOKEN_MEAN) && v[1] > 0.0 ? v[0] / v[1] : v[0];
         w.seq_coef[blockIdx.x] = 0.0;  // all bits
+        w.seq_top[blockIdx.x] = 0;
     }
     if (!all || !is_last_block(w.head, &last)) return;
     const double by = pairs_of(a, w);
@@ -296,49 +297,63 @@ pref_seq_kernel(PairArgs a, const float* __restrict__ ref_logp, float* __restric
     for (int i = threadIdx.x >> 5; i < a.n_seq; i += kWarps) coefficient(a, w, i, by);
 }
 
-// Many pairs: every generation's slopes are added up as whole numbers, in which the order of the additions makes no difference, of
-// 2^-41 of the largest slope's power of two (2^20 pairs that all hold one generation come to 2^61 at most).  A warp for each generation
-// that goes through all pairs, as above, would be at 2^20 pairs of 2^20 generations for minutes.
+// Many pairs: every generation's slopes are added up as whole numbers, in which the order of the additions makes no difference, in two
+// words: of 2^-41 of the largest of the generation's own slopes, to a power of two, and what that leaves of 2^-83 of it, so that a sum is as
+// good as one in double whatever the slopes of other generations (2^20 pairs that all hold one generation come to 2^61 in either
+// word at most).  A warp for each generation that goes through all pairs, as above, would be at 2^20 pairs of 2^20 generations for minutes.
 constexpr int kPairThreads = 1024;
-constexpr int kNotFinite = (int)0x80000000;  // in seq_bad, after its sum: the generation is in a pair whose slope is not finite
+constexpr int kWordBits = 41;
+constexpr double kLowWord = 4398046511104.0;  // 2^42 of the low word's are one of the high word's
 __global__ void __launch_bounds__(kPairThreads) pref_pairs_kernel(PairArgs a, Scratch w) {
-    __shared__ unsigned long long top;
-    if (threadIdx.x == 0) top = 0;
     const double by = pairs_of(a, w);
-    __syncthreads();
-    for (int p = threadIdx.x; p < a.n_pairs; p += kPairThreads) {
-        const double x = fabs(w.pair_slope[p]);  // this thread's own
-        if (isfinite(x)) atomicMax(&top, (unsigned long long)__double_as_longlong(x));
+    if (threadIdx.x == 0) w.sums[0] = by;
+}
+// The largest of every generation's slopes, as the bits of a double, which for numbers of one sign are in their order (infinite ones
+// and NaN above all others).  By the block above it would save a launch, and 2^20 pairs would take 3.0 ms instead of 2.0.  The sums of
+// log-ratios have been read by now: their place becomes the low words'.
+__global__ void __launch_bounds__(kThreads) pref_tops_kernel(PairArgs a, Scratch w) {
+    const int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (k < a.n_seq) w.seq_sum[k] = 0.0;  // all bits
+    if (k >= a.n_pairs) return;
+    const int i = a.pairs[2 * k], j = a.pairs[2 * k + 1];
+    const unsigned long long x = (unsigned long long)__double_as_longlong(fabs(w.pair_slope[k]));
+    if (i == j || x == 0) return;  // (a pair that is left out has a slope of 0)
+    if (__ldcg(w.seq_top + i) < x) atomicMax(w.seq_top + i, x);  // (what is read may be old, and is then smaller)
+    if (__ldcg(w.seq_top + j) < x) atomicMax(w.seq_top + j, x);
+}
+__device__ __forceinline__ int top_exponent(unsigned long long top) {  // all slopes are below 2^this; of what is not finite, 1025
+    return max((int)(top >> 52) - 1022, -900);
+}
+__device__ __forceinline__ void add_slope(const Scratch& w, int n, double x) {
+    unsigned long long *high = reinterpret_cast<unsigned long long*>(w.seq_coef) + n, *low = reinterpret_cast<unsigned long long*>(w.seq_sum) + n;
+    const int e = top_exponent(w.seq_top[n]);
+    if (e > 1024) {  // the others make no difference; bits: one is positive, one is negative
+        if (!isfinite(x)) atomicOr(high, isnan(x) ? 3ull : x > 0.0 ? 1ull : 2ull);
+        return;
     }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        int e = 0;
-        frexp(__longlong_as_double((long long)top), &e);
-        e = max(e, -900);
-        w.sums[0] = ldexp(1.0, 41 - e);
-        w.sums[1] = ldexp(by, e - 41);
-    }
+    const double y = ldexp(x, kWordBits - e), whole = rint(y);
+    atomicAdd(high, (unsigned long long)(long long)whole);
+    const long long rest = (long long)rint((y - whole) * kLowWord);
+    if (rest != 0) atomicAdd(low, (unsigned long long)rest);
 }
 __global__ void __launch_bounds__(kThreads) pref_slopes_kernel(PairArgs a, Scratch w) {
     const int p = blockIdx.x * kThreads + threadIdx.x;
     if (p >= a.n_pairs) return;
     const int i = a.pairs[2 * p], j = a.pairs[2 * p + 1];
     const double x = w.pair_slope[p];
-    if (i == j || x == 0.0) return;  // (a pair that is left out has a slope of 0)
-    if (!isfinite(x)) {
-        atomicOr(w.seq_bad + i, kNotFinite);
-        atomicOr(w.seq_bad + j, kNotFinite);
-        return;
-    }
-    const long long n = __double2ll_rn(x * w.sums[0]);
-    unsigned long long* sum = reinterpret_cast<unsigned long long*>(w.seq_coef);
-    atomicAdd(sum + i, (unsigned long long)-n);
-    atomicAdd(sum + j, (unsigned long long)n);
+    if (i == j || x == 0.0) return;
+    add_slope(w, i, -x);
+    add_slope(w, j, x);
 }
 __global__ void __launch_bounds__(kThreads) pref_coef_kernel(PairArgs a, Scratch w) {
     const int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (n >= a.n_seq) return;
-    const double s = w.seq_bad[n] < 0 ? (double)NAN : (double)__double_as_longlong(w.seq_coef[n]) * w.sums[1];
+    const int e = top_exponent(w.seq_top[n]);
+    const long long high = __double_as_longlong(w.seq_coef[n]), low = __double_as_longlong(w.seq_sum[n]);
+    double s;
+    if (e > 1024) s = high == 3 ? (double)NAN : high == 1 ? (double)INFINITY : -(double)INFINITY;
+    else s = ldexp((double)high + (double)low * (1.0 / kLowWord), e - kWordBits);
+    s *= w.sums[0];
     const int rows = w.seq_rows[n];
     w.seq_coef[n] = (a.flags & RAPID_PREF_TOKEN_MEAN) && rows > 0 ? s / (double)rows : s;
 }
@@ -490,8 +505,10 @@ rapid_status_t rapid_preference_loss(const rapid_pref_desc_t* desc, const void* 
     if (!all) {
         pref_pairs_kernel<<<1, kPairThreads, 0, st>>>(pa, w);
         if (dlogits) {
-            pref_slopes_kernel<<<(unsigned)((d.n_pairs + kThreads - 1) / kThreads), kThreads, 0, st>>>(pa, w);
-            pref_coef_kernel<<<(unsigned)(((int64_t)d.n_seq + kThreads - 1) / kThreads), kThreads, 0, st>>>(pa, w);
+            const unsigned by_pair = (unsigned)((d.n_pairs + kThreads - 1) / kThreads), by_seq = (unsigned)(((int64_t)d.n_seq + kThreads - 1) / kThreads);
+            pref_tops_kernel<<<by_pair > by_seq ? by_pair : by_seq, kThreads, 0, st>>>(pa, w);
+            pref_slopes_kernel<<<by_pair, kThreads, 0, st>>>(pa, w);
+            pref_coef_kernel<<<by_seq, kThreads, 0, st>>>(pa, w);
         }
     }
     if (cudaGetLastError() != cudaSuccess) return RAPID_ERR_CUDA;
