@@ -163,7 +163,9 @@ rapid_status_t rapid_distill_loss_workspace_bytes(const rapid_distill_desc_t* de
  *                     that is negative) and q_0 = sum of q_v outside the list:  loss_r += p_0 (log p_0 - log q_0)
  *     loss = w sum_r loss_r over the rows that count,  w = scale / (their number)
  *     dlogits[r, v] = w / tau (q_v - p_j [v == i_j]),  and w / tau q_v (1 - p_0 / q_0) outside the list where top_lse is given
- * (tau^2, the usual factor of a softened loss, goes into `scale`.)
+ * (tau^2, the usual factor of a softened loss, goes into `scale`.)  Where the student has nothing outside the list (q_0 = 0: it holds the
+ * whole vocabulary, or the rest is masked), a p_0 within 2^-21 max(1, |top_lse_r|), what a float leaves of 0, counts as 0; a larger
+ * one is an infinite loss.
  *   top_index  [T, ld_top] int32; a negative index is a place without an entry, whatever its logit
  *   top_logit  [T, ld_top] float; -inf is an entry of probability 0
  *   top_lse    [T] float, log sum over the teacher's whole vocabulary of exp(t / tau)

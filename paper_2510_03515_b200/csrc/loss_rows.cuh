@@ -687,7 +687,12 @@ __device__ __forceinline__ void values(const DistillOp& op, const RowsArgs& a, i
         z[j] = (float)(row.w * (exp2_short(lq) - p));
     }
     loss = lanes_sum<W>(loss);
-    if (row.p0 > 0.0) loss += row.p0 * (row.lp0 - (st.lse2 - row.list_sum));
+    if (row.p0 > 0.0) {
+        // A student with nothing outside the list: infinite, unless the teacher has nothing there either.  Then p_0 is what the rounding of
+        // its log-sum-exp to a float left of 0 (half a step is 2^-24 of it; four steps allow for one that was summed in float).
+        const bool empty = row.p0 <= fmax(1.0, fabs(row.teacher) * kLn2D) * 0x1p-21;
+        if (st.lse2 > -INFINITY || !empty) loss += row.p0 * (row.lp0 - (st.lse2 - row.list_sum));
+    }
     if (lane == 0 && live) a.w.value[r] = loss * kLn2D;
 }
 
