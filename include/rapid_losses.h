@@ -163,6 +163,7 @@ rapid_status_t rapid_distill_loss_workspace_bytes(const rapid_distill_desc_t* de
  *                     that is negative) and q_0 = sum of q_v outside the list:  loss_r += p_0 (log p_0 - log q_0)
  *     loss = w sum_r loss_r over the rows that count,  w = scale / (their number)
  *     dlogits[r, v] = w / tau (q_v - p_j [v == i_j]),  and w / tau q_v (1 - p_0 / q_0) outside the list where top_lse is given
+ *     (where top_lse is below the list's own log-sum-exp and sum_j p_j = m > 1: w / tau (m q_v - p_j [v == i_j]))
  * (tau^2, the usual factor of a softened loss, goes into `scale`.)  Where the student has nothing outside the list (q_0 = 0: it holds the
  * whole vocabulary, or the rest is masked), a p_0 within 2^-21 max(1, |top_lse_r|), what a float leaves of 0, counts as 0; a larger
  * one is an infinite loss.

@@ -609,7 +609,7 @@ __device__ __forceinline__ ClipRow look(const ClipOp&, const ClipHead& in, doubl
 }
 struct DistillRow {
     double teacher, w;
-    double p0, lp0;   // probability of the tokens beside the list, and its logarithm
+    double p0, lp0;   // probability of the tokens beside the list (below 0 where top_lse is too small for the list), and its logarithm
     double list_sum;  // the list's sum of 2^(x - top's x); after finish() the student's log-sum-exp over the whole vocabulary
     float top;        // the list's largest logit
 };
@@ -649,6 +649,8 @@ __device__ __forceinline__ void values(const ClipOp&, const RowsArgs& a, int64_t
     a.w.value[r] = row.lp;
 }
 
+// The teacher's probabilities together: 1, or those of the list where they come to more.  The student's term is as many times q_v.
+__device__ __forceinline__ double teacher_mass(const DistillRow& row) { return row.p0 < 0.0 ? 1.0 - row.p0 : 1.0; }
 // The columns outside the list: w (q_v - p_0 q_v / q_0).  Where the student has less mass there than the teacher, p_0 / q_0 is above one and
 // may be beyond any type (a student that is sure of the list, or whose other columns are masked by a large negative number), while
 // the gradient is not: it is then a factor w p_0 (q_0 / p_0 - 1) of the softmax over these columns alone, which st.lse2 belongs to.
@@ -664,6 +666,7 @@ __device__ __forceinline__ RowGrad finish(const DistillOp& op, const RowsArgs&, 
     const double top = fmax(st.lse2, x0);
     if (top == -INFINITY) return g;
     // (the list's sum holds its largest term, 1, so neither logarithm's argument is small)
+    g.a = row.w * teacher_mass(row);
     lse2 = g.lse2 = top + log2_short(row.list_sum * exp2_short(x0 - top) + exp2_short(st.lse2 - top));
     if (row.p0 > 0.0 && st.lse2 > -INFINITY) {
         const double over = row.lp0 - (st.lse2 - lse2);  // log2 of p_0 / q_0
@@ -684,7 +687,7 @@ __device__ __forceinline__ void values(const DistillOp& op, const RowsArgs& a, i
         const double lt = (double)t[j] * op.kd - row.teacher, lq = (double)z[j] * op.kd - row.list_sum;
         const double p = exp2_short(lt);
         if (p > 0.0) loss += p * (lt - lq);
-        z[j] = (float)(row.w * (exp2_short(lq) - p));
+        z[j] = (float)(row.w * (teacher_mass(row) * exp2_short(lq) - p));
     }
     loss = lanes_sum<W>(loss);
     if (row.p0 > 0.0) {
