@@ -222,7 +222,9 @@ __device__ double pairs_of(const PairArgs& a, const Scratch& w) {
                 slope = 2.0 * (h - 0.5);
             } else {
                 f = (1.0 - a.smoothing) * softplus(-h) + a.smoothing * softplus(h);
-                slope = 1.0 / (1.0 + exp(-h)) - (1.0 - a.smoothing);
+                // e sigmoid(h) - (1 - e) sigmoid(-h), each by itself: with e = 0 a far pair's slope is small, not a difference from one
+                const double t = exp(-fabs(h)), big = 1.0 / (1.0 + t), small = t * big;
+                slope = h >= 0.0 ? a.smoothing * big - (1.0 - a.smoothing) * small : a.smoothing * small - (1.0 - a.smoothing) * big;
             }
             v[0] += f;
             v[1] += h;
