@@ -215,13 +215,13 @@ __device__ double pairs_of(const PairArgs& a, const Scratch& w) {
             h = a.beta * (__ldcg(w.seq_sum + i) - __ldcg(w.seq_sum + j)) - a.margin;
             double f;
             if (a.flags & RAPID_PREF_HINGE) {
-                f = fmax(1.0 - h, 0.0);
-                slope = h < 1.0 ? -1.0 : 0.0;
+                f = h >= 1.0 ? 0.0 : 1.0 - h;  // of NaN, NaN
+                slope = h >= 1.0 ? 0.0 : h < 1.0 ? -1.0 : (double)NAN;
             } else if (a.flags & RAPID_PREF_SQUARED) {
                 f = (h - 0.5) * (h - 0.5);
                 slope = 2.0 * (h - 0.5);
             } else {
-                f = (1.0 - a.smoothing) * softplus(-h) + a.smoothing * softplus(h);
+                f = (1.0 - a.smoothing) * softplus(-h) + (a.smoothing > 0.0 ? a.smoothing * softplus(h) : 0.0);  // (nothing times infinity)
                 // e sigmoid(h) - (1 - e) sigmoid(-h), each by itself: with e = 0 a far pair's slope is small, not a difference from one
                 const double t = exp(-fabs(h)), big = 1.0 / (1.0 + t), small = t * big;
                 slope = h >= 0.0 ? a.smoothing * big - (1.0 - a.smoothing) * small : a.smoothing * small - (1.0 - a.smoothing) * big;
