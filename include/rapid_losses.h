@@ -17,8 +17,10 @@
  *
  * Common arguments:
  *   logits     [T, ld] of desc->dtype, only the first `vocab` entries of a row are used.  Entries may be -inf or the dtype's
- *              lowest finite value (probability and gradient exactly 0) as long as every live row has a finite entry; +inf and
- *              NaN are not accepted (results unspecified, but memory-safe).  Rows that do not count are never read.
+ *              lowest finite value (probability and gradient exactly 0) as long as every live row has a finite entry.  The largest
+ *              other entry of a row (and with a teacher's log-sum-exp the largest outside the list) over the temperature has to lie
+ *              within +-2^27.  Beyond that, and with +inf and NaN, results are unspecified, but memory-safe.  Rows that do not
+ *              count are never read.
  *   targets    [T] int32, the token y_r; a row whose token lies outside [0, vocab) counts as masked and is counted in stats
  *   mask       [T] uint8, non-zero = the row counts; NULL = all ones
  *   dlogits    [T, ld_grad] out, the type of the logits: the gradient of `loss`, rounded once.  Rows that do not count are

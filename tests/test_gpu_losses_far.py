@@ -59,3 +59,24 @@ def test_clip_and_preference(rows, v, dtype, offset):
     pairs = torch.arange(rows // 2 * 2, dtype=torch.int32, device="cuda").view(-1, 2)
     want = lu.preference(z, targets, None, pairs, rows, lp.float(), beta=0.3)
     lu.check(want, rb.preference_loss(z, targets, None, pairs, rows, 1, lp.float(), beta=0.3, stats=stats), rb.read_loss_stats(stats), dtype)
+
+
+@pytest.mark.parametrize("rows,v", SHAPES)
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("offset,tau", [(2.0 ** 27, 1.0), (-(2.0 ** 27), 1.0), (2.0 ** 17, 0.001), (-130048.0, 0.001)])
+def test_at_the_end_of_the_range(rows, v, dtype, offset, tau):
+    """Logits over the temperature of 2^27: rows of equal largest ones, the others a step of the type below, which is far."""
+    step = 2.0 ** (math.floor(math.log2(abs(offset))) - 6)
+    z, _, g = _near(rows, v, dtype, offset - step if offset > 0 else offset + 2 * step, step, seed=v)
+    index = torch.stack([torch.randperm(min(v, 400), generator=g)[:4] for _ in range(rows)]).to(torch.int32).cuda()
+    logit = tau * torch.randn(rows, 4, generator=g).cuda()
+    lse = (torch.logsumexp(logit.double() / tau, 1) + 0.2).float()
+    for top_lse in (None, lse):
+        want = lu.distill(z, index, logit, None, top_lse, tau)
+        got = rb.distill_loss(z, index, logit, None, top_lse, tau)
+        room = want["grad_tol"] + (lu.HALF[dtype] + lu.P) * want["grad"].abs() + 2.0 ** -126
+        ok = want["grad"].isfinite().all(1)  # (where q_0 is 0 in double too, the utility's 0 x infinity)
+        assert bool(((got.dlogits.double() - want["grad"]).abs() <= room)[ok].all()) and bool(got.dlogits.isfinite().all())
+        exact = want["token"]
+        assert bool(((got.token_loss.double() - exact).abs() <= 2 * lu.LSE + 2.0 ** -23 * exact.abs())[exact.isfinite()].all())
+        assert not bool(got.token_loss.isnan().any())
