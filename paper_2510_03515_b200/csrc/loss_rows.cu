@@ -43,6 +43,9 @@ struct Slot {
     float* z;
 };
 constexpr int kSlotEntry = 8;  // bytes of one of them
+// Without a gradient the clipped loss's rows are read by loss_tokens.cu.
+template <class Op>
+constexpr bool kAlwaysGrad = std::is_same<Op, ClipOp>::value;
 // With the teacher's logits behind them, where there is a teacher (12 bytes for all would cost clip at 16384 bf16 one of its seven groups).
 template <class Op>
 constexpr int kSlotEntryT = std::is_same<Op, DistillOp>::value ? 12 : 8;
@@ -99,7 +102,7 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
     return warp_wait_long(bar, parity, abort_flag);
 }
 
-// kWarps consumer warps, kVecs 16-byte vectors of a thread in a chunk, kKeep chunks in registers, kBlocks blocks on an SM
+// kWarps consumer warps, kVecs 16-byte vectors of a thread in a chunk, kKeep chunks in registers (0: without a gradient), kBlocks blocks on an SM
 template <int DT, class Op, int kWarps, int kVecs, int kKeep, int kBlocks>
 __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsArgs a, Op op, RingShape sh) {
     using E = Elem<DT>;
@@ -140,9 +143,9 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
     __syncthreads();
     volatile int* abortp = &bd.abort_flag;
 
-    const bool grad = a.grad != nullptr;
+    constexpr bool grad = kKeep > 0;
     const int nvec = a.vocab / E::kPer, rest = a.vocab - nvec * E::kPer;
-    const int keep = grad ? kKeep : 0;  // chunks that stay in registers
+    constexpr int keep = kKeep;
 
     if (warp == kWarps) {
         // ------------------------------- producer -------------------------------------------
@@ -536,7 +539,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
     }
     if (threadIdx.x == 0) abort_flag = 0;
     volatile int* abortp = &abort_flag;
-    const bool grad = a.grad != nullptr, ex = exclude(op);
+    const bool grad = kAlwaysGrad<Op> || a.grad != nullptr, ex = exclude(op);
     const int nvec = a.vocab / E::kPer, rest = a.vocab - nvec * E::kPer, all = nvec + (rest ? 1 : 0);
     const int n_list = list_size(op), id = group + 1;
     const unsigned int n_rows = (unsigned int)a.n_rows;
@@ -844,7 +847,7 @@ __global__ void __launch_bounds__(512, 1) short_kernel(RowsArgs a, Op op, ShortS
     __syncthreads();
     volatile int* abortp = &abort_flag;
     const double shared = weight;
-    const bool grad = a.grad != nullptr, ex = exclude(op);
+    const bool grad = kAlwaysGrad<Op> || a.grad != nullptr, ex = exclude(op);
     const int nvec = a.vocab / E::kPer, rest = a.vocab - nvec * E::kPer, all = nvec + (rest ? 1 : 0);
     const int n_list = list_size(op);
     const unsigned int n_rows = (unsigned int)a.n_rows, n_sets = (n_rows + kTogether - 1) / kTogether;
@@ -1114,12 +1117,14 @@ cudaError_t launch(const RowsArgs& a, const Op& op, int list, int sm_count, cuda
         if (row_bytes <= 73728) return go_groups(group_kernel<DT, Op, 4>, 4, kBatch<4>);
         if (row_bytes <= 110 * 1024) return go_groups(group_kernel<DT, Op, 8>, 8, kBatch<8>);
         constexpr size_t b16 = sizeof(Board<16>);
-        if (a.grad && row_bytes <= 172 * 1024) return go(ring_kernel<DT, Op, 8, 4, 2, 2>, 8, 4, 2, 2, sizeof(Board<8>), Board<8>::kStages);
+        const bool grad = kAlwaysGrad<Op> || a.grad;
+        if (grad && row_bytes <= 172 * 1024) return go(ring_kernel<DT, Op, 8, 4, 2, 2>, 8, 4, 2, 2, sizeof(Board<8>), Board<8>::kStages);
         // Lists need room beside the stages: chunks of 24 KB leave it, seven of 32 KB do not (16 x 512 rows of 151936 with 128 entries 844 us,
         // with a chunk that has to be loaded again 1174); without lists 32 KB cost a little less (4096 rows: 462, 469).
         constexpr int kV = std::is_same<Op, DistillOp>::value ? 3 : 4, kK = 7 - kV;
-        if (a.grad) return go(ring_kernel<DT, Op, 16, kV, kK, 1>, 16, kV, kK, 1, b16, Board<16>::kStages);
-        return go(ring_kernel<DT, Op, 16, 4, 0, 1>, 16, 4, 0, 1, b16, Board<16>::kStages);
+        if (grad) return go(ring_kernel<DT, Op, 16, kV, kK, 1>, 16, kV, kK, 1, b16, Board<16>::kStages);
+        if constexpr (!kAlwaysGrad<Op>) return go(ring_kernel<DT, Op, 16, 4, 0, 1>, 16, 4, 0, 1, b16, Board<16>::kStages);
+        return cudaErrorInvalidValue;
     };
     return a.dtype == RAPID_BF16 ? by_type(std::integral_constant<int, RAPID_BF16>{}) : by_type(std::integral_constant<int, RAPID_F32>{});
 }
