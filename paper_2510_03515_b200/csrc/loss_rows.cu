@@ -27,6 +27,46 @@ namespace losses {
 
 namespace {
 
+// Vector `at` of a row, from place `p`; columns behind the last one read as -inf.
+template <int DT>
+__device__ __forceinline__ uint4 edge_vector(const uint4* p, int at, int nvec, int rest) {
+    using E = Elem<DT>;
+    constexpr uint32_t kNone = DT == RAPID_BF16 ? 0xff80ff80u : 0xff800000u;
+    uint4 v = make_uint4(kNone, kNone, kNone, kNone);
+    if (at < nvec) v = *p;
+    else if (at == nvec && rest) {
+        const typename E::T* e = reinterpret_cast<const typename E::T*>(p);
+        uint32_t w[4] = {kNone, kNone, kNone, kNone};
+#pragma unroll
+        for (int i = 0; i < E::kPer; ++i) {
+            if (i >= rest) continue;
+            if constexpr (DT == RAPID_BF16) {
+                const uint32_t b = e[i];
+                w[i / 2] = (i & 1) ? ((w[i / 2] & 0xffffu) | (b << 16)) : ((w[i / 2] & 0xffff0000u) | b);
+            } else {
+                w[i] = __float_as_uint(e[i]);
+            }
+        }
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return v;
+}
+// And its gradient, without the columns behind the last one.
+template <int DT>
+__device__ __forceinline__ void write_edge_vector(typename Elem<DT>::T* out, int at, const uint4& y, int nvec, int rest) {
+    using E = Elem<DT>;
+    if (at < nvec) st_stream(reinterpret_cast<uint4*>(out) + at, y);
+    else if (at == nvec && rest) {
+        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int i = 0; i < E::kPer; ++i) {
+            if (i >= rest) continue;
+            if constexpr (DT == RAPID_BF16) out[nvec * E::kPer + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+            else out[nvec * E::kPer + i] = __uint_as_float(w[i]);
+        }
+    }
+}
+
 // ---- the longest rows ------------------------------------------------------------------------------------------
 
 struct RingShape {
@@ -317,28 +357,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
 #pragma unroll
             for (int j = 0; j < kVecs; ++j) v[j] = sv[j * kLanes];
         };
-        // vector `at` of the row from place `sv`; columns behind the last read as -inf
-        auto read_edge = [&](const uint4* sv, int at) {
-            constexpr uint32_t kNone = DT == RAPID_BF16 ? 0xff80ff80u : 0xff800000u;
-            uint4 v = make_uint4(kNone, kNone, kNone, kNone);
-            if (at < nvec) v = *sv;
-            else if (at == nvec && rest) {
-                const T* e = reinterpret_cast<const T*>(sv);
-                uint32_t w[4] = {kNone, kNone, kNone, kNone};
-#pragma unroll
-                for (int i = 0; i < E::kPer; ++i) {
-                    if (i >= rest) continue;
-                    if constexpr (DT == RAPID_BF16) {
-                        const uint32_t b = e[i];
-                        w[i / 2] = (i & 1) ? ((w[i / 2] & 0xffffu) | (b << 16)) : ((w[i / 2] & 0xffff0000u) | b);
-                    } else {
-                        w[i] = __float_as_uint(e[i]);
-                    }
-                }
-                v = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-            return v;
-        };
+        auto read_edge = [&](const uint4* sv, int at) { return edge_vector<DT>(sv, at, nvec, rest); };
         for (uint32_t jq = 0;; ++jq) {
             if (!warp_wait(&bd.row[jq % kQueue], (jq / kQueue) & 1u, abortp)) break;
             const int64_t r = bd.row_q[jq % kQueue];
@@ -427,17 +446,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
                 for (int j = 0; j < kVecs; ++j) {
                     const int at = whole * kChunkVecs + j * kLanes + tid;
                     if (at - lane > nvec) break;
-                    const uint4 y = row_grad().vector(read_edge(my_ring + s * kChunkVecs + j * kLanes, at));
-                    if (at < nvec) st_stream(reinterpret_cast<uint4*>(out) + at, y);
-                    else if (at == nvec && rest) {
-                        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                        for (int i = 0; i < E::kPer; ++i) {
-                            if (i >= rest) continue;
-                            if constexpr (DT == RAPID_BF16) out[nvec * E::kPer + i] = (T)(w[i / 2] >> (16 * (i & 1)));
-                            else out[nvec * E::kPer + i] = __uint_as_float(w[i]);
-                        }
-                    }
+                    write_edge_vector<DT>(out, at, row_grad().vector(read_edge(my_ring + s * kChunkVecs + j * kLanes, at)), nvec, rest);
                 }
                 give_back(s);
             };
@@ -635,28 +644,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
             }
         const auto in = head(op, row);
         if (!grad) announce();
-        // vector `at` of the row; columns behind the last read as -inf
-        auto read = [&](int at) {
-            constexpr uint32_t kNone = DT == RAPID_BF16 ? 0xff80ff80u : 0xff800000u;
-            uint4 v = make_uint4(kNone, kNone, kNone, kNone);
-            if (at < nvec) v = row_place[at];
-            else if (at == nvec && rest) {
-                const T* e = reinterpret_cast<const T*>(row_place + at);
-                uint32_t w[4] = {kNone, kNone, kNone, kNone};
-#pragma unroll
-                for (int i = 0; i < E::kPer; ++i) {
-                    if (i >= rest) continue;
-                    if constexpr (DT == RAPID_BF16) {
-                        const uint32_t b = e[i];
-                        w[i / 2] = (i & 1) ? ((w[i / 2] & 0xffffu) | (b << 16)) : ((w[i / 2] & 0xffff0000u) | b);
-                    } else {
-                        w[i] = __float_as_uint(e[i]);
-                    }
-                }
-                v = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-            return v;
-        };
+        auto read = [&](int at) { return edge_vector<DT>(row_place + at, at, nvec, rest); };
         long long next = 0;
         // this warp has read part p for the last time; the last one to say so has the next row's loaded there
         auto hand_over = [&](int p) {
@@ -752,19 +740,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
                     for (int j = 0; j < U; ++j) st_stream(ov + v + j * kLanes, gr.vector(w[j]));
                 }
 #pragma unroll 1
-                for (; v - lane < end; v += kLanes) {
-                    const uint4 y = gr.vector(read(v));
-                    if (v < nvec) st_stream(ov + v, y);
-                    else if (v == nvec && rest) {
-                        const uint32_t x[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                        for (int i = 0; i < E::kPer; ++i) {
-                            if (i >= rest) continue;
-                            if constexpr (DT == RAPID_BF16) out[nvec * E::kPer + i] = (T)(x[i / 2] >> (16 * (i & 1)));
-                            else out[nvec * E::kPer + i] = __uint_as_float(x[i]);
-                        }
-                    }
-                }
+                for (; v - lane < end; v += kLanes) write_edge_vector<DT>(out, v, gr.vector(read(v)), nvec, rest);
                 hand_over(q);
             }
         }
@@ -910,28 +886,7 @@ __global__ void __launch_bounds__(512, 1) short_kernel(RowsArgs a, Op op, ShortS
                     if (lane < rest) out[nvec * E::kPer + lane] = E::put(0.f);
                 }
         __syncwarp();
-        // vector `at` of the row at `p`; columns behind the last read as -inf
-        auto read = [&](const uint4* p, int at) {
-            constexpr uint32_t kNone = DT == RAPID_BF16 ? 0xff80ff80u : 0xff800000u;
-            uint4 v = make_uint4(kNone, kNone, kNone, kNone);
-            if (at < nvec) v = p[at];
-            else if (at == nvec && rest) {
-                const T* e = reinterpret_cast<const T*>(p + at);
-                uint32_t w[4] = {kNone, kNone, kNone, kNone};
-#pragma unroll
-                for (int i = 0; i < E::kPer; ++i) {
-                    if (i >= rest) continue;
-                    if constexpr (DT == RAPID_BF16) {
-                        const uint32_t b = e[i];
-                        w[i / 2] = (i & 1) ? ((w[i / 2] & 0xffffu) | (b << 16)) : ((w[i / 2] & 0xffff0000u) | b);
-                    } else {
-                        w[i] = __float_as_uint(e[i]);
-                    }
-                }
-                v = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-            return v;
-        };
+        auto read = [&](const uint4* p, int at) { return edge_vector<DT>(p + at, at, nvec, rest); };
         auto hand_over = [&](int k) {  // place k has been read for the last time
             __syncwarp();
             if (lane == 0 && (live_next >> k & 1u)) load_row(next * kTogether + k, k);
@@ -1013,19 +968,7 @@ __global__ void __launch_bounds__(512, 1) short_kernel(RowsArgs a, Op op, ShortS
                     for (int j = 0; j < U; ++j) st_stream(ov + v + j * 32, gr.vector(q[j]));
                 }
 #pragma unroll 1
-                for (; v - lane < all; v += 32) {
-                    const uint4 y = gr.vector(read(p, v));
-                    if (v < nvec) st_stream(ov + v, y);
-                    else if (v == nvec && rest) {
-                        const uint32_t x[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                        for (int i = 0; i < E::kPer; ++i) {
-                            if (i >= rest) continue;
-                            if constexpr (DT == RAPID_BF16) out[nvec * E::kPer + i] = (T)(x[i / 2] >> (16 * (i & 1)));
-                            else out[nvec * E::kPer + i] = __uint_as_float(x[i]);
-                        }
-                    }
-                }
+                for (; v - lane < all; v += 32) write_edge_vector<DT>(out, v, gr.vector(read(p, v)), nvec, rest);
                 hand_over(k);
 #pragma unroll 1
                 for (int j = lane; j < n_list; j += 32) {  // the chosen columns over the vectors
