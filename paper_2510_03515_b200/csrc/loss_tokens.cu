@@ -63,7 +63,7 @@ constexpr int kGradThreads = 256;
 constexpr int kPiece = 16 * 32;
 
 template <int DT>
-__global__ void __launch_bounds__(kGradThreads)
+__global__ void __launch_bounds__(kGradThreads, 4)  // (of bf16 three else: 8192 x 32000 280 us instead of 277)
 token_grads_kernel(RowsArgs a, const int32_t* __restrict__ targets, const double* __restrict__ coef, Divisor seq_len, uint32_t pieces, uint32_t total) {
     using E = Elem<DT>;
     using T = typename E::T;
