@@ -128,6 +128,7 @@ rapid_status_t rapid_preference_loss_workspace_bytes(const rapid_pref_desc_t* de
  *     h_p = beta (s_c - s_j) - margin for pair p = (c, j), c preferred to j
  *     loss = scale / P sum_p f(h_p),  f(h) = -(1 - e) log sigmoid(h) - e log sigmoid(-h), e = label_smoothing (or see the flags)
  *     dlogits[r, v] = g_n (softmax(z[r, .])_v - 1[v == y_r]),   g_n = - d loss / d s_n  (/ len_n with RAPID_PREF_TOKEN_MEAN)
+ * (The squared form is that of the margin h itself; published forms that take (s_c - s_j - 1 / (2 beta))^2 are 1 / beta^2 of it.)
  * A generation may be in any number of pairs.  A pair with an index outside [0, N) is left out (P is then the number of the
  * others); a generation without rows that count has s_n = 0.
  *   pairs      [P][2] int32: preferred, other

@@ -13,9 +13,9 @@
 //
 // Every wait on a barrier is bounded; a wait that gives up raises RAPID_ERR_TIMEOUT in the scratch and never traps.
 //
-// What bounds it: the bytes, at full length (8 x 1024 ragged rows of 151936 bf16: 640 us, 0.95 of a copy's rate; with lists of 64 and a
-// bucket 682, 0.90).  Where all rows count, the two sweeps do: an element costs two exponentials and some ten instructions (4096 rows
-// of 151936: 453 us, 0.85).
+// What bounds it: the bytes, at full length (8 x 1024 ragged rows of 151936 bf16: 633 us back to back, 0.99 of a copy's rate; with lists of
+// 64 and a bucket 670, 0.93).  Where all rows count, the two sweeps do: an element costs two exponentials and some ten instructions
+// (4096 rows of 151936: 449 us, 0.86).
 #include <algorithm>
 #include <type_traits>
 
@@ -493,7 +493,7 @@ __global__ void __launch_bounds__((kWarps + 4) * 32, kBlocks) ring_kernel(RowsAr
 // side by side on an SM and hide one another's latencies.  A row comes in kParts bulk copies; the last warp to have read a part for the
 // last time has the next row's part loaded in its place, so the warps meet only twice a row: to join their sums, and for the
 // factor.  Rows are drawn from a counter, two ahead.  An element's instructions, and the two meetings, bound it: 32768 rows of 8192
-// bf16 take 230 us (0.72 of a copy's rate), 16384 of 16384 216 (0.77), 8192 of 32000 224 (0.72), 8192 of 50000 308 (0.82).
+// bf16 take 229 us (0.73 of a copy's rate), 16384 of 16384 209 (0.79), 8192 of 32000 221 (0.73), 8192 of 50000 306 (0.83).
 
 constexpr int kParts = 2;
 
@@ -776,7 +776,7 @@ __global__ void __launch_bounds__(512, 1) group_kernel(RowsArgs a, Op op, GroupS
 // Up to 8 KB a warp holds two rows at a time: it reads them one after the other, then does what is done once a row for both of them
 // at once, half a warp each, and writes them one after the other.  That arithmetic, one value a row in double, is a chain of some
 // thousands of cycles in which a warp that holds one row does nothing else: when 65536 rows of 4096 bf16 with 8 entries took 240 us so,
-// they took 300 with one row a warp, and 297 with four, which leave six warps an SM.  Now 208; floor 146.
+// they took 300 with one row a warp, and 297 with four, which leave six warps an SM.  Now 211; floor 146.
 constexpr int kTogether = 2;
 
 struct ShortShape {
