@@ -157,8 +157,9 @@ inline rapid_status_t check_device(int* sm_count) {
 
 // ---- a row's statistics -----------------------------------------------------------------------------------------
 
-// log2(e) / tau, as a sum of two floats: k1 has 16 significant bits, so that its product with a bf16 logit (8 bits) is exact, and
-// k2 > 0 carries the next 24 (k2 is never 0, or -inf * k2 would be NaN).  k is the nearest float.
+// log2(e) / tau, as a sum of two floats: k1, cut after 24 bits, and k2 > 0 with the next 24 (k2 is never 0, or -inf * k2 would be NaN).
+// z k1 - sh is rounded once, at the size of z k2 or of the difference, so that at |z| k of 2^28 it is still off by less than 2^-18.
+// k is the nearest float.
 struct Factor {
     double kd;
     float k1, k2, k;
@@ -168,7 +169,7 @@ inline Factor make_factor(double tau) {
     f.kd = kLog2eD / tau;
     int e = 0;
     const double m = frexp(f.kd, &e);  // in [1/2, 1)
-    f.k1 = (float)ldexp(floor(ldexp(m, 16)), e - 16);
+    f.k1 = (float)ldexp(floor(ldexp(m, 24)), e - 24);
     f.k2 = (float)(f.kd - (double)f.k1);
     if (!(f.k2 > 0.f)) f.k2 = 1e-30f;
     f.k = (float)f.kd;

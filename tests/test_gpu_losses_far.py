@@ -80,3 +80,30 @@ def test_at_the_end_of_the_range(rows, v, dtype, offset, tau):
         exact = want["token"]
         assert bool(((got.token_loss.double() - exact).abs() <= 2 * lu.LSE + 2.0 ** -23 * exact.abs())[exact.isfinite()].all())
         assert not bool(got.token_loss.isnan().any())
+
+
+@pytest.mark.parametrize("rows,v", SHAPES)
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("offset,tau", [(12345.6789, 0.001), (123456.789, 0.001), (-98765.4321, 0.001), (7654321.0, 0.07), (1.1e8, 0.9)])
+def test_the_log_sum_exp_of_far_rows(rows, v, dtype, offset, tau):
+    """Numbers without many zeros: neighbours of the offset in the type, of which the largest hold the row's sum."""
+    g = torch.Generator().manual_seed(v)
+    top = torch.tensor(offset).to(dtype)
+    down = top
+    for _ in range(1 if dtype == BF else 2):
+        down = torch.nextafter(down, torch.tensor(-math.inf, dtype=dtype))
+    z = torch.full((rows, -(-v // 8) * 8), math.nan, dtype=dtype)
+    z[:, :v] = torch.where(torch.rand(rows, v, generator=g) < 0.3, top, down)
+    z[:, 0] = top
+    z = z.cuda()[:, :v]
+    index = torch.stack([torch.randperm(v, generator=g)[:3] for _ in range(rows)]).to(torch.int32).cuda()
+    logit = tau * torch.randn(rows, 3, generator=g).cuda()
+    stats = rb.alloc_stats()
+    want = lu.distill(z, index, logit, None, None, tau)
+    got = rb.distill_loss(z, index, logit, None, None, tau, stats=stats)
+    lu.check(want, got, rb.read_loss_stats(stats), dtype)
+    targets = index[:, 0].contiguous()
+    lp = lu._token_logp(z, targets, torch.ones(rows, dtype=torch.bool, device="cuda"))[0]
+    if tau == 0.9:  # and without a temperature
+        got = rb.clip_loss(z, targets, None, lp.float() + 0.1, torch.ones(rows, device="cuda"), rows, 1, stats=stats)
+        lu.check(lu.clip(z, targets, None, lp.float() + 0.1, torch.ones(rows, device="cuda"), rows), got, rb.read_loss_stats(stats), dtype)
