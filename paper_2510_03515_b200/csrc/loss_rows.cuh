@@ -74,6 +74,13 @@ inline int stat_pieces(int32_t vocab, int32_t dtype) {
     return n < 1 ? 1 : n > 4 ? 4 : (int)n;
 }
 
+// Vectors of a piece of a row whose gradient is written by token_grads_kernel, and such pieces of a row.
+constexpr int kPieceVecs = 16 * 32;
+inline int64_t grad_pieces(int32_t vocab, int32_t dtype) {
+    const int64_t n = (vocab / (16 / (int64_t)elem_size(dtype)) + kPieceVecs - 1) / kPieceVecs;
+    return n < 1 ? 1 : n;
+}
+
 // Carve `base` (256-byte aligned); returns the bytes used.
 inline size_t carve(int64_t T, int64_t N, int64_t P, int pieces, int need, void* base, Scratch* out) {
     size_t off = 0;

@@ -1,7 +1,5 @@
 // The losses of rapid_losses.h where a row's gradient waits for other rows, or is not wanted: one kernel reads the logits for the
 // tokens' log-probabilities, another reads them again and writes the gradient.  Both are one pass at the rate of the memory.
-#include <algorithm>
-
 #include "loss_rows.cuh"
 
 namespace rapid {
@@ -60,7 +58,6 @@ token_stats_kernel(RowsArgs a, const int32_t* __restrict__ targets, const uint8_
 // ---- gradients ----------------------------------------------------------------------------------------------------
 // A warp for each piece of a row, 16 vectors of a lane; it forms the row's constants itself.  Nothing waits for anything.
 constexpr int kGradThreads = 256;
-constexpr int kPiece = 16 * 32;
 
 template <int DT>
 __global__ void __launch_bounds__(kGradThreads, 4)  // (of bf16 three else: 8192 x 32000 280 us instead of 277)
@@ -73,9 +70,9 @@ token_grads_kernel(RowsArgs a, const int32_t* __restrict__ targets, const double
     piece = total - 1 - piece;  // from the end: what the first reading read last may still be in L2
     const int lane = threadIdx.x & 31;
     const uint32_t r = piece / pieces;
-    const int first = (int)(piece - r * pieces) * kPiece;  // first vector
-    const int nvec = a.vocab / E::kPer, end = min(first + kPiece, nvec);
-    const bool last = first + kPiece >= nvec;
+    const int first = (int)(piece - r * pieces) * kPieceVecs;  // first vector
+    const int nvec = a.vocab / E::kPer, end = min(first + kPieceVecs, nvec);
+    const bool last = first + kPieceVecs >= nvec;
     T* out = static_cast<T*>(a.grad) + (int64_t)r * a.ld_grad;
     uint4* ov = reinterpret_cast<uint4*>(out);
     const double g = a.w.state[r] == ROW_OK ? coef[divide(r, seq_len)] : 0.0;
@@ -117,8 +114,7 @@ token_grads_kernel(RowsArgs a, const int32_t* __restrict__ targets, const double
 }  // namespace
 
 cudaError_t launch_token_stats(const RowsArgs& a, const int32_t* targets, const uint8_t* mask, bool keep, cudaStream_t stream) {
-    const int64_t pieces = stat_pieces(a.vocab, a.dtype), total = pieces * a.n_rows;
-    if (total > 0x7fffffffll) return cudaErrorInvalidValue;  // 34 TB of logits
+    const int64_t pieces = stat_pieces(a.vocab, a.dtype), total = pieces * a.n_rows;  // 31 bits: checked
     const unsigned grid = (unsigned)((total + kStatThreads / 32 - 1) / (kStatThreads / 32));
     auto go = [&](auto kern) {
         kern<<<grid, kStatThreads, 0, stream>>>(a, targets, mask, (uint32_t)pieces, (uint32_t)total);
@@ -129,9 +125,7 @@ cudaError_t launch_token_stats(const RowsArgs& a, const int32_t* targets, const 
 }
 
 cudaError_t launch_token_grads(const RowsArgs& a, const int32_t* targets, const double* coef, const Divisor& seq_len, cudaStream_t stream) {
-    const int64_t nvec = a.vocab / (16 / (int64_t)elem_size(a.dtype));
-    const int64_t pieces = std::max<int64_t>(1, (nvec + kPiece - 1) / kPiece), total = pieces * a.n_rows;
-    if (total > 0x7fffffffll) return cudaErrorInvalidValue;  // 17 TB of gradient
+    const int64_t pieces = grad_pieces(a.vocab, a.dtype), total = pieces * a.n_rows;  // 31 bits: checked
     const unsigned grid = (unsigned)((total + kGradThreads / 32 - 1) / (kGradThreads / 32));
     auto go = [&](auto kern) {
         kern<<<grid, kGradThreads, 0, stream>>>(a, targets, coef, seq_len, (uint32_t)pieces, (uint32_t)total);

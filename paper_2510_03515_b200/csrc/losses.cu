@@ -1,6 +1,8 @@
 // The losses of rapid_losses.h around their rows: states and numbers of the rows before them, sums over rows, pairs and
 // generations after them, and the C calls.  All of it is double and touches a few values a row, so a call's time beside the rows
 // is that of the launches.
+#include <algorithm>
+
 #include "loss_rows.cuh"
 
 namespace rapid {
@@ -398,8 +400,10 @@ inline bool arrays_aligned(const void* a, const void* b, const void* c, const vo
 rapid_status_t check_clip(const rapid_clip_desc_t* d) {
     if (!d || d->n_seq <= 0 || d->seq_len <= 0 || d->reserved != 0) return RAPID_ERR_INVALID_ARG;
     if (!(d->eps_low >= 0.0) || !(d->eps_high >= 0.0) || !(d->kl_beta >= 0.0) || !isfinite(d->kl_beta)) return RAPID_ERR_INVALID_ARG;
-    return check_shape((int64_t)d->n_seq * d->seq_len, d->vocab, d->dtype, d->ld, d->ld_grad, d->flags,
-                       RAPID_LOSS_NORM_SEQ | RAPID_LOSS_NORM_GIVEN | RAPID_CLIP_ADV_TOKEN, d->scale, d->norm_z);
+    const rapid_status_t s = check_shape((int64_t)d->n_seq * d->seq_len, d->vocab, d->dtype, d->ld, d->ld_grad, d->flags,
+                                         RAPID_LOSS_NORM_SEQ | RAPID_LOSS_NORM_GIVEN | RAPID_CLIP_ADV_TOKEN, d->scale, d->norm_z);
+    // the numbers of the rows' pieces stay within 31 bits: 34 TB of logits
+    return s == RAPID_OK && (int64_t)d->n_seq * d->seq_len * stat_pieces(d->vocab, d->dtype) > 0x7fffffffll ? RAPID_ERR_UNSUPPORTED : s;
 }
 size_t carve_clip(const rapid_clip_desc_t& d, void* base, Scratch* w) {
     return carve((int64_t)d.n_seq * d.seq_len, d.n_seq, 0, stat_pieces(d.vocab, d.dtype), (d.flags & RAPID_LOSS_NORM_SEQ) ? NEED_SEQ : 0, base, w);
@@ -415,7 +419,8 @@ rapid_status_t check_pref(const rapid_pref_desc_t* d) {
                                          RAPID_LOSS_NORM_GIVEN | RAPID_PREF_HINGE | RAPID_PREF_SQUARED | RAPID_PREF_TOKEN_MEAN, d->scale,
                                          d->norm_z);
     if (s != RAPID_OK) return s;
-    return d->n_pairs > (1 << 20) ? RAPID_ERR_UNSUPPORTED : RAPID_OK;
+    const int64_t pieces = std::max<int64_t>(stat_pieces(d->vocab, d->dtype), grad_pieces(d->vocab, d->dtype));
+    return d->n_pairs > (1 << 20) || (int64_t)d->n_seq * d->seq_len * pieces > 0x7fffffffll ? RAPID_ERR_UNSUPPORTED : RAPID_OK;  // 17 TB
 }
 size_t carve_pref(const rapid_pref_desc_t& d, void* base, Scratch* w) {
     return carve((int64_t)d.n_seq * d.seq_len, d.n_seq, d.n_pairs, stat_pieces(d.vocab, d.dtype), NEED_SEQ | NEED_PAIRS, base, w);

@@ -23,3 +23,19 @@ def test_rows_whose_numbers_would_pass_31_bits_within_a_block(kind):
         assert _call(kind, d, dlogits=None, logits=1 << 48) == rb.RAPID_ERR_UNSUPPORTED
         with pytest.raises(rb.RapidError):
             getattr(rb, f"rapid_{kind}_loss_workspace_bytes")(d)
+
+
+@pytest.mark.parametrize("kind", ["clip", "preference"])
+def test_more_pieces_of_rows_than_31_bits_number(kind):
+    """Refused before anything is enqueued, not by the second of a call's launches."""
+    d = _desc(kind, n=1 << 10, length=1 << 20, v=1 << 20)
+    assert _call(kind, d, dlogits=None, logits=1 << 58) == rb.RAPID_ERR_UNSUPPORTED
+
+
+@no_gpu
+@pytest.mark.parametrize("kind", ["clip", "preference"])
+def test_as_many_pieces_as_31_bits_number(kind):
+    v = {"clip": 1 << 20, "preference": 4096 * 512}[kind]  # four pieces of a row's reading, 512 of its gradient
+    n = {"clip": (1 << 29) - 1, "preference": (1 << 22) - 1}[kind]
+    d = _desc(kind, n=n, length=1, v=v)
+    assert _call(kind, d, dlogits=None, logits=1 << 58, ws_bytes=1 << 60) == rb.RAPID_ERR_CUDA
