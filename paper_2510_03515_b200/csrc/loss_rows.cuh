@@ -164,21 +164,25 @@ inline rapid_status_t check_device(int* sm_count) {
 
 // ---- a row's statistics -----------------------------------------------------------------------------------------
 
-// log2(e) / tau, as a sum of two floats: k1, cut after 24 bits, and k2 > 0 with the next 24 (k2 is never 0, or -inf * k2 would be NaN).
-// z k1 - sh is rounded once, at the size of z k2 or of the difference, so that at |z| k of 2^28 it is still off by less than 2^-18.
-// k is the nearest float.
+// log2(e) / tau, as a sum of two floats: k1, cut after some bits, and k2 > 0 with the next 24 (k2 is never 0, or -inf * k2 would be NaN).
+// bf16: 16 bits, so that the product with a logit (8 bits) and its difference from the shift are exact, and the argument is rounded once.
+// float: 24, as it is rounded twice anyhow; the first time at the size of z k2, which for logits far from 0 has to be small (with 16
+// a log-sum-exp is off by 1e-4 at |z| / tau of 2^27).  `rest` is ln(2) times what the two leave of kd: it is the same for all terms of a size,
+// so their sum is put right.  k is the nearest float.
 struct Factor {
-    double kd;
+    double kd, rest;
     float k1, k2, k;
 };
-inline Factor make_factor(double tau) {
+inline Factor make_factor(double tau, int32_t dtype) {
+    const int bits = dtype == RAPID_BF16 ? 16 : 24;
     Factor f;
     f.kd = kLog2eD / tau;
     int e = 0;
     const double m = frexp(f.kd, &e);  // in [1/2, 1)
-    f.k1 = (float)ldexp(floor(ldexp(m, 24)), e - 24);
+    f.k1 = (float)ldexp(floor(ldexp(m, bits)), e - bits);
     f.k2 = (float)(f.kd - (double)f.k1);
     if (!(f.k2 > 0.f)) f.k2 = 1e-30f;
+    f.rest = (f.kd - ((double)f.k1 + (double)f.k2)) * kLn2D;
     f.k = (float)f.kd;
     return f;
 }
@@ -370,7 +374,7 @@ __device__ __forceinline__ WarpPart warp_part(const Part& p, const Factor& f) {
     w.sh = warp_top(p.s > 0.f ? p.sh : -INFINITY);
     double s = 0.0;
     if (p.s > 0.f) {
-        s = ((double)p.s + (double)p.c - (double)p.term(p.m, f)) * (1.0 / (1.0 + (double)kEx2Mean)) + exp2_short((double)p.m * f.kd - (double)p.sh);
+        s = ((double)p.s + (double)p.c - (double)p.term(p.m, f)) * fma((double)p.m, f.rest, 1.0 / (1.0 + (double)kEx2Mean)) + exp2_short((double)p.m * f.kd - (double)p.sh);
         s *= (double)ex2_approx(p.sh - w.sh);  // an exact power of two
     }
     w.s = warp_sum(s);

@@ -467,7 +467,7 @@ rapid_status_t rapid_clip_loss(const rapid_clip_desc_t* desc, const void* logits
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool by_seq = (d.flags & RAPID_LOSS_NORM_SEQ) != 0;
     const Totals end{token_logp, loss, stats, dlogits && T <= kFewRows, dlogits ? 0 : stat_pieces(d.vocab, d.dtype)};
-    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, make_factor(1.0), w, end};
+    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, make_factor(1.0, d.dtype), w, end};
     int blocks = 0;
     if (dlogits) {
         if (launch_prepare_tokens(d.n_seq, d.seq_len, d.vocab, targets, mask, w, by_seq, &blocks, st) != cudaSuccess) return RAPID_ERR_CUDA;
@@ -504,7 +504,7 @@ rapid_status_t rapid_preference_loss(const rapid_pref_desc_t* desc, const void* 
     int sms = 0;
     if ((s = check_device(&sms)) != RAPID_OK) return s;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, make_factor(1.0), w, Totals{}};
+    const RowsArgs a{logits, dlogits, d.ld, d.ld_grad, T, d.vocab, d.dtype, make_factor(1.0, d.dtype), w, Totals{}};
     if (launch_token_stats(a, targets, mask, dlogits != nullptr, st) != cudaSuccess) return RAPID_ERR_CUDA;
     const PairArgs pa{pairs, d.n_pairs, d.n_seq, d.seq_len, d.flags, d.beta, d.margin, d.label_smoothing, d.scale, d.norm_z, margins, loss, stats};
     const int all = d.n_pairs <= 4096 && (int64_t)d.n_pairs * d.n_seq <= 1 << 16;  // some ten microseconds of one block at most
@@ -544,7 +544,7 @@ rapid_status_t rapid_distill_loss(const rapid_distill_desc_t* desc, const void* 
     int sms = 0;
     if ((s = check_device(&sms)) != RAPID_OK) return s;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const Factor f = make_factor(d.temperature);
+    const Factor f = make_factor(d.temperature, d.dtype);
     int blocks = 0;
     if (launch_prepare_lists(d, f.kd, top_index, top_logit, top_lse, mask, w, &blocks, st) != cudaSuccess) return RAPID_ERR_CUDA;
     const DistillOp op{top_index, top_logit, w.teacher_lse2, w.counts, d.ld_top, d.k, top_lse != nullptr, blocks, d.flags, 1.0 / d.temperature,
